@@ -60,7 +60,8 @@ enum {
   LLC_FLAG_SHARED_RACE = 8,/* llc_compress_select only: the baseline scheme of Section 5.3, in
                               which all decoders share one set of random numbers: the encoder's
                               pool and every decoder use the race times of the first set    */
-  LLC_FLAG_DRY_RUN = 4,    /* llc_couple, llc_couple_is, llc_compress_select, llc_verify: check
+  LLC_FLAG_DRY_RUN = 4,    /* llc_couple, llc_couple_is, llc_compress_select, llc_verify and the calls
+                              at the vocabulary's two ends (llc_token_logprobs and below): check
                               the arguments, plan every launch of the call and check the
                               workspace against the plan, then return without launching
                               anything (no pointer is dereferenced)                    */
@@ -372,6 +373,165 @@ typedef struct llc_lml_args {
   void *stream;
   void *ev_begin, *ev_end;  /* optional hipEvent_t pair recorded around the kernel        */
 } llc_lml_args;
+
+/* ---- The vocabulary's two ends around the sampler: scores of drawn tokens, their gradient, the
+ * embedding of tokens, its gradient, and clipping.  No randomness. */
+
+/* Arguments of llc_token_logprobs: what a row's distribution gives to tokens.
+ *
+ * Inputs.  x[r*stride_r + i] denotes p = softmax(x / temp) (LLC_LOGITS) or the normalised exp(x)
+ * (LLC_LOGW; temp ignored; LLC_PROBS is refused), with NaN, +inf and -inf entries carrying no mass.
+ * tokens[r*tok_stride_r + g], g = 0..G-1, are ids in [0, V); a negative one is an empty slot.
+ *
+ * Outputs.  logp[r,g] = ln p of the token: 0 for an empty slot, -inf for an id of V or more, an entry
+ * without mass and a row without mass.  entropy[r] = -sum_i p_i ln p_i (0 without mass).  lse[r] holds
+ * ln sum_i exp(x_i / temp) in two parts, fp64: the largest x (0 without mass) and ln sum_i exp((x_i - it) / temp)
+ * (-inf without mass); it / temp plus the second would lose the second where a row's values are large.  top_ids / top_logp[r,m] = the M entries with
+ * the largest x, larger first, equal ones by index, and their ln p; -1 and -inf where fewer entries
+ * have mass.  These are lists as llc_couple_topm takes them (kind LLC_LOGW).
+ * Sums are taken in fp32 within a thread and joined in fp64. */
+#define LLC_TOP_MAX 128
+typedef struct llc_token_logprobs_args {
+  int64_t R, V, G, M;       /* R >= 0, V in 1..2^31 - 5, G in 0..65535, M in 0..LLC_TOP_MAX */
+  int32_t dtype;            /* LLC_F32 | LLC_BF16                                        */
+  int32_t kind;             /* LLC_LOGITS | LLC_LOGW                                     */
+  const void *x;            /* device [R,V] */
+  int64_t stride_r;         /* elements */
+  float temp;               /* > 0; LLC_LOGITS only                                      */
+  const int32_t *tokens;    /* device [R,G]; may be NULL when G == 0                     */
+  int64_t tok_stride_r;
+  float *logp;              /* [R,G] required unless G == 0                              */
+  float *entropy;           /* [R]   optional                                            */
+  double *lse;              /* [R,2] optional                                            */
+  int32_t *top_ids;         /* [R,M] required unless M == 0                              */
+  float *top_logp;          /* [R,M] required unless M == 0                              */
+  void *workspace;          /* device, 256-byte aligned, >= llc_token_logprobs_workspace_size() */
+  size_t workspace_bytes;
+  void *stream;
+  int32_t flags;            /* LLC_FLAG_DRY_RUN                                          */
+  int32_t v_chunks;         /* 0 = choose; else workgroups a row is split over (1..64).  Which ids are
+                               listed does not depend on it; sums do by their rounding       */
+  void *ev_begin, *ev_end;  /* optional hipEvent_t pair recorded around the kernels      */
+} llc_token_logprobs_args;
+
+/* Arguments of llc_token_logprobs_grad: the gradient of
+ *   sum_g grad_logp[r,g] logp[r,g] + grad_entropy[r] entropy[r]
+ * with respect to x[r,:],
+ *   grad[r,i] = (sum_g a_g [i == t_g] - p_i (A + b (ln p_i + H))) / temp,
+ * a_g over the slots that hold an id in [0, V) (the others' are not looked at), A their sum, b the
+ * entropy's weight; 0 for an entry without mass, and in a row without mass.  Rounded once to the
+ * inputs' type.  grad may be x itself (same stride).  Either the row's lse, and with
+ * grad_entropy its entropy, are given as llc_token_logprobs returned them, or (lse == NULL) the call
+ * forms them itself and returns logp, entropy and lse on request: a loss whose weights are known beforehand
+ * then takes one call and, where a row fits a workgroup's registers, one pass. */
+typedef struct llc_token_logprobs_grad_args {
+  int64_t R, V, G;          /* as above                                                  */
+  int32_t dtype, kind;      /* as above                                                  */
+  const void *x;            /* device [R,V] */
+  int64_t stride_r;
+  float temp;
+  const int32_t *tokens;    /* device [R,G]; may be NULL when G == 0                     */
+  int64_t tok_stride_r;
+  const float *grad_logp;   /* device [R,G]; may be NULL when G == 0                     */
+  int64_t grad_logp_stride_r;
+  const float *grad_entropy;/* device [R] or NULL                                        */
+  const double *lse_in;     /* device [R,2] or NULL                                       */
+  const float *entropy_in;  /* device [R]; required with lse_in and grad_entropy         */
+  void *grad;               /* [R,V] of the inputs' type, required                       */
+  int64_t grad_stride_r;
+  float *logp;              /* [R,G] optional; LLC_E_OPTION with lse_in                  */
+  float *entropy;           /* [R]   optional; LLC_E_OPTION with lse_in                  */
+  double *lse;              /* [R,2] optional; LLC_E_OPTION with lse_in                  */
+  void *workspace;          /* device, 256-byte aligned, >= llc_token_logprobs_workspace_size(R, V, 0);
+                               may be NULL with lse_in                                   */
+  size_t workspace_bytes;
+  void *stream;
+  int32_t flags;            /* LLC_FLAG_DRY_RUN                                          */
+  int32_t v_chunks;         /* 0 = choose; else workgroups a row is split over (1..64)   */
+  void *ev_begin, *ev_end;
+} llc_token_logprobs_grad_args;
+
+/* Arguments of llc_embed: out[t,:] = scale * table[tokens[t],:], rounded once to the output's type;
+ * zeros for a token outside [0, N). */
+typedef struct llc_embed_args {
+  int64_t T, N, D;          /* T in 0..2^31 - 5, N, D in 1..2^31 - 5                     */
+  int32_t dtype, out_dtype; /* of table and of out: LLC_F32 | LLC_BF16                   */
+  const void *table;        /* device [N,D] */
+  int64_t table_stride_n;
+  const int32_t *tokens;    /* device [T] */
+  int64_t tok_stride;
+  float scale;              /* finite */
+  void *out;                /* [T,D] */
+  int64_t out_stride_t;
+  void *stream;
+  int32_t flags;            /* LLC_FLAG_DRY_RUN */
+  void *ev_begin, *ev_end;
+} llc_embed_args;
+
+/* Arguments of llc_embed_grad: grad[n,:] = scale * sum over t with tokens[t] == n of g[t,:], summed in
+ * fp32 in an order that follows t alone (the tokens are sorted, no floating-point atomics: the
+ * same inputs give the same bits) and rounded once; tokens outside [0, N) take no part.
+ * add == 0: every row of grad is written, zeros where no token is.  add != 0: the sum is added to the rows whose
+ * tokens occur (in fp32, then rounded), the others are not touched. */
+typedef struct llc_embed_grad_args {
+  int64_t T, N, D;          /* as above; N at most 2^27                                  */
+  int32_t dtype, grad_dtype;/* of g and of grad                                          */
+  const void *g;            /* device [T,D] */
+  int64_t g_stride_t;
+  const int32_t *tokens;    /* device [T] */
+  int64_t tok_stride;
+  float scale;              /* finite */
+  int32_t add;
+  void *grad;               /* [N,D] */
+  int64_t grad_stride_n;
+  void *workspace;          /* device, 256-byte aligned, >= llc_embed_grad_workspace_size() */
+  size_t workspace_bytes;
+  void *stream;
+  int32_t flags;            /* LLC_FLAG_DRY_RUN */
+  void *ev_begin, *ev_end;
+} llc_embed_grad_args;
+
+/* Arguments of llc_clip_grad_norm: norm = sqrt of the sum of squares over all n tensors (fp64 throughout,
+ * so that squares neither overflow nor vanish; rounded once), and out_j = grad_j * min(1, max_norm / norm),
+ * the factor in fp32, each product rounded once.  A norm that is not finite leaves the gradients as they are (the caller sees
+ * it in `norm`).  The arrays grads, numel, dtype and out are HOST arrays, read before the call returns;
+ * their pointers are device pointers to contiguous tensors.  out == NULL: in place.  max_norm may be +inf: the
+ * norm alone (out, if given, gets copies).  Tensors must not overlap each other unless out_j is grad_j. */
+typedef struct llc_clip_grad_norm_args {
+  int64_t n;                /* 0 <= n <= 2^20 */
+  void *const *grads;
+  const int64_t *numel;     /* each >= 0; 2^40 in all at most */
+  const int32_t *dtype;     /* of each: LLC_F32 | LLC_BF16 */
+  void *const *out;
+  float max_norm;           /* > 0 */
+  float *norm;              /* device, required */
+  void *workspace;          /* device, 256-byte aligned, >= llc_clip_grad_norm_workspace_size(n) */
+  size_t workspace_bytes;
+  void *stream;
+  int32_t flags;            /* LLC_FLAG_DRY_RUN */
+  void *ev_begin, *ev_end;
+} llc_clip_grad_norm_args;
+
+/* Scores of tokens (log probability, entropy, top alternatives).  Asynchronous. */
+int llc_token_logprobs(const llc_token_logprobs_args *a);
+
+/* Their gradient, in one call with the scores themselves or from what they returned.  Asynchronous. */
+int llc_token_logprobs_grad(const llc_token_logprobs_grad_args *a);
+
+/* Bytes of device scratch both need for this shape with v_chunks = 0 (M = 0 for the gradient); an explicit
+ * v_chunks = c needs c * R * (32 + 8 M) + 32 R + 512.  0 on bad shapes. */
+size_t llc_token_logprobs_workspace_size(int64_t R, int64_t V, int64_t M);
+
+/* Embedding lookup.  Asynchronous. */
+int llc_embed(const llc_embed_args *a);
+
+/* Its gradient by sorted tokens.  Asynchronous. */
+int llc_embed_grad(const llc_embed_grad_args *a);
+size_t llc_embed_grad_workspace_size(int64_t T, int64_t N, int64_t D);
+
+/* Clipping by the global norm.  Asynchronous. */
+int llc_clip_grad_norm(const llc_clip_grad_norm_args *a);
+size_t llc_clip_grad_norm_workspace_size(int64_t n);
 
 /* Algorithm 1 on a batch (Section 3).  Asynchronous on a->stream. */
 int llc_couple(const llc_couple_args *a);

@@ -29,7 +29,8 @@ FLAG_DRAFT_ONLY = 32  # the draft side alone: no target, no Y, no accept test
 _KINDS = {"logits": LOGITS, "probs": PROBS, "logw": LOGW}
 EXPORTS = ["llc_couple", "llc_couple_static", "llc_couple_is", "llc_couple_topm", "llc_compress_select", "llc_verify", "llc_lml_bound",
            "llc_couple_workspace_size", "llc_verify_workspace_size", "llc_lml_workspace_size", "llc_status_string",
-           "llc_version"]
+           "llc_version", "llc_token_logprobs", "llc_token_logprobs_grad", "llc_token_logprobs_workspace_size", "llc_embed",
+           "llc_embed_grad", "llc_embed_grad_workspace_size", "llc_clip_grad_norm", "llc_clip_grad_norm_workspace_size"]
 
 
 class LlcStats(ctypes.Structure):
@@ -159,6 +160,74 @@ class LmlArgs(ctypes.Structure):
     ]
 
 
+TOP_MAX = 128
+
+
+class TokenLogprobsArgs(ctypes.Structure):
+    _fields_ = [
+        ("R", ctypes.c_int64), ("V", ctypes.c_int64), ("G", ctypes.c_int64), ("M", ctypes.c_int64),
+        ("dtype", ctypes.c_int32), ("kind", ctypes.c_int32),
+        ("x", ctypes.c_void_p), ("stride_r", ctypes.c_int64), ("temp", ctypes.c_float),
+        ("tokens", ctypes.c_void_p), ("tok_stride_r", ctypes.c_int64),
+        ("logp", ctypes.c_void_p), ("entropy", ctypes.c_void_p), ("lse", ctypes.c_void_p),
+        ("top_ids", ctypes.c_void_p), ("top_logp", ctypes.c_void_p),
+        ("workspace", ctypes.c_void_p), ("workspace_bytes", ctypes.c_size_t),
+        ("stream", ctypes.c_void_p), ("flags", ctypes.c_int32), ("v_chunks", ctypes.c_int32),
+        ("ev_begin", ctypes.c_void_p), ("ev_end", ctypes.c_void_p),
+    ]
+
+
+class TokenLogprobsGradArgs(ctypes.Structure):
+    _fields_ = [
+        ("R", ctypes.c_int64), ("V", ctypes.c_int64), ("G", ctypes.c_int64),
+        ("dtype", ctypes.c_int32), ("kind", ctypes.c_int32),
+        ("x", ctypes.c_void_p), ("stride_r", ctypes.c_int64), ("temp", ctypes.c_float),
+        ("tokens", ctypes.c_void_p), ("tok_stride_r", ctypes.c_int64),
+        ("grad_logp", ctypes.c_void_p), ("grad_logp_stride_r", ctypes.c_int64),
+        ("grad_entropy", ctypes.c_void_p), ("lse_in", ctypes.c_void_p), ("entropy_in", ctypes.c_void_p),
+        ("grad", ctypes.c_void_p), ("grad_stride_r", ctypes.c_int64),
+        ("logp", ctypes.c_void_p), ("entropy", ctypes.c_void_p), ("lse", ctypes.c_void_p),
+        ("workspace", ctypes.c_void_p), ("workspace_bytes", ctypes.c_size_t),
+        ("stream", ctypes.c_void_p), ("flags", ctypes.c_int32), ("v_chunks", ctypes.c_int32),
+        ("ev_begin", ctypes.c_void_p), ("ev_end", ctypes.c_void_p),
+    ]
+
+
+class EmbedArgs(ctypes.Structure):
+    _fields_ = [
+        ("T", ctypes.c_int64), ("N", ctypes.c_int64), ("D", ctypes.c_int64),
+        ("dtype", ctypes.c_int32), ("out_dtype", ctypes.c_int32),
+        ("table", ctypes.c_void_p), ("table_stride_n", ctypes.c_int64),
+        ("tokens", ctypes.c_void_p), ("tok_stride", ctypes.c_int64), ("scale", ctypes.c_float),
+        ("out", ctypes.c_void_p), ("out_stride_t", ctypes.c_int64),
+        ("stream", ctypes.c_void_p), ("flags", ctypes.c_int32),
+        ("ev_begin", ctypes.c_void_p), ("ev_end", ctypes.c_void_p),
+    ]
+
+
+class EmbedGradArgs(ctypes.Structure):
+    _fields_ = [
+        ("T", ctypes.c_int64), ("N", ctypes.c_int64), ("D", ctypes.c_int64),
+        ("dtype", ctypes.c_int32), ("grad_dtype", ctypes.c_int32),
+        ("g", ctypes.c_void_p), ("g_stride_t", ctypes.c_int64),
+        ("tokens", ctypes.c_void_p), ("tok_stride", ctypes.c_int64), ("scale", ctypes.c_float), ("add", ctypes.c_int32),
+        ("grad", ctypes.c_void_p), ("grad_stride_n", ctypes.c_int64),
+        ("workspace", ctypes.c_void_p), ("workspace_bytes", ctypes.c_size_t),
+        ("stream", ctypes.c_void_p), ("flags", ctypes.c_int32),
+        ("ev_begin", ctypes.c_void_p), ("ev_end", ctypes.c_void_p),
+    ]
+
+
+class ClipGradNormArgs(ctypes.Structure):
+    _fields_ = [
+        ("n", ctypes.c_int64), ("grads", ctypes.c_void_p), ("numel", ctypes.c_void_p), ("dtype", ctypes.c_void_p),
+        ("out", ctypes.c_void_p), ("max_norm", ctypes.c_float), ("norm", ctypes.c_void_p),
+        ("workspace", ctypes.c_void_p), ("workspace_bytes", ctypes.c_size_t),
+        ("stream", ctypes.c_void_p), ("flags", ctypes.c_int32),
+        ("ev_begin", ctypes.c_void_p), ("ev_end", ctypes.c_void_p),
+    ]
+
+
 _lib = None
 _empties = None
 
@@ -197,6 +266,14 @@ def load():
         lib.llc_couple_workspace_size.restype = ctypes.c_size_t
         lib.llc_verify_workspace_size.argtypes = [ctypes.c_int64] * 4
         lib.llc_verify_workspace_size.restype = ctypes.c_size_t
+        for name, args in (("llc_token_logprobs", TokenLogprobsArgs), ("llc_token_logprobs_grad", TokenLogprobsGradArgs),
+                           ("llc_embed", EmbedArgs), ("llc_embed_grad", EmbedGradArgs), ("llc_clip_grad_norm", ClipGradNormArgs)):
+            getattr(lib, name).argtypes = [ctypes.POINTER(args)]
+            getattr(lib, name).restype = ctypes.c_int
+        for name, count in (("llc_token_logprobs_workspace_size", 3), ("llc_embed_grad_workspace_size", 3),
+                            ("llc_clip_grad_norm_workspace_size", 1)):
+            getattr(lib, name).argtypes = [ctypes.c_int64] * count
+            getattr(lib, name).restype = ctypes.c_size_t
         lib.llc_status_string.argtypes = [ctypes.c_int]
         lib.llc_status_string.restype = ctypes.c_char_p
         lib.llc_version.restype = ctypes.c_int
@@ -656,6 +733,284 @@ def llc_lml_bound(draft: torch.Tensor, target: torch.Tensor, ks, *, kind="logits
         raise LlcError(rc)
     out["_workspace"] = workspace  # keeps the scratch alive until the caller drops the result
     return out
+
+
+_TYPES = {torch.float32: F32, torch.bfloat16: BF16}
+
+
+def llc_token_logprobs_workspace_size(R: int, V: int, M: int) -> int:
+    return load().llc_token_logprobs_workspace_size(R, V, M)
+
+
+def llc_embed_grad_workspace_size(T: int, N: int, D: int) -> int:
+    return load().llc_embed_grad_workspace_size(T, N, D)
+
+
+def llc_clip_grad_norm_workspace_size(n: int) -> int:
+    return load().llc_clip_grad_norm_workspace_size(n)
+
+
+def _row_stride(t):
+    # (the stride of a single row, or of none, says nothing)
+    return t.stride(0) if t.shape[0] > 1 else max(t.stride(0), t.shape[1])
+
+
+def _scored(name, x, tokens, kind):
+    """The checks that scores and their gradient share; (R, V, G)."""
+    if not x.is_cuda or not (tokens is None or tokens.is_cuda):
+        raise ValueError(f"{name} needs device tensors (there is no CPU path)")
+    if x.dtype not in _TYPES or x.dim() != 2 or (x.stride(1) != 1 and x.shape[1] > 1):
+        raise ValueError("logits must be [R,V], float32 or bfloat16, last dimension contiguous")
+    if kind not in ("logits", "logw"):
+        raise ValueError("kind must be logits or logw")
+    R, V = x.shape
+    if tokens is None:
+        return R, V, 0
+    if tokens.device != x.device or tokens.dtype != torch.int32 or tokens.dim() not in (1, 2) or tokens.shape[0] != R or (
+            tokens.dim() == 2 and tokens.stride(1) != 1 and tokens.shape[1] > 1):
+        raise ValueError("tokens must be [R] or [R,G] int32 on the logits' device, last dimension of [R,G] contiguous")
+    return R, V, 1 if tokens.dim() == 1 else tokens.shape[1]
+
+
+def _score_workspace(R, V, M, v_chunks, device):
+    n = llc_token_logprobs_workspace_size(R, V, M)
+    if v_chunks > 0:
+        n = max(n, v_chunks * R * (32 + 8 * M) + 32 * R + 512)
+    return torch.empty(max(n, 256), dtype=torch.uint8, device=device)
+
+
+def llc_token_logprobs(logits: torch.Tensor, tokens: Optional[torch.Tensor], M: int = 0, *, kind="logits", temp: float = 1.0,
+                       want_entropy: bool = True, want_lse: bool = False, workspace: Optional[torch.Tensor] = None,
+                       out: Optional[dict] = None, flags: int = 0, v_chunks: int = 0, events=None) -> dict:
+    """Log probabilities of given tokens, entropy and top alternatives of every row.
+
+    logits: [R,V] float32 or bfloat16 (kind "logits", with the temperature, or "logw"); tokens: [R] or [R,G] int32
+    (negative: an empty slot), or None.  Returns float32 logp (the tokens' shape; 0 for an empty slot, -inf for a token
+    without mass), if asked entropy [R] and lse [R,2] (float64: the largest logit and ln of the sum of exp((logit - it) / temp)), and for M > 0 the M likeliest entries of a row: top_ids
+    [R,M] int32 and top_logp [R,M], likelier first, equal ones by index, -1 and -inf where fewer have mass.  The lists go into
+    llc_couple_topm as they are (kind "logw").  Asynchronous on torch's current stream.
+    """
+    lib = load()
+    R, V, G = _scored("llc_token_logprobs", logits, tokens, kind)
+    dev = logits.device
+    if out is None:
+        specs = {}
+        if tokens is not None:
+            specs["logp"] = (torch.float32, *tokens.shape)
+        if want_entropy:
+            specs["entropy"] = (torch.float32, R)
+        if want_lse:
+            specs["lse"] = (torch.float64, R, 2)
+        if M > 0:
+            specs["top_ids"] = (torch.int32, R, M)
+            specs["top_logp"] = (torch.float32, R, M)
+        out = _new(dev, specs)
+    if workspace is None:
+        workspace = _score_workspace(R, V, M, v_chunks, dev)
+    a = TokenLogprobsArgs()
+    a.R, a.V, a.G, a.M = R, V, G, M
+    a.dtype, a.kind = _TYPES[logits.dtype], _KINDS[kind]
+    a.x, a.stride_r, a.temp = logits.data_ptr(), logits.stride(0), temp
+    if tokens is not None:
+        a.tokens, a.tok_stride_r = tokens.data_ptr(), tokens.stride(0)
+    a.logp, a.entropy, a.lse = _ptr(out.get("logp")), _ptr(out.get("entropy")), _ptr(out.get("lse"))
+    a.top_ids, a.top_logp = _ptr(out.get("top_ids")), _ptr(out.get("top_logp"))
+    a.workspace, a.workspace_bytes = workspace.data_ptr(), workspace.numel()
+    a.stream = _stream_handle(dev)
+    a.flags, a.v_chunks = flags, v_chunks
+    if events is not None:
+        a.ev_begin, a.ev_end = events
+    rc = lib.llc_token_logprobs(ctypes.byref(a))
+    if rc != 0:
+        raise LlcError(rc)
+    return out
+
+
+def llc_token_logprobs_grad(logits: torch.Tensor, tokens: Optional[torch.Tensor], grad_logp: Optional[torch.Tensor], *,
+                            grad_entropy: Optional[torch.Tensor] = None, lse: Optional[torch.Tensor] = None,
+                            entropy: Optional[torch.Tensor] = None, kind="logits", temp: float = 1.0,
+                            want_scores: bool = True, workspace: Optional[torch.Tensor] = None, out: Optional[dict] = None,
+                            flags: int = 0, v_chunks: int = 0, events=None) -> dict:
+    """The gradient of sum(grad_logp * logp) + sum(grad_entropy * entropy) with respect to the logits.
+
+    logits, tokens, kind, temp as in llc_token_logprobs; grad_logp has the tokens' shape, grad_entropy is [R], both float32.
+    Returns grad [R,V] in the logits' type (out["grad"] may be the logits themselves).  With `lse` (and, with grad_entropy,
+    `entropy`) as llc_token_logprobs returned them the gradient is formed from them; without, the call forms the scores
+    itself and, if asked, returns logp and entropy too: a loss whose weights are known beforehand takes one call.
+    Asynchronous on torch's current stream.
+    """
+    lib = load()
+    R, V, G = _scored("llc_token_logprobs_grad", logits, tokens, kind)
+    dev = logits.device
+    if tokens is not None and (grad_logp is None or grad_logp.device != dev or grad_logp.dtype != torch.float32
+                               or grad_logp.shape != tokens.shape
+                               or (grad_logp.dim() == 2 and grad_logp.stride(1) != 1 and G > 1)):
+        raise ValueError("grad_logp must be float32 of the tokens' shape on the logits' device, last dimension contiguous")
+    for t, dtype, shape in ((grad_entropy, torch.float32, (R,)), (entropy, torch.float32, (R,)), (lse, torch.float64, (R, 2))):
+        if t is not None and (t.device != dev or t.dtype != dtype or tuple(t.shape) != shape or not t.is_contiguous()):
+            raise ValueError("grad_entropy and entropy must be [R] float32, lse [R,2] float64, contiguous on the logits' device")
+    if out is None:
+        specs = {"grad": (logits.dtype, R, V)}
+        if want_scores and lse is None:
+            if tokens is not None:
+                specs["logp"] = (torch.float32, *tokens.shape)
+            specs["entropy"] = (torch.float32, R)
+        out = _new(dev, specs)
+    grad = out["grad"]
+    if grad.device != dev or grad.dtype != logits.dtype or tuple(grad.shape) != (R, V) or (grad.stride(1) != 1 and V > 1):
+        raise ValueError("grad must be [R,V] of the logits' type, last dimension contiguous")
+    if workspace is None and lse is None:
+        workspace = _score_workspace(R, V, 0, v_chunks, dev)
+    a = TokenLogprobsGradArgs()
+    a.R, a.V, a.G = R, V, G
+    a.dtype, a.kind = _TYPES[logits.dtype], _KINDS[kind]
+    a.x, a.stride_r, a.temp = logits.data_ptr(), logits.stride(0), temp
+    if tokens is not None:
+        a.tokens, a.tok_stride_r = tokens.data_ptr(), tokens.stride(0)
+        a.grad_logp, a.grad_logp_stride_r = grad_logp.data_ptr(), grad_logp.stride(0)
+    a.grad_entropy, a.lse_in, a.entropy_in = _ptr(grad_entropy), _ptr(lse), _ptr(entropy)
+    a.grad, a.grad_stride_r = grad.data_ptr(), _row_stride(grad)
+    a.logp, a.entropy, a.lse = _ptr(out.get("logp")), _ptr(out.get("entropy")), _ptr(out.get("lse"))
+    if workspace is not None:
+        a.workspace, a.workspace_bytes = workspace.data_ptr(), workspace.numel()
+    a.stream = _stream_handle(dev)
+    a.flags, a.v_chunks = flags, v_chunks
+    if events is not None:
+        a.ev_begin, a.ev_end = events
+    rc = lib.llc_token_logprobs_grad(ctypes.byref(a))
+    if rc != 0:
+        raise LlcError(rc)
+    return out
+
+
+def llc_embed(table: torch.Tensor, tokens: torch.Tensor, *, scale: float = 1.0, out_dtype: Optional[torch.dtype] = None,
+              out: Optional[torch.Tensor] = None, flags: int = 0, events=None) -> dict:
+    """Embedding lookup: out[..., :] = scale * table[tokens[...], :], zeros for tokens outside the table.
+
+    table: [N,D] float32 or bfloat16; tokens: int32 of any shape (a transposed or otherwise strided one is made
+    contiguous first); out has the tokens' shape and D, in out_dtype (default: the table's).  Asynchronous.
+    """
+    lib = load()
+    if not (table.is_cuda and tokens.device == table.device):
+        raise ValueError("llc_embed needs device tensors of one device (there is no CPU path)")
+    if table.dtype not in _TYPES or table.dim() != 2 or (table.stride(1) != 1 and table.shape[1] > 1) or tokens.dtype != torch.int32:
+        raise ValueError("table must be [N,D] float32 or bfloat16, last dimension contiguous; tokens int32")
+    N, D = table.shape
+    tokens, shape = _flat(tokens), tokens.shape
+    if out is None:
+        out = _new(table.device, {"out": (out_dtype or table.dtype, tokens.shape[0], D)})["out"].view(*shape, D)
+    rows = out if out.dim() == 2 else out.view(-1, out.shape[-1])
+    if (out.device != table.device or out.dtype not in _TYPES or out_dtype not in (None, out.dtype) or tuple(out.shape) != (*shape, D)
+            or (rows.stride(1) != 1 and D > 1)):
+        raise ValueError("out must have the tokens' shape and D, float32 or bfloat16, rows contiguous")
+    a = EmbedArgs()
+    a.T, a.N, a.D = tokens.shape[0], N, D
+    a.dtype, a.out_dtype = _TYPES[table.dtype], _TYPES[out.dtype]
+    a.table, a.table_stride_n = table.data_ptr(), table.stride(0)
+    a.tokens, a.tok_stride, a.scale = tokens.data_ptr(), tokens.stride(0), scale
+    a.out, a.out_stride_t = out.data_ptr(), _row_stride(rows)
+    a.stream = _stream_handle(table.device)
+    a.flags = flags
+    if events is not None:
+        a.ev_begin, a.ev_end = events
+    rc = lib.llc_embed(ctypes.byref(a))
+    if rc != 0:
+        raise LlcError(rc)
+    return {"out": out}
+
+
+def _flat(tokens):
+    return tokens if tokens.dim() == 1 else tokens.reshape(-1)
+
+
+def llc_embed_grad(g: torch.Tensor, tokens: torch.Tensor, N: int, *, scale: float = 1.0, out_dtype: Optional[torch.dtype] = None,
+                   out: Optional[torch.Tensor] = None, add: bool = False, workspace: Optional[torch.Tensor] = None,
+                   flags: int = 0, events=None) -> dict:
+    """The gradient of llc_embed with respect to its table: grad[n] = scale * the sum of g over the tokens n.
+
+    g: the tokens' shape and D, float32 or bfloat16; tokens int32.  Returns grad [N,D] in out_dtype (default: g's), every
+    row written; with add=True the sums are added to `out` instead and rows without a token are left alone.  The sums'
+    order follows the tokens alone: the same inputs give the same bits.  Asynchronous.
+    """
+    lib = load()
+    if not (g.is_cuda and tokens.device == g.device):
+        raise ValueError("llc_embed_grad needs device tensors of one device (there is no CPU path)")
+    if g.dtype not in _TYPES or g.shape[:-1] != tokens.shape or tokens.dtype != torch.int32 or g.dim() < 2:
+        raise ValueError("g must have the tokens' shape and D, float32 or bfloat16; tokens int32")
+    D = g.shape[-1]
+    tokens = _flat(tokens)
+    rows = g if g.dim() == 2 else g.reshape(-1, D)
+    if rows.stride(1) != 1 and D > 1:
+        raise ValueError("g's last dimension must be contiguous")
+    if add and out is None:
+        raise ValueError("add=True needs the gradient to add to")
+    if out is None:
+        out = _new(g.device, {"grad": (out_dtype or g.dtype, N, D)})["grad"]
+    if (out.device != g.device or out.dtype not in _TYPES or out_dtype not in (None, out.dtype) or tuple(out.shape) != (N, D)
+            or (out.stride(1) != 1 and D > 1)):
+        raise ValueError("out must be [N,D], float32 or bfloat16, last dimension contiguous")
+    T = rows.shape[0]
+    if workspace is None:
+        workspace = torch.empty(max(llc_embed_grad_workspace_size(T, N, D), 256), dtype=torch.uint8, device=g.device)
+    a = EmbedGradArgs()
+    a.T, a.N, a.D = T, N, D
+    a.dtype, a.grad_dtype = _TYPES[g.dtype], _TYPES[out.dtype]
+    a.g, a.g_stride_t = rows.data_ptr(), rows.stride(0)
+    a.tokens, a.tok_stride, a.scale, a.add = tokens.data_ptr(), tokens.stride(0), scale, 1 if add else 0
+    a.grad, a.grad_stride_n = out.data_ptr(), _row_stride(out)
+    a.workspace, a.workspace_bytes = workspace.data_ptr(), workspace.numel()
+    a.stream = _stream_handle(g.device)
+    a.flags = flags
+    if events is not None:
+        a.ev_begin, a.ev_end = events
+    rc = lib.llc_embed_grad(ctypes.byref(a))
+    if rc != 0:
+        raise LlcError(rc)
+    return {"grad": out}
+
+
+def llc_clip_grad_norm(grads, max_norm: float, *, out=None, workspace: Optional[torch.Tensor] = None, flags: int = 0,
+                       events=None) -> dict:
+    """Scales gradients so that their common norm (the root of the sum of all squares) is at most max_norm.
+
+    grads: contiguous float32 or bfloat16 tensors of one device, mixed as they come; in place, or into `out`, tensors of the same sizes
+    and types.  max_norm = inf: the norm alone.  Returns norm, a float32 scalar on the device; where it is
+    not finite the gradients are left as they are.  Asynchronous on torch's current stream.
+    """
+    lib = load()
+    grads = list(grads)
+    if not grads:
+        raise ValueError("no gradients")
+    n, dev = len(grads), grads[0].device
+    to = grads if out is None else list(out)
+    if len(to) != n:
+        raise ValueError("out must hold one tensor for each gradient")
+    pointers, outs, numel, dtype = (ctypes.c_void_p * n)(), (ctypes.c_void_p * n)(), (ctypes.c_int64 * n)(), (ctypes.c_int32 * n)()
+    for j in range(n):
+        t, o = grads[j], to[j]
+        if not t.is_cuda or t.device != dev or t.dtype not in _TYPES or not t.is_contiguous():
+            raise ValueError("gradients must be contiguous float32 or bfloat16 tensors of one device (there is no CPU path)")
+        if o is not t and (o.device != dev or o.dtype != t.dtype or o.shape != t.shape or not o.is_contiguous()):
+            raise ValueError("out must have the gradients' sizes and types, contiguous, on their device")
+        pointers[j], outs[j], numel[j], dtype[j] = t.data_ptr(), o.data_ptr(), t.numel(), _TYPES[t.dtype]
+    norm = torch.empty((), dtype=torch.float32, device=dev)
+    if workspace is None:
+        workspace = torch.empty(max(llc_clip_grad_norm_workspace_size(n), 256), dtype=torch.uint8, device=dev)
+    a = ClipGradNormArgs()
+    a.n = n
+    a.grads, a.numel, a.dtype = (ctypes.cast(v, ctypes.c_void_p) for v in (pointers, numel, dtype))
+    if out is not None:
+        a.out = ctypes.cast(outs, ctypes.c_void_p)
+    a.max_norm, a.norm = max_norm, norm.data_ptr()
+    a.workspace, a.workspace_bytes = workspace.data_ptr(), workspace.numel()
+    a.stream = _stream_handle(dev)
+    a.flags = flags
+    if events is not None:
+        a.ev_begin, a.ev_end = events
+    rc = lib.llc_clip_grad_norm(ctypes.byref(a))
+    if rc != 0:
+        raise LlcError(rc)
+    return {"norm": norm}
 
 
 def new_workspace(B: int, K: int, V: int, device, v_chunks: int = 0) -> torch.Tensor:

@@ -1,0 +1,260 @@
+"""Embedding lookup, its gradient and clipping against plain evaluations (needs an MI355X)."""
+import math
+
+import numpy as np
+import pytest
+import torch
+
+import paper_2506_05632_amd as llc
+
+pytestmark = pytest.mark.gpu
+DEV = "cuda:0"
+F32, BF16 = torch.float32, torch.bfloat16
+TYPES = [(F32, F32), (F32, BF16), (BF16, F32), (BF16, BF16)]
+
+
+def _gen(seed):
+    g = torch.Generator(device=DEV)
+    g.manual_seed(seed)
+    return g
+
+
+def _normal(shape, dtype, seed):
+    return torch.randn(shape, generator=_gen(seed), device=DEV).to(dtype)
+
+
+def _ids(T, N, seed, hot=0.0):
+    t = torch.randint(-1, N + 1, (T,), generator=_gen(seed), device=DEV)  # (-1 and N lie outside)
+    t = torch.where(torch.rand(T, generator=_gen(seed + 1), device=DEV) < hot, N // 2, t)
+    return t.to(torch.int32)
+
+
+def _plain_lookup(table, t, scale, dtype):
+    there = (t >= 0) & (t < table.shape[0])
+    rows = table[t.clamp(0, table.shape[0] - 1).long()].float() * np.float32(scale)
+    return torch.where(there[..., None], rows, 0.0).to(dtype)
+
+
+@pytest.mark.parametrize("types", TYPES)
+@pytest.mark.parametrize("T,N,D", [(1, 1, 1), (1, 50, 4096), (3, 7, 5), (7, 300, 63), (64, 1000, 64), (33, 2000, 1537), (1000, 50257, 130),
+                                   (129, 512, 2048), (5, 9, 20011)])
+def test_lookup(T, N, D, types):
+    table, t = _normal((N, D), types[0], T), _ids(T, N, D)
+    for scale in (1.0, 45.25, -0.3):
+        got = llc.llc_embed(table, t, scale=scale, out_dtype=types[1])["out"]
+        assert got.dtype == types[1] and torch.equal(got, _plain_lookup(table, t, scale, types[1]))  # (one product, one rounding)
+
+
+def test_lookup_shapes_strides_and_guards():
+    table = _normal((40, 99 + 7), BF16, 1)[:, 3:102]
+    t = _ids(24, 40, 2).view(4, 6)
+    assert torch.equal(llc.llc_embed(table, t)["out"], _plain_lookup(table, t, 1.0, BF16))
+    assert torch.equal(llc.llc_embed(table, t.t())["out"], _plain_lookup(table, t.t(), 1.0, BF16))
+    assert torch.equal(llc.llc_embed(table, t[:, 2])["out"], _plain_lookup(table, t[:, 2], 1.0, BF16))
+    wide = torch.full((24, 120), 7.0, device=DEV)
+    llc.llc_embed(table, t.view(-1), out=wide[:, 5:104])
+    assert torch.equal(wide[:, 5:104], _plain_lookup(table, t.view(-1), 1.0, F32))
+    assert (wide[:, :5] == 7).all() and (wide[:, 104:] == 7).all()
+    one = llc.llc_embed(table, torch.tensor(5, dtype=torch.int32, device=DEV))["out"]
+    assert one.shape == (99,) and torch.equal(one, table[5])
+    assert llc.llc_embed(table, t[:0])["out"].shape == (0, 6, 99)
+
+
+def test_a_table_beyond_32_bits():
+    N, D = (1 << 19) + 3, 4096  # 2^31 and some entries
+    table = torch.empty(N, D, dtype=BF16, device=DEV)
+    t = torch.tensor([0, N - 1, N - 2, 1 << 18, N], dtype=torch.int32, device=DEV)
+    table[t[:4].long()] = _normal((4, D), BF16, 1)
+    assert torch.equal(llc.llc_embed(table, t, scale=2.0)["out"], _plain_lookup(table, t, 2.0, BF16))
+    g = _normal((5, D), BF16, 2)
+    before = table[t[:4].long()].clone()
+    llc.llc_embed_grad(g, t, N, out=table, add=True)
+    assert torch.equal(table[t[:4].long()], (before.float() + g[:4].float()).to(BF16))
+
+
+# the sum over a row's n tokens in fp32: n roundings of at most the sum of the sizes, then the scale's and the output's
+def _check_grad(got, g, t, N, scale, before=None):
+    g64, s = g.double(), float(np.float32(scale))
+    there = (t >= 0) & (t < N)
+    rows = t[there].long()
+    want = torch.zeros(N, g.shape[1], dtype=torch.float64, device=DEV).index_put_((rows,), g64[there], accumulate=True) * s
+    size = torch.zeros_like(want).index_put_((rows,), g64[there].abs(), accumulate=True) * abs(s)
+    n = torch.zeros(N, dtype=torch.float64, device=DEV).index_put_((rows,), torch.ones(rows.numel(), dtype=torch.float64, device=DEV), accumulate=True)
+    if before is not None:
+        want = want + before.double()
+        size = size + before.double().abs()
+    tol = (n[:, None] + 3) * 2.0 ** -24 * size + (2.0 ** -8 if got.dtype == BF16 else 2.0 ** -23) * want.abs()
+    far = (got.double() - want).abs() - tol
+    assert far.max().item() <= 0, (far.max().item(), divmod(far.argmax().item(), g.shape[1]))
+    if before is not None:
+        untouched = n == 0
+        assert torch.equal(got[untouched], before[untouched])
+
+
+@pytest.mark.parametrize("types", TYPES)
+@pytest.mark.parametrize("T,N,D,hot", [(1, 1, 1, 0.0), (1, 300, 4096, 0.0), (3, 7, 5, 0.0), (64, 9, 64, 0.5), (65, 2000, 63, 0.0), (300, 1, 130, 0.0),
+                                       (1000, 50, 1537, 0.3), (1001, 50257, 40, 0.1), (5000, 700, 257, 1.0), (4097, 33, 512, 0.0),
+                                       (20000, 3000, 96, 0.4), (70000, 128, 64, 0.2), (129, 5, 20011, 0.9)])
+def test_gradient(T, N, D, hot, types):
+    g, t = _normal((T, D), types[0], T), _ids(T, N, D, hot)
+    for scale in (1.0, 45.25):
+        got = llc.llc_embed_grad(g, t, N, scale=scale, out_dtype=types[1])["grad"]
+        _check_grad(got, g, t, N, scale)
+        assert torch.equal(got, llc.llc_embed_grad(g, t, N, scale=scale, out_dtype=types[1])["grad"])  # the same bits again
+        before = _normal((N, D), types[1], 5)
+        got = llc.llc_embed_grad(g, t, N, scale=scale, out=before.clone(), add=True)["grad"]
+        _check_grad(got, g, t, N, scale, before)
+
+
+@pytest.mark.parametrize("T", [0, 1, 200])
+def test_gradient_without_valid_tokens(T):
+    g = _normal((T, 70), F32, 1)
+    t = torch.where(torch.arange(T, device=DEV) % 2 == 0, -1, 50).to(torch.int32)
+    assert torch.count_nonzero(llc.llc_embed_grad(g, t, 50)["grad"]) == 0
+    before = _normal((50, 70), F32, 2)
+    assert torch.equal(llc.llc_embed_grad(g, t, 50, out=before.clone(), add=True)["grad"], before)
+
+
+@pytest.mark.parametrize("add", [False, True])
+def test_gradient_strides_and_guards(add):
+    T, N, D = 500, 60, 99
+    g = _normal((T, 120), BF16, 1)[:, 7:7 + D]
+    t = _ids(2 * T, N, 2)[::2]
+    wide = torch.full((N, 120), 7.0, device=DEV)
+    before = wide[:, 5:5 + D].clone()
+    llc.llc_embed_grad(g, t, N, out=wide[:, 5:5 + D], add=add)
+    _check_grad(wide[:, 5:5 + D], g, t, N, 1.0, before if add else None)
+    assert (wide[:, :5] == 7).all() and (wide[:, 5 + D:] == 7).all()
+    # one row of gradients for all tokens, and tokens of a grid
+    one = _normal((1, D), F32, 3).expand(T, D)
+    _check_grad(llc.llc_embed_grad(one, t, N)["grad"], one, t, N, 1.0)
+    grid, tg = _normal((20, 25, D), F32, 4), t.reshape(20, 25)
+    assert torch.equal(llc.llc_embed_grad(grid, tg, N)["grad"], llc.llc_embed_grad(grid.view(T, D), t, N)["grad"])
+
+
+def test_lookup_and_gradient_agree_in_their_pairing():
+    # both are linear: <g, lookup(W)> = <W, gradient(g)>, each side rounded per entry to 2^-23 of it
+    T, N, D = 3000, 400, 77
+    table, g, t = _normal((N, D), F32, 1), _normal((T, D), F32, 2), _ids(T, N, 3)
+    left = (llc.llc_embed(table, t, scale=1.7)["out"].double() * g.double()).sum()
+    right = (llc.llc_embed_grad(g, t, N, scale=1.7)["grad"].double() * table.double()).sum()
+    assert abs(left - right) <= 2.0 ** -20 * 1.7 * math.sqrt(T * D) * 4
+    # against a difference: lookup(W + dW) - lookup(W) paired with g is <dW, gradient>
+    step = _normal((N, D), F32, 4)
+    moved = llc.llc_embed(table + step, t, scale=1.7)["out"].double() - llc.llc_embed(table, t, scale=1.7)["out"].double()
+    right = (llc.llc_embed_grad(g, t, N, scale=1.7)["grad"].double() * ((table + step).double() - table.double())).sum()
+    assert abs((moved * g.double()).sum() - right) <= 2.0 ** -20 * 1.7 * math.sqrt(T * D) * 8
+
+
+def test_embed_on_another_stream_and_in_a_graph():
+    table, t, g = _normal((500, 300), F32, 1), _ids(2000, 500, 2, 0.3), _normal((2000, 300), F32, 3)
+    want, want_grad = llc.llc_embed(table, t)["out"], llc.llc_embed_grad(g, t, 500)["grad"]
+    grads = [_normal((n,), F32, n) for n in (5, 100, 7777)]
+    torch.cuda.synchronize()
+    side = torch.cuda.Stream()
+    with torch.cuda.stream(side):
+        got, got_grad = llc.llc_embed(table, t)["out"], llc.llc_embed_grad(g, t, 500)["grad"]
+    side.synchronize()
+    assert torch.equal(got, want) and torch.equal(got_grad, want_grad)
+    still, clipped = t.clone(), [torch.empty_like(v) for v in grads]
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        held_grad = llc.llc_embed_grad(g, still, 500)["grad"]
+        held = llc.llc_embed(held_grad, still)["out"]
+        norm = llc.llc_clip_grad_norm(grads, 1.0, out=clipped)["norm"]
+    for n in range(4):
+        still.copy_(t.roll(n))
+        grads[1].mul_(1.5)
+        graph.replay()
+        torch.cuda.synchronize()
+        now = llc.llc_embed_grad(g, still, 500)["grad"]
+        again = [torch.empty_like(v) for v in grads]
+        assert torch.equal(held_grad, now) and torch.equal(held, llc.llc_embed(now, still)["out"]), n
+        assert torch.equal(norm, llc.llc_clip_grad_norm(grads, 1.0, out=again)["norm"]), n
+        assert all(torch.equal(u, v) for u, v in zip(clipped, again)), n
+
+
+def _grads(sizes, dtypes, scale=0.01):
+    return [(scale * torch.randn(s, generator=_gen(11 + n), device=DEV)).to(dtypes[n % len(dtypes)]) for n, s in enumerate(sizes)]
+
+
+# the norm is formed in fp64 and rounded once; factor, product and output are rounded once each
+def _check_clip(grads, got, norm, most):
+    want = math.sqrt(math.fsum(float(t.double().square().sum()) for t in grads))
+    assert abs(norm.item() - want) <= 2.0 ** -23 * want
+    factor = min(1.0, most / want) if want > 0 else 1.0
+    for t, c in zip(grads, got):
+        if factor == 1.0:
+            assert torch.equal(t, c)
+            continue
+        tol = (2.0 ** -8 if t.dtype == BF16 else 2.0 ** -22) * (t.double() * factor).abs() + 2.0 ** -133
+        assert ((c.double() - t.double() * factor).abs() <= tol).all()
+
+
+@pytest.mark.parametrize("dtypes", [(F32,), (BF16,), (BF16, F32, F32)])
+@pytest.mark.parametrize("sizes", [[1], [0, 3, 0], [5, 1023, 64, 1], [(300, 77), 77, (4096, 33), 1], [1000003], [3] * 700, [70001] * 3 + [0] + [(9, 9)] * 130])
+def test_clip(sizes, dtypes):
+    grads = _grads(sizes, dtypes)
+    for most in (1e-3, 0.1, 1e9, math.inf):
+        clipped = [torch.full_like(t, 9.0) for t in grads]
+        found = llc.llc_clip_grad_norm(grads, most, out=clipped)
+        _check_clip(grads, clipped, found["norm"], most)
+        mine = [t.clone() for t in grads]
+        again = llc.llc_clip_grad_norm(mine, most)
+        assert torch.equal(again["norm"], found["norm"]) and all(torch.equal(u, v) for u, v in zip(mine, clipped))
+
+
+def test_clip_views_at_any_element():
+    flat = _grads([100000], (BF16,))[0]
+    grads = [flat[1:4], flat[7:1000], flat[1001:50002], flat[50003:50003 + 2 * 99].view(2, 99), flat[60001:99999]]
+    mine = flat.clone()
+    views = [mine[1:4], mine[7:1000], mine[1001:50002], mine[50003:50003 + 2 * 99].view(2, 99), mine[60001:99999]]
+    found = llc.llc_clip_grad_norm(views, 0.01)
+    _check_clip(grads, views, found["norm"], 0.01)
+    between = torch.ones(100000, dtype=torch.bool, device=DEV)
+    for lo, hi in ((1, 4), (7, 1000), (1001, 50002), (50003, 50201), (60001, 99999)):
+        between[lo:hi] = False
+    assert torch.equal(mine[between], flat[between])
+
+
+def test_clip_sizes_of_all_magnitudes():
+    for scale in (1e-30, 1e-20, 1e19, 1e30):  # (squares in fp32 would vanish or overflow)
+        for dtype in (F32, BF16):
+            grads = _grads([1000, 77], (dtype,), scale)
+            clipped = [torch.empty_like(t) for t in grads]
+            norm = llc.llc_clip_grad_norm(grads, 1.0, out=clipped)["norm"]
+            _check_clip(grads, clipped, norm, 1.0)
+
+
+def test_clip_leaves_gradients_without_a_finite_norm():
+    for value in (math.inf, -math.inf, math.nan):
+        grads = _grads([3000, 50], (F32, BF16))
+        grads[0][1234] = value
+        mine = [t.clone() for t in grads]
+        norm = llc.llc_clip_grad_norm(mine, 0.5)["norm"]
+        assert not torch.isfinite(norm)
+        assert all(torch.equal(u.view(torch.uint8), v.view(torch.uint8)) for u, v in zip(grads, mine))
+    zeros = [torch.zeros(100, device=DEV)]
+    assert llc.llc_clip_grad_norm(zeros, 1.0)["norm"] == 0 and torch.count_nonzero(zeros[0]) == 0
+
+
+def test_refusals():
+    table, t, g = _normal((50, 8), F32, 1), _ids(6, 50, 1), _normal((6, 8), F32, 2)
+    for bad in (lambda: llc.llc_embed(table.cpu(), t.cpu()), lambda: llc.llc_embed(table, t.long()), lambda: llc.llc_embed(table.half(), t),
+                lambda: llc.llc_embed(table.t(), t), lambda: llc.llc_embed(table, t, out=torch.empty(5, 8, device=DEV)),
+                lambda: llc.llc_embed_grad(g, t[:5], 50), lambda: llc.llc_embed_grad(g, t, 50, add=True),
+                lambda: llc.llc_embed_grad(g, t, 50, out=torch.empty(49, 8, device=DEV)), lambda: llc.llc_embed_grad(g.cpu(), t, 50),
+                lambda: llc.llc_clip_grad_norm([], 1.0), lambda: llc.llc_clip_grad_norm([g.cpu()], 1.0), lambda: llc.llc_clip_grad_norm([g.t()], 1.0),
+                lambda: llc.llc_clip_grad_norm([g.half()], 1.0), lambda: llc.llc_clip_grad_norm([g], 1.0, out=[]),
+                lambda: llc.llc_clip_grad_norm([g], 1.0, out=[g.bfloat16()])):
+        with pytest.raises(ValueError):
+            bad()
+    small = torch.empty(0, dtype=torch.uint8, device=DEV)
+    for code, bad in ((-8, lambda: llc.llc_embed(table, t, scale=math.nan)), (-2, lambda: llc.llc_embed(table, t, out=torch.empty(8, device=DEV).expand(6, 8))),
+                      (-6, lambda: llc.llc_embed_grad(g, t, 50, workspace=small)), (-8, lambda: llc.llc_embed_grad(g, t, 50, scale=math.inf)),
+                      (-2, lambda: llc.llc_embed_grad(g, t, 50, out=torch.empty(8, device=DEV).expand(50, 8))),
+                      (-6, lambda: llc.llc_clip_grad_norm([g], 1.0, workspace=small)), (-8, lambda: llc.llc_clip_grad_norm([g], 0.0)),
+                      (-8, lambda: llc.llc_clip_grad_norm([g], math.nan))):
+        with pytest.raises(llc.LlcError) as e:
+            bad()
+        assert e.value.code == code
