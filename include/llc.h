@@ -454,7 +454,8 @@ typedef struct llc_token_logprobs_grad_args {
 /* Arguments of llc_embed: out[t,:] = scale * table[tokens[t],:], rounded once to the output's type;
  * zeros for a token outside [0, N). */
 typedef struct llc_embed_args {
-  int64_t T, N, D;          /* T in 0..2^31 - 5, N, D in 1..2^31 - 5                     */
+  int64_t T, N, D;          /* T in 0..2^31 - 5, N, D in 1..2^31 - 5; LLC_E_SHAPE also where a launch would
+                               need more than 2^24 - 1 workgroups (a wavefront takes 4 KB of a row) */
   int32_t dtype, out_dtype; /* of table and of out: LLC_F32 | LLC_BF16                   */
   const void *table;        /* device [N,D] */
   int64_t table_stride_n;

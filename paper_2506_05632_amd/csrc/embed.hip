@@ -1,8 +1,28 @@
-// Embedding lookup with scaling, and its gradient.  One workgroup a token, or a row of the gradient.
+// Embedding lookup with scaling, and its gradient by sorted tokens.  Both move rows and compute next to nothing: memory
+// bounds them.
+//
+// Gradient: grad[n] = scale * sum over t with tokens[t] == n of g[t].  Floating-point atomics would make the sums' order,
+// and so their bits, a matter of timing; instead the positions are sorted by token first (a stable counting sort), and a row of the
+// gradient is one wavefront's, or several wavefronts' by columns, which adds its tokens' rows up in registers in the order of their positions, in fp32, and
+// writes it once.  Rows that no token names are written as zeros by the same launch.
+// Tokens as in text name a few rows very often: a row of more than kWindow tokens is added up by windows of kWindow
+// sorted positions, each a wavefront's, whose partial sums (fp32, in the workspace) a last launch joins.  A window touches at most
+// two such rows, the one it starts in and the one it ends in, so two partial rows a window are room enough, and a window's place
+// follows from its number: nothing is counted or handed out at run time.
 #include "ends.hpp"
 
 namespace llc {
 namespace {
+
+constexpr int kWindow = 32;       // sorted positions a wavefront adds up
+constexpr int kJoinThreads = 1024;
+constexpr int kMostRange = 896;   // rows of the table that a workgroup of the sort takes (its counters: 60 KB of LDS)
+constexpr long long kMostRows = 1LL << 27;
+
+// A sorted position: its number, the row it names, and where that row's places start and how many they are.
+struct alignas(16) Place {
+  int t, row, start, count;
+};
 
 struct EmbedParams {
   long long T, N, D;
@@ -14,42 +34,281 @@ struct EmbedParams {
   int add;
   void *to;                 // output, or the gradient of the table
   long long to_stride;
+  int team;                 // wavefronts that share a row's columns
+  // the gradient's
+  int range;                // rows a workgroup of the sort takes
+  Place *places;            // [T] the positions by token
+  int32_t *starts;          // [N + 1] where a row's places start
+  float *partial;           // [windows][2][D]
+  long long windows;
+  unsigned window_blocks, sum_blocks;  // of the summing launch: windows, then sorted positions, then rows without a token
 };
 
+// ---- lookup: a wavefront, or several by columns, a token
 template <typename A, typename B> __global__ void __launch_bounds__(kBlock) embed_kernel(const EmbedParams p) {
-  for (long long t = blockIdx.x; t < p.T; t += gridDim.x) {
-    const long long n = p.tokens[t * p.tok_stride];
-    B *to = reinterpret_cast<B *>(p.to) + t * p.to_stride;
-    const bool there = n >= 0 && n < p.N;
-    const A *from = reinterpret_cast<const A *>(p.from) + (there ? n : 0) * p.from_stride;
-    for (long long d = threadIdx.x; d < p.D; d += kBlock) to[d] = narrow<B>(there ? widen(from[d]) * p.scale : 0.0f);
+  constexpr int N = kWide<A>;
+  const long long wave = (long long)blockIdx.x * (kBlock / 64) + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const long long t = wave / p.team;
+  if (t >= p.T) return;
+  const long long n = p.tokens[t * p.tok_stride];
+  const bool there = n >= 0 && n < p.N;
+  const A *from = reinterpret_cast<const A *>(p.from) + (there ? n : 0) * p.from_stride;
+  B *to = reinterpret_cast<B *>(p.to) + t * p.to_stride;
+  for (long long d = (wave % p.team * 64 + (threadIdx.x & 63)) * N; d < p.D; d += (long long)p.team * 64 * N) {
+    float v[N] = {};
+    if (there) load_first<N>(from + d, p.D - d, v);
+#pragma unroll
+    for (int i = 0; i < N; ++i) v[i] *= p.scale;
+    if (!there) {
+#pragma unroll
+      for (int i = 0; i < N; ++i) v[i] = 0.0f;  // (not -0)
+    }
+    store_first<N>(to + d, p.D - d, v);
   }
 }
 
-template <typename A, typename B> __global__ void __launch_bounds__(kBlock) embed_grad_kernel(const EmbedParams p) {
-  __shared__ int s_any;
-  __shared__ uint8_t s_hit[kBlock];
-  for (long long item = blockIdx.x, slabs = (p.D + kBlock - 1) / kBlock; item < p.N * slabs; item += gridDim.x) {
-    const long long n = item / slabs, d0 = item % slabs * kBlock;
-    B *to = reinterpret_cast<B *>(p.to) + n * p.to_stride;
-    const long long d = d0 + threadIdx.x;
-    float sum = 0.0f;
-    bool met = false;
-    for (long long t0 = 0; t0 < p.T; t0 += kBlock) {
-      const long long mine = t0 + threadIdx.x;
-      __syncthreads();
-      if (threadIdx.x == 0) s_any = 0;
-      __syncthreads();
-      const bool hit = mine < p.T && p.tokens[mine * p.tok_stride] == n;
-      s_hit[threadIdx.x] = hit ? 1 : 0;
-      if (hit) s_any = 1;
-      __syncthreads();
-      if (s_any == 0) continue;
-      met = true;
-      for (int j = 0; j < kBlock; ++j)
-        if (s_hit[j] != 0 && d < p.D) sum += widen(reinterpret_cast<const A *>(p.from)[(t0 + j) * p.from_stride + d]);
+// ---- the sort: a workgroup takes a range of rows, reads all tokens twice (they lie in the caches) and needs
+// nothing from the other workgroups: where its rows start follows from how many tokens name a row below.
+__device__ __forceinline__ int add_over_wave(int v) {
+#pragma unroll
+  for (int d = 32; d >= 1; d >>= 1) v += __shfl_xor(v, d);
+  return v;
+}
+
+constexpr int kSortAhead = 16;  // groups of 64 tokens that are fetched together
+__device__ __forceinline__ void load_ids(const EmbedParams &p, long long t, long long until, unsigned (&id)[kSortAhead]) {
+#pragma unroll
+  for (int u = 0; u < kSortAhead; ++u) id[u] = t + u * 64 < until ? (unsigned)p.tokens[(t + u * 64) * p.tok_stride] : 0xFFFFFFFFu;
+}
+
+template <int WAVES> __global__ void __launch_bounds__(WAVES * 64) embed_sort_kernel(const EmbedParams p) {
+  extern __shared__ int counts[];  // [WAVES][range], then where the rows' places start, [range + 1]
+  __shared__ int s_wave[WAVES];
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), range = p.range;
+  int *begins = counts + WAVES * range;
+  const long long low = (long long)blockIdx.x * range;
+  const int rows = (int)(p.N - low < range ? p.N - low : range);
+  // a wavefront takes consecutive positions, so that the order of the positions is kept
+  const long long share = ((p.T + WAVES - 1) / WAVES + 63) & ~63LL;
+  const long long from = wave * share, until = from + share < p.T ? from + share : p.T;
+  unsigned id[kSortAhead];
+  load_ids(p, from + lane, until, id);
+  for (int i = tid; i < WAVES * range; i += WAVES * 64) counts[i] = 0;
+  __syncthreads();
+  int *mine = counts + wave * range;
+  int below = 0;
+  for (long long t0 = from; t0 < until; t0 += 64 * kSortAhead) {
+    if (t0 != from) load_ids(p, t0 + lane, until, id);
+#pragma unroll
+    for (int u = 0; u < kSortAhead; ++u) {
+      below += id[u] < (unsigned long long)low ? 1 : 0;
+      if (id[u] - (unsigned)low < (unsigned)rows) atomicAdd(&mine[id[u] - (unsigned)low], 1);
     }
-    if (d < p.D && (met || p.add == 0)) to[d] = narrow<B>((p.add != 0 ? widen(to[d]) : 0.0f) + sum * p.scale);
+  }
+  below = add_over_wave(below);
+  if (lane == 0) s_wave[wave] = below;
+  __syncthreads();
+  int base = 0;
+  for (int w = 0; w < WAVES; ++w) base += s_wave[w];
+  // a thread takes a row at a time: its tokens, and how many come before it
+  for (int r0 = 0; r0 < rows; r0 += WAVES * 64) {
+    const int r = r0 + tid;
+    int total = 0;
+    if (r < rows)
+      for (int w = 0; w < WAVES; ++w) total += counts[w * range + r];
+    int upto = total;
+#pragma unroll
+    for (int d = 1; d < 64; d <<= 1) {
+      const int o = __shfl_up(upto, d);
+      if (lane >= d) upto += o;
+    }
+    __syncthreads();
+    if (lane == 63) s_wave[wave] = upto;
+    __syncthreads();
+    int at = base + upto - total;
+    for (int w = 0; w < WAVES; ++w) {
+      at += w < wave ? s_wave[w] : 0;
+      base += s_wave[w];
+    }
+    if (r < rows) {
+      p.starts[low + r] = at;
+      begins[r] = at;
+      for (int w = 0; w < WAVES; ++w) {
+        const int n = counts[w * range + r];
+        counts[w * range + r] = at;
+        at += n;
+      }
+    }
+  }
+  if (tid == 0) {
+    begins[rows] = base;
+    if (low + rows == p.N) p.starts[p.N] = base;
+  }
+  __syncthreads();
+  for (long long t0 = from; t0 < until; t0 += 64 * kSortAhead) {
+    if (share > 64 * kSortAhead) load_ids(p, t0 + lane, until, id);  // (else they are still there)
+#pragma unroll
+    for (int u = 0; u < kSortAhead; ++u) {
+      const unsigned at_row = id[u] - (unsigned)low;
+      unsigned long long left = __ballot(at_row < (unsigned)rows);
+      while (left != 0) {  // (uniform; one round for every row that the 64 tokens name)
+        const unsigned row = __builtin_amdgcn_readlane(at_row, __builtin_ctzll(left));
+        const unsigned long long same = __ballot(at_row == row);
+        const int first = mine[row], begin = begins[row];  // (the first is this wavefront's own counter)
+        if (at_row == row)
+          p.places[first + (int)__builtin_popcountll(same & ((1ull << lane) - 1))] =
+              Place{(int)(t0 + u * 64 + lane), (int)(low + row), begin, begins[row + 1] - begin};
+        mine[row] = first + (int)__builtin_popcountll(same);  // (by every lane: each has read it itself)
+        left &= ~same;
+      }
+    }
+  }
+}
+
+// ---- sums
+// The rows of g at places [from, from + n), n at most 64, N columns from d on, in the order of the positions.
+// `t`: lane i holds place from + i's position.
+template <typename A, int N>
+__device__ __forceinline__ void add_positions(const EmbedParams &p, int t, int n, long long d, float (&sum)[N]) {
+  const A *g = reinterpret_cast<const A *>(p.from) + d;
+  const long long left = p.D - d;
+  int j = 0;
+  for (; j + 4 <= n; j += 4) {
+    float v[4][N];
+#pragma unroll
+    for (int u = 0; u < 4; ++u) load_first<N>(g + (long long)__builtin_amdgcn_readlane(t, j + u) * p.from_stride, left, v[u]);
+#pragma unroll
+    for (int u = 0; u < 4; ++u)
+#pragma unroll
+      for (int i = 0; i < N; ++i) sum[i] += v[u][i];
+  }
+  for (; j < n; ++j) {
+    float v[N];
+    load_first<N>(g + (long long)__builtin_amdgcn_readlane(t, j) * p.from_stride, left, v);
+#pragma unroll
+    for (int i = 0; i < N; ++i) sum[i] += v[i];
+  }
+}
+
+template <typename B, int N>
+__device__ __forceinline__ void write_row(const EmbedParams &p, long long row, long long d, float (&sum)[N]) {
+  B *to = reinterpret_cast<B *>(p.to) + row * p.to_stride + d;
+  float before[N] = {};
+  if (p.add != 0) load_first<N>(to, p.D - d, before);
+#pragma unroll
+  for (int i = 0; i < N; ++i) sum[i] = p.add != 0 ? fmaf(sum[i], p.scale, before[i]) : sum[i] * p.scale;
+  stream_first<N>(to, p.D - d, sum);
+}
+
+template <typename A, typename B> __global__ void __launch_bounds__(kBlock) embed_sum_kernel(const EmbedParams p) {
+  constexpr int N = kWide<A>;
+  const int in_block = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
+  const long long wave = (long long)blockIdx.x * (kBlock / 64) + in_block, step = (long long)p.team * 64 * N;
+  const long long item = wave / p.team, d0 = (wave % p.team * 64 + lane) * N;
+  const long long windows = (long long)p.window_blocks * (kBlock / 64) / p.team, sums = (long long)p.sum_blocks * (kBlock / 64) / p.team;
+  if (blockIdx.x < p.window_blocks) {
+    const long long begin = item * kWindow;
+    if (begin >= p.T) return;
+    const int total = p.starts[p.N];
+    const int room = (int)(p.T - begin < kWindow ? p.T - begin : kWindow);
+    const Place mine = p.places[begin + (lane < room ? lane : room - 1)];  // (not written from place `total` on)
+    if (begin >= total) return;
+    const int n = total - begin < room ? (int)(total - begin) : room;  // the window's places
+    const int a_end = __builtin_amdgcn_readlane(mine.start, 0) + __builtin_amdgcn_readlane(mine.count, 0);
+    const int b_begin = __builtin_amdgcn_readlane(mine.start, n - 1);
+    const bool a_long = __builtin_amdgcn_readlane(mine.count, 0) > kWindow;
+    const bool b_long = b_begin > begin && __builtin_amdgcn_readlane(mine.count, n - 1) > kWindow;
+    for (int slot = 0; slot < 2; ++slot) {
+      if (slot == 0 ? !a_long : !b_long) continue;
+      float *to = p.partial + (item * 2 + slot) * p.D;
+      const int skip = slot == 0 ? 0 : (int)(b_begin - begin), upto = slot == 0 && a_end - begin < n ? (int)(a_end - begin) : n;
+      const int t = __shfl(mine.t, lane + skip);
+      for (long long d = d0; d < p.D; d += step) {
+        float sum[N] = {};
+        add_positions<A, N>(p, t, upto - skip, d, sum);
+        store_first<N>(to + d, p.D - d, sum);
+      }
+    }
+    return;
+  }
+  if (blockIdx.x < p.window_blocks + p.sum_blocks) {  // the places where a row starts
+    const int total = p.starts[p.N];
+    for (long long n = item - windows; n < p.T; n += sums) {
+      const long long at = n + lane < p.T ? n + lane : p.T - 1;
+      const Place mine = p.places[at];
+      if (n >= total) return;
+      const int count = __builtin_amdgcn_readfirstlane(mine.count);
+      if (__builtin_amdgcn_readfirstlane(mine.start) != n || count > kWindow) continue;
+      const int row = __builtin_amdgcn_readfirstlane(mine.row);
+      for (long long d = d0; d < p.D; d += step) {
+        float sum[N] = {};
+        add_positions<A, N>(p, mine.t, count, d, sum);
+        write_row<B, N>(p, row, d, sum);
+      }
+    }
+    return;
+  }
+  // the rows without a token, last: their stores keep the memory busy by themselves (between the others: 276 us for 229)
+  const long long zeros = (long long)(gridDim.x - p.window_blocks - p.sum_blocks) * (kBlock / 64) / p.team;
+  for (long long row = item - windows - sums; row < p.N; row += zeros) {
+    if (p.starts[row] != p.starts[row + 1]) continue;
+    const float none[N] = {};
+    for (long long d = d0; d < p.D; d += step) stream_first<N>(reinterpret_cast<B *>(p.to) + row * p.to_stride + d, p.D - d, none);
+  }
+}
+
+// Joins the windows of long rows.  A wavefront looks whether a long row starts in its window; the workgroup then takes such
+// rows one after the other, 256 columns of them, every sixteenth window a wavefront, in an order that follows from the row's place alone.
+template <typename B> __global__ void __launch_bounds__(kJoinThreads) embed_join_kernel(const EmbedParams p) {
+  constexpr int N = 4, kWaves = kJoinThreads / 64, kAhead = 8;
+  __shared__ float s_sum[kWaves][64 * N];
+  __shared__ int s_row[kWaves];
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  {
+    const long long begin = ((long long)blockIdx.x * kWaves + wave) * kWindow;
+    int row = -1;
+    if (begin < p.T) {
+      const int total = p.starts[p.N];
+      const int until = p.T - begin < kWindow ? (int)p.T : (int)begin + kWindow;
+      Place last = p.places[until - 1];
+      if (total < until && total > begin) last = p.places[total - 1];  // (places are written up to `total`)
+      if (total > begin && last.start >= begin && last.count > kWindow) row = last.row;
+    }
+    s_row[wave] = row;
+  }
+  __syncthreads();
+  for (int i = 0; i < kWaves; ++i) {
+    const int row = s_row[i];
+    if (row < 0) continue;  // (uniform)
+    const long long w = (long long)blockIdx.x * kWaves + i, last = (p.starts[row + 1] - 1) / kWindow;
+    const bool inside = p.starts[row] != w * kWindow;  // (of its first window: then the second of the two partial rows)
+    for (long long d0 = (long long)blockIdx.y * 64 * N; d0 < p.D; d0 += (long long)gridDim.y * 64 * N) {
+      const long long d = d0 + lane * N;
+      float sum[N] = {};
+      if (d < p.D)
+        for (long long v = w + wave; v <= last; v += kWaves * kAhead) {
+          float part[kAhead][N] = {};
+#pragma unroll
+          for (int u = 0; u < kAhead; ++u) {
+            const long long at = v + u * kWaves;
+            if (at <= last) load_first<N>(p.partial + (at * 2 + (at == w && inside ? 1 : 0)) * p.D + d, p.D - d, part[u]);
+          }
+#pragma unroll
+          for (int u = 0; u < kAhead; ++u)
+#pragma unroll
+            for (int j = 0; j < N; ++j) sum[j] += part[u][j];
+        }
+      __syncthreads();
+#pragma unroll
+      for (int j = 0; j < N; ++j) s_sum[wave][lane * N + j] = sum[j];
+      __syncthreads();
+      if (wave == 0 && d < p.D) {
+#pragma unroll
+        for (int j = 0; j < N; ++j)
+          for (int v = 1; v < kWaves; ++v) sum[j] += s_sum[v][lane * N + j];
+        write_row<B, N>(p, row, d, sum);
+      }
+    }
   }
 }
 
@@ -62,9 +321,28 @@ bool sizes_ok(long long T, long long N, long long D) {
   return T >= 0 && T <= kMaxIndex && N >= 1 && N <= kMaxIndex && D >= 1 && D <= kMaxIndex;
 }
 
-unsigned blocks(long long items) { return (unsigned)(items < (1 << 20) ? items : 1 << 20); }
+// Wavefronts that share a row: as many as have columns, up to a workgroup's four.
+int team_of(long long D, int from) {
+  const long long slabs = (D * (long long)type_size(from) + 1023) / 1024;
+  return slabs >= 4 ? 4 : slabs >= 2 ? 2 : 1;
+}
 
-constexpr long long kMostRows = 1LL << 27;
+struct GradLayout {
+  size_t places, starts, partial, total;
+};
+GradLayout grad_layout(long long T, long long N, long long D) {
+  const auto up = [](size_t n) { return (n + 255) & ~(size_t)255; };
+  GradLayout l;
+  size_t at = 0;
+  l.places = at; at += up((size_t)T * sizeof(Place));
+  l.starts = at; at += up((size_t)(N + 1) * 4);
+  l.partial = at; at += T > kWindow ? up((size_t)((T + kWindow - 1) / kWindow) * 2 * (size_t)D * 4) : 0;
+  l.total = at;
+  return l;
+}
+
+constexpr long long kMostBlocks = 0xFFFFFFFFLL / kBlock;  // of a launch
+constexpr long long kRowBlocks = 1LL << 22;  // of a launch's that take rows (they take several where there are more)
 
 }  // namespace
 }  // namespace llc
@@ -80,19 +358,25 @@ extern "C" int llc_embed(const llc_embed_args *a) {
   if (a->table_stride_n < 0 || a->tok_stride < 0 || a->out_stride_t < a->D) return LLC_E_SHAPE;
   if (!known_type(a->dtype) || !known_type(a->out_dtype)) return LLC_E_DTYPE;
   if (!fits(a->table, type_size(a->dtype)) || !fits(a->out, type_size(a->out_dtype)) || !fits(a->tokens, 4)) return LLC_E_ALIGN;
+  EmbedParams p = {};
+  p.T = a->T; p.N = a->N; p.D = a->D;
+  p.from = a->table; p.from_stride = a->table_stride_n; p.tokens = a->tokens; p.tok_stride = a->tok_stride;
+  p.scale = a->scale; p.to = a->out; p.to_stride = a->out_stride_t;
+  p.team = team_of(a->D, a->dtype);
+  const long long blocks = (a->T * p.team + kBlock / 64 - 1) / (kBlock / 64);
+  if (blocks > kMostBlocks) return LLC_E_SHAPE;
   if ((a->flags & LLC_FLAG_DRY_RUN) != 0) return LLC_OK;
-  EmbedParams p = {a->T, a->N, a->D, a->table, a->table_stride_n, a->tokens, a->tok_stride, a->scale, 0, a->out, a->out_stride_t};
   hipStream_t st = (hipStream_t)a->stream;
   return between_events(a->ev_begin, a->ev_end, st, [&] {
     return by_types(a->dtype, a->out_dtype, [&](auto from, auto to) {
-      embed_kernel<decltype(from), decltype(to)><<<blocks(p.T), kBlock, 0, st>>>(p);
+      embed_kernel<decltype(from), decltype(to)><<<(unsigned)blocks, kBlock, 0, st>>>(p);
       return hipGetLastError();
     });
   });
 }
 
 extern "C" size_t llc_embed_grad_workspace_size(int64_t T, int64_t N, int64_t D) {
-  return sizes_ok(T, N, D) && N <= kMostRows ? 256 : 0;
+  return sizes_ok(T, N, D) && N <= kMostRows ? grad_layout(T, N, D).total : 0;
 }
 
 extern "C" int llc_embed_grad(const llc_embed_grad_args *a) {
@@ -104,14 +388,45 @@ extern "C" int llc_embed_grad(const llc_embed_grad_args *a) {
   if (a->g_stride_t < 0 || a->tok_stride < 0 || a->grad_stride_n < a->D) return LLC_E_SHAPE;
   if (!known_type(a->dtype) || !known_type(a->grad_dtype)) return LLC_E_DTYPE;
   if (!fits(a->g, type_size(a->dtype)) || !fits(a->grad, type_size(a->grad_dtype)) || !fits(a->tokens, 4)) return LLC_E_ALIGN;
-  if (a->workspace == nullptr || !fits(a->workspace, 256) || a->workspace_bytes < llc_embed_grad_workspace_size(a->T, a->N, a->D))
-    return LLC_E_WORKSPACE;
+  const GradLayout l = grad_layout(a->T, a->N, a->D);
+  if (a->workspace == nullptr || !fits(a->workspace, 256) || a->workspace_bytes < l.total) return LLC_E_WORKSPACE;
+  EmbedParams p = {};
+  p.T = a->T; p.N = a->N; p.D = a->D;
+  p.from = a->g; p.from_stride = a->g_stride_t; p.tokens = a->tokens; p.tok_stride = a->tok_stride;
+  p.scale = a->scale; p.add = a->add; p.to = a->grad; p.to_stride = a->grad_stride_n;
+  p.team = team_of(a->D, a->dtype);
+  char *work = (char *)a->workspace;
+  p.places = (Place *)(work + l.places); p.starts = (int32_t *)(work + l.starts);
+  p.partial = (float *)(work + l.partial);
+  // (a workgroup of the sort on every CU, as long as its counters fit)
+  p.range = (int)((a->N + 255) / 256 < kMostRange ? (a->N + 255) / 256 : kMostRange);
+  const long long sort_blocks = (a->N + p.range - 1) / p.range;
+  p.windows = a->T > kWindow ? (a->T + kWindow - 1) / kWindow : 0;
+  const long long a_block = kBlock / 64, window_blocks = (p.windows * p.team + a_block - 1) / a_block;
+  const auto row_blocks = [&](long long rows) {
+    const long long blocks = (rows * p.team + a_block - 1) / a_block;
+    return blocks < kRowBlocks ? blocks : kRowBlocks;
+  };
+  const long long sum_blocks = row_blocks(a->T), zero_blocks = p.add != 0 ? 0 : row_blocks(a->N);
+  if (window_blocks > kMostBlocks - 2 * kRowBlocks) return LLC_E_SHAPE;
+  p.window_blocks = (unsigned)window_blocks; p.sum_blocks = (unsigned)sum_blocks;
   if ((a->flags & LLC_FLAG_DRY_RUN) != 0) return LLC_OK;
-  EmbedParams p = {a->T, a->N, a->D, a->g, a->g_stride_t, a->tokens, a->tok_stride, a->scale, a->add, a->grad, a->grad_stride_n};
   hipStream_t st = (hipStream_t)a->stream;
   return between_events(a->ev_begin, a->ev_end, st, [&] {
+    // (few tokens: four wavefronts take them in one go, and are sooner done than sixteen)
+    if (a->T <= 4 * 64 * kSortAhead)
+      embed_sort_kernel<4><<<(unsigned)sort_blocks, 256, ((size_t)4 * p.range + p.range + 1) * 4, st>>>(p);
+    else
+      embed_sort_kernel<16><<<(unsigned)sort_blocks, 1024, ((size_t)16 * p.range + p.range + 1) * 4, st>>>(p);
+    hipError_t e = hipGetLastError();
+    if (e != hipSuccess) return e;
     return by_types(a->dtype, a->grad_dtype, [&](auto from, auto to) {
-      embed_grad_kernel<decltype(from), decltype(to)><<<blocks(p.N * ((p.D + kBlock - 1) / kBlock)), kBlock, 0, st>>>(p);
+      embed_sum_kernel<decltype(from), decltype(to)><<<(unsigned)(window_blocks + sum_blocks + zero_blocks), kBlock, 0, st>>>(p);
+      e = hipGetLastError();
+      if (e != hipSuccess || p.windows == 0) return e;
+      const long long groups = (p.windows + kJoinThreads / 64 - 1) / (kJoinThreads / 64);
+      const long long slabs = (a->D + 255) / 256, most = kMostBlocks / 4 / groups, join = slabs < most ? slabs : most;
+      embed_join_kernel<decltype(to)><<<dim3((unsigned)groups, (unsigned)(join < 1 ? 1 : join < 64 ? join : 64)), kJoinThreads, 0, st>>>(p);
       return hipGetLastError();
     });
   });
