@@ -15,6 +15,7 @@ namespace llc {
 namespace {
 
 constexpr int kWindow = 32;       // sorted positions a wavefront adds up
+constexpr int kAhead = 4;         // rows that are fetched together (8 take the registers of three wavefronts a SIMD: 65 536 tokens 402 us for 338)
 constexpr int kJoinThreads = 1024;
 constexpr int kMostRange = 896;   // rows of the table that a workgroup of the sort takes (its counters: 60 KB of LDS)
 constexpr long long kMostRows = 1LL << 27;
@@ -34,27 +35,27 @@ struct EmbedParams {
   int add;
   void *to;                 // output, or the gradient of the table
   long long to_stride;
-  int team;                 // wavefronts that share a row's columns
+  int team_log;             // log2 of the wavefronts that share a row's columns (divisions would take longer than a short row)
   // the gradient's
   int range;                // rows a workgroup of the sort takes
   Place *places;            // [T] the positions by token
   int32_t *starts;          // [N + 1] where a row's places start
   float *partial;           // [windows][2][D]
   long long windows;
-  unsigned window_blocks, sum_blocks;  // of the summing launch: windows, then sorted positions, then rows without a token
+  unsigned window_blocks, sum_blocks;  // of the summing launch: windows, then sorted positions
 };
 
 // ---- lookup: a wavefront, or several by columns, a token
 template <typename A, typename B> __global__ void __launch_bounds__(kBlock) embed_kernel(const EmbedParams p) {
   constexpr int N = kWide<A>;
   const long long wave = (long long)blockIdx.x * (kBlock / 64) + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const long long t = wave / p.team;
+  const long long t = wave >> p.team_log;
   if (t >= p.T) return;
   const long long n = p.tokens[t * p.tok_stride];
   const bool there = n >= 0 && n < p.N;
   const A *from = reinterpret_cast<const A *>(p.from) + (there ? n : 0) * p.from_stride;
   B *to = reinterpret_cast<B *>(p.to) + t * p.to_stride;
-  for (long long d = (wave % p.team * 64 + (threadIdx.x & 63)) * N; d < p.D; d += (long long)p.team * 64 * N) {
+  for (long long d = ((wave & ((1 << p.team_log) - 1)) * 64 + (threadIdx.x & 63)) * N; d < p.D; d += 64LL * N << p.team_log) {
     float v[N] = {};
     if (there) load_first<N>(from + d, p.D - d, v);
 #pragma unroll
@@ -166,35 +167,47 @@ template <int WAVES> __global__ void __launch_bounds__(WAVES * 64) embed_sort_ke
 }
 
 // ---- sums
+// The next K of the places whose positions lane i of t holds.  (ALL: the N columns are there.  The choice is made once, outside: made at
+// every load it would make each wait for the one before.)
+template <bool ALL, int K, typename A, int N>
+__device__ __forceinline__ void add_some(const EmbedParams &p, const A *g, long long left, int t, int &j, float (&sum)[N]) {
+  float v[K][N];
+#pragma unroll
+  for (int u = 0; u < K; ++u) {
+    const A *from = g + (long long)__builtin_amdgcn_readlane(t, j + u) * p.from_stride;
+    if (ALL) load_some<N>(from, v[u]);
+    else load_first<N>(from, left, v[u]);
+  }
+#pragma unroll
+  for (int u = 0; u < K; ++u)
+#pragma unroll
+    for (int i = 0; i < N; ++i) sum[i] += v[u][i];
+  j += K;
+}
+template <bool ALL, typename A, int N>
+__device__ __forceinline__ void add_all(const EmbedParams &p, const A *g, long long left, int t, int n, float (&sum)[N]) {
+  int j = 0;
+  while (n - j >= kAhead) add_some<ALL, kAhead>(p, g, left, t, j, sum);
+  if (n - j >= 2) add_some<ALL, 2>(p, g, left, t, j, sum);
+  if (n - j >= 1) add_some<ALL, 1>(p, g, left, t, j, sum);
+}
+
 // The rows of g at places [from, from + n), n at most 64, N columns from d on, in the order of the positions.
 // `t`: lane i holds place from + i's position.
 template <typename A, int N>
 __device__ __forceinline__ void add_positions(const EmbedParams &p, int t, int n, long long d, float (&sum)[N]) {
   const A *g = reinterpret_cast<const A *>(p.from) + d;
-  const long long left = p.D - d;
-  int j = 0;
-  for (; j + 4 <= n; j += 4) {
-    float v[4][N];
-#pragma unroll
-    for (int u = 0; u < 4; ++u) load_first<N>(g + (long long)__builtin_amdgcn_readlane(t, j + u) * p.from_stride, left, v[u]);
-#pragma unroll
-    for (int u = 0; u < 4; ++u)
-#pragma unroll
-      for (int i = 0; i < N; ++i) sum[i] += v[u][i];
-  }
-  for (; j < n; ++j) {
-    float v[N];
-    load_first<N>(g + (long long)__builtin_amdgcn_readlane(t, j) * p.from_stride, left, v);
-#pragma unroll
-    for (int i = 0; i < N; ++i) sum[i] += v[i];
-  }
+  if (p.D - d >= N) add_all<true>(p, g, p.D - d, t, n, sum);
+  else add_all<false>(p, g, p.D - d, t, n, sum);
 }
 
 template <typename B, int N>
-__device__ __forceinline__ void write_row(const EmbedParams &p, long long row, long long d, float (&sum)[N]) {
+__device__ __forceinline__ void read_row(const EmbedParams &p, long long row, long long d, float (&before)[N]) {
+  if (p.add != 0) load_first<N>(reinterpret_cast<const B *>(p.to) + row * p.to_stride + d, p.D - d, before);
+}
+template <typename B, int N>
+__device__ __forceinline__ void write_row(const EmbedParams &p, long long row, long long d, const float (&before)[N], float (&sum)[N]) {
   B *to = reinterpret_cast<B *>(p.to) + row * p.to_stride + d;
-  float before[N] = {};
-  if (p.add != 0) load_first<N>(to, p.D - d, before);
 #pragma unroll
   for (int i = 0; i < N; ++i) sum[i] = p.add != 0 ? fmaf(sum[i], p.scale, before[i]) : sum[i] * p.scale;
   stream_first<N>(to, p.D - d, sum);
@@ -203,9 +216,10 @@ __device__ __forceinline__ void write_row(const EmbedParams &p, long long row, l
 template <typename A, typename B> __global__ void __launch_bounds__(kBlock) embed_sum_kernel(const EmbedParams p) {
   constexpr int N = kWide<A>;
   const int in_block = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
-  const long long wave = (long long)blockIdx.x * (kBlock / 64) + in_block, step = (long long)p.team * 64 * N;
-  const long long item = wave / p.team, d0 = (wave % p.team * 64 + lane) * N;
-  const long long windows = (long long)p.window_blocks * (kBlock / 64) / p.team, sums = (long long)p.sum_blocks * (kBlock / 64) / p.team;
+  const long long wave = (long long)blockIdx.x * (kBlock / 64) + in_block, step = 64LL * N << p.team_log;
+  const long long item = wave >> p.team_log, d0 = ((wave & ((1 << p.team_log) - 1)) * 64 + lane) * N;
+  const long long windows = (long long)p.window_blocks * (kBlock / 64) >> p.team_log,
+                  sums = (long long)p.sum_blocks * (kBlock / 64) >> p.team_log;
   if (blockIdx.x < p.window_blocks) {
     const long long begin = item * kWindow;
     if (begin >= p.T) return;
@@ -231,60 +245,68 @@ template <typename A, typename B> __global__ void __launch_bounds__(kBlock) embe
     }
     return;
   }
-  if (blockIdx.x < p.window_blocks + p.sum_blocks) {  // the places where a row starts
-    const int total = p.starts[p.N];
-    for (long long n = item - windows; n < p.T; n += sums) {
-      const long long at = n + lane < p.T ? n + lane : p.T - 1;
-      const Place mine = p.places[at];
-      if (n >= total) return;
-      const int count = __builtin_amdgcn_readfirstlane(mine.count);
-      if (__builtin_amdgcn_readfirstlane(mine.start) != n || count > kWindow) continue;
-      const int row = __builtin_amdgcn_readfirstlane(mine.row);
-      for (long long d = d0; d < p.D; d += step) {
-        float sum[N] = {};
-        add_positions<A, N>(p, mine.t, count, d, sum);
-        write_row<B, N>(p, row, d, sum);
-      }
+  // the places where a row starts
+  const int total = p.starts[p.N];
+  for (long long n = item - windows; n < p.T; n += sums) {
+    const long long at = n + lane < p.T ? n + lane : p.T - 1;
+    const Place mine = p.places[at];
+    if (n >= total) return;
+    const int count = __builtin_amdgcn_readfirstlane(mine.count);
+    if (__builtin_amdgcn_readfirstlane(mine.start) != n || count > kWindow) continue;
+    const int row = __builtin_amdgcn_readfirstlane(mine.row);
+    for (long long d = d0; d < p.D; d += step) {
+      float sum[N] = {}, before[N] = {};
+      read_row<B, N>(p, row, d, before);
+      add_positions<A, N>(p, mine.t, count, d, sum);
+      write_row<B, N>(p, row, d, before, sum);
     }
-    return;
-  }
-  // the rows without a token, last: their stores keep the memory busy by themselves (between the others: 276 us for 229)
-  const long long zeros = (long long)(gridDim.x - p.window_blocks - p.sum_blocks) * (kBlock / 64) / p.team;
-  for (long long row = item - windows - sums; row < p.N; row += zeros) {
-    if (p.starts[row] != p.starts[row + 1]) continue;
-    const float none[N] = {};
-    for (long long d = d0; d < p.D; d += step) stream_first<N>(reinterpret_cast<B *>(p.to) + row * p.to_stride + d, p.D - d, none);
   }
 }
+
+// The rows without a token: 4 KB a workgroup, one store a thread, in a launch of its own with next to nothing to set up.  Memory takes such a stream best
+// (0.95 GB: 149 us, 6.4 TB/s; two stores a thread 166 to 190, 64 rows a workgroup 206; in the summing launch, whose wavefronts carry more
+// registers, 208).
+constexpr int kZeroRows = 32768;
+template <typename B>
+__global__ void __launch_bounds__(kBlock) embed_zero_kernel(const int32_t *starts, B *to, long long to_stride, long long D, long long row0, long long N) {
+  constexpr int kStore = kWide<B>;
+  const long long row = row0 + (long long)blockIdx.z * kZeroRows + blockIdx.y;
+  if (row >= N || starts[row] != starts[row + 1]) return;
+  const long long d = ((long long)blockIdx.x * kBlock + threadIdx.x) * kStore;
+  const float none[kStore] = {};
+  if (d < D) stream_first<kStore>(to + row * to_stride + d, D - d, none);
+}
+
 
 // Joins the windows of long rows.  A wavefront looks whether a long row starts in its window; the workgroup then takes such
 // rows one after the other, 256 columns of them, every sixteenth window a wavefront, in an order that follows from the row's place alone.
 template <typename B> __global__ void __launch_bounds__(kJoinThreads) embed_join_kernel(const EmbedParams p) {
-  constexpr int N = 4, kWaves = kJoinThreads / 64, kAhead = 8;
+  constexpr int N = 4, kWaves = kJoinThreads / 64;
   __shared__ float s_sum[kWaves][64 * N];
-  __shared__ int s_row[kWaves];
+  __shared__ Place s_row[kWaves];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   {
     const long long begin = ((long long)blockIdx.x * kWaves + wave) * kWindow;
-    int row = -1;
+    Place row = {0, -1, 0, 0};
     if (begin < p.T) {
       const int total = p.starts[p.N];
       const int until = p.T - begin < kWindow ? (int)p.T : (int)begin + kWindow;
       Place last = p.places[until - 1];
       if (total < until && total > begin) last = p.places[total - 1];  // (places are written up to `total`)
-      if (total > begin && last.start >= begin && last.count > kWindow) row = last.row;
+      if (total > begin && last.start >= begin && last.count > kWindow) row = last;
     }
     s_row[wave] = row;
   }
   __syncthreads();
   for (int i = 0; i < kWaves; ++i) {
-    const int row = s_row[i];
+    const int row = s_row[i].row;
     if (row < 0) continue;  // (uniform)
-    const long long w = (long long)blockIdx.x * kWaves + i, last = (p.starts[row + 1] - 1) / kWindow;
-    const bool inside = p.starts[row] != w * kWindow;  // (of its first window: then the second of the two partial rows)
+    const long long w = (long long)blockIdx.x * kWaves + i, last = ((long long)s_row[i].start + s_row[i].count - 1) / kWindow;
+    const bool inside = s_row[i].start != w * kWindow;  // (of its first window: then the second of the two partial rows)
     for (long long d0 = (long long)blockIdx.y * 64 * N; d0 < p.D; d0 += (long long)gridDim.y * 64 * N) {
       const long long d = d0 + lane * N;
-      float sum[N] = {};
+      float sum[N] = {}, before[N] = {};
+      if (wave == 0 && d < p.D) read_row<B, N>(p, row, d, before);
       if (d < p.D)
         for (long long v = w + wave; v <= last; v += kWaves * kAhead) {
           float part[kAhead][N] = {};
@@ -306,7 +328,7 @@ template <typename B> __global__ void __launch_bounds__(kJoinThreads) embed_join
 #pragma unroll
         for (int j = 0; j < N; ++j)
           for (int v = 1; v < kWaves; ++v) sum[j] += s_sum[v][lane * N + j];
-        write_row<B, N>(p, row, d, sum);
+        write_row<B, N>(p, row, d, before, sum);
       }
     }
   }
@@ -321,10 +343,10 @@ bool sizes_ok(long long T, long long N, long long D) {
   return T >= 0 && T <= kMaxIndex && N >= 1 && N <= kMaxIndex && D >= 1 && D <= kMaxIndex;
 }
 
-// Wavefronts that share a row: as many as have columns, up to a workgroup's four.
-int team_of(long long D, int from) {
+// log2 of the wavefronts that share a row: as many as have columns, up to a workgroup's four.
+int team_log_of(long long D, int from) {
   const long long slabs = (D * (long long)type_size(from) + 1023) / 1024;
-  return slabs >= 4 ? 4 : slabs >= 2 ? 2 : 1;
+  return slabs >= 4 ? 2 : slabs >= 2 ? 1 : 0;
 }
 
 struct GradLayout {
@@ -362,8 +384,8 @@ extern "C" int llc_embed(const llc_embed_args *a) {
   p.T = a->T; p.N = a->N; p.D = a->D;
   p.from = a->table; p.from_stride = a->table_stride_n; p.tokens = a->tokens; p.tok_stride = a->tok_stride;
   p.scale = a->scale; p.to = a->out; p.to_stride = a->out_stride_t;
-  p.team = team_of(a->D, a->dtype);
-  const long long blocks = (a->T * p.team + kBlock / 64 - 1) / (kBlock / 64);
+  p.team_log = team_log_of(a->D, a->dtype);
+  const long long blocks = ((a->T << p.team_log) + kBlock / 64 - 1) / (kBlock / 64);
   if (blocks > kMostBlocks) return LLC_E_SHAPE;
   if ((a->flags & LLC_FLAG_DRY_RUN) != 0) return LLC_OK;
   hipStream_t st = (hipStream_t)a->stream;
@@ -394,7 +416,7 @@ extern "C" int llc_embed_grad(const llc_embed_grad_args *a) {
   p.T = a->T; p.N = a->N; p.D = a->D;
   p.from = a->g; p.from_stride = a->g_stride_t; p.tokens = a->tokens; p.tok_stride = a->tok_stride;
   p.scale = a->scale; p.add = a->add; p.to = a->grad; p.to_stride = a->grad_stride_n;
-  p.team = team_of(a->D, a->dtype);
+  p.team_log = team_log_of(a->D, a->dtype);
   char *work = (char *)a->workspace;
   p.places = (Place *)(work + l.places); p.starts = (int32_t *)(work + l.starts);
   p.partial = (float *)(work + l.partial);
@@ -402,13 +424,13 @@ extern "C" int llc_embed_grad(const llc_embed_grad_args *a) {
   p.range = (int)((a->N + 255) / 256 < kMostRange ? (a->N + 255) / 256 : kMostRange);
   const long long sort_blocks = (a->N + p.range - 1) / p.range;
   p.windows = a->T > kWindow ? (a->T + kWindow - 1) / kWindow : 0;
-  const long long a_block = kBlock / 64, window_blocks = (p.windows * p.team + a_block - 1) / a_block;
+  const long long a_block = kBlock / 64, window_blocks = ((p.windows << p.team_log) + a_block - 1) / a_block;
   const auto row_blocks = [&](long long rows) {
-    const long long blocks = (rows * p.team + a_block - 1) / a_block;
+    const long long blocks = ((rows << p.team_log) + a_block - 1) / a_block;
     return blocks < kRowBlocks ? blocks : kRowBlocks;
   };
-  const long long sum_blocks = row_blocks(a->T), zero_blocks = p.add != 0 ? 0 : row_blocks(a->N);
-  if (window_blocks > kMostBlocks - 2 * kRowBlocks) return LLC_E_SHAPE;
+  const long long sum_blocks = row_blocks(a->T), chunks = (a->D * (long long)type_size(a->grad_dtype) + 4095) / 4096;
+  if (window_blocks > kMostBlocks - kRowBlocks) return LLC_E_SHAPE;
   p.window_blocks = (unsigned)window_blocks; p.sum_blocks = (unsigned)sum_blocks;
   if ((a->flags & LLC_FLAG_DRY_RUN) != 0) return LLC_OK;
   hipStream_t st = (hipStream_t)a->stream;
@@ -421,7 +443,16 @@ extern "C" int llc_embed_grad(const llc_embed_grad_args *a) {
     hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
     return by_types(a->dtype, a->grad_dtype, [&](auto from, auto to) {
-      embed_sum_kernel<decltype(from), decltype(to)><<<(unsigned)(window_blocks + sum_blocks + zero_blocks), kBlock, 0, st>>>(p);
+      using B = decltype(to);
+      const long long most_rows = kRowBlocks / chunks < 1 ? 1 : kRowBlocks / chunks;  // of a launch
+      for (long long row0 = 0; p.add == 0 && row0 < p.N && e == hipSuccess; row0 += most_rows) {
+        const long long rows = p.N - row0 < most_rows ? p.N - row0 : most_rows;
+        const dim3 grid((unsigned)chunks, (unsigned)(rows < kZeroRows ? rows : kZeroRows), (unsigned)((rows + kZeroRows - 1) / kZeroRows));
+        embed_zero_kernel<B><<<grid, kBlock, 0, st>>>(p.starts, (B *)p.to, p.to_stride, p.D, row0, row0 + rows);
+        e = hipGetLastError();
+      }
+      if (e != hipSuccess || p.T == 0) return e;
+      embed_sum_kernel<decltype(from), B><<<(unsigned)(window_blocks + sum_blocks), kBlock, 0, st>>>(p);
       e = hipGetLastError();
       if (e != hipSuccess || p.windows == 0) return e;
       const long long groups = (p.windows + kJoinThreads / 64 - 1) / (kJoinThreads / 64);
