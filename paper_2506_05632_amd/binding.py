@@ -7,6 +7,7 @@ missing, `load()` raises.
 import ctypes
 import importlib.util
 import os
+import struct
 import sysconfig
 from typing import Optional
 
@@ -230,11 +231,12 @@ class ClipGradNormArgs(ctypes.Structure):
 
 _lib = None
 _empties = None
+_tensor_list = None
 
 
 def load():
     """Load the HIP library (built by paper_2506_05632_amd/build.py); raise if it is not there."""
-    global _lib, _empties
+    global _lib, _empties, _tensor_list
     if _lib is None:
         path = LIB_PATH
         if not os.path.exists(path):
@@ -245,6 +247,7 @@ def load():
             module = importlib.util.module_from_spec(spec)
             spec.loader.exec_module(module)
             _empties = module.empties
+            _tensor_list = module.tensor_list
         lib = ctypes.CDLL(path)
         lib.llc_couple.argtypes = [ctypes.POINTER(CoupleArgs)]
         lib.llc_couple.restype = ctypes.c_int
@@ -969,6 +972,21 @@ def llc_embed_grad(g: torch.Tensor, tokens: torch.Tensor, N: int, *, scale: floa
     return {"grad": out}
 
 
+def _checked_list(grads, out):
+    """The pointers of both lists, the sizes and the types, as the library takes them."""
+    to = grads if out is None else out
+    if len(to) != len(grads):
+        raise ValueError("out must hold one tensor for each gradient")
+    for t, o in zip(grads, to):
+        if not t.is_cuda or t.device != grads[0].device or t.dtype not in _TYPES or not t.is_contiguous():
+            raise ValueError("gradients must be contiguous float32 or bfloat16 tensors of one device (there is no CPU path)")
+        if o is not t and (o.device != t.device or o.dtype != t.dtype or o.shape != t.shape or not o.is_contiguous()):
+            raise ValueError("out must have the gradients' sizes and types, contiguous, on their device")
+    n = len(grads)
+    return struct.pack(f"{n}Q{n}Q{n}q{n}i", *(t.data_ptr() for t in grads), *(o.data_ptr() for o in to), *(t.numel() for t in grads),
+                       *(_TYPES[t.dtype] for t in grads))
+
+
 def llc_clip_grad_norm(grads, max_norm: float, *, out=None, workspace: Optional[torch.Tensor] = None, flags: int = 0,
                        events=None) -> dict:
     """Scales gradients so that their common norm (the root of the sum of all squares) is at most max_norm.
@@ -979,28 +997,21 @@ def llc_clip_grad_norm(grads, max_norm: float, *, out=None, workspace: Optional[
     """
     lib = load()
     grads = list(grads)
+    if out is not None:
+        out = list(out)
     if not grads:
         raise ValueError("no gradients")
     n, dev = len(grads), grads[0].device
-    to = grads if out is None else list(out)
-    if len(to) != n:
-        raise ValueError("out must hold one tensor for each gradient")
-    pointers, outs, numel, dtype = (ctypes.c_void_p * n)(), (ctypes.c_void_p * n)(), (ctypes.c_int64 * n)(), (ctypes.c_int32 * n)()
-    for j in range(n):
-        t, o = grads[j], to[j]
-        if not t.is_cuda or t.device != dev or t.dtype not in _TYPES or not t.is_contiguous():
-            raise ValueError("gradients must be contiguous float32 or bfloat16 tensors of one device (there is no CPU path)")
-        if o is not t and (o.device != dev or o.dtype != t.dtype or o.shape != t.shape or not o.is_contiguous()):
-            raise ValueError("out must have the gradients' sizes and types, contiguous, on their device")
-        pointers[j], outs[j], numel[j], dtype[j] = t.data_ptr(), o.data_ptr(), t.numel(), _TYPES[t.dtype]
+    arrays = _tensor_list(grads, out) if _tensor_list is not None else None
+    arrays = arrays[0] if arrays is not None else _checked_list(grads, out)
     norm = torch.empty((), dtype=torch.float32, device=dev)
     if workspace is None:
         workspace = torch.empty(max(llc_clip_grad_norm_workspace_size(n), 256), dtype=torch.uint8, device=dev)
     a = ClipGradNormArgs()
-    a.n = n
-    a.grads, a.numel, a.dtype = (ctypes.cast(v, ctypes.c_void_p) for v in (pointers, numel, dtype))
+    at = ctypes.cast(arrays, ctypes.c_void_p).value  # (bytes that live as long as this call, which is as long as they are read)
+    a.n, a.grads, a.numel, a.dtype = n, at, at + 16 * n, at + 24 * n
     if out is not None:
-        a.out = ctypes.cast(outs, ctypes.c_void_p)
+        a.out = at + 8 * n
     a.max_norm, a.norm = max_norm, norm.data_ptr()
     a.workspace, a.workspace_bytes = workspace.data_ptr(), workspace.numel()
     a.stream = _stream_handle(dev)

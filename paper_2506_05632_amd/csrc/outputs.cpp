@@ -1,4 +1,4 @@
-// Output tensors of a call, made in one step: most of the binding's own time was torch.empty from Python, 1.3 us
+// What the binding does faster here than in Python.  Output tensors of a call, made in one step: most of the binding's own time was torch.empty from Python, 1.3 us
 // each, and a call returns up to seven with its workspace.  Candidate lists with keys, 1024 rows of 50, us a call: 15.5 from
 // Python, 13.3 with one tensor after the other made and wrapped, 11.0 with all made before any is wrapped.
 // They are what torch.empty gives: separate tensors from torch's allocator, through its dispatcher, with its errors, and
@@ -61,7 +61,41 @@ PyObject *empties(PyObject *, PyObject *const *args, Py_ssize_t n_args) {
   END_HANDLE_TH_ERRORS
 }
 
+// A list of gradients as llc_clip_grad_norm takes them, with the checks that the binding makes: a call on 21 small tensors 32 us with the list made in
+// Python, 11.4 so.
+// tensor_list(tensors, tensors or None) -> (bytes of n pointers, n pointers, n sizes (8 bytes each), n types (4), device index), or None
+// where a check fails (the binding then finds out which)
+PyObject *tensor_list(PyObject *, PyObject *const *args, Py_ssize_t n_args) {
+  HANDLE_TH_ERRORS
+  TORCH_CHECK_TYPE(n_args == 2 && PyList_Check(args[0]) && (args[1] == Py_None || PyList_Check(args[1])), "tensor_list: a list, and a list or None");
+  const bool same = args[1] == Py_None;
+  const Py_ssize_t n = PyList_GET_SIZE(args[0]);
+  if (n < 1 || (!same && PyList_GET_SIZE(args[1]) != n)) Py_RETURN_NONE;
+  THPObjectPtr out(PyBytes_FromStringAndSize(nullptr, n * 28));
+  if (!out) return nullptr;
+  int64_t *from = (int64_t *)PyBytes_AS_STRING(out.get()), *to = from + n, *sizes = to + n;
+  int32_t *types = (int32_t *)(sizes + n);
+  c10::DeviceIndex device = -1;
+  for (Py_ssize_t j = 0; j < n; ++j) {
+    PyObject *a = PyList_GET_ITEM(args[0], j), *b = same ? a : PyList_GET_ITEM(args[1], j);
+    if (!THPVariable_CheckExact(a) && !THPVariable_Check(a)) Py_RETURN_NONE;
+    if (b != a && !THPVariable_Check(b)) Py_RETURN_NONE;
+    const at::Tensor &t = THPVariable_Unpack(a), &o = THPVariable_Unpack(b);
+    const at::ScalarType type = t.scalar_type();
+    if (j == 0) device = t.get_device();
+    if (!t.is_cuda() || t.get_device() != device || (type != at::kFloat && type != at::kBFloat16) || !t.is_contiguous()) Py_RETURN_NONE;
+    if (b != a && (!o.is_cuda() || o.get_device() != device || o.scalar_type() != type || o.sizes() != t.sizes() || !o.is_contiguous())) Py_RETURN_NONE;
+    from[j] = (int64_t)t.data_ptr();
+    to[j] = (int64_t)o.data_ptr();
+    sizes[j] = t.numel();
+    types[j] = type == at::kFloat ? 0 : 1;
+  }
+  return Py_BuildValue("(Ni)", out.release(), (int)device);
+  END_HANDLE_TH_ERRORS
+}
+
 PyMethodDef methods[] = {
+    {"tensor_list", (PyCFunction)(void (*)())tensor_list, METH_FASTCALL, "pointers, sizes and types of gradients"},
     {"empties", (PyCFunction)(void (*)())empties, METH_FASTCALL, "uninitialised device tensors, one per (dtype, size, ...)"},
     {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_outputs", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};

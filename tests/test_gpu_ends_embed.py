@@ -204,6 +204,17 @@ def test_clip(sizes, dtypes):
         assert torch.equal(again["norm"], found["norm"]) and all(torch.equal(u, v) for u, v in zip(mine, clipped))
 
 
+def test_the_list_of_gradients_is_the_same_from_both_makers():
+    from paper_2506_05632_amd import binding
+    binding.load()
+    grads = _grads([5, 0, (300, 77), 1], (BF16, F32))
+    out = [torch.empty_like(t) for t in grads]
+    for to in (None, out):
+        assert binding._tensor_list(grads, to) == (binding._checked_list(grads, to), 0)
+    for bad in ((grads, out[:3]), (grads + [grads[2].t()], None), (grads, [t.double() for t in out]), (grads + [torch.ones(2)], None), ([1], None), ([], None)):
+        assert binding._tensor_list(*bad) is None
+
+
 def test_clip_views_at_any_element():
     flat = _grads([100000], (BF16,))[0]
     grads = [flat[1:4], flat[7:1000], flat[1001:50002], flat[50003:50003 + 2 * 99].view(2, 99), flat[60001:99999]]
