@@ -1,9 +1,37 @@
-// Scores of tokens: their log probability, the rows' entropy and top alternatives, and the gradient of the
-// first two.  One workgroup a row, one pass for the row's largest entry, one for the sums, one for each alternative.
+// Scores of tokens: their log probability, the rows' entropy and top alternatives, and the gradient of the first two.
+//
+// Forward.  With a reference m, c = log2(e) / T and d_i = (x_i - m) c, a row needs S = sum 2^d_i and D = sum d_i 2^d_i: ln p_t = (x_t - m) / T - ln S
+// and the entropy is ln S - ln 2 D / S.  One pass over the row forms both: a wavefront keeps its largest entry so far as its m, every lane its shares
+// of S and D in fp32, scaled over when m grows (which happens a dozen times a row); lanes, wavefronts and chunks are joined in fp64.
+// The same pass finds the top alternatives.  An entry is a candidate if it is above a bound that M entries of the row are known to reach: first the
+// smallest, over the wavefronts, of the ceil(M / wavefronts) largest of what their lanes' first entries are (each lane's largest of 16), so that a row of 128 256 leaves
+// a thousand candidates for fifty, and a tile of 16 entries a lane that has none costs one comparison a lane.  Candidates go to a list of the wavefront's in LDS as
+// whole numbers that order as (value, lower index first); a full list is cut to its M largest, which raises the wavefront's bound.  At the end a
+// histogram over the numbers' range finds a bound that at most kSelected of them reach, and those are ranked by comparing all with all.
+// What bounds it: reading the row (10 issue slots an entry, against 16 that fp32 logits at 6.3 TB/s leave).
 #include "ends.hpp"
 
 namespace llc {
 namespace {
+
+constexpr float kInf = __builtin_huge_valf();
+constexpr float kLog2e = 1.44269504088896340736f;
+constexpr double kLn2 = 0.693147180559945309417232121458;
+constexpr int kList = 256;      // candidates of a wavefront in LDS
+constexpr int kSelected = 256;  // candidates that are ranked
+constexpr int kBins = 1024;
+constexpr int kPer = 16;        // entries of a lane and tile
+constexpr int kMostSplit = 64;  // workgroups a row is split over
+
+typedef unsigned long long u64;
+
+// What a workgroup knows of a chunk of a row, when a row is split.
+struct Share {
+  double s, d;    // sum 2^((x - top) c), sum of (x - top) c 2^(...)
+  double unused;
+  float top;      // largest entry, -inf without mass
+  int count;      // keys in the list behind the shares
+};
 
 struct ScoreParams {
   long long R;
@@ -17,6 +45,9 @@ struct ScoreParams {
   double *lse;
   int32_t *top_ids;
   float *top_logp;
+  int chunks, chunk;  // workgroups a row is split over, entries of one
+  Share *shares;      // [R][chunks]
+  u64 *keys;          // [R][chunks][M]
   // the gradient
   const float *a;
   long long a_stride_r;
@@ -27,80 +58,349 @@ struct ScoreParams {
   long long grad_stride_r;
 };
 
-constexpr float kInf = __builtin_huge_valf();
-
 __device__ __forceinline__ bool with_mass(float v) { return fabsf(v) < kInf; }
-
-// The order of the values, larger first, then of the indexes, smaller first, as one number (0: no mass).
-__device__ __forceinline__ unsigned long long order_of(float v, int i) {
-  if (!with_mass(v)) return 0;
-  const uint32_t b = __float_as_uint(v + 0.0f);  // (-0 and 0 are equal)
-  const uint32_t o = (b & 0x80000000u) != 0 ? ~b : b | 0x80000000u;
-  return ((unsigned long long)o << 32) | (0xFFFFFFFFu - (uint32_t)i);
+__device__ __forceinline__ uint32_t ordered(float v) {  // larger for larger values; equal for 0 and -0
+  const uint32_t b = __float_as_uint(v + 0.0f);
+  return (b & 0x80000000u) != 0 ? ~b : b | 0x80000000u;
 }
+__device__ __forceinline__ float unordered(uint32_t o) { return __uint_as_float((o & 0x80000000u) != 0 ? o & 0x7FFFFFFFu : ~o); }
+__device__ __forceinline__ u64 key_of(float v, uint32_t i) { return ((u64)ordered(v) << 32) | (0xFFFFFFFFu - i); }
+__device__ __forceinline__ float key_value(u64 k) { return unordered((uint32_t)(k >> 32)); }
+__device__ __forceinline__ int key_index(u64 k) { return (int)(0xFFFFFFFFu - (uint32_t)k); }
 
-template <typename T, typename F> __device__ T over_workgroup(T v, F join, T *scratch) {
-  for (int d = 32; d >= 1; d >>= 1) v = join(v, __shfl_xor(v, d));
-  __syncthreads();
-  if ((threadIdx.x & 63) == 0) scratch[threadIdx.x >> 6] = v;
-  __syncthreads();
-  v = scratch[0];
-  for (int w = 1; w < (int)(blockDim.x >> 6); ++w) v = join(v, scratch[w]);
+__device__ __forceinline__ float wave_max(float v) {  // the same in every lane; no NaN among them
+#define LLC_STEP(CTRL, ROWS) \
+  v = fmaxf(v, __uint_as_float(__builtin_amdgcn_update_dpp(__float_as_uint(v), __float_as_uint(v), CTRL, ROWS, 0xF, false)))
+  LLC_STEP(0x111, 0xF); LLC_STEP(0x112, 0xF); LLC_STEP(0x114, 0xF); LLC_STEP(0x118, 0xF);  // row_shr 1, 2, 4, 8
+  LLC_STEP(0x142, 0xA); LLC_STEP(0x143, 0xC);                                              // row_bcast 15, 31
+#undef LLC_STEP
+  return __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(v), 63));
+}
+__device__ __forceinline__ double wave_sum(double v) {
+#pragma unroll
+  for (int d = 32; d >= 1; d >>= 1) v += __shfl_xor(v, d);
   return v;
 }
+__device__ __forceinline__ int lanes_below(u64 mask) {
+  return __builtin_amdgcn_mbcnt_hi((uint32_t)(mask >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)mask, 0));
+}
+__device__ __forceinline__ float max3(float a, float b, float c) {  // (NaN only if all are, or where one is a signalling one)
+  float r;
+  asm("v_max3_f32 %0, %1, %2, %3" : "=v"(r) : "v"(a), "v"(b), "v"(c));
+  return r;
+}
 
-template <typename E> __global__ void __launch_bounds__(kBlock) score_kernel(const ScoreParams p) {
-  __shared__ double s_double[kBlock / 64];
-  __shared__ unsigned long long s_order[kBlock / 64];
-  const long long r = blockIdx.x;
-  const E *x = reinterpret_cast<const E *>(p.x) + r * p.stride_r;
-  const double inv_t = 1.0 / (double)p.temp;
-  const auto larger = [](unsigned long long u, unsigned long long v) { return u > v ? u : v; };
-  const auto sum = [](double u, double v) { return u + v; };
-  unsigned long long best = 0;
-  for (int i = threadIdx.x; i < p.V; i += kBlock) best = larger(best, order_of(widen(x[i]), i));
-  best = over_workgroup(best, larger, s_order);
-  const bool any = best != 0;
-  const double top = any ? (double)widen(x[0xFFFFFFFFu - (uint32_t)best]) : 0.0;
-  double s = 0.0, d = 0.0;
-  for (int i = threadIdx.x; any && i < p.V; i += kBlock) {
-    const float v = widen(x[i]);
-    if (!with_mass(v)) continue;
-    const float y = (float)(((double)v - top) * inv_t), e = expf(y);
-    s += (double)e;
-    if (e > 0.0f) d += (double)e * (double)y;
+// kPer entries of a lane: 16 bytes at a time, 64 lanes side by side.  `left`: entries from the lane's first on; what lies beyond is -inf.
+template <typename E> __device__ __forceinline__ void load_tile(const E *x, long long left, float (&v)[kPer]) {
+  constexpr int N = kWide<E>;
+#pragma unroll
+  for (int u = 0; u < kPer / N; ++u) {
+    float w[N];
+    load_some<N>(x + u * 64 * N, w);
+#pragma unroll
+    for (int i = 0; i < N; ++i) v[u * N + i] = w[i];
   }
-  s = over_workgroup(s, sum, s_double);
-  d = over_workgroup(d, sum, s_double);
-  const double rest = any ? log(s) : -(double)kInf;
-  const double entropy = any ? rest - d / s : 0.0;
-  const auto logp_of = [&](float v) { return (float)(((double)v - top) * inv_t - rest); };
+}
+template <typename E> __device__ __forceinline__ void load_tile_end(const E *x, long long left, float (&v)[kPer]) {
+  constexpr int N = kWide<E>;
+#pragma unroll
+  for (int u = 0; u < kPer / N; ++u)
+#pragma unroll
+    for (int i = 0; i < N; ++i) v[u * N + i] = u * 64 * N + i < left ? widen(x[u * 64 * N + i]) : -kInf;
+}
+
+// A wavefront's sums and candidates.
+template <typename E> struct Scan {
+  float m = -kInf;      // largest entry so far
+  float s = 0.0f, d = 0.0f;
+  float bound = -kInf;  // candidates are above it
+  u64 least = 0;        // and have larger keys than this
+  int count = 0;        // of the list
+};
+
+// The list's M largest stay.
+__device__ __forceinline__ u64 cut_list(u64 *list, int &count, int M) {
+  const int lane = threadIdx.x & 63;
+  u64 k[kList / 64];
+#pragma unroll
+  for (int i = 0; i < kList / 64; ++i) k[i] = i * 64 + lane < count ? list[i * 64 + lane] : 0;
+  u64 t = 0;  // the M-th largest, bit by bit
+  for (int bit = 63; bit >= 0; --bit) {
+    const u64 with = t | (1ull << bit);
+    int n = 0;
+#pragma unroll
+    for (int i = 0; i < kList / 64; ++i) n += (int)__builtin_popcountll(__ballot(k[i] >= with));
+    if (n >= M) t = with;
+  }
+  count = 0;
+#pragma unroll
+  for (int i = 0; i < kList / 64; ++i) {
+    const bool stays = k[i] >= t && k[i] != 0;
+    const u64 mask = __ballot(stays);
+    if (stays) list[count + lanes_below(mask)] = k[i];
+    count += (int)__builtin_popcountll(mask);
+  }
+  return t;
+}
+
+// One tile: `first` is the index in the row of the lane's first entry.
+template <typename E> __device__ __forceinline__ void take_tile(Scan<E> &w, float (&v)[kPer], uint32_t first, float c, int M, u64 *list) {
+  constexpr int N = kWide<E>;
+  const auto largest = [&] {
+    float t = max3(v[0], v[1], v[2]);
+#pragma unroll
+    for (int i = 3; i + 1 < kPer; i += 2) t = max3(t, v[i], v[i + 1]);
+    return max3(t, v[kPer - 1], v[kPer - 1]);
+  };
+  float t = largest();
+  if (__ballot(!(t <= w.bound)) != 0) {  // (a NaN comes here too)
+    if (__ballot(!(t < kInf)) != 0) {    // entries without mass
+#pragma unroll
+      for (int i = 0; i < kPer; ++i) v[i] = with_mass(v[i]) ? v[i] : -kInf;
+      t = largest();
+    }
+    if (__ballot(t > w.m) != 0) {
+      const float m = wave_max(t), by = fmaxf((w.m - m) * c, -200.0f), scale = __builtin_amdgcn_exp2f(by);
+      w.d = (w.d + w.s * by) * scale;
+      w.s *= scale;
+      w.m = m;
+      if (M == 0) w.bound = m;
+    }
+    if (M > 0) {
+#pragma unroll
+      for (int i = 0; i < kPer; ++i) {
+        if (__ballot(v[i] > w.bound) == 0) continue;
+        if (w.count + 64 > kList) {
+          w.least = cut_list(list, w.count, M);
+          // (what is equal to the least kept and lies in a later tile comes after it; in this one, `least` decides)
+        }
+        const u64 key = key_of(v[i], first + (i / N) * 64 * N + i % N);
+        const u64 mask = __ballot(v[i] > w.bound && key > w.least);
+        if (v[i] > w.bound && key > w.least) list[w.count + lanes_below(mask)] = key;
+        w.count += (int)__builtin_popcountll(mask);
+      }
+      if (w.least != 0) w.bound = fmaxf(w.bound, key_value(w.least));
+    }
+  }
+#pragma unroll
+  for (int i = 0; i < kPer; ++i) {
+    const float d = fmaxf((v[i] - w.m) * c, -200.0f), e = __builtin_amdgcn_exp2f(d);  // (no mass: 2^-200 is 0)
+    w.s += e;
+    w.d = fmaf(e, d, w.d);
+  }
+}
+
+// The n-th largest of the lanes' values, as `ordered`; 0 if there are fewer than n lanes.
+__device__ __forceinline__ uint32_t nth_of_lanes(float v, int n) {
+  const uint32_t o = ordered(v);
+  uint32_t t = 0;
+  if (n > 64) return 0;
+  for (int bit = 31; bit >= 0; --bit) {
+    const uint32_t with = t | (1u << bit);
+    if ((int)__builtin_popcountll(__ballot(o >= with)) >= n) t = with;
+  }
+  return t;
+}
+
+// The M largest of the lists' keys in order: emit(rank, key), key 0 where there are fewer.  Lists of `stride` keys, list i of count[i].
+template <int THREADS, typename F>
+__device__ __forceinline__ void select_top(const u64 *lists, int n_lists, int stride, const int *count, int total, u64 low, u64 high, int M, F emit) {
+  __shared__ int s_bins[kBins];
+  __shared__ u64 s_keys[kSelected];
+  __shared__ int s_wave[THREADS / 64], s_bin, s_above, s_n;
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+  u64 least = 1;
+  if (total > kSelected) {
+    int need = M, above = 0;  // `above` keys are larger than `high`
+    for (;;) {
+      const u64 range = high - low;
+      const int bits = range == 0 ? 0 : 64 - __builtin_clzll(range), shift = bits > 10 ? bits - 10 : 0;
+      for (int i = tid; i < kBins; i += THREADS) s_bins[i] = 0;
+      __syncthreads();
+      for (int l = wave; l < n_lists; l += THREADS / 64)
+        for (int i = lane; i < count[l]; i += 64) {
+          const u64 k = lists[(size_t)l * stride + i];
+          if (k >= low && k <= high) atomicAdd(&s_bins[(k - low) >> shift], 1);
+        }
+      __syncthreads();
+      // a thread takes kBins / THREADS bins, the first thread the uppermost
+      constexpr int kEach = kBins / THREADS;
+      int mine = 0;
+#pragma unroll
+      for (int i = 0; i < kEach; ++i) mine += s_bins[kBins - 1 - (tid * kEach + i)];
+      int upto = mine;
+#pragma unroll
+      for (int d = 1; d < 64; d <<= 1) {
+        const int o = __shfl_up(upto, d);
+        if (lane >= d) upto += o;
+      }
+      if (lane == 63) s_wave[wave] = upto;
+      __syncthreads();
+      for (int w = 0; w < wave; ++w) upto += s_wave[w];
+      if (upto >= need && upto - mine < need) {  // (one thread)
+        int n = upto - mine;
+        for (int i = 0; i < kEach; ++i) {
+          const int bin = kBins - 1 - (tid * kEach + i), here = s_bins[bin];
+          if (n + here >= need) { s_bin = bin; s_above = n; s_n = n + here; break; }
+          n += here;
+        }
+      }
+      __syncthreads();
+      least = low + ((u64)s_bin << shift);
+      if (above + s_n <= kSelected || shift == 0) break;
+      high = least + ((1ull << shift) - 1);
+      low = least;
+      need -= s_above;
+      above += s_above;
+      __syncthreads();
+    }
+  }
+  __syncthreads();
+  if (tid == 0) s_n = 0;
+  __syncthreads();
+  for (int l = wave; l < n_lists; l += THREADS / 64)
+    for (int i = lane; i < count[l]; i += 64) {
+      const u64 k = lists[(size_t)l * stride + i];
+      if (k >= least) s_keys[atomicAdd(&s_n, 1)] = k;
+    }
+  __syncthreads();
+  const int n = s_n;
+  for (int i = tid; i < n; i += THREADS) {
+    const u64 k = s_keys[i];
+    int rank = 0;
+    for (int j = 0; j < n; ++j) rank += s_keys[j] > k ? 1 : 0;
+    if (rank < M) emit(rank, k);
+  }
+  for (int m = n + tid; m < M; m += THREADS) emit(m, (u64)0);
+}
+
+// What a row's sums give, the same in every thread.
+struct Row {
+  double top, rest, entropy, inv_t;
+  __device__ __forceinline__ float logp(float v) const { return with_mass(v) ? (float)(((double)v - top) * inv_t - rest) : -kInf; }
+};
+__device__ __forceinline__ Row row_of(float top, double s, double d, float temp) {
+  Row r;
+  const bool any = top > -kInf;
+  r.top = any ? (double)top : 0.0;
+  r.rest = any ? log(s) : -(double)kInf;
+  r.entropy = any ? r.rest - kLn2 * d / s : 0.0;
+  r.inv_t = 1.0 / (double)temp;
+  return r;
+}
+template <typename E> __device__ __forceinline__ void write_scores(const ScoreParams &p, long long r, const Row &row, int threads) {
   if (threadIdx.x == 0) {
-    if (p.lse != nullptr) { p.lse[2 * r] = top; p.lse[2 * r + 1] = rest; }
-    if (p.entropy != nullptr) p.entropy[r] = (float)entropy;
+    if (p.lse != nullptr) { p.lse[2 * r] = row.top; p.lse[2 * r + 1] = row.rest; }
+    if (p.entropy != nullptr) p.entropy[r] = (float)row.entropy;
   }
-  if (p.logp != nullptr) {
-    for (int g = threadIdx.x; g < p.G; g += kBlock) {
-      const int t = p.tokens[r * p.tok_stride_r + g];
-      float out = t < 0 ? 0.0f : -kInf;
-      if (t >= 0 && t < p.V && with_mass(widen(x[t]))) out = logp_of(widen(x[t]));
-      p.logp[r * p.G + g] = out;
-    }
+  if (p.logp == nullptr) return;
+  const E *x = reinterpret_cast<const E *>(p.x) + r * p.stride_r;
+  for (int g = threadIdx.x; g < p.G; g += threads) {
+    const int t = p.tokens[r * p.tok_stride_r + g];
+    p.logp[r * p.G + g] = t < 0 ? 0.0f : t < p.V ? row.logp(widen(x[t])) : -kInf;
   }
-  unsigned long long last = ~0ull;
-  for (int m = 0; m < p.M; ++m) {
-    best = 0;
-    for (int i = threadIdx.x; last != 0 && i < p.V; i += kBlock) {
-      const unsigned long long o = order_of(widen(x[i]), i);
-      if (o < last) best = larger(best, o);
+}
+__device__ __forceinline__ void write_top(const ScoreParams &p, long long r, const Row &row, int rank, u64 key) {
+  p.top_ids[r * p.M + rank] = key != 0 ? key_index(key) : -1;
+  p.top_logp[r * p.M + rank] = key != 0 ? row.logp(key_value(key)) : -kInf;
+}
+
+// Sums that the lanes hold, each relative to its own largest entry, as one relative to the largest of all.
+__device__ __forceinline__ void join_shares(double &s, double &d, float mine, float top, float c) {
+  const double by = mine > -kInf ? (double)fmaxf((mine - top) * c, -200.0f) : -200.0, scale = exp2(by);
+  d = wave_sum((d + s * by) * scale);
+  s = wave_sum(s * scale);
+}
+
+// One workgroup a row, or a chunk of it.
+template <typename E, int WAVES> __global__ void __launch_bounds__(WAVES * 64) score_kernel(const ScoreParams p) {
+  constexpr int N = kWide<E>, kTile = 64 * kPer;
+  __shared__ u64 s_list[WAVES * kList];
+  __shared__ double s_s[WAVES], s_d[WAVES];
+  __shared__ float s_m[WAVES];
+  __shared__ int s_count[WAVES];
+  __shared__ uint32_t s_nth[WAVES];
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const long long r = p.chunks > 1 ? blockIdx.x / p.chunks : blockIdx.x;
+  const int part = p.chunks > 1 ? (int)(blockIdx.x - r * p.chunks) : 0;
+  const long long begin = (long long)part * p.chunk, end = begin + p.chunk < p.V ? begin + p.chunk : p.V;
+  const E *x = reinterpret_cast<const E *>(p.x) + r * p.stride_r;
+  const float c = kLog2e / p.temp;
+  u64 *list = s_list + wave * kList;
+  Scan<E> w;
+  float v[kPer], next[kPer];
+  long long at = begin + (long long)wave * kTile;
+  const auto load = [&](long long from, float (&to)[kPer]) {
+    if (from + kTile <= end) load_tile(x + from + lane * N, 0, to);
+    else load_tile_end(x + from + lane * N, end - from - lane * N, to);
+  };
+  if (at < end) load(at, v);
+  uint32_t low = 0;
+  if (p.M > 0) {
+    // a bound that M entries reach: every wavefront's share of them is in its first tile
+    float t = -kInf;
+    if (at < end) {
+#pragma unroll
+      for (int i = 0; i < kPer; ++i) t = fmaxf(t, with_mass(v[i]) ? v[i] : -kInf);
     }
-    last = over_workgroup(best, larger, s_order);
-    if (threadIdx.x == 0) {
-      const int i = last != 0 ? (int)(0xFFFFFFFFu - (uint32_t)last) : -1;
-      p.top_ids[r * p.M + m] = i;
-      p.top_logp[r * p.M + m] = i >= 0 ? logp_of(widen(x[i])) : -kInf;
-    }
+    const uint32_t nth = nth_of_lanes(t, (p.M + WAVES - 1) / WAVES);
+    if (lane == 0) s_nth[wave] = nth;
+    __syncthreads();
+    low = 0xFFFFFFFFu;
+    for (int i = 0; i < WAVES; ++i) low = s_nth[i] < low ? s_nth[i] : low;
+    if (low > ordered(-kInf)) w.bound = unordered(low - (low == ordered(0.0f) ? 2 : 1));  // (what is equal to it counts; below 0 comes -0, its equal)
   }
+  for (; at < end; at += (long long)WAVES * kTile) {
+    const long long after = at + (long long)WAVES * kTile;
+    if (after < end) load(after, next);
+    take_tile<E>(w, v, (uint32_t)(at + lane * N), c, p.M, list);
+#pragma unroll
+    for (int i = 0; i < kPer; ++i) v[i] = next[i];
+  }
+  // the wavefronts' sums
+  const double ws = wave_sum((double)w.s), wd = wave_sum((double)w.d);
+  if (lane == 0) { s_s[wave] = ws; s_d[wave] = wd; s_m[wave] = w.m; s_count[wave] = w.count; }
+  __syncthreads();
+  const int mine = lane < WAVES ? lane : 0;
+  const float my_top = lane < WAVES ? s_m[mine] : -kInf, top = wave_max(my_top);
+  double s = lane < WAVES ? s_s[mine] : 0.0, d = lane < WAVES ? s_d[mine] : 0.0;
+  join_shares(s, d, my_top, top, c);
+  int total = 0;
+  for (int i = 0; i < WAVES; ++i) total += s_count[i];
+  const u64 high = key_of(top > -kInf ? top : 0.0f, 0), least = (u64)(low > 0 ? low : 1) << 32;
+  if (p.chunks > 1) {
+    u64 *keys = p.keys + (r * p.chunks + part) * p.M;
+    if (threadIdx.x == 0) p.shares[r * p.chunks + part] = Share{s, d, 0.0, top, total < p.M ? total : p.M};
+    if (p.M > 0) select_top<WAVES * 64>(s_list, WAVES, kList, s_count, total, least, high, p.M, [&](int rank, u64 key) { keys[rank] = key; });
+    return;
+  }
+  const Row row = row_of(top, s, d, p.temp);
+  write_scores<E>(p, r, row, WAVES * 64);
+  if (p.M > 0) select_top<WAVES * 64>(s_list, WAVES, kList, s_count, total, least, high, p.M, [&](int rank, u64 key) { write_top(p, r, row, rank, key); });
+}
+
+// Joins a row's chunks.
+template <typename E> __global__ void __launch_bounds__(kBlock) score_join_kernel(const ScoreParams p) {
+  __shared__ int s_count[kMostSplit];
+  const long long r = blockIdx.x;
+  const Share *shares = p.shares + r * p.chunks;
+  const float c = kLog2e / p.temp;
+  const int lane = threadIdx.x & 63;
+  Share share = {0.0, 0.0, 0.0, -kInf, 0};
+  if (lane < p.chunks) share = shares[lane];
+  const float top = wave_max(share.top);
+  int total = share.count;
+#pragma unroll
+  for (int i = 32; i >= 1; i >>= 1) total += __shfl_xor(total, i);
+  double s = share.s, d = share.d;
+  join_shares(s, d, share.top, top, c);
+  const Row row = row_of(top, s, d, p.temp);
+  write_scores<E>(p, r, row, kBlock);
+  if (p.M == 0) return;
+  if ((int)threadIdx.x < p.chunks) s_count[threadIdx.x] = share.count;
+  __syncthreads();
+  select_top<kBlock>(p.keys + r * p.chunks * p.M, p.chunks, p.M, s_count, total, 1ull << 32, key_of(top > -kInf ? top : 0.0f, 0), p.M,
+                     [&](int rank, u64 key) { write_top(p, r, row, rank, key); });
 }
 
 template <typename E> __global__ void __launch_bounds__(kBlock) score_grad_kernel(const ScoreParams p) {
@@ -128,12 +428,44 @@ template <typename E> __global__ void __launch_bounds__(kBlock) score_grad_kerne
   }
 }
 
+constexpr long long kMostGrid = 0xFFFFFFFFLL / kBlock;  // workgroups of a launch (those of 1024 threads: launches of fewer than 1024)
+
 bool rows_ok(long long R, long long V, long long G, long long M) {
-  return R >= 0 && R < (1LL << 24) && V >= 1 && V <= kMaxIndex && G >= 0 && G <= 65535 && M >= 0 && M <= LLC_TOP_MAX;
+  return R >= 0 && R <= kMostGrid && V >= 1 && V <= kMaxIndex && G >= 0 && G <= 65535 && M >= 0 && M <= LLC_TOP_MAX;
 }
 
-size_t rows_workspace(long long R, long long M, long long chunks) {
-  return (size_t)chunks * (size_t)R * (32 + 8 * (size_t)M) + 32 * (size_t)R + 512;
+static_assert(sizeof(Share) == 32, "what the interface states of the workspace");
+size_t rows_workspace(long long R, long long M, long long chunks) {  // shares and keys, then (gradient) lse and entropy
+  return (size_t)chunks * (size_t)R * (sizeof(Share) + 8 * (size_t)M) + 32 * (size_t)R + 512;
+}
+
+// Workgroups that a row is split over.
+#ifndef SPLIT
+#define SPLIT 1
+#endif
+int auto_split(long long R, long long V) { return SPLIT; }
+
+// Cuts a row into `want` chunks of whole 16-byte loads.
+void split_rows(ScoreParams &p, long long want) {
+  const long long each = ((p.V + want - 1) / want + 15) & ~15LL;
+  p.chunk = (int)(each < kMaxIndex ? each : kMaxIndex);
+  p.chunks = (int)((p.V + each - 1) / each);
+}
+
+template <typename E> hipError_t launch_scores(const ScoreParams &p, hipStream_t st) {
+  const unsigned blocks = (unsigned)(p.R * p.chunks);
+  const long long tiles = (p.chunk + 64 * kPer - 1) / (64 * kPer);
+#ifdef NW
+  score_kernel<E, NW><<<blocks, NW * 64, 0, st>>>(p);
+#else
+  if (tiles <= 1) score_kernel<E, 1><<<blocks, 64, 0, st>>>(p);
+  else if (tiles <= 8 || blocks >= 1024) score_kernel<E, 4><<<blocks, 256, 0, st>>>(p);
+  else score_kernel<E, 16><<<blocks, 1024, 0, st>>>(p);
+#endif
+  hipError_t e = hipGetLastError();
+  if (e != hipSuccess || p.chunks == 1) return e;
+  score_join_kernel<E><<<(unsigned)p.R, kBlock, 0, st>>>(p);
+  return hipGetLastError();
 }
 
 }  // namespace
@@ -142,7 +474,7 @@ size_t rows_workspace(long long R, long long M, long long chunks) {
 using namespace llc;
 
 extern "C" size_t llc_token_logprobs_workspace_size(int64_t R, int64_t V, int64_t M) {
-  return rows_ok(R, V, 0, M) ? rows_workspace(R, M, 1) : 0;
+  return rows_ok(R, V, 0, M) ? rows_workspace(R, M, auto_split(R, V)) : 0;
 }
 
 extern "C" int llc_token_logprobs(const llc_token_logprobs_args *a) {
@@ -158,21 +490,19 @@ extern "C" int llc_token_logprobs(const llc_token_logprobs_args *a) {
   const bool logits = a->kind == LLC_LOGITS;
   if (logits && !(std::isfinite(a->temp) && a->temp > 0.0f)) return LLC_E_TEMP;
   if (!fits(a->x, type_size(a->dtype)) || !fits(a->tokens, 4)) return LLC_E_ALIGN;
-  if (a->workspace == nullptr || !fits(a->workspace, 256) ||
-      a->workspace_bytes < rows_workspace(a->R, a->M, a->v_chunks > 1 ? a->v_chunks : 1))
-    return LLC_E_WORKSPACE;
+  const long long split = a->v_chunks > 0 ? a->v_chunks : auto_split(a->R, a->V);
+  if (a->workspace == nullptr || !fits(a->workspace, 256) || a->workspace_bytes < rows_workspace(a->R, a->M, split)) return LLC_E_WORKSPACE;
+  if (a->R * split > kMostGrid) return LLC_E_SHAPE;
   if ((a->flags & LLC_FLAG_DRY_RUN) != 0) return LLC_OK;
   ScoreParams p = {};
   p.R = a->R; p.V = (int)a->V; p.G = (int)a->G; p.M = (int)a->M;
   p.x = a->x; p.stride_r = a->stride_r; p.temp = logits ? a->temp : 1.0f;
   p.tokens = a->tokens; p.tok_stride_r = a->tok_stride_r;
   p.logp = a->logp; p.entropy = a->entropy; p.lse = a->lse; p.top_ids = a->top_ids; p.top_logp = a->top_logp;
+  split_rows(p, split);
+  p.shares = (Share *)a->workspace; p.keys = (u64 *)(p.shares + p.R * p.chunks);
   hipStream_t st = (hipStream_t)a->stream;
-  return between_events(a->ev_begin, a->ev_end, st, [&] {
-    if (a->dtype == LLC_F32) score_kernel<float><<<(unsigned)p.R, kBlock, 0, st>>>(p);
-    else score_kernel<uint16_t><<<(unsigned)p.R, kBlock, 0, st>>>(p);
-    return hipGetLastError();
-  });
+  return between_events(a->ev_begin, a->ev_end, st, [&] { return a->dtype == LLC_F32 ? launch_scores<float>(p, st) : launch_scores<uint16_t>(p, st); });
 }
 
 extern "C" int llc_token_logprobs_grad(const llc_token_logprobs_grad_args *a) {
@@ -191,9 +521,10 @@ extern "C" int llc_token_logprobs_grad(const llc_token_logprobs_grad_args *a) {
   if (logits && !(std::isfinite(a->temp) && a->temp > 0.0f)) return LLC_E_TEMP;
   if (!fits(a->x, type_size(a->dtype)) || !fits(a->grad, type_size(a->dtype)) || !fits(a->tokens, 4) || !fits(a->grad_logp, 4))
     return LLC_E_ALIGN;
-  if (a->lse_in == nullptr && (a->workspace == nullptr || !fits(a->workspace, 256) ||
-      a->workspace_bytes < rows_workspace(a->R, 0, a->v_chunks > 1 ? a->v_chunks : 1)))
+  const long long split = a->v_chunks > 0 ? a->v_chunks : auto_split(a->R, a->V);
+  if (a->lse_in == nullptr && (a->workspace == nullptr || !fits(a->workspace, 256) || a->workspace_bytes < rows_workspace(a->R, 0, split)))
     return LLC_E_WORKSPACE;
+  if (a->R * split > kMostGrid) return LLC_E_SHAPE;
   if ((a->flags & LLC_FLAG_DRY_RUN) != 0) return LLC_OK;
   ScoreParams p = {};
   p.R = a->R; p.V = (int)a->V; p.G = (int)a->G; p.M = 0;
@@ -202,16 +533,18 @@ extern "C" int llc_token_logprobs_grad(const llc_token_logprobs_grad_args *a) {
   p.a = a->grad_logp; p.a_stride_r = a->grad_logp_stride_r; p.b = a->grad_entropy;
   p.grad = a->grad; p.grad_stride_r = a->grad_stride_r;
   p.logp = a->logp;
-  p.lse = a->lse != nullptr ? a->lse : (double *)a->workspace;
-  p.entropy = a->entropy != nullptr ? a->entropy : (float *)((double *)a->workspace + 2 * a->R);
+  split_rows(p, split);
+  p.shares = (Share *)a->workspace;
+  double *kept = (double *)(p.shares + p.R * p.chunks);
+  p.lse = a->lse != nullptr ? a->lse : kept;
+  p.entropy = a->entropy != nullptr ? a->entropy : (float *)(kept + 2 * a->R);
   p.lse_in = a->lse_in != nullptr ? a->lse_in : p.lse;
   p.entropy_in = a->lse_in != nullptr ? a->entropy_in : p.entropy;
   hipStream_t st = (hipStream_t)a->stream;
   return between_events(a->ev_begin, a->ev_end, st, [&] {
     if (a->lse_in == nullptr) {
-      if (a->dtype == LLC_F32) score_kernel<float><<<(unsigned)p.R, kBlock, 0, st>>>(p);
-      else score_kernel<uint16_t><<<(unsigned)p.R, kBlock, 0, st>>>(p);
-      if (hipGetLastError() != hipSuccess) return hipErrorUnknown;
+      const hipError_t e = a->dtype == LLC_F32 ? launch_scores<float>(p, st) : launch_scores<uint16_t>(p, st);
+      if (e != hipSuccess) return e;
     }
     if (a->dtype == LLC_F32) score_grad_kernel<float><<<(unsigned)p.R, kBlock, 0, st>>>(p);
     else score_grad_kernel<uint16_t><<<(unsigned)p.R, kBlock, 0, st>>>(p);
