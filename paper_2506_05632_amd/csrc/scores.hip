@@ -76,10 +76,22 @@ __device__ __forceinline__ float wave_max(float v) {  // the same in every lane;
 #undef LLC_STEP
   return __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(v), 63));
 }
-__device__ __forceinline__ double wave_sum(double v) {
-#pragma unroll
-  for (int d = 32; d >= 1; d >>= 1) v += __shfl_xor(v, d);
-  return v;
+template <int CTRL, int ROWS> __device__ __forceinline__ double from_lane(double v) {  // of the rows that do not take part: 0
+  const u64 b = __builtin_bit_cast(u64, v);
+  const uint32_t low = __builtin_amdgcn_update_dpp(0, (uint32_t)b, CTRL, ROWS, 0xF, false);
+  const uint32_t high = __builtin_amdgcn_update_dpp(0, (uint32_t)(b >> 32), CTRL, ROWS, 0xF, false);
+  return __builtin_bit_cast(double, ((u64)high << 32) | low);
+}
+__device__ __forceinline__ double wave_sum(double v) {  // the same in every lane
+  v += from_lane<0x111, 0xF>(v);  // row_shr 1, 2, 4, 8
+  v += from_lane<0x112, 0xF>(v);
+  v += from_lane<0x114, 0xF>(v);
+  v += from_lane<0x118, 0xF>(v);
+  v += from_lane<0x142, 0xA>(v);  // row_bcast 15, 31
+  v += from_lane<0x143, 0xC>(v);
+  const u64 b = __builtin_bit_cast(u64, v);
+  return __builtin_bit_cast(double, ((u64)(uint32_t)__builtin_amdgcn_readlane((uint32_t)(b >> 32), 63) << 32) |
+                                        (uint32_t)__builtin_amdgcn_readlane((uint32_t)b, 63));
 }
 __device__ __forceinline__ int lanes_below(u64 mask) {
   return __builtin_amdgcn_mbcnt_hi((uint32_t)(mask >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)mask, 0));
@@ -96,7 +108,7 @@ template <typename E> __device__ __forceinline__ void load_tile(const E *x, long
 #pragma unroll
   for (int u = 0; u < kPer / N; ++u) {
     float w[N];
-    load_some<N>(x + u * 64 * N, w);
+    fetch_some<N>(x + u * 64 * N, w);
 #pragma unroll
     for (int i = 0; i < N; ++i) v[u * N + i] = w[i];
   }
@@ -114,7 +126,6 @@ template <typename E> struct Scan {
   float m = -kInf;      // largest entry so far
   float s = 0.0f, d = 0.0f;
   float bound = -kInf;  // candidates are above it
-  u64 least = 0;        // and have larger keys than this
   int count = 0;        // of the list
 };
 
@@ -146,11 +157,14 @@ __device__ __forceinline__ u64 cut_list(u64 *list, int &count, int M) {
 // One tile: `first` is the index in the row of the lane's first entry.
 template <typename E> __device__ __forceinline__ void take_tile(Scan<E> &w, float (&v)[kPer], uint32_t first, float c, int M, u64 *list) {
   constexpr int N = kWide<E>;
+  float half[2];  // the largest of either half of the entries
   const auto largest = [&] {
-    float t = max3(v[0], v[1], v[2]);
 #pragma unroll
-    for (int i = 3; i + 1 < kPer; i += 2) t = max3(t, v[i], v[i + 1]);
-    return max3(t, v[kPer - 1], v[kPer - 1]);
+    for (int h = 0; h < 2; ++h) {
+      const float *o = v + h * (kPer / 2);
+      half[h] = max3(max3(o[0], o[1], o[2]), max3(o[3], o[4], o[5]), max3(o[6], o[7], o[7]));
+    }
+    return max3(half[0], half[1], half[1]);
   };
   float t = largest();
   if (__ballot(!(t <= w.bound)) != 0) {  // (a NaN comes here too)
@@ -167,19 +181,45 @@ template <typename E> __device__ __forceinline__ void take_tile(Scan<E> &w, floa
       if (M == 0) w.bound = m;
     }
     if (M > 0) {
+      u64 lanes = __ballot(t > w.bound);
+      int most = kPer * (int)__builtin_popcountll(lanes);
+      if (w.count + most > kList) {
+        most = 0;
 #pragma unroll
-      for (int i = 0; i < kPer; ++i) {
-        if (__ballot(v[i] > w.bound) == 0) continue;
-        if (w.count + 64 > kList) {
-          w.least = cut_list(list, w.count, M);
-          // (what is equal to the least kept and lies in a later tile comes after it; in this one, `least` decides)
-        }
-        const u64 key = key_of(v[i], first + (i / N) * 64 * N + i % N);
-        const u64 mask = __ballot(v[i] > w.bound && key > w.least);
-        if (v[i] > w.bound && key > w.least) list[w.count + lanes_below(mask)] = key;
-        w.count += (int)__builtin_popcountll(mask);
+        for (int i = 0; i < kPer; ++i) most += (int)__builtin_popcountll(__ballot(v[i] > w.bound));
       }
-      if (w.least != 0) w.bound = fmaxf(w.bound, key_value(w.least));
+      if (w.count + most <= kList) {
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+          if (__ballot(half[h] > w.bound) == 0) continue;
+#pragma unroll
+          for (int i = h * (kPer / 2); i < (h + 1) * (kPer / 2); ++i) {
+            const u64 mask = __ballot(v[i] > w.bound);
+            if (mask == 0) continue;
+            if (v[i] > w.bound) list[w.count + lanes_below(mask)] = key_of(v[i], first + (i / N) * 64 * N + i % N);
+            w.count += (int)__builtin_popcountll(mask);
+          }
+        }
+      } else {  // as many as may not fit: a lane's at a time, and the list is cut where it is full
+        const int lane = threadIdx.x & 63;
+        u64 least = 0;
+        for (; lanes != 0; lanes &= lanes - 1) {
+          const int from = __builtin_ctzll(lanes);
+          float mine = -kInf;
+#pragma unroll
+          for (int i = 0; i < kPer; ++i) {
+            const float o = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(v[i]), from));
+            if (lane == i) mine = o;
+          }
+          if (w.count + kPer > kList) least = cut_list(list, w.count, M);
+          const u64 key = key_of(mine, __builtin_amdgcn_readlane(first, from) + (lane / N) * 64 * N + lane % N);
+          const bool offered = mine > w.bound && key > least;
+          const u64 mask = __ballot(offered);
+          if (offered) list[w.count + lanes_below(mask)] = key;
+          w.count += (int)__builtin_popcountll(mask);
+        }
+        if (least != 0) w.bound = fmaxf(w.bound, key_value(least));  // (what equals the least kept one comes after it in a later tile)
+      }
     }
   }
 #pragma unroll
@@ -190,27 +230,88 @@ template <typename E> __device__ __forceinline__ void take_tile(Scan<E> &w, floa
   }
 }
 
-// The n-th largest of the lanes' values, as `ordered`; 0 if there are fewer than n lanes.
-__device__ __forceinline__ uint32_t nth_of_lanes(float v, int n) {
-  const uint32_t o = ordered(v);
+// A number that n of the lanes' K ordered values each reach, and little below the n-th largest of them (its upper 16 bits); 0 if there are fewer than n.
+template <int K> __device__ __forceinline__ uint32_t reached_by(const uint32_t (&o)[K], int n) {
   uint32_t t = 0;
-  if (n > 64) return 0;
-  for (int bit = 31; bit >= 0; --bit) {
+#pragma unroll 4
+  for (int bit = 31; bit >= 16; --bit) {
     const uint32_t with = t | (1u << bit);
-    if ((int)__builtin_popcountll(__ballot(o >= with)) >= n) t = with;
+    int reach = 0;
+#pragma unroll
+    for (int i = 0; i < K; ++i) reach += (int)__builtin_popcountll(__ballot(o[i] >= with));
+    if (reach >= n) t = with;
   }
   return t;
+}
+// What all wavefronts have said so far.
+__device__ __forceinline__ uint32_t least_said(const uint32_t *said, int waves) {
+  const int lane = threadIdx.x & 63;
+  uint32_t v = 0xFFFFFFFFu;
+  if (lane < waves) v = *(const volatile uint32_t *)&said[lane];
+  v = min(v, (uint32_t)__builtin_amdgcn_update_dpp(v, v, 0x111, 0xF, 0xF, false));
+  v = min(v, (uint32_t)__builtin_amdgcn_update_dpp(v, v, 0x112, 0xF, 0xF, false));
+  v = min(v, (uint32_t)__builtin_amdgcn_update_dpp(v, v, 0x114, 0xF, 0xF, false));
+  v = min(v, (uint32_t)__builtin_amdgcn_update_dpp(v, v, 0x118, 0xF, 0xF, false));
+  return __builtin_amdgcn_readlane(v, 15);  // (at most 16 wavefronts)
+}
+
+// The largest bound that lets through whatever orders as `o` or more.
+__device__ __forceinline__ float just_below(uint32_t o) {
+  return o > ordered(-kInf) ? unordered(o - (o == ordered(0.0f) ? 2 : 1)) : -kInf;  // (below 0 comes -0, its equal)
+}
+
+// A wavefront looks at its list: it says what `share` of its entries reach and, told what M of the row's entries reach then, drops the others.
+// K: 64ths of the list that are in use.
+template <int K> __device__ __forceinline__ float look_at_list(u64 *list, int &count, int share, uint32_t *said, int waves, int wave) {
+  const int lane = threadIdx.x & 63;
+  u64 k[K];
+  uint32_t o[K];
+#pragma unroll
+  for (int i = 0; i < K; ++i) {
+    k[i] = i * 64 + lane < count ? list[i * 64 + lane] : 0;
+    o[i] = (uint32_t)(k[i] >> 32);
+  }
+  const uint32_t nth = reached_by(o, share);
+  if (lane == 0) said[wave] = nth;
+  const uint32_t all = least_said(said, waves);
+  count = 0;
+#pragma unroll
+  for (int i = 0; i < K; ++i) {
+    const bool stays = k[i] != 0 && o[i] >= all;
+    const u64 mask = __ballot(stays);
+    if (stays) list[count + lanes_below(mask)] = k[i];
+    count += (int)__builtin_popcountll(mask);
+  }
+  return just_below(all);
 }
 
 // The M largest of the lists' keys in order: emit(rank, key), key 0 where there are fewer.  Lists of `stride` keys, list i of count[i].
 template <int THREADS, typename F>
-__device__ __forceinline__ void select_top(const u64 *lists, int n_lists, int stride, const int *count, int total, u64 low, u64 high, int M, F emit) {
+__device__ __forceinline__ void select_top(const u64 *lists, int n_lists, int stride, const int *count, u64 low, u64 high, int M, F emit) {
   __shared__ int s_bins[kBins];
   __shared__ u64 s_keys[kSelected];
   __shared__ int s_wave[THREADS / 64], s_bin, s_above, s_n;
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-  u64 least = 1;
-  if (total > kSelected) {
+  u64 least = low;  // (M keys or all reach it)
+  if (tid == 0) s_n = 0;
+  __syncthreads();
+  // those go to a list of their own, unless they are too many
+  const auto gather = [&] {
+    for (int l = wave; l < n_lists; l += THREADS / 64)
+      for (int i0 = 0; i0 < count[l]; i0 += 64) {
+        const u64 k = i0 + lane < count[l] ? lists[(size_t)l * stride + i0 + lane] : 0;
+        const bool in = k >= least && k != 0;
+        const u64 mask = __ballot(in);
+        if (mask == 0) continue;
+        int at = 0;
+        if (lane == 0) at = atomicAdd(&s_n, (int)__builtin_popcountll(mask));
+        at = __builtin_amdgcn_readfirstlane(at) + lanes_below(mask);
+        if (in && at < kSelected) s_keys[at] = k;
+      }
+  };
+  gather();
+  __syncthreads();
+  if (s_n > kSelected) {
     int need = M, above = 0;  // `above` keys are larger than `high`
     for (;;) {
       const u64 range = high - low;
@@ -254,16 +355,12 @@ __device__ __forceinline__ void select_top(const u64 *lists, int n_lists, int st
       above += s_above;
       __syncthreads();
     }
+    __syncthreads();
+    if (tid == 0) s_n = 0;
+    __syncthreads();
+    gather();
+    __syncthreads();
   }
-  __syncthreads();
-  if (tid == 0) s_n = 0;
-  __syncthreads();
-  for (int l = wave; l < n_lists; l += THREADS / 64)
-    for (int i = lane; i < count[l]; i += 64) {
-      const u64 k = lists[(size_t)l * stride + i];
-      if (k >= least) s_keys[atomicAdd(&s_n, 1)] = k;
-    }
-  __syncthreads();
   const int n = s_n;
   for (int i = tid; i < n; i += THREADS) {
     const u64 k = s_keys[i];
@@ -288,14 +385,14 @@ __device__ __forceinline__ Row row_of(float top, double s, double d, float temp)
   r.inv_t = 1.0 / (double)temp;
   return r;
 }
-template <typename E> __device__ __forceinline__ void write_scores(const ScoreParams &p, long long r, const Row &row, int threads) {
+template <typename E> __device__ __forceinline__ void write_scores(const ScoreParams &p, long long r, const Row &row, int from, int threads) {
   if (threadIdx.x == 0) {
     if (p.lse != nullptr) { p.lse[2 * r] = row.top; p.lse[2 * r + 1] = row.rest; }
     if (p.entropy != nullptr) p.entropy[r] = (float)row.entropy;
   }
   if (p.logp == nullptr) return;
   const E *x = reinterpret_cast<const E *>(p.x) + r * p.stride_r;
-  for (int g = threadIdx.x; g < p.G; g += threads) {
+  for (int g = from + threadIdx.x; g < p.G; g += threads) {
     const int t = p.tokens[r * p.tok_stride_r + g];
     p.logp[r * p.G + g] = t < 0 ? 0.0f : t < p.V ? row.logp(widen(x[t])) : -kInf;
   }
@@ -307,7 +404,7 @@ __device__ __forceinline__ void write_top(const ScoreParams &p, long long r, con
 
 // Sums that the lanes hold, each relative to its own largest entry, as one relative to the largest of all.
 __device__ __forceinline__ void join_shares(double &s, double &d, float mine, float top, float c) {
-  const double by = mine > -kInf ? (double)fmaxf((mine - top) * c, -200.0f) : -200.0, scale = exp2(by);
+  const double by = mine > -kInf ? (double)fmaxf((mine - top) * c, -200.0f) : -200.0, scale = (double)__builtin_amdgcn_exp2f((float)by);  // (off by 2^-23 of a wavefront's share)
   d = wave_sum((d + s * by) * scale);
   s = wave_sum(s * scale);
 }
@@ -335,28 +432,45 @@ template <typename E, int WAVES> __global__ void __launch_bounds__(WAVES * 64) s
     else load_tile_end(x + from + lane * N, end - from - lane * N, to);
   };
   if (at < end) load(at, v);
-  uint32_t low = 0;
+  if (at + (long long)WAVES * kTile < end) load(at + (long long)WAVES * kTile, next);
+  // tokens and their entries are on their way too
+  int token = -1;
+  float token_x = 0.0f;
+  if (p.chunks == 1 && (int)threadIdx.x < p.G) {
+    token = p.tokens[r * p.tok_stride_r + threadIdx.x];
+    if (token >= 0 && token < p.V) token_x = widen(x[token]);
+  }
+  // A bound that M entries reach: every wavefront's share of them is among what it has seen.  First each lane's largest of the first tile; later,
+  // whenever a wavefront has seen twice as much, the candidates in its list.  What a wavefront has once said stays true, so nobody waits.
+  const int share = (p.M + WAVES - 1) / WAVES;
   if (p.M > 0) {
-    // a bound that M entries reach: every wavefront's share of them is in its first tile
     float t = -kInf;
     if (at < end) {
 #pragma unroll
       for (int i = 0; i < kPer; ++i) t = fmaxf(t, with_mass(v[i]) ? v[i] : -kInf);
     }
-    const uint32_t nth = nth_of_lanes(t, (p.M + WAVES - 1) / WAVES);
+    const uint32_t o[1] = {ordered(t)}, nth = share <= 64 ? reached_by(o, share) : 0;
     if (lane == 0) s_nth[wave] = nth;
     __syncthreads();
-    low = 0xFFFFFFFFu;
-    for (int i = 0; i < WAVES; ++i) low = s_nth[i] < low ? s_nth[i] : low;
-    if (low > ordered(-kInf)) w.bound = unordered(low - (low == ordered(0.0f) ? 2 : 1));  // (what is equal to it counts; below 0 comes -0, its equal)
+    w.bound = just_below(least_said(s_nth, WAVES));
   }
-  for (; at < end; at += (long long)WAVES * kTile) {
-    const long long after = at + (long long)WAVES * kTile;
-    if (after < end) load(after, next);
+  const auto look = [&] {
+    if (w.count < share) return;
+    w.bound = fmaxf(w.bound, w.count <= 64 ? look_at_list<1>(list, w.count, share, s_nth, WAVES, wave)
+                                           : look_at_list<kList / 64>(list, w.count, share, s_nth, WAVES, wave));
+  };
+  // two tiles in turn, so that one is on its way while the other is taken
+  const long long step = (long long)WAVES * kTile;
+  for (int tiles = 1; at < end; tiles += 2, at += 2 * step) {
     take_tile<E>(w, v, (uint32_t)(at + lane * N), c, p.M, list);
-#pragma unroll
-    for (int i = 0; i < kPer; ++i) v[i] = next[i];
+    if (at + 2 * step < end) load(at + 2 * step, v);
+    if (p.M > 0 && (tiles & (tiles - 1)) == 0) look();
+    if (at + step >= end) break;
+    take_tile<E>(w, next, (uint32_t)(at + step + lane * N), c, p.M, list);
+    if (at + 3 * step < end) load(at + 3 * step, next);
+    if (p.M > 0 && (tiles & (tiles + 1)) == 0) look();
   }
+  if (p.M > 0) look();
   // the wavefronts' sums
   const double ws = wave_sum((double)w.s), wd = wave_sum((double)w.d);
   if (lane == 0) { s_s[wave] = ws; s_d[wave] = wd; s_m[wave] = w.m; s_count[wave] = w.count; }
@@ -367,16 +481,19 @@ template <typename E, int WAVES> __global__ void __launch_bounds__(WAVES * 64) s
   join_shares(s, d, my_top, top, c);
   int total = 0;
   for (int i = 0; i < WAVES; ++i) total += s_count[i];
-  const u64 high = key_of(top > -kInf ? top : 0.0f, 0), least = (u64)(low > 0 ? low : 1) << 32;
+  const u64 high = key_of(top > -kInf ? top : 0.0f, 0);
+  u64 least = 1;
+  if (p.M > 0) { const uint32_t said = least_said(s_nth, WAVES); least = (u64)(said > 0 ? said : 1) << 32; }
   if (p.chunks > 1) {
     u64 *keys = p.keys + (r * p.chunks + part) * p.M;
     if (threadIdx.x == 0) p.shares[r * p.chunks + part] = Share{s, d, 0.0, top, total < p.M ? total : p.M};
-    if (p.M > 0) select_top<WAVES * 64>(s_list, WAVES, kList, s_count, total, least, high, p.M, [&](int rank, u64 key) { keys[rank] = key; });
+    if (p.M > 0) select_top<WAVES * 64>(s_list, WAVES, kList, s_count, least, high, p.M, [&](int rank, u64 key) { keys[rank] = key; });
     return;
   }
   const Row row = row_of(top, s, d, p.temp);
-  write_scores<E>(p, r, row, WAVES * 64);
-  if (p.M > 0) select_top<WAVES * 64>(s_list, WAVES, kList, s_count, total, least, high, p.M, [&](int rank, u64 key) { write_top(p, r, row, rank, key); });
+  if ((int)threadIdx.x < p.G && p.logp != nullptr) p.logp[r * p.G + threadIdx.x] = token < 0 ? 0.0f : token < p.V ? row.logp(token_x) : -kInf;
+  write_scores<E>(p, r, row, WAVES * 64, WAVES * 64);
+  if (p.M > 0) select_top<WAVES * 64>(s_list, WAVES, kList, s_count, least, high, p.M, [&](int rank, u64 key) { write_top(p, r, row, rank, key); });
 }
 
 // Joins a row's chunks.
@@ -395,11 +512,11 @@ template <typename E> __global__ void __launch_bounds__(kBlock) score_join_kerne
   double s = share.s, d = share.d;
   join_shares(s, d, share.top, top, c);
   const Row row = row_of(top, s, d, p.temp);
-  write_scores<E>(p, r, row, kBlock);
+  write_scores<E>(p, r, row, 0, kBlock);
   if (p.M == 0) return;
   if ((int)threadIdx.x < p.chunks) s_count[threadIdx.x] = share.count;
   __syncthreads();
-  select_top<kBlock>(p.keys + r * p.chunks * p.M, p.chunks, p.M, s_count, total, 1ull << 32, key_of(top > -kInf ? top : 0.0f, 0), p.M,
+  select_top<kBlock>(p.keys + r * p.chunks * p.M, p.chunks, p.M, s_count, 1, key_of(top > -kInf ? top : 0.0f, 0), p.M,
                      [&](int rank, u64 key) { write_top(p, r, row, rank, key); });
 }
 
@@ -459,7 +576,8 @@ template <typename E> hipError_t launch_scores(const ScoreParams &p, hipStream_t
   score_kernel<E, NW><<<blocks, NW * 64, 0, st>>>(p);
 #else
   if (tiles <= 1) score_kernel<E, 1><<<blocks, 64, 0, st>>>(p);
-  else if (tiles <= 8 || blocks >= 1024) score_kernel<E, 4><<<blocks, 256, 0, st>>>(p);
+  else if (tiles <= 4 || blocks > 512) score_kernel<E, 4><<<blocks, 256, 0, st>>>(p);
+  else if (blocks > 256) score_kernel<E, 8><<<blocks, 512, 0, st>>>(p);
   else score_kernel<E, 16><<<blocks, 1024, 0, st>>>(p);
 #endif
   hipError_t e = hipGetLastError();
