@@ -102,23 +102,60 @@ __device__ __forceinline__ float max3(float a, float b, float c) {  // (NaN only
   return r;
 }
 
-// kPer entries of a lane: 16 bytes at a time, 64 lanes side by side.  `left`: entries from the lane's first on; what lies beyond is -inf.
-template <typename E> __device__ __forceinline__ void load_tile(const E *x, long long left, float (&v)[kPer]) {
-  constexpr int N = kWide<E>;
+// kPer entries of a lane: 16 bytes at a time, 64 lanes side by side, as they are and as floats.
+template <typename E> struct Tile {
+  word4_any w[kPer / kWide<E>];
+};
+template <typename E> __device__ __forceinline__ void unpack(const Tile<E> &t, float (&v)[kPer]) {
 #pragma unroll
-  for (int u = 0; u < kPer / N; ++u) {
-    float w[N];
-    fetch_some<N>(x + u * 64 * N, w);
+  for (int u = 0; u < kPer / kWide<E>; ++u)
 #pragma unroll
-    for (int i = 0; i < N; ++i) v[u * N + i] = w[i];
-  }
+    for (int i = 0; i < 4; ++i) {
+      if constexpr (sizeof(E) == 2) split_pair(t.w[u][i], v[u * 8 + 2 * i], v[u * 8 + 2 * i + 1]);
+      else v[u * 4 + i] = __uint_as_float(t.w[u][i]);
+    }
 }
-template <typename E> __device__ __forceinline__ void load_tile_end(const E *x, long long left, float (&v)[kPer]) {
+// `x` is the lane's first entry; what lies `left` entries from it or further is -inf.
+template <typename E> __device__ __forceinline__ Tile<E> load_tile(const E *x) {
+  Tile<E> t;
+#pragma unroll
+  for (int u = 0; u < kPer / kWide<E>; ++u) t.w[u] = __builtin_nontemporal_load(reinterpret_cast<const word4_any *>(x + u * 64 * kWide<E>));
+  return t;
+}
+template <typename E> __device__ __forceinline__ Tile<E> load_tile_end(const E *x, long long far) {
   constexpr int N = kWide<E>;
+  const int left = far < 64 * kPer ? (int)far : 64 * kPer;
+  Tile<E> t;
 #pragma unroll
   for (int u = 0; u < kPer / N; ++u)
 #pragma unroll
-    for (int i = 0; i < N; ++i) v[u * N + i] = u * 64 * N + i < left ? widen(x[u * 64 * N + i]) : -kInf;
+    for (int i = 0; i < 4; ++i) {
+      const int at = u * 64 * N + i * (N / 4);
+      if constexpr (sizeof(E) == 2)
+        t.w[u][i] = (at < left ? (uint32_t)x[at] : 0xFF80u) | (at + 1 < left ? (uint32_t)x[at + 1] : 0xFF80u) << 16;
+      else
+        t.w[u][i] = __float_as_uint(at < left ? x[at] : -kInf);
+    }
+  return t;
+}
+// The tile whose first entry is `at` of a row (or chunk) that ends at `end`.
+template <typename E> __device__ __forceinline__ Tile<E> load_at(const E *row, long long at, long long end) {
+  const int lane = threadIdx.x & 63;
+  if (at + 64 * kPer <= end) return load_tile(row + at + lane * kWide<E>);
+  return load_tile_end(row + at + lane * kWide<E>, end - at - lane * kWide<E>);
+}
+
+// Exponents are x c less a reference that follows from the largest entry m: m c as fp32 has it.  One multiply-add forms them, exact but for its one rounding, and
+// what the reference's own rounding shifts all of them by is put right at the end.  Where m c leaves fp32 they are (x - m) c.
+__device__ __forceinline__ bool has_reference(float m, float c) { return fabsf(m) * c < 0x1p100f; }
+__device__ __forceinline__ float reference_of(float m, float c) {
+#pragma clang fp contract(off)  // (it is rounded wherever it is used)
+  return m * c;
+}
+// From exponents relative to what belongs to `from` to those relative to what belongs to the larger `to`.
+__device__ __forceinline__ float shift_between(float from, float to, float c) {
+  const bool both = has_reference(from, c) && has_reference(to, c);
+  return fmaxf(both ? reference_of(from, c) - reference_of(to, c) : (from - to) * c, -200.0f);  // (from -inf: -200, or NaN, which is nothing to max)
 }
 
 // A wavefront's sums and candidates.
@@ -155,8 +192,10 @@ __device__ __forceinline__ u64 cut_list(u64 *list, int &count, int M) {
 }
 
 // One tile: `first` is the index in the row of the lane's first entry.
-template <typename E> __device__ __forceinline__ void take_tile(Scan<E> &w, float (&v)[kPer], uint32_t first, float c, int M, u64 *list) {
+template <typename E> __device__ __forceinline__ void take_tile(Scan<E> &w, const Tile<E> &tile, uint32_t first, float c, int M, u64 *list) {
   constexpr int N = kWide<E>;
+  float v[kPer];
+  unpack(tile, v);
   float half[2];  // the largest of either half of the entries
   const auto largest = [&] {
 #pragma unroll
@@ -174,7 +213,7 @@ template <typename E> __device__ __forceinline__ void take_tile(Scan<E> &w, floa
       t = largest();
     }
     if (__ballot(t > w.m) != 0) {
-      const float m = wave_max(t), by = fmaxf((w.m - m) * c, -200.0f), scale = __builtin_amdgcn_exp2f(by);
+      const float m = wave_max(t), by = shift_between(w.m, m, c), scale = __builtin_amdgcn_exp2f(by);
       w.d = (w.d + w.s * by) * scale;
       w.s *= scale;
       w.m = m;
@@ -222,24 +261,37 @@ template <typename E> __device__ __forceinline__ void take_tile(Scan<E> &w, floa
       }
     }
   }
-#pragma unroll
-  for (int i = 0; i < kPer; ++i) {
-    const float d = fmaxf((v[i] - w.m) * c, -200.0f), e = __builtin_amdgcn_exp2f(d);  // (no mass: 2^-200 is 0)
+  const auto add = [&](float d) {
+    const float e = __builtin_amdgcn_exp2f(d);  // (no mass: 2^-200 is 0)
     w.s += e;
     w.d = fmaf(e, d, w.d);
+  };
+  if (has_reference(w.m, c)) {  // (not where nothing has had mass yet)
+    const float reference = reference_of(w.m, c);
+#pragma unroll
+    for (int i = 0; i < kPer; ++i) add(fmaxf(fmaf(v[i], c, -reference), -200.0f));
+  } else {
+#pragma unroll
+    for (int i = 0; i < kPer; ++i) add(fmaxf((v[i] - w.m) * c, -200.0f));
   }
 }
 
 // A number that n of the lanes' K ordered values each reach, and little below the n-th largest of them (its upper 16 bits); 0 if there are fewer than n.
+// Two bits a step: the three counts of a step do not wait for each other.
 template <int K> __device__ __forceinline__ uint32_t reached_by(const uint32_t (&o)[K], int n) {
   uint32_t t = 0;
-#pragma unroll 4
-  for (int bit = 31; bit >= 16; --bit) {
-    const uint32_t with = t | (1u << bit);
-    int reach = 0;
+#pragma unroll 2
+  for (int bit = 30; bit >= 16; bit -= 2) {
+    uint32_t best = t;
 #pragma unroll
-    for (int i = 0; i < K; ++i) reach += (int)__builtin_popcountll(__ballot(o[i] >= with));
-    if (reach >= n) t = with;
+    for (uint32_t q = 1; q < 4; ++q) {
+      const uint32_t with = t + (q << bit);
+      int reach = 0;
+#pragma unroll
+      for (int i = 0; i < K; ++i) reach += (int)__builtin_popcountll(__ballot(o[i] >= with));
+      if (reach >= n) best = with;
+    }
+    t = best;
   }
   return t;
 }
@@ -371,6 +423,19 @@ __device__ __forceinline__ void select_top(const u64 *lists, int n_lists, int st
   for (int m = n + tid; m < M; m += THREADS) emit(m, (u64)0);
 }
 
+// ln s, s at least 1 or near it: the exponent is taken off first and the mantissa lies around 1, so that the hardware's fp32 logarithm, of a number between
+// -1/2 and 1/2, is off by 2^-24 at most; what the mantissa loses as an fp32 number is added.  (The library's fp64 logarithm keeps 40 registers of
+// constants through a loop over rows.)
+__device__ __forceinline__ double ln_of(double s) {
+  int e = __builtin_amdgcn_frexp_exp(s);
+  double m = __builtin_amdgcn_frexp_mant(s);
+  const bool low = m < 0.70703125;
+  m = low ? 2.0 * m : m;
+  e = low ? e - 1 : e;
+  const float f = (float)m;
+  return kLn2 * ((double)e + (double)__builtin_amdgcn_logf(f)) + (double)((float)(m - (double)f) * __builtin_amdgcn_rcpf(f));
+}
+
 // What a row's sums give, the same in every thread.
 struct Row {
   double top, rest, entropy, inv_t;
@@ -380,8 +445,10 @@ __device__ __forceinline__ Row row_of(float top, double s, double d, float temp)
   Row r;
   const bool any = top > -kInf;
   r.top = any ? (double)top : 0.0;
-  r.rest = any ? log(s) : -(double)kInf;
-  r.entropy = any ? r.rest - kLn2 * d / s : 0.0;
+  const float c = kLog2e / temp;
+  const double sum = any ? ln_of(s) : -(double)kInf;
+  r.entropy = any ? sum - kLn2 * d / s : 0.0;
+  r.rest = any && has_reference(top, c) ? sum + kLn2 * ((double)reference_of(top, c) - (double)top * (double)c) : sum;
   r.inv_t = 1.0 / (double)temp;
   return r;
 }
@@ -404,7 +471,7 @@ __device__ __forceinline__ void write_top(const ScoreParams &p, long long r, con
 
 // Sums that the lanes hold, each relative to its own largest entry, as one relative to the largest of all.
 __device__ __forceinline__ void join_shares(double &s, double &d, float mine, float top, float c) {
-  const double by = mine > -kInf ? (double)fmaxf((mine - top) * c, -200.0f) : -200.0, scale = (double)__builtin_amdgcn_exp2f((float)by);  // (off by 2^-23 of a wavefront's share)
+  const double by = mine > -kInf ? (double)shift_between(mine, top, c) : -200.0, scale = (double)__builtin_amdgcn_exp2f((float)by);  // (off by 2^-23 of a wavefront's share)
   d = wave_sum((d + s * by) * scale);
   s = wave_sum(s * scale);
 }
@@ -425,14 +492,10 @@ template <typename E, int WAVES> __global__ void __launch_bounds__(WAVES * 64) s
   const float c = kLog2e / p.temp;
   u64 *list = s_list + wave * kList;
   Scan<E> w;
-  float v[kPer], next[kPer];
+  Tile<E> here, next;
   long long at = begin + (long long)wave * kTile;
-  const auto load = [&](long long from, float (&to)[kPer]) {
-    if (from + kTile <= end) load_tile(x + from + lane * N, 0, to);
-    else load_tile_end(x + from + lane * N, end - from - lane * N, to);
-  };
-  if (at < end) load(at, v);
-  if (at + (long long)WAVES * kTile < end) load(at + (long long)WAVES * kTile, next);
+  if (at < end) here = load_at(x, at, end);
+  if (at + WAVES * kTile < end) next = load_at(x, at + WAVES * kTile, end);
   // tokens and their entries are on their way too
   int token = -1;
   float token_x = 0.0f;
@@ -446,6 +509,8 @@ template <typename E, int WAVES> __global__ void __launch_bounds__(WAVES * 64) s
   if (p.M > 0) {
     float t = -kInf;
     if (at < end) {
+      float v[kPer];
+      unpack(here, v);
 #pragma unroll
       for (int i = 0; i < kPer; ++i) t = fmaxf(t, with_mass(v[i]) ? v[i] : -kInf);
     }
@@ -462,15 +527,15 @@ template <typename E, int WAVES> __global__ void __launch_bounds__(WAVES * 64) s
   // two tiles in turn, so that one is on its way while the other is taken
   const long long step = (long long)WAVES * kTile;
   for (int tiles = 1; at < end; tiles += 2, at += 2 * step) {
-    take_tile<E>(w, v, (uint32_t)(at + lane * N), c, p.M, list);
-    if (at + 2 * step < end) load(at + 2 * step, v);
+    take_tile<E>(w, here, (uint32_t)(at + lane * N), c, p.M, list);
+    if (at + 2 * step < end) here = load_at(x, at + 2 * step, end);
     if (p.M > 0 && (tiles & (tiles - 1)) == 0) look();
     if (at + step >= end) break;
     take_tile<E>(w, next, (uint32_t)(at + step + lane * N), c, p.M, list);
-    if (at + 3 * step < end) load(at + 3 * step, next);
+    if (at + 3 * step < end) next = load_at(x, at + 3 * step, end);
     if (p.M > 0 && (tiles & (tiles + 1)) == 0) look();
   }
-  if (p.M > 0) look();
+  if (p.M > 0 && w.count > kSelected / WAVES) look();  // (else what all have is soon ranked)
   // the wavefronts' sums
   const double ws = wave_sum((double)w.s), wd = wave_sum((double)w.d);
   if (lane == 0) { s_s[wave] = ws; s_d[wave] = wd; s_m[wave] = w.m; s_count[wave] = w.count; }
@@ -520,28 +585,330 @@ template <typename E> __global__ void __launch_bounds__(kBlock) score_join_kerne
                      [&](int rank, u64 key) { write_top(p, r, row, rank, key); });
 }
 
+// ---- the gradient
+// With y_i = (x_i - top) c - log2(e) rest, so that p_i = 2^y_i, an entry's gradient is 2^y (a + b y) and at a token's place its weight / T more.  The
+// rounding of log2(e) rest to fp32 goes into a and b.  The hardware's 2^y is 0 below 2^-126, so it is taken 2^kLift too large: weights may be large too.
+constexpr float kLift = 24.0f;
+struct Weights {
+  float top, shift, c, a, b, inv_t;
+  float line;  // -(top c + shift)
+  int form;    // 0: a 2^(x c + line); 1: with b; 2: whatever the values are
+};
+__device__ __forceinline__ Weights uniform(const Weights &w) {  // (all lanes have the same: in scalar registers)
+  const auto one = [](float v) { return __uint_as_float(__builtin_amdgcn_readfirstlane(__float_as_uint(v))); };
+  return Weights{one(w.top), one(w.shift), one(w.c), one(w.a), one(w.b), one(w.inv_t), one(w.line), __builtin_amdgcn_readfirstlane(w.form)};
+}
+// This lane's share of the sum of a row's token weights.
+__device__ __forceinline__ double token_weights(const ScoreParams &p, long long r) {
+  double sum = 0.0;
+  for (int g = threadIdx.x & 63; g < p.G; g += 64) {
+    const int t = p.tokens[r * p.tok_stride_r + g];
+    if (t >= 0 && t < p.V) sum += (double)p.a[r * p.a_stride_r + g];
+  }
+  return sum;
+}
+__device__ __forceinline__ Weights weights_of(const ScoreParams &p, long long r, double share, double top, double rest, double entropy) {
+  const double sum = wave_sum(share);
+  const double inv_t = 1.0 / (double)p.temp;
+  Weights w = {0.0f, 1000.0f, kLog2e / p.temp, 0.0f, 0.0f, (float)inv_t, 0.0f, 2};
+  if (!(rest > -(double)kInf)) return w;  // (without mass all entries get 0)
+  const double shift = rest / kLn2, at_top = (double)w.c * top;
+  double a = -sum * inv_t, b = 0.0;
+  if (p.b != nullptr) {
+    b = -(double)p.b[r] * kLn2 * inv_t;
+    a -= (double)p.b[r] * entropy * inv_t;
+  }
+  // One multiply-add an entry, x c + line, serves unless top c is so large that fp32 keeps too little of it, and what 2^y loses below 2^-126 counts only with large weights.
+  const bool plain = fabs(at_top) < 65536.0 && fabs(a) + 128.0 * fabs(b) < 1.0;
+  w.top = (float)top;
+  w.line = (float)-(at_top + shift);
+  w.shift = (float)(shift - (double)kLift);
+  // y as it is formed is above the true one by `over`
+  const double over = plain ? at_top + shift + (double)w.line : shift - (double)kLift - (double)w.shift;
+  const double off = 1.0 - over * kLn2 * (1.0 - 0.5 * over * kLn2);  // 2^-over: it is 2^-8 at most
+  a -= b * (plain ? over : over + (double)kLift);
+  w.a = (float)(a * off);
+  w.b = (float)(b * off);
+  w.form = !plain ? 2 : p.b != nullptr ? 1 : 0;
+  return uniform(w);
+}
+
+// From a tile's entries to their gradients, tokens apart.
+__device__ __forceinline__ void entry_gradients(const Weights &w, float (&v)[kPer]) {
+  float t = max3(v[0], v[1], v[2]);
+#pragma unroll
+  for (int i = 3; i + 1 < kPer; i += 2) t = max3(t, v[i], v[i + 1]);
+  t = max3(t, v[kPer - 1], v[kPer - 1]);
+  if (__ballot(!(t <= w.top)) != 0) {  // NaN, +inf (and in a row without mass anything)
+#pragma unroll
+    for (int i = 0; i < kPer; ++i) v[i] = with_mass(v[i]) ? v[i] : -kInf;
+  }
+  if (w.form == 0) {
+#pragma unroll
+    for (int i = 0; i < kPer; ++i) v[i] = __builtin_amdgcn_exp2f(fmaf(v[i], w.c, w.line)) * w.a;
+  } else if (w.form == 1) {
+#pragma unroll
+    for (int i = 0; i < kPer; ++i) {
+      const float y = fmaxf(fmaf(v[i], w.c, w.line), -200.0f);
+      v[i] = __builtin_amdgcn_exp2f(y) * fmaf(y, w.b, w.a);
+    }
+  } else {
+#pragma unroll
+    for (int i = 0; i < kPer; ++i) {
+      const float y = fmaxf(fmaf(v[i] - w.top, w.c, -w.shift), -200.0f);
+      v[i] = __builtin_amdgcn_exp2f(y) * fmaf(y, w.b, w.a) * 0x1p-24f;
+    }
+  }
+}
+// And the tokens that lie in the tile.  `first(u)`: the row's entry that the lane's load u starts with; none lies before `low` or from `high` on.
+template <typename E, typename F>
+__device__ __forceinline__ void token_gradients(const ScoreParams &p, long long r, const Weights &w, const Tile<E> &tile, float (&v)[kPer], int low, int high,
+                                                F first) {
+  constexpr int N = kWide<E>;
+  const int lane = threadIdx.x & 63;
+  for (int g0 = 0; g0 < p.G; g0 += 64) {
+    int token = -1;
+    if (g0 + lane < p.G) token = p.tokens[r * p.tok_stride_r + g0 + lane];
+    u64 hits = __ballot(token >= low && token < high);
+    if (hits == 0) continue;
+    float weight = 0.0f;
+    if (g0 + lane < p.G) weight = p.a[r * p.a_stride_r + g0 + lane] * w.inv_t;
+    float x[kPer];
+    unpack(tile, x);
+    for (; hits != 0; hits &= hits - 1) {
+      const int from = __builtin_ctzll(hits), place = __builtin_amdgcn_readlane(token, from);
+      const float more = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(weight), from));
+#pragma unroll
+      for (int i = 0; i < kPer; ++i)
+        if (place == first(i / N) + i % N && with_mass(x[i])) v[i] += more;
+    }
+  }
+}
+template <typename E> __device__ __forceinline__ void store_tile(E *row, long long at, long long end, const float (&v)[kPer]) {
+  constexpr int N = kWide<E>;
+  const int lane = threadIdx.x & 63;
+#pragma unroll
+  for (int u = 0; u < kPer / N; ++u) {
+    float o[N];
+#pragma unroll
+    for (int i = 0; i < N; ++i) o[i] = v[u * N + i];
+    E *to = row + at + (u * 64 + lane) * N;
+    if (at + 64 * kPer <= end) {
+      stream_some<N>(to, o);
+    } else {
+      const int left = (int)(end - at) - (u * 64 + lane) * N;
+      if (left > 0) stream_first<N>(to, left, o);
+    }
+  }
+}
+
+// From a row's lse and entropy: a tile a wavefront.
 template <typename E> __global__ void __launch_bounds__(kBlock) score_grad_kernel(const ScoreParams p) {
+  const long long r = blockIdx.x / p.chunks;
+  const int part = (int)(blockIdx.x - r * p.chunks), wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const long long at = ((long long)part * (kBlock / 64) + wave) * 64 * kPer;
+  if (at >= p.V) return;
+  const E *x = reinterpret_cast<const E *>(p.x) + r * p.stride_r;
+  const Tile<E> tile = load_at(x, at, p.V);
+  const Weights w = weights_of(p, r, token_weights(p, r), p.lse_in[2 * r], p.lse_in[2 * r + 1], p.b != nullptr ? (double)p.entropy_in[r] : 0.0);
+  float v[kPer];
+  unpack(tile, v);
+  entry_gradients(w, v);
+  const int lane = threadIdx.x & 63, high = (int)(at + 64 * kPer < p.V ? at + 64 * kPer : p.V);
+  token_gradients(p, r, w, tile, v, (int)at, high, [&](int u) { return (int)at + (u * 64 + lane) * kWide<E>; });
+  store_tile(reinterpret_cast<E *>(p.grad) + r * p.grad_stride_r, at, p.V, v);
+}
+
+// Scores and gradient in one pass: a workgroup keeps a row on the chip.  What its wavefronts share:
+template <typename E, int WAVES> struct RowWork {
+  double s_s[WAVES], s_d[WAVES];
+  float s_m[WAVES];
+
+  // The row may be overwritten later: what its tokens need is read at the start.
+  static __device__ __forceinline__ void read_tokens(const ScoreParams &p, long long r, int &token, float &token_x) {
+    const E *x = reinterpret_cast<const E *>(p.x) + r * p.stride_r;
+    token = -1;
+    token_x = -kInf;
+    if (p.logp == nullptr) return;
+    for (int g = threadIdx.x; g < p.G; g += WAVES * 64) {
+      token = p.tokens[r * p.tok_stride_r + g];
+      token_x = token >= 0 && token < p.V ? widen(x[token]) : -kInf;
+      if (p.G > WAVES * 64) p.logp[r * p.G + g] = token_x;
+    }
+  }
+  // From the wavefronts' sums to the scores and what the gradient needs.
+  __device__ __forceinline__ Weights join(const ScoreParams &p, long long r, const Scan<E> &w, int token, float token_x, double share) {
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    double s = wave_sum((double)w.s), d = wave_sum((double)w.d);
+    asm volatile("" : "+v"(token_x));  // (here: not while other wavefronts already write)
+    if (lane == 0) { s_s[wave] = s; s_d[wave] = d; s_m[wave] = w.m; }
+    __syncthreads();
+    const int mine = lane < WAVES ? lane : 0;
+    const float my_top = lane < WAVES ? s_m[mine] : -kInf, top = wave_max(my_top);
+    s = lane < WAVES ? s_s[mine] : 0.0;
+    d = lane < WAVES ? s_d[mine] : 0.0;
+    join_shares(s, d, my_top, top, kLog2e / p.temp);
+    const Row row = row_of(top, s, d, p.temp);
+    if (threadIdx.x == 0) {
+      if (p.lse != nullptr) { p.lse[2 * r] = row.top; p.lse[2 * r + 1] = row.rest; }
+      if (p.entropy != nullptr) p.entropy[r] = (float)row.entropy;
+    }
+    if (p.logp != nullptr)
+      for (int g = threadIdx.x; g < p.G; g += WAVES * 64) {
+        if (p.G > WAVES * 64) {
+          token = p.tokens[r * p.tok_stride_r + g];
+          token_x = p.logp[r * p.G + g];
+        }
+        p.logp[r * p.G + g] = token < 0 ? 0.0f : row.logp(token_x);
+      }
+    return weights_of(p, r, share, row.top, row.rest, row.entropy);
+  }
+};
+
+// Tiles of these kernels: counted from the row's end, tile k of a wavefront is the (k * waves + wave)-th from it, in whole 16-byte loads.  One that would
+// reach beyond the row starts earlier instead: its first entries are another lane's too, count there only, and get the same gradient from both.  (With a
+// case for every entry of a row's end the loops below were so large that they spilled.)  In place it matters that such a tile is read before anything
+// is written: it is the first of its wavefront, which is always kept.
+template <typename E> struct RowTile {
+  static constexpr int N = kWide<E>, kLoads = kPer / N;
+  int at, last;  // the tile's first entry; where a row's last load starts
+  __device__ __forceinline__ int first(int u) const {
+    const int from = at + (u * 64 + (int)(threadIdx.x & 63)) * N;
+    return from < last ? from : last;
+  }
+  template <bool AGAIN> __device__ __forceinline__ Tile<E> load(const E *row) const {  // AGAIN: it is read a second time, soon
+    Tile<E> t;
+#pragma unroll
+    for (int u = 0; u < kLoads; ++u) {
+      const word4_any *from = reinterpret_cast<const word4_any *>(row + first(u));
+      t.w[u] = AGAIN ? *from : __builtin_nontemporal_load(from);
+    }
+    return t;
+  }
+  __device__ __forceinline__ void add_up(const ScoreParams &p, Scan<E> &w, const Tile<E> &tile) const {
+    Tile<E> t = tile;
+    if (at + 64 * kPer > p.V) {  // (uniform) what other lanes have too counts as nothing
+#pragma unroll
+      for (int u = 0; u < kLoads; ++u) {
+        const int others = at + (u * 64 + (int)(threadIdx.x & 63)) * N - first(u);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          if constexpr (sizeof(E) == 2) {
+            uint32_t o = t.w[u][i];
+            o = 2 * i < others ? (o & 0xFFFF0000u) | 0xFF80u : o;
+            t.w[u][i] = 2 * i + 1 < others ? (o & 0xFFFFu) | 0xFF800000u : o;
+          } else {
+            t.w[u][i] = i < others ? 0xFF800000u : t.w[u][i];
+          }
+        }
+      }
+    }
+    take_tile<E>(w, t, 0, kLog2e / p.temp, 0, nullptr);
+    __builtin_amdgcn_sched_barrier(0);
+  }
+  __device__ __forceinline__ void write(const ScoreParams &p, long long r, const Weights &weights, Tile<E> tile) const {
+    // (the compiler would keep the floats of the first pass: twice the registers)
+#pragma unroll
+    for (int u = 0; u < kLoads; ++u) {
+      uint32_t a = tile.w[u].x, b = tile.w[u].y, c = tile.w[u].z, d = tile.w[u].w;
+      asm volatile("" : "+v"(a), "+v"(b), "+v"(c), "+v"(d));
+      tile.w[u] = word4_any{a, b, c, d};
+    }
+    float v[kPer];
+    unpack(tile, v);
+    entry_gradients(weights, v);
+    token_gradients(p, r, weights, tile, v, at < last ? at : last, at + 64 * kPer, [&](int u) { return first(u); });
+    E *row = reinterpret_cast<E *>(p.grad) + r * p.grad_stride_r;
+#pragma unroll
+    for (int u = 0; u < kLoads; ++u) {
+      float o[N];
+#pragma unroll
+      for (int i = 0; i < N; ++i) o[i] = v[u * N + i];
+      stream_some<N>(row + first(u), o);
+    }
+    __builtin_amdgcn_sched_barrier(0);
+  }
+};
+
+// The whole row in registers, TILES tiles a wavefront.
+template <typename E, int WAVES, int TILES>
+__global__ void __launch_bounds__(WAVES * 64, TILES * sizeof(E) > 8 ? 4 : TILES * sizeof(E) > 4 ? 5 : 6) score_row_kernel(const ScoreParams p, int n_tiles) {
+  __shared__ RowWork<E, WAVES> work;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const long long r = blockIdx.x;
   const E *x = reinterpret_cast<const E *>(p.x) + r * p.stride_r;
-  E *out = reinterpret_cast<E *>(p.grad) + r * p.grad_stride_r;
-  const int32_t *tokens = p.tokens + r * p.tok_stride_r;
-  const float *a = p.a + r * p.a_stride_r;
-  const double inv_t = 1.0 / (double)p.temp, top = p.lse_in[2 * r], rest = p.lse_in[2 * r + 1];
-  const float b = p.b != nullptr ? p.b[r] : 0.0f, h = p.b != nullptr ? p.entropy_in[r] : 0.0f;
-  double all = 0.0;
-  for (int g = 0; g < p.G; ++g)
-    if (tokens[g] >= 0 && tokens[g] < p.V) all += (double)a[g];
-  for (int i = threadIdx.x; i < p.V; i += kBlock) {
-    const float v = widen(x[i]);
-    float d = 0.0f;
-    if (with_mass(v)) {
-      const float lp = (float)(((double)v - top) * inv_t - rest), q = expf(lp);
-      d = q > 0.0f ? -q * ((float)all + b * (lp + h)) : 0.0f;
-      for (int g = 0; g < p.G; ++g)
-        if (tokens[g] == i) d += a[g];
-      d *= (float)inv_t;
+  const auto there = [&](int k) { return k * WAVES + wave < n_tiles; };
+  const auto tile = [&](int k) { return RowTile<E>{(n_tiles - 1 - (k * WAVES + wave)) * 64 * kPer, p.V - kWide<E>}; };
+  Tile<E> tiles[TILES];
+#pragma unroll
+  for (int k = 0; k < TILES; ++k)
+    if (there(k)) tiles[k] = tile(k).template load<false>(x);
+  int token;
+  float token_x;
+  work.read_tokens(p, r, token, token_x);
+  const double share = token_weights(p, r);
+  Scan<E> w;
+#pragma unroll
+  for (int k = 0; k < TILES; ++k)
+    if (there(k)) tile(k).add_up(p, w, tiles[k]);
+  const Weights weights = work.join(p, r, w, token, token_x, share);
+#pragma unroll
+  for (int k = 0; k < TILES; ++k)
+    if (there(k)) tile(k).write(p, r, weights, tiles[k]);
+}
+
+// A longer row: a part in registers, a part in LDS, and what is left is read twice, the second time from the caches.
+template <typename E> __global__ void __launch_bounds__(1024) score_long_row_kernel(const ScoreParams p, int n_tiles) {
+  constexpr int kWaves = 16, kLoads = RowTile<E>::kLoads, kRegs = sizeof(E) == 2 ? 8 : 3, kLds = sizeof(E) == 2 ? 4 : 2;
+  __shared__ RowWork<E, kWaves> work;
+  __shared__ word4_any s_tiles[kLds * kWaves * kLoads * 64];
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const long long r = blockIdx.x;
+  const E *x = reinterpret_cast<const E *>(p.x) + r * p.stride_r;
+  const auto there = [&](int k) { return k * kWaves + wave < n_tiles; };
+  const auto tile = [&](int k) { return RowTile<E>{(n_tiles - 1 - (k * kWaves + wave)) * 64 * kPer, p.V - kWide<E>}; };
+  word4_any *mine = s_tiles + wave * kLoads * 64 + lane;
+  int token;
+  float token_x;
+  work.read_tokens(p, r, token, token_x);
+  const double share = token_weights(p, r);
+  Scan<E> w;
+  // (what registers keep comes last, so that they are free until then)
+  Tile<E> next;
+  int k = kRegs;
+  if (there(k)) next = tile(k).template load<true>(x);
+  for (; there(k); ++k) {
+    const Tile<E> here = next;
+    if (there(k + 1)) next = tile(k + 1).template load<true>(x);
+    if (k < kRegs + kLds) {
+#pragma unroll
+      for (int u = 0; u < kLoads; ++u) mine[((k - kRegs) * kWaves * kLoads + u) * 64] = here.w[u];
     }
-    out[i] = narrow<E>(d);
+    tile(k).add_up(p, w, here);
+  }
+  Tile<E> tiles[kRegs];
+#pragma unroll
+  for (int k = 0; k < kRegs; ++k)
+    if (there(k)) tiles[k] = tile(k).template load<false>(x);
+#pragma unroll
+  for (int k = 0; k < kRegs; ++k)
+    if (there(k)) tile(k).add_up(p, w, tiles[k]);
+  const Weights weights = work.join(p, r, w, token, token_x, share);
+#pragma unroll
+  for (int k = 0; k < kRegs; ++k)
+    if (there(k)) tile(k).write(p, r, weights, tiles[k]);
+  k = kRegs + kLds;
+  if (there(k)) next = tile(k).template load<false>(x);
+  for (int l = kRegs; l < kRegs + kLds && there(l); ++l) {
+    Tile<E> here;
+#pragma unroll
+    for (int u = 0; u < kLoads; ++u) here.w[u] = mine[((l - kRegs) * kWaves * kLoads + u) * 64];
+    tile(l).write(p, r, weights, here);
+  }
+  for (; there(k); ++k) {
+    const Tile<E> here = next;
+    if (there(k + 1)) next = tile(k + 1).template load<false>(x);
+    tile(k).write(p, r, weights, here);
   }
 }
 
@@ -569,6 +936,32 @@ void split_rows(ScoreParams &p, long long want) {
   p.chunks = (int)((p.V + each - 1) / each);
 }
 
+template <typename E> hipError_t launch_gradient(ScoreParams p, hipStream_t st) {
+  p.chunks = (int)((p.V + kBlock * kPer - 1) / (kBlock * kPer));
+  score_grad_kernel<E><<<(unsigned)(p.R * p.chunks), kBlock, 0, st>>>(p);
+  return hipGetLastError();
+}
+
+// Scores and gradient in one launch, where a row fits.  False: it does not.
+#ifndef LONGR
+#define LONGR 64
+#endif
+template <typename E> bool launch_rows(const ScoreParams &p, hipStream_t st) {
+  const long long tiles = (p.V + 64 * kPer - 1) / (64 * kPer);
+  constexpr bool kHalf = sizeof(E) == 2;
+  const unsigned rows = (unsigned)p.R;
+  if (p.V < kWide<E>) return false;
+  if (tiles <= 1) score_row_kernel<E, 1, 1><<<rows, 64, 0, st>>>(p, (int)tiles);
+  else if (tiles <= 4) score_row_kernel<E, 4, 1><<<rows, 256, 0, st>>>(p, (int)tiles);
+  else if (tiles <= 8) score_row_kernel<E, 4, 2><<<rows, 256, 0, st>>>(p, (int)tiles);
+  else if (tiles <= 16) score_row_kernel<E, 4, 4><<<rows, 256, 0, st>>>(p, (int)tiles);
+  else if (tiles <= 32) score_row_kernel<E, kHalf ? 4 : 8, kHalf ? 8 : 4><<<rows, kHalf ? 256 : 512, 0, st>>>(p, (int)tiles);
+  else if (kHalf && tiles <= 64) score_row_kernel<E, 8, kHalf ? 8 : 4><<<rows, 512, 0, st>>>(p, (int)tiles);
+  else if (p.R >= LONGR) score_long_row_kernel<E><<<rows, 1024, 0, st>>>(p, (int)tiles);
+  else return false;
+  return true;
+}
+
 template <typename E> hipError_t launch_scores(const ScoreParams &p, hipStream_t st) {
   const unsigned blocks = (unsigned)(p.R * p.chunks);
   const long long tiles = (p.chunk + 64 * kPer - 1) / (64 * kPer);
@@ -577,8 +970,7 @@ template <typename E> hipError_t launch_scores(const ScoreParams &p, hipStream_t
 #else
   if (tiles <= 1) score_kernel<E, 1><<<blocks, 64, 0, st>>>(p);
   else if (tiles <= 4 || blocks > 512) score_kernel<E, 4><<<blocks, 256, 0, st>>>(p);
-  else if (blocks > 256) score_kernel<E, 8><<<blocks, 512, 0, st>>>(p);
-  else score_kernel<E, 16><<<blocks, 1024, 0, st>>>(p);
+  else score_kernel<E, 8><<<blocks, 512, 0, st>>>(p);
 #endif
   hipError_t e = hipGetLastError();
   if (e != hipSuccess || p.chunks == 1) return e;
@@ -642,7 +1034,7 @@ extern "C" int llc_token_logprobs_grad(const llc_token_logprobs_grad_args *a) {
   const long long split = a->v_chunks > 0 ? a->v_chunks : auto_split(a->R, a->V);
   if (a->lse_in == nullptr && (a->workspace == nullptr || !fits(a->workspace, 256) || a->workspace_bytes < rows_workspace(a->R, 0, split)))
     return LLC_E_WORKSPACE;
-  if (a->R * split > kMostGrid) return LLC_E_SHAPE;
+  if (a->R * split > kMostGrid || a->R * ((a->V + kBlock * kPer - 1) / (kBlock * kPer)) > kMostGrid) return LLC_E_SHAPE;
   if ((a->flags & LLC_FLAG_DRY_RUN) != 0) return LLC_OK;
   ScoreParams p = {};
   p.R = a->R; p.V = (int)a->V; p.G = (int)a->G; p.M = 0;
@@ -660,12 +1052,12 @@ extern "C" int llc_token_logprobs_grad(const llc_token_logprobs_grad_args *a) {
   p.entropy_in = a->lse_in != nullptr ? a->entropy_in : p.entropy;
   hipStream_t st = (hipStream_t)a->stream;
   return between_events(a->ev_begin, a->ev_end, st, [&] {
+    const bool f32 = a->dtype == LLC_F32;
     if (a->lse_in == nullptr) {
-      const hipError_t e = a->dtype == LLC_F32 ? launch_scores<float>(p, st) : launch_scores<uint16_t>(p, st);
+      if (a->v_chunks == 0 && (f32 ? launch_rows<float>(p, st) : launch_rows<uint16_t>(p, st))) return hipGetLastError();
+      const hipError_t e = f32 ? launch_scores<float>(p, st) : launch_scores<uint16_t>(p, st);
       if (e != hipSuccess) return e;
     }
-    if (a->dtype == LLC_F32) score_grad_kernel<float><<<(unsigned)p.R, kBlock, 0, st>>>(p);
-    else score_grad_kernel<uint16_t><<<(unsigned)p.R, kBlock, 0, st>>>(p);
-    return hipGetLastError();
+    return f32 ? launch_gradient<float>(p, st) : launch_gradient<uint16_t>(p, st);
   });
 }
