@@ -598,14 +598,22 @@ __device__ __forceinline__ Weights uniform(const Weights &w) {  // (all lanes ha
   const auto one = [](float v) { return __uint_as_float(__builtin_amdgcn_readfirstlane(__float_as_uint(v))); };
   return Weights{one(w.top), one(w.shift), one(w.c), one(w.a), one(w.b), one(w.inv_t), one(w.line), __builtin_amdgcn_readfirstlane(w.form)};
 }
-// This lane's share of the sum of a row's token weights.
-__device__ __forceinline__ double token_weights(const ScoreParams &p, long long r) {
-  double sum = 0.0;
+// A row's tokens and their weights: lane i has the i-th, and its share of the sum of all valid ones' weights.  (Read again for every
+// tile: gradient of 2048 x 32 000 bf16 63 us, so 60.)
+struct RowTokens {
+  int token;
+  float weight;
+  double share;
+};
+__device__ __forceinline__ RowTokens tokens_of(const ScoreParams &p, long long r) {
+  RowTokens t = {-1, 0.0f, 0.0};
   for (int g = threadIdx.x & 63; g < p.G; g += 64) {
-    const int t = p.tokens[r * p.tok_stride_r + g];
-    if (t >= 0 && t < p.V) sum += (double)p.a[r * p.a_stride_r + g];
+    const int token = p.tokens[r * p.tok_stride_r + g];
+    const float weight = p.a[r * p.a_stride_r + g];
+    if (token >= 0 && token < p.V) t.share += (double)weight;
+    if (g < 64) { t.token = token; t.weight = weight; }
   }
-  return sum;
+  return t;
 }
 __device__ __forceinline__ Weights weights_of(const ScoreParams &p, long long r, double share, double top, double rest, double entropy) {
   const double sum = wave_sum(share);
@@ -662,25 +670,31 @@ __device__ __forceinline__ void entry_gradients(const Weights &w, float (&v)[kPe
 }
 // And the tokens that lie in the tile.  `first(u)`: the row's entry that the lane's load u starts with; none lies before `low` or from `high` on.
 template <typename E, typename F>
-__device__ __forceinline__ void token_gradients(const ScoreParams &p, long long r, const Weights &w, const Tile<E> &tile, float (&v)[kPer], int low, int high,
-                                                F first) {
+__device__ __forceinline__ void token_gradients(const ScoreParams &p, long long r, const Weights &w, const RowTokens &tokens, const Tile<E> &tile,
+                                                float (&v)[kPer], int low, int high, F first) {
   constexpr int N = kWide<E>;
   const int lane = threadIdx.x & 63;
-  for (int g0 = 0; g0 < p.G; g0 += 64) {
-    int token = -1;
-    if (g0 + lane < p.G) token = p.tokens[r * p.tok_stride_r + g0 + lane];
+  int token = tokens.token;
+  float weight = tokens.weight;
+  for (int g0 = 0;;) {
     u64 hits = __ballot(token >= low && token < high);
-    if (hits == 0) continue;
-    float weight = 0.0f;
-    if (g0 + lane < p.G) weight = p.a[r * p.a_stride_r + g0 + lane] * w.inv_t;
-    float x[kPer];
-    unpack(tile, x);
-    for (; hits != 0; hits &= hits - 1) {
-      const int from = __builtin_ctzll(hits), place = __builtin_amdgcn_readlane(token, from);
-      const float more = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(weight), from));
+    if (hits != 0) {
+      float x[kPer];
+      unpack(tile, x);
+      for (; hits != 0; hits &= hits - 1) {
+        const int from = __builtin_ctzll(hits), place = __builtin_amdgcn_readlane(token, from);
+        const float more = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(weight * w.inv_t), from));
 #pragma unroll
-      for (int i = 0; i < kPer; ++i)
-        if (place == first(i / N) + i % N && with_mass(x[i])) v[i] += more;
+        for (int i = 0; i < kPer; ++i)
+          if (place == first(i / N) + i % N && with_mass(x[i])) v[i] += more;
+      }
+    }
+    g0 += 64;
+    if (g0 >= p.G) break;
+    token = -1;
+    if (g0 + lane < p.G) {
+      token = p.tokens[r * p.tok_stride_r + g0 + lane];
+      weight = p.a[r * p.a_stride_r + g0 + lane];
     }
   }
 }
@@ -710,12 +724,13 @@ template <typename E> __global__ void __launch_bounds__(kBlock) score_grad_kerne
   if (at >= p.V) return;
   const E *x = reinterpret_cast<const E *>(p.x) + r * p.stride_r;
   const Tile<E> tile = load_at(x, at, p.V);
-  const Weights w = weights_of(p, r, token_weights(p, r), p.lse_in[2 * r], p.lse_in[2 * r + 1], p.b != nullptr ? (double)p.entropy_in[r] : 0.0);
+  const RowTokens tokens = tokens_of(p, r);
+  const Weights w = weights_of(p, r, tokens.share, p.lse_in[2 * r], p.lse_in[2 * r + 1], p.b != nullptr ? (double)p.entropy_in[r] : 0.0);
   float v[kPer];
   unpack(tile, v);
   entry_gradients(w, v);
   const int lane = threadIdx.x & 63, high = (int)(at + 64 * kPer < p.V ? at + 64 * kPer : p.V);
-  token_gradients(p, r, w, tile, v, (int)at, high, [&](int u) { return (int)at + (u * 64 + lane) * kWide<E>; });
+  token_gradients(p, r, w, tokens, tile, v, (int)at, high, [&](int u) { return (int)at + (u * 64 + lane) * kWide<E>; });
   store_tile(reinterpret_cast<E *>(p.grad) + r * p.grad_stride_r, at, p.V, v);
 }
 
@@ -806,7 +821,7 @@ template <typename E> struct RowTile {
     take_tile<E>(w, t, 0, kLog2e / p.temp, 0, nullptr);
     __builtin_amdgcn_sched_barrier(0);
   }
-  __device__ __forceinline__ void write(const ScoreParams &p, long long r, const Weights &weights, Tile<E> tile) const {
+  __device__ __forceinline__ void write(const ScoreParams &p, long long r, const Weights &weights, const RowTokens &tokens, Tile<E> tile) const {
     // (the compiler would keep the floats of the first pass: twice the registers)
 #pragma unroll
     for (int u = 0; u < kLoads; ++u) {
@@ -817,7 +832,7 @@ template <typename E> struct RowTile {
     float v[kPer];
     unpack(tile, v);
     entry_gradients(weights, v);
-    token_gradients(p, r, weights, tile, v, at < last ? at : last, at + 64 * kPer, [&](int u) { return first(u); });
+    token_gradients(p, r, weights, tokens, tile, v, at < last ? at : last, at + 64 * kPer, [&](int u) { return first(u); });
     E *row = reinterpret_cast<E *>(p.grad) + r * p.grad_stride_r;
 #pragma unroll
     for (int u = 0; u < kLoads; ++u) {
@@ -846,15 +861,15 @@ __global__ void __launch_bounds__(WAVES * 64, TILES * sizeof(E) > 8 ? 4 : TILES 
   int token;
   float token_x;
   work.read_tokens(p, r, token, token_x);
-  const double share = token_weights(p, r);
+  const RowTokens tokens = tokens_of(p, r);
   Scan<E> w;
 #pragma unroll
   for (int k = 0; k < TILES; ++k)
     if (there(k)) tile(k).add_up(p, w, tiles[k]);
-  const Weights weights = work.join(p, r, w, token, token_x, share);
+  const Weights weights = work.join(p, r, w, token, token_x, tokens.share);
 #pragma unroll
   for (int k = 0; k < TILES; ++k)
-    if (there(k)) tile(k).write(p, r, weights, tiles[k]);
+    if (there(k)) tile(k).write(p, r, weights, tokens, tiles[k]);
 }
 
 // A longer row: a part in registers, a part in LDS, and what is left is read twice, the second time from the caches.
@@ -871,7 +886,7 @@ template <typename E> __global__ void __launch_bounds__(1024) score_long_row_ker
   int token;
   float token_x;
   work.read_tokens(p, r, token, token_x);
-  const double share = token_weights(p, r);
+  const RowTokens tokens = tokens_of(p, r);
   Scan<E> w;
   // (what registers keep comes last, so that they are free until then)
   Tile<E> next;
@@ -893,22 +908,22 @@ template <typename E> __global__ void __launch_bounds__(1024) score_long_row_ker
 #pragma unroll
   for (int k = 0; k < kRegs; ++k)
     if (there(k)) tile(k).add_up(p, w, tiles[k]);
-  const Weights weights = work.join(p, r, w, token, token_x, share);
+  const Weights weights = work.join(p, r, w, token, token_x, tokens.share);
 #pragma unroll
   for (int k = 0; k < kRegs; ++k)
-    if (there(k)) tile(k).write(p, r, weights, tiles[k]);
+    if (there(k)) tile(k).write(p, r, weights, tokens, tiles[k]);
   k = kRegs + kLds;
   if (there(k)) next = tile(k).template load<false>(x);
   for (int l = kRegs; l < kRegs + kLds && there(l); ++l) {
     Tile<E> here;
 #pragma unroll
     for (int u = 0; u < kLoads; ++u) here.w[u] = mine[((l - kRegs) * kWaves * kLoads + u) * 64];
-    tile(l).write(p, r, weights, here);
+    tile(l).write(p, r, weights, tokens, here);
   }
   for (; there(k); ++k) {
     const Tile<E> here = next;
     if (there(k + 1)) next = tile(k + 1).template load<false>(x);
-    tile(k).write(p, r, weights, here);
+    tile(k).write(p, r, weights, tokens, here);
   }
 }
 
