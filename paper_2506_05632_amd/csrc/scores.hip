@@ -206,7 +206,7 @@ template <typename E> __device__ __forceinline__ void take_tile(Scan<E> &w, cons
     return max3(half[0], half[1], half[1]);
   };
   float t = largest();
-  if (__ballot(!(t <= w.bound)) != 0) {  // (a NaN comes here too)
+  if (__ballot(!(t <= fminf(w.bound, w.m))) != 0) {  // (a NaN comes here too; where few entries are, the bound may be above them all)
     if (__ballot(!(t < kInf)) != 0) {    // entries without mass
 #pragma unroll
       for (int i = 0; i < kPer; ++i) v[i] = with_mass(v[i]) ? v[i] : -kInf;
@@ -314,7 +314,7 @@ __device__ __forceinline__ float just_below(uint32_t o) {
 
 // A wavefront looks at its list: it says what `share` of its entries reach and, told what M of the row's entries reach then, drops the others.
 // K: 64ths of the list that are in use.
-template <int K> __device__ __forceinline__ float look_at_list(u64 *list, int &count, int share, uint32_t *said, int waves, int wave) {
+template <int K> __device__ __forceinline__ float look_at_list(u64 *list, int &count, int share, bool speaks, uint32_t *said, int waves, int wave) {
   const int lane = threadIdx.x & 63;
   u64 k[K];
   uint32_t o[K];
@@ -323,8 +323,10 @@ template <int K> __device__ __forceinline__ float look_at_list(u64 *list, int &c
     k[i] = i * 64 + lane < count ? list[i * 64 + lane] : 0;
     o[i] = (uint32_t)(k[i] >> 32);
   }
-  const uint32_t nth = reached_by(o, share);
-  if (lane == 0) said[wave] = nth;
+  if (speaks) {
+    const uint32_t nth = reached_by(o, share);
+    if (lane == 0) said[wave] = nth;
+  }
   const uint32_t all = least_said(said, waves);
   count = 0;
 #pragma unroll
@@ -505,7 +507,10 @@ template <typename E, int WAVES> __global__ void __launch_bounds__(WAVES * 64) s
   }
   // A bound that M entries reach: every wavefront's share of them is among what it has seen.  First each lane's largest of the first tile; later,
   // whenever a wavefront has seen twice as much, the candidates in its list.  What a wavefront has once said stays true, so nobody waits.
-  const int share = (p.M + WAVES - 1) / WAVES;
+  // (Of wavefronts whose first tile is whole: one with a few entries, or none, would have nothing to say.)
+  const int whole = (int)((end - begin) / kTile), speakers = whole < 1 ? 1 : whole < WAVES ? whole : WAVES;
+  const bool speaks = wave < speakers;
+  const int share = (p.M + speakers - 1) / speakers;
   if (p.M > 0) {
     float t = -kInf;
     if (at < end) {
@@ -514,15 +519,15 @@ template <typename E, int WAVES> __global__ void __launch_bounds__(WAVES * 64) s
 #pragma unroll
       for (int i = 0; i < kPer; ++i) t = fmaxf(t, with_mass(v[i]) ? v[i] : -kInf);
     }
-    const uint32_t o[1] = {ordered(t)}, nth = share <= 64 ? reached_by(o, share) : 0;
+    const uint32_t o[1] = {ordered(t)}, nth = !speaks ? 0xFFFFFFFFu : share <= 64 ? reached_by(o, share) : 0;
     if (lane == 0) s_nth[wave] = nth;
     __syncthreads();
     w.bound = just_below(least_said(s_nth, WAVES));
   }
   const auto look = [&] {
     if (w.count < share) return;
-    w.bound = fmaxf(w.bound, w.count <= 64 ? look_at_list<1>(list, w.count, share, s_nth, WAVES, wave)
-                                           : look_at_list<kList / 64>(list, w.count, share, s_nth, WAVES, wave));
+    w.bound = fmaxf(w.bound, w.count <= 64 ? look_at_list<1>(list, w.count, share, speaks, s_nth, WAVES, wave)
+                                           : look_at_list<kList / 64>(list, w.count, share, speaks, s_nth, WAVES, wave));
   };
   // two tiles in turn, so that one is on its way while the other is taken
   const long long step = (long long)WAVES * kTile;
@@ -580,8 +585,17 @@ template <typename E> __global__ void __launch_bounds__(kBlock) score_join_kerne
   write_scores<E>(p, r, row, 0, kBlock);
   if (p.M == 0) return;
   if ((int)threadIdx.x < p.chunks) s_count[threadIdx.x] = share.count;
+  // M keys reach the least that a chunk with M has
+  const u64 *keys = p.keys + r * p.chunks * p.M;
+  u64 least = lane < p.chunks && share.count == p.M ? keys[lane * p.M + p.M - 1] : 0;
+#pragma unroll
+  for (int i = 32; i >= 1; i >>= 1) {
+    const u64 other = __shfl_xor(least, i);
+    least = other > least ? other : least;
+  }
+  least = least != 0 ? least : 1;
   __syncthreads();
-  select_top<kBlock>(p.keys + r * p.chunks * p.M, p.chunks, p.M, s_count, 1, key_of(top > -kInf ? top : 0.0f, 0), p.M,
+  select_top<kBlock>(keys, p.chunks, p.M, s_count, least, key_of(top > -kInf ? top : 0.0f, 0), p.M,
                      [&](int rank, u64 key) { write_top(p, r, row, rank, key); });
 }
 
@@ -938,11 +952,14 @@ size_t rows_workspace(long long R, long long M, long long chunks) {  // shares a
   return (size_t)chunks * (size_t)R * (sizeof(Share) + 8 * (size_t)M) + 32 * (size_t)R + 512;
 }
 
-// Workgroups that a row is split over.
-#ifndef SPLIT
-#define SPLIT 1
-#endif
-int auto_split(long long R, long long V) { return SPLIT; }
+// Workgroups that a row is split over: as many as leave each 16 000 entries, as far as there are CUs for them, if that is three or more: the second launch takes
+// some 3 us.  us a call of 50 alternatives, whole and split: 1 x 128 256 fp32 28, 19 (8); 64 x 128 256 32, 25 (4); 128 x 152 064 bf16 34, 30 (2, not taken);
+// 4 x 32 000 bf16 15.7, 18.0 (2, not taken); 1 x 4 194 304 fp32 405, 43 (64).
+int auto_split(long long R, long long V) {
+  long long split = V / 16000;
+  if (split > 256 / (R > 0 ? R : 1)) split = 256 / (R > 0 ? R : 1);
+  return (int)(split < 3 ? 1 : split < kMostSplit ? split : kMostSplit);
+}
 
 // Cuts a row into `want` chunks of whole 16-byte loads.
 void split_rows(ScoreParams &p, long long want) {
