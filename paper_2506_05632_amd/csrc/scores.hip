@@ -231,9 +231,13 @@ template <typename E> __device__ __forceinline__ void take_tile(Scan<E> &w, cons
 #pragma unroll
         for (int h = 0; h < 2; ++h) {
           if (__ballot(half[h] > w.bound) == 0) continue;
+          u64 masks[kPer];  // (all comparisons first: none waits for the branch before it)
+#pragma unroll
+          for (int i = h * (kPer / 2); i < (h + 1) * (kPer / 2); ++i) masks[i] = __ballot(v[i] > w.bound);
+          __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
           for (int i = h * (kPer / 2); i < (h + 1) * (kPer / 2); ++i) {
-            const u64 mask = __ballot(v[i] > w.bound);
+            const u64 mask = masks[i];
             if (mask == 0) continue;
             if (v[i] > w.bound) list[w.count + lanes_below(mask)] = key_of(v[i], first + (i / N) * 64 * N + i % N);
             w.count += (int)__builtin_popcountll(mask);
@@ -261,19 +265,22 @@ template <typename E> __device__ __forceinline__ void take_tile(Scan<E> &w, cons
       }
     }
   }
-  const auto add = [&](float d) {
+  float s[2] = {w.s, 0.0f}, sd[2] = {w.d, 0.0f};  // (two sums of either kind, so that one's additions do not wait for each other)
+  const auto add = [&](int i, float d) {
     const float e = __builtin_amdgcn_exp2f(d);  // (no mass: 2^-200 is 0)
-    w.s += e;
-    w.d = fmaf(e, d, w.d);
+    s[i & 1] += e;
+    sd[i & 1] = fmaf(e, d, sd[i & 1]);
   };
   if (has_reference(w.m, c)) {  // (not where nothing has had mass yet)
     const float reference = reference_of(w.m, c);
 #pragma unroll
-    for (int i = 0; i < kPer; ++i) add(fmaxf(fmaf(v[i], c, -reference), -200.0f));
+    for (int i = 0; i < kPer; ++i) add(i, fmaxf(fmaf(v[i], c, -reference), -200.0f));
   } else {
 #pragma unroll
-    for (int i = 0; i < kPer; ++i) add(fmaxf((v[i] - w.m) * c, -200.0f));
+    for (int i = 0; i < kPer; ++i) add(i, fmaxf((v[i] - w.m) * c, -200.0f));
   }
+  w.s = s[0] + s[1];
+  w.d = sd[0] + sd[1];
 }
 
 // A number that n of the lanes' K ordered values each reach, and little below the n-th largest of them (its upper 16 bits); 0 if there are fewer than n.
