@@ -4,7 +4,7 @@
 // Gradient: grad[n] = scale * sum over t with tokens[t] == n of g[t].  Floating-point atomics would make the sums' order,
 // and so their bits, a matter of timing; instead the positions are sorted by token first (a stable counting sort), and a row of the
 // gradient is one wavefront's, or several wavefronts' by columns, which adds its tokens' rows up in registers in the order of their positions, in fp32, and
-// writes it once.  Rows that no token names are written as zeros by the same launch.
+// writes it once.  Rows that no token names are written as zeros by a launch of their own.
 // Tokens as in text name a few rows very often: a row of more than kWindow tokens is added up by windows of kWindow
 // sorted positions, each a wavefront's, whose partial sums (fp32, in the workspace) a last launch joins.  A window touches at most
 // two such rows, the one it starts in and the one it ends in, so two partial rows a window are room enough, and a window's place
@@ -167,57 +167,91 @@ template <int WAVES> __global__ void __launch_bounds__(WAVES * 64) embed_sort_ke
 }
 
 // ---- sums
-// The next K of the places whose positions lane i of t holds.  (ALL: the N columns are there.  The choice is made once, outside: made at
-// every load it would make each wait for the one before.)
+// The N columns that a lane adds up.  Every lane of a wavefront stays at work, also one whose columns lie past the end: the rows' numbers are read
+// out of the lanes, and a lane that a branch has left holds nothing that could be relied on.  So a lane that the end cuts short, or that
+// lies past it, adds up the row's last N columns and keeps what is its own of them.
+template <int N> struct Columns {
+  long long first;  // the columns that are read
+  long long mine;   // the lane's own begin here (at `first`, or after it)
+  long long left;   // columns from `first` on
+};
+// ALL: rows have N columns at least.
+template <bool ALL, int N> __device__ __forceinline__ Columns<N> columns_at(long long d, long long D) {
+  const long long first = ALL && d > D - N ? D - N : d;
+  return Columns<N>{first, d, D - first};
+}
+template <bool ALL, int N, typename B> __device__ __forceinline__ void load_columns(const B *row, const Columns<N> &c, float (&v)[N]) {
+  if constexpr (ALL) load_some<N>(row + c.first, v);
+  else load_first<N>(row + c.first, c.left, v);
+}
+template <int N, bool STREAM, typename B> __device__ __forceinline__ void store_columns(B *row, const Columns<N> &c, const float (&v)[N]) {
+  if (c.first == c.mine && c.left >= N) {
+    if constexpr (STREAM) stream_some<N>(row + c.first, v);
+    else store_some<N>(row + c.first, v);
+    return;
+  }
+#pragma unroll
+  for (int i = 0; i < N; ++i)
+    if (c.first + i >= c.mine && i < c.left) row[c.first + i] = narrow<B>(v[i]);
+}
+
+// The next K of the places whose positions lane i of t holds.
 template <bool ALL, int K, typename A, int N>
-__device__ __forceinline__ void add_some(const EmbedParams &p, const A *g, long long left, int t, int &j, float (&sum)[N]) {
+__device__ __forceinline__ void add_some(const EmbedParams &p, const Columns<N> &c, int t, int &j, float (&sum)[N]) {
   float v[K][N];
 #pragma unroll
-  for (int u = 0; u < K; ++u) {
-    const A *from = g + (long long)__builtin_amdgcn_readlane(t, j + u) * p.from_stride;
-    if (ALL) load_some<N>(from, v[u]);
-    else load_first<N>(from, left, v[u]);
-  }
+  for (int u = 0; u < K; ++u)
+    load_columns<ALL, N>(reinterpret_cast<const A *>(p.from) + (long long)__builtin_amdgcn_readlane(t, j + u) * p.from_stride, c, v[u]);
 #pragma unroll
   for (int u = 0; u < K; ++u)
 #pragma unroll
     for (int i = 0; i < N; ++i) sum[i] += v[u][i];
   j += K;
 }
+// The rows of g at n places, at most 64, in the order of the positions, which the lanes of t hold.
 template <bool ALL, typename A, int N>
-__device__ __forceinline__ void add_all(const EmbedParams &p, const A *g, long long left, int t, int n, float (&sum)[N]) {
+__device__ __forceinline__ void add_positions(const EmbedParams &p, const Columns<N> &c, int t, int n, float (&sum)[N]) {
   int j = 0;
-  while (n - j >= kAhead) add_some<ALL, kAhead>(p, g, left, t, j, sum);
-  if (n - j >= 2) add_some<ALL, 2>(p, g, left, t, j, sum);
-  if (n - j >= 1) add_some<ALL, 1>(p, g, left, t, j, sum);
+  while (n - j >= kAhead) add_some<ALL, kAhead, A, N>(p, c, t, j, sum);
+  if (n - j >= 2) add_some<ALL, 2, A, N>(p, c, t, j, sum);
+  if (n - j >= 1) add_some<ALL, 1, A, N>(p, c, t, j, sum);
 }
 
-// The rows of g at places [from, from + n), n at most 64, N columns from d on, in the order of the positions.
-// `t`: lane i holds place from + i's position.
-template <typename A, int N>
-__device__ __forceinline__ void add_positions(const EmbedParams &p, int t, int n, long long d, float (&sum)[N]) {
-  const A *g = reinterpret_cast<const A *>(p.from) + d;
-  if (p.D - d >= N) add_all<true>(p, g, p.D - d, t, n, sum);
-  else add_all<false>(p, g, p.D - d, t, n, sum);
-}
-
-template <typename B, int N>
-__device__ __forceinline__ void read_row(const EmbedParams &p, long long row, long long d, float (&before)[N]) {
-  if (p.add != 0) load_first<N>(reinterpret_cast<const B *>(p.to) + row * p.to_stride + d, p.D - d, before);
-}
-template <typename B, int N>
-__device__ __forceinline__ void write_row(const EmbedParams &p, long long row, long long d, const float (&before)[N], float (&sum)[N]) {
-  B *to = reinterpret_cast<B *>(p.to) + row * p.to_stride + d;
+// What a row of the gradient becomes.
+template <int N> __device__ __forceinline__ void add_scaled(const EmbedParams &p, const float (&before)[N], float (&sum)[N]) {
 #pragma unroll
   for (int i = 0; i < N; ++i) sum[i] = p.add != 0 ? fmaf(sum[i], p.scale, before[i]) : sum[i] * p.scale;
-  stream_first<N>(to, p.D - d, sum);
+}
+
+// A wavefront's columns of one row, or of a window's share of a row, whose n positions lane i of t holds.
+template <bool ALL, typename A>
+__device__ __forceinline__ void sum_window(const EmbedParams &p, float *to, int t, int n, long long d0, long long step, int lane) {
+  constexpr int N = kWide<A>;
+  for (long long d = d0; d < p.D; d += step) {  // (uniform)
+    const Columns<N> c = columns_at<ALL, N>(d + lane * N, p.D);
+    float sum[N] = {};
+    add_positions<ALL, A, N>(p, c, t, n, sum);
+    store_columns<N, false>(to, c, sum);
+  }
+}
+template <bool ALL, typename A, typename B>
+__device__ __forceinline__ void sum_row(const EmbedParams &p, B *to, int t, int n, long long d0, long long step, int lane) {
+  constexpr int N = kWide<A>;
+  for (long long d = d0; d < p.D; d += step) {  // (uniform)
+    const Columns<N> c = columns_at<ALL, N>(d + lane * N, p.D);
+    float sum[N] = {}, before[N] = {};
+    if (p.add != 0) load_columns<ALL, N>(to, c, before);
+    add_positions<ALL, A, N>(p, c, t, n, sum);
+    add_scaled<N>(p, before, sum);
+    store_columns<N, true>(to, c, sum);
+  }
 }
 
 template <typename A, typename B> __global__ void __launch_bounds__(kBlock) embed_sum_kernel(const EmbedParams p) {
   constexpr int N = kWide<A>;
   const int in_block = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
   const long long wave = (long long)blockIdx.x * (kBlock / 64) + in_block, step = 64LL * N << p.team_log;
-  const long long item = wave >> p.team_log, d0 = ((wave & ((1 << p.team_log) - 1)) * 64 + lane) * N;
+  const long long item = wave >> p.team_log, d0 = (wave & ((1 << p.team_log) - 1)) * 64 * N;
   const long long windows = (long long)p.window_blocks * (kBlock / 64) >> p.team_log,
                   sums = (long long)p.sum_blocks * (kBlock / 64) >> p.team_log;
   if (blockIdx.x < p.window_blocks) {
@@ -237,11 +271,8 @@ template <typename A, typename B> __global__ void __launch_bounds__(kBlock) embe
       float *to = p.partial + (item * 2 + slot) * p.D;
       const int skip = slot == 0 ? 0 : (int)(b_begin - begin), upto = slot == 0 && a_end - begin < n ? (int)(a_end - begin) : n;
       const int t = __shfl(mine.t, lane + skip);
-      for (long long d = d0; d < p.D; d += step) {
-        float sum[N] = {};
-        add_positions<A, N>(p, t, upto - skip, d, sum);
-        store_first<N>(to + d, p.D - d, sum);
-      }
+      if (p.D >= N) sum_window<true, A>(p, to, t, upto - skip, d0, step, lane);
+      else sum_window<false, A>(p, to, t, upto - skip, d0, step, lane);
     }
     return;
   }
@@ -253,13 +284,9 @@ template <typename A, typename B> __global__ void __launch_bounds__(kBlock) embe
     if (n >= total) return;
     const int count = __builtin_amdgcn_readfirstlane(mine.count);
     if (__builtin_amdgcn_readfirstlane(mine.start) != n || count > kWindow) continue;
-    const int row = __builtin_amdgcn_readfirstlane(mine.row);
-    for (long long d = d0; d < p.D; d += step) {
-      float sum[N] = {}, before[N] = {};
-      read_row<B, N>(p, row, d, before);
-      add_positions<A, N>(p, mine.t, count, d, sum);
-      write_row<B, N>(p, row, d, before, sum);
-    }
+    B *to = reinterpret_cast<B *>(p.to) + (long long)__builtin_amdgcn_readfirstlane(mine.row) * p.to_stride;
+    if (p.D >= N) sum_row<true, A>(p, to, mine.t, count, d0, step, lane);
+    else sum_row<false, A>(p, to, mine.t, count, d0, step, lane);
   }
 }
 
@@ -276,7 +303,6 @@ __global__ void __launch_bounds__(kBlock) embed_zero_kernel(const int32_t *start
   const float none[kStore] = {};
   if (d < D) stream_first<kStore>(to + row * to_stride + d, D - d, none);
 }
-
 
 // Joins the windows of long rows.  A wavefront looks whether a long row starts in its window; the workgroup then takes such
 // rows one after the other, 256 columns of them, every sixteenth window a wavefront, in an order that follows from the row's place alone.
@@ -306,7 +332,8 @@ template <typename B> __global__ void __launch_bounds__(kJoinThreads) embed_join
     for (long long d0 = (long long)blockIdx.y * 64 * N; d0 < p.D; d0 += (long long)gridDim.y * 64 * N) {
       const long long d = d0 + lane * N;
       float sum[N] = {}, before[N] = {};
-      if (wave == 0 && d < p.D) read_row<B, N>(p, row, d, before);
+      B *to = reinterpret_cast<B *>(p.to) + (long long)row * p.to_stride + d;
+      if (wave == 0 && d < p.D && p.add != 0) load_first<N>(to, p.D - d, before);
       if (d < p.D)
         for (long long v = w + wave; v <= last; v += kWaves * kAhead) {
           float part[kAhead][N] = {};
@@ -328,7 +355,8 @@ template <typename B> __global__ void __launch_bounds__(kJoinThreads) embed_join
 #pragma unroll
         for (int j = 0; j < N; ++j)
           for (int v = 1; v < kWaves; ++v) sum[j] += s_sum[v][lane * N + j];
-        write_row<B, N>(p, row, d, before, sum);
+        add_scaled<N>(p, before, sum);
+        stream_first<N>(to, p.D - d, sum);
       }
     }
   }

@@ -106,6 +106,24 @@ def test_gradient(T, N, D, hot, types):
         _check_grad(got, g, t, N, scale, before)
 
 
+@pytest.mark.parametrize("types", TYPES)
+@pytest.mark.parametrize("D", [1, 2, 3, 4, 5, 7, 8, 9, 255, 257, 511, 513, 1023, 1025, 1031, 2049, 4095, 4097])
+def test_gradient_at_the_last_columns(D, types):
+    # a row of one token, rows of some, one of more than a window; columns that a lane holds in part, and lanes with none
+    T, N = 150, 6
+    g, t = _normal((T, D + 3), types[0], D)[:, 2:2 + D], _ids(T, N, D, 0.5)
+    t[t == 1] = 0
+    t[70] = 1
+    wide = torch.full((N + 2, D + 5), 7.0, dtype=types[1], device=DEV)
+    mine = wide[1:-1, 3:3 + D]
+    before = mine.clone()
+    llc.llc_embed_grad(g, t, N, out=mine, add=True)
+    _check_grad(mine, g, t, N, 1.0, before)
+    llc.llc_embed_grad(g, t, N, out=mine)
+    _check_grad(mine, g, t, N, 1.0)
+    assert (wide[:, :3] == 7).all() and (wide[:, 3 + D:] == 7).all() and (wide[0] == 7).all() and (wide[-1] == 7).all()
+
+
 @pytest.mark.parametrize("T", [0, 1, 200])
 def test_gradient_without_valid_tokens(T):
     g = _normal((T, 70), F32, 1)
