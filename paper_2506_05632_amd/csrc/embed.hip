@@ -8,7 +8,7 @@
 // Tokens as in text name a few rows very often: a row of more than kWindow tokens is added up by windows of kWindow
 // sorted positions, each a wavefront's, whose partial sums (fp32, in the workspace) a last launch joins.  A window touches at most
 // two such rows, the one it starts in and the one it ends in, so two partial rows a window are room enough, and a window's place
-// follows from its number: nothing is counted or handed out at run time.
+// follows from its number: which wavefront adds what is not decided at run time.  (Of few windows the row's last wavefront at work does the joining; the order is the same.)
 #include "ends.hpp"
 
 namespace llc {
@@ -41,6 +41,7 @@ struct EmbedParams {
   Place *places;            // [T] the positions by token
   int32_t *starts;          // [N + 1] where a row's places start
   float *partial;           // [windows][2][D]
+  int *arrived;             // [windows][team] wavefronts that are done with the long row that starts in a window; null: a launch of its own joins them
   long long windows;
   unsigned window_blocks, sum_blocks;  // of the summing launch: windows, then sorted positions
 };
@@ -92,6 +93,8 @@ template <int WAVES> __global__ void __launch_bounds__(WAVES * 64) embed_sort_ke
   // a wavefront takes consecutive positions, so that the order of the positions is kept
   const long long share = ((p.T + WAVES - 1) / WAVES + 63) & ~63LL;
   const long long from = wave * share, until = from + share < p.T ? from + share : p.T;
+  if (p.arrived != nullptr && blockIdx.x == 0)
+    for (int i = tid; i < (int)p.windows << p.team_log; i += WAVES * 64) p.arrived[i] = 0;
   unsigned id[kSortAhead];
   load_ids(p, from + lane, until, id);
   for (int i = tid; i < WAVES * range; i += WAVES * 64) counts[i] = 0;
@@ -247,6 +250,32 @@ __device__ __forceinline__ void sum_row(const EmbedParams &p, B *to, int t, int 
   }
 }
 
+// A wavefront's columns of a long row whose windows are all summed, the same whoever comes last.
+template <bool ALL, typename A, typename B>
+__device__ __forceinline__ void join_row(const EmbedParams &p, int row, int start, int count, long long d0, long long step, int lane) {
+  constexpr int N = kWide<A>;
+  const int first = start / kWindow, last = (start + count - 1) / kWindow;
+  const int slot = start != first * kWindow ? 1 : 0;  // (of the first window)
+  B *to = reinterpret_cast<B *>(p.to) + (long long)row * p.to_stride;
+  for (long long d = d0; d < p.D; d += step) {  // (uniform)
+    const Columns<N> c = columns_at<ALL, N>(d + lane * N, p.D);
+    float sum[N] = {}, before[N] = {};
+    if (p.add != 0) load_columns<ALL, N>(to, c, before);
+    for (int v = first; v <= last; v += kAhead) {
+      float part[kAhead][N] = {};
+#pragma unroll
+      for (int u = 0; u < kAhead; ++u)
+        if (v + u <= last) load_columns<ALL, N>(p.partial + ((v + u) * 2LL + (v + u == first ? slot : 0)) * p.D, c, part[u]);
+#pragma unroll
+      for (int u = 0; u < kAhead; ++u)
+#pragma unroll
+        for (int i = 0; i < N; ++i) sum[i] += part[u][i];
+    }
+    add_scaled<N>(p, before, sum);
+    store_columns<N, true>(to, c, sum);
+  }
+}
+
 template <typename A, typename B> __global__ void __launch_bounds__(kBlock) embed_sum_kernel(const EmbedParams p) {
   constexpr int N = kWide<A>;
   const int in_block = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
@@ -273,6 +302,17 @@ template <typename A, typename B> __global__ void __launch_bounds__(kBlock) embe
       const int t = __shfl(mine.t, lane + skip);
       if (p.D >= N) sum_window<true, A>(p, to, t, upto - skip, d0, step, lane);
       else sum_window<false, A>(p, to, t, upto - skip, d0, step, lane);
+      if (p.arrived == nullptr) continue;
+      const int from = slot == 0 ? 0 : n - 1;
+      const int row = __builtin_amdgcn_readlane(mine.row, from), start = __builtin_amdgcn_readlane(mine.start, from),
+                count = __builtin_amdgcn_readlane(mine.count, from), first = start / kWindow, last = (start + count - 1) / kWindow;
+      __threadfence();  // (what this wavefront has written is there for the one that joins)
+      int before = 0;
+      if (lane == 0) before = atomicAdd(&p.arrived[(first << p.team_log) + (int)(wave & ((1 << p.team_log) - 1))], 1);
+      if (__builtin_amdgcn_readfirstlane(before) != last - first) continue;
+      __threadfence();
+      if (p.D >= N) join_row<true, A, B>(p, row, start, count, d0, step, lane);
+      else join_row<false, A, B>(p, row, start, count, d0, step, lane);
     }
     return;
   }
@@ -377,8 +417,13 @@ int team_log_of(long long D, int from) {
   return slabs >= 4 ? 2 : slabs >= 2 ? 1 : 0;
 }
 
+// Up to that many windows the last of a long row's wavefronts joins it, which spares a launch; that wavefront's sums follow each other, so the joins of
+// more windows are workgroups' of their own.  us a call, bf16 rows of 1537 into fp32, with the launch and without: 1001 tokens that hardly
+// repeat 13.0, 9.3; three in ten by one token 16.3, 15.4; all by one token 16.2, 18.4.  4096 tokens: 21.2, 17.6; 22.2, 25.7; 21.7, 44.5.
+constexpr int kFewWindows = 32;
+
 struct GradLayout {
-  size_t places, starts, partial, total;
+  size_t places, starts, arrived, partial, total;
 };
 GradLayout grad_layout(long long T, long long N, long long D) {
   const auto up = [](size_t n) { return (n + 255) & ~(size_t)255; };
@@ -386,6 +431,7 @@ GradLayout grad_layout(long long T, long long N, long long D) {
   size_t at = 0;
   l.places = at; at += up((size_t)T * sizeof(Place));
   l.starts = at; at += up((size_t)(N + 1) * 4);
+  l.arrived = at; at += T > kWindow && T <= kFewWindows * kWindow ? up(kFewWindows * 4 * 4) : 0;
   l.partial = at; at += T > kWindow ? up((size_t)((T + kWindow - 1) / kWindow) * 2 * (size_t)D * 4) : 0;
   l.total = at;
   return l;
@@ -452,6 +498,7 @@ extern "C" int llc_embed_grad(const llc_embed_grad_args *a) {
   p.range = (int)((a->N + 255) / 256 < kMostRange ? (a->N + 255) / 256 : kMostRange);
   const long long sort_blocks = (a->N + p.range - 1) / p.range;
   p.windows = a->T > kWindow ? (a->T + kWindow - 1) / kWindow : 0;
+  p.arrived = p.windows > 0 && p.windows <= kFewWindows ? (int *)(work + l.arrived) : nullptr;
   const long long a_block = kBlock / 64, window_blocks = ((p.windows << p.team_log) + a_block - 1) / a_block;
   const auto row_blocks = [&](long long rows) {
     const long long blocks = ((rows << p.team_log) + a_block - 1) / a_block;
@@ -463,7 +510,8 @@ extern "C" int llc_embed_grad(const llc_embed_grad_args *a) {
   if ((a->flags & LLC_FLAG_DRY_RUN) != 0) return LLC_OK;
   hipStream_t st = (hipStream_t)a->stream;
   return between_events(a->ev_begin, a->ev_end, st, [&] {
-    // (few tokens: four wavefronts take them in one go, and are sooner done than sixteen)
+    // Few tokens: four wavefronts take them in one go, and are sooner done than sixteen.  (us a call with four and with sixteen, rows of 256: 256 tokens
+    // 12.3, 13.4; 4096 14.0, 14.6; 8192 18.6, 16.0; 16 384 26.6, 18.8.)
     if (a->T <= 4 * 64 * kSortAhead)
       embed_sort_kernel<4><<<(unsigned)sort_blocks, 256, ((size_t)4 * p.range + p.range + 1) * 4, st>>>(p);
     else
@@ -482,7 +530,7 @@ extern "C" int llc_embed_grad(const llc_embed_grad_args *a) {
       if (e != hipSuccess || p.T == 0) return e;
       embed_sum_kernel<decltype(from), B><<<(unsigned)(window_blocks + sum_blocks), kBlock, 0, st>>>(p);
       e = hipGetLastError();
-      if (e != hipSuccess || p.windows == 0) return e;
+      if (e != hipSuccess || p.windows == 0 || p.arrived != nullptr) return e;
       const long long groups = (p.windows + kJoinThreads / 64 - 1) / (kJoinThreads / 64);
       const long long slabs = (a->D + 255) / 256, most = kMostBlocks / 4 / groups, join = slabs < most ? slabs : most;
       embed_join_kernel<decltype(to)><<<dim3((unsigned)groups, (unsigned)(join < 1 ? 1 : join < 64 ? join : 64)), kJoinThreads, 0, st>>>(p);

@@ -192,6 +192,31 @@ def test_embed_on_another_stream_and_in_a_graph():
         assert all(torch.equal(u, v) for u, v in zip(clipped, again)), n
 
 
+@pytest.mark.parametrize("types", [(F32, F32), (BF16, F32), (BF16, BF16)])
+@pytest.mark.parametrize("T", [32, 33, 64, 65, 1023, 1024, 1025])
+def test_gradient_of_rows_that_many_tokens_name(T, types):
+    # the same call again and again on one workspace, with rows that start and end at other places of a window each time
+    N, D = 40, 1030
+    g = _normal((T, D), types[0], T)
+    workspace = torch.full((llc.llc_embed_grad_workspace_size(T, N, D),), 255, dtype=torch.uint8, device=DEV)
+    grad = torch.empty(N, D, dtype=types[1], device=DEV)
+    still = torch.empty(T, dtype=torch.int32, device=DEV)
+    graph = torch.cuda.CUDAGraph()
+    draws = [torch.full_like(still, 7), _ids(T, 3, 1), _ids(T, N, 2, 0.9), torch.full_like(still, -1), _ids(T, N, 3, 0.4), _ids(T, N, 4)]
+    still.copy_(draws[0])
+    llc.llc_embed_grad(g, still, N, out=grad, workspace=workspace)
+    torch.cuda.synchronize()
+    with torch.cuda.graph(graph):
+        llc.llc_embed_grad(g, still, N, out=grad, workspace=workspace)
+    for t in draws + draws[::-1]:
+        still.copy_(t)
+        grad.fill_(9.0)
+        graph.replay()
+        torch.cuda.synchronize()
+        _check_grad(grad, g, t, N, 1.0)
+        assert torch.equal(grad, llc.llc_embed_grad(g, t, N, out_dtype=types[1])["grad"])
+
+
 def _grads(sizes, dtypes, scale=0.01):
     return [(scale * torch.randn(s, generator=_gen(11 + n), device=DEV)).to(dtypes[n % len(dtypes)]) for n, s in enumerate(sizes)]
 
