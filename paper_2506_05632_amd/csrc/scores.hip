@@ -3,12 +3,14 @@
 // Forward.  With a reference m, c = log2(e) / T and d_i = (x_i - m) c, a row needs S = sum 2^d_i and D = sum d_i 2^d_i: ln p_t = (x_t - m) / T - ln S
 // and the entropy is ln S - ln 2 D / S.  One pass over the row forms both: a wavefront keeps its largest entry so far as its m, every lane its shares
 // of S and D in fp32, scaled over when m grows (which happens a dozen times a row); lanes, wavefronts and chunks are joined in fp64.
-// The same pass finds the top alternatives.  An entry is a candidate if it is above a bound that M entries of the row are known to reach: first the
-// smallest, over the wavefronts, of the ceil(M / wavefronts) largest of what their lanes' first entries are (each lane's largest of 16), so that a row of 128 256 leaves
-// a thousand candidates for fifty, and a tile of 16 entries a lane that has none costs one comparison a lane.  Candidates go to a list of the wavefront's in LDS as
+// The same pass finds the top alternatives.  An entry is a candidate if it is above a bound that M entries of the row are known to reach: every
+// wavefront says a value that its share of the M reach, at first among its lanes' first entries (each lane's largest of 16), later among the
+// candidates in its list, and the smallest said is the bound.  A row of 128 256 leaves a few hundred candidates for fifty, and a tile of 16 entries a lane that has
+// none costs one comparison a lane.  Candidates go to a list of the wavefront's in LDS as
 // whole numbers that order as (value, lower index first); a full list is cut to its M largest, which raises the wavefront's bound.  At the end a
 // histogram over the numbers' range finds a bound that at most kSelected of them reach, and those are ranked by comparing all with all.
-// What bounds it: reading the row (10 issue slots an entry, against 16 that fp32 logits at 6.3 TB/s leave).
+// What bounds it: reading the rows where there are many (1024 x 128 256 fp32 with 50 alternatives 91 us, 5.8 TB/s), and otherwise how long one workgroup's steps
+// take one after the other (256 x 32 000 bf16 with 20 alternatives 15 us, 8.5 without any).
 #include "ends.hpp"
 
 namespace llc {
@@ -26,9 +28,8 @@ constexpr int kMostSplit = 64;  // workgroups a row is split over
 typedef unsigned long long u64;
 
 // What a workgroup knows of a chunk of a row, when a row is split.
-struct Share {
+struct alignas(32) Share {
   double s, d;    // sum 2^((x - top) c), sum of (x - top) c 2^(...)
-  double unused;
   float top;      // largest entry, -inf without mass
   int count;      // keys in the list behind the shares
 };
@@ -563,7 +564,7 @@ template <typename E, int WAVES> __global__ void __launch_bounds__(WAVES * 64) s
   if (p.M > 0) { const uint32_t said = least_said(s_nth, WAVES); least = (u64)(said > 0 ? said : 1) << 32; }
   if (p.chunks > 1) {
     u64 *keys = p.keys + (r * p.chunks + part) * p.M;
-    if (threadIdx.x == 0) p.shares[r * p.chunks + part] = Share{s, d, 0.0, top, total < p.M ? total : p.M};
+    if (threadIdx.x == 0) p.shares[r * p.chunks + part] = Share{s, d, top, total < p.M ? total : p.M};
     if (p.M > 0) select_top<WAVES * 64>(s_list, WAVES, kList, s_count, least, high, p.M, [&](int rank, u64 key) { keys[rank] = key; });
     return;
   }
@@ -580,7 +581,7 @@ template <typename E> __global__ void __launch_bounds__(kBlock) score_join_kerne
   const Share *shares = p.shares + r * p.chunks;
   const float c = kLog2e / p.temp;
   const int lane = threadIdx.x & 63;
-  Share share = {0.0, 0.0, 0.0, -kInf, 0};
+  Share share = {0.0, 0.0, -kInf, 0};
   if (lane < p.chunks) share = shares[lane];
   const float top = wave_max(share.top);
   int total = share.count;
@@ -823,7 +824,7 @@ template <typename E> struct RowTile {
   }
   __device__ __forceinline__ void add_up(const ScoreParams &p, Scan<E> &w, const Tile<E> &tile) const {
     Tile<E> t = tile;
-    if (at + 64 * kPer > p.V) {  // (uniform) what other lanes have too counts as nothing
+    if (at > p.V - 64 * kPer) {  // (uniform) what other lanes have too counts as nothing
 #pragma unroll
       for (int u = 0; u < kLoads; ++u) {
         const int others = at + (u * 64 + (int)(threadIdx.x & 63)) * N - first(u);
@@ -853,7 +854,7 @@ template <typename E> struct RowTile {
     float v[kPer];
     unpack(tile, v);
     entry_gradients(weights, v);
-    token_gradients(p, r, weights, tokens, tile, v, at < last ? at : last, at + 64 * kPer, [&](int u) { return first(u); });
+    token_gradients(p, r, weights, tokens, tile, v, at < last ? at : last, at > p.V - 64 * kPer ? p.V : at + 64 * kPer, [&](int u) { return first(u); });
     E *row = reinterpret_cast<E *>(p.grad) + r * p.grad_stride_r;
 #pragma unroll
     for (int u = 0; u < kLoads; ++u) {
@@ -981,10 +982,10 @@ template <typename E> hipError_t launch_gradient(ScoreParams p, hipStream_t st) 
   return hipGetLastError();
 }
 
-// Scores and gradient in one launch, where a row fits.  False: it does not.
-#ifndef LONGR
-#define LONGR 64
-#endif
+// Scores and gradient in one launch: as many wavefronts as keep the row in registers.  Rows too long for that are a workgroup's too where the scores would
+// not be split (many rows: a CU has one at least), else scores and gradient are two launches over all CUs.  us a call, one launch and two (three where
+// split): 70 001 fp32 of 64 rows 19.0, 17.0, of 96 19.7, 23.7, of 256 31.3, 42.1; 128 256 fp32 28.0, 24.9; 28.6, 36.0; 46.8, 67.9; 152 064
+// bf16 33.0, 22.1; 33.2, 32.9; 38.7, 49.5; 300 000 bf16 55.4, 31.0; 55.3, 54.6; 69.0, 86.7.  False: nothing was launched.
 template <typename E> bool launch_rows(const ScoreParams &p, hipStream_t st) {
   const long long tiles = (p.V + 64 * kPer - 1) / (64 * kPer);
   constexpr bool kHalf = sizeof(E) == 2;
@@ -996,7 +997,7 @@ template <typename E> bool launch_rows(const ScoreParams &p, hipStream_t st) {
   else if (tiles <= 16) score_row_kernel<E, 4, 4><<<rows, 256, 0, st>>>(p, (int)tiles);
   else if (tiles <= 32) score_row_kernel<E, kHalf ? 4 : 8, kHalf ? 8 : 4><<<rows, kHalf ? 256 : 512, 0, st>>>(p, (int)tiles);
   else if (kHalf && tiles <= 64) score_row_kernel<E, 8, kHalf ? 8 : 4><<<rows, 512, 0, st>>>(p, (int)tiles);
-  else if (p.R >= LONGR) score_long_row_kernel<E><<<rows, 1024, 0, st>>>(p, (int)tiles);
+  else if (p.chunks == 1) score_long_row_kernel<E><<<rows, 1024, 0, st>>>(p, (int)tiles);
   else return false;
   return true;
 }
@@ -1004,13 +1005,11 @@ template <typename E> bool launch_rows(const ScoreParams &p, hipStream_t st) {
 template <typename E> hipError_t launch_scores(const ScoreParams &p, hipStream_t st) {
   const unsigned blocks = (unsigned)(p.R * p.chunks);
   const long long tiles = (p.chunk + 64 * kPer - 1) / (64 * kPer);
-#ifdef NW
-  score_kernel<E, NW><<<blocks, NW * 64, 0, st>>>(p);
-#else
+  // us a call with four wavefronts and with eight: 32 000 bf16, 50 alternatives, 256 rows 21.9, 17.7; 512 24.7, 22.6; 768 28.1, 28.3; 2048 53.7, 59.5;
+  // 128 256 fp32 256 rows 50.7, 35.4; 512 55.9, 52.2; 768 71.1, 77.3.  (Sixteen: 19.2 and 33.6 at 256 rows, 60 at 512 of the latter.)
   if (tiles <= 1) score_kernel<E, 1><<<blocks, 64, 0, st>>>(p);
   else if (tiles <= 4 || blocks > 512) score_kernel<E, 4><<<blocks, 256, 0, st>>>(p);
   else score_kernel<E, 8><<<blocks, 512, 0, st>>>(p);
-#endif
   hipError_t e = hipGetLastError();
   if (e != hipSuccess || p.chunks == 1) return e;
   score_join_kernel<E><<<(unsigned)p.R, kBlock, 0, st>>>(p);
