@@ -775,11 +775,26 @@ def _scored(name, x, tokens, kind):
     return R, V, 1 if tokens.dim() == 1 else tokens.shape[1]
 
 
-def _score_workspace(R, V, M, v_chunks, device):
+def _scratch(workspace, nbytes, device):
+    """The caller's workspace, or a new one (`nbytes`: a function, for the size is not needed otherwise)."""
+    if workspace is None:
+        return torch.empty(max(nbytes(), 256), dtype=torch.uint8, device=device)
+    if workspace.device != device or workspace.dtype != torch.uint8 or not workspace.is_contiguous():
+        raise ValueError("workspace must be contiguous uint8 on the call's device")
+    return workspace
+
+
+def _score_bytes(R, V, M, v_chunks):
     n = llc_token_logprobs_workspace_size(R, V, M)
-    if v_chunks > 0:
-        n = max(n, v_chunks * R * (32 + 8 * M) + 32 * R + 512)
-    return torch.empty(max(n, 256), dtype=torch.uint8, device=device)
+    return max(n, v_chunks * R * (32 + 8 * M) + 32 * R + 512) if v_chunks > 0 else n
+
+
+def _check_given(out, device, specs):
+    """The caller's outputs against what would have been made."""
+    for name, (dtype, *shape) in specs.items():
+        t = out.get(name)
+        if t is not None and (t.device != device or t.dtype != dtype or list(t.shape) != shape or not t.is_contiguous()):
+            raise ValueError(f"{name} must be {dtype} of {shape}, contiguous, on the logits' device")
 
 
 def llc_token_logprobs(logits: torch.Tensor, tokens: Optional[torch.Tensor], M: int = 0, *, kind="logits", temp: float = 1.0,
@@ -808,8 +823,10 @@ def llc_token_logprobs(logits: torch.Tensor, tokens: Optional[torch.Tensor], M: 
             specs["top_ids"] = (torch.int32, R, M)
             specs["top_logp"] = (torch.float32, R, M)
         out = _new(dev, specs)
-    if workspace is None:
-        workspace = _score_workspace(R, V, M, v_chunks, dev)
+    else:
+        _check_given(out, dev, {"logp": (torch.float32, *(tokens.shape if tokens is not None else ())), "entropy": (torch.float32, R),
+                                "lse": (torch.float64, R, 2), "top_ids": (torch.int32, R, M), "top_logp": (torch.float32, R, M)})
+    workspace = _scratch(workspace, lambda: _score_bytes(R, V, M, v_chunks), dev)
     a = TokenLogprobsArgs()
     a.R, a.V, a.G, a.M = R, V, G, M
     a.dtype, a.kind = _TYPES[logits.dtype], _KINDS[kind]
@@ -859,11 +876,14 @@ def llc_token_logprobs_grad(logits: torch.Tensor, tokens: Optional[torch.Tensor]
                 specs["logp"] = (torch.float32, *tokens.shape)
             specs["entropy"] = (torch.float32, R)
         out = _new(dev, specs)
+    else:
+        _check_given(out, dev, {"logp": (torch.float32, *(tokens.shape if tokens is not None else ())), "entropy": (torch.float32, R),
+                                "lse": (torch.float64, R, 2)})
     grad = out["grad"]
     if grad.device != dev or grad.dtype != logits.dtype or tuple(grad.shape) != (R, V) or (grad.stride(1) != 1 and V > 1):
         raise ValueError("grad must be [R,V] of the logits' type, last dimension contiguous")
-    if workspace is None and lse is None:
-        workspace = _score_workspace(R, V, 0, v_chunks, dev)
+    if lse is None:
+        workspace = _scratch(workspace, lambda: _score_bytes(R, V, 0, v_chunks), dev)
     a = TokenLogprobsGradArgs()
     a.R, a.V, a.G = R, V, G
     a.dtype, a.kind = _TYPES[logits.dtype], _KINDS[kind]
@@ -874,7 +894,7 @@ def llc_token_logprobs_grad(logits: torch.Tensor, tokens: Optional[torch.Tensor]
     a.grad_entropy, a.lse_in, a.entropy_in = _ptr(grad_entropy), _ptr(lse), _ptr(entropy)
     a.grad, a.grad_stride_r = grad.data_ptr(), _row_stride(grad)
     a.logp, a.entropy, a.lse = _ptr(out.get("logp")), _ptr(out.get("entropy")), _ptr(out.get("lse"))
-    if workspace is not None:
+    if lse is None:
         a.workspace, a.workspace_bytes = workspace.data_ptr(), workspace.numel()
     a.stream = _stream_handle(dev)
     a.flags, a.v_chunks = flags, v_chunks
@@ -953,8 +973,7 @@ def llc_embed_grad(g: torch.Tensor, tokens: torch.Tensor, N: int, *, scale: floa
             or (out.stride(1) != 1 and D > 1)):
         raise ValueError("out must be [N,D], float32 or bfloat16, last dimension contiguous")
     T = rows.shape[0]
-    if workspace is None:
-        workspace = torch.empty(max(llc_embed_grad_workspace_size(T, N, D), 256), dtype=torch.uint8, device=g.device)
+    workspace = _scratch(workspace, lambda: llc_embed_grad_workspace_size(T, N, D), g.device)
     a = EmbedGradArgs()
     a.T, a.N, a.D = T, N, D
     a.dtype, a.grad_dtype = _TYPES[g.dtype], _TYPES[out.dtype]
@@ -1005,8 +1024,7 @@ def llc_clip_grad_norm(grads, max_norm: float, *, out=None, workspace: Optional[
     arrays = _tensor_list(grads, out) if _tensor_list is not None else None
     arrays = arrays[0] if arrays is not None else _checked_list(grads, out)
     norm = torch.empty((), dtype=torch.float32, device=dev)
-    if workspace is None:
-        workspace = torch.empty(max(llc_clip_grad_norm_workspace_size(n), 256), dtype=torch.uint8, device=dev)
+    workspace = _scratch(workspace, lambda: llc_clip_grad_norm_workspace_size(n), dev)
     a = ClipGradNormArgs()
     at = ctypes.cast(arrays, ctypes.c_void_p).value  # (bytes that live as long as this call, which is as long as they are read)
     a.n, a.grads, a.numel, a.dtype = n, at, at + 16 * n, at + 24 * n

@@ -278,6 +278,52 @@ def test_gradient_in_place(R, V, dtype):
     _check_grad(x, t, a, None, 1.0, None, got)
 
 
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("V", [4, 6, 1023, 1024, 1025, 1031, 4096, 4097, 8192, 8195, 16384, 16391, 32768, 32775, 40003, 65536, 65543])
+def test_gradient_where_a_row_takes_one_more_tile(V, dtype):
+    R = 3
+    for G, pad in ((2, 0), (300, 3), (1100, 5)):  # (more tokens than a wavefront, and than a workgroup)
+        x, t = _rows(R, V, dtype, V + G, pad=pad, offset=pad // 2), _tokens(R, G, V, V)
+        t[:, -1] = V - 1
+        a, b = torch.randn(R, G, generator=_gen(V), device=DEV), torch.randn(R, generator=_gen(V + 1), device=DEV)
+        wide = torch.full((R, V + 2 * pad), 77.0, dtype=dtype, device=DEV)
+        out = llc.llc_token_logprobs_grad(x, t, a, grad_entropy=b)
+        _check_grad(x, t, a, b, 1.0, out, out["grad"])
+        llc.llc_token_logprobs_grad(x, t, a, grad_entropy=b, out={"grad": wide[:, pad:pad + V]})
+        assert torch.equal(wide[:, pad:pad + V], out["grad"])
+        assert (wide[:, :pad] == 77).all() and (wide[:, pad + V:] == 77).all()
+        again = x.clone()
+        assert torch.equal(llc.llc_token_logprobs_grad(again, t, a, grad_entropy=b, out={"grad": again})["grad"], out["grad"])
+
+
+@pytest.mark.parametrize("R,V,dtype", [(90, 66001, F32), (90, 100003, F32), (87, 131072, BF16), (90, 140001, BF16), (86, 200003, BF16), (86, 49153, F32)])
+def test_gradient_of_many_long_rows(R, V, dtype):
+    inf = float("inf")
+    x, t = _rows(R, V, dtype, V).clone(), _tokens(R, 3, V, V)
+    x[1] = -inf
+    x[2] = LOWEST[dtype]
+    x[3] = -inf; x[3, V - 1] = 1.0
+    x[4, : V - 700] = -inf
+    x[5, ::3] = inf; x[5, 1::3] = float("nan")
+    x[6, 500:] = LOWEST[dtype]
+    t[:, 0] = V - 1
+    a, b = torch.randn(R, 3, generator=_gen(1), device=DEV), torch.randn(R, generator=_gen(2), device=DEV)
+    out = llc.llc_token_logprobs_grad(x, t, a, grad_entropy=b)
+    _check_grad(x[:12], t[:12], a[:12], b[:12], 1.0, {k: v[:12] for k, v in out.items()}, out["grad"][:12])
+    _check_grad(x[-2:], t[-2:], a[-2:], b[-2:], 1.0, {k: v[-2:] for k, v in out.items()}, out["grad"][-2:])
+    few = llc.llc_token_logprobs_grad(x[:4], t[:4], a[:4], grad_entropy=b[:4])  # (split over more workgroups)
+    _check_grad(x[:4], t[:4], a[:4], b[:4], 1.0, few, few["grad"])
+    again = x.clone()
+    assert torch.equal(llc.llc_token_logprobs_grad(again, t, a, grad_entropy=b, out={"grad": again})["grad"], out["grad"])
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("R,V", [(1, 47999), (1, 48000), (5, 63999), (85, 50001), (86, 50001), (4, 300007)])
+def test_scores_where_rows_begin_to_be_split(R, V, dtype):
+    x, t = _rows(R, V, dtype, R + V), _tokens(R, 300 if R < 6 else 2, V, R)
+    ref.check_scores(llc.llc_token_logprobs(x, t, 40, temp=0.8, want_lse=True), x, t, 40, 0.8)
+
+
 def test_gradient_against_differences():
     # f(x + h v) - f(x - h v) over 2 h for directions v of length one: the third derivative of these sums is below
     # 2 (|a| + |b| (1 + ln V)) / T^3, and f is known to 2e-6 of its weights, so h = 2^-5 leaves 3e-4 of them
@@ -322,6 +368,27 @@ def test_refusals():
         with pytest.raises(llc.LlcError) as e:
             bad()
         assert e.value.code == code
+
+
+def test_refusals_of_outputs_and_workspaces():
+    x, t = _rows(4, 100, F32, 1), _tokens(4, 2, 100, 1)
+    a = torch.zeros(4, 2, device=DEV)
+    f32 = lambda *shape: torch.zeros(shape, device=DEV)  # noqa: E731
+    for out in ({"logp": f32(4)}, {"logp": f32(2, 4).t()}, {"logp": f32(4, 2).double()}, {"logp": torch.zeros(4, 2)},
+                {"logp": f32(4, 2), "entropy": f32(3)}, {"logp": f32(4, 2), "lse": f32(4, 2)}, {"logp": f32(4, 2), "top_ids": f32(4, 3), "top_logp": f32(4, 3)}):
+        with pytest.raises(ValueError):
+            llc.llc_token_logprobs(x, t, 3, out=out)
+    for out in ({"grad": f32(4, 100), "logp": f32(4)}, {"grad": f32(4, 100), "entropy": f32(4, 1)}, {"grad": f32(4, 99)}, {"grad": torch.zeros(4, 100)}):
+        with pytest.raises(ValueError):
+            llc.llc_token_logprobs_grad(x, t, a, out=out)
+    for workspace in (torch.zeros(1 << 16, dtype=torch.uint8), f32(1 << 14), torch.zeros(1 << 17, dtype=torch.uint8, device=DEV)[::2]):
+        for bad in (lambda: llc.llc_token_logprobs(x, t, workspace=workspace), lambda: llc.llc_token_logprobs_grad(x, t, a, workspace=workspace),
+                    lambda: llc.llc_embed_grad(x, t[:, 0], 9, workspace=workspace), lambda: llc.llc_clip_grad_norm([x], 1.0, workspace=workspace)):
+            with pytest.raises(ValueError):
+                bad()
+    with pytest.raises(llc.LlcError) as e:
+        llc.llc_token_logprobs(x, t, 3, out={"entropy": f32(4)})
+    assert e.value.code == -1
 
 
 def test_a_dry_run_writes_nothing():
