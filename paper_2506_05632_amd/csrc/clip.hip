@@ -4,6 +4,8 @@
 // Squares are added up in fp32 by a thread (32 of them a piece) and joined in fp64; a thread whose sum leaves the range in which fp32 squares are
 // neither lost nor infinite forms it again in fp64 from its registers.  Which piece a workgroup takes and the order in which partial sums
 // are joined follow from the sizes alone.
+// 534 M entries in 219 tensors, bf16 but for norms' gains, into other buffers: 0.52 ms, 6.2 TB/s of the 3.2 GB read, read again and written.  Small
+// lists: the host's call and two launches that wait for each other (21 tensors 11.6 us).
 #include "ends.hpp"
 
 namespace llc {
@@ -12,8 +14,11 @@ namespace {
 constexpr int kTable = 140;         // tensors a launch (a launch's arguments are 4 KB at most)
 constexpr int kVectors = 4;         // 16-byte loads of a thread and piece
 constexpr int kPiece = kBlock * kVectors * 16;  // bytes
-constexpr int kSquareBlocks = 2048; // workgroups of a table's first pass, and its partial sums, at most
-constexpr int kFewPartials = 1024;  // up to so many every workgroup of the second pass joins them itself
+// Workgroups of a table's first pass, and its partial sums, at most.  (1024: 16 x 1 M fp32 29.3 us, 4096: 28.2, so 27.2; 16 x 4 M 86.3, 83.0, 82.9.)
+constexpr int kSquareBlocks = 2048;
+// Up to so many every workgroup of the second pass joins them itself, which spares a launch.  us a call with that launch and without: 10 x 262 144 fp32
+// 12.1, 11.5; 20 x 200 000 12.2, 11.6; beyond: 16 x 1 M 26.8, 30.1; 100 x 2 M 242, 274.
+constexpr int kFewPartials = 1024;
 constexpr unsigned kScaleBlocks = 1u << 22;
 constexpr long long kBf16 = 1LL << 62;
 
