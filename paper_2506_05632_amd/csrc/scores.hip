@@ -146,6 +146,38 @@ template <typename E> __device__ __forceinline__ Tile<E> load_at(const E *row, l
   return load_tile_end(row + at + lane * kWide<E>, end - at - lane * kWide<E>);
 }
 
+// The same without a branch, for what is asked for ahead: a load that would reach beyond `end` starts at `last`, the place of the last whole one, instead.  (A
+// load under a condition is waited for at once: the compiler copies what it brought, word by word, to where both ways meet.)
+template <typename E> __device__ __forceinline__ uint32_t held(uint32_t from, uint32_t last) { return from < last ? from : last; }
+template <typename E, bool AGAIN> __device__ __forceinline__ Tile<E> load_held(const E *row, uint32_t at, uint32_t last) {  // AGAIN: it is read a second time, soon
+  constexpr int N = kWide<E>;
+  Tile<E> t;
+#pragma unroll
+  for (int u = 0; u < kPer / N; ++u) {
+    const word4_any *from = reinterpret_cast<const word4_any *>(row + held<E>(at + (u * 64 + (threadIdx.x & 63)) * N, last));
+    t.w[u] = AGAIN ? *from : __builtin_nontemporal_load(from);
+  }
+  return t;
+}
+// What such loads have brought of other lanes' entries counts as nothing.
+template <typename E> __device__ __forceinline__ void drop_others(Tile<E> &t, uint32_t at, uint32_t last) {
+  constexpr int N = kWide<E>;
+#pragma unroll
+  for (int u = 0; u < kPer / N; ++u) {
+    const uint32_t from = at + (u * 64 + (threadIdx.x & 63)) * N, others = from - held<E>(from, last);
+#pragma unroll
+    for (uint32_t i = 0; i < 4; ++i) {
+      if constexpr (sizeof(E) == 2) {
+        uint32_t o = t.w[u][i];
+        o = 2 * i < others ? (o & 0xFFFF0000u) | 0xFF80u : o;
+        t.w[u][i] = 2 * i + 1 < others ? (o & 0xFFFFu) | 0xFF800000u : o;
+      } else {
+        t.w[u][i] = i < others ? 0xFF800000u : t.w[u][i];
+      }
+    }
+  }
+}
+
 // Exponents are x c less a reference that follows from the largest entry m: m c as fp32 has it.  One multiply-add forms them, exact but for its one rounding, and
 // what the reference's own rounding shifts all of them by is put right at the end.  Where m c leaves fp32 they are (x - m) c.
 __device__ __forceinline__ bool has_reference(float m, float c) { return fabsf(m) * c < 0x1p100f; }
@@ -192,8 +224,8 @@ __device__ __forceinline__ u64 cut_list(u64 *list, int &count, int M) {
   return t;
 }
 
-// One tile: `first` is the index in the row of the lane's first entry.
-template <typename E> __device__ __forceinline__ void take_tile(Scan<E> &w, const Tile<E> &tile, uint32_t first, float c, int M, u64 *list) {
+// One tile: `first` is the index in the row of the lane's first entry, and where its loads start `last` at the most.
+template <typename E> __device__ __forceinline__ void take_tile(Scan<E> &w, const Tile<E> &tile, uint32_t first, uint32_t last, float c, int M, u64 *list) {
   constexpr int N = kWide<E>;
   float v[kPer];
   unpack(tile, v);
@@ -240,7 +272,7 @@ template <typename E> __device__ __forceinline__ void take_tile(Scan<E> &w, cons
           for (int i = h * (kPer / 2); i < (h + 1) * (kPer / 2); ++i) {
             const u64 mask = masks[i];
             if (mask == 0) continue;
-            if (v[i] > w.bound) list[w.count + lanes_below(mask)] = key_of(v[i], first + (i / N) * 64 * N + i % N);
+            if (v[i] > w.bound) list[w.count + lanes_below(mask)] = key_of(v[i], held<E>(first + (i / N) * 64 * N, last) + i % N);
             w.count += (int)__builtin_popcountll(mask);
           }
         }
@@ -256,7 +288,7 @@ template <typename E> __device__ __forceinline__ void take_tile(Scan<E> &w, cons
             if (lane == i) mine = o;
           }
           if (w.count + kPer > kList) least = cut_list(list, w.count, M);
-          const u64 key = key_of(mine, __builtin_amdgcn_readlane(first, from) + (lane / N) * 64 * N + lane % N);
+          const u64 key = key_of(mine, held<E>(__builtin_amdgcn_readlane(first, from) + (lane / N) * 64 * N, last) + lane % N);
           const bool offered = mine > w.bound && key > least;
           const u64 mask = __ballot(offered);
           if (offered) list[w.count + lanes_below(mask)] = key;
@@ -307,7 +339,7 @@ template <int K> __device__ __forceinline__ uint32_t reached_by(const uint32_t (
 __device__ __forceinline__ uint32_t least_said(const uint32_t *said, int waves) {
   const int lane = threadIdx.x & 63;
   uint32_t v = 0xFFFFFFFFu;
-  if (lane < waves) v = *(const volatile uint32_t *)&said[lane];
+  if (lane < waves) v = __hip_atomic_load(&said[lane], __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_WORKGROUP);
   v = min(v, (uint32_t)__builtin_amdgcn_update_dpp(v, v, 0x111, 0xF, 0xF, false));
   v = min(v, (uint32_t)__builtin_amdgcn_update_dpp(v, v, 0x112, 0xF, 0xF, false));
   v = min(v, (uint32_t)__builtin_amdgcn_update_dpp(v, v, 0x114, 0xF, 0xF, false));
@@ -333,7 +365,7 @@ template <int K> __device__ __forceinline__ float look_at_list(u64 *list, int &c
   }
   if (speaks) {
     const uint32_t nth = reached_by(o, share);
-    if (lane == 0) said[wave] = nth;
+    if (lane == 0) __hip_atomic_store(&said[wave], nth, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_WORKGROUP);
   }
   const uint32_t all = least_said(said, waves);
   count = 0;
@@ -486,8 +518,8 @@ __device__ __forceinline__ void join_shares(double &s, double &d, float mine, fl
   s = wave_sum(s * scale);
 }
 
-// One workgroup a row, or a chunk of it.
-template <typename E, int WAVES> __global__ void __launch_bounds__(WAVES * 64) score_kernel(const ScoreParams p) {
+// One workgroup a row, or a chunk of it.  TINY: rows shorter than a load.
+template <typename E, int WAVES, bool TINY = false> __global__ void __launch_bounds__(WAVES * 64) score_kernel(const ScoreParams p) {
   constexpr int N = kWide<E>, kTile = 64 * kPer;
   __shared__ u64 s_list[WAVES * kList];
   __shared__ double s_s[WAVES], s_d[WAVES];
@@ -504,15 +536,19 @@ template <typename E, int WAVES> __global__ void __launch_bounds__(WAVES * 64) s
   Scan<E> w;
   Tile<E> here, next;
   long long at = begin + (long long)wave * kTile;
-  if (at < end) here = load_at(x, at, end);
-  if (at + WAVES * kTile < end) next = load_at(x, at + WAVES * kTile, end);
-  // tokens and their entries are on their way too
+  // (loads return in order: tokens are asked for before the row, their entries after it)
   int token = -1;
-  float token_x = 0.0f;
-  if (p.chunks == 1 && (int)threadIdx.x < p.G) {
-    token = p.tokens[r * p.tok_stride_r + threadIdx.x];
-    if (token >= 0 && token < p.V) token_x = widen(x[token]);
-  }
+  if (p.chunks == 1 && (int)threadIdx.x < p.G) token = p.tokens[r * p.tok_stride_r + threadIdx.x];
+  __builtin_amdgcn_sched_barrier(0);
+  const uint32_t last = TINY ? 0u : (uint32_t)end - N;
+  const auto load = [&](long long from) {
+    if constexpr (TINY) return load_at(x, from, end);
+    else return load_held<E, false>(x, (uint32_t)from, last);
+  };
+  here = load(at);
+  next = load(at + WAVES * kTile);
+  __builtin_amdgcn_sched_barrier(0);
+  const E token_raw = x[token >= 0 && token < p.V ? token : 0];
   // A bound that M entries reach: every wavefront's share of them is among what it has seen.  First each lane's largest of the first tile; later,
   // whenever a wavefront has seen twice as much, the candidates in its list.  What a wavefront has once said stays true, so nobody waits.
   // (Of wavefronts whose first tile is whole: one with a few entries, or none, would have nothing to say.)
@@ -521,9 +557,11 @@ template <typename E, int WAVES> __global__ void __launch_bounds__(WAVES * 64) s
   const int share = (p.M + speakers - 1) / speakers;
   if (p.M > 0) {
     float t = -kInf;
-    if (at < end) {
+    if (speaks || at < end) {
+      Tile<E> first = here;
+      if (!TINY && at + kTile > end) drop_others<E>(first, (uint32_t)at, last);
       float v[kPer];
-      unpack(here, v);
+      unpack(first, v);
 #pragma unroll
       for (int i = 0; i < kPer; ++i) t = fmaxf(t, with_mass(v[i]) ? v[i] : -kInf);
     }
@@ -543,13 +581,17 @@ template <typename E, int WAVES> __global__ void __launch_bounds__(WAVES * 64) s
   const int first_look = share > 16 ? 1 : 2;
   // two tiles in turn, so that one is on its way while the other is taken
   const long long step = (long long)WAVES * kTile;
+  const auto take = [&](Tile<E> tile, long long from) {
+    if (!TINY && from + kTile > end) drop_others<E>(tile, (uint32_t)from, last);  // (uniform)
+    take_tile<E>(w, tile, (uint32_t)(from + lane * N), TINY ? 0xFFFFFFFFu : last, c, p.M, list);
+  };
   for (int tiles = 1; at < end; tiles += 2, at += 2 * step) {
-    take_tile<E>(w, here, (uint32_t)(at + lane * N), c, p.M, list);
-    if (at + 2 * step < end) here = load_at(x, at + 2 * step, end);
+    take(here, at);
+    here = load(at + 2 * step);
     if (at + step >= end) break;
     if (p.M > 0 && tiles >= first_look && (tiles & (tiles - 1)) == 0) look();
-    take_tile<E>(w, next, (uint32_t)(at + step + lane * N), c, p.M, list);
-    if (at + 3 * step < end) next = load_at(x, at + 3 * step, end);
+    take(next, at + step);
+    next = load(at + 3 * step);
     if (p.M > 0 && (tiles & (tiles + 1)) == 0 && at + 2 * step < end) look();
   }
   if (p.M > 0 && w.count > kSelected / WAVES) look();  // (else what all have is soon ranked)
@@ -573,7 +615,7 @@ template <typename E, int WAVES> __global__ void __launch_bounds__(WAVES * 64) s
     return;
   }
   const Row row = row_of(top, s, d, p.temp);
-  if ((int)threadIdx.x < p.G && p.logp != nullptr) p.logp[r * p.G + threadIdx.x] = token < 0 ? 0.0f : token < p.V ? row.logp(token_x) : -kInf;
+  if ((int)threadIdx.x < p.G && p.logp != nullptr) p.logp[r * p.G + threadIdx.x] = token < 0 ? 0.0f : token < p.V ? row.logp(widen(token_raw)) : -kInf;
   write_scores<E>(p, r, row, WAVES * 64, WAVES * 64);
   if (p.M > 0) select_top<WAVES * 64>(s_list, WAVES, kList, s_count, least, high, p.M, [&](int rank, u64 key) { write_top(p, r, row, rank, key); });
 }
@@ -631,13 +673,29 @@ struct RowTokens {
   float weight;
   double share;
 };
-__device__ __forceinline__ RowTokens tokens_of(const ScoreParams &p, long long r) {
-  RowTokens t = {-1, 0.0f, 0.0};
-  for (int g = threadIdx.x & 63; g < p.G; g += 64) {
+// Loads return in order, so what is known of the tokens at once is asked for before the row: their use waits for the row's loads otherwise.
+struct FirstTokens {
+  int token, mine;  // the lane's of the first 64, the thread's of all
+  float weight;
+};
+__device__ __forceinline__ FirstTokens first_tokens(const ScoreParams &p, long long r) {
+  const int lane = threadIdx.x & 63;
+  FirstTokens t = {-1, -1, 0.0f};
+  if (lane < p.G) {
+    t.token = p.tokens[r * p.tok_stride_r + lane];
+    t.weight = p.a[r * p.a_stride_r + lane];
+  }
+  if (p.logp != nullptr && (int)threadIdx.x < p.G) t.mine = p.tokens[r * p.tok_stride_r + threadIdx.x];
+  __builtin_amdgcn_sched_barrier(0);
+  return t;
+}
+__device__ __forceinline__ RowTokens tokens_of(const ScoreParams &p, long long r, const FirstTokens &first) {
+  RowTokens t = {first.token, first.weight, 0.0};
+  if (first.token >= 0 && first.token < p.V) t.share = (double)first.weight;
+  for (int g = (int)(threadIdx.x & 63) + 64; g < p.G; g += 64) {
     const int token = p.tokens[r * p.tok_stride_r + g];
     const float weight = p.a[r * p.a_stride_r + g];
     if (token >= 0 && token < p.V) t.share += (double)weight;
-    if (g < 64) { t.token = token; t.weight = weight; }
   }
   return t;
 }
@@ -749,8 +807,10 @@ template <typename E> __global__ void __launch_bounds__(kBlock) score_grad_kerne
   const long long at = ((long long)part * (kBlock / 64) + wave) * 64 * kPer;
   if (at >= p.V) return;
   const E *x = reinterpret_cast<const E *>(p.x) + r * p.stride_r;
+  const FirstTokens asked = first_tokens(p, r);
   const Tile<E> tile = load_at(x, at, p.V);
-  const RowTokens tokens = tokens_of(p, r);
+  __builtin_amdgcn_sched_barrier(0);
+  const RowTokens tokens = tokens_of(p, r, asked);
   const Weights w = weights_of(p, r, tokens.share, p.lse_in[2 * r], p.lse_in[2 * r + 1], p.b != nullptr ? (double)p.entropy_in[r] : 0.0);
   float v[kPer];
   unpack(tile, v);
@@ -765,22 +825,21 @@ template <typename E, int WAVES> struct RowWork {
   double s_s[WAVES], s_d[WAVES];
   float s_m[WAVES];
 
-  // The row may be overwritten later: what its tokens need is read at the start.
-  static __device__ __forceinline__ void read_tokens(const ScoreParams &p, long long r, int &token, float &token_x) {
+  // The row may be overwritten later: what its tokens need is read at the start.  (The thread's own as it is: what became of it here would be waited for.)
+  static __device__ __forceinline__ E read_tokens(const ScoreParams &p, long long r, int token) {
     const E *x = reinterpret_cast<const E *>(p.x) + r * p.stride_r;
-    token = -1;
-    token_x = -kInf;
-    if (p.logp == nullptr) return;
-    for (int g = threadIdx.x; g < p.G; g += WAVES * 64) {
-      token = p.tokens[r * p.tok_stride_r + g];
-      token_x = token >= 0 && token < p.V ? widen(x[token]) : -kInf;
-      if (p.G > WAVES * 64) p.logp[r * p.G + g] = token_x;
-    }
+    if (p.logp != nullptr && p.G > WAVES * 64)
+      for (int g = threadIdx.x; g < p.G; g += WAVES * 64) {
+        const int other = p.tokens[r * p.tok_stride_r + g];
+        p.logp[r * p.G + g] = other >= 0 && other < p.V ? widen(x[other]) : -kInf;
+      }
+    return x[token >= 0 && token < p.V ? token : 0];
   }
   // From the wavefronts' sums to the scores and what the gradient needs.
-  __device__ __forceinline__ Weights join(const ScoreParams &p, long long r, const Scan<E> &w, int token, float token_x, double share) {
+  __device__ __forceinline__ Weights join(const ScoreParams &p, long long r, const Scan<E> &w, int token, E token_raw, double share) {
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     double s = wave_sum((double)w.s), d = wave_sum((double)w.d);
+    float token_x = token >= 0 && token < p.V ? widen(token_raw) : -kInf;
     asm volatile("" : "+v"(token_x));  // (here: not while other wavefronts already write)
     if (lane == 0) { s_s[wave] = s; s_d[wave] = d; s_m[wave] = w.m; }
     __syncthreads();
@@ -812,39 +871,13 @@ template <typename E, int WAVES> struct RowWork {
 // is written: it is the first of its wavefront, which is always kept.
 template <typename E> struct RowTile {
   static constexpr int N = kWide<E>, kLoads = kPer / N;
-  int at, last;  // the tile's first entry; where a row's last load starts
-  __device__ __forceinline__ int first(int u) const {
-    const int from = at + (u * 64 + (int)(threadIdx.x & 63)) * N;
-    return from < last ? from : last;
-  }
-  template <bool AGAIN> __device__ __forceinline__ Tile<E> load(const E *row) const {  // AGAIN: it is read a second time, soon
-    Tile<E> t;
-#pragma unroll
-    for (int u = 0; u < kLoads; ++u) {
-      const word4_any *from = reinterpret_cast<const word4_any *>(row + first(u));
-      t.w[u] = AGAIN ? *from : __builtin_nontemporal_load(from);
-    }
-    return t;
-  }
+  uint32_t at, last;  // the tile's first entry; where a row's last load starts (a tile that is not there: both are the same)
+  __device__ __forceinline__ int first(int u) const { return (int)held<E>(at + (u * 64 + (threadIdx.x & 63)) * N, last); }
+  template <bool AGAIN> __device__ __forceinline__ Tile<E> load(const E *row) const { return load_held<E, AGAIN>(row, at, last); }
   __device__ __forceinline__ void add_up(const ScoreParams &p, Scan<E> &w, const Tile<E> &tile) const {
     Tile<E> t = tile;
-    if (at > p.V - 64 * kPer) {  // (uniform) what other lanes have too counts as nothing
-#pragma unroll
-      for (int u = 0; u < kLoads; ++u) {
-        const int others = at + (u * 64 + (int)(threadIdx.x & 63)) * N - first(u);
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          if constexpr (sizeof(E) == 2) {
-            uint32_t o = t.w[u][i];
-            o = 2 * i < others ? (o & 0xFFFF0000u) | 0xFF80u : o;
-            t.w[u][i] = 2 * i + 1 < others ? (o & 0xFFFFu) | 0xFF800000u : o;
-          } else {
-            t.w[u][i] = i < others ? 0xFF800000u : t.w[u][i];
-          }
-        }
-      }
-    }
-    take_tile<E>(w, t, 0, kLog2e / p.temp, 0, nullptr);
+    if (at + 64 * kPer > (uint32_t)p.V) drop_others<E>(t, at, last);  // (uniform)
+    take_tile<E>(w, t, 0, 0, kLog2e / p.temp, 0, nullptr);
     __builtin_amdgcn_sched_barrier(0);
   }
   __device__ __forceinline__ void write(const ScoreParams &p, long long r, const Weights &weights, const RowTokens &tokens, Tile<E> tile) const {
@@ -858,7 +891,7 @@ template <typename E> struct RowTile {
     float v[kPer];
     unpack(tile, v);
     entry_gradients(weights, v);
-    token_gradients(p, r, weights, tokens, tile, v, at < last ? at : last, at > p.V - 64 * kPer ? p.V : at + 64 * kPer, [&](int u) { return first(u); });
+    token_gradients(p, r, weights, tokens, tile, v, (int)(at < last ? at : last), (int)min(at + 64 * kPer, (uint32_t)p.V), [&](int u) { return first(u); });
     E *row = reinterpret_cast<E *>(p.grad) + r * p.grad_stride_r;
 #pragma unroll
     for (int u = 0; u < kLoads; ++u) {
@@ -879,20 +912,20 @@ __global__ void __launch_bounds__(WAVES * 64, TILES * sizeof(E) > 8 ? 4 : TILES 
   const long long r = blockIdx.x;
   const E *x = reinterpret_cast<const E *>(p.x) + r * p.stride_r;
   const auto there = [&](int k) { return k * WAVES + wave < n_tiles; };
-  const auto tile = [&](int k) { return RowTile<E>{(n_tiles - 1 - (k * WAVES + wave)) * 64 * kPer, p.V - kWide<E>}; };
+  const uint32_t last = (uint32_t)(p.V - kWide<E>);
+  const auto tile = [&](int k) { return RowTile<E>{there(k) ? (uint32_t)(n_tiles - 1 - (k * WAVES + wave)) * 64 * kPer : last, last}; };
+  const FirstTokens asked = first_tokens(p, r);
   Tile<E> tiles[TILES];
 #pragma unroll
-  for (int k = 0; k < TILES; ++k)
-    if (there(k)) tiles[k] = tile(k).template load<false>(x);
-  int token;
-  float token_x;
-  work.read_tokens(p, r, token, token_x);
-  const RowTokens tokens = tokens_of(p, r);
+  for (int k = 0; k < TILES; ++k) tiles[k] = tile(k).template load<false>(x);
+  __builtin_amdgcn_sched_barrier(0);
+  const E token_raw = work.read_tokens(p, r, asked.mine);
+  const RowTokens tokens = tokens_of(p, r, asked);
   Scan<E> w;
 #pragma unroll
   for (int k = 0; k < TILES; ++k)
     if (there(k)) tile(k).add_up(p, w, tiles[k]);
-  const Weights weights = work.join(p, r, w, token, token_x, tokens.share);
+  const Weights weights = work.join(p, r, w, asked.mine, token_raw, tokens.share);
 #pragma unroll
   for (int k = 0; k < TILES; ++k)
     if (there(k)) tile(k).write(p, r, weights, tokens, tiles[k]);
@@ -907,20 +940,20 @@ template <typename E> __global__ void __launch_bounds__(1024) score_long_row_ker
   const long long r = blockIdx.x;
   const E *x = reinterpret_cast<const E *>(p.x) + r * p.stride_r;
   const auto there = [&](int k) { return k * kWaves + wave < n_tiles; };
-  const auto tile = [&](int k) { return RowTile<E>{(n_tiles - 1 - (k * kWaves + wave)) * 64 * kPer, p.V - kWide<E>}; };
+  const uint32_t last = (uint32_t)(p.V - kWide<E>);
+  const auto tile = [&](int k) { return RowTile<E>{there(k) ? (uint32_t)(n_tiles - 1 - (k * kWaves + wave)) * 64 * kPer : last, last}; };
   word4_any *mine = s_tiles + wave * kLoads * 64 + lane;
-  int token;
-  float token_x;
-  work.read_tokens(p, r, token, token_x);
-  const RowTokens tokens = tokens_of(p, r);
-  Scan<E> w;
+  const FirstTokens asked = first_tokens(p, r);
   // (what registers keep comes last, so that they are free until then)
-  Tile<E> next;
   int k = kRegs;
-  if (there(k)) next = tile(k).template load<true>(x);
+  Tile<E> next = tile(k).template load<true>(x);
+  __builtin_amdgcn_sched_barrier(0);
+  const E token_raw = work.read_tokens(p, r, asked.mine);
+  const RowTokens tokens = tokens_of(p, r, asked);
+  Scan<E> w;
   for (; there(k); ++k) {
     const Tile<E> here = next;
-    if (there(k + 1)) next = tile(k + 1).template load<true>(x);
+    next = tile(k + 1).template load<true>(x);
     if (k < kRegs + kLds) {
 #pragma unroll
       for (int u = 0; u < kLoads; ++u) mine[((k - kRegs) * kWaves * kLoads + u) * 64] = here.w[u];
@@ -929,17 +962,16 @@ template <typename E> __global__ void __launch_bounds__(1024) score_long_row_ker
   }
   Tile<E> tiles[kRegs];
 #pragma unroll
-  for (int k = 0; k < kRegs; ++k)
-    if (there(k)) tiles[k] = tile(k).template load<false>(x);
+  for (int k = 0; k < kRegs; ++k) tiles[k] = tile(k).template load<false>(x);
 #pragma unroll
   for (int k = 0; k < kRegs; ++k)
     if (there(k)) tile(k).add_up(p, w, tiles[k]);
-  const Weights weights = work.join(p, r, w, token, token_x, tokens.share);
+  const Weights weights = work.join(p, r, w, asked.mine, token_raw, tokens.share);
 #pragma unroll
   for (int k = 0; k < kRegs; ++k)
     if (there(k)) tile(k).write(p, r, weights, tokens, tiles[k]);
   k = kRegs + kLds;
-  if (there(k)) next = tile(k).template load<false>(x);
+  next = tile(k).template load<false>(x);
   for (int l = kRegs; l < kRegs + kLds && there(l); ++l) {
     Tile<E> here;
 #pragma unroll
@@ -948,7 +980,7 @@ template <typename E> __global__ void __launch_bounds__(1024) score_long_row_ker
   }
   for (; there(k); ++k) {
     const Tile<E> here = next;
-    if (there(k + 1)) next = tile(k + 1).template load<false>(x);
+    next = tile(k + 1).template load<false>(x);
     tile(k).write(p, r, weights, tokens, here);
   }
 }
@@ -1011,7 +1043,8 @@ template <typename E> hipError_t launch_scores(const ScoreParams &p, hipStream_t
   const long long tiles = (p.chunk + 64 * kPer - 1) / (64 * kPer);
   // us a call with four wavefronts and with eight: 32 000 bf16, 50 alternatives, 256 rows 21.9, 17.7; 512 24.7, 22.6; 768 28.1, 28.3; 2048 53.7, 59.5;
   // 128 256 fp32 256 rows 50.7, 35.4; 512 55.9, 52.2; 768 71.1, 77.3.  (Sixteen: 19.2 and 33.6 at 256 rows, 60 at 512 of the latter.)
-  if (tiles <= 1) score_kernel<E, 1><<<blocks, 64, 0, st>>>(p);
+  if (p.V < kWide<E>) score_kernel<E, 1, true><<<blocks, 64, 0, st>>>(p);
+  else if (tiles <= 1) score_kernel<E, 1><<<blocks, 64, 0, st>>>(p);
   else if (tiles <= 4 || blocks > 512) score_kernel<E, 4><<<blocks, 256, 0, st>>>(p);
   else score_kernel<E, 8><<<blocks, 512, 0, st>>>(p);
   hipError_t e = hipGetLastError();
