@@ -156,31 +156,36 @@ __global__ void __launch_bounds__(kBlock) clip_kernel(const ClipParams p) {
     return (numel & ~kBf16) * ((numel & kBf16) != 0 ? 2 : 4) - (long long)(piece - p.first[j]) * kPiece;
   };
   const auto start = [&](const void *tensor) { return reinterpret_cast<const char *>(tensor) + (long long)(piece - p.first[j]) * kPiece; };
-  // the first piece is on its way while the factor is formed
-  long long left = bytes_left();
-  Piece v;
-  if (left >= kPiece) v = fetch_piece(start(p.from[j]));
-  float factor;
-  if (p.n_partials > 0) {
+  const auto form = [&] {
+    if (p.n_partials == 0) return *p.factor;
     const double norm = sqrt(sum_over_workgroup(sum_of_partials(p.partials, p.n_partials, threadIdx.x, kBlock)));
     if (p.norm != nullptr && blockIdx.x == 0 && threadIdx.x == 0) *p.norm = (float)norm;
-    factor = factor_of(norm, p.max_norm);
+    return factor_of(norm, p.max_norm);
+  };
+  const auto rest = [&](float factor) {
+    if (factor == 1.0f && p.from[j] == p.to[j]) return;
+    char *to = const_cast<char *>(start(p.to[j]));
+    if ((p.numel[j] & kBf16) != 0) scale_rest((const uint16_t *)start(p.from[j]), (uint16_t *)to, bytes_left() / 2, factor);
+    else scale_rest((const float *)start(p.from[j]), (float *)to, bytes_left() / 4, factor);
+  };
+  const auto whole = [&](const Piece &v, float factor) {
+    if (factor != 1.0f || p.from[j] != p.to[j]) scale_whole(v, const_cast<char *>(start(p.to[j])), (p.numel[j] & kBf16) != 0, factor);
+  };
+  // The first piece is on its way while the factor is formed.  (On a way of its own: a load under a condition is waited for where the ways meet.)
+  float factor;
+  if (bytes_left() >= kPiece) {
+    const Piece v = fetch_piece(start(p.from[j]));
+    factor = form();
+    whole(v, factor);
   } else {
-    factor = *p.factor;
+    factor = form();
+    rest(factor);
   }
-  for (;;) {
-    if (factor != 1.0f || p.from[j] != p.to[j]) {
-      const bool bf16 = (p.numel[j] & kBf16) != 0;
-      char *to = const_cast<char *>(start(p.to[j]));
-      if (left >= kPiece) scale_whole(v, to, bf16, factor);
-      else if (bf16) scale_rest((const uint16_t *)start(p.from[j]), (uint16_t *)to, left / 2, factor);
-      else scale_rest((const float *)start(p.from[j]), (float *)to, left / 4, factor);
-    }
-    if (piece < gridDim.x) return;
+  while (piece >= gridDim.x) {
     piece -= gridDim.x;
     j = __builtin_amdgcn_readfirstlane(tensor_of(p, piece));
-    left = bytes_left();
-    if (left >= kPiece) v = fetch_piece(start(p.from[j]));
+    if (bytes_left() >= kPiece) whole(fetch_piece(start(p.from[j])), factor);
+    else rest(factor);
   }
 }
 

@@ -220,10 +220,10 @@ __device__ __forceinline__ void add_positions(const EmbedParams &p, const Column
   if (n - j >= 1) add_some<ALL, 1, A, N>(p, c, t, j, sum);
 }
 
-// What a row of the gradient becomes.
-template <int N> __device__ __forceinline__ void add_scaled(const EmbedParams &p, const float (&before)[N], float (&sum)[N]) {
+// What a row of the gradient becomes.  (ADD is known to the compiler: a load under a condition would be waited for at once.)
+template <bool ADD, int N> __device__ __forceinline__ void add_scaled(const EmbedParams &p, const float (&before)[N], float (&sum)[N]) {
 #pragma unroll
-  for (int i = 0; i < N; ++i) sum[i] = p.add != 0 ? fmaf(sum[i], p.scale, before[i]) : sum[i] * p.scale;
+  for (int i = 0; i < N; ++i) sum[i] = ADD ? fmaf(sum[i], p.scale, before[i]) : sum[i] * p.scale;
 }
 
 // A wavefront's columns of one row, or of a window's share of a row, whose n positions lane i of t holds.
@@ -237,21 +237,21 @@ __device__ __forceinline__ void sum_window(const EmbedParams &p, float *to, int 
     store_columns<N, false>(to, c, sum);
   }
 }
-template <bool ALL, typename A, typename B>
+template <bool ALL, bool ADD, typename A, typename B>
 __device__ __forceinline__ void sum_row(const EmbedParams &p, B *to, int t, int n, long long d0, long long step, int lane) {
   constexpr int N = kWide<A>;
   for (long long d = d0; d < p.D; d += step) {  // (uniform)
     const Columns<N> c = columns_at<ALL, N>(d + lane * N, p.D);
     float sum[N] = {}, before[N] = {};
-    if (p.add != 0) load_columns<ALL, N>(to, c, before);
+    if constexpr (ADD) load_columns<ALL, N>(to, c, before);
     add_positions<ALL, A, N>(p, c, t, n, sum);
-    add_scaled<N>(p, before, sum);
+    add_scaled<ADD, N>(p, before, sum);
     store_columns<N, true>(to, c, sum);
   }
 }
 
 // A wavefront's columns of a long row whose windows are all summed, the same whoever comes last.
-template <bool ALL, typename A, typename B>
+template <bool ALL, bool ADD, typename A, typename B>
 __device__ __forceinline__ void join_row(const EmbedParams &p, int row, int start, int count, long long d0, long long step, int lane) {
   constexpr int N = kWide<A>;
   const int first = start / kWindow, last = (start + count - 1) / kWindow;
@@ -260,23 +260,25 @@ __device__ __forceinline__ void join_row(const EmbedParams &p, int row, int star
   for (long long d = d0; d < p.D; d += step) {  // (uniform)
     const Columns<N> c = columns_at<ALL, N>(d + lane * N, p.D);
     float sum[N] = {}, before[N] = {};
-    if (p.add != 0) load_columns<ALL, N>(to, c, before);
+    if constexpr (ADD) load_columns<ALL, N>(to, c, before);
     for (int v = first; v <= last; v += kAhead) {
-      float part[kAhead][N] = {};
+      float part[kAhead][N];
+#pragma unroll
+      for (int u = 0; u < kAhead; ++u) {  // (without a branch, the last one again where there are fewer)
+        const int at = min(v + u, last);
+        load_columns<ALL, N>(p.partial + (at * 2LL + (at == first ? slot : 0)) * p.D, c, part[u]);
+      }
 #pragma unroll
       for (int u = 0; u < kAhead; ++u)
-        if (v + u <= last) load_columns<ALL, N>(p.partial + ((v + u) * 2LL + (v + u == first ? slot : 0)) * p.D, c, part[u]);
 #pragma unroll
-      for (int u = 0; u < kAhead; ++u)
-#pragma unroll
-        for (int i = 0; i < N; ++i) sum[i] += part[u][i];
+        for (int i = 0; i < N; ++i) sum[i] += v + u <= last ? part[u][i] : 0.0f;
     }
-    add_scaled<N>(p, before, sum);
+    add_scaled<ADD, N>(p, before, sum);
     store_columns<N, true>(to, c, sum);
   }
 }
 
-template <typename A, typename B> __global__ void __launch_bounds__(kBlock) embed_sum_kernel(const EmbedParams p) {
+template <typename A, typename B, bool ADD> __global__ void __launch_bounds__(kBlock) embed_sum_kernel(const EmbedParams p) {
   constexpr int N = kWide<A>;
   const int in_block = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
   const long long wave = (long long)blockIdx.x * (kBlock / 64) + in_block, step = 64LL * N << p.team_log;
@@ -311,8 +313,8 @@ template <typename A, typename B> __global__ void __launch_bounds__(kBlock) embe
       if (lane == 0) before = atomicAdd(&p.arrived[(first << p.team_log) + (int)(wave & ((1 << p.team_log) - 1))], 1);
       if (__builtin_amdgcn_readfirstlane(before) != last - first) continue;
       __threadfence();
-      if (p.D >= N) join_row<true, A, B>(p, row, start, count, d0, step, lane);
-      else join_row<false, A, B>(p, row, start, count, d0, step, lane);
+      if (p.D >= N) join_row<true, ADD, A, B>(p, row, start, count, d0, step, lane);
+      else join_row<false, ADD, A, B>(p, row, start, count, d0, step, lane);
     }
     return;
   }
@@ -325,8 +327,8 @@ template <typename A, typename B> __global__ void __launch_bounds__(kBlock) embe
     const int count = __builtin_amdgcn_readfirstlane(mine.count);
     if (__builtin_amdgcn_readfirstlane(mine.start) != n || count > kWindow) continue;
     B *to = reinterpret_cast<B *>(p.to) + (long long)__builtin_amdgcn_readfirstlane(mine.row) * p.to_stride;
-    if (p.D >= N) sum_row<true, A>(p, to, mine.t, count, d0, step, lane);
-    else sum_row<false, A>(p, to, mine.t, count, d0, step, lane);
+    if (p.D >= N) sum_row<true, ADD, A>(p, to, mine.t, count, d0, step, lane);
+    else sum_row<false, ADD, A>(p, to, mine.t, count, d0, step, lane);
   }
 }
 
@@ -346,7 +348,39 @@ __global__ void __launch_bounds__(kBlock) embed_zero_kernel(const int32_t *start
 
 // Joins the windows of long rows.  A wavefront looks whether a long row starts in its window; the workgroup then takes such
 // rows one after the other, 256 columns of them, every sixteenth window a wavefront, in an order that follows from the row's place alone.
-template <typename B> __global__ void __launch_bounds__(kJoinThreads) embed_join_kernel(const EmbedParams p) {
+// A row's joined columns, all wavefronts of a workgroup.
+template <bool ALL, bool ADD, typename B>
+__device__ __forceinline__ void join_columns(const EmbedParams &p, float (&s_sum)[kJoinThreads / 64][64 * 4], B *to, long long first, long long last, int slot,
+                                             long long d0) {
+  constexpr int N = 4, kWaves = kJoinThreads / 64;
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const Columns<N> c = columns_at<ALL, N>(d0 + lane * N, p.D);
+  float sum[N] = {}, before[N] = {};
+  if constexpr (ADD) load_columns<ALL, N>(to, c, before);
+  for (long long v = first + wave; v <= last; v += kWaves * kAhead) {
+    float part[kAhead][N];
+#pragma unroll
+    for (int u = 0; u < kAhead; ++u) {  // (without a branch, the last one again where there are fewer)
+      const long long at = v + u * kWaves < last ? v + u * kWaves : last;
+      load_columns<ALL, N>(p.partial + (at * 2 + (at == first ? slot : 0)) * p.D, c, part[u]);
+    }
+#pragma unroll
+    for (int u = 0; u < kAhead; ++u)
+#pragma unroll
+      for (int j = 0; j < N; ++j) sum[j] += v + u * kWaves <= last ? part[u][j] : 0.0f;
+  }
+  __syncthreads();
+#pragma unroll
+  for (int j = 0; j < N; ++j) s_sum[wave][lane * N + j] = sum[j];
+  __syncthreads();
+  if (wave != 0) return;
+#pragma unroll
+  for (int j = 0; j < N; ++j)
+    for (int v = 1; v < kWaves; ++v) sum[j] += s_sum[v][lane * N + j];
+  add_scaled<ADD, N>(p, before, sum);
+  store_columns<N, true>(to, c, sum);
+}
+template <typename B, bool ADD> __global__ void __launch_bounds__(kJoinThreads) embed_join_kernel(const EmbedParams p) {
   constexpr int N = 4, kWaves = kJoinThreads / 64;
   __shared__ float s_sum[kWaves][64 * N];
   __shared__ Place s_row[kWaves];
@@ -369,35 +403,10 @@ template <typename B> __global__ void __launch_bounds__(kJoinThreads) embed_join
     if (row < 0) continue;  // (uniform)
     const long long w = (long long)blockIdx.x * kWaves + i, last = ((long long)s_row[i].start + s_row[i].count - 1) / kWindow;
     const bool inside = s_row[i].start != w * kWindow;  // (of its first window: then the second of the two partial rows)
+    B *to = reinterpret_cast<B *>(p.to) + (long long)row * p.to_stride;
     for (long long d0 = (long long)blockIdx.y * 64 * N; d0 < p.D; d0 += (long long)gridDim.y * 64 * N) {
-      const long long d = d0 + lane * N;
-      float sum[N] = {}, before[N] = {};
-      B *to = reinterpret_cast<B *>(p.to) + (long long)row * p.to_stride + d;
-      if (wave == 0 && d < p.D && p.add != 0) load_first<N>(to, p.D - d, before);
-      if (d < p.D)
-        for (long long v = w + wave; v <= last; v += kWaves * kAhead) {
-          float part[kAhead][N] = {};
-#pragma unroll
-          for (int u = 0; u < kAhead; ++u) {
-            const long long at = v + u * kWaves;
-            if (at <= last) load_first<N>(p.partial + (at * 2 + (at == w && inside ? 1 : 0)) * p.D + d, p.D - d, part[u]);
-          }
-#pragma unroll
-          for (int u = 0; u < kAhead; ++u)
-#pragma unroll
-            for (int j = 0; j < N; ++j) sum[j] += part[u][j];
-        }
-      __syncthreads();
-#pragma unroll
-      for (int j = 0; j < N; ++j) s_sum[wave][lane * N + j] = sum[j];
-      __syncthreads();
-      if (wave == 0 && d < p.D) {
-#pragma unroll
-        for (int j = 0; j < N; ++j)
-          for (int v = 1; v < kWaves; ++v) sum[j] += s_sum[v][lane * N + j];
-        add_scaled<N>(p, before, sum);
-        stream_first<N>(to, p.D - d, sum);
-      }
+      if (p.D >= N) join_columns<true, ADD>(p, s_sum, to, w, last, inside ? 1 : 0, d0);
+      else join_columns<false, ADD>(p, s_sum, to, w, last, inside ? 1 : 0, d0);
     }
   }
 }
@@ -530,12 +539,16 @@ extern "C" int llc_embed_grad(const llc_embed_grad_args *a) {
         e = hipGetLastError();
       }
       if (e != hipSuccess || p.T == 0) return e;
-      embed_sum_kernel<decltype(from), B><<<(unsigned)(window_blocks + sum_blocks), kBlock, 0, st>>>(p);
+      const unsigned sums = (unsigned)(window_blocks + sum_blocks);
+      if (p.add != 0) embed_sum_kernel<decltype(from), B, true><<<sums, kBlock, 0, st>>>(p);
+      else embed_sum_kernel<decltype(from), B, false><<<sums, kBlock, 0, st>>>(p);
       e = hipGetLastError();
       if (e != hipSuccess || p.windows == 0 || p.arrived != nullptr) return e;
       const long long groups = (p.windows + kJoinThreads / 64 - 1) / (kJoinThreads / 64);
       const long long slabs = (a->D + 255) / 256, most = kMostBlocks / 4 / groups, join = slabs < most ? slabs : most;
-      embed_join_kernel<decltype(to)><<<dim3((unsigned)groups, (unsigned)(join < 1 ? 1 : join < 64 ? join : 64)), kJoinThreads, 0, st>>>(p);
+      const dim3 grid((unsigned)groups, (unsigned)(join < 1 ? 1 : join < 64 ? join : 64));
+      if (p.add != 0) embed_join_kernel<B, true><<<grid, kJoinThreads, 0, st>>>(p);
+      else embed_join_kernel<B, false><<<grid, kJoinThreads, 0, st>>>(p);
       return hipGetLastError();
     });
   });
