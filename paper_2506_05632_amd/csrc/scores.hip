@@ -9,8 +9,8 @@
 // none costs one comparison a lane.  Candidates go to a list of the wavefront's in LDS as
 // whole numbers that order as (value, lower index first); a full list is cut to its M largest, which raises the wavefront's bound.  At the end a
 // histogram over the numbers' range finds a bound that at most kSelected of them reach, and those are ranked by comparing all with all.
-// What bounds it: reading the rows where there are many (1024 x 128 256 fp32 with 50 alternatives 91 us, 5.8 TB/s), and otherwise how long one workgroup's steps
-// take one after the other (256 x 32 000 bf16 with 20 alternatives 15 us, 8.5 without any).
+// What bounds it: reading the rows where there are many (1024 x 128 256 fp32 with 50 alternatives 88 us, 6.0 TB/s), and otherwise how long one workgroup's steps
+// take one after the other (256 x 32 000 bf16 with 20 alternatives 15 us, 8 without any).
 #include "ends.hpp"
 
 namespace llc {
@@ -576,8 +576,8 @@ template <typename E, int WAVES, bool TINY = false> __global__ void __launch_bou
                                            : look_at_list<kList / 64>(list, w.count, share, speaks, s_nth, WAVES, wave));
   };
   // A list is looked at after the wavefront's second, fourth, eighth tile, and so on, unless nothing follows; after the first too where so large a share soon
-  // fills it.  (Always after the first, and never: 4 x 32 000 bf16 with 5 alternatives 12.5 us, 12.0; 300 rows with 20 19.9, 18.3; but 1024 rows with 128
-  // of four wavefronts 41.5, 52.  From the fourth on: 256 x 128 256 bf16 with 50 35.3 for 32.6, from the eighth 45.3.)
+  // fills it.  (Always after the first, and never: 4 x 32 000 bf16 with 5 alternatives 12.7 us, 11.2; 300 rows with 20 19.8, 18.3; but 1024 rows with 128
+  // of four wavefronts 41.0, 51.7.  From the eighth on 256 x 128 256 bf16 with 50 takes 45 for 32.)
   const int first_look = share > 16 ? 1 : 2;
   // two tiles in turn, so that one is on its way while the other is taken
   const long long step = (long long)WAVES * kTile;
@@ -667,7 +667,7 @@ __device__ __forceinline__ Weights uniform(const Weights &w) {  // (all lanes ha
   return Weights{one(w.top), one(w.shift), one(w.c), one(w.a), one(w.b), one(w.inv_t), one(w.line), __builtin_amdgcn_readfirstlane(w.form)};
 }
 // A row's tokens and their weights: lane i has the i-th, and its share of the sum of all valid ones' weights.  (Read again for every
-// tile: gradient of 2048 x 32 000 bf16 63 us, so 60.)
+// tile they cost the gradient of 2048 x 32 000 bf16 3 us.)
 struct RowTokens {
   int token;
   float weight;
@@ -820,7 +820,9 @@ template <typename E> __global__ void __launch_bounds__(kBlock) score_grad_kerne
   store_tile(reinterpret_cast<E *>(p.grad) + r * p.grad_stride_r, at, p.V, v);
 }
 
-// Scores and gradient in one pass: a workgroup keeps a row on the chip.  What its wavefronts share:
+// Scores and gradient in one pass: a workgroup keeps a row on the chip.  Memory bounds it, and the issue of two exponentials an entry: 2048 x 32 000 bf16
+// 50 us, 5.2 TB/s read and written; 768 x 128 256 fp32 with 8 tokens and entropies 152 us, as much.  (A CU's rows load, join and write in part at the same time:
+// of 25 us that a bf16 row takes there, 12 pass until all of it is summed, 3 until its wavefronts know so, 7 with writing.)  What its wavefronts share:
 template <typename E, int WAVES> struct RowWork {
   double s_s[WAVES], s_d[WAVES];
   float s_m[WAVES];
@@ -931,7 +933,8 @@ __global__ void __launch_bounds__(WAVES * 64, TILES * sizeof(E) > 8 ? 4 : TILES 
     if (there(k)) tile(k).write(p, r, weights, tokens, tiles[k]);
 }
 
-// A longer row: a part in registers, a part in LDS, and what is left is read twice, the second time from the caches.
+// A longer row: a part in registers, a part in LDS, and what is left is read twice, the second time from the caches.  (768 x 128 256 fp32 with four tiles in
+// registers 157 us for 154 with three; five spill, 160.)
 template <typename E> __global__ void __launch_bounds__(1024) score_long_row_kernel(const ScoreParams p, int n_tiles) {
   constexpr int kWaves = 16, kLoads = RowTile<E>::kLoads, kRegs = sizeof(E) == 2 ? 8 : 3, kLds = sizeof(E) == 2 ? 4 : 2;
   __shared__ RowWork<E, kWaves> work;
@@ -996,10 +999,12 @@ size_t rows_workspace(long long R, long long M, long long chunks) {  // shares a
   return (size_t)chunks * (size_t)R * (sizeof(Share) + 8 * (size_t)M) + 32 * (size_t)R + 512;
 }
 
-// Workgroups that a row is split over: as many as leave each 16 000 entries, as far as there are CUs for them, if that is three or more: the second launch takes
-// some 3 us.  us a call of 50 alternatives, whole and split: 1 x 128 256 fp32 28, 19 (8); 64 x 128 256 32, 25 (4); 128 x 152 064 bf16 34, 30 (2, not taken);
-// 4 x 32 000 bf16 15.7, 18.0 (2, not taken); 1 x 4 194 304 fp32 405, 43 (64).
+// Workgroups that a row is split over: as many as leave each 16 000 entries, as far as there are CUs for them, if that is three or more and the row has 64 000: the
+// second launch takes some 3 us.  us a call with 50 alternatives, whole and split: 1 x 128 256 fp32 27.4, 19.3 (8); 64 x 128 256 30.2, 24.9 (4); 85 x 128 256 bf16
+// 30.2, 24.9 (3); 1 x 4 194 304 fp32 321, 42 (64); 64 x 64 000 22.8, 21.3 (4); not taken: 1 x 50 257 17.2, 18.6 (3); 85 x 50 257 19.5, 21.6 (3); 128 x 152 064
+// bf16 31.8, 28.3 (2), 4 x 32 000 bf16 15.2, 17.2 (2).
 int auto_split(long long R, long long V) {
+  if (V < 64000) return 1;
   long long split = V / 16000;
   if (split > 256 / (R > 0 ? R : 1)) split = 256 / (R > 0 ? R : 1);
   return (int)(split < 3 ? 1 : split < kMostSplit ? split : kMostSplit);
@@ -1020,8 +1025,8 @@ template <typename E> hipError_t launch_gradient(ScoreParams p, hipStream_t st) 
 
 // Scores and gradient in one launch: as many wavefronts as keep the row in registers.  Rows too long for that are a workgroup's too where the scores would
 // not be split (many rows: a CU has one at least), else scores and gradient are two launches over all CUs.  us a call, one launch and two (three where
-// split): 70 001 fp32 of 64 rows 19.0, 17.0, of 96 19.7, 23.7, of 256 31.3, 42.1; 128 256 fp32 28.0, 24.9; 28.6, 36.0; 46.8, 67.9; 152 064
-// bf16 33.0, 22.1; 33.2, 32.9; 38.7, 49.5; 300 000 bf16 55.4, 31.0; 55.3, 54.6; 69.0, 86.7.  False: nothing was launched.
+// split): 70 001 fp32 of 64 rows 18.0, 16.9, of 96 18.9, 22.6, of 256 29.9, 41.4; 128 256 fp32 26.8, 24.0; 27.4, 33.7; 45.8, 66.6; 152 064
+// bf16 29.2, 20.4; 29.6, 29.7; 35.1, 46.3; 300 000 bf16 52.7, 29.6; 53.5, 48.4; 65.6, 82.4.  False: nothing was launched.
 template <typename E> bool launch_rows(const ScoreParams &p, hipStream_t st) {
   const long long tiles = (p.V + 64 * kPer - 1) / (64 * kPer);
   constexpr bool kHalf = sizeof(E) == 2;
@@ -1041,8 +1046,8 @@ template <typename E> bool launch_rows(const ScoreParams &p, hipStream_t st) {
 template <typename E> hipError_t launch_scores(const ScoreParams &p, hipStream_t st) {
   const unsigned blocks = (unsigned)(p.R * p.chunks);
   const long long tiles = (p.chunk + 64 * kPer - 1) / (64 * kPer);
-  // us a call with four wavefronts and with eight: 32 000 bf16, 50 alternatives, 256 rows 21.9, 17.7; 512 24.7, 22.6; 768 28.1, 28.3; 2048 53.7, 59.5;
-  // 128 256 fp32 256 rows 50.7, 35.4; 512 55.9, 52.2; 768 71.1, 77.3.  (Sixteen: 19.2 and 33.6 at 256 rows, 60 at 512 of the latter.)
+  // us a call with four wavefronts and with eight: 32 000 bf16, 50 alternatives, 256 rows 23.0, 17.7; 512 24.9, 22.8; 768 28.5, 27.5; 2048 52.7, 58.6; without
+  // alternatives 768 13.4, 14.3; 128 256 fp32 256 rows 45.7, 32.8; 512 53.9, 50.4; 2048 166, 165.  (Sixteen: 16.9 and 32.5 at 256 rows, 29.7 and 59 at 512.)
   if (p.V < kWide<E>) score_kernel<E, 1, true><<<blocks, 64, 0, st>>>(p);
   else if (tiles <= 1) score_kernel<E, 1><<<blocks, 64, 0, st>>>(p);
   else if (tiles <= 4 || blocks > 512) score_kernel<E, 4><<<blocks, 256, 0, st>>>(p);

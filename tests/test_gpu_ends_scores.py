@@ -318,7 +318,7 @@ def test_gradient_of_many_long_rows(R, V, dtype):
 
 
 @pytest.mark.parametrize("dtype", [F32, BF16])
-@pytest.mark.parametrize("R,V", [(1, 47999), (1, 48000), (5, 63999), (85, 50001), (86, 50001), (4, 300007)])
+@pytest.mark.parametrize("R,V", [(1, 47999), (1, 48000), (5, 63999), (5, 64000), (85, 50001), (86, 50001), (85, 64001), (86, 64001), (4, 300007)])
 def test_scores_where_rows_begin_to_be_split(R, V, dtype):
     x, t = _rows(R, V, dtype, R + V), _tokens(R, 300 if R < 6 else 2, V, R)
     ref.check_scores(llc.llc_token_logprobs(x, t, 40, temp=0.8, want_lse=True), x, t, 40, 0.8)
