@@ -775,8 +775,11 @@ def _scored(name, x, tokens, kind):
     return R, V, 1 if tokens.dim() == 1 else tokens.shape[1]
 
 
-def _scratch(workspace, nbytes, device):
-    """The caller's workspace, or a new one (`nbytes`: a function, for the size is not needed otherwise)."""
+def _scratch(workspace, nbytes, device, specs=None):
+    """The caller's workspace, or a new one (`nbytes`: a function, for the size is not needed otherwise), or its entry among tensors still to be made."""
+    if workspace is None and specs is not None:
+        specs["workspace"] = (torch.uint8, max(nbytes(), 256))
+        return None
     if workspace is None:
         return torch.empty(max(nbytes(), 256), dtype=torch.uint8, device=device)
     if workspace.device != device or workspace.dtype != torch.uint8 or not workspace.is_contiguous():
@@ -822,11 +825,14 @@ def llc_token_logprobs(logits: torch.Tensor, tokens: Optional[torch.Tensor], M: 
         if M > 0:
             specs["top_ids"] = (torch.int32, R, M)
             specs["top_logp"] = (torch.float32, R, M)
+        workspace = _scratch(workspace, lambda: _score_bytes(R, V, M, v_chunks), dev, specs)
         out = _new(dev, specs)
+        if workspace is None:
+            workspace = out.pop("workspace")
     else:
         _check_given(out, dev, {"logp": (torch.float32, *(tokens.shape if tokens is not None else ())), "entropy": (torch.float32, R),
                                 "lse": (torch.float64, R, 2), "top_ids": (torch.int32, R, M), "top_logp": (torch.float32, R, M)})
-    workspace = _scratch(workspace, lambda: _score_bytes(R, V, M, v_chunks), dev)
+        workspace = _scratch(workspace, lambda: _score_bytes(R, V, M, v_chunks), dev)
     a = TokenLogprobsArgs()
     a.R, a.V, a.G, a.M = R, V, G, M
     a.dtype, a.kind = _TYPES[logits.dtype], _KINDS[kind]
@@ -875,15 +881,19 @@ def llc_token_logprobs_grad(logits: torch.Tensor, tokens: Optional[torch.Tensor]
             if tokens is not None:
                 specs["logp"] = (torch.float32, *tokens.shape)
             specs["entropy"] = (torch.float32, R)
+        if lse is None:
+            workspace = _scratch(workspace, lambda: _score_bytes(R, V, 0, v_chunks), dev, specs)
         out = _new(dev, specs)
+        if lse is None and workspace is None:
+            workspace = out.pop("workspace")
     else:
         _check_given(out, dev, {"logp": (torch.float32, *(tokens.shape if tokens is not None else ())), "entropy": (torch.float32, R),
                                 "lse": (torch.float64, R, 2)})
+        if lse is None:
+            workspace = _scratch(workspace, lambda: _score_bytes(R, V, 0, v_chunks), dev)
     grad = out["grad"]
     if grad.device != dev or grad.dtype != logits.dtype or tuple(grad.shape) != (R, V) or (grad.stride(1) != 1 and V > 1):
         raise ValueError("grad must be [R,V] of the logits' type, last dimension contiguous")
-    if lse is None:
-        workspace = _scratch(workspace, lambda: _score_bytes(R, V, 0, v_chunks), dev)
     a = TokenLogprobsGradArgs()
     a.R, a.V, a.G = R, V, G
     a.dtype, a.kind = _TYPES[logits.dtype], _KINDS[kind]
@@ -921,7 +931,10 @@ def llc_embed(table: torch.Tensor, tokens: torch.Tensor, *, scale: float = 1.0, 
     N, D = table.shape
     tokens, shape = _flat(tokens), tokens.shape
     if out is None:
-        out = _new(table.device, {"out": (out_dtype or table.dtype, tokens.shape[0], D)})["out"].view(*shape, D)
+        if len(shape) < 4:
+            out = _new(table.device, {"out": (out_dtype or table.dtype, *shape, D)})["out"]
+        else:
+            out = _new(table.device, {"out": (out_dtype or table.dtype, tokens.shape[0], D)})["out"].view(*shape, D)
     rows = out if out.dim() == 2 else out.view(-1, out.shape[-1])
     if (out.device != table.device or out.dtype not in _TYPES or out_dtype not in (None, out.dtype) or tuple(out.shape) != (*shape, D)
             or (rows.stride(1) != 1 and D > 1)):

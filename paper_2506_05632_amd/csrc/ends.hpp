@@ -46,24 +46,6 @@ template <int N> __device__ __forceinline__ void load_some(const uint16_t *p, fl
     split_pair(t.x, v[0], v[1]); split_pair(t.y, v[2], v[3]); split_pair(t.z, v[4], v[5]); split_pair(t.w, v[6], v[7]);
   }
 }
-// The same for what is not read again soon.
-template <int N> __device__ __forceinline__ void fetch_some(const float *p, float (&v)[N]) {
-#pragma unroll
-  for (int i = 0; i < N; i += 4) {
-    const float4_any t = __builtin_nontemporal_load(reinterpret_cast<const float4_any *>(p + i));
-    v[i] = t.x; v[i + 1] = t.y; v[i + 2] = t.z; v[i + 3] = t.w;
-  }
-}
-template <int N> __device__ __forceinline__ void fetch_some(const uint16_t *p, float (&v)[N]) {
-  static_assert(N == 4 || N == 8, "a load of 8 or 16 bytes");
-  if constexpr (N == 4) {
-    const word2_any t = __builtin_nontemporal_load(reinterpret_cast<const word2_any *>(p));
-    split_pair(t.x, v[0], v[1]); split_pair(t.y, v[2], v[3]);
-  } else {
-    const word4_any t = __builtin_nontemporal_load(reinterpret_cast<const word4_any *>(p));
-    split_pair(t.x, v[0], v[1]); split_pair(t.y, v[2], v[3]); split_pair(t.z, v[4], v[5]); split_pair(t.w, v[6], v[7]);
-  }
-}
 template <int N> __device__ __forceinline__ void store_some(float *p, const float (&v)[N]) {
 #pragma unroll
   for (int i = 0; i < N; i += 4) *reinterpret_cast<float4_any *>(p + i) = float4_any{v[i], v[i + 1], v[i + 2], v[i + 3]};

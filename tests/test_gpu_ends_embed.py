@@ -60,6 +60,14 @@ def test_lookup_shapes_strides_and_guards():
     assert llc.llc_embed(table, t[:0])["out"].shape == (0, 6, 99)
 
 
+def test_lookup_of_tokens_of_any_shape():
+    table = _normal((50, 33), BF16, 1)
+    for shape in ((), (1,), (3, 1), (2, 3, 4), (2, 1, 3, 2), (2, 1, 3, 2, 2), (0,), (2, 0, 3)):
+        t = _ids(max(math.prod(shape), 1), 50, 4)[: math.prod(shape)].view(shape)
+        out = llc.llc_embed(table, t, out_dtype=F32)["out"]
+        assert out.shape == (*shape, 33) and out.is_contiguous() and torch.equal(out, _plain_lookup(table, t, 1.0, F32))
+
+
 def test_a_table_beyond_32_bits():
     N, D = (1 << 19) + 3, 4096  # 2^31 and some entries
     table = torch.empty(N, D, dtype=BF16, device=DEV)
