@@ -800,24 +800,43 @@ template <typename E> __device__ __forceinline__ void store_tile(E *row, long lo
   }
 }
 
-// From a row's lse and entropy: a tile a wavefront.
+// From a row's lse and entropy: a wavefront takes 4 KB of it, in one tile or two.  (us with one tile, with two and with four: 2048 x 32 000 bf16 52, 46 (5.7 TB/s), 52;
+// 512 x 152 064 bf16 with entropies 56, 52, 58; 768 x 128 256 fp32 with entropies 126 (6.3 TB/s), 132, 142.)
+template <typename E> constexpr int kTilesOf = sizeof(E) == 2 ? 2 : 1;
 template <typename E> __global__ void __launch_bounds__(kBlock) score_grad_kernel(const ScoreParams p) {
+  constexpr int kTile = 64 * kPer, TILES = kTilesOf<E>;
   const long long r = blockIdx.x / p.chunks;
-  const int part = (int)(blockIdx.x - r * p.chunks), wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const long long at = ((long long)part * (kBlock / 64) + wave) * 64 * kPer;
-  if (at >= p.V) return;
+  const int part = (int)(blockIdx.x - r * p.chunks), wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
+  const long long begin = ((long long)part * (kBlock / 64) + wave) * kTile * TILES;
+  if (begin >= p.V) return;
   const E *x = reinterpret_cast<const E *>(p.x) + r * p.stride_r;
+  E *grad = reinterpret_cast<E *>(p.grad) + r * p.grad_stride_r;
   const FirstTokens asked = first_tokens(p, r);
-  const Tile<E> tile = load_at(x, at, p.V);
-  __builtin_amdgcn_sched_barrier(0);
-  const RowTokens tokens = tokens_of(p, r, asked);
-  const Weights w = weights_of(p, r, tokens.share, p.lse_in[2 * r], p.lse_in[2 * r + 1], p.b != nullptr ? (double)p.entropy_in[r] : 0.0);
-  float v[kPer];
-  unpack(tile, v);
-  entry_gradients(w, v);
-  const int lane = threadIdx.x & 63, high = (int)(at + 64 * kPer < p.V ? at + 64 * kPer : p.V);
-  token_gradients(p, r, w, tokens, tile, v, (int)at, high, [&](int u) { return (int)at + (u * 64 + lane) * kWide<E>; });
-  store_tile(reinterpret_cast<E *>(p.grad) + r * p.grad_stride_r, at, p.V, v);
+  const auto weights = [&](const RowTokens &tokens) {
+    return weights_of(p, r, tokens.share, p.lse_in[2 * r], p.lse_in[2 * r + 1], p.b != nullptr ? (double)p.entropy_in[r] : 0.0);
+  };
+  const auto write = [&](const Weights &w, const RowTokens &tokens, const Tile<E> &tile, long long at) {
+    float v[kPer];
+    unpack(tile, v);
+    entry_gradients(w, v);
+    const int high = (int)(at + kTile < p.V ? at + kTile : p.V);
+    token_gradients(p, r, w, tokens, tile, v, (int)at, high, [&](int u) { return (int)at + (u * 64 + lane) * kWide<E>; });
+    store_tile(grad, at, p.V, v);
+  };
+  if (begin + kTile * TILES <= p.V) {
+    Tile<E> tiles[TILES];
+#pragma unroll
+    for (int k = 0; k < TILES; ++k) tiles[k] = load_tile(x + begin + k * kTile + lane * kWide<E>);
+    __builtin_amdgcn_sched_barrier(0);
+    const RowTokens tokens = tokens_of(p, r, asked);
+    const Weights w = weights(tokens);
+#pragma unroll
+    for (int k = 0; k < TILES; ++k) write(w, tokens, tiles[k], begin + k * kTile);
+  } else {
+    const RowTokens tokens = tokens_of(p, r, asked);
+    const Weights w = weights(tokens);
+    for (long long at = begin; at < p.V; at += kTile) write(w, tokens, load_at(x, at, p.V), at);
+  }
 }
 
 // Scores and gradient in one pass: a workgroup keeps a row on the chip.  Memory bounds it, and the issue of two exponentials an entry: 2048 x 32 000 bf16
@@ -1018,7 +1037,7 @@ void split_rows(ScoreParams &p, long long want) {
 }
 
 template <typename E> hipError_t launch_gradient(ScoreParams p, hipStream_t st) {
-  p.chunks = (int)((p.V + kBlock * kPer - 1) / (kBlock * kPer));
+  p.chunks = (int)(((long long)p.V + kBlock * kPer * kTilesOf<E> - 1) / (kBlock * kPer * kTilesOf<E>));
   score_grad_kernel<E><<<(unsigned)(p.R * p.chunks), kBlock, 0, st>>>(p);
   return hipGetLastError();
 }
@@ -1028,7 +1047,7 @@ template <typename E> hipError_t launch_gradient(ScoreParams p, hipStream_t st) 
 // split): 70 001 fp32 of 64 rows 18.0, 16.9, of 96 18.9, 22.6, of 256 29.9, 41.4; 128 256 fp32 26.8, 24.0; 27.4, 33.7; 45.8, 66.6; 152 064
 // bf16 29.2, 20.4; 29.6, 29.7; 35.1, 46.3; 300 000 bf16 52.7, 29.6; 53.5, 48.4; 65.6, 82.4.  False: nothing was launched.
 template <typename E> bool launch_rows(const ScoreParams &p, hipStream_t st) {
-  const long long tiles = (p.V + 64 * kPer - 1) / (64 * kPer);
+  const long long tiles = ((long long)p.V + 64 * kPer - 1) / (64 * kPer);
   constexpr bool kHalf = sizeof(E) == 2;
   const unsigned rows = (unsigned)p.R;
   if (p.V < kWide<E>) return false;
@@ -1045,7 +1064,7 @@ template <typename E> bool launch_rows(const ScoreParams &p, hipStream_t st) {
 
 template <typename E> hipError_t launch_scores(const ScoreParams &p, hipStream_t st) {
   const unsigned blocks = (unsigned)(p.R * p.chunks);
-  const long long tiles = (p.chunk + 64 * kPer - 1) / (64 * kPer);
+  const long long tiles = ((long long)p.chunk + 64 * kPer - 1) / (64 * kPer);
   // us a call with four wavefronts and with eight: 32 000 bf16, 50 alternatives, 256 rows 23.0, 17.7; 512 24.9, 22.8; 768 28.5, 27.5; 2048 52.7, 58.6; without
   // alternatives 768 13.4, 14.3; 128 256 fp32 256 rows 45.7, 32.8; 512 53.9, 50.4; 2048 166, 165.  (Sixteen: 16.9 and 32.5 at 256 rows, 29.7 and 59 at 512.)
   if (p.V < kWide<E>) score_kernel<E, 1, true><<<blocks, 64, 0, st>>>(p);

@@ -324,6 +324,28 @@ def test_scores_where_rows_begin_to_be_split(R, V, dtype):
     ref.check_scores(llc.llc_token_logprobs(x, t, 40, temp=0.8, want_lse=True), x, t, 40, 0.8)
 
 
+def test_the_longest_row():
+    V = 2 ** 31 - 5
+    x = torch.full((1, V), -float("inf"), dtype=BF16, device=DEV)
+    places = [0, 5, V // 2, V - 1030, V - 1025, V - 9, V - 2, V - 1]
+    values = torch.tensor([0.5, -1.0, 2.0, 1.0, 0.25, -2.0, 3.0, 1.5], dtype=BF16)
+    x[0, places] = values.to(DEV)
+    small = values.float().view(1, -1)  # (the same row without what has no mass)
+    t = torch.tensor([[V - 1, 0, -1, V - 1030]], dtype=torch.int32, device=DEV)
+    a, b = torch.tensor([[0.5, -1.0, 2.0, 0.25]], device=DEV), torch.tensor([0.7], device=DEV)
+    for chunks in (0, 1):
+        out = llc.llc_token_logprobs(x, t, 10, want_lse=True, v_chunks=chunks)
+        ref.check_scores({k: out[k] for k in ("entropy", "lse")}, small, None, 0, 1.0)
+        order = torch.argsort(values.float(), descending=True)
+        assert out["top_ids"][0].tolist() == [places[i] for i in order] + [-1, -1]
+        lp = torch.log_softmax(values.double(), 0)
+        assert (out["logp"][0].cpu().double() - torch.stack([lp[7], lp[0], lp.new_zeros(()), lp[3]])).abs().max() < 1e-5
+    want, tol = ref.gradient(small, torch.tensor([[7, 0, -1, 3]]), a.cpu(), b.cpu(), 1.0)
+    got = llc.llc_token_logprobs_grad(x, t, a, grad_entropy=b, out={"grad": x})["grad"]
+    assert torch.count_nonzero(got) == 8
+    assert (np.abs(got[0, places].cpu().double().numpy() - want[0]) <= tol[0] + ref.OUT[BF16] * np.abs(want[0])).all()
+
+
 def test_gradient_against_differences():
     # f(x + h v) - f(x - h v) over 2 h for directions v of length one: the third derivative of these sums is below
     # 2 (|a| + |b| (1 + ln V)) / T^3, and f is known to 2e-6 of its weights, so h = 2^-5 leaves 3e-4 of them
