@@ -1044,8 +1044,8 @@ template <typename E> hipError_t launch_gradient(ScoreParams p, hipStream_t st) 
 
 // Scores and gradient in one launch: as many wavefronts as keep the row in registers.  Rows too long for that are a workgroup's too where the scores would
 // not be split (many rows: a CU has one at least), else scores and gradient are two launches over all CUs.  us a call, one launch and two (three where
-// split): 70 001 fp32 of 64 rows 18.0, 16.9, of 96 18.9, 22.6, of 256 29.9, 41.4; 128 256 fp32 26.8, 24.0; 27.4, 33.7; 45.8, 66.6; 152 064
-// bf16 29.2, 20.4; 29.6, 29.7; 35.1, 46.3; 300 000 bf16 52.7, 29.6; 53.5, 48.4; 65.6, 82.4.  False: nothing was launched.
+// split): 70 001 fp32 of 64 rows 18.1, 18.4, of 96 18.5, 22.5, of 256 30.2, 40.9; 128 256 fp32 26.9, 23.8; 27.3, 33.4; 45.9, 66.1; 152 064
+// bf16 29.4, 19.3; 29.8, 28.9; 34.8, 45.3; 300 000 bf16 53.0, 29.1; 53.6, 48.0; 66.6, 80.5.  False: nothing was launched.
 template <typename E> bool launch_rows(const ScoreParams &p, hipStream_t st) {
   const long long tiles = ((long long)p.V + 64 * kPer - 1) / (64 * kPer);
   constexpr bool kHalf = sizeof(E) == 2;
