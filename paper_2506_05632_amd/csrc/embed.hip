@@ -17,6 +17,7 @@ namespace {
 constexpr int kWindow = 32;       // sorted positions a wavefront adds up
 constexpr int kAhead = 4;         // rows that are fetched together (8 take the registers of three wavefronts a SIMD: 65 536 tokens 402 us for 338)
 constexpr int kJoinThreads = 1024;
+constexpr int kFewJoins = 16;     // windows of a row that a wavefront joins by itself
 constexpr int kMostRange = 896;   // rows of the table that a workgroup of the sort takes (its counters: 60 KB of LDS)
 constexpr long long kMostRows = 1LL << 27;
 
@@ -43,6 +44,7 @@ struct EmbedParams {
   float *partial;           // [windows][2][D]
   int *arrived;             // [windows][team] wavefronts that are done with the long row that starts in a window; null: a launch of its own joins them
   long long windows;
+  int join_each;            // windows that a wavefront of the joining launch looks at, 64 at most
   unsigned window_blocks, sum_blocks;  // of the summing launch: windows, then sorted positions
 };
 
@@ -346,8 +348,8 @@ __global__ void __launch_bounds__(kBlock) embed_zero_kernel(const int32_t *start
   if (d < D) stream_first<kStore>(to + row * to_stride + d, D - d, none);
 }
 
-// Joins the windows of long rows.  A wavefront looks whether a long row starts in its window; the workgroup then takes such
-// rows one after the other, 256 columns of them, every sixteenth window a wavefront, in an order that follows from the row's place alone.
+// Joins the windows of long rows, 256 columns a workgroup.  A wavefront looks whether long rows start in its windows and joins the shorter ones; the longer ones are
+// the workgroup's, one after the other, every sixteenth window a wavefront, in an order that follows from the row's place alone.
 // A row's joined columns, all wavefronts of a workgroup.
 template <bool ALL, bool ADD, typename B>
 __device__ __forceinline__ void join_columns(const EmbedParams &p, float (&s_sum)[kJoinThreads / 64][64 * 4], B *to, long long first, long long last, int slot,
@@ -383,30 +385,43 @@ __device__ __forceinline__ void join_columns(const EmbedParams &p, float (&s_sum
 template <typename B, bool ADD> __global__ void __launch_bounds__(kJoinThreads) embed_join_kernel(const EmbedParams p) {
   constexpr int N = 4, kWaves = kJoinThreads / 64;
   __shared__ float s_sum[kWaves][64 * N];
-  __shared__ Place s_row[kWaves];
+  __shared__ Place s_row[64 + 1];  // (rows that start in the workgroup's windows, each more than kFewJoins of them long)
+  __shared__ int s_n;
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  {
-    const long long begin = ((long long)blockIdx.x * kWaves + wave) * kWindow;
-    Place row = {0, -1, 0, 0};
-    if (begin < p.T) {
-      const int total = p.starts[p.N];
-      const int until = p.T - begin < kWindow ? (int)p.T : (int)begin + kWindow;
-      Place last = p.places[until - 1];
-      if (total < until && total > begin) last = p.places[total - 1];  // (places are written up to `total`)
-      if (total > begin && last.start >= begin && last.count > kWindow) row = last;
+  if (threadIdx.x == 0) s_n = 0;
+  __syncthreads();
+  Place mine = {0, -1, 0, 0};
+  const long long begin = (((long long)blockIdx.x * kWaves + wave) * p.join_each + lane) * kWindow;
+  if (lane < p.join_each && begin < p.T) {
+    const int total = p.starts[p.N];
+    const int until = p.T - begin < kWindow ? (int)p.T : (int)begin + kWindow;
+    Place last = p.places[until - 1];
+    if (total < until && total > begin) last = p.places[total - 1];  // (places are written up to `total`)
+    if (total > begin && last.start >= begin && last.count > kWindow) mine = last;
+  }
+  const long long d0 = (long long)blockIdx.y * 64 * N, step = (long long)gridDim.y * 64 * N;
+  for (unsigned long long left = __ballot(mine.row >= 0); left != 0; left &= left - 1) {  // (uniform)
+    const int from = __builtin_ctzll(left);
+    const Place row = {0, (int)__builtin_amdgcn_readlane(mine.row, from), (int)__builtin_amdgcn_readlane(mine.start, from),
+                       (int)__builtin_amdgcn_readlane(mine.count, from)};
+    if (row.count > kFewJoins * kWindow) {
+      if (lane == 0) s_row[atomicAdd(&s_n, 1)] = row;
+    } else if (p.D >= N) {
+      join_row<true, ADD, float, B>(p, row.row, row.start, row.count, d0, step, lane);
+    } else {
+      join_row<false, ADD, float, B>(p, row.row, row.start, row.count, d0, step, lane);
     }
-    s_row[wave] = row;
   }
   __syncthreads();
-  for (int i = 0; i < kWaves; ++i) {
-    const int row = s_row[i].row;
-    if (row < 0) continue;  // (uniform)
-    const long long w = (long long)blockIdx.x * kWaves + i, last = ((long long)s_row[i].start + s_row[i].count - 1) / kWindow;
-    const bool inside = s_row[i].start != w * kWindow;  // (of its first window: then the second of the two partial rows)
-    B *to = reinterpret_cast<B *>(p.to) + (long long)row * p.to_stride;
-    for (long long d0 = (long long)blockIdx.y * 64 * N; d0 < p.D; d0 += (long long)gridDim.y * 64 * N) {
-      if (p.D >= N) join_columns<true, ADD>(p, s_sum, to, w, last, inside ? 1 : 0, d0);
-      else join_columns<false, ADD>(p, s_sum, to, w, last, inside ? 1 : 0, d0);
+  const int n = s_n;
+  for (int i = 0; i < n; ++i) {  // (uniform)
+    const Place row = s_row[i];
+    const long long first = row.start / kWindow, last = ((long long)row.start + row.count - 1) / kWindow;
+    const int slot = row.start != first * kWindow ? 1 : 0;  // (of its first window)
+    B *to = reinterpret_cast<B *>(p.to) + (long long)row.row * p.to_stride;
+    for (long long d = d0; d < p.D; d += step) {
+      if (p.D >= N) join_columns<true, ADD>(p, s_sum, to, first, last, slot, d);
+      else join_columns<false, ADD>(p, s_sum, to, first, last, slot, d);
     }
   }
 }
@@ -544,11 +559,14 @@ extern "C" int llc_embed_grad(const llc_embed_grad_args *a) {
       else embed_sum_kernel<decltype(from), B, false><<<sums, kBlock, 0, st>>>(p);
       e = hipGetLastError();
       if (e != hipSuccess || p.windows == 0 || p.arrived != nullptr) return e;
-      const long long groups = (p.windows + kJoinThreads / 64 - 1) / (kJoinThreads / 64);
-      const long long slabs = (a->D + 255) / 256, most = kMostBlocks / 4 / groups, join = slabs < most ? slabs : most;
-      const dim3 grid((unsigned)groups, (unsigned)(join < 1 ? 1 : join < 64 ? join : 64));
-      if (p.add != 0) embed_join_kernel<B, true><<<grid, kJoinThreads, 0, st>>>(p);
-      else embed_join_kernel<B, false><<<grid, kJoinThreads, 0, st>>>(p);
+      // (a workgroup a CU, where that leaves a wavefront 64 windows: more of them wait for each other)
+      const long long slabs = (a->D + 255) / 256, columns = slabs < 64 ? slabs : 64, waves = kJoinThreads / 64;
+      const long long each = (p.windows * columns + 256 * waves - 1) / (256 * waves);
+      EmbedParams q = p;
+      q.join_each = (int)(each < 64 ? each : 64);
+      const dim3 grid((unsigned)((p.windows + q.join_each * waves - 1) / (q.join_each * waves)), (unsigned)columns);
+      if (p.add != 0) embed_join_kernel<B, true><<<grid, kJoinThreads, 0, st>>>(q);
+      else embed_join_kernel<B, false><<<grid, kJoinThreads, 0, st>>>(q);
       return hipGetLastError();
     });
   });
