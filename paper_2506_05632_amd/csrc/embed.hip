@@ -14,7 +14,7 @@
 namespace llc {
 namespace {
 
-constexpr int kWindow = 32;       // sorted positions a wavefront adds up
+constexpr int kWindow = 32;       // sorted positions a wavefront adds up (16: 16 384 x 4096 sums and joins 41 + 7 us for 46 + 5; all by one token x 1537 52.6 for 44.1)
 constexpr int kAhead = 4;         // rows that are fetched together (8 take the registers of three wavefronts a SIMD: 65 536 tokens 402 us for 338)
 constexpr int kJoinThreads = 1024;
 constexpr int kFewJoins = 16;     // windows of a row that a wavefront joins by itself
@@ -443,9 +443,9 @@ int team_log_of(long long D, int from) {
 
 // Up to that many windows the last of a long row's wavefronts joins it, which spares a launch; that wavefront's sums follow each other, so the joins of
 // more windows are workgroups' of their own.  us a call, bf16 rows of 1537 into fp32, with the launch and without: 1001 tokens that hardly
-// repeat 13.0, 9.3; three in ten by one token 16.3, 15.4; all by one token 16.2, 18.4.  4096 tokens: 21.2, 17.6; 22.2, 25.7; 21.7, 44.5.
-// (A tree of such joins, without the other launch at all: 16 384 x 4096 bf16, a quarter by one token, 147 us for the sums, where sums and joins take 47 and 11: every
-// fence writes back what the L2 holds.)
+// repeat 14.3, 10.5; three in ten by one token 15.2, 15.5; all by one token 15.7, 19.2.  4096 tokens, when the launch took 5 us more: 21.2, 17.6; 22.2, 25.7; 21.7,
+// 44.5.  (A tree of such joins, without the other launch at all: 16 384 x 4096 bf16, a quarter by one token, 147 us for the sums, where sums and joins take 46 and
+// 5: every fence writes back what the L2 holds.)
 constexpr int kFewWindows = 32;
 
 struct GradLayout {
