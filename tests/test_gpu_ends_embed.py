@@ -225,6 +225,17 @@ def test_gradient_of_rows_that_many_tokens_name(T, types):
         assert torch.equal(grad, llc.llc_embed_grad(g, t, N, out_dtype=types[1])["grad"])
 
 
+@pytest.mark.parametrize("add", [False, True])
+@pytest.mark.parametrize("N,hot", [(60, 0.0), (150, 0.3), (4, 0.0), (900, 0.9)])
+def test_gradient_where_a_wavefront_joins_several_windows(N, hot, add):
+    T, D = 40000, 4099
+    g, t = _normal((T, D), BF16, N), _ids(T, N, N, hot)
+    before = _normal((N, D), F32, 5)
+    got = llc.llc_embed_grad(g, t, N, out=before.clone(), add=add)["grad"]
+    _check_grad(got, g, t, N, 1.0, before if add else None)
+    assert torch.equal(got, llc.llc_embed_grad(g, t, N, out=before.clone(), add=add)["grad"])
+
+
 def _grads(sizes, dtypes, scale=0.01):
     return [(scale * torch.randn(s, generator=_gen(11 + n), device=DEV)).to(dtypes[n % len(dtypes)]) for n, s in enumerate(sizes)]
 
