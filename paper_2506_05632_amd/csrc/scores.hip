@@ -103,6 +103,10 @@ __device__ __forceinline__ float max3(float a, float b, float c) {  // (NaN only
   return r;
 }
 
+__device__ __forceinline__ float largest3(float a, float b, float c) {  // NaN if one of them is, of either kind
+  return __builtin_elementwise_maximum(__builtin_elementwise_maximum(a, b), c);
+}
+
 // kPer entries of a lane: 16 bytes at a time, 64 lanes side by side, as they are and as floats.
 template <typename E> struct Tile {
   word4_any w[kPer / kWide<E>];
@@ -229,17 +233,19 @@ template <typename E> __device__ __forceinline__ void take_tile(Scan<E> &w, cons
   constexpr int N = kWide<E>;
   float v[kPer];
   unpack(tile, v);
-  float half[2];  // the largest of either half of the entries
+  // The largest of either half of the entries.  (A NaN has to show in it.  v_max3_f32 lets a number beside a quiet NaN through, and quiets a signalling one, which the next step
+  // then takes for less than any number, with all that it was compared to: a lane would miss its largest entry, and what is put into the list would not have been counted.)
+  float half[2];
   const auto largest = [&] {
 #pragma unroll
     for (int h = 0; h < 2; ++h) {
       const float *o = v + h * (kPer / 2);
-      half[h] = max3(max3(o[0], o[1], o[2]), max3(o[3], o[4], o[5]), max3(o[6], o[7], o[7]));
+      half[h] = largest3(largest3(o[0], o[1], o[2]), largest3(o[3], o[4], o[5]), largest3(o[6], o[7], o[7]));
     }
-    return max3(half[0], half[1], half[1]);
+    return largest3(half[0], half[1], half[1]);
   };
   float t = largest();
-  if (__ballot(!(t <= fminf(w.bound, w.m))) != 0) {  // (a NaN comes here too; where few entries are, the bound may be above them all)
+  if (__ballot(!(t <= fminf(w.bound, w.m))) != 0) {  // (a lane with a NaN comes here too; where few entries are, the bound may be above them all)
     if (__ballot(!(t < kInf)) != 0) {    // entries without mass
 #pragma unroll
       for (int i = 0; i < kPer; ++i) v[i] = with_mass(v[i]) ? v[i] : -kInf;
