@@ -97,11 +97,6 @@ __device__ __forceinline__ double wave_sum(double v) {  // the same in every lan
 __device__ __forceinline__ int lanes_below(u64 mask) {
   return __builtin_amdgcn_mbcnt_hi((uint32_t)(mask >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)mask, 0));
 }
-__device__ __forceinline__ float max3(float a, float b, float c) {  // (NaN only if all are, or where one is a signalling one)
-  float r;
-  asm("v_max3_f32 %0, %1, %2, %3" : "=v"(r) : "v"(a), "v"(b), "v"(c));
-  return r;
-}
 
 __device__ __forceinline__ float largest3(float a, float b, float c) {  // NaN if one of them is, of either kind
   return __builtin_elementwise_maximum(__builtin_elementwise_maximum(a, b), c);
@@ -733,11 +728,11 @@ __device__ __forceinline__ Weights weights_of(const ScoreParams &p, long long r,
 
 // From a tile's entries to their gradients, tokens apart.
 __device__ __forceinline__ void entry_gradients(const Weights &w, float (&v)[kPer]) {
-  float t = max3(v[0], v[1], v[2]);
+  float t = largest3(v[0], v[1], v[2]);
 #pragma unroll
-  for (int i = 3; i + 1 < kPer; i += 2) t = max3(t, v[i], v[i + 1]);
-  t = max3(t, v[kPer - 1], v[kPer - 1]);
-  if (__ballot(!(t <= w.top)) != 0) {  // NaN, +inf (and in a row without mass anything)
+  for (int i = 3; i + 1 < kPer; i += 2) t = largest3(t, v[i], v[i + 1]);
+  t = largest3(t, v[kPer - 1], v[kPer - 1]);
+  if (__ballot(!(t <= w.top)) != 0) {  // a NaN among them, +inf (and in a row without mass anything)
 #pragma unroll
     for (int i = 0; i < kPer; ++i) v[i] = with_mass(v[i]) ? v[i] : -kInf;
   }

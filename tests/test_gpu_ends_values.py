@@ -56,3 +56,64 @@ def test_scores_beside_signalling_NaNs(V, dtype):
     for M in (1, 20, 128):
         for chunks in (0, 1, 3):
             ref.check_scores(llc.llc_token_logprobs(x, t, M, temp=0.8, want_lse=True, v_chunks=chunks), x, t, M, 0.8)
+
+
+def _check_grad(x, t, a, b, temp, out, rows):
+    """`rows` of a gradient, and of the scores beside it."""
+    part = lambda v: None if v is None else v[rows]  # noqa: E731
+    want, tol = ref.gradient(x[rows], t[rows], a[rows], part(b), temp)
+    far = np.abs(out["grad"][rows].detach().cpu().double().numpy() - want) - tol
+    assert far.max() <= 0, (far.max(), np.unravel_index(far.argmax(), far.shape))
+    if "logp" in out:
+        ref.check_scores({k: v[rows] for k, v in out.items()}, x[rows], t[rows], 0, temp)
+
+
+def _gradients(x, t, a, b, temp, rows):
+    """Every way to the gradient: in one pass (or over split rows), over rows split in three, in place, from given sums."""
+    for chunks in (0, 3):
+        _check_grad(x, t, a, b, temp, llc.llc_token_logprobs_grad(x, t, a, grad_entropy=b, temp=temp, v_chunks=chunks), rows)
+    again = x.clone()
+    _check_grad(x, t, a, b, temp, llc.llc_token_logprobs_grad(again, t, a, grad_entropy=b, temp=temp, out={"grad": again}), rows)
+    s = llc.llc_token_logprobs(x, t, 0, temp=temp, want_lse=True)
+    _check_grad(x, t, a, b, temp, llc.llc_token_logprobs_grad(x, t, a, grad_entropy=b, temp=temp, lse=s["lse"], entropy=s["entropy"]), rows)
+
+
+# the mean's weights: few enough that one multiply-add an entry forms the gradient; with them the entropy's; weights too large for that
+WEIGHTS = {"mean": (1.0, 0.0), "entropy": (1.0, 0.3), "large": (100.0, 0.0), "large, entropy": (100.0, 30.0)}
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("R,V", [(20, 61), (20, 1030), (20, 9001), (20, 40003), (90, 70001)])
+@pytest.mark.parametrize("weights", WEIGHTS)
+def test_gradient_where_a_NaN_lies_among_numbers(R, V, dtype, weights):
+    x = _rows(R, V, dtype, V)
+    t = torch.randint(0, V, (R, 3), generator=_gen(V), device=DEV).to(torch.int32)
+    for r in range(R):
+        x[r, (41 * r) % V] = float("nan")
+        if r % 2 == 0:
+            x[r, V - 1] = float("nan")
+    t[:, 0] = (torch.arange(R, device=DEV) * 41) % V  # (a token without mass)
+    x[3, ::7] = float("nan")
+    x[4, ::2] = -float("inf")
+    x[5, 1::2] = float("inf")
+    size, bonus = WEIGHTS[weights]
+    a = size * torch.rand(R, 3, generator=_gen(1), device=DEV) / R
+    b = torch.full((R,), bonus / R, device=DEV) if bonus else None
+    _gradients(x, t, a, b, 1.0, slice(0, 20))
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("V", [61, 1030, 9001, 40003, 70001])
+@pytest.mark.parametrize("weights", WEIGHTS)
+def test_gradient_beside_signalling_NaNs(V, dtype, weights):
+    x = _with_signalling(V, dtype)
+    if V > 65536:
+        x = torch.cat([x] * 5)  # (so many that a row is a workgroup's)
+    R = x.shape[0]
+    t = torch.randint(0, V, (R, 5), generator=_gen(V), device=DEV).to(torch.int32)
+    t[:, 0] = (torch.arange(R, device=DEV) % 20 * 37) % (V - 2) + 1
+    t[:, 1] = t[:, 0] - 1
+    size, bonus = WEIGHTS[weights]
+    a = size * torch.rand(R, 5, generator=_gen(1), device=DEV) / R
+    b = torch.full((R,), bonus / R, device=DEV) if bonus else None
+    _gradients(x, t, a, b, 0.8, slice(0, 20))
