@@ -178,16 +178,19 @@ template <typename E> __device__ __forceinline__ void drop_others(Tile<E> &t, ui
 }
 
 // Exponents are x c less a reference that follows from the largest entry m: m c as fp32 has it.  One multiply-add forms them, exact but for its one rounding, and
-// what the reference's own rounding shifts all of them by is put right at the end.  Where m c leaves fp32 they are (x - m) c.
-__device__ __forceinline__ bool has_reference(float m, float c) { return fabsf(m) * c < 0x1p100f; }
+// what the reference's own rounding shifts all of them by is put right at the end.  That shift has to stay small beside the range of 2^y: it is 2^-3 at most
+// below 2^22, where the reference stops (from 2^31 on it may be 128).  Beyond, exponents are (x - m) c.
+__device__ __forceinline__ bool has_reference(float m, float c) { return fabsf(m) * c < 0x1p22f; }
 __device__ __forceinline__ float reference_of(float m, float c) {
 #pragma clang fp contract(off)  // (it is rounded wherever it is used)
   return m * c;
 }
 // From exponents relative to what belongs to `from` to those relative to what belongs to the larger `to`.
 __device__ __forceinline__ float shift_between(float from, float to, float c) {
-  const bool both = has_reference(from, c) && has_reference(to, c);
-  return fmaxf(both ? reference_of(from, c) - reference_of(to, c) : (from - to) * c, -200.0f);  // (from -inf: -200, or NaN, which is nothing to max)
+  const bool at_from = has_reference(from, c), at_to = has_reference(to, c);
+  const float by = at_from ? at_to ? reference_of(from, c) - reference_of(to, c) : -fmaf(to, c, -reference_of(from, c))
+                           : at_to ? fmaf(from, c, -reference_of(to, c)) : (from - to) * c;
+  return fmaxf(by, -200.0f);  // (from -inf: -200, or NaN, which is nothing to max)
 }
 
 // A wavefront's sums and candidates.

@@ -117,3 +117,50 @@ def test_gradient_beside_signalling_NaNs(V, dtype, weights):
     a = size * torch.rand(R, 5, generator=_gen(1), device=DEV) / R
     b = torch.full((R,), bonus / R, device=DEV) if bonus else None
     _gradients(x, t, a, b, 0.8, slice(0, 20))
+
+
+MASKS = [1e9, -1e9, -3e9, 1e10, -1e10, -3e10, 1e20, -1e20, 1e30, -1e30]
+
+
+def _large(V, dtype, temp):
+    """Rows that begin with, or are, large finite values, and rows around the size where they stop to be told by fp32 products."""
+    x = _rows(3 * len(MASKS) + 8, V, dtype, V)
+    noise = _rows(8, V, F32, V + 1)
+    for i, mask in enumerate(MASKS):
+        x[3 * i, : V - V // 3] = mask          # a block before the others
+        x[3 * i + 1] = mask                    # nothing else: uniform
+        x[3 * i + 2] = mask * (1.0 + 1e-3 * noise[0].abs()).to(dtype)
+    edge = 2.0 ** 22 * temp / 1.4426950408889634
+    steps = torch.linspace(-40, 40, V, device=DEV)
+    for i, row in enumerate((edge + steps, edge - steps, -edge + steps, -edge - steps, edge / 2 + noise[1], -edge / 2 + noise[2], 4 * edge + noise[3], noise[4] * edge)):
+        x[3 * len(MASKS) + i] = row.to(dtype)
+    return x
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("V", [300, 9001, 70001])
+@pytest.mark.parametrize("temp", [0.7, 1.0, 2.0])
+def test_scores_of_large_finite_values(temp, V, dtype):
+    x = _large(V, dtype, temp)
+    R = x.shape[0]
+    t = torch.randint(0, V, (R, 4), generator=_gen(V), device=DEV).to(torch.int32)
+    t[:, 0], t[:, 1] = 0, V - 1
+    for chunks in (0, 1, 5):
+        ref.check_scores(llc.llc_token_logprobs(x, t, 10, temp=temp, want_lse=True, v_chunks=chunks), x, t, 10, temp)
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("V", [300, 9001, 40003, 70001])
+@pytest.mark.parametrize("temp,weights", [(0.7, "mean"), (1.0, "entropy"), (1.0, "large"), (2.0, "large, entropy")])
+def test_gradient_of_large_finite_values(temp, weights, V, dtype):
+    x = _large(V, dtype, temp)
+    rows = slice(0, x.shape[0])
+    if V > 65536:
+        x = torch.cat([x] * 3)
+    R = x.shape[0]
+    t = torch.randint(0, V, (R, 4), generator=_gen(V), device=DEV).to(torch.int32)
+    t[:, 0], t[:, 1] = 0, V - 1
+    size, bonus = WEIGHTS[weights]
+    a = size * torch.rand(R, 4, generator=_gen(1), device=DEV) / R
+    b = torch.full((R,), bonus / R, device=DEV) if bonus else None
+    _gradients(x, t, a, b, temp, rows)
