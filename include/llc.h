@@ -389,7 +389,7 @@ typedef struct llc_lml_args {
  * (-inf without mass); it / temp plus the second would lose the second where a row's values are large.  top_ids / top_logp[r,m] = the M entries with
  * the largest x, larger first, equal ones by index, and their ln p; -1 and -inf where fewer entries
  * have mass.  These are lists as llc_couple_topm takes them (kind LLC_LOGW).
- * Sums are taken in fp32 within a thread and joined in fp64. */
+ * Sums are taken in fp32 over 16 entries of a thread and in fp64 beyond, whatever the length. */
 #define LLC_TOP_MAX 128
 typedef struct llc_token_logprobs_args {
   int64_t R, V, G, M;       /* R >= 0, V in 1..2^31 - 5, G in 0..65535, M in 0..LLC_TOP_MAX */

@@ -2,7 +2,7 @@
 //
 // Forward.  With a reference m, c = log2(e) / T and d_i = (x_i - m) c, a row needs S = sum 2^d_i and D = sum d_i 2^d_i: ln p_t = (x_t - m) / T - ln S
 // and the entropy is ln S - ln 2 D / S.  One pass over the row forms both: a wavefront keeps its largest entry so far as its m, every lane its shares
-// of S and D in fp32, scaled over when m grows (which happens a dozen times a row); lanes, wavefronts and chunks are joined in fp64.
+// of S and D, 16 entries in fp32 and those sums in fp64, scaled over when m grows (which happens a dozen times a row); lanes, wavefronts and chunks are joined in fp64.
 // The same pass finds the top alternatives.  An entry is a candidate if it is above a bound that M entries of the row are known to reach: every
 // wavefront says a value that its share of the M reach, at first among its lanes' first entries (each lane's largest of 16), later among the
 // candidates in its list, and the smallest said is the bound.  A row of 128 256 leaves a few hundred candidates for fifty, and a tile of 16 entries a lane that has
@@ -196,7 +196,7 @@ __device__ __forceinline__ float shift_between(float from, float to, float c) {
 // A wavefront's sums and candidates.
 template <typename E> struct Scan {
   float m = -kInf;      // largest entry so far
-  float s = 0.0f, d = 0.0f;
+  double s = 0.0, d = 0.0;  // (a tile's 16 entries are added up in fp32, tiles in fp64: a running fp32 sum of equal terms is off by 4e-6 after 4096 of them, 6e-5 after 16 384)
   float bound = -kInf;  // candidates are above it
   int count = 0;        // of the list
 };
@@ -302,11 +302,11 @@ template <typename E> __device__ __forceinline__ void take_tile(Scan<E> &w, cons
       }
     }
   }
-  float s[2] = {w.s, 0.0f}, sd[2] = {w.d, 0.0f};  // (two sums of either kind, so that one's additions do not wait for each other)
+  float s[2], sd[2];  // (two sums of either kind, so that one's additions do not wait for each other)
   const auto add = [&](int i, float d) {
     const float e = __builtin_amdgcn_exp2f(d);  // (no mass: 2^-200 is 0)
-    s[i & 1] += e;
-    sd[i & 1] = fmaf(e, d, sd[i & 1]);
+    s[i & 1] = i < 2 ? e : s[i & 1] + e;
+    sd[i & 1] = i < 2 ? e * d : fmaf(e, d, sd[i & 1]);
   };
   if (has_reference(w.m, c)) {  // (not where nothing has had mass yet)
     const float reference = reference_of(w.m, c);
@@ -316,8 +316,8 @@ template <typename E> __device__ __forceinline__ void take_tile(Scan<E> &w, cons
 #pragma unroll
     for (int i = 0; i < kPer; ++i) add(i, fmaxf((v[i] - w.m) * c, -200.0f));
   }
-  w.s = s[0] + s[1];
-  w.d = sd[0] + sd[1];
+  w.s += (double)(s[0] + s[1]);
+  w.d += (double)(sd[0] + sd[1]);
 }
 
 // A number that n of the lanes' K ordered values each reach, and little below the n-th largest of them (its upper 16 bits); 0 if there are fewer than n.
@@ -600,7 +600,7 @@ template <typename E, int WAVES, bool TINY = false> __global__ void __launch_bou
   }
   if (p.M > 0 && w.count > kSelected / WAVES) look();  // (else what all have is soon ranked)
   // the wavefronts' sums
-  const double ws = wave_sum((double)w.s), wd = wave_sum((double)w.d);
+  const double ws = wave_sum(w.s), wd = wave_sum(w.d);
   if (lane == 0) { s_s[wave] = ws; s_d[wave] = wd; s_m[wave] = w.m; s_count[wave] = w.count; }
   __syncthreads();
   const int mine = lane < WAVES ? lane : 0;
@@ -863,7 +863,7 @@ template <typename E, int WAVES> struct RowWork {
   // From the wavefronts' sums to the scores and what the gradient needs.
   __device__ __forceinline__ Weights join(const ScoreParams &p, long long r, const Scan<E> &w, int token, E token_raw, double share) {
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    double s = wave_sum((double)w.s), d = wave_sum((double)w.d);
+    double s = wave_sum(w.s), d = wave_sum(w.d);
     float token_x = token >= 0 && token < p.V ? widen(token_raw) : -kInf;
     asm volatile("" : "+v"(token_x));  // (here: not while other wavefronts already write)
     if (lane == 0) { s_s[wave] = s; s_d[wave] = d; s_m[wave] = w.m; }

@@ -164,3 +164,21 @@ def test_gradient_of_large_finite_values(temp, weights, V, dtype):
     a = size * torch.rand(R, 4, generator=_gen(1), device=DEV) / R
     b = torch.full((R,), bonus / R, device=DEV) if bonus else None
     _gradients(x, t, a, b, temp, rows)
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("R,V,chunks", [(600, 128256, 0), (90, 152064, 0), (1, 1 << 20, 1), (1, 1 << 22, 1), (2, (1 << 25) + 77, 1)])
+def test_sums_of_long_rows_of_equal_entries(R, V, chunks, dtype):
+    # equal terms round alike in all lanes, so that what running sums lose does not average out; the value is no power of two
+    x = torch.full((R, V), -1.3, device=DEV).to(dtype)
+    x[:, 5] = 0.25
+    t = torch.zeros(R, 2, dtype=torch.int32, device=DEV)
+    t[:, 1] = 5
+    out = llc.llc_token_logprobs(x, t, 0, want_lse=True, v_chunks=chunks)
+    ref.check_scores({k: v[:1] for k, v in out.items()}, x[:1], t[:1], 0, 1.0)
+    for v in out.values():
+        assert torch.equal(v, v[:1].expand_as(v))
+    if chunks == 0:  # (the gradient's pass over rows that stay on the chip)
+        a = torch.full((R, 2), 0.1, device=DEV)
+        out = llc.llc_token_logprobs_grad(x, t, a)
+        ref.check_scores({k: out[k][:1] for k in ("logp", "entropy")}, x[:1], t[:1], 0, 1.0)
