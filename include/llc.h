@@ -494,8 +494,8 @@ typedef struct llc_embed_grad_args {
 
 /* Arguments of llc_clip_grad_norm: norm = sqrt of the sum of squares over all n tensors (fp64 throughout,
  * so that squares neither overflow nor vanish; rounded once), and out_j = grad_j * min(1, max_norm / norm),
- * the factor in fp32, each product rounded once.  A norm that is not finite leaves the gradients as they are (the caller sees
- * it in `norm`).  The arrays grads, numel, dtype and out are HOST arrays, read before the call returns;
+ * the factor in fp32, each product rounded once.  A norm that is not finite in fp32 leaves the gradients as they are (the caller
+ * sees it in `norm`).  The arrays grads, numel, dtype and out are HOST arrays, read before the call returns;
  * their pointers are device pointers to contiguous tensors.  out == NULL: in place.  max_norm may be +inf: the
  * norm alone (out, if given, gets copies).  Tensors must not overlap each other unless out_j is grad_j. */
 typedef struct llc_clip_grad_norm_args {

@@ -98,8 +98,8 @@ __device__ __forceinline__ double sum_of_partials(const double *partials, int n,
   for (int i = from; i < n; i += step) s += partials[i];
   return s;
 }
-__device__ __forceinline__ float factor_of(double norm, float max_norm) {
-  return norm > (double)max_norm && norm < __builtin_huge_val() ? (float)((double)max_norm / norm) : 1.0f;
+__device__ __forceinline__ float factor_of(double norm, float max_norm) {  // (the norm as the caller sees it says whether it is finite)
+  return norm > (double)max_norm && (float)norm < __builtin_huge_valf() ? (float)((double)max_norm / norm) : 1.0f;
 }
 
 // Many partial sums are joined once.
