@@ -897,7 +897,7 @@ def llc_token_logprobs_grad(logits: torch.Tensor, tokens: Optional[torch.Tensor]
     a = TokenLogprobsGradArgs()
     a.R, a.V, a.G = R, V, G
     a.dtype, a.kind = _TYPES[logits.dtype], _KINDS[kind]
-    a.x, a.stride_r, a.temp = logits.data_ptr(), logits.stride(0), temp
+    a.x, a.stride_r, a.temp = logits.data_ptr(), _row_stride(logits), temp
     if tokens is not None:
         a.tokens, a.tok_stride_r = tokens.data_ptr(), tokens.stride(0)
         a.grad_logp, a.grad_logp_stride_r = grad_logp.data_ptr(), grad_logp.stride(0)

@@ -182,3 +182,17 @@ def test_sums_of_long_rows_of_equal_entries(R, V, chunks, dtype):
         a = torch.full((R, 2), 0.1, device=DEV)
         out = llc.llc_token_logprobs_grad(x, t, a)
         ref.check_scores({k: out[k][:1] for k in ("logp", "entropy")}, x[:1], t[:1], 0, 1.0)
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+def test_gradient_in_place_of_a_single_row_of_any_stride(dtype):
+    # the stride of one row says nothing: the transpose of a column has (1, 1)
+    V = 5003
+    x = _rows(V, 1, dtype, 1).t()
+    t, a = torch.tensor([[7, V - 1]], dtype=torch.int32, device=DEV), torch.tensor([[0.5, -0.2]], device=DEV)
+    want = llc.llc_token_logprobs_grad(x.clone(), t, a)["grad"]
+    for temp_x in (x.clone().t().contiguous().t(), torch.cat([x, x])[:1]):
+        lse = llc.llc_token_logprobs(temp_x, t, 0, want_lse=True)["lse"]
+        other = temp_x.t().clone().t()
+        assert torch.equal(llc.llc_token_logprobs_grad(temp_x, t, a, out={"grad": temp_x})["grad"], want)
+        assert llc.llc_token_logprobs_grad(other, t, a, lse=lse, out={"grad": other})["grad"].shape == (1, V)
