@@ -659,8 +659,8 @@ template <typename E> __global__ void __launch_bounds__(kBlock) score_join_kerne
 
 // ---- the gradient
 // With y_i = (x_i - top) c - log2(e) rest, so that p_i = 2^y_i, an entry's gradient is 2^y (a + b y) and at a token's place its weight / T more.  The
-// rounding of log2(e) rest to fp32 goes into a and b.  The hardware's 2^y is 0 below 2^-126, so it is taken 2^kLift too large: weights may be large too.
-constexpr float kLift = 24.0f;
+// rounding of log2(e) rest to fp32 goes into a and b.  The hardware's 2^y is 0 below 2^-126, so what multiplies it is brought near 1: 2^y is taken as much larger as a and b are made
+// smaller.
 struct Weights {
   float top, shift, c, a, b, inv_t;
   float line;  // -(top c + shift)
@@ -715,16 +715,19 @@ __device__ __forceinline__ Weights weights_of(const ScoreParams &p, long long r,
     a -= (double)p.b[r] * entropy * inv_t;
   }
   // One multiply-add an entry, x c + line, serves unless top c is so large that fp32 keeps too little of it, and what 2^y loses below 2^-126 counts only with large weights.
-  const bool plain = fabs(at_top) < 65536.0 && fabs(a) + 128.0 * fabs(b) < 1.0;
+  const double size = fabs(a) + 128.0 * fabs(b);
+  const bool plain = fabs(at_top) < 65536.0 && size < 1.0;
+  const int lift = size < 1.0 ? 0 : min(__builtin_amdgcn_frexp_exp(size), 127);
   w.top = (float)top;
   w.line = (float)-(at_top + shift);
-  w.shift = (float)(shift - (double)kLift);
+  w.shift = (float)(shift - (double)lift);
   // y as it is formed is above the true one by `over`
-  const double over = plain ? at_top + shift + (double)w.line : shift - (double)kLift - (double)w.shift;
+  const double over = plain ? at_top + shift + (double)w.line : shift - (double)lift - (double)w.shift;
   const double off = 1.0 - over * kLn2 * (1.0 - 0.5 * over * kLn2);  // 2^-over: it is 2^-8 at most
-  a -= b * (plain ? over : over + (double)kLift);
-  w.a = (float)(a * off);
-  w.b = (float)(b * off);
+  const double scale = ldexp(off, -lift);
+  a -= b * (over + (double)lift);
+  w.a = (float)(a * scale);
+  w.b = (float)(b * scale);
   w.form = !plain ? 2 : p.b != nullptr ? 1 : 0;
   return uniform(w);
 }
@@ -752,7 +755,7 @@ __device__ __forceinline__ void entry_gradients(const Weights &w, float (&v)[kPe
 #pragma unroll
     for (int i = 0; i < kPer; ++i) {
       const float y = fmaxf(fmaf(v[i] - w.top, w.c, -w.shift), -200.0f);
-      v[i] = __builtin_amdgcn_exp2f(y) * fmaf(y, w.b, w.a) * 0x1p-24f;
+      v[i] = __builtin_amdgcn_exp2f(y) * fmaf(y, w.b, w.a);
     }
   }
 }

@@ -196,3 +196,19 @@ def test_gradient_in_place_of_a_single_row_of_any_stride(dtype):
         other = temp_x.t().clone().t()
         assert torch.equal(llc.llc_token_logprobs_grad(temp_x, t, a, out={"grad": temp_x})["grad"], want)
         assert llc.llc_token_logprobs_grad(other, t, a, lse=lse, out={"grad": other})["grad"].shape == (1, V)
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("V", [300, 9001, 40003])
+@pytest.mark.parametrize("size,temp", [(1e30, 1.0), (1e33, 1.0), (1e36, 1.0), (0.1, 1e-33), (1e-3, 2.0 ** -126), (1e-32, 1.0), (1e-32, 1e-3)])
+def test_gradient_with_weights_of_all_sizes(size, temp, V, dtype):
+    x = _rows(6, V, dtype, V) * temp
+    x[1] = 1.5                                      # uniform
+    x[2, 3:] = -float("inf")
+    x[3, V // 2] = 60.0 * temp                      # p of the others down to 2^-90
+    x[4, V // 2] = 110.0 * temp                     # and below 2^-126
+    t = torch.randint(0, V, (6, 4), generator=_gen(V), device=DEV).to(torch.int32)
+    t[:, 0] = V // 2
+    a = size * torch.rand(6, 4, generator=_gen(1), device=DEV)
+    for b in (None, size * torch.rand(6, generator=_gen(2), device=DEV)):
+        _gradients(x, t, a, b, temp, slice(0, 6))
