@@ -397,7 +397,7 @@ typedef struct llc_token_logprobs_args {
   int32_t kind;             /* LLC_LOGITS | LLC_LOGW                                     */
   const void *x;            /* device [R,V] */
   int64_t stride_r;         /* elements */
-  float temp;               /* > 0; LLC_LOGITS only                                      */
+  float temp;               /* 2^-126 or more, finite; LLC_LOGITS only                   */
   const int32_t *tokens;    /* device [R,G]; may be NULL when G == 0                     */
   int64_t tok_stride_r;
   float *logp;              /* [R,G] required unless G == 0                              */
@@ -429,7 +429,7 @@ typedef struct llc_token_logprobs_grad_args {
   int32_t dtype, kind;      /* as above                                                  */
   const void *x;            /* device [R,V] */
   int64_t stride_r;
-  float temp;
+  float temp;               /* as above */
   const int32_t *tokens;    /* device [R,G]; may be NULL when G == 0                     */
   int64_t tok_stride_r;
   const float *grad_logp;   /* device [R,G]; may be NULL when G == 0                     */

@@ -491,7 +491,7 @@ const char *llc_status_string(int code) {
     case LLC_OK: return "ok";
     case LLC_E_NULL: return "a required pointer is NULL";
     case LLC_E_SHAPE: return "bad shape or strides";
-    case LLC_E_TEMP: return "temperature must be finite and > 0";
+    case LLC_E_TEMP: return "temperature must be finite and > 0 (of scores and their gradient: 2^-126 at least)";
     case LLC_E_DTYPE: return "unsupported dtype or kind";
     case LLC_E_ALIGN: return "input pointer not aligned to its element size";
     case LLC_E_WORKSPACE: return "workspace missing, misaligned or too small";

@@ -1036,6 +1036,9 @@ int auto_split(long long R, long long V) {
   return (int)(split < 3 ? 1 : split < kMostSplit ? split : kMostSplit);
 }
 
+// (Below 2^-126 log2(e) / temp and 1 / temp leave fp32.)
+bool good_temp(float t) { return std::isfinite(t) && t >= 0x1p-126f; }
+
 // Cuts a row into `want` chunks of whole 16-byte loads.
 void split_rows(ScoreParams &p, long long want) {
   const long long each = ((p.V + want - 1) / want + 15) & ~15LL;
@@ -1104,7 +1107,7 @@ extern "C" int llc_token_logprobs(const llc_token_logprobs_args *a) {
   if (a->stride_r < 0 || a->tok_stride_r < 0) return LLC_E_SHAPE;
   if (!known_type(a->dtype) || (a->kind != LLC_LOGITS && a->kind != LLC_LOGW)) return LLC_E_DTYPE;
   const bool logits = a->kind == LLC_LOGITS;
-  if (logits && !(std::isfinite(a->temp) && a->temp > 0.0f)) return LLC_E_TEMP;
+  if (logits && !good_temp(a->temp)) return LLC_E_TEMP;
   if (!fits(a->x, type_size(a->dtype)) || !fits(a->tokens, 4)) return LLC_E_ALIGN;
   const long long split = a->v_chunks > 0 ? a->v_chunks : auto_split(a->R, a->V);
   if (a->workspace == nullptr || !fits(a->workspace, 256) || a->workspace_bytes < rows_workspace(a->R, a->M, split)) return LLC_E_WORKSPACE;
@@ -1134,7 +1137,7 @@ extern "C" int llc_token_logprobs_grad(const llc_token_logprobs_grad_args *a) {
   if (a->x == a->grad && a->stride_r != a->grad_stride_r) return LLC_E_SHAPE;
   if (!known_type(a->dtype) || (a->kind != LLC_LOGITS && a->kind != LLC_LOGW)) return LLC_E_DTYPE;
   const bool logits = a->kind == LLC_LOGITS;
-  if (logits && !(std::isfinite(a->temp) && a->temp > 0.0f)) return LLC_E_TEMP;
+  if (logits && !good_temp(a->temp)) return LLC_E_TEMP;
   if (!fits(a->x, type_size(a->dtype)) || !fits(a->grad, type_size(a->dtype)) || !fits(a->tokens, 4) || !fits(a->grad_logp, 4))
     return LLC_E_ALIGN;
   const long long split = a->v_chunks > 0 ? a->v_chunks : auto_split(a->R, a->V);

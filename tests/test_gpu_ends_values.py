@@ -212,3 +212,19 @@ def test_gradient_with_weights_of_all_sizes(size, temp, V, dtype):
     a = size * torch.rand(6, 4, generator=_gen(1), device=DEV)
     for b in (None, size * torch.rand(6, generator=_gen(2), device=DEV)):
         _gradients(x, t, a, b, temp, slice(0, 6))
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("temp", [2.0 ** -126, 1e-30, 1e-10, 3e38])
+@pytest.mark.parametrize("V", [300, 40003, 70001])
+def test_scores_at_extreme_temperatures(V, temp, dtype):
+    x = _rows(4, V, dtype, V)
+    x[1, ::2] = 7.0
+    x[2] = -1.25
+    x[3, 5:] = -float("inf")
+    t = torch.randint(0, V, (4, 4), generator=_gen(V), device=DEV).to(torch.int32)
+    t[:, 0], t[:, 1] = 0, V - 1
+    for chunks in (0, 1, 5):
+        ref.check_scores(llc.llc_token_logprobs(x, t, 10, temp=temp, want_lse=True, v_chunks=chunks), x, t, 10, temp)
+    a = torch.full((4, 4), temp if temp < 1 else 0.1, device=DEV)
+    _gradients(x, t, a, None, temp, slice(0, 4))
