@@ -971,7 +971,7 @@ def llc_embed_grad(g: torch.Tensor, tokens: torch.Tensor, N: int, *, scale: floa
     lib = load()
     if not (g.is_cuda and tokens.device == g.device):
         raise ValueError("llc_embed_grad needs device tensors of one device (there is no CPU path)")
-    if g.dtype not in _TYPES or g.shape[:-1] != tokens.shape or tokens.dtype != torch.int32 or g.dim() < 2:
+    if g.dtype not in _TYPES or g.dim() < 1 or g.shape[:-1] != tokens.shape or tokens.dtype != torch.int32:
         raise ValueError("g must have the tokens' shape and D, float32 or bfloat16; tokens int32")
     D = g.shape[-1]
     tokens = _flat(tokens)
