@@ -1025,15 +1025,17 @@ size_t rows_workspace(long long R, long long M, long long chunks) {  // shares a
   return (size_t)chunks * (size_t)R * (sizeof(Share) + 8 * (size_t)M) + 32 * (size_t)R + 512;
 }
 
-// Workgroups that a row is split over: as many as leave each 16 000 entries, as far as there are CUs for them, if that is three or more and the row has 64 000: the
-// second launch takes some 3 us.  us a call with 50 alternatives, whole and split: 1 x 128 256 fp32 27.4, 19.3 (8); 64 x 128 256 30.2, 24.9 (4); 85 x 128 256 bf16
-// 30.2, 24.9 (3); 1 x 4 194 304 fp32 321, 42 (64); 64 x 64 000 22.8, 21.3 (4); not taken: 1 x 50 257 17.2, 18.6 (3); 85 x 50 257 19.5, 21.6 (3); 128 x 152 064
-// bf16 31.8, 28.3 (2), 4 x 32 000 bf16 15.2, 17.2 (2).
+// Workgroups that a row is split over: as many as leave each 16 000 entries, as far as there are CUs for them, if that is three or more and the row has 64 000 (the
+// second launch takes some 3 us), or two and the row has 128 000.  us a call with 50 alternatives, whole and split: 1 x 128 256 fp32 27.4, 19.3 (8); 64 x 128 256
+// 30.2, 24.9 (4); 85 x 128 256 bf16 30.2, 24.9 (3); 1 x 4 194 304 fp32 321, 42 (64); 64 x 64 000 22.8, 21.3 (4); in two: 107 x 128 256 bf16 30.5, 28.9, fp32 30.6,
+// 29.0; 128 x 152 064 bf16 32.5, 29.6 (without alternatives 16.6, 14.1), fp32 32.4, 30.3 (18.2, 18.2); 128 x 400 000 bf16 57.7, 45.5.  Not taken: 1 x 50 257 17.2,
+// 18.6 (3); 85 x 50 257 19.5, 21.6 (3); 107 x 100 000 bf16 26.4, 26.2 (2; 128 alternatives 32.4, 33.2); 128 x 64 000 22.9, 23.7 (2); 4 x 32 000 bf16 15.2, 17.2 (2).
 int auto_split(long long R, long long V) {
   if (V < 64000) return 1;
   long long split = V / 16000;
   if (split > 256 / (R > 0 ? R : 1)) split = 256 / (R > 0 ? R : 1);
-  return (int)(split < 3 ? 1 : split < kMostSplit ? split : kMostSplit);
+  if (split < 3) return split == 2 && V >= 128000 ? 2 : 1;
+  return (int)(split < kMostSplit ? split : kMostSplit);
 }
 
 // (Below 2^-126 log2(e) / temp and 1 / temp leave fp32.)
@@ -1052,10 +1054,11 @@ template <typename E> hipError_t launch_gradient(ScoreParams p, hipStream_t st) 
   return hipGetLastError();
 }
 
-// Scores and gradient in one launch: as many wavefronts as keep the row in registers.  Rows too long for that are a workgroup's too where the scores would
-// not be split (many rows: a CU has one at least), else scores and gradient are two launches over all CUs.  us a call, one launch and two (three where
-// split): 70 001 fp32 of 64 rows 18.1, 18.4, of 96 18.5, 22.5, of 256 30.2, 40.9; 128 256 fp32 26.9, 23.8; 27.3, 33.4; 45.9, 66.1; 152 064
-// bf16 29.4, 19.3; 29.8, 28.9; 34.8, 45.3; 300 000 bf16 53.0, 29.1; 53.6, 48.0; 66.6, 80.5.  False: nothing was launched.
+// Scores and gradient in one launch: as many wavefronts as keep the row in registers.  Rows too long for that are a workgroup's too where there are 86 or more: a
+// CU in three has one at least.  With fewer, or up to 128 rows so long that reading them twice costs a workgroup more than splitting them in two, scores and gradient are two or
+// three launches over all CUs.  us a call, one launch and several: 70 001 fp32 of 64 rows 18.1, 18.4, of 96 18.5, 22.5, of 256 30.2, 40.9; 128 256 fp32 of 64
+// rows 26.9, 23.8, of 107 27.9, 35.3, of 256 45.9, 66.1; 152 064 bf16 of 64 29.4, 19.3, of 107 26.8, 28.7, of 256 34.8, 45.3; 107 rows of 200 000 bf16 32.3,
+// 34.3, of 262 144 41.2, 41.0 (with entropies 46.0, 40.9), of 400 000 60.6, 55.0; of 400 000 fp32 82.3, 86.8, of 600 000 137, 127.  False: nothing was launched.
 template <typename E> bool launch_rows(const ScoreParams &p, hipStream_t st) {
   const long long tiles = ((long long)p.V + 64 * kPer - 1) / (64 * kPer);
   constexpr bool kHalf = sizeof(E) == 2;
@@ -1067,7 +1070,7 @@ template <typename E> bool launch_rows(const ScoreParams &p, hipStream_t st) {
   else if (tiles <= 16) score_row_kernel<E, 4, 4><<<rows, 256, 0, st>>>(p, (int)tiles);
   else if (tiles <= 32) score_row_kernel<E, kHalf ? 4 : 8, kHalf ? 8 : 4><<<rows, kHalf ? 256 : 512, 0, st>>>(p, (int)tiles);
   else if (kHalf && tiles <= 64) score_row_kernel<E, 8, kHalf ? 8 : 4><<<rows, 512, 0, st>>>(p, (int)tiles);
-  else if (p.chunks == 1) score_long_row_kernel<E><<<rows, 1024, 0, st>>>(p, (int)tiles);
+  else if (p.chunks == 1 || (p.chunks == 2 && p.V < (kHalf ? 1 << 18 : 1 << 19))) score_long_row_kernel<E><<<rows, 1024, 0, st>>>(p, (int)tiles);
   else return false;
   return true;
 }

@@ -228,3 +228,16 @@ def test_scores_at_extreme_temperatures(V, temp, dtype):
         ref.check_scores(llc.llc_token_logprobs(x, t, 10, temp=temp, want_lse=True, v_chunks=chunks), x, t, 10, temp)
     a = torch.full((4, 4), temp if temp < 1 else 0.1, device=DEV)
     _gradients(x, t, a, None, temp, slice(0, 4))
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("R,V", [(86, 127999), (86, 128000), (128, 152064), (129, 152064), (86, 262143), (90, 262144), (86, 524288)])
+def test_scores_and_gradient_where_rows_begin_to_be_split_in_two(R, V, dtype):
+    x = _rows(R, V, dtype, R + V)
+    t = torch.randint(0, V, (R, 2), generator=_gen(V), device=DEV).to(torch.int32)
+    for M in (0, 40):
+        out = llc.llc_token_logprobs(x, t, M, temp=0.8, want_lse=True)
+        for rows in (slice(0, 4), slice(R - 4, R)):
+            ref.check_scores({k: v[rows] for k, v in out.items()}, x[rows], t[rows], M, 0.8)
+    a = torch.rand(R, 2, generator=_gen(1), device=DEV) / R
+    _gradients(x, t, a, None, 0.8, slice(R - 4, R))
