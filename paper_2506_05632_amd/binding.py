@@ -935,10 +935,10 @@ def llc_embed(table: torch.Tensor, tokens: torch.Tensor, *, scale: float = 1.0, 
             out = _new(table.device, {"out": (out_dtype or table.dtype, *shape, D)})["out"]
         else:
             out = _new(table.device, {"out": (out_dtype or table.dtype, tokens.shape[0], D)})["out"].view(*shape, D)
-    rows = out if out.dim() == 2 else out.view(-1, out.shape[-1])
-    if (out.device != table.device or out.dtype not in _TYPES or out_dtype not in (None, out.dtype) or tuple(out.shape) != (*shape, D)
-            or (rows.stride(1) != 1 and D > 1)):
-        raise ValueError("out must have the tokens' shape and D, float32 or bfloat16, rows contiguous")
+    bad = out.device != table.device or out.dtype not in _TYPES or out_dtype not in (None, out.dtype) or tuple(out.shape) != (*shape, D)
+    rows = None if bad else out if out.dim() == 2 else _as_rows(out, tokens.shape[0], D)
+    if rows is None or (rows.stride(1) != 1 and D > 1):
+        raise ValueError("out must have the tokens' shape and D, float32 or bfloat16, rows contiguous and a stride apart")
     a = EmbedArgs()
     a.T, a.N, a.D = tokens.shape[0], N, D
     a.dtype, a.out_dtype = _TYPES[table.dtype], _TYPES[out.dtype]
@@ -953,6 +953,13 @@ def llc_embed(table: torch.Tensor, tokens: torch.Tensor, *, scale: float = 1.0, 
     if rc != 0:
         raise LlcError(rc)
     return {"out": out}
+
+
+def _as_rows(out, T, D):
+    try:
+        return out.view(T, D)
+    except RuntimeError:  # (its rows lie at more than one distance)
+        return None
 
 
 def _flat(tokens):
@@ -975,7 +982,7 @@ def llc_embed_grad(g: torch.Tensor, tokens: torch.Tensor, N: int, *, scale: floa
         raise ValueError("g must have the tokens' shape and D, float32 or bfloat16; tokens int32")
     D = g.shape[-1]
     tokens = _flat(tokens)
-    rows = g if g.dim() == 2 else g.reshape(-1, D)
+    rows = g if g.dim() == 2 else g.reshape(tokens.shape[0], D)
     if rows.stride(1) != 1 and D > 1:
         raise ValueError("g's last dimension must be contiguous")
     if add and out is None:

@@ -24,3 +24,21 @@ def test_gradient_of_tokens_of_any_shape(shape):
         llc.llc_embed_grad(out.unsqueeze(0), t, 50)
     with pytest.raises(ValueError):
         llc.llc_embed_grad(torch.zeros((), device=DEV), t, 50)
+
+
+def test_lookup_outputs_that_cannot_be_taken():
+    table = torch.arange(50 * 6, device=DEV, dtype=torch.float32).view(50, 6)
+    t = torch.tensor([[1, 2, 3], [4, 50, -1]], dtype=torch.int32, device=DEV)
+    for out in (torch.empty((), device=DEV), torch.empty(2, 3, 0, device=DEV), torch.empty(36, device=DEV), torch.empty(3, 2, 6, device=DEV).transpose(0, 1),
+                torch.empty(2, 6, 3, device=DEV).transpose(1, 2), torch.empty(2, 4, 6, device=DEV)[:, :3]):
+        with pytest.raises(ValueError):
+            llc.llc_embed(table, t, out=out)
+    want = llc.llc_embed(table, t)["out"]
+    for out in (torch.empty(2, 3, 6, device=DEV), torch.empty(2, 3, 9, device=DEV)[:, :, :6], torch.empty(1, 3, 2, 6, device=DEV)[0].view(2, 3, 6)):
+        assert torch.equal(llc.llc_embed(table, t, out=out)["out"], want)
+    assert llc.llc_embed(table, t[:0], out=torch.empty(0, 3, 6, device=DEV))["out"].shape == (0, 3, 6)
+    for none in (lambda: llc.llc_embed(torch.empty(50, 0, device=DEV), t), lambda: llc.llc_embed_grad(torch.empty(2, 3, 0, device=DEV), t, 50),
+                 lambda: llc.llc_embed(torch.empty(0, 6, device=DEV), t)):
+        with pytest.raises(llc.LlcError) as e:
+            none()
+        assert e.value.code == -2
