@@ -64,7 +64,7 @@ enum {
                               at the vocabulary's two ends (llc_token_logprobs and below): check
                               the arguments, plan every launch of the call and check the
                               workspace against the plan, then return without launching
-                              anything (no pointer is dereferenced)                    */
+                              anything (no device pointer is dereferenced)             */
   LLC_FLAG_DRAFT_ONLY = 32,/* llc_couple, llc_couple_static, llc_couple_is: the draft side alone, i.e. the
                               drafters' step of Algorithm 2 (Section 4.2: every draft k samples its
                               next token X^(k) = argmin_i S_i^(k) / p_i^(k) with the randomness that
@@ -392,7 +392,8 @@ typedef struct llc_lml_args {
  * Sums are taken in fp32 over 16 entries of a thread and in fp64 beyond, whatever the length. */
 #define LLC_TOP_MAX 128
 typedef struct llc_token_logprobs_args {
-  int64_t R, V, G, M;       /* R >= 0, V in 1..2^31 - 5, G in 0..65535, M in 0..LLC_TOP_MAX */
+  int64_t R, V, G, M;       /* R in 0..2^24 - 1, V in 1..2^31 - 5, G in 0..65535, M in 0..LLC_TOP_MAX; LLC_E_SHAPE also
+                               where R times the workgroups of a row (v_chunks) passes 2^24 - 1       */
   int32_t dtype;            /* LLC_F32 | LLC_BF16                                        */
   int32_t kind;             /* LLC_LOGITS | LLC_LOGW                                     */
   const void *x;            /* device [R,V] */
@@ -419,13 +420,13 @@ typedef struct llc_token_logprobs_args {
  * with respect to x[r,:],
  *   grad[r,i] = (sum_g a_g [i == t_g] - p_i (A + b (ln p_i + H))) / temp,
  * a_g over the slots that hold an id in [0, V) (the others' are not looked at), A their sum, b the
- * entropy's weight; 0 for an entry without mass, and in a row without mass.  Rounded once to the
- * inputs' type.  grad may be x itself (same stride).  Either the row's lse, and with
+ * entropy's weight; 0 for an entry without mass, and in a row without mass.  Formed in fp32 (a weight over temp that fp32
+ * cannot hold is not told from infinity) and rounded to the inputs' type.  grad may be x itself (same stride).  Either the row's lse, and with
  * grad_entropy its entropy, are given as llc_token_logprobs returned them, or (lse == NULL) the call
  * forms them itself and returns logp, entropy and lse on request: a loss whose weights are known beforehand
  * then takes one call and, where a row fits a workgroup's registers, one pass. */
 typedef struct llc_token_logprobs_grad_args {
-  int64_t R, V, G;          /* as above                                                  */
+  int64_t R, V, G;          /* as above; R times V / 4096, rounded up, at most 2^24 - 1  */
   int32_t dtype, kind;      /* as above                                                  */
   const void *x;            /* device [R,V] */
   int64_t stride_r;
@@ -451,11 +452,11 @@ typedef struct llc_token_logprobs_grad_args {
   void *ev_begin, *ev_end;
 } llc_token_logprobs_grad_args;
 
-/* Arguments of llc_embed: out[t,:] = scale * table[tokens[t],:], rounded once to the output's type;
+/* Arguments of llc_embed: out[t,:] = scale * table[tokens[t],:], the product in fp32 and rounded to the output's type;
  * zeros for a token outside [0, N). */
 typedef struct llc_embed_args {
-  int64_t T, N, D;          /* T in 0..2^31 - 5, N, D in 1..2^31 - 5; LLC_E_SHAPE also where a launch would
-                               need more than 2^24 - 1 workgroups (a wavefront takes 4 KB of a row) */
+  int64_t T, N, D;          /* T in 0..2^31 - 5, N, D in 1..2^31 - 5; LLC_E_SHAPE also where T times the wavefronts of a row (1 for
+                               rows of the input of up to 1 KB, 2 up to 3 KB, 4 beyond) passes 2^26 - 4 */
   int32_t dtype, out_dtype; /* of table and of out: LLC_F32 | LLC_BF16                   */
   const void *table;        /* device [N,D] */
   int64_t table_stride_n;
@@ -471,11 +472,11 @@ typedef struct llc_embed_args {
 
 /* Arguments of llc_embed_grad: grad[n,:] = scale * sum over t with tokens[t] == n of g[t,:], summed in
  * fp32 in an order that follows t alone (the tokens are sorted, no floating-point atomics: the
- * same inputs give the same bits) and rounded once; tokens outside [0, N) take no part.
+ * same inputs give the same bits), scaled in fp32 and rounded to the gradient's type; tokens outside [0, N) take no part.
  * add == 0: every row of grad is written, zeros where no token is.  add != 0: the sum is added to the rows whose
  * tokens occur (in fp32, then rounded), the others are not touched. */
 typedef struct llc_embed_grad_args {
-  int64_t T, N, D;          /* as above; N at most 2^27                                  */
+  int64_t T, N, D;          /* as above; N at most 2^27; T / 32 times those wavefronts at most 3 * 2^24 - 4 */
   int32_t dtype, grad_dtype;/* of g and of grad                                          */
   const void *g;            /* device [T,D] */
   int64_t g_stride_t;
@@ -494,7 +495,7 @@ typedef struct llc_embed_grad_args {
 
 /* Arguments of llc_clip_grad_norm: norm = sqrt of the sum of squares over all n tensors (fp64 throughout,
  * so that squares neither overflow nor vanish; rounded once), and out_j = grad_j * min(1, max_norm / norm),
- * the factor in fp32, each product rounded once.  A norm that is not finite in fp32 leaves the gradients as they are (the caller
+ * factor and products in fp32, these rounded to the gradients' type.  A norm that is not finite in fp32 leaves the gradients as they are (the caller
  * sees it in `norm`).  The arrays grads, numel, dtype and out are HOST arrays, read before the call returns;
  * their pointers are device pointers to contiguous tensors.  out == NULL: in place.  max_norm may be +inf: the
  * norm alone (out, if given, gets copies).  Tensors must not overlap each other unless out_j is grad_j. */

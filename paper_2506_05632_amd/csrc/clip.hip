@@ -5,7 +5,7 @@
 // leaves its range: 519.0 us for 520.4 of the half billion below.)  Which piece a workgroup takes and the order in which partial sums are joined follow
 // from the sizes alone.
 // 534 M entries in 219 tensors, bf16 but for norms' gains, into other buffers: 0.52 ms, 6.2 TB/s of the 3.2 GB read, read again and written.  Small
-// lists: the host's call and two launches that wait for each other (21 tensors 11.6 us).
+// lists: the host's call and two launches that wait for each other (21 tensors 11.8 us).
 #include "ends.hpp"
 
 namespace llc {

@@ -335,7 +335,7 @@ template <typename A, typename B, bool ADD> __global__ void __launch_bounds__(kB
 }
 
 // The rows without a token: 4 KB a workgroup, one store a thread, in a launch of its own with next to nothing to set up.  Memory takes such a stream best
-// (0.95 GB: 149 us, 6.4 TB/s; two stores a thread 166 to 190, 64 rows a workgroup 206; in the summing launch, whose wavefronts carry more
+// (1.006 GB: 149 to 152 us, 6.7 TB/s; two stores a thread 166 to 190, 64 rows a workgroup 206; in the summing launch, whose wavefronts carry more
 // registers, 208).
 constexpr int kZeroRows = 32768;
 template <typename B>
