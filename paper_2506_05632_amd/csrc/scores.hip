@@ -1054,8 +1054,8 @@ template <typename E> hipError_t launch_gradient(ScoreParams p, hipStream_t st) 
   return hipGetLastError();
 }
 
-// Scores and gradient in one launch: as many wavefronts as keep the row in registers.  Rows too long for that are a workgroup's too where there are 86 or more: a
-// CU in three has one at least.  With fewer, or up to 128 rows so long that reading them twice costs a workgroup more than splitting them in two, scores and gradient are two or
+// Scores and gradient in one launch: as many wavefronts as keep the row in registers.  Rows too long for that are a workgroup's too where the scores would not be
+// split over more than two: under 64 000 entries, or 86 rows and more, so that a CU in three has one at least.  With fewer, or up to 128 rows so long that reading them twice costs a workgroup more than splitting them in two, scores and gradient are two or
 // three launches over all CUs.  us a call, one launch and several: 70 001 fp32 of 64 rows 18.1, 18.4, of 96 18.5, 22.5, of 256 30.2, 40.9; 128 256 fp32 of 64
 // rows 26.9, 23.8, of 107 27.9, 35.3, of 256 45.9, 66.1; 152 064 bf16 of 64 29.4, 19.3, of 107 26.8, 28.7, of 256 34.8, 45.3; 107 rows of 200 000 bf16 32.3,
 // 34.3, of 262 144 41.2, 41.0 (with entropies 46.0, 40.9), of 400 000 60.6, 55.0; of 400 000 fp32 82.3, 86.8, of 600 000 137, 127.  False: nothing was launched.
