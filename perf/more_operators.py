@@ -228,12 +228,12 @@ def run(state):
         if op == "truncate":
             return llc.llc_truncate(state["x"], **state["settings"])
         if op == "matvec":
-            return llc.llc_matvec4(state["x"], state["codes"], state["scales"], zeros=state["zeros"], group=case["G"], out_dtype=TYPES[case["out"]])
+            return llc.llc_matvec_quantized(state["x"], state["codes"], state["scales"], zeros=state["zeros"], group=case["G"], out_dtype=TYPES[case["out"]])
         if op == "embed":
-            return llc.llc_embed4(state["codes"], state["scales"], state["tokens"], case["D"], zeros=state["zeros"], group=case["G"],
+            return llc.llc_embed_quantized(state["codes"], state["scales"], state["tokens"], case["D"], zeros=state["zeros"], group=case["G"],
                                   scale=case["scale"], out_dtype=TYPES[case["out"]])
-        q = llc.llc_quantize4(state["w"], group=case["G"], zeros=case["zeros"], scales_dtype=TYPES[case["scales"]])
-        back = llc.llc_embed4(q["codes"], q["scales"], state["rows"], case["D"], zeros=q.get("zeros"), group=case["G"], out_dtype=TYPES[case["out"]])
+        q = llc.llc_quantize(state["w"], group=case["G"], zeros=case["zeros"], scales_dtype=TYPES[case["scales"]])
+        back = llc.llc_embed_quantized(q["codes"], q["scales"], state["rows"], case["D"], zeros=q.get("zeros"), group=case["G"], out_dtype=TYPES[case["out"]])
         return {"values": back["out"], "scales": q["scales"], "zeros": q.get("zeros")}
     if op == "sample":
         return _plain_sample(state["x"], state["u"], state["settings"])
