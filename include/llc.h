@@ -514,6 +514,139 @@ typedef struct llc_clip_grad_norm_args {
   void *ev_begin, *ev_end;
 } llc_clip_grad_norm_args;
 
+/* ---- The end of a drafting step: sampling from a cut distribution, the cut rows themselves, and layers
+ * held in 4 bits.  The random numbers are inputs. */
+
+/* What is left of a row's distribution, by the settings that llc_sample and llc_truncate share.  A row's entries are taken
+ * in the order of their values, larger first, equal ones by index; those of NaN, +inf and -inf carry no mass.
+ * The kept ones are the longest run of that order, never shorter than one entry, which is within all of
+ *   top_k: the first top_k entries (0: all);
+ *   top_p: the shortest run whose mass is at least top_p times the mass that top_k leaves (1: all);
+ *   min_p: the entries whose probability is at least min_p times the first one's (0: all).
+ * Masses are exp((x_i - x_1) / temp), taken and summed in fp64 (where a long run is cut by its mass, by whole numbers of 2^-51 of the
+ * first one's, or of what 62 bits hold of the row's): which entries are kept does not depend on timing.
+ * A row's own settings are those of its entry in the arrays, where given, and else the call's: temp finite and 2^-126 or
+ * more (LLC_LOGITS only), top_k of 0 or less is off, top_p of 1 or more is off and of 0 or less leaves the first entry, min_p of 0 or
+ * less is off and of 1 or more leaves the first one's equals.  Entries of the arrays are not checked on the host: a temperature outside its range, or a
+ * NaN, makes the row one without mass. */
+
+/* Arguments of llc_sample: tokens[r,s] = the first index i with sum over the kept j <= i of p_j > u[r,s] times the kept
+ * mass; u below 0 counts as 0, of 1 or more takes the last kept index, and a NaN gives token -1.  logp[r,s] = ln of the token's probability among
+ * the kept ones (-inf with token -1), kept[r] = how many they are.  A row without mass: -1, -inf, 0. */
+typedef struct llc_sample_args {
+  int64_t R, V, S;          /* R in 0..2^24 - 1, V in 1..2^31 - 5, S in 0..65535         */
+  int32_t dtype;            /* LLC_F32 | LLC_BF16                                        */
+  int32_t kind;             /* LLC_LOGITS | LLC_LOGW                                     */
+  const void *x;            /* device [R,V] */
+  int64_t stride_r;         /* elements */
+  float temp, top_p, min_p; /* 2^-126 or more, finite; in (0, 1]; in [0, 1]              */
+  int32_t top_k;            /* >= 0 */
+  const float *row_temp;    /* device [R] or NULL, in the place of the call's            */
+  const float *row_top_p;
+  const float *row_min_p;
+  const int32_t *row_top_k;
+  const float *u;           /* device [R,S]; may be NULL when S == 0                     */
+  int64_t u_stride_r;
+  int32_t *tokens;          /* [R,S] required unless S == 0                              */
+  float *logp;              /* [R,S] optional                                            */
+  int32_t *kept;            /* [R]   optional                                            */
+  void *stream;
+  int32_t flags;            /* LLC_FLAG_DRY_RUN                                          */
+  void *ev_begin, *ev_end;  /* optional hipEvent_t pair recorded around the kernels      */
+} llc_sample_args;
+
+/* Arguments of llc_truncate: out[r,i] = x[r,i] where i is kept, else -inf: rows that every call of this library takes as
+ * it takes x, with the same kind and temperature.  out may be x itself (same stride). */
+typedef struct llc_truncate_args {
+  int64_t R, V;             /* as above */
+  int32_t dtype, kind;
+  const void *x;            /* device [R,V] */
+  int64_t stride_r;
+  float temp, top_p, min_p; /* as above */
+  int32_t top_k;
+  const float *row_temp;
+  const float *row_top_p;
+  const float *row_min_p;
+  const int32_t *row_top_k;
+  void *out;                /* [R,V] of the inputs' type, required                       */
+  int64_t out_stride_r;     /* >= V */
+  int32_t *kept;            /* [R]   optional                                            */
+  void *stream;
+  int32_t flags;            /* LLC_FLAG_DRY_RUN                                          */
+  void *ev_begin, *ev_end;
+} llc_truncate_args;
+
+/* Layers in 4 bits.  A weight is w[n,d] = scales[n,g] * (q[n,d] - zeros[n,g]), g = d / group, q in 0..15; without zeros
+ * they are 8.  codes[n*codes_stride_n + d/2] holds q[n,d] in its lower half for even d, in its upper half for odd d; where D is odd the
+ * last upper half is not looked at (llc_quantize writes it as 0).  Rows may start at any byte. */
+
+/* Arguments of llc_quantize: w [N,D] to 4 bits.  Without zeros: scale = the largest |w| of the group over 7, q = the nearest
+ * whole number to w / scale, plus 8.  With zeros: low = the smallest entry or 0, high = the largest or 0, scale = (high - low) / 15,
+ * zero = the nearest whole number to -low / scale, q = the nearest to w / scale, plus zero.  The scale is formed in fp32 and rounded to its type, and
+ * the quotients are those of the rounded scale, as real numbers; ties to even; codes and zeros are held to 0..15.  A group whose scale rounds to 0
+ * has codes (and zero) 8.  Entries that are not finite take no part in the scale: NaN is coded as 0, an infinity as the group's outermost code. */
+typedef struct llc_quantize_args {
+  int64_t N, D;             /* N in 0..2^31 - 5, D in 1..2^31 - 5; LLC_E_SHAPE also where N times D / 2048, rounded up, passes 2^31 */
+  int32_t group;            /* 32 | 64 | 128 (else LLC_E_OPTION)                         */
+  int32_t dtype, scales_dtype; /* of w and of scales: LLC_F32 | LLC_BF16                 */
+  const void *w;            /* device [N,D] */
+  int64_t w_stride_n;       /* elements */
+  uint8_t *codes;           /* [N, (D + 1) / 2] */
+  int64_t codes_stride_n;   /* bytes */
+  void *scales;             /* [N, D / group rounded up] */
+  int64_t scales_stride_n;
+  uint8_t *zeros;           /* as scales; NULL: without zeros */
+  int64_t zeros_stride_n;
+  void *stream;
+  int32_t flags;            /* LLC_FLAG_DRY_RUN */
+  void *ev_begin, *ev_end;
+} llc_quantize_args;
+
+/* Arguments of llc_embed_quantized: out[t,:] = scale * w[tokens[t],:] of a layer in 4 bits, the products in fp32 and rounded to the output's
+ * type; zeros for a token outside [0, N). */
+typedef struct llc_embed_quantized_args {
+  int64_t T, N, D;          /* T in 0..2^31 - 5, N and D as above; LLC_E_SHAPE also where T times D / 2048, rounded up, passes 2^31 */
+  int32_t group;
+  int32_t scales_dtype, out_dtype;
+  const uint8_t *codes;
+  int64_t codes_stride_n;
+  const void *scales;
+  int64_t scales_stride_n;
+  const uint8_t *zeros;     /* or NULL */
+  int64_t zeros_stride_n;
+  const int32_t *tokens;    /* device [T] */
+  int64_t tok_stride;
+  float scale;              /* finite */
+  void *out;                /* [T,D] */
+  int64_t out_stride_t;
+  void *stream;
+  int32_t flags;            /* LLC_FLAG_DRY_RUN */
+  void *ev_begin, *ev_end;
+} llc_embed_quantized_args;
+
+/* Arguments of llc_matvec_quantized: out[r,n] = sum over d of x[r,d] w[n,d], w a layer in 4 bits.  The products x (q - zero) are summed
+ * over a group in fp32 (x of 32 bits as three parts of 8 bits, which hold all of it), those sums are multiplied by their scales and summed in fp32 and the
+ * result is rounded to the output's type.  A row of x with an entry that is not finite, or over 2^120 in size, gives outputs that need not be what
+ * the formula gives in that row; other rows are not touched by it.  Made for few rows: they are taken 64 at a time, and each such pass reads the layer. */
+typedef struct llc_matvec_quantized_args {
+  int64_t R, N, D;          /* R in 0..2^20, N in 1..2^31 - 5, D in 1..2^27              */
+  int32_t group;
+  int32_t dtype, scales_dtype, out_dtype; /* of x, of scales and of out                  */
+  const void *x;            /* device [R,D] */
+  int64_t x_stride_r;
+  const uint8_t *codes;
+  int64_t codes_stride_n;
+  const void *scales;
+  int64_t scales_stride_n;
+  const uint8_t *zeros;     /* or NULL */
+  int64_t zeros_stride_n;
+  void *out;                /* [R,N] */
+  int64_t out_stride_r;
+  void *stream;
+  int32_t flags;            /* LLC_FLAG_DRY_RUN */
+  void *ev_begin, *ev_end;
+} llc_matvec_quantized_args;
+
 /* Scores of tokens (log probability, entropy, top alternatives).  Asynchronous. */
 int llc_token_logprobs(const llc_token_logprobs_args *a);
 
@@ -534,6 +667,21 @@ size_t llc_embed_grad_workspace_size(int64_t T, int64_t N, int64_t D);
 /* Clipping by the global norm.  Asynchronous. */
 int llc_clip_grad_norm(const llc_clip_grad_norm_args *a);
 size_t llc_clip_grad_norm_workspace_size(int64_t n);
+
+/* Sampling from given random numbers, with cuts.  Asynchronous. */
+int llc_sample(const llc_sample_args *a);
+
+/* The cut rows themselves.  Asynchronous. */
+int llc_truncate(const llc_truncate_args *a);
+
+/* A layer to 4 bits.  Asynchronous. */
+int llc_quantize(const llc_quantize_args *a);
+
+/* Lookup in a table of 4 bits.  Asynchronous. */
+int llc_embed_quantized(const llc_embed_quantized_args *a);
+
+/* Products with a layer of 4 bits.  Asynchronous. */
+int llc_matvec_quantized(const llc_matvec_quantized_args *a);
 
 /* Algorithm 1 on a batch (Section 3).  Asynchronous on a->stream. */
 int llc_couple(const llc_couple_args *a);

@@ -31,7 +31,8 @@ _KINDS = {"logits": LOGITS, "probs": PROBS, "logw": LOGW}
 EXPORTS = ["llc_couple", "llc_couple_static", "llc_couple_is", "llc_couple_topm", "llc_compress_select", "llc_verify", "llc_lml_bound",
            "llc_couple_workspace_size", "llc_verify_workspace_size", "llc_lml_workspace_size", "llc_status_string",
            "llc_version", "llc_token_logprobs", "llc_token_logprobs_grad", "llc_token_logprobs_workspace_size", "llc_embed",
-           "llc_embed_grad", "llc_embed_grad_workspace_size", "llc_clip_grad_norm", "llc_clip_grad_norm_workspace_size"]
+           "llc_embed_grad", "llc_embed_grad_workspace_size", "llc_clip_grad_norm", "llc_clip_grad_norm_workspace_size",
+           "llc_sample", "llc_truncate", "llc_quantize", "llc_embed_quantized", "llc_matvec_quantized"]
 
 
 class LlcStats(ctypes.Structure):
@@ -229,6 +230,58 @@ class ClipGradNormArgs(ctypes.Structure):
     ]
 
 
+_CUTS = [("temp", ctypes.c_float), ("top_p", ctypes.c_float), ("min_p", ctypes.c_float), ("top_k", ctypes.c_int32),
+         ("row_temp", ctypes.c_void_p), ("row_top_p", ctypes.c_void_p), ("row_min_p", ctypes.c_void_p), ("row_top_k", ctypes.c_void_p)]
+_LAYER = [("codes", ctypes.c_void_p), ("codes_stride_n", ctypes.c_int64), ("scales", ctypes.c_void_p), ("scales_stride_n", ctypes.c_int64),
+          ("zeros", ctypes.c_void_p), ("zeros_stride_n", ctypes.c_int64)]
+_END = [("stream", ctypes.c_void_p), ("flags", ctypes.c_int32), ("ev_begin", ctypes.c_void_p), ("ev_end", ctypes.c_void_p)]
+
+
+class SampleArgs(ctypes.Structure):
+    _fields_ = [
+        ("R", ctypes.c_int64), ("V", ctypes.c_int64), ("S", ctypes.c_int64),
+        ("dtype", ctypes.c_int32), ("kind", ctypes.c_int32),
+        ("x", ctypes.c_void_p), ("stride_r", ctypes.c_int64), *_CUTS,
+        ("u", ctypes.c_void_p), ("u_stride_r", ctypes.c_int64),
+        ("tokens", ctypes.c_void_p), ("logp", ctypes.c_void_p), ("kept", ctypes.c_void_p), *_END,
+    ]
+
+
+class TruncateArgs(ctypes.Structure):
+    _fields_ = [
+        ("R", ctypes.c_int64), ("V", ctypes.c_int64),
+        ("dtype", ctypes.c_int32), ("kind", ctypes.c_int32),
+        ("x", ctypes.c_void_p), ("stride_r", ctypes.c_int64), *_CUTS,
+        ("out", ctypes.c_void_p), ("out_stride_r", ctypes.c_int64), ("kept", ctypes.c_void_p), *_END,
+    ]
+
+
+class QuantizeArgs(ctypes.Structure):
+    _fields_ = [
+        ("N", ctypes.c_int64), ("D", ctypes.c_int64), ("group", ctypes.c_int32),
+        ("dtype", ctypes.c_int32), ("scales_dtype", ctypes.c_int32),
+        ("w", ctypes.c_void_p), ("w_stride_n", ctypes.c_int64), *_LAYER, *_END,
+    ]
+
+
+class EmbedQuantizedArgs(ctypes.Structure):
+    _fields_ = [
+        ("T", ctypes.c_int64), ("N", ctypes.c_int64), ("D", ctypes.c_int64), ("group", ctypes.c_int32),
+        ("scales_dtype", ctypes.c_int32), ("out_dtype", ctypes.c_int32), *_LAYER,
+        ("tokens", ctypes.c_void_p), ("tok_stride", ctypes.c_int64), ("scale", ctypes.c_float),
+        ("out", ctypes.c_void_p), ("out_stride_t", ctypes.c_int64), *_END,
+    ]
+
+
+class MatvecQuantizedArgs(ctypes.Structure):
+    _fields_ = [
+        ("R", ctypes.c_int64), ("N", ctypes.c_int64), ("D", ctypes.c_int64), ("group", ctypes.c_int32),
+        ("dtype", ctypes.c_int32), ("scales_dtype", ctypes.c_int32), ("out_dtype", ctypes.c_int32),
+        ("x", ctypes.c_void_p), ("x_stride_r", ctypes.c_int64), *_LAYER,
+        ("out", ctypes.c_void_p), ("out_stride_r", ctypes.c_int64), *_END,
+    ]
+
+
 _lib = None
 _empties = None
 _tensor_list = None
@@ -270,7 +323,9 @@ def load():
         lib.llc_verify_workspace_size.argtypes = [ctypes.c_int64] * 4
         lib.llc_verify_workspace_size.restype = ctypes.c_size_t
         for name, args in (("llc_token_logprobs", TokenLogprobsArgs), ("llc_token_logprobs_grad", TokenLogprobsGradArgs),
-                           ("llc_embed", EmbedArgs), ("llc_embed_grad", EmbedGradArgs), ("llc_clip_grad_norm", ClipGradNormArgs)):
+                           ("llc_embed", EmbedArgs), ("llc_embed_grad", EmbedGradArgs), ("llc_clip_grad_norm", ClipGradNormArgs),
+                           ("llc_sample", SampleArgs), ("llc_truncate", TruncateArgs), ("llc_quantize", QuantizeArgs),
+                           ("llc_embed_quantized", EmbedQuantizedArgs), ("llc_matvec_quantized", MatvecQuantizedArgs)):
             getattr(lib, name).argtypes = [ctypes.POINTER(args)]
             getattr(lib, name).restype = ctypes.c_int
         for name, count in (("llc_token_logprobs_workspace_size", 3), ("llc_embed_grad_workspace_size", 3),
@@ -1060,6 +1115,233 @@ def llc_clip_grad_norm(grads, max_norm: float, *, out=None, workspace: Optional[
     if rc != 0:
         raise LlcError(rc)
     return {"norm": norm}
+
+
+def _called(function, a, device):
+    """The call, on the tensors' device whichever is the current one."""
+    if device.index == torch._C._cuda_getDevice():
+        rc = function(ctypes.byref(a))
+    else:
+        with torch.cuda.device(device):
+            rc = function(ctypes.byref(a))
+    if rc != 0:
+        raise LlcError(rc)
+
+
+def _cut_into(a, name, logits, kind, temp, top_k, top_p, min_p):
+    """The checks that sampling and cutting share, and their arguments."""
+    R, V, _ = _scored(name, logits, None, kind)
+    dev = logits.device
+    a.R, a.V, a.dtype, a.kind = R, V, _TYPES[logits.dtype], _KINDS[kind]
+    a.x, a.stride_r = logits.data_ptr(), logits.stride(0)
+    if type(temp) is float and type(top_k) is int and type(top_p) is float and type(min_p) is float and top_k < 1 << 31:
+        a.temp, a.top_k, a.top_p, a.min_p = temp, top_k, top_p, min_p
+        return R, V, dev
+    for field, value, dtype in (("temp", temp, torch.float32), ("top_k", top_k, torch.int32), ("top_p", top_p, torch.float32),
+                                ("min_p", min_p, torch.float32)):
+        if not isinstance(value, torch.Tensor):
+            if field == "top_k" and (int(value) != value or value >= 1 << 31):
+                raise ValueError("top_k must be a whole number below 2^31")
+            setattr(a, field, int(value) if field == "top_k" else float(value))
+            continue
+        if value.device != dev or value.dtype != dtype or tuple(value.shape) != (R,) or not value.is_contiguous():
+            raise ValueError(f"{field} must be a number, or {dtype} of [R], contiguous, on the logits' device")
+        setattr(a, "row_" + field, value.data_ptr())
+    return R, V, dev
+
+
+def llc_sample(logits: torch.Tensor, u: torch.Tensor, *, temp=1.0, top_k=0, top_p=1.0, min_p=0.0, kind="logits", want_logp: bool = True,
+               want_kept: bool = False, out: Optional[dict] = None, flags: int = 0, events=None) -> dict:
+    """Draws tokens of every row's cut distribution with given uniform numbers.
+
+    logits: [R,V] float32 or bfloat16 (kind "logits", with the temperature, or "logw"); u: [R] or [R,S] float32 in [0, 1).
+    What is kept: the likeliest top_k entries (0: all), of them the fewest that hold top_p of their mass (1: all), and of those
+    the ones at least min_p times as likely as the likeliest (0: all); equal entries by index.  Each setting is a number or a
+    tensor [R] of the rows' own (float32, top_k int32).  Returns int32 tokens (u's shape): the first index up to which the kept
+    mass exceeds u of it; if asked float32 logp, ln of the tokens' probabilities among the kept, and int32 kept [R].
+    A row without mass: -1, -inf and 0.  Asynchronous on torch's current stream.
+    """
+    lib = load()
+    a = SampleArgs()
+    R, V, dev = _cut_into(a, "llc_sample", logits, kind, temp, top_k, top_p, min_p)
+    if u.device != dev or u.dtype != torch.float32 or u.dim() not in (1, 2) or u.shape[0] != R or (
+            u.dim() == 2 and u.stride(1) != 1 and u.shape[1] > 1):
+        raise ValueError("u must be [R] or [R,S] float32 on the logits' device, last dimension of [R,S] contiguous")
+    shape = tuple(u.shape)
+    if out is None:
+        specs = {"tokens": (torch.int32, *shape)}
+        if want_logp:
+            specs["logp"] = (torch.float32, *shape)
+        if want_kept:
+            specs["kept"] = (torch.int32, R)
+        out = _new(dev, specs)
+    else:
+        _check_given(out, dev, {"tokens": (torch.int32, *shape), "logp": (torch.float32, *shape), "kept": (torch.int32, R)})
+        if out.get("tokens") is None:
+            raise ValueError("out must hold tokens")
+    a.S = 1 if u.dim() == 1 else shape[1]
+    a.u, a.u_stride_r = u.data_ptr(), u.stride(0)
+    a.tokens, a.logp, a.kept = out["tokens"].data_ptr(), _ptr(out.get("logp")), _ptr(out.get("kept"))
+    a.stream = _stream_handle(dev)
+    a.flags = flags
+    if events is not None:
+        a.ev_begin, a.ev_end = events
+    _called(lib.llc_sample, a, dev)
+    return out
+
+
+def llc_truncate(logits: torch.Tensor, *, temp=1.0, top_k=0, top_p=1.0, min_p=0.0, kind="logits", want_kept: bool = True,
+                 out: Optional[dict] = None, flags: int = 0, events=None) -> dict:
+    """Rows with what the cuts leave of them: kept entries as they are, -inf elsewhere.
+
+    logits, settings and kind as in llc_sample.  Returns logits [R,V] in the inputs' type (out["logits"] may be the logits
+    themselves), which every call here takes as it takes the uncut rows, with the same kind and temperature, and if
+    asked int32 kept [R].  Asynchronous on torch's current stream.
+    """
+    lib = load()
+    a = TruncateArgs()
+    R, V, dev = _cut_into(a, "llc_truncate", logits, kind, temp, top_k, top_p, min_p)
+    if out is None:
+        specs = {"logits": (logits.dtype, R, V)}
+        if want_kept:
+            specs["kept"] = (torch.int32, R)
+        out = _new(dev, specs)
+    else:
+        _check_given(out, dev, {"kept": (torch.int32, R)})
+    to = out["logits"]
+    if to.device != dev or to.dtype != logits.dtype or tuple(to.shape) != (R, V) or (to.stride(1) != 1 and V > 1):
+        raise ValueError("out['logits'] must be [R,V] of the logits' type, last dimension contiguous")
+    a.stride_r, a.out, a.out_stride_r = _row_stride(logits), to.data_ptr(), _row_stride(to)
+    a.kept = _ptr(out.get("kept"))
+    a.stream = _stream_handle(dev)
+    a.flags = flags
+    if events is not None:
+        a.ev_begin, a.ev_end = events
+    _called(lib.llc_truncate, a, dev)
+    return out
+
+
+def _layer_into(a, codes, scales, zeros, D, group):
+    """The checks of a layer in 4 bits, and its arguments; its rows."""
+    if not codes.is_cuda:
+        raise ValueError("layers in 4 bits are device tensors (there is no CPU path)")
+    if codes.dtype != torch.uint8 or codes.dim() != 2 or codes.shape[1] != (D + 1) // 2 or (codes.stride(1) != 1 and codes.shape[1] > 1):
+        raise ValueError("codes must be [N, (D + 1) // 2] uint8, last dimension contiguous")
+    if group not in (32, 64, 128):
+        raise ValueError("group must be 32, 64 or 128")
+    N, groups = codes.shape[0], -(-D // group)
+    if scales.device != codes.device or scales.dtype not in _TYPES or tuple(scales.shape) != (N, groups) or (scales.stride(1) != 1 and groups > 1):
+        raise ValueError("scales must be [N, D / group rounded up], float32 or bfloat16, on the codes' device, last dimension contiguous")
+    a.group, a.scales_dtype = group, _TYPES[scales.dtype]
+    a.codes, a.codes_stride_n = codes.data_ptr(), _row_stride(codes)
+    a.scales, a.scales_stride_n = scales.data_ptr(), _row_stride(scales)
+    if zeros is not None:
+        if zeros.device != codes.device or zeros.dtype != torch.uint8 or zeros.shape != scales.shape or (zeros.stride(1) != 1 and groups > 1):
+            raise ValueError("zeros must be uint8 of the scales' shape, on the codes' device, last dimension contiguous")
+        a.zeros, a.zeros_stride_n = zeros.data_ptr(), _row_stride(zeros)
+    return N
+
+
+def llc_quantize(w: torch.Tensor, *, group: int = 128, zeros: bool = False, scales_dtype: torch.dtype = torch.bfloat16,
+                  out: Optional[dict] = None, flags: int = 0, events=None) -> dict:
+    """A layer [N,D] to 4 bits: w[n,d] is near scales[n,g] * (q[n,d] - zeros[n,g]), g = d // group, q in 0..15.
+
+    w: float32 or bfloat16; group 32, 64 or 128.  Returns uint8 codes [N, (D + 1) // 2], two columns a byte (even ones in
+    the lower half), scales [N, D / group rounded up] and, with zeros=True, uint8 zeros of that shape; without, zeros are 8
+    and the scale a seventh of the group's largest entry.  Asynchronous on torch's current stream.
+    """
+    lib = load()
+    if not w.is_cuda:
+        raise ValueError("llc_quantize needs device tensors (there is no CPU path)")
+    if w.dtype not in _TYPES or w.dim() != 2 or w.shape[1] < 1 or (w.stride(1) != 1 and w.shape[1] > 1):
+        raise ValueError("w must be [N,D], float32 or bfloat16, last dimension contiguous")
+    if group not in (32, 64, 128) or scales_dtype not in _TYPES:
+        raise ValueError("group must be 32, 64 or 128, scales_dtype float32 or bfloat16")
+    N, D = w.shape
+    groups = -(-D // group)
+    if out is None:
+        specs = {"codes": (torch.uint8, N, (D + 1) // 2), "scales": (scales_dtype, N, groups)}
+        if zeros:
+            specs["zeros"] = (torch.uint8, N, groups)
+        out = _new(w.device, specs)
+    if out["codes"].device != w.device or (out.get("zeros") is not None) != zeros or out["scales"].dtype != scales_dtype or out["codes"].shape[0] != N:
+        raise ValueError("out must hold codes, scales of scales_dtype and, exactly with zeros=True, zeros, on w's device")
+    a = QuantizeArgs()
+    _layer_into(a, out["codes"], out["scales"], out.get("zeros"), D, group)
+    a.N, a.D, a.dtype = N, D, _TYPES[w.dtype]
+    a.w, a.w_stride_n = w.data_ptr(), w.stride(0)
+    a.stream = _stream_handle(w.device)
+    a.flags = flags
+    if events is not None:
+        a.ev_begin, a.ev_end = events
+    _called(lib.llc_quantize, a, w.device)
+    return out
+
+
+def llc_embed_quantized(codes: torch.Tensor, scales: torch.Tensor, tokens: torch.Tensor, D: int, *, zeros: Optional[torch.Tensor] = None,
+               group: int = 128, scale: float = 1.0, out_dtype: Optional[torch.dtype] = None, out: Optional[torch.Tensor] = None,
+               flags: int = 0, events=None) -> dict:
+    """llc_embed of a table in 4 bits: out[..., :] = scale * w[tokens[...], :], zeros for tokens outside the table.
+
+    codes, scales, zeros, group: as llc_quantize returned them, of a table [N,D]; tokens: int32 of any shape; out has the tokens'
+    shape and D, in out_dtype (default: the scales').  Asynchronous on torch's current stream.
+    """
+    lib = load()
+    a = EmbedQuantizedArgs()
+    N = _layer_into(a, codes, scales, zeros, D, group)
+    if tokens.device != codes.device or tokens.dtype != torch.int32:
+        raise ValueError("tokens must be int32 on the codes' device")
+    tokens, shape = _flat(tokens), tokens.shape
+    if out is None:
+        specs = {"out": (out_dtype or scales.dtype, *shape, D) if len(shape) < 4 else (out_dtype or scales.dtype, tokens.shape[0], D)}
+        out = _new(codes.device, specs)["out"].view(*shape, D)
+    bad = out.device != codes.device or out.dtype not in _TYPES or out_dtype not in (None, out.dtype) or tuple(out.shape) != (*shape, D)
+    rows = None if bad else out if out.dim() == 2 else _as_rows(out, tokens.shape[0], D)
+    if rows is None or (rows.stride(1) != 1 and D > 1):
+        raise ValueError("out must have the tokens' shape and D, float32 or bfloat16, rows contiguous and a stride apart")
+    a.T, a.N, a.D = tokens.shape[0], N, D
+    a.out_dtype = _TYPES[out.dtype]
+    a.tokens, a.tok_stride, a.scale = tokens.data_ptr(), tokens.stride(0), scale
+    a.out, a.out_stride_t = out.data_ptr(), _row_stride(rows)
+    a.stream = _stream_handle(codes.device)
+    a.flags = flags
+    if events is not None:
+        a.ev_begin, a.ev_end = events
+    _called(lib.llc_embed_quantized, a, codes.device)
+    return {"out": out}
+
+
+def llc_matvec_quantized(x: torch.Tensor, codes: torch.Tensor, scales: torch.Tensor, *, zeros: Optional[torch.Tensor] = None, group: int = 128,
+                out_dtype: Optional[torch.dtype] = None, out: Optional[torch.Tensor] = None, flags: int = 0, events=None) -> dict:
+    """Products with a layer in 4 bits: out[r,n] = sum over d of x[r,d] * w[n,d].
+
+    x: [R,D] float32 or bfloat16, last dimension contiguous; codes, scales, zeros, group: as llc_quantize returned them, of a
+    layer [N,D].  Returns out [R,N] in out_dtype (default: x's).  Sums are in fp32, of exact products.  For few rows: every
+    64 of them read the layer once.  Asynchronous on torch's current stream.
+    """
+    lib = load()
+    if x.dtype not in _TYPES or x.dim() != 2 or x.shape[1] < 1 or (x.stride(1) != 1 and x.shape[1] > 1):
+        raise ValueError("x must be [R,D], float32 or bfloat16, last dimension contiguous")
+    R, D = x.shape
+    a = MatvecQuantizedArgs()
+    N = _layer_into(a, codes, scales, zeros, D, group)
+    if x.device != codes.device:
+        raise ValueError("x must be on the codes' device")
+    if out is None:
+        out = _new(x.device, {"out": (out_dtype or x.dtype, R, N)})["out"]
+    if (out.device != x.device or out.dtype not in _TYPES or out_dtype not in (None, out.dtype) or tuple(out.shape) != (R, N)
+            or (out.stride(1) != 1 and N > 1)):
+        raise ValueError("out must be [R,N], float32 or bfloat16, last dimension contiguous")
+    a.R, a.N, a.D = R, N, D
+    a.dtype, a.out_dtype = _TYPES[x.dtype], _TYPES[out.dtype]
+    a.x, a.x_stride_r = x.data_ptr(), x.stride(0)
+    a.out, a.out_stride_r = out.data_ptr(), _row_stride(out)
+    a.stream = _stream_handle(x.device)
+    a.flags = flags
+    if events is not None:
+        a.ev_begin, a.ev_end = events
+    _called(lib.llc_matvec_quantized, a, x.device)
+    return {"out": out}
 
 
 def new_workspace(B: int, K: int, V: int, device, v_chunks: int = 0) -> torch.Tensor:

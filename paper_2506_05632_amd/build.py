@@ -13,10 +13,10 @@ CSRC = os.path.join(HERE, "csrc")
 OBJ = os.path.join(HERE, "_build")
 LIB = os.path.join(HERE, "libllc_hip.so")
 PROBE_LIB = os.path.join(HERE, "libllc_probe.so")   # machine probes for bench.py --workload peaks
-SOURCES = ["api.hip", "static_scratch.hip", "finalize.hip", "topm.hip", "lml.hip", "scores.hip", "embed.hip", "clip.hip", "scan_f32_shared.hip", "scan_f32_perk.hip",
+SOURCES = ["api.hip", "static_scratch.hip", "finalize.hip", "topm.hip", "lml.hip", "scores.hip", "embed.hip", "clip.hip", "cut.hip", "quantized.hip", "matvec_quantized_bf16.hip", "matvec_quantized_f32.hip", "scan_f32_shared.hip", "scan_f32_perk.hip",
            "scan_bf16_shared.hip", "scan_bf16_perk.hip", "scan_f32_shared_minf.hip", "scan_f32_perk_minf.hip",
            "scan_bf16_shared_minf.hip", "scan_bf16_perk_minf.hip"]
-HEADERS = ["common.hpp", "scan.hpp", "finalize_row.hpp", "lml_search.hpp", "ends.hpp", os.path.join("..", "..", "include", "llc.h")]
+HEADERS = ["common.hpp", "scan.hpp", "finalize_row.hpp", "lml_search.hpp", "ends.hpp", "quantized.hpp", "matvec_quantized.hpp", os.path.join("..", "..", "include", "llc.h")]
 FLAGS = ["--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC", "-Wall",
          "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops"]
 

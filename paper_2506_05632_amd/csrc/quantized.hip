@@ -1,0 +1,286 @@
+// Layers held in 4 bits: making one, looking rows of it up, and the host side of the products with it.  The first two move data and compute next to
+// nothing beside it: memory bounds them.  A lane takes eight neighbouring columns (a word of codes), a wavefront 512, four times over.
+#include "quantized.hpp"
+
+namespace llc {
+namespace {
+
+constexpr int kPieces = 4;                    // of 512 columns that a wavefront has in flight
+constexpr int kUnit = 512 * kPieces;
+constexpr long long kMostUnitBlocks = 1LL << 22;  // of a launch; its workgroups take several units each where there are more
+constexpr long long kMostUnits = 1LL << 31;
+
+struct QuantizedParams {
+  long long N, D;           // rows (tokens of the lookup) and columns
+  long long table;          // rows of the lookup's table
+  unsigned units_row;       // units of a row
+  long long units;
+  const void *w;
+  long long w_stride;
+  uint8_t *codes;
+  long long codes_stride;
+  void *scales;
+  long long scales_stride;
+  uint8_t *zeros;
+  long long zeros_stride;
+  const int32_t *tokens;
+  long long tok_stride;
+  float scale;
+  void *out;
+  long long out_stride;
+};
+
+template <int CTRL> __device__ __forceinline__ float dpp_max(float v) {
+  return fmaxf(v, __builtin_bit_cast(float, __builtin_amdgcn_update_dpp(0, __builtin_bit_cast(int, v), CTRL, 0xF, 0xF, true)));
+}
+template <int LANES> __device__ __forceinline__ float max_lanes(float v) {  // over 4, 8 or 16 neighbours, in each of them
+  v = dpp_max<0xB1>(v);
+  v = dpp_max<0x4E>(v);
+  if constexpr (LANES >= 8) v = dpp_max<0x141>(v);
+  if constexpr (LANES >= 16) v = dpp_max<0x140>(v);
+  return v;
+}
+
+// The whole number nearest to w / s, ties to even, for a quotient of at most some 16: a product with the rounded reciprocal finds it within one, and the sign of w - (n + 1/2) s,
+// which a fused multiply-add rounds rightly, decides.  (fp32 division, ten operations, makes ties of quotients that are none: half of a group's
+// largest entry is three and a half times its scale but for the scale's rounding.)
+__device__ __forceinline__ float nearest(float w, float s, float inverse) {
+  const float n = floorf(fminf(fmaxf(w * inverse, -20.0f), 20.0f));
+  const float d = fmaf(-(n + 0.5f), s, w);
+  return d > 0.0f ? n + 1.0f : d < 0.0f ? n : n + (float)((int)n & 1);
+}
+
+template <int G, typename A, typename S, bool ZEROS> __global__ void __launch_bounds__(kBlock) quantize_kernel(const QuantizedParams p) {
+  const int lane = threadIdx.x & 63;
+  for (long long unit = (long long)blockIdx.x * (kBlock / 64) + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6); unit < p.units;
+       unit += (long long)gridDim.x * (kBlock / 64)) {
+    const long long n = unit / p.units_row, first = (unit - n * p.units_row) * kUnit + lane * 8;
+    const A *row = reinterpret_cast<const A *>(p.w) + n * p.w_stride;
+    float v[kPieces][8];
+#pragma unroll
+    for (int i = 0; i < kPieces; ++i) {
+      const long long at = first + i * 512;
+      if (at < p.D) {
+        load_first<8>(row + at, p.D - at, v[i]);
+      } else {
+#pragma unroll
+        for (int j = 0; j < 8; ++j) v[i][j] = 0.0f;
+      }
+    }
+#pragma unroll
+    for (int i = 0; i < kPieces; ++i) {
+      const long long at = first + i * 512;
+      float low = 0.0f, high = 0.0f;  // (of -w where there are zeros)
+#pragma unroll
+      for (int j = 0; j < 8; ++j) {
+        const float f = fabsf(v[i][j]) < INFINITY ? v[i][j] : 0.0f;
+        high = fmaxf(high, ZEROS ? f : fabsf(f));
+        if constexpr (ZEROS) low = fmaxf(low, -f);
+      }
+      high = max_lanes<G / 8>(high);
+      if constexpr (ZEROS) low = max_lanes<G / 8>(low);
+      float scale;
+      if constexpr (ZEROS) scale = high + low < INFINITY ? (high + low) / 15.0f : (0.5f * high + 0.5f * low) / 7.5f;
+      else scale = high / 7.0f;
+      const S kept = narrow<S>(scale);
+      scale = widen(kept);
+      // (scales whose reciprocal would not be a number: both sides are raised, exactly)
+      const float lift = scale < 0x1p-100f ? 0x1p64f : 1.0f, s = scale * lift, inverse = __builtin_amdgcn_rcpf(s);
+      float zero = 8.0f;
+      if constexpr (ZEROS) zero = scale > 0.0f ? fminf(nearest(low * lift, s, inverse), 15.0f) : 8.0f;
+      if (at >= p.D) continue;
+      uint32_t word = 0;
+#pragma unroll
+      for (int j = 0; j < 8; ++j) {
+        float q = nearest(v[i][j] * lift, s, inverse) + zero;
+        q = fminf(fmaxf(q, 0.0f), 15.0f);
+        q = scale > 0.0f && v[i][j] == v[i][j] ? q : zero;
+        word |= (at + j < p.D ? (uint32_t)q : 0u) << (4 * j);
+      }
+      uint8_t *to = p.codes + n * p.codes_stride + at / 2;
+      if (at + 8 <= p.D) {
+        *reinterpret_cast<word1_byte *>(to) = word;
+      } else {
+#pragma unroll
+        for (int j = 0; j < 4; ++j)
+          if (at + 2 * j < p.D) to[j] = (uint8_t)(word >> (8 * j));
+      }
+      if (at % G == 0) {
+        reinterpret_cast<S *>(p.scales)[n * p.scales_stride + at / G] = kept;
+        if constexpr (ZEROS) p.zeros[n * p.zeros_stride + at / G] = (uint8_t)zero;
+      }
+    }
+  }
+}
+
+template <int G, typename S, typename B> __global__ void __launch_bounds__(kBlock) embed_quantized_kernel(const QuantizedParams p) {
+  const int lane = threadIdx.x & 63;
+  for (long long unit = (long long)blockIdx.x * (kBlock / 64) + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6); unit < p.units;
+       unit += (long long)gridDim.x * (kBlock / 64)) {
+    const long long t = unit / p.units_row, first = (unit - t * p.units_row) * kUnit + lane * 8;
+    const long long n = p.tokens[t * p.tok_stride];
+    const bool there = n >= 0 && n < p.table;
+    const uint8_t *codes = p.codes + (there ? n : 0) * p.codes_stride;
+    const S *scales = reinterpret_cast<const S *>(p.scales) + (there ? n : 0) * p.scales_stride;
+    const uint8_t *zeros = p.zeros != nullptr ? p.zeros + (there ? n : 0) * p.zeros_stride : nullptr;
+    B *to = reinterpret_cast<B *>(p.out) + t * p.out_stride;
+    uint32_t word[kPieces];
+    float scale[kPieces], zero[kPieces];
+#pragma unroll
+    for (int i = 0; i < kPieces; ++i) {
+      const long long at = first + i * 512;
+      word[i] = 0; scale[i] = 0.0f; zero[i] = 8.0f;
+      if (at < p.D) {
+        word[i] = load_codes(codes, at, p.D);
+        scale[i] = widen(scales[at / G]);
+        if (zeros != nullptr) zero[i] = (float)zeros[at / G];
+      }
+    }
+#pragma unroll
+    for (int i = 0; i < kPieces; ++i) {
+      const long long at = first + i * 512;
+      if (at >= p.D) continue;
+      float v[8];
+#pragma unroll
+      for (int j = 0; j < 8; ++j) {
+        const float w = p.scale * (scale[i] * ((float)((word[i] >> (4 * j)) & 15) - zero[i]));
+        v[j] = there ? w : 0.0f;
+      }
+      stream_first<8>(to + at, p.D - at, v);
+    }
+  }
+}
+
+template <typename F> hipError_t by_group(int group, F launch) {
+  if (group == 128) return launch(std::integral_constant<int, 128>());
+  if (group == 64) return launch(std::integral_constant<int, 64>());
+  return launch(std::integral_constant<int, 32>());
+}
+template <typename F> hipError_t by_type(int type, F launch) { return type == LLC_F32 ? launch(float()) : launch(uint16_t()); }
+
+// A layer's sizes and rows, the same in every call.
+int check_layer(long long N, long long D, int group, const void *codes, long long codes_stride, const void *scales, int scales_dtype, long long scales_stride,
+                const void *zeros, long long zeros_stride) {
+  (void)N;
+  if (codes == nullptr || scales == nullptr) return LLC_E_NULL;
+  const long long groups = groups_of(D, group);
+  if (codes_stride < (D + 1) / 2 || scales_stride < groups || (zeros != nullptr && zeros_stride < groups)) return LLC_E_SHAPE;
+  if (!known_type(scales_dtype)) return LLC_E_DTYPE;
+  return fits(scales, type_size(scales_dtype)) ? LLC_OK : LLC_E_ALIGN;
+}
+bool units_of(QuantizedParams &p) {
+  p.units_row = (unsigned)((p.D + kUnit - 1) / kUnit);
+  p.units = p.N * p.units_row;
+  return p.units <= kMostUnits;
+}
+unsigned unit_blocks(const QuantizedParams &p) {
+  const long long blocks = (p.units + kBlock / 64 - 1) / (kBlock / 64);
+  return (unsigned)(blocks < kMostUnitBlocks ? blocks : kMostUnitBlocks);
+}
+
+}  // namespace
+}  // namespace llc
+
+using namespace llc;
+
+extern "C" int llc_quantize(const llc_quantize_args *a) {
+  if (a == nullptr) return LLC_E_NULL;
+  if (a->N < 0 || a->N > kMaxIndex || a->D < 1 || a->D > kMaxIndex) return LLC_E_SHAPE;
+  if ((a->flags & ~LLC_FLAG_DRY_RUN) != 0 || !known_group(a->group)) return LLC_E_OPTION;
+  if (a->N == 0) return LLC_OK;
+  if (a->w == nullptr) return LLC_E_NULL;
+  const int bad = check_layer(a->N, a->D, a->group, a->codes, a->codes_stride_n, a->scales, a->scales_dtype, a->scales_stride_n, a->zeros, a->zeros_stride_n);
+  if (bad != LLC_OK) return bad;
+  if (a->w_stride_n < 0) return LLC_E_SHAPE;
+  if (!known_type(a->dtype)) return LLC_E_DTYPE;
+  if (!fits(a->w, type_size(a->dtype))) return LLC_E_ALIGN;
+  QuantizedParams p = {};
+  p.N = a->N; p.D = a->D; p.w = a->w; p.w_stride = a->w_stride_n; p.codes = a->codes; p.codes_stride = a->codes_stride_n;
+  p.scales = a->scales; p.scales_stride = a->scales_stride_n; p.zeros = a->zeros; p.zeros_stride = a->zeros_stride_n;
+  if (!units_of(p)) return LLC_E_SHAPE;
+  if ((a->flags & LLC_FLAG_DRY_RUN) != 0) return LLC_OK;
+  hipStream_t st = (hipStream_t)a->stream;
+  return between_events(a->ev_begin, a->ev_end, st, [&] {
+    return by_group(a->group, [&](auto group) {
+      return by_type(a->dtype, [&](auto from) {
+        return by_type(a->scales_dtype, [&](auto scale) {
+          constexpr int G = decltype(group)::value;
+          if (p.zeros != nullptr) quantize_kernel<G, decltype(from), decltype(scale), true><<<unit_blocks(p), kBlock, 0, st>>>(p);
+          else quantize_kernel<G, decltype(from), decltype(scale), false><<<unit_blocks(p), kBlock, 0, st>>>(p);
+          return hipGetLastError();
+        });
+      });
+    });
+  });
+}
+
+extern "C" int llc_embed_quantized(const llc_embed_quantized_args *a) {
+  if (a == nullptr) return LLC_E_NULL;
+  if (a->T < 0 || a->T > kMaxIndex || a->N < 1 || a->N > kMaxIndex || a->D < 1 || a->D > kMaxIndex) return LLC_E_SHAPE;
+  if ((a->flags & ~LLC_FLAG_DRY_RUN) != 0 || !known_group(a->group) || !std::isfinite(a->scale)) return LLC_E_OPTION;
+  if (a->T == 0) return LLC_OK;
+  if (a->tokens == nullptr || a->out == nullptr) return LLC_E_NULL;
+  const int bad = check_layer(a->N, a->D, a->group, a->codes, a->codes_stride_n, a->scales, a->scales_dtype, a->scales_stride_n, a->zeros, a->zeros_stride_n);
+  if (bad != LLC_OK) return bad;
+  if (a->tok_stride < 0 || a->out_stride_t < a->D) return LLC_E_SHAPE;
+  if (!known_type(a->out_dtype)) return LLC_E_DTYPE;
+  if (!fits(a->out, type_size(a->out_dtype)) || !fits(a->tokens, 4)) return LLC_E_ALIGN;
+  QuantizedParams p = {};
+  p.N = a->T; p.D = a->D; p.table = a->N; p.codes = const_cast<uint8_t *>(a->codes); p.codes_stride = a->codes_stride_n;
+  p.scales = const_cast<void *>(a->scales); p.scales_stride = a->scales_stride_n; p.zeros = const_cast<uint8_t *>(a->zeros); p.zeros_stride = a->zeros_stride_n;
+  p.tokens = a->tokens; p.tok_stride = a->tok_stride; p.scale = a->scale; p.out = a->out; p.out_stride = a->out_stride_t;
+  if (!units_of(p)) return LLC_E_SHAPE;
+  if ((a->flags & LLC_FLAG_DRY_RUN) != 0) return LLC_OK;
+  hipStream_t st = (hipStream_t)a->stream;
+  return between_events(a->ev_begin, a->ev_end, st, [&] {
+    return by_group(a->group, [&](auto group) {
+      return by_type(a->scales_dtype, [&](auto scale) {
+        return by_type(a->out_dtype, [&](auto to) {
+          embed_quantized_kernel<decltype(group)::value, decltype(scale), decltype(to)><<<unit_blocks(p), kBlock, 0, st>>>(p);
+          return hipGetLastError();
+        });
+      });
+    });
+  });
+}
+
+extern "C" int llc_matvec_quantized(const llc_matvec_quantized_args *a) {
+  if (a == nullptr) return LLC_E_NULL;
+  if (a->R < 0 || a->R > (1LL << 20) || a->N < 1 || a->N > kMaxIndex || a->D < 1 || a->D > (1LL << 27)) return LLC_E_SHAPE;
+  if ((a->flags & ~LLC_FLAG_DRY_RUN) != 0 || !known_group(a->group)) return LLC_E_OPTION;
+  if (a->R == 0) return LLC_OK;
+  if (a->x == nullptr || a->out == nullptr) return LLC_E_NULL;
+  const int bad = check_layer(a->N, a->D, a->group, a->codes, a->codes_stride_n, a->scales, a->scales_dtype, a->scales_stride_n, a->zeros, a->zeros_stride_n);
+  if (bad != LLC_OK) return bad;
+  if (a->x_stride_r < 0 || a->out_stride_r < a->N) return LLC_E_SHAPE;
+  if (!known_type(a->dtype) || !known_type(a->out_dtype)) return LLC_E_DTYPE;
+  if (!fits(a->x, type_size(a->dtype)) || !fits(a->out, type_size(a->out_dtype))) return LLC_E_ALIGN;
+  MatvecParams p = {};
+  p.R = a->R; p.N = a->N; p.D = a->D; p.x = a->x; p.x_stride = a->x_stride_r;
+  p.codes = a->codes; p.codes_stride = a->codes_stride_n; p.scales = a->scales; p.scales_stride = a->scales_stride_n;
+  p.zeros = a->zeros; p.zeros_stride = a->zeros_stride_n; p.out = a->out; p.out_stride = a->out_stride_r; p.out_type = a->out_dtype;
+  p.groups = (int)groups_of(a->D, a->group);
+  p.slabs = (int)((a->D + 127) / 128);
+  const int rows = (int)(a->R < kMatvecRows ? a->R : kMatvecRows), tiles = (rows + 15) / 16, parts = a->dtype == LLC_F32 ? 3 : 1;
+  const long long column_tiles = (a->N + 15) / 16;
+  // Few columns: wavefronts share a tile by its columns until some 2048 of them are at work, eight a CU.
+  constexpr int waves = kMatvecThreads / 64;
+  constexpr size_t kXBytes = 64 << 10;  // of LDS for x
+  long long most = (long long)(kXBytes / matvec_x_bytes(parts, rows, 1));
+  if (most < 1) most = 1;
+  while (p.share_log < 3 && (column_tiles << p.share_log) < 2048 && (2 << p.share_log) <= p.slabs && (2 << p.share_log) <= most) ++p.share_log;
+  const long long wanted = (p.slabs + (1 << p.share_log) - 1) >> p.share_log << p.share_log;
+  most = most >> p.share_log << p.share_log;
+  p.chunk_slabs = (int)(wanted < most ? wanted : most);
+  const int each = waves >> p.share_log;
+  p.tile_blocks = (unsigned)((column_tiles + each - 1) / each);
+  const size_t lds = matvec_x_bytes(parts, rows, p.chunk_slabs) + matvec_sum_bytes(tiles, a->group, p.chunk_slabs) + matvec_join_bytes(tiles, waves, p.share_log);
+  const unsigned passes = (unsigned)((a->R + kMatvecRows - 1) / kMatvecRows);
+  const dim3 grid(p.tile_blocks < 1024 ? p.tile_blocks : 1024, passes);
+  if ((a->flags & LLC_FLAG_DRY_RUN) != 0) return LLC_OK;
+  hipStream_t st = (hipStream_t)a->stream;
+  return between_events(a->ev_begin, a->ev_end, st, [&] {
+    return a->dtype == LLC_F32 ? launch_matvec_f32(p, tiles, a->group, a->scales_dtype, grid, waves * 64, lds, st)
+                               : launch_matvec_bf16(p, tiles, a->group, a->scales_dtype, grid, waves * 64, lds, st);
+  });
+}

@@ -1,0 +1,103 @@
+"""Host-side checks of the calls at a drafting step's end: struct layout and argument errors (no GPU)."""
+import ctypes
+import os
+import subprocess
+
+import pytest
+import torch
+
+import paper_2506_05632_amd as llc
+from paper_2506_05632_amd import binding
+
+ROOT = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
+STRUCTS = {"llc_sample_args": binding.SampleArgs, "llc_truncate_args": binding.TruncateArgs, "llc_quantize_args": binding.QuantizeArgs,
+           "llc_embed_quantized_args": binding.EmbedQuantizedArgs, "llc_matvec_quantized_args": binding.MatvecQuantizedArgs}
+
+
+def test_every_field_lies_where_the_binding_has_it(tmp_path):
+    lines = []
+    for name, struct in STRUCTS.items():
+        lines.append(f'printf("%zu\\n", sizeof({name}));')
+        lines += [f'printf("%zu\\n", offsetof({name}, {field}));' for field, _ in struct._fields_]
+    src = tmp_path / "layout.c"
+    src.write_text('#include <stdio.h>\n#include <stddef.h>\n#include "llc.h"\nint main(void){\n' + "\n".join(lines) + "\nreturn 0;}\n")
+    exe = tmp_path / "layout"
+    subprocess.run(["gcc", "-std=c99", "-Wall", "-Werror", "-pedantic", "-I", os.path.join(ROOT, "include"), str(src), "-o", str(exe)], check=True)
+    got = [int(v) for v in subprocess.run([str(exe)], capture_output=True, text=True, check=True).stdout.split()]
+    want = []
+    for struct in STRUCTS.values():
+        want += [ctypes.sizeof(struct)] + [getattr(struct, field).offset for field, _ in struct._fields_]
+    assert got == want
+
+
+def _code(name, base, kw):
+    a = STRUCTS[name + "_args"]()
+    for k, v in {**base, **kw}.items():
+        setattr(a, k, v)
+    return getattr(llc.load(), name)(ctypes.byref(a))
+
+
+CUT = dict(R=4, V=64, dtype=0, kind=0, x=0x1000, stride_r=64, temp=1.0, top_p=1.0, min_p=0.0, top_k=0)
+BAD_CUTS = [(dict(x=None), -1), (dict(R=-1), -2), (dict(R=1 << 24), -2), (dict(V=0), -2), (dict(V=(1 << 31) - 4), -2), (dict(stride_r=-1), -2),
+            (dict(temp=0.0), -3), (dict(temp=1e-39), -3), (dict(temp=float("inf")), -3), (dict(temp=float("nan")), -3),
+            (dict(dtype=2), -4), (dict(kind=1), -4), (dict(kind=3), -4), (dict(x=0x1002), -5), (dict(row_temp=0x1001), -5), (dict(row_top_k=0x1002), -5),
+            (dict(kept=0x1002), -5), (dict(top_p=0.0), -8), (dict(top_p=1.1), -8), (dict(top_p=float("nan")), -8), (dict(min_p=-0.1), -8), (dict(min_p=1.5), -8),
+            (dict(min_p=float("nan")), -8), (dict(top_k=-1), -8), (dict(flags=1), -8), (dict(flags=4), 0), (dict(flags=4, kind=2, temp=0.0), 0),
+            (dict(flags=4, row_temp=0x3000, temp=0.0), 0), (dict(flags=4, row_top_p=0x3000, top_p=0.0), 0), (dict(flags=4, row_min_p=0x3000, min_p=9.0), 0),
+            (dict(flags=4, row_top_k=0x3000, top_k=-9), 0), (dict(R=0, x=None), 0), (dict(flags=4, R=(1 << 24) - 1, V=(1 << 31) - 5), 0)]
+
+
+@pytest.mark.parametrize("kw,code", BAD_CUTS + [
+    (dict(u=None), -1), (dict(tokens=None), -1), (dict(S=-1), -2), (dict(S=65536), -2), (dict(u_stride_r=-1), -2), (dict(u=0x2001), -5), (dict(tokens=0x2002), -5),
+    (dict(logp=0x2002), -5), (dict(flags=4, S=0, u=None, tokens=None), 0)])
+def test_sample_arguments(kw, code):
+    assert _code("llc_sample", dict(CUT, S=2, u=0x2000, u_stride_r=2, tokens=0x4000), kw) == code
+    assert llc.load().llc_sample(None) == -1
+
+
+@pytest.mark.parametrize("kw,code", BAD_CUTS + [
+    (dict(out=None), -1), (dict(out_stride_r=63), -2), (dict(out=0x5002), -5), (dict(out=0x1000, out_stride_r=65), -2), (dict(flags=4, out=0x1000), 0)])
+def test_truncate_arguments(kw, code):
+    assert _code("llc_truncate", dict(CUT, out=0x5000, out_stride_r=max(64, kw.get("V", 64))), kw) == code
+    assert llc.load().llc_truncate(None) == -1
+
+
+LAYER = dict(N=10, D=100, group=32, scales_dtype=1, codes=0x1001, codes_stride_n=50, scales=0x2000, scales_stride_n=4, zeros=0x3001, zeros_stride_n=4)
+BAD_LAYERS = [(dict(codes=None), -1), (dict(scales=None), -1), (dict(D=0), -2), (dict(codes_stride_n=49), -2), (dict(scales_stride_n=3), -2), (dict(zeros_stride_n=3), -2),
+              (dict(D=101), -2), (dict(group=16), -8), (dict(group=0), -8), (dict(group=256), -8), (dict(scales_dtype=2), -4), (dict(scales=0x2001), -5), (dict(flags=2), -8),
+              (dict(flags=4), 0), (dict(flags=4, zeros=None, zeros_stride_n=0), 0), (dict(flags=4, group=128, scales_stride_n=1, zeros_stride_n=1), 0)]
+
+
+@pytest.mark.parametrize("kw,code", BAD_LAYERS + [
+    (dict(w=None), -1), (dict(N=-1), -2), (dict(N=1 << 31), -2), (dict(D=(1 << 31) - 5, codes_stride_n=1 << 31, scales_stride_n=1 << 31, zeros_stride_n=1 << 31, N=1 << 20), -2),
+    (dict(w_stride_n=-1), -2), (dict(dtype=5), -4), (dict(w=0x4002), -5), (dict(N=0, w=None), 0), (dict(flags=4, dtype=1, w=0x4002), 0)])
+def test_quantize_arguments(kw, code):
+    assert _code("llc_quantize", dict(LAYER, dtype=0, w=0x4000, w_stride_n=100), kw) == code
+    assert llc.load().llc_quantize(None) == -1
+
+
+@pytest.mark.parametrize("kw,code", BAD_LAYERS + [
+    (dict(tokens=None), -1), (dict(out=None), -1), (dict(T=-1), -2), (dict(N=0), -2), (dict(tok_stride=-1), -2), (dict(out_stride_t=99), -2), (dict(out_dtype=3), -4),
+    (dict(out=0x6002), -5), (dict(tokens=0x5002), -5), (dict(scale=float("nan")), -8), (dict(T=0, tokens=None), 0)])
+def test_embed_arguments(kw, code):
+    assert _code("llc_embed_quantized", dict(LAYER, T=3, out_dtype=0, tokens=0x5000, tok_stride=1, scale=1.0, out=0x6000, out_stride_t=100), kw) == code
+    assert llc.load().llc_embed_quantized(None) == -1
+
+
+@pytest.mark.parametrize("kw,code", BAD_LAYERS + [
+    (dict(x=None), -1), (dict(out=None), -1), (dict(R=-1), -2), (dict(R=(1 << 20) + 1), -2), (dict(N=0), -2), (dict(D=(1 << 27) + 1), -2), (dict(x_stride_r=-1), -2),
+    (dict(out_stride_r=9), -2), (dict(dtype=2), -4), (dict(out_dtype=-1), -4), (dict(x=0x7002), -5), (dict(out=0x6002), -5), (dict(R=0, x=None), 0),
+    (dict(flags=4, R=1 << 20), 0), (dict(flags=4, N=(1 << 31) - 5, out_stride_r=1 << 31), 0),
+    (dict(flags=4, D=1 << 27, codes_stride_n=1 << 26, scales_stride_n=1 << 22, zeros_stride_n=1 << 22), 0)])
+def test_matvec_arguments(kw, code):
+    assert _code("llc_matvec_quantized", dict(LAYER, R=3, dtype=0, out_dtype=0, x=0x7000, x_stride_r=100, out=0x6000, out_stride_r=10), kw) == code
+    assert llc.load().llc_matvec_quantized(None) == -1
+
+
+def test_the_binding_refuses_tensors_of_the_host():
+    x, u = torch.zeros(2, 8), torch.zeros(2)
+    codes, scales = torch.zeros(3, 4, dtype=torch.uint8), torch.zeros(3, 1)
+    for call in (lambda: llc.llc_sample(x, u), lambda: llc.llc_truncate(x), lambda: llc.llc_quantize(x), lambda: llc.llc_matvec_quantized(x, codes, scales),
+                 lambda: llc.llc_embed_quantized(codes, scales, torch.zeros(2, dtype=torch.int32), 8)):
+        with pytest.raises(ValueError):
+            call()
