@@ -1,28 +1,34 @@
 // Sampling from a cut distribution with given random numbers, and the cut rows themselves.
 //
 // The kept entries of a row are a run of its entries in the order of their values (larger first, equal ones by index), so a
-// cut is a place of that order: the key of its last entry and that entry's index.  A workgroup takes a row.
-//   1. The largest entry, and with it every thread's own.
-//   2. A bound that the cut cannot be below, from the threads' largest entries (the k-th largest of them has k entries at or above it) or from
-//      min_p; what is at or above it goes into a list, in the order of the indexes.  In the same pass, where a share of the whole mass is asked for, the mass.
+// cut is a place of that order: the key of its last entry and that entry's index.  A workgroup takes a row, two are at work on a CU, and
+// most rows are read once:
+//   1. Each wavefront's first entries are a sample of the row.  A value that the sample has often enough above it, or min_p's from the sample's largest,
+//      bounds a list of entries that is likely to hold the kept ones.
+//   2. The rest of the row goes by: its largest, the list, in the order of the indexes, and, where a share of the whole mass is
+//      asked for, or no cut at all, the masses.
 //   3. The list is sorted, its masses are summed along the order, and the cut is read off; the tokens follow from sums along the indexes.
-// Rows whose kept entries the list does not hold are narrowed down instead: a histogram of the masses (or counts) by value finds the range that the cut is
-// in, histograms by the keys' bits find the key, and a count of its equals the index; tokens follow from the sums of tiles of the row.
+// Rows whose kept entries the list turns out not to hold are narrowed down instead: a histogram of the masses (or counts) by value finds the range that the
+// cut is in, a list of that range's entries the place (histograms by the keys' bits, where they are too many), and tokens follow from the sums of tiles of the row.
 //
-// Masses are exp((x - largest) / temp) in fp64: a border in a run of 128 000 entries that share the mass is hit by rounding otherwise.  Histograms add them as whole numbers,
-// whose sum does not depend on the order.
+// Masses are exp((x - reference) / temp) in fp64: a border in a run of 128 000 entries that share the mass is hit by rounding otherwise.  (An fp64 multiply-add takes
+// as long as one in fp32 here; an entry takes some 23 operations, which at 128 256 entries is 19 us of a CU and about what its share of the memory takes for rows
+// in bf16.)  Histograms add masses as whole numbers, whose sum does not depend on the order.
 #include "ends.hpp"
 
 namespace llc {
 namespace {
 
-constexpr int kThreads = 1024, kWaves = kThreads / 64;
+constexpr int kThreads = 512, kWaves = kThreads / 64;
 constexpr int kList = 2048;       // entries of the list
-constexpr int kBuckets = 2048;    // of a histogram
+constexpr int kBuckets = 4096;    // of a histogram
+constexpr int kBucketsLog = 12;
 constexpr int kMostTiles = 2048;  // of a row, whose masses LDS holds
 constexpr int kPiece = 512;       // entries that a wavefront takes at a time, eight a lane
-constexpr int kByMass = 192;      // threads' largest entries that bound the list where a share of the mass is asked for
-constexpr int kByCount = 512;     // top_k up to which the list is tried
+template <typename E> constexpr int kAhead = 8 / sizeof(E);  // pieces that it asks for together: 64 bytes a lane
+constexpr int kSample = 2;        // pieces of a wavefront that the sample has
+constexpr int kByMass = 256;      // entries that the list aims at where a share of the mass is asked for
+constexpr int kByCount = 1200;    // top_k up to which the list is tried
 constexpr unsigned kMostRowBlocks = 1u << 20;
 
 struct CutParams {
@@ -71,33 +77,33 @@ __device__ __forceinline__ Cut cut_of(const CutParams &p, long long r) {
   return c;
 }
 
-// Values as whole numbers in their order; both zeros are one.  A distance is the largest one's less the value's.
+// Values as whole numbers in their order, the largest first; both zeros are one.
 __device__ __forceinline__ uint32_t key_of(float x) {
   const uint32_t u = __float_as_uint(x + 0.0f);
-  return u ^ ((uint32_t)((int32_t)u >> 31) | 0x80000000u);
+  return u ^ ((uint32_t)~((int32_t)u >> 31) & 0x7FFFFFFFu);
 }
-__device__ __forceinline__ float value_of(uint32_t key) { return __uint_as_float((key & 0x80000000u) != 0 ? key ^ 0x80000000u : ~key); }
+__device__ __forceinline__ float value_of(uint32_t key) { return __uint_as_float((key & 0x80000000u) != 0 ? key : key ^ 0x7FFFFFFFu); }
+constexpr uint32_t kLastKey = 0xFF7FFFFFu;  // of the least finite number
 __device__ __forceinline__ bool has_mass(float x) { return fabsf(x) < INFINITY; }
 
-// 2^t for t <= 0, to some 2^-50 of it; 0 below 2^-1000.
-__device__ __forceinline__ double exp2_down(double t) {
-  const double whole = rint(t), f = (t - whole) * 0.6931471805599453;
-  double y = 1.0 / 479001600.0;  // exp(f), |f| <= 0.35, by its series: f^13 / 13! is 2e-16
-  y = fma(y, f, 1.0 / 39916800.0);
-  y = fma(y, f, 1.0 / 3628800.0);
-  y = fma(y, f, 1.0 / 362880.0);
-  y = fma(y, f, 1.0 / 40320.0);
-  y = fma(y, f, 1.0 / 5040.0);
-  y = fma(y, f, 1.0 / 720.0);
-  y = fma(y, f, 1.0 / 120.0);
-  y = fma(y, f, 1.0 / 24.0);
-  y = fma(y, f, 1.0 / 6.0);
-  y = fma(y, f, 0.5);
+// 2^t, to some 2^-51 of it (the polynomial of degree ten through the Chebyshev points of [-1/2, 1/2]; at 0 it is 1); 0 for -inf.
+__device__ __forceinline__ double exp2_of(double t) {
+  t = fmax(t, -1200.0);
+  const double whole = rint(t), f = t - whole;
+  double y = 7.072585949269224e-09;
+  y = fma(y, f, 1.0208690299958306e-07);
+  y = fma(y, f, 1.321544258792169e-06);
+  y = fma(y, f, 1.5252657260200837e-05);
+  y = fma(y, f, 0.0001540353044173605);
+  y = fma(y, f, 0.0013333558230164974);
+  y = fma(y, f, 0.009618129107606888);
+  y = fma(y, f, 0.05550410866444772);
+  y = fma(y, f, 0.24022650695910097);
+  y = fma(y, f, 0.69314718055995);
   y = fma(y, f, 1.0);
-  y = fma(y, f, 1.0);
-  return t > -1000.0 ? ldexp(y, (int)whole) : 0.0;
+  return ldexp(y, (int)whole);
 }
-__device__ __forceinline__ double mass_of(float x, double top, double scale) { return exp2_down(((double)x - top) * scale); }
+__device__ __forceinline__ double mass_of(float x, double reference, double scale) { return exp2_of(((double)x - reference) * scale); }
 
 // Sums over a workgroup and along its threads.
 __device__ __forceinline__ double wave_sum(double v) {
@@ -117,28 +123,31 @@ template <typename T> __device__ __forceinline__ T wave_scan(T v, int lane) {  /
 struct Shared {
   union {
     unsigned long long histogram[kBuckets];
-    unsigned long long sorted[kList];  // distance and index
-    double along[kMostTiles > kList ? kMostTiles : kList];  // masses summed along the indexes
+    struct {
+      unsigned long long sorted[kList];  // key and index
+      double masses[kList];              // summed along the order
+    };
   };
-  double masses[kList];  // summed along the order
-  uint32_t list_distance[kList];
+  double along[kMostTiles];              // masses summed along the indexes: of the list's entries, or of tiles
+  uint32_t list_key[kList];
   int list_index[kList];
-  float largest[kThreads];
+  uint32_t sample[kThreads];             // a histogram of the sample's largest
   union {
     double wave_double[kWaves];
     unsigned long long wave_whole[kWaves];
   };
-  int wave_count[kWaves + 1];
-  float wave_float[kWaves];
+  int wave_count[kWaves];
+  float wave_high[kWaves], wave_low[kWaves];
   int overflow;
   unsigned long long pick_above;
   int pick;
   long long pick_index;
 };
+static_assert(kMostTiles >= kList, "sums of the list's entries go where tiles' go");
 
 // Over the threads' values: the sum of those before, and of all.
 template <typename T> __device__ __forceinline__ T block_scan_before(T v, T *s_wave, T &all) {
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const T upto = wave_scan(v, lane);
   __syncthreads();
   if (lane == 63) s_wave[wave] = upto;
@@ -157,64 +166,174 @@ template <typename T> __device__ __forceinline__ T block_sum(T v, T *s_wave) {
   return all;
 }
 
-// A row's entries as a wavefront has them: `f(index of the first, its eight)` for its pieces in turn; those behind the row's end are -inf.
-template <typename E> __device__ __forceinline__ void load_piece(const E *row, long long at, long long V, float (&v)[8]) {
+// A row's entries as a wavefront has them: `f(index of the first, its eight)` for its pieces in turn, from piece `skip` on; those behind the row's end,
+// and those without mass, are -inf.
+// A lane's entries of a piece as they lie in memory.
+template <typename E> struct Raw;
+template <> struct Raw<float> { float4_any a, b; };
+template <> struct Raw<uint16_t> { word4_any a; };
+template <typename E> __device__ __forceinline__ Raw<E> load_raw(const E *row, long long at, long long V) {
+  Raw<E> r;
   if (at + 8 <= V) {
-    load_some<8>(row + at, v);
+    r.a = *reinterpret_cast<const decltype(r.a) *>(row + at);
+    if constexpr (sizeof(E) == 4) r.b = *reinterpret_cast<const decltype(r.b) *>(row + at + 4);
+  } else if constexpr (sizeof(E) == 4) {
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      r.a[j] = at + j < V ? row[at + j] : -INFINITY;
+      r.b[j] = at + j + 4 < V ? row[at + j + 4] : -INFINITY;
+    }
   } else {
 #pragma unroll
-    for (int j = 0; j < 8; ++j) v[j] = at + j < V ? widen(row[at + j]) : -INFINITY;
+    for (int j = 0; j < 4; ++j)
+      r.a[j] = (at + 2 * j < V ? row[at + 2 * j] : 0xFF80u) | (uint32_t)(at + 2 * j + 1 < V ? row[at + 2 * j + 1] : 0xFF80u) << 16;
+  }
+  return r;
+}
+template <typename E> __device__ __forceinline__ void widen_raw(const Raw<E> &r, float (&v)[8]) {
+#pragma unroll
+  for (int j = 0; j < 4; ++j) {
+    if constexpr (sizeof(E) == 4) {
+      v[j] = r.a[j]; v[j + 4] = r.b[j];
+    } else {
+      split_pair(r.a[j], v[2 * j], v[2 * j + 1]);
+    }
   }
 }
-template <typename E, typename F> __device__ __forceinline__ void each_piece(const E *row, const CutParams &p, int wave, int lane, F f) {
-  constexpr int kAhead = 4;
-  const long long first = (long long)wave * p.tiles_wave * p.pieces_tile * kPiece;
-  const long long last0 = first + (long long)p.tiles_wave * p.pieces_tile * kPiece, last = last0 < p.V ? last0 : p.V;
-  for (long long at = first; at < last; at += kAhead * kPiece) {  // (uniform)
-    float v[kAhead][8];
+template <typename E> __device__ __forceinline__ void load_piece(const E *row, long long at, long long V, float (&v)[8]) { widen_raw(load_raw(row, at, V), v); }
+__device__ __forceinline__ void drop_massless(float (&v)[8]) {
 #pragma unroll
-    for (int i = 0; i < kAhead; ++i)
-      if (at + i * kPiece < last) load_piece(row, at + i * kPiece + lane * 8, p.V, v[i]);
+  for (int j = 0; j < 8; ++j) v[j] = has_mass(v[j]) ? v[j] : -INFINITY;
+}
+struct Part {
+  long long first, last;  // entries of a wavefront
+};
+__device__ __forceinline__ Part part_of(const CutParams &p, int wave) {
+  const long long each = (long long)p.tiles_wave * p.pieces_tile * kPiece, first = wave * each, last = first + each;
+  return {first < p.V ? first : p.V, last < p.V ? last : p.V};
+}
+template <typename E, typename F> __device__ __forceinline__ void each_piece(const E *row, const CutParams &p, Part part, int lane, int skip, F f) {
+  constexpr int kTurn = kAhead<E>;
+  for (long long at = part.first + skip * kPiece; at < part.last; at += kTurn * kPiece) {  // (uniform)
+    Raw<E> raw[kTurn];
 #pragma unroll
-    for (int i = 0; i < kAhead; ++i)
-      if (at + i * kPiece < last) f(at + i * kPiece + lane * 8, v[i]);
+    for (int i = 0; i < kTurn; ++i)
+      if (at + i * kPiece < part.last) raw[i] = load_raw(row, at + i * kPiece + lane * 8, p.V);
+#pragma unroll
+    for (int i = 0; i < kTurn; ++i)
+      if (at + i * kPiece < part.last) {
+        float v[8];
+        widen_raw(raw[i], v);
+        drop_massless(v);
+        f(at + i * kPiece + lane * 8, v);
+        __builtin_amdgcn_sched_barrier(0);  // (pieces side by side would take more registers than there are)
+      }
   }
+}
+// The masses of a lane's entries, four at a time for the same reason.
+template <typename F> __device__ __forceinline__ double mass_of_eight(F value, double reference, double scale) {
+  double sum = 0.0;
+#pragma unroll
+  for (int h = 0; h < 8; h += 4) {
+    double m[4];
+#pragma unroll
+    for (int j = 0; j < 4; ++j) m[j] = mass_of(value(h + j), reference, scale);
+    sum += (m[0] + m[1]) + (m[2] + m[3]);
+    __builtin_amdgcn_sched_barrier(0);
+  }
+  return sum;
 }
 
-// The least bound that at least `n` of the threads' largest entries reach (-inf where fewer have one): to a bf16 number's bits, downwards.
-__device__ __forceinline__ float bound_of(const float *largest, int n) {
-  const int lane = threadIdx.x & 63;
-  uint32_t key[kThreads / 64];
+// The lanes before, and those of all: how many entries are marked.
+__device__ __forceinline__ int marked_before(const bool (&hit)[8], int &all) {
+  int before = 0;
+  all = 0;
 #pragma unroll
-  for (int i = 0; i < kThreads / 64; ++i) key[i] = has_mass(largest[i * 64 + lane]) ? key_of(largest[i * 64 + lane]) : 0u;
-  uint32_t bound = 0;
-  for (uint32_t bit = 0x80000000u; bit >= 0x8000u; bit >>= 1) {
-    const uint32_t to = bound | bit;
-    int count = 0;
-#pragma unroll
-    for (int i = 0; i < kThreads / 64; ++i) count += __popcll(__ballot(key[i] >= to));
-    if (count >= n) bound = to;
+  for (int j = 0; j < 8; ++j) {
+    const unsigned long long m = __ballot(hit[j]);
+    before = __builtin_amdgcn_mbcnt_hi((uint32_t)(m >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)m, before));
+    all += __popcll(m);
   }
-  return bound <= 0x007FFFFFu ? -INFINITY : value_of(bound);  // (keys of numbers begin above)
+  return before;
 }
 
-// The place of the order where the weights' sum reaches `target`: a whole number's histogram by values, then by keys.  Entries behind `distance` (and,
-// at it, behind `index`) take no part.  weight(x): the entry's, a whole number.
+// The list: each wavefront's entries in a part of its own, in the order of their indexes.
+struct Lister {
+  int room, count;
+  __device__ __forceinline__ void add(Shared &s, int wave, long long at, const float (&v)[8], const bool (&hit)[8], bool any) {
+    if (__ballot(any) == 0) return;
+    int all, to = count + marked_before(hit, all);
+#pragma unroll
+    for (int j = 0; j < 8; ++j)
+      if (hit[j]) {
+        if (to < room) { s.list_key[wave * room + to] = key_of(v[j]); s.list_index[wave * room + to] = (int)(at + j); }
+        ++to;
+      }
+    count += all;
+  }
+};
+__device__ __forceinline__ int room_of(const CutParams &p) {
+  const int waves = (p.tiles + p.tiles_wave - 1) / p.tiles_wave;  // at work
+  return kList / (waves <= 1 ? 1 : waves <= 2 ? 2 : waves <= 4 ? 4 : 8);
+}
+// The wavefronts' parts to one run; false where one did not hold its entries.  The run is in `sorted` too, not sorted yet.
+__device__ __forceinline__ bool join_list(Shared &s, const Lister &l, int lane, int wave, int &n) {
+  __syncthreads();
+  if (lane == 0) s.wave_count[wave] = l.count;
+  __syncthreads();
+  int before = 0;
+  bool whole = true;
+  n = 0;
+#pragma unroll
+  for (int w = 0; w < kWaves; ++w) {
+    const int c = s.wave_count[w];
+    if (w < wave) before += c;
+    n += c;
+    whole = whole && c <= l.room;
+  }
+  if (!whole) return false;
+  for (int e = lane; e < l.count; e += 64) s.sorted[before + e] = (unsigned long long)s.list_key[wave * l.room + e] << 32 | (unsigned)s.list_index[wave * l.room + e];
+  __syncthreads();
+  for (int e = threadIdx.x; e < n; e += kThreads) { s.list_key[e] = (uint32_t)(s.sorted[e] >> 32); s.list_index[e] = (int)(unsigned)s.sorted[e]; }
+  __syncthreads();
+  return true;
+}
+// Sorts the run: pairs at a distance below 128 are one wavefront's, whose steps follow each other without waiting for others.
+__device__ __forceinline__ void sort_list(Shared &s, int n) {
+  int size = 2;
+  while (size < n) size <<= 1;
+  for (int e = n + threadIdx.x; e < size; e += kThreads) s.sorted[e] = ~0ULL;
+  __syncthreads();
+  for (int run = 2; run <= size; run <<= 1)
+    for (int gap = run >> 1; gap > 0; gap >>= 1) {
+      for (int t = threadIdx.x; t < size / 2; t += kThreads) {
+        const int a = 2 * t - (t & (gap - 1)), b = a + gap;
+        const unsigned long long va = s.sorted[a], vb = s.sorted[b];
+        if ((va > vb) == ((a & run) == 0)) { s.sorted[a] = vb; s.sorted[b] = va; }
+      }
+      if (gap > 64 || (gap == 1 && run >= 128)) __syncthreads();  // (the next step's pairs may be others')
+      else __builtin_amdgcn_wave_barrier();
+    }
+  __syncthreads();
+}
+
+// The place of the order where the weights' sum reaches `target`: a whole number's histogram by values, then the entries of the bucket.
 struct Place {
-  uint32_t distance;  // of the last entry
+  uint32_t key;     // of the last entry
   long long index;
 };
 __device__ __forceinline__ int bucket_of(float x, float top, float per) {
   const float at = (top - x) * per;  // (both roundings keep the order; an infinite `per` gives NaN at the top itself, and that 0)
   return at >= (float)(kBuckets - 1) ? kBuckets - 1 : (int)fmaxf(at, 0.0f);
 }
-// The bucket where the sum of those up to it reaches `target`; -1: none.  `above`: the sum of those before.
-__device__ __forceinline__ int pick_bucket(Shared &s, unsigned long long target, unsigned long long &above) {
+// The bucket where the sum of those up to it reaches `target(sum of all)`; -1: none.  `above`: the sum of those before.
+template <typename T> __device__ __forceinline__ int pick_bucket(Shared &s, T target_of, unsigned long long &target, unsigned long long &above) {
   constexpr int kEach = kBuckets / kThreads;
   unsigned long long mine = 0, all;
 #pragma unroll
   for (int i = 0; i < kEach; ++i) mine += s.histogram[threadIdx.x * kEach + i];
   unsigned long long before = block_scan_before(mine, s.wave_whole, all);
+  target = target_of(all);
   if (threadIdx.x == 0) s.pick = -1;
   __syncthreads();
   if (before < target && before + mine >= target) {
@@ -231,41 +350,81 @@ __device__ __forceinline__ int pick_bucket(Shared &s, unsigned long long target,
   __syncthreads();
   return pick;
 }
-template <typename E, typename W>
-__device__ __forceinline__ bool narrow_down(const E *row, const CutParams &p, Shared &s, float top, double temp, unsigned long long target, W weight, Place &place) {
+// Entries behind `until` take no part.  weight(x): the entry's, a whole number; target_of(sum of all).  False: the sum of all does not reach the target.
+template <typename E, typename W, typename T>
+__device__ __forceinline__ bool narrow_down(const E *row, const CutParams &p, Shared &s, Part part, float top, double temp, Place until, W weight, T target_of, Place &place) {
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const uint32_t top_key = key_of(top);
-  const float per = 64.0f / (float)temp;
-  uint32_t low = 0, high = top_key - key_of(-3.4028234663852886e38f);
-  unsigned long long above = 0;
-  for (int level = 0; low < high; ++level) {
+  const float per = 128.0f / (float)temp;  // (the last bucket has what is 32 units of ln and more below the top)
+  uint32_t low = key_of(top), high = kLastKey;
+  unsigned long long above = 0, target = 0;
+  const auto inside = [&](uint32_t key, long long i) { return key < until.key || (key == until.key && i <= until.index); };
+  for (int level = 0; level == 0 || low < high; ++level) {
     const uint32_t span = high - low;
-    const int shift = span >= kBuckets ? 32 - __builtin_clz(span) - 11 : 0;
+    const int shift = span >= kBuckets ? 32 - __builtin_clz(span) - kBucketsLog : 0;
+    if (level > 0) {  // few entries: sorted, they show the place
+      Lister list = {room_of(p), 0};
+      each_piece(row, p, part, lane, 0, [&](long long at, const float (&v)[8]) {
+        bool hit[8], any = false;
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+          const uint32_t key = key_of(v[j]);
+          hit[j] = key >= low && key <= high && inside(key, at + j);
+          any = any || hit[j];
+        }
+        list.add(s, wave, at, v, hit, any);
+      });
+      int n;
+      if (join_list(s, list, lane, wave, n)) {
+        sort_list(s, n);
+        constexpr int kEach = kList / kThreads;
+        const int e0 = threadIdx.x * kEach;
+        unsigned long long w[kEach], mine = 0, all;
+#pragma unroll
+        for (int i = 0; i < kEach; ++i) {
+          w[i] = e0 + i < n ? weight(value_of((uint32_t)(s.sorted[e0 + i] >> 32))) : 0;
+          mine += w[i];
+        }
+        unsigned long long before = above + block_scan_before(mine, s.wave_whole, all);
+        if (threadIdx.x == 0) s.pick = n - 1;
+        __syncthreads();
+#pragma unroll
+        for (int i = 0; i < kEach; ++i) {
+          if (before < target && before + w[i] >= target) s.pick = e0 + i;
+          before += w[i];
+        }
+        __syncthreads();
+        const unsigned long long last = s.sorted[s.pick];
+        place.key = (uint32_t)(last >> 32);
+        place.index = (int)(unsigned)last;
+        __syncthreads();
+        return true;
+      }
+    }
     __syncthreads();
     for (int i = threadIdx.x; i < kBuckets; i += kThreads) s.histogram[i] = 0;
     __syncthreads();
-    each_piece(row, p, wave, lane, [&](long long, const float (&v)[8]) {
+    each_piece(row, p, part, lane, 0, [&](long long at, const float (&v)[8]) {
 #pragma unroll
       for (int j = 0; j < 8; ++j) {
-        if (!has_mass(v[j])) continue;
-        const uint32_t distance = top_key - key_of(v[j]);
-        if (distance < low || distance > high) continue;
-        const int bucket = level == 0 ? bucket_of(v[j], top, per) : (int)((distance - low) >> shift);
+        const uint32_t key = key_of(v[j]);
+        if (key < low || key > high || !inside(key, at + j)) continue;
+        const int bucket = level == 0 ? bucket_of(v[j], top, per) : (int)((key - low) >> shift);
         const unsigned long long w = weight(v[j]);
         if (w != 0) atomicAdd(&s.histogram[bucket], w);
       }
     });
     __syncthreads();
     unsigned long long before;
-    const int bucket = pick_bucket(s, target - above, before);
+    const int bucket = level == 0 ? pick_bucket(s, target_of, target, before) : pick_bucket(s, [&](unsigned long long) { return target - above; }, target, before);
     if (bucket < 0) return false;
+    if (level > 0) target += above;
     above += before;
     if (level == 0) {  // the bucket's ends, by halving: the buckets follow the values
       const auto first_at_least = [&](int b) {
-        uint32_t a = low, z = high + 1;  // (the first distance whose bucket is b or more; distances end below 2^32 - 1)
+        uint32_t a = low, z = high + 1;  // (the first key whose bucket is b or more; keys end below 2^32 - 1)
         while (a < z) {
           const uint32_t mid = a + (z - a) / 2;
-          if (bucket_of(value_of(top_key - mid), top, per) >= b) z = mid; else a = mid + 1;
+          if (bucket_of(value_of(mid), top, per) >= b) z = mid; else a = mid + 1;
         }
         return a;
       };
@@ -278,13 +437,12 @@ __device__ __forceinline__ bool narrow_down(const E *row, const CutParams &p, Sh
     }
   }
   // of the equals, as many as it takes
-  const unsigned long long each = weight(value_of(top_key - low));
-  unsigned long long count = each > 0 ? (target - above + each - 1) / each : 1;
+  const unsigned long long each = weight(value_of(low));
+  const unsigned long long count = each > 0 ? (target - above + each - 1) / each : 1;
   int equals = 0;
-  const auto is_equal = [&](float x) { return has_mass(x) && top_key - key_of(x) == low; };
-  each_piece(row, p, wave, lane, [&](long long, const float (&v)[8]) {
+  each_piece(row, p, part, lane, 0, [&](long long, const float (&v)[8]) {
 #pragma unroll
-    for (int j = 0; j < 8; ++j) equals += is_equal(v[j]) ? 1 : 0;
+    for (int j = 0; j < 8; ++j) equals += key_of(v[j]) == low ? 1 : 0;
   });
   for (int d = 1; d < 64; d <<= 1) equals += __shfl_xor(equals, d);
   __syncthreads();
@@ -294,20 +452,20 @@ __device__ __forceinline__ bool narrow_down(const E *row, const CutParams &p, Sh
   unsigned long long before = 0;
   for (int w = 0; w < wave; ++w) before += (unsigned)s.wave_count[w];
   if (before < count && before + (unsigned)equals >= count) {  // (uniform: this wavefront has the last)
-    each_piece(row, p, wave, lane, [&](long long at, const float (&v)[8]) {
-      int mine = 0;
+    each_piece(row, p, part, lane, 0, [&](long long at, const float (&v)[8]) {
+      bool hit[8];
 #pragma unroll
-      for (int j = 0; j < 8; ++j) mine += is_equal(v[j]) ? 1 : 0;
-      const int upto = wave_scan(mine, lane);
-      unsigned long long here = before + (unsigned)(upto - mine);
+      for (int j = 0; j < 8; ++j) hit[j] = key_of(v[j]) == low;
+      int all;
+      unsigned long long here = before + (unsigned)marked_before(hit, all);
 #pragma unroll
       for (int j = 0; j < 8; ++j)
-        if (is_equal(v[j]) && ++here == count) s.pick_index = at + j;
-      before += (unsigned)__shfl(upto, 63);
+        if (hit[j] && ++here == count) s.pick_index = at + j;
+      before += (unsigned)all;
     });
   }
   __syncthreads();
-  place.distance = low;
+  place.key = low;
   place.index = s.pick_index;
   __syncthreads();
   return true;
@@ -325,258 +483,304 @@ template <typename E, bool SAMPLE> __device__ __forceinline__ void write_none(co
   if (threadIdx.x == 0 && p.kept != nullptr) p.kept[r] = 0;
 }
 
+// A value that `wanted` of the threads' largest entries of the sample reach (-inf where fewer have one); top: the largest of them.
+__device__ __forceinline__ float bound_of(Shared &s, float mine, float top, float least, int wanted) {
+  const float per = (float)(kThreads - 1) / (top - least);
+  s.sample[threadIdx.x] = 0;
+  __syncthreads();
+  const int at = (int)fminf(fmaxf((top - mine) * per, 0.0f), (float)(kThreads - 1));
+  if (mine > -INFINITY) atomicAdd(&s.sample[at], 1u);
+  if (threadIdx.x == 0) s.pick = -1;
+  __syncthreads();
+  unsigned long long all;
+  const unsigned long long here = s.sample[threadIdx.x], before = block_scan_before(here, s.wave_whole, all);
+  if (before < (unsigned)wanted && before + here >= (unsigned)wanted) s.pick = threadIdx.x;
+  __syncthreads();
+  const int pick = s.pick;
+  // (a bucket further down than the one: what rounding has put there is above it)
+  return pick < 0 ? -INFINITY : top == least ? top : top - (float)(pick + 2) / per;
+}
+
 template <typename E, bool SAMPLE> __device__ __forceinline__ void cut_row(const CutParams &p, long long r, Shared &s) {
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const E *row = reinterpret_cast<const E *>(p.x) + r * p.stride;
   E *out = SAMPLE ? nullptr : reinterpret_cast<E *>(p.out) + r * p.out_stride;
+  const Part part = part_of(p, wave);
+  // 1. the sample
+  Raw<E> first[kSample];
+#pragma unroll
+  for (int i = 0; i < kSample; ++i) first[i] = load_raw(row, part.first + i * kPiece < part.last ? part.first + i * kPiece + lane * 8 : p.V, p.V);
   const Cut cut = cut_of(p, r);
-
-  // 1. the largest
-  float largest = -INFINITY;
-  each_piece(row, p, wave, lane, [&](long long, const float (&v)[8]) {
-#pragma unroll
-    for (int j = 0; j < 8; ++j) largest = fmaxf(largest, has_mass(v[j]) ? v[j] : -INFINITY);
-  });
-  __syncthreads();  // (the last row's)
-  s.largest[threadIdx.x] = largest;
-#pragma unroll
-  for (int d = 1; d < 64; d <<= 1) largest = fmaxf(largest, __shfl_xor(largest, d));
-  if (lane == 0) s.wave_float[wave] = largest;
-  if (threadIdx.x == 0) s.overflow = 0;
-  __syncthreads();
-  float top = -INFINITY;
-  for (int w = 0; w < kWaves; ++w) top = fmaxf(top, s.wave_float[w]);
-  if (cut.bad || top == -INFINITY) {
-    write_none<E, SAMPLE>(p, r, out);
-    return;
-  }
-  const uint32_t top_key = key_of(top);
-  const double top_wide = (double)top;
-  const double least = cut.min_p > 0.0f ? cut.temp * log((double)cut.min_p) : -INFINITY;  // x - top of what min_p keeps
-  const auto over_least = [&](float x) { return (double)x - top_wide >= least; };
-
-  // 2. the list
-  bool listed = false;
-  int n = 0;
-  double all_mass = 0.0;
   const bool by_mass = cut.top_p < 1.0f;
   // (top_p's share is of what top_k leaves, whatever min_p says: where there is a share, min_p does not shorten the list)
   const bool least_too = cut.min_p > 0.0f && !by_mass;
+  const double least = cut.min_p > 0.0f ? cut.temp * log((double)cut.min_p) : -INFINITY;  // x - top of what min_p keeps
+  const bool uncut = !by_mass && cut.top_k == 0 && cut.min_p == 0.0f;
   const bool try_list = least_too || (cut.top_k > 0 ? cut.top_k <= kByCount : by_mass);
-  if (try_list) {
-    const int wanted = cut.top_k > 0 ? (cut.top_k <= kByCount ? (int)cut.top_k : 0) : by_mass ? kByMass : 0;
-    const float bound = wanted > 0 ? bound_of(s.largest, wanted) : -INFINITY;
-    const bool need_mass = by_mass && cut.top_k == 0;
-    const int waves = (p.tiles + p.tiles_wave - 1) / p.tiles_wave;  // at work
-    const int room = kList / (waves <= 1 ? 1 : waves <= 2 ? 2 : waves <= 4 ? 4 : waves <= 8 ? 8 : 16);
-    int mine = 0;
-    double mass = 0.0;
-    each_piece(row, p, wave, lane, [&](long long at, const float (&v)[8]) {
-      unsigned hits = 0;
+  const bool need_mass = by_mass && cut.top_k == 0;
+  float largest = -INFINITY;
 #pragma unroll
-      for (int j = 0; j < 8; ++j) {
-        const bool there = has_mass(v[j]);
-        if (need_mass) mass += there ? mass_of(v[j], top_wide, cut.scale) : 0.0;
-        if (there && v[j] >= bound && (!least_too || over_least(v[j]))) hits |= 1u << j;
-      }
-      if (__ballot(hits != 0) != 0) {
-        const int count = __popc(hits), upto = wave_scan(count, lane);
-        int to = mine + upto - count;
+  for (int i = 0; i < kSample; ++i) {
+    float v[8];
+    widen_raw(first[i], v);
+    drop_massless(v);
 #pragma unroll
-        for (int j = 0; j < 8; ++j)
-          if ((hits >> j & 1) != 0) {
-            if (to < room) { s.list_distance[wave * room + to] = top_key - key_of(v[j]); s.list_index[wave * room + to] = (int)(at + j); }
-            ++to;
-          }
-        mine += __shfl(upto, 63);
-      }
-    });
-    if (lane == 0) {
-      s.wave_count[wave] = mine;
-      if (mine > room) s.overflow = 1;
-    }
-    if (need_mass) all_mass = block_sum(wave_sum(mass) * (lane == 0 ? 1.0 : 0.0), s.wave_double);
+    for (int j = 0; j < 8; ++j) largest = fmaxf(largest, v[j]);
+  }
+  const auto block_ends = [&](float high, float low, float &top, float &end) {
+#pragma unroll
+    for (int d = 1; d < 64; d <<= 1) { high = fmaxf(high, __shfl_xor(high, d)); low = fminf(low, __shfl_xor(low, d)); }
     __syncthreads();
-    listed = s.overflow == 0;
-    if (listed) {
-      // to one run: a wavefront's part to where the parts before it end
-      int before = 0;
-      for (int w = 0; w < kWaves; ++w) {
-        if (w < wave) before += s.wave_count[w];
-        n += s.wave_count[w];
-      }
-      const int count = s.wave_count[wave];
-      for (int e = lane; e < count; e += 64) s.sorted[before + e] = (unsigned long long)s.list_distance[wave * room + e] << 32 | (unsigned)s.list_index[wave * room + e];
-      __syncthreads();
-      for (int e = threadIdx.x; e < n; e += kThreads) { s.list_distance[e] = (uint32_t)(s.sorted[e] >> 32); s.list_index[e] = (int)(unsigned)s.sorted[e]; }
-      // 3. sorted, by distance and index
-      int size = 2;
-      while (size < n) size <<= 1;
-      __syncthreads();
-      for (int e = n + threadIdx.x; e < size; e += kThreads) s.sorted[e] = ~0ULL;
-      for (int run = 2; run <= size; run <<= 1)
-        for (int gap = run >> 1; gap > 0; gap >>= 1) {
-          __syncthreads();
-          for (int t = threadIdx.x; t < size / 2; t += kThreads) {
-            const int a = 2 * t - (t & (gap - 1)), b = a + gap;
-            const unsigned long long va = s.sorted[a], vb = s.sorted[b];
-            if ((va > vb) == ((a & run) == 0)) { s.sorted[a] = vb; s.sorted[b] = va; }
-          }
-        }
-      __syncthreads();
-      // masses summed along the order, two a thread
-      constexpr int kEach = kList / kThreads;
-      double m[kEach], total;
-      const int e0 = threadIdx.x * kEach;
+    if (lane == 0) { s.wave_high[wave] = high; s.wave_low[wave] = low; }
+    __syncthreads();
+    top = s.wave_high[0]; end = s.wave_low[0];
 #pragma unroll
-      for (int i = 0; i < kEach; ++i) m[i] = e0 + i < n ? mass_of(value_of(top_key - (uint32_t)(s.sorted[e0 + i] >> 32)), top_wide, cut.scale) : 0.0;
-      double sum = block_scan_before(m[0] + m[1], s.wave_double, total);
+    for (int w = 1; w < kWaves; ++w) { top = fmaxf(top, s.wave_high[w]); end = fminf(end, s.wave_low[w]); }
+  };
+  float reference, sample_low;
+  block_ends(largest, largest > -INFINITY ? largest : INFINITY, reference, sample_low);
+  if (cut.bad) reference = -INFINITY;
+  else if (reference == -INFINITY) {  // (uniform: the sample has no mass)
+    float high = -INFINITY;
+    each_piece(row, p, part, lane, kSample, [&](long long, const float (&v)[8]) {
+#pragma unroll
+      for (int j = 0; j < 8; ++j) high = fmaxf(high, v[j]);
+    });
+    block_ends(high, INFINITY, reference, sample_low);
+  }
+  if (reference == -INFINITY) {
+    write_none<E, SAMPLE>(p, r, out);
+    return;
+  }
+  // What the sample is of the row decides how far down the list goes: so that the kept entries are in it but for some four chances in a thousand of
+  // a row in random order.  (A row that they are not in after all takes the longer way.)
+  float bound = -INFINITY;
+  bool by_least = false;  // the bound is min_p's
+  if (try_list) {
+    const long long sampled = (long long)kThreads * kSample * 8;
+    const float share = p.V <= sampled ? 1.0f : (float)sampled / (float)p.V;
+    const bool counted = cut.top_k > 0 && cut.top_k <= kByCount;
+    if (counted || need_mass) {
+      const float expected = share * (float)(counted ? (int)cut.top_k : kByMass);
+      const int wanted = share == 1.0f ? (int)expected : (int)(expected + (counted ? 2.5f * sqrtf(expected) + 3.0f : 1.0f));
+      bound = bound_of(s, largest, reference, sample_low, wanted);
+    }
+    if (least_too) {
+      const float to = (float)((double)reference + least);
+      const float below = to - fabsf(to) * 0x1p-23f - 1e-38f;  // (not above what min_p keeps, whatever the rounding)
+      if (below > bound || !(counted || need_mass)) { by_least = true; bound = below > bound ? below : bound; }
+    }
+  }
+
+  // 2. the row goes by
+  float high = -INFINITY;
+  double mass = 0.0;
+  Lister list = {room_of(p), 0};
+  int piece = 0, count = 0;  // (count: the wavefront's kept)
+  long long tile = (long long)wave * p.tiles_wave;
+  const double reference_wide = (double)reference;
+  const auto see = [&](long long at, const float (&v)[8]) {
+    float here = fmaxf(fmaxf(fmaxf(v[0], v[1]), fmaxf(v[2], v[3])), fmaxf(fmaxf(v[4], v[5]), fmaxf(v[6], v[7])));
+    high = fmaxf(high, here);
+    if (need_mass || (SAMPLE && uncut)) {
+      mass += mass_of_eight([&](int j) { return v[j]; }, reference_wide, cut.scale);
+    }
+    if (SAMPLE && uncut) {
+#pragma unroll
+      for (int j = 0; j < 8; ++j) count += __popcll(__ballot(v[j] > -INFINITY));
+    }
+    if (try_list) {
+      bool hit[8];
+#pragma unroll
+      for (int j = 0; j < 8; ++j) hit[j] = v[j] >= bound && v[j] > -INFINITY;
+      list.add(s, wave, at, v, hit, here >= bound);
+    }
+    if (SAMPLE && uncut && (++piece == p.pieces_tile || at - lane * 8 + kPiece >= p.V)) {
+      const double sum = wave_sum(mass);
+      if (lane == 0) s.along[tile] = sum;
+      ++tile; piece = 0; mass = 0.0;
+    }
+  };
+#pragma unroll
+  for (int i = 0; i < kSample; ++i)
+    if (part.first + i * kPiece < part.last) {
+      float v[8];
+      widen_raw(first[i], v);
+      drop_massless(v);
+      see(part.first + i * kPiece + lane * 8, v);
+    }
+  each_piece(row, p, part, lane, kSample, see);
+  float top, unused;
+  block_ends(high, 0.0f, top, unused);
+  const double top_wide = (double)top;
+  const auto over_least = [&](float x) { return (double)x - top_wide >= least; };
+
+  // 3. the list
+  int n = 0;
+  double all_mass = 0.0;
+  if (need_mass) all_mass = block_sum(mass, s.wave_double) * exp2_of((reference_wide - top_wide) * cut.scale);
+  bool listed = try_list && join_list(s, list, lane, wave, n);
+  if (listed && cut.top_k > n && bound > -INFINITY && !by_least) listed = false;
+  if (listed) {
+    sort_list(s, n);
+    // masses summed along the order
+    constexpr int kEach = kList / kThreads;
+    double m[kEach], total;
+    const int e0 = threadIdx.x * kEach;
+    int first_n = cut.top_k > 0 && cut.top_k < n ? (int)cut.top_k : n;
+    if (by_mass) {
+      double sum = 0.0;
+#pragma unroll
+      for (int i = 0; i < kEach; ++i) {
+        m[i] = e0 + i < n ? mass_of(value_of((uint32_t)(s.sorted[e0 + i] >> 32)), top_wide, cut.scale) : 0.0;
+        sum += m[i];
+      }
+      sum = block_scan_before(sum, s.wave_double, total);
 #pragma unroll
       for (int i = 0; i < kEach; ++i) { sum += m[i]; s.masses[e0 + i] = sum; }
       __syncthreads();
-      // how many of them are kept
-      int first_n = cut.top_k > 0 && cut.top_k < n ? (int)cut.top_k : n;
-      const double of = cut.top_k > 0 ? s.masses[first_n - 1] : all_mass;
-      if (by_mass) {
-        const double target = (double)cut.top_p * of;
-        int a = 0, z = first_n;  // the first whose sum reaches the target
-        while (a < z) {
-          const int mid = (a + z) / 2;
-          if (s.masses[mid] >= target) z = mid; else a = mid + 1;
-        }
-        if (a >= first_n) {
-          if (cut.top_k > 0) a = first_n - 1;
-          else listed = over_least(value_of(top_key - (uint32_t)(s.sorted[n - 1] >> 32))) ? false : listed;  // (min_p may cut in the list all the same)
-        }
-        first_n = a + 1 < first_n ? a + 1 : first_n;
+      const double target = (double)cut.top_p * (cut.top_k > 0 ? s.masses[first_n - 1] : all_mass);
+      int a = 0, z = first_n;  // the first whose sum reaches the target
+      while (a < z) {
+        const int mid = (a + z) / 2;
+        if (s.masses[mid] >= target) z = mid; else a = mid + 1;
       }
-      if (cut.min_p > 0.0f) {
-        int a = 0, z = first_n;  // the first that it does not keep
-        while (a < z) {
-          const int mid = (a + z) / 2;
-          if (over_least(value_of(top_key - (uint32_t)(s.sorted[mid] >> 32)))) a = mid + 1; else z = mid;
-        }
-        first_n = a > 0 ? a : 1;
+      // (the list may end before; min_p may cut in it all the same)
+      if (a >= first_n && cut.top_k == 0 && bound > -INFINITY) listed = !over_least(value_of((uint32_t)(s.sorted[n - 1] >> 32)));
+      first_n = a + 1 < first_n ? a + 1 : first_n;
+    }
+    if (cut.min_p > 0.0f) {
+      int a = 0, z = first_n;  // the first that it does not keep
+      while (a < z) {
+        const int mid = (a + z) / 2;
+        if (over_least(value_of((uint32_t)(s.sorted[mid] >> 32)))) a = mid + 1; else z = mid;
       }
-      if (listed) {
-        const unsigned long long last = s.sorted[first_n - 1];
-        if (threadIdx.x == 0 && p.kept != nullptr) p.kept[r] = first_n;
+      first_n = a > 0 ? a : 1;
+    }
+    if (listed) {
+      const unsigned long long last = s.sorted[first_n - 1];
+      if (threadIdx.x == 0 && p.kept != nullptr) p.kept[r] = first_n;
+      if constexpr (SAMPLE) {
+        // masses of the kept summed along the indexes
+        double sum = 0.0;
+#pragma unroll
+        for (int i = 0; i < kEach; ++i) {
+          const int e = e0 + i;
+          const bool is_kept = e < n && ((unsigned long long)s.list_key[e] << 32 | (unsigned)s.list_index[e]) <= last;
+          m[i] = is_kept ? mass_of(value_of(s.list_key[e]), top_wide, cut.scale) : 0.0;
+          sum += m[i];
+        }
+        sum = block_scan_before(sum, s.wave_double, total);
+#pragma unroll
+        for (int i = 0; i < kEach; ++i) { sum += m[i]; s.along[e0 + i] = sum; }
         __syncthreads();
-        if constexpr (SAMPLE) {
-          // masses of the kept summed along the indexes
-#pragma unroll
-          for (int i = 0; i < kEach; ++i) {
-            const int e = e0 + i;
-            const bool is_kept = e < n && ((unsigned long long)s.list_distance[e] << 32 | (unsigned)s.list_index[e]) <= last;
-            m[i] = is_kept ? mass_of(value_of(top_key - s.list_distance[e]), top_wide, cut.scale) : 0.0;
+        total = s.along[n - 1];
+        for (int i = threadIdx.x; i < p.S; i += kThreads) {
+          const float u = p.u[r * p.u_stride + i];
+          const double target = (double)fmaxf(u, 0.0f) * total;
+          int a = 0, z = n;  // the first whose sum is over the target
+          while (a < z) {
+            const int mid = (a + z) / 2;
+            if (s.along[mid] > target) z = mid; else a = mid + 1;
           }
-          double along = block_scan_before(m[0] + m[1], s.wave_double, total);
-#pragma unroll
-          for (int i = 0; i < kEach; ++i) { along += m[i]; s.along[e0 + i] = along; }
-          __syncthreads();
-          total = s.along[n - 1];
-          for (int i = threadIdx.x; i < p.S; i += kThreads) {
-            const float u = p.u[r * p.u_stride + i];
-            const double target = (double)fmaxf(u, 0.0f) * total;
-            int a = 0, z = n;  // the first whose sum is over the target
-            while (a < z) {
-              const int mid = (a + z) / 2;
-              if (s.along[mid] > target) z = mid; else a = mid + 1;
-            }
-            if (a >= n) {  // the last kept
-              a = n - 1;
-              while (a > 0 && ((unsigned long long)s.list_distance[a] << 32 | (unsigned)s.list_index[a]) > last) --a;
-            }
-            p.tokens[r * p.S + i] = u == u ? s.list_index[a] : -1;
-            if (p.logp != nullptr)
-              p.logp[r * p.S + i] = u == u ? (float)(((double)value_of(top_key - s.list_distance[a]) - top_wide) / cut.temp - log(total)) : -INFINITY;
+          if (a >= n) {  // the last kept
+            a = n - 1;
+            while (a > 0 && ((unsigned long long)s.list_key[a] << 32 | (unsigned)s.list_index[a]) > last) --a;
           }
-        } else {
-          const uint32_t last_distance = (uint32_t)(last >> 32);
-          const int last_index = (int)(unsigned)last;
-          each_piece(row, p, wave, lane, [&](long long at, const float (&v)[8]) {
-            float w[8];
-#pragma unroll
-            for (int j = 0; j < 8; ++j) {
-              const uint32_t d = top_key - key_of(v[j]);
-              w[j] = has_mass(v[j]) && (d < last_distance || (d == last_distance && at + j <= last_index)) ? v[j] : -INFINITY;
-            }
-            if (at < p.V) store_first<8>(out + at, p.V - at, w);
-          });
+          p.tokens[r * p.S + i] = u == u ? s.list_index[a] : -1;
+          if (p.logp != nullptr) p.logp[r * p.S + i] = u == u ? (float)(((double)value_of(s.list_key[a]) - top_wide) / cut.temp - log(total)) : -INFINITY;
         }
-        return;
+      } else {
+        // the row is written as nothing, then the kept entries as they were (out may be x: they are read before)
+        E was[kEach];
+#pragma unroll
+        for (int i = 0; i < kEach; ++i) {
+          const int e = i * kThreads + threadIdx.x;
+          if (e < n) was[i] = row[s.list_index[e]];
+        }
+        __syncthreads();
+        const float none[8] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY, -INFINITY, -INFINITY, -INFINITY, -INFINITY};
+        for (long long at = part.first + lane * 8; at < part.last; at += kPiece) store_first<8>(out + at, p.V - at, none);
+        __syncthreads();
+#pragma unroll
+        for (int i = 0; i < kEach; ++i) {
+          const int e = i * kThreads + threadIdx.x;
+          if (e < n && ((unsigned long long)s.list_key[e] << 32 | (unsigned)s.list_index[e]) <= last) out[s.list_index[e]] = was[i];
+        }
       }
+      __syncthreads();
+      return;
     }
   }
 
   // The list does not hold them: narrowed down.
   Place place = {0xFFFFFFFFu, p.V};
   if (cut.top_k > 0) {
-    __syncthreads();
-    if (!narrow_down(row, p, s, top, cut.temp, (unsigned long long)cut.top_k, [](float) { return 1ULL; }, place)) place = {0xFFFFFFFFu, p.V};
+    const unsigned long long wanted = (unsigned long long)cut.top_k;
+    Place by;
+    if (narrow_down(row, p, s, part, top, cut.temp, place, [](float) { return 1ULL; }, [&](unsigned long long) { return wanted; }, by)) place = by;
   }
-  const auto inside = [&](float x, long long i) {
-    const uint32_t d = top_key - key_of(x);
-    return has_mass(x) && (d < place.distance || (d == place.distance && i <= place.index));
-  };
   if (by_mass) {
     // The unit of the whole numbers: 2^-51 of the largest entry's mass, or more where 62 bits would not hold the row's, which is at most
     // the sum over the threads of their largest one's times their entries.
-    const double most = s.largest[threadIdx.x] > -INFINITY ? mass_of(s.largest[threadIdx.x], top_wide, cut.scale) * (double)(p.tiles_wave * (long long)p.pieces_tile * 8) : 0.0;
-    const double bound = block_sum(most, s.wave_double);
-    int exponent = ilogb(bound) + 1;
-    exponent = 62 - exponent < 51 ? 62 - exponent : 51;
-    const double unit = ldexp(1.0, exponent);
+    const long long entries = (long long)p.tiles_wave * p.pieces_tile * 8;
+    const double bound_all = block_sum(high > -INFINITY ? mass_of(high, top_wide, cut.scale) * (double)entries : 0.0, s.wave_double);
+    const int room = 62 - (ilogb(bound_all) + 1);
+    const double unit = ldexp(1.0, room < 51 ? room : 51);
     const auto whole = [&](float x) { return (unsigned long long)(mass_of(x, top_wide, cut.scale) * unit + 0.5); };
-    unsigned long long mass = 0;
-    each_piece(row, p, wave, lane, [&](long long at, const float (&v)[8]) {
-#pragma unroll
-      for (int j = 0; j < 8; ++j) mass += inside(v[j], at + j) ? whole(v[j]) : 0ULL;
-    });
-    mass = block_sum(mass, s.wave_whole);
-    unsigned long long target = (unsigned long long)ceil((double)cut.top_p * (double)mass);
-    if (target < 1) target = 1;
-    Place by = place;
-    if (narrow_down(row, p, s, top, cut.temp, target, whole, by)) place = by;
+    const auto share = [&](unsigned long long all) {
+      const unsigned long long target = (unsigned long long)ceil((double)cut.top_p * (double)all);
+      return target < 1 ? 1 : target;
+    };
+    Place by;
+    if (narrow_down(row, p, s, part, top, cut.temp, place, whole, share, by)) place = by;
   }
-  if (cut.min_p > 0.0f) {  // the last distance that it keeps
-    uint32_t a = 0, z = top_key - key_of(-3.4028234663852886e38f) + 1;
+  if (cut.min_p > 0.0f) {  // the last key that it keeps
+    uint32_t a = key_of(top), z = kLastKey + 1;
     while (a < z) {
       const uint32_t mid = a + (z - a) / 2;
-      if (over_least(value_of(top_key - mid))) a = mid + 1; else z = mid;
+      if (over_least(value_of(mid))) a = mid + 1; else z = mid;
     }
-    const uint32_t last = a > 0 ? a - 1 : 0;
-    if (last < place.distance) place = {last, p.V};
+    const uint32_t last = a > key_of(top) ? a - 1 : a;
+    if (last < place.key) place = {last, p.V};
   }
-  int count = 0;
+  const auto inside = [&](float x, long long i) {
+    const uint32_t key = key_of(x);
+    return x > -INFINITY && (key < place.key || (key == place.key && i <= place.index));
+  };
   if constexpr (SAMPLE) {
-    // masses of the tiles
+    // masses of the tiles (an uncut row's are there, by the sample's reference)
+    const double by_wide = uncut ? reference_wide : top_wide;
     __syncthreads();
-    double tile = 0.0;
-    int piece = 0;
-    long long t = (long long)wave * p.tiles_wave;
-    each_piece(row, p, wave, lane, [&](long long at, const float (&v)[8]) {
+    if (!uncut) {
+      double sum_tile = 0.0;
+      piece = 0;
+      tile = (long long)wave * p.tiles_wave;
+      each_piece(row, p, part, lane, 0, [&](long long at, const float (&v)[8]) {
+        float kept[8];
 #pragma unroll
-      for (int j = 0; j < 8; ++j) {
-        const bool in = inside(v[j], at + j);
-        count += in ? 1 : 0;
-        tile += in ? mass_of(v[j], top_wide, cut.scale) : 0.0;
-      }
-      if (++piece == p.pieces_tile || at - lane * 8 + kPiece >= p.V) {
-        const double sum = wave_sum(tile);
-        if (lane == 0) s.masses[t] = sum;
-        ++t; piece = 0; tile = 0.0;
-      }
-    });
+        for (int j = 0; j < 8; ++j) {
+          const bool in = inside(v[j], at + j);
+          count += __popcll(__ballot(in));
+          kept[j] = in ? v[j] : -INFINITY;
+        }
+        sum_tile += mass_of_eight([&](int j) { return kept[j]; }, top_wide, cut.scale);
+        if (++piece == p.pieces_tile || at - lane * 8 + kPiece >= p.V) {
+          const double sum = wave_sum(sum_tile);
+          if (lane == 0) s.along[tile] = sum;
+          ++tile; piece = 0; sum_tile = 0.0;
+        }
+      });
+    }
     __syncthreads();
     constexpr int kEach = kMostTiles / kThreads;
     const int t0 = threadIdx.x * kEach;
-    double m[kEach], total;
+    double m[kEach], total, sum = 0.0;
 #pragma unroll
-    for (int i = 0; i < kEach; ++i) m[i] = t0 + i < p.tiles ? s.masses[t0 + i] : 0.0;
-    double along = block_scan_before(m[0] + m[1], s.wave_double, total);
+    for (int i = 0; i < kEach; ++i) { m[i] = t0 + i < p.tiles ? s.along[t0 + i] : 0.0; sum += m[i]; }
+    sum = block_scan_before(sum, s.wave_double, total);
 #pragma unroll
-    for (int i = 0; i < kEach; ++i) { along += m[i]; s.along[t0 + i] = along; }
+    for (int i = 0; i < kEach; ++i) { sum += m[i]; s.along[t0 + i] = sum; }
     __syncthreads();
     total = s.along[p.tiles - 1];
     for (int i = wave; i < p.S; i += kWaves) {  // a wavefront a token
@@ -598,25 +802,26 @@ template <typename E, bool SAMPLE> __device__ __forceinline__ void cut_row(const
         const long long at = at0 + lane * 8;
         float v[8];
         load_piece(row, at, p.V, v);
+        drop_massless(v);
         double w[8], mine = 0.0;
         long long last = -1;
 #pragma unroll
         for (int j = 0; j < 8; ++j) {
           const bool in = inside(v[j], at + j);
-          w[j] = in ? mass_of(v[j], top_wide, cut.scale) : 0.0;
+          w[j] = mass_of(in ? v[j] : -INFINITY, by_wide, cut.scale);
           mine += w[j];
           if (in) last = at + j;
         }
         const double upto = wave_scan(mine, lane);
         double here = before + (upto - mine);
-        long long first = -1;
+        long long hit = -1;
 #pragma unroll
         for (int j = 0; j < 8; ++j) {
           here += w[j];
-          if (first < 0 && w[j] > 0.0 && here > target) first = at + j;
+          if (hit < 0 && w[j] > 0.0 && here > target) hit = at + j;
         }
-        const unsigned long long any = __ballot(first >= 0), some = __ballot(last >= 0);
-        if (any != 0) found = __shfl(first, __builtin_ctzll(any));
+        const unsigned long long any = __ballot(hit >= 0), some = __ballot(last >= 0);
+        if (any != 0) found = __shfl(hit, __builtin_ctzll(any));
         if (some != 0) last_kept = __shfl(last, 63 - __builtin_clzll(some));
         before += __shfl(upto, 63);
       }
@@ -624,22 +829,21 @@ template <typename E, bool SAMPLE> __device__ __forceinline__ void cut_row(const
       if (lane == 0) {
         const bool number = u == u && found >= 0;
         p.tokens[r * p.S + i] = number ? (int)found : -1;
-        if (p.logp != nullptr) p.logp[r * p.S + i] = number ? (float)(((double)widen(row[found]) - top_wide) / cut.temp - log(total)) : -INFINITY;
+        if (p.logp != nullptr) p.logp[r * p.S + i] = number ? (float)(((double)widen(row[found]) - by_wide) / cut.temp - log(total)) : -INFINITY;
       }
     }
   } else {
-    each_piece(row, p, wave, lane, [&](long long at, const float (&v)[8]) {
+    each_piece(row, p, part, lane, 0, [&](long long at, const float (&v)[8]) {
       float w[8];
 #pragma unroll
       for (int j = 0; j < 8; ++j) {
         const bool in = inside(v[j], at + j);
-        count += in ? 1 : 0;
+        count += __popcll(__ballot(in));
         w[j] = in ? v[j] : -INFINITY;
       }
       if (at < p.V) store_first<8>(out + at, p.V - at, w);
     });
   }
-  for (int d = 1; d < 64; d <<= 1) count += __shfl_xor(count, d);
   __syncthreads();
   if (lane == 0) s.wave_count[wave] = count;
   __syncthreads();
@@ -648,9 +852,10 @@ template <typename E, bool SAMPLE> __device__ __forceinline__ void cut_row(const
     for (int w = 0; w < kWaves; ++w) sum += s.wave_count[w];
     p.kept[r] = sum;
   }
+  __syncthreads();
 }
 
-template <typename E, bool SAMPLE> __global__ void __launch_bounds__(kThreads) cut_kernel(const CutParams p) {
+template <typename E, bool SAMPLE> __global__ void __launch_bounds__(kThreads, 4) cut_kernel(const CutParams p) {
   __shared__ Shared s;
   for (long long r = blockIdx.x; r < p.R; r += gridDim.x) cut_row<E, SAMPLE>(p, r, s);
 }
