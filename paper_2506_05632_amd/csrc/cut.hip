@@ -25,14 +25,14 @@ constexpr int kBuckets = 4096;    // of a histogram
 constexpr int kBucketsLog = 12;
 constexpr int kMostTiles = 2048;  // of a row, whose masses LDS holds
 constexpr int kPiece = 512;       // entries that a wavefront takes at a time, eight a lane
-template <typename E> constexpr int kAhead = 8 / sizeof(E);  // pieces that it asks for together: 64 bytes a lane
+template <typename E> constexpr int kAhead = sizeof(E) == 2 ? 4 : 3;  // pieces that it has asked for
 constexpr int kSample = 2;        // pieces of a wavefront that the sample has
 constexpr int kByMass = 256;      // entries that the list aims at where a share of the mass is asked for
 constexpr int kByCount = 1200;    // top_k up to which the list is tried
-constexpr unsigned kMostRowBlocks = 1u << 20;
+constexpr long long kMostRowBlocks = 1LL << 22;  // rows of a launch
 
 struct CutParams {
-  long long R, V;
+  long long R, V, row0;
   const void *x;
   long long stride;
   int logits;  // the temperature counts
@@ -105,27 +105,45 @@ __device__ __forceinline__ double exp2_of(double t) {
 }
 __device__ __forceinline__ double mass_of(float x, double reference, double scale) { return exp2_of(((double)x - reference) * scale); }
 
-// Sums over a workgroup and along its threads.
-__device__ __forceinline__ double wave_sum(double v) {
+// Along a wavefront's lanes, without LDS: each lane's value and those of the lanes before, joined; `none`: what joins without effect.
+template <int CTRL, int ROWS, typename T> __device__ __forceinline__ T from_lane(T v, T none) {
+  constexpr int kWords = sizeof(T) / 4;
+  struct Words { int w[kWords]; };
+  const Words a = __builtin_bit_cast(Words, v), b = __builtin_bit_cast(Words, none);
+  Words r;
 #pragma unroll
-  for (int d = 1; d < 64; d <<= 1) v += __shfl_xor(v, d);
+  for (int i = 0; i < kWords; ++i) r.w[i] = __builtin_amdgcn_update_dpp(b.w[i], a.w[i], CTRL, ROWS, 0xF, false);
+  return __builtin_bit_cast(T, r);
+}
+template <typename T, typename F> __device__ __forceinline__ T wave_join(T v, T none, F join) {
+  v = join(v, from_lane<0x111, 0xF>(v, none));  // from one lane before, within rows of 16
+  v = join(v, from_lane<0x112, 0xF>(v, none));
+  v = join(v, from_lane<0x114, 0xF>(v, none));
+  v = join(v, from_lane<0x118, 0xF>(v, none));
+  v = join(v, from_lane<0x142, 0xA>(v, none));  // the first and third row's last to the rows after
+  v = join(v, from_lane<0x143, 0xC>(v, none));  // the second row's last to the third and fourth
   return v;
 }
-template <typename T> __device__ __forceinline__ T wave_scan(T v, int lane) {  // inclusive
+template <typename T> __device__ __forceinline__ T lane_value(T v, int lane) {  // (lane: uniform)
+  constexpr int kWords = sizeof(T) / 4;
+  struct Words { int w[kWords]; };
+  Words a = __builtin_bit_cast(Words, v);
 #pragma unroll
-  for (int d = 1; d < 64; d <<= 1) {
-    const T o = __shfl_up(v, d);
-    if (lane >= d) v += o;
-  }
-  return v;
+  for (int i = 0; i < kWords; ++i) a.w[i] = __builtin_amdgcn_readlane(a.w[i], lane);
+  return __builtin_bit_cast(T, a);
 }
+template <typename T> __device__ __forceinline__ T wave_scan(T v) { return wave_join(v, T(0), [](T a, T b) { return a + b; }); }
+template <typename T> __device__ __forceinline__ T wave_sum(T v) { return lane_value(wave_scan(v), 63); }
 
 struct Shared {
   union {
     unsigned long long histogram[kBuckets];
     struct {
       unsigned long long sorted[kList];  // key and index
-      double masses[kList];              // summed along the order
+      union {
+        double masses[kList];            // summed along the order
+        unsigned long long whole[kList]; // weights
+      };
     };
   };
   double along[kMostTiles];              // masses summed along the indexes: of the list's entries, or of tiles
@@ -148,7 +166,7 @@ static_assert(kMostTiles >= kList, "sums of the list's entries go where tiles' g
 // Over the threads' values: the sum of those before, and of all.
 template <typename T> __device__ __forceinline__ T block_scan_before(T v, T *s_wave, T &all) {
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const T upto = wave_scan(v, lane);
+  const T upto = wave_scan(v);
   __syncthreads();
   if (lane == 63) s_wave[wave] = upto;
   __syncthreads();
@@ -166,31 +184,30 @@ template <typename T> __device__ __forceinline__ T block_sum(T v, T *s_wave) {
   return all;
 }
 
-// A row's entries as a wavefront has them: `f(index of the first, its eight)` for its pieces in turn, from piece `skip` on; those behind the row's end,
-// and those without mass, are -inf.
 // A lane's entries of a piece as they lie in memory.
 template <typename E> struct Raw;
 template <> struct Raw<float> { float4_any a, b; };
 template <> struct Raw<uint16_t> { word4_any a; };
-template <typename E> __device__ __forceinline__ Raw<E> load_raw(const E *row, long long at, long long V) {
+// Where a lane's eight of a piece begin: of the last ones, where the piece is the row's end; with an entry a lane in rows of fewer than eight.
+__device__ __forceinline__ long long begin_of(long long piece, int lane, long long V) {
+  if (V < 8) return lane;
+  const long long at = piece + lane * 8;
+  return at + 8 <= V ? at : V - 8;
+}
+template <typename E> __device__ __forceinline__ Raw<E> load_raw(const E *row, long long piece, int lane, long long V) {
   Raw<E> r;
-  if (at + 8 <= V) {
-    r.a = *reinterpret_cast<const decltype(r.a) *>(row + at);
-    if constexpr (sizeof(E) == 4) r.b = *reinterpret_cast<const decltype(r.b) *>(row + at + 4);
-  } else if constexpr (sizeof(E) == 4) {
-#pragma unroll
-    for (int j = 0; j < 4; ++j) {
-      r.a[j] = at + j < V ? row[at + j] : -INFINITY;
-      r.b[j] = at + j + 4 < V ? row[at + j + 4] : -INFINITY;
-    }
+  if (V >= 8) {  // (uniform)
+    const E *from = row + begin_of(piece, lane, V);
+    r.a = *reinterpret_cast<const decltype(r.a) *>(from);
+    if constexpr (sizeof(E) == 4) r.b = *reinterpret_cast<const decltype(r.b) *>(from + 4);
   } else {
-#pragma unroll
-    for (int j = 0; j < 4; ++j)
-      r.a[j] = (at + 2 * j < V ? row[at + 2 * j] : 0xFF80u) | (uint32_t)(at + 2 * j + 1 < V ? row[at + 2 * j + 1] : 0xFF80u) << 16;
+    const E one = row[lane < V ? lane : 0];
+    if constexpr (sizeof(E) == 4) r.a[0] = one; else r.a[0] = (uint32_t)one;
   }
   return r;
 }
-template <typename E> __device__ __forceinline__ void widen_raw(const Raw<E> &r, float (&v)[8]) {
+// The entries as numbers: -inf those without mass, and those that another lane has.
+template <typename E> __device__ __forceinline__ void widen_raw(const Raw<E> &r, long long piece, int lane, long long V, float (&v)[8]) {
 #pragma unroll
   for (int j = 0; j < 4; ++j) {
     if constexpr (sizeof(E) == 4) {
@@ -199,45 +216,58 @@ template <typename E> __device__ __forceinline__ void widen_raw(const Raw<E> &r,
       split_pair(r.a[j], v[2 * j], v[2 * j + 1]);
     }
   }
-}
-template <typename E> __device__ __forceinline__ void load_piece(const E *row, long long at, long long V, float (&v)[8]) { widen_raw(load_raw(row, at, V), v); }
-__device__ __forceinline__ void drop_massless(float (&v)[8]) {
 #pragma unroll
   for (int j = 0; j < 8; ++j) v[j] = has_mass(v[j]) ? v[j] : -INFINITY;
+  if (piece + kPiece > V) {  // (uniform: the row's end)
+    const long long others = V < 8 ? 0 : piece + lane * 8 - begin_of(piece, lane, V);
+#pragma unroll
+    for (int j = 0; j < 8; ++j) v[j] = V < 8 ? (j == 0 && lane < V ? v[j] : -INFINITY) : j >= others ? v[j] : -INFINITY;
+  }
 }
+// A wavefront's entries: `f(index of the first, its eight)` for its pieces in turn, from piece `skip` on.
 struct Part {
-  long long first, last;  // entries of a wavefront
+  long long first, last;
 };
 __device__ __forceinline__ Part part_of(const CutParams &p, int wave) {
   const long long each = (long long)p.tiles_wave * p.pieces_tile * kPiece, first = wave * each, last = first + each;
   return {first < p.V ? first : p.V, last < p.V ? last : p.V};
 }
-template <typename E, typename F> __device__ __forceinline__ void each_piece(const E *row, const CutParams &p, Part part, int lane, int skip, F f) {
-  constexpr int kTurn = kAhead<E>;
-  for (long long at = part.first + skip * kPiece; at < part.last; at += kTurn * kPiece) {  // (uniform)
-    Raw<E> raw[kTurn];
+template <typename E> struct Ring {
+  static constexpr int kDepth = kAhead<E>;
+  Raw<E> raw[kDepth];
+  long long at, last;  // pieces (parts begin at whole ones; one behind the last is that one again)
+  __device__ __forceinline__ void fill(const E *row, const CutParams &p, Part part, int lane) {
+    at = part.first;
+    last = part.first < part.last ? (part.last - 1) / kPiece * kPiece : part.first - kPiece;
 #pragma unroll
-    for (int i = 0; i < kTurn; ++i)
-      if (at + i * kPiece < part.last) raw[i] = load_raw(row, at + i * kPiece + lane * 8, p.V);
-#pragma unroll
-    for (int i = 0; i < kTurn; ++i)
-      if (at + i * kPiece < part.last) {
-        float v[8];
-        widen_raw(raw[i], v);
-        drop_massless(v);
-        f(at + i * kPiece + lane * 8, v);
-        __builtin_amdgcn_sched_barrier(0);  // (pieces side by side would take more registers than there are)
-      }
+    for (int i = 0; i < kDepth; ++i)
+      if (at <= last) raw[i] = load_raw(row, at + i * kPiece < last ? at + i * kPiece : last, lane, p.V);
   }
+  template <typename F> __device__ __forceinline__ void run(const E *row, const CutParams &p, int lane, F f) {
+#pragma unroll 1
+    for (; at <= last; at += kPiece) {  // (uniform)
+      float v[8];
+      widen_raw(raw[0], at, lane, p.V, v);
+#pragma unroll
+      for (int i = 0; i + 1 < kDepth; ++i) raw[i] = raw[i + 1];
+      raw[kDepth - 1] = load_raw(row, at + kDepth * kPiece < last ? at + kDepth * kPiece : last, lane, p.V);
+      f(at, begin_of(at, lane, p.V), v);
+    }
+  }
+};
+template <typename E, typename F> __device__ __forceinline__ void each_piece(const E *row, const CutParams &p, Part part, int lane, F f) {
+  Ring<E> ring;
+  ring.fill(row, p, part, lane);
+  ring.run(row, p, lane, f);
 }
-// The masses of a lane's entries, four at a time for the same reason.
-template <typename F> __device__ __forceinline__ double mass_of_eight(F value, double reference, double scale) {
+// The masses of a lane's entries, four at a time: all at once would take more registers than there are.
+__device__ __forceinline__ double mass_of_eight(const float (&v)[8], double reference, double scale) {
   double sum = 0.0;
 #pragma unroll
   for (int h = 0; h < 8; h += 4) {
     double m[4];
 #pragma unroll
-    for (int j = 0; j < 4; ++j) m[j] = mass_of(value(h + j), reference, scale);
+    for (int j = 0; j < 4; ++j) m[j] = mass_of(v[h + j], reference, scale);
     sum += (m[0] + m[1]) + (m[2] + m[3]);
     __builtin_amdgcn_sched_barrier(0);
   }
@@ -326,44 +356,55 @@ __device__ __forceinline__ int bucket_of(float x, float top, float per) {
   const float at = (top - x) * per;  // (both roundings keep the order; an infinite `per` gives NaN at the top itself, and that 0)
   return at >= (float)(kBuckets - 1) ? kBuckets - 1 : (int)fmaxf(at, 0.0f);
 }
-// The bucket where the sum of those up to it reaches `target(sum of all)`; -1: none.  `above`: the sum of those before.
-template <typename T> __device__ __forceinline__ int pick_bucket(Shared &s, T target_of, unsigned long long &target, unsigned long long &above) {
+// The bucket where the sum of those up to it and of `above` reaches the target; -1: none.  before: the sum of those in front.  share > 0: the target is that share of all.
+__device__ __forceinline__ int pick_bucket(Shared &s, float share, unsigned long long above, unsigned long long &target, unsigned long long &before) {
   constexpr int kEach = kBuckets / kThreads;
   unsigned long long mine = 0, all;
 #pragma unroll
   for (int i = 0; i < kEach; ++i) mine += s.histogram[threadIdx.x * kEach + i];
-  unsigned long long before = block_scan_before(mine, s.wave_whole, all);
-  target = target_of(all);
+  unsigned long long upto = above + block_scan_before(mine, s.wave_whole, all);
+  if (share > 0.0f) {
+    target = (unsigned long long)ceil((double)share * (double)all);
+    if (target < 1) target = 1;
+  }
   if (threadIdx.x == 0) s.pick = -1;
   __syncthreads();
-  if (before < target && before + mine >= target) {
-#pragma unroll
+  if (upto < target && upto + mine >= target) {
+#pragma unroll 1
     for (int i = 0; i < kEach; ++i) {
       const unsigned long long here = s.histogram[threadIdx.x * kEach + i];
-      if (before < target && before + here >= target) { s.pick = threadIdx.x * kEach + i; s.pick_above = before; }
-      before += here;
+      if (upto < target && upto + here >= target) { s.pick = threadIdx.x * kEach + i; s.pick_above = upto - above; }
+      upto += here;
     }
   }
   __syncthreads();
-  above = s.pick_above;
+  before = s.pick_above;
   const int pick = s.pick;
   __syncthreads();
   return pick;
 }
-// Entries behind `until` take no part.  weight(x): the entry's, a whole number; target_of(sum of all).  False: the sum of all does not reach the target.
-template <typename E, typename W, typename T>
-__device__ __forceinline__ bool narrow_down(const E *row, const CutParams &p, Shared &s, Part part, float top, double temp, Place until, W weight, T target_of, Place &place) {
+// Weights: of an entry 1, or its mass in units, rounded.
+struct Weight {
+  bool counted;
+  double top, scale, unit;
+  __device__ __forceinline__ unsigned long long of(float x) const { return counted ? 1ULL : (unsigned long long)(mass_of(x, top, scale) * unit + 0.5); }
+};
+// Entries behind `until` take no part.  The target is `share` of the sum of all, of weights that are masses, or `wanted`.  False: the sum of all does not reach it.
+template <typename E>
+__device__ __forceinline__ bool narrow_down(const E *row, const CutParams &p, Shared &s, Part part, float top, double temp, Place until, const Weight weight, float share,
+                                            unsigned long long wanted, Place &place) {
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const float per = 128.0f / (float)temp;  // (the last bucket has what is 32 units of ln and more below the top)
   uint32_t low = key_of(top), high = kLastKey;
-  unsigned long long above = 0, target = 0;
+  unsigned long long above = 0, target = wanted;
   const auto inside = [&](uint32_t key, long long i) { return key < until.key || (key == until.key && i <= until.index); };
+#pragma unroll 1
   for (int level = 0; level == 0 || low < high; ++level) {
     const uint32_t span = high - low;
     const int shift = span >= kBuckets ? 32 - __builtin_clz(span) - kBucketsLog : 0;
     if (level > 0) {  // few entries: sorted, they show the place
       Lister list = {room_of(p), 0};
-      each_piece(row, p, part, lane, 0, [&](long long at, const float (&v)[8]) {
+      each_piece(row, p, part, lane, [&](long long, long long at, const float (&v)[8]) {
         bool hit[8], any = false;
 #pragma unroll
         for (int j = 0; j < 8; ++j) {
@@ -378,19 +419,21 @@ __device__ __forceinline__ bool narrow_down(const E *row, const CutParams &p, Sh
         sort_list(s, n);
         constexpr int kEach = kList / kThreads;
         const int e0 = threadIdx.x * kEach;
-        unsigned long long w[kEach], mine = 0, all;
-#pragma unroll
+        unsigned long long mine = 0, all;
+#pragma unroll 1
         for (int i = 0; i < kEach; ++i) {
-          w[i] = e0 + i < n ? weight(value_of((uint32_t)(s.sorted[e0 + i] >> 32))) : 0;
-          mine += w[i];
+          const unsigned long long w = e0 + i < n ? weight.of(value_of((uint32_t)(s.sorted[e0 + i] >> 32))) : 0;
+          s.whole[e0 + i] = w;
+          mine += w;
         }
         unsigned long long before = above + block_scan_before(mine, s.wave_whole, all);
         if (threadIdx.x == 0) s.pick = n - 1;
         __syncthreads();
-#pragma unroll
+#pragma unroll 1
         for (int i = 0; i < kEach; ++i) {
-          if (before < target && before + w[i] >= target) s.pick = e0 + i;
-          before += w[i];
+          const unsigned long long w = s.whole[e0 + i];
+          if (before < target && before + w >= target) s.pick = e0 + i;
+          before += w;
         }
         __syncthreads();
         const unsigned long long last = s.sorted[s.pick];
@@ -403,33 +446,31 @@ __device__ __forceinline__ bool narrow_down(const E *row, const CutParams &p, Sh
     __syncthreads();
     for (int i = threadIdx.x; i < kBuckets; i += kThreads) s.histogram[i] = 0;
     __syncthreads();
-    each_piece(row, p, part, lane, 0, [&](long long at, const float (&v)[8]) {
+    each_piece(row, p, part, lane, [&](long long, long long at, const float (&v)[8]) {
 #pragma unroll
       for (int j = 0; j < 8; ++j) {
         const uint32_t key = key_of(v[j]);
-        if (key < low || key > high || !inside(key, at + j)) continue;
-        const int bucket = level == 0 ? bucket_of(v[j], top, per) : (int)((key - low) >> shift);
-        const unsigned long long w = weight(v[j]);
-        if (w != 0) atomicAdd(&s.histogram[bucket], w);
+        const unsigned long long w = key >= low && key <= high && inside(key, at + j) ? weight.of(v[j]) : 0;
+        if (w != 0) atomicAdd(&s.histogram[level == 0 ? bucket_of(v[j], top, per) : (int)((key - low) >> shift)], w);
       }
     });
     __syncthreads();
     unsigned long long before;
-    const int bucket = level == 0 ? pick_bucket(s, target_of, target, before) : pick_bucket(s, [&](unsigned long long) { return target - above; }, target, before);
+    const int bucket = pick_bucket(s, level == 0 && !weight.counted ? share : 0.0f, above, target, before);
     if (bucket < 0) return false;
-    if (level > 0) target += above;
     above += before;
     if (level == 0) {  // the bucket's ends, by halving: the buckets follow the values
-      const auto first_at_least = [&](int b) {
-        uint32_t a = low, z = high + 1;  // (the first key whose bucket is b or more; keys end below 2^32 - 1)
+      uint32_t ends[2];
+#pragma unroll 1
+      for (int b = 0; b < 2; ++b) {
+        uint32_t a = low, z = high + 1;  // (the first key whose bucket is at least the one, or the next; keys end below 2^32 - 1)
         while (a < z) {
           const uint32_t mid = a + (z - a) / 2;
-          if (bucket_of(value_of(mid), top, per) >= b) z = mid; else a = mid + 1;
+          if (bucket_of(value_of(mid), top, per) >= bucket + b) z = mid; else a = mid + 1;
         }
-        return a;
-      };
-      const uint32_t from = first_at_least(bucket), to = bucket == kBuckets - 1 ? high : first_at_least(bucket + 1) - 1;
-      low = from; high = to;
+        if (b == 0) ends[0] = a; else ends[1] = a - 1;
+      }
+      low = ends[0]; high = ends[1];
     } else {
       low += (uint32_t)bucket << shift;
       const uint32_t end = low + ((1u << shift) - 1);
@@ -437,14 +478,13 @@ __device__ __forceinline__ bool narrow_down(const E *row, const CutParams &p, Sh
     }
   }
   // of the equals, as many as it takes
-  const unsigned long long each = weight(value_of(low));
+  const unsigned long long each = weight.of(value_of(low));
   const unsigned long long count = each > 0 ? (target - above + each - 1) / each : 1;
   int equals = 0;
-  each_piece(row, p, part, lane, 0, [&](long long, const float (&v)[8]) {
+  each_piece(row, p, part, lane, [&](long long, long long, const float (&v)[8]) {
 #pragma unroll
-    for (int j = 0; j < 8; ++j) equals += key_of(v[j]) == low ? 1 : 0;
+    for (int j = 0; j < 8; ++j) equals += __popcll(__ballot(key_of(v[j]) == low));
   });
-  for (int d = 1; d < 64; d <<= 1) equals += __shfl_xor(equals, d);
   __syncthreads();
   if (lane == 0) s.wave_count[wave] = equals;
   if (threadIdx.x == 0) s.pick_index = p.V;
@@ -452,7 +492,7 @@ __device__ __forceinline__ bool narrow_down(const E *row, const CutParams &p, Sh
   unsigned long long before = 0;
   for (int w = 0; w < wave; ++w) before += (unsigned)s.wave_count[w];
   if (before < count && before + (unsigned)equals >= count) {  // (uniform: this wavefront has the last)
-    each_piece(row, p, part, lane, 0, [&](long long at, const float (&v)[8]) {
+    each_piece(row, p, part, lane, [&](long long, long long at, const float (&v)[8]) {
       bool hit[8];
 #pragma unroll
       for (int j = 0; j < 8; ++j) hit[j] = key_of(v[j]) == low;
@@ -507,9 +547,8 @@ template <typename E, bool SAMPLE> __device__ __forceinline__ void cut_row(const
   E *out = SAMPLE ? nullptr : reinterpret_cast<E *>(p.out) + r * p.out_stride;
   const Part part = part_of(p, wave);
   // 1. the sample
-  Raw<E> first[kSample];
-#pragma unroll
-  for (int i = 0; i < kSample; ++i) first[i] = load_raw(row, part.first + i * kPiece < part.last ? part.first + i * kPiece + lane * 8 : p.V, p.V);
+  Ring<E> ring;
+  ring.fill(row, p, part, lane);
   const Cut cut = cut_of(p, r);
   const bool by_mass = cut.top_p < 1.0f;
   // (top_p's share is of what top_k leaves, whatever min_p says: where there is a share, min_p does not shorten the list)
@@ -521,15 +560,16 @@ template <typename E, bool SAMPLE> __device__ __forceinline__ void cut_row(const
   float largest = -INFINITY;
 #pragma unroll
   for (int i = 0; i < kSample; ++i) {
-    float v[8];
-    widen_raw(first[i], v);
-    drop_massless(v);
+    if (ring.at + i * kPiece <= ring.last) {
+      float v[8];
+      widen_raw(ring.raw[i], ring.at + i * kPiece, lane, p.V, v);
 #pragma unroll
-    for (int j = 0; j < 8; ++j) largest = fmaxf(largest, v[j]);
+      for (int j = 0; j < 8; ++j) largest = fmaxf(largest, v[j]);
+    }
   }
   const auto block_ends = [&](float high, float low, float &top, float &end) {
-#pragma unroll
-    for (int d = 1; d < 64; d <<= 1) { high = fmaxf(high, __shfl_xor(high, d)); low = fminf(low, __shfl_xor(low, d)); }
+    high = lane_value(wave_join(high, -INFINITY, [](float a, float b) { return fmaxf(a, b); }), 63);
+    low = lane_value(wave_join(low, INFINITY, [](float a, float b) { return fminf(a, b); }), 63);
     __syncthreads();
     if (lane == 0) { s.wave_high[wave] = high; s.wave_low[wave] = low; }
     __syncthreads();
@@ -542,7 +582,7 @@ template <typename E, bool SAMPLE> __device__ __forceinline__ void cut_row(const
   if (cut.bad) reference = -INFINITY;
   else if (reference == -INFINITY) {  // (uniform: the sample has no mass)
     float high = -INFINITY;
-    each_piece(row, p, part, lane, kSample, [&](long long, const float (&v)[8]) {
+    each_piece(row, p, part, lane, [&](long long, long long, const float (&v)[8]) {
 #pragma unroll
       for (int j = 0; j < 8; ++j) high = fmaxf(high, v[j]);
     });
@@ -579,11 +619,11 @@ template <typename E, bool SAMPLE> __device__ __forceinline__ void cut_row(const
   int piece = 0, count = 0;  // (count: the wavefront's kept)
   long long tile = (long long)wave * p.tiles_wave;
   const double reference_wide = (double)reference;
-  const auto see = [&](long long at, const float (&v)[8]) {
+  const auto see = [&](long long from, long long at, const float (&v)[8]) {
     float here = fmaxf(fmaxf(fmaxf(v[0], v[1]), fmaxf(v[2], v[3])), fmaxf(fmaxf(v[4], v[5]), fmaxf(v[6], v[7])));
     high = fmaxf(high, here);
     if (need_mass || (SAMPLE && uncut)) {
-      mass += mass_of_eight([&](int j) { return v[j]; }, reference_wide, cut.scale);
+      mass += mass_of_eight(v, reference_wide, cut.scale);
     }
     if (SAMPLE && uncut) {
 #pragma unroll
@@ -595,21 +635,13 @@ template <typename E, bool SAMPLE> __device__ __forceinline__ void cut_row(const
       for (int j = 0; j < 8; ++j) hit[j] = v[j] >= bound && v[j] > -INFINITY;
       list.add(s, wave, at, v, hit, here >= bound);
     }
-    if (SAMPLE && uncut && (++piece == p.pieces_tile || at - lane * 8 + kPiece >= p.V)) {
+    if (SAMPLE && uncut && (++piece == p.pieces_tile || from + kPiece >= p.V)) {
       const double sum = wave_sum(mass);
       if (lane == 0) s.along[tile] = sum;
       ++tile; piece = 0; mass = 0.0;
     }
   };
-#pragma unroll
-  for (int i = 0; i < kSample; ++i)
-    if (part.first + i * kPiece < part.last) {
-      float v[8];
-      widen_raw(first[i], v);
-      drop_massless(v);
-      see(part.first + i * kPiece + lane * 8, v);
-    }
-  each_piece(row, p, part, lane, kSample, see);
+  ring.run(row, p, lane, see);
   float top, unused;
   block_ends(high, 0.0f, top, unused);
   const double top_wide = (double)top;
@@ -715,25 +747,19 @@ template <typename E, bool SAMPLE> __device__ __forceinline__ void cut_row(const
 
   // The list does not hold them: narrowed down.
   Place place = {0xFFFFFFFFu, p.V};
-  if (cut.top_k > 0) {
-    const unsigned long long wanted = (unsigned long long)cut.top_k;
+#pragma unroll 1
+  for (int turn = 0; turn < 2; ++turn) {  // by count, then by mass
+    if (turn == 0 ? cut.top_k == 0 : !by_mass) continue;
+    Weight weight = {turn == 0, top_wide, cut.scale, 1.0};
+    if (turn == 1) {
+      // The unit of the whole numbers: 2^-51 of the largest entry's mass, or more where 62 bits would not hold the row's, which is at most
+      // the sum over the threads of their largest one's times their entries.
+      const long long entries = (long long)p.tiles_wave * p.pieces_tile * 8;
+      const int room = 62 - (ilogb(block_sum(mass_of(high, top_wide, cut.scale) * (double)entries, s.wave_double)) + 1);
+      weight.unit = ldexp(1.0, room < 51 ? room : 51);
+    }
     Place by;
-    if (narrow_down(row, p, s, part, top, cut.temp, place, [](float) { return 1ULL; }, [&](unsigned long long) { return wanted; }, by)) place = by;
-  }
-  if (by_mass) {
-    // The unit of the whole numbers: 2^-51 of the largest entry's mass, or more where 62 bits would not hold the row's, which is at most
-    // the sum over the threads of their largest one's times their entries.
-    const long long entries = (long long)p.tiles_wave * p.pieces_tile * 8;
-    const double bound_all = block_sum(high > -INFINITY ? mass_of(high, top_wide, cut.scale) * (double)entries : 0.0, s.wave_double);
-    const int room = 62 - (ilogb(bound_all) + 1);
-    const double unit = ldexp(1.0, room < 51 ? room : 51);
-    const auto whole = [&](float x) { return (unsigned long long)(mass_of(x, top_wide, cut.scale) * unit + 0.5); };
-    const auto share = [&](unsigned long long all) {
-      const unsigned long long target = (unsigned long long)ceil((double)cut.top_p * (double)all);
-      return target < 1 ? 1 : target;
-    };
-    Place by;
-    if (narrow_down(row, p, s, part, top, cut.temp, place, whole, share, by)) place = by;
+    if (narrow_down(row, p, s, part, top, cut.temp, place, weight, cut.top_p, (unsigned long long)cut.top_k, by)) place = by;
   }
   if (cut.min_p > 0.0f) {  // the last key that it keeps
     uint32_t a = key_of(top), z = kLastKey + 1;
@@ -756,7 +782,7 @@ template <typename E, bool SAMPLE> __device__ __forceinline__ void cut_row(const
       double sum_tile = 0.0;
       piece = 0;
       tile = (long long)wave * p.tiles_wave;
-      each_piece(row, p, part, lane, 0, [&](long long at, const float (&v)[8]) {
+      each_piece(row, p, part, lane, [&](long long from, long long at, const float (&v)[8]) {
         float kept[8];
 #pragma unroll
         for (int j = 0; j < 8; ++j) {
@@ -764,8 +790,8 @@ template <typename E, bool SAMPLE> __device__ __forceinline__ void cut_row(const
           count += __popcll(__ballot(in));
           kept[j] = in ? v[j] : -INFINITY;
         }
-        sum_tile += mass_of_eight([&](int j) { return kept[j]; }, top_wide, cut.scale);
-        if (++piece == p.pieces_tile || at - lane * 8 + kPiece >= p.V) {
+        sum_tile += mass_of_eight(kept, top_wide, cut.scale);
+        if (++piece == p.pieces_tile || from + kPiece >= p.V) {
           const double sum = wave_sum(sum_tile);
           if (lane == 0) s.along[tile] = sum;
           ++tile; piece = 0; sum_tile = 0.0;
@@ -799,10 +825,9 @@ template <typename E, bool SAMPLE> __device__ __forceinline__ void cut_row(const
       long long found = -1, last_kept = -1;
       const long long begin = (long long)a * p.pieces_tile * kPiece, end0 = begin + (long long)p.pieces_tile * kPiece, end = end0 < p.V ? end0 : p.V;
       for (long long at0 = begin; at0 < end && found < 0; at0 += kPiece) {
-        const long long at = at0 + lane * 8;
+        const long long at = begin_of(at0, lane, p.V);
         float v[8];
-        load_piece(row, at, p.V, v);
-        drop_massless(v);
+        widen_raw(load_raw(row, at0, lane, p.V), at0, lane, p.V, v);
         double w[8], mine = 0.0;
         long long last = -1;
 #pragma unroll
@@ -812,7 +837,7 @@ template <typename E, bool SAMPLE> __device__ __forceinline__ void cut_row(const
           mine += w[j];
           if (in) last = at + j;
         }
-        const double upto = wave_scan(mine, lane);
+        const double upto = wave_scan(mine);
         double here = before + (upto - mine);
         long long hit = -1;
 #pragma unroll
@@ -821,9 +846,9 @@ template <typename E, bool SAMPLE> __device__ __forceinline__ void cut_row(const
           if (hit < 0 && w[j] > 0.0 && here > target) hit = at + j;
         }
         const unsigned long long any = __ballot(hit >= 0), some = __ballot(last >= 0);
-        if (any != 0) found = __shfl(hit, __builtin_ctzll(any));
-        if (some != 0) last_kept = __shfl(last, 63 - __builtin_clzll(some));
-        before += __shfl(upto, 63);
+        if (any != 0) found = lane_value(hit, __builtin_ctzll(any));
+        if (some != 0) last_kept = lane_value(last, 63 - __builtin_clzll(some));
+        before += lane_value(upto, 63);
       }
       if (found < 0) found = last_kept;  // (rounding alone keeps the sum below the target)
       if (lane == 0) {
@@ -833,7 +858,7 @@ template <typename E, bool SAMPLE> __device__ __forceinline__ void cut_row(const
       }
     }
   } else {
-    each_piece(row, p, part, lane, 0, [&](long long at, const float (&v)[8]) {
+    each_piece(row, p, part, lane, [&](long long from, long long at, const float (&v)[8]) {
       float w[8];
 #pragma unroll
       for (int j = 0; j < 8; ++j) {
@@ -841,7 +866,13 @@ template <typename E, bool SAMPLE> __device__ __forceinline__ void cut_row(const
         count += __popcll(__ballot(in));
         w[j] = in ? v[j] : -INFINITY;
       }
-      if (at < p.V) store_first<8>(out + at, p.V - at, w);
+      if (from + kPiece <= p.V) {
+        store_some<8>(out + at, w);
+      } else {  // (a lane's own alone)
+#pragma unroll
+        for (int j = 0; j < 8; ++j)
+          if (p.V < 8 ? j == 0 && at < p.V : at + j >= from + lane * 8) out[at + j] = narrow<E>(w[j]);
+      }
     });
   }
   __syncthreads();
@@ -857,7 +888,17 @@ template <typename E, bool SAMPLE> __device__ __forceinline__ void cut_row(const
 
 template <typename E, bool SAMPLE> __global__ void __launch_bounds__(kThreads, 4) cut_kernel(const CutParams p) {
   __shared__ Shared s;
-  for (long long r = blockIdx.x; r < p.R; r += gridDim.x) cut_row<E, SAMPLE>(p, r, s);
+  cut_row<E, SAMPLE>(p, p.row0 + blockIdx.x, s);
+}
+template <bool SAMPLE> hipError_t launch_cut(CutParams p, int dtype, hipStream_t st) {
+  hipError_t e = hipSuccess;
+  for (; p.row0 < p.R && e == hipSuccess; p.row0 += kMostRowBlocks) {
+    const unsigned blocks = (unsigned)(p.R - p.row0 < kMostRowBlocks ? p.R - p.row0 : kMostRowBlocks);
+    if (dtype == LLC_F32) cut_kernel<float, SAMPLE><<<blocks, kThreads, 0, st>>>(p);
+    else cut_kernel<uint16_t, SAMPLE><<<blocks, kThreads, 0, st>>>(p);
+    e = hipGetLastError();
+  }
+  return e;
 }
 
 template <typename A> int check_cut(const A *a) {
@@ -885,7 +926,6 @@ template <typename A> int fill_cut(const A *a, CutParams &p) {
   p.tiles_wave = (p.tiles + kWaves - 1) / kWaves;
   return LLC_OK;
 }
-unsigned row_blocks(long long R) { return R < (long long)kMostRowBlocks ? (unsigned)R : kMostRowBlocks; }
 
 }  // namespace
 }  // namespace llc
@@ -907,11 +947,7 @@ extern "C" int llc_sample(const llc_sample_args *a) {
   p.S = (int)a->S; p.u = a->u; p.u_stride = a->u_stride_r; p.tokens = a->tokens; p.logp = a->logp;
   if ((a->flags & LLC_FLAG_DRY_RUN) != 0) return LLC_OK;
   hipStream_t st = (hipStream_t)a->stream;
-  return between_events(a->ev_begin, a->ev_end, st, [&] {
-    if (a->dtype == LLC_F32) cut_kernel<float, true><<<row_blocks(p.R), kThreads, 0, st>>>(p);
-    else cut_kernel<uint16_t, true><<<row_blocks(p.R), kThreads, 0, st>>>(p);
-    return hipGetLastError();
-  });
+  return between_events(a->ev_begin, a->ev_end, st, [&] { return launch_cut<true>(p, a->dtype, st); });
 }
 
 extern "C" int llc_truncate(const llc_truncate_args *a) {
@@ -928,9 +964,5 @@ extern "C" int llc_truncate(const llc_truncate_args *a) {
   p.out = a->out; p.out_stride = a->out_stride_r;
   if ((a->flags & LLC_FLAG_DRY_RUN) != 0) return LLC_OK;
   hipStream_t st = (hipStream_t)a->stream;
-  return between_events(a->ev_begin, a->ev_end, st, [&] {
-    if (a->dtype == LLC_F32) cut_kernel<float, false><<<row_blocks(p.R), kThreads, 0, st>>>(p);
-    else cut_kernel<uint16_t, false><<<row_blocks(p.R), kThreads, 0, st>>>(p);
-    return hipGetLastError();
-  });
+  return between_events(a->ev_begin, a->ev_end, st, [&] { return launch_cut<false>(p, a->dtype, st); });
 }
