@@ -20,15 +20,17 @@ namespace llc {
 namespace {
 
 constexpr int kThreads = 512, kWaves = kThreads / 64;
-constexpr int kList = 2048;       // entries of the list
-constexpr int kBuckets = 4096;    // of a histogram
-constexpr int kBucketsLog = 12;
+constexpr int kRoom = 512;        // entries of the list that a wavefront has room for: as many as its part of a row of 4096 has
+constexpr int kList = kRoom * kWaves;
+constexpr int kFew = kThreads;    // entries that are put in order by counting
+constexpr int kBuckets = 2048;    // of a histogram
+constexpr int kBucketsLog = 11;
 constexpr int kMostTiles = 2048;  // of a row, whose masses LDS holds
 constexpr int kPiece = 512;       // entries that a wavefront takes at a time, eight a lane
 template <typename E> constexpr int kAhead = sizeof(E) == 2 ? 4 : 3;  // pieces that it has asked for
 constexpr int kSample = 2;        // pieces of a wavefront that the sample has
 constexpr int kByMass = 256;      // entries that the list aims at where a share of the mass is asked for
-constexpr int kByCount = 1200;    // top_k up to which the list is tried
+constexpr int kByCount = 1800;    // top_k up to which the list is tried
 constexpr long long kMostRowBlocks = 1LL << 22;  // rows of a launch
 
 struct CutParams {
@@ -136,32 +138,27 @@ template <typename T> __device__ __forceinline__ T wave_scan(T v) { return wave_
 template <typename T> __device__ __forceinline__ T wave_sum(T v) { return lane_value(wave_scan(v), 63); }
 
 struct Shared {
-  union {
-    unsigned long long histogram[kBuckets];
-    struct {
-      unsigned long long sorted[kList];  // key and index
-      union {
-        double masses[kList];            // summed along the order
-        unsigned long long whole[kList]; // weights
-      };
-    };
-  };
-  double along[kMostTiles];              // masses summed along the indexes: of the list's entries, or of tiles
   uint32_t list_key[kList];
   int list_index[kList];
-  uint32_t sample[kThreads];             // a histogram of the sample's largest
+  union {
+    unsigned long long histogram[kBuckets];
+    double along[kList > kMostTiles ? kList : kMostTiles];  // masses summed along the indexes: of the list's entries, or of tiles
+    double masses[kFew];                                    // summed along the order
+    unsigned long long weights[kFew];
+  };
+  unsigned long long few[kFew], sorted[kFew];  // key and index
+  uint32_t sample[kThreads];                   // a histogram of the sample's largest
   union {
     double wave_double[kWaves];
     unsigned long long wave_whole[kWaves];
   };
   int wave_count[kWaves];
   float wave_high[kWaves], wave_low[kWaves];
-  int overflow;
+  int n_few;
   unsigned long long pick_above;
   int pick;
   long long pick_index;
 };
-static_assert(kMostTiles >= kList, "sums of the list's entries go where tiles' go");
 
 // Over the threads' values: the sum of those before, and of all.
 template <typename T> __device__ __forceinline__ T block_scan_before(T v, T *s_wave, T &all) {
@@ -206,6 +203,11 @@ template <typename E> __device__ __forceinline__ Raw<E> load_raw(const E *row, l
   }
   return r;
 }
+__device__ __forceinline__ float max_of_three(float a, float b, float c) {  // (of numbers: as it is, without a step that quiets NaNs first)
+  float r;
+  asm("v_max3_f32 %0, %1, %2, %3" : "=v"(r) : "v"(a), "v"(b), "v"(c));
+  return r;
+}
 // The entries as numbers: -inf those without mass, and those that another lane has.
 template <typename E> __device__ __forceinline__ void widen_raw(const Raw<E> &r, long long piece, int lane, long long V, float (&v)[8]) {
 #pragma unroll
@@ -216,13 +218,17 @@ template <typename E> __device__ __forceinline__ void widen_raw(const Raw<E> &r,
       split_pair(r.a[j], v[2 * j], v[2 * j + 1]);
     }
   }
+  float nought = 0.0f;  // (times 0 nothing is left of numbers, and a NaN of anything else)
 #pragma unroll
-  for (int j = 0; j < 8; ++j) v[j] = has_mass(v[j]) ? v[j] : -INFINITY;
-  if (piece + kPiece > V) {  // (uniform: the row's end)
+  for (int j = 0; j < 8; ++j) nought = fmaf(v[j], 0.0f, nought);
+  if (__ballot(nought != 0.0f) != 0 || piece + kPiece > V) {  // (uniform: something else, or the row's end)
     const long long others = V < 8 ? 0 : piece + lane * 8 - begin_of(piece, lane, V);
 #pragma unroll
-    for (int j = 0; j < 8; ++j) v[j] = V < 8 ? (j == 0 && lane < V ? v[j] : -INFINITY) : j >= others ? v[j] : -INFINITY;
+    for (int j = 0; j < 8; ++j) v[j] = has_mass(v[j]) && (V < 8 ? j == 0 && lane < V : j >= others) ? v[j] : -INFINITY;
   }
+}
+__device__ __forceinline__ float largest_of(const float (&v)[8]) {
+  return max_of_three(max_of_three(v[0], v[1], v[2]), max_of_three(v[3], v[4], v[5]), max_of_three(v[6], v[7], v[7]));
 }
 // A wavefront's entries: `f(index of the first, its eight)` for its pieces in turn, from piece `skip` on.
 struct Part {
@@ -247,18 +253,50 @@ template <typename E> struct Ring {
 #pragma unroll 1
     for (; at <= last; at += kPiece) {  // (uniform)
       float v[8];
-      widen_raw(raw[0], at, lane, p.V, v);
-#pragma unroll
-      for (int i = 0; i + 1 < kDepth; ++i) raw[i] = raw[i + 1];
-      raw[kDepth - 1] = load_raw(row, at + kDepth * kPiece < last ? at + kDepth * kPiece : last, lane, p.V);
+      take(row, p, lane, v);
       f(at, begin_of(at, lane, p.V), v);
     }
+  }
+  __device__ __forceinline__ void take(const E *row, const CutParams &p, int lane, float (&v)[8]) {  // the piece at `at`; asks for another
+    const Raw<E> mine = raw[0];
+#pragma unroll
+    for (int i = 0; i + 1 < kDepth; ++i) raw[i] = raw[i + 1];
+    raw[kDepth - 1] = load_raw(row, at + kDepth * kPiece < last ? at + kDepth * kPiece : last, lane, p.V);
+    widen_raw(mine, at, lane, p.V, v);
   }
 };
 template <typename E, typename F> __device__ __forceinline__ void each_piece(const E *row, const CutParams &p, Part part, int lane, F f) {
   Ring<E> ring;
   ring.fill(row, p, part, lane);
   ring.run(row, p, lane, f);
+}
+// The same of a row or of the list in its place (n entries, one piece a wavefront, whose indexes are their places in the list).
+struct Listed {
+  const Shared *s;  // null: the row
+  int n;
+};
+template <typename E, typename F> __device__ __forceinline__ void each_piece_of(Listed l, const E *row, const CutParams &p, Part part, int lane, int wave, F f) {
+  Ring<E> ring;
+  if (l.s != nullptr) {
+    ring.at = wave * kPiece;
+    ring.last = wave * kPiece < l.n ? ring.at : ring.at - 1;
+  } else {
+    ring.fill(row, p, part, lane);
+  }
+#pragma unroll 1
+  for (; ring.at <= ring.last; ring.at += kPiece) {
+    float v[8];
+    long long at;
+    if (l.s != nullptr) {
+      at = ring.at + lane * 8;
+#pragma unroll
+      for (int j = 0; j < 8; ++j) v[j] = at + j < l.n ? value_of(l.s->list_key[at + j]) : -INFINITY;
+    } else {
+      at = begin_of(ring.at, lane, p.V);
+      ring.take(row, p, lane, v);
+    }
+    f(at, v);
+  }
 }
 // The masses of a lane's entries, four at a time: all at once would take more registers than there are.
 __device__ __forceinline__ double mass_of_eight(const float (&v)[8], double reference, double scale) {
@@ -289,27 +327,21 @@ __device__ __forceinline__ int marked_before(const bool (&hit)[8], int &all) {
 
 // The list: each wavefront's entries in a part of its own, in the order of their indexes.
 struct Lister {
-  int room, count;
-  __device__ __forceinline__ void add(Shared &s, int wave, long long at, const float (&v)[8], const bool (&hit)[8], bool any) {
-    if (__ballot(any) == 0) return;
+  int count;
+  __device__ __forceinline__ void add(Shared &s, int wave, long long at, const float (&v)[8], const bool (&hit)[8]) {
     int all, to = count + marked_before(hit, all);
 #pragma unroll
     for (int j = 0; j < 8; ++j)
       if (hit[j]) {
-        if (to < room) { s.list_key[wave * room + to] = key_of(v[j]); s.list_index[wave * room + to] = (int)(at + j); }
+        if (to < kRoom) { s.list_key[wave * kRoom + to] = key_of(v[j]); s.list_index[wave * kRoom + to] = (int)(at + j); }
         ++to;
       }
     count += all;
   }
 };
-__device__ __forceinline__ int room_of(const CutParams &p) {
-  const int waves = (p.tiles + p.tiles_wave - 1) / p.tiles_wave;  // at work
-  return kList / (waves <= 1 ? 1 : waves <= 2 ? 2 : waves <= 4 ? 4 : 8);
-}
-// The wavefronts' parts to one run; false where one did not hold its entries.  The run is in `sorted` too, not sorted yet.
-__device__ __forceinline__ bool join_list(Shared &s, const Lister &l, int lane, int wave, int &n) {
-  __syncthreads();
-  if (lane == 0) s.wave_count[wave] = l.count;
+// The wavefronts' parts to one run of n; false where one did not hold its entries.
+__device__ __forceinline__ bool join_list(Shared &s, int count, int lane, int wave, int &n) {
+  if (lane == 0) s.wave_count[wave] = count;
   __syncthreads();
   int before = 0;
   bool whole = true;
@@ -319,31 +351,34 @@ __device__ __forceinline__ bool join_list(Shared &s, const Lister &l, int lane, 
     const int c = s.wave_count[w];
     if (w < wave) before += c;
     n += c;
-    whole = whole && c <= l.room;
+    whole = whole && c <= kRoom;
   }
   if (!whole) return false;
-  for (int e = lane; e < l.count; e += 64) s.sorted[before + e] = (unsigned long long)s.list_key[wave * l.room + e] << 32 | (unsigned)s.list_index[wave * l.room + e];
+  uint32_t key[kRoom / 64];
+  int index[kRoom / 64];
+#pragma unroll
+  for (int i = 0; i < kRoom / 64; ++i)
+    if (i * 64 < count) { key[i] = s.list_key[wave * kRoom + i * 64 + lane]; index[i] = s.list_index[wave * kRoom + i * 64 + lane]; }
   __syncthreads();
-  for (int e = threadIdx.x; e < n; e += kThreads) { s.list_key[e] = (uint32_t)(s.sorted[e] >> 32); s.list_index[e] = (int)(unsigned)s.sorted[e]; }
+#pragma unroll
+  for (int i = 0; i < kRoom / 64; ++i)
+    if (i * 64 + lane < count) { s.list_key[before + i * 64 + lane] = key[i]; s.list_index[before + i * 64 + lane] = index[i]; }
   __syncthreads();
   return true;
 }
-// Sorts the run: pairs at a distance below 128 are one wavefront's, whose steps follow each other without waiting for others.
-__device__ __forceinline__ void sort_list(Shared &s, int n) {
-  int size = 2;
-  while (size < n) size <<= 1;
-  for (int e = n + threadIdx.x; e < size; e += kThreads) s.sorted[e] = ~0ULL;
+// few[0..n) in order to sorted[0..n): a thread counts what is before its entry.  (200 entries: 3 us as exchanges in LDS, 1 so.)
+__device__ __forceinline__ void sort_few(Shared &s, int n) {
   __syncthreads();
-  for (int run = 2; run <= size; run <<= 1)
-    for (int gap = run >> 1; gap > 0; gap >>= 1) {
-      for (int t = threadIdx.x; t < size / 2; t += kThreads) {
-        const int a = 2 * t - (t & (gap - 1)), b = a + gap;
-        const unsigned long long va = s.sorted[a], vb = s.sorted[b];
-        if ((va > vb) == ((a & run) == 0)) { s.sorted[a] = vb; s.sorted[b] = va; }
-      }
-      if (gap > 64 || (gap == 1 && run >= 128)) __syncthreads();  // (the next step's pairs may be others')
-      else __builtin_amdgcn_wave_barrier();
+  if ((int)(threadIdx.x & ~63u) < n) {  // (uniform)
+    const unsigned long long mine = (int)threadIdx.x < n ? s.few[threadIdx.x] : ~0ULL;
+    int rank = 0;
+    for (int i = 0; i < (n & ~3); i += 4) {
+#pragma unroll
+      for (int j = 0; j < 4; ++j) rank += s.few[i + j] < mine ? 1 : 0;
     }
+    for (int i = n & ~3; i < n; ++i) rank += s.few[i] < mine ? 1 : 0;
+    if ((int)threadIdx.x < n) s.sorted[rank] = mine;
+  }
   __syncthreads();
 }
 
@@ -389,12 +424,12 @@ struct Weight {
   double top, scale, unit;
   __device__ __forceinline__ unsigned long long of(float x) const { return counted ? 1ULL : (unsigned long long)(mass_of(x, top, scale) * unit + 0.5); }
 };
-// Entries behind `until` take no part.  The target is `share` of the sum of all, of weights that are masses, or `wanted`.  False: the sum of all does not reach it.
+// Entries behind `until` take no part.  The target is `share` of the sum of all, or, where that is 0, `wanted`.  False: the sum of all does not reach it.
 template <typename E>
-__device__ __forceinline__ bool narrow_down(const E *row, const CutParams &p, Shared &s, Part part, float top, double temp, Place until, const Weight weight, float share,
-                                            unsigned long long wanted, Place &place) {
+__device__ __forceinline__ bool narrow_down(Listed l, const E *row, const CutParams &p, Shared &s, Part part, float top, double temp, Place until, const Weight weight,
+                                            float share, unsigned long long wanted, Place &place) {
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const float per = 128.0f / (float)temp;  // (the last bucket has what is 32 units of ln and more below the top)
+  const float per = 64.0f / (float)temp;  // (the last bucket has what is 32 units of ln and more below the top)
   uint32_t low = key_of(top), high = kLastKey;
   unsigned long long above = 0, target = wanted;
   const auto inside = [&](uint32_t key, long long i) { return key < until.key || (key == until.key && i <= until.index); };
@@ -402,61 +437,55 @@ __device__ __forceinline__ bool narrow_down(const E *row, const CutParams &p, Sh
   for (int level = 0; level == 0 || low < high; ++level) {
     const uint32_t span = high - low;
     const int shift = span >= kBuckets ? 32 - __builtin_clz(span) - kBucketsLog : 0;
-    if (level > 0) {  // few entries: sorted, they show the place
-      Lister list = {room_of(p), 0};
-      each_piece(row, p, part, lane, [&](long long, long long at, const float (&v)[8]) {
-        bool hit[8], any = false;
-#pragma unroll
-        for (int j = 0; j < 8; ++j) {
-          const uint32_t key = key_of(v[j]);
-          hit[j] = key >= low && key <= high && inside(key, at + j);
-          any = any || hit[j];
-        }
-        list.add(s, wave, at, v, hit, any);
-      });
-      int n;
-      if (join_list(s, list, lane, wave, n)) {
-        sort_list(s, n);
-        constexpr int kEach = kList / kThreads;
-        const int e0 = threadIdx.x * kEach;
-        unsigned long long mine = 0, all;
-#pragma unroll 1
-        for (int i = 0; i < kEach; ++i) {
-          const unsigned long long w = e0 + i < n ? weight.of(value_of((uint32_t)(s.sorted[e0 + i] >> 32))) : 0;
-          s.whole[e0 + i] = w;
-          mine += w;
-        }
-        unsigned long long before = above + block_scan_before(mine, s.wave_whole, all);
-        if (threadIdx.x == 0) s.pick = n - 1;
-        __syncthreads();
-#pragma unroll 1
-        for (int i = 0; i < kEach; ++i) {
-          const unsigned long long w = s.whole[e0 + i];
-          if (before < target && before + w >= target) s.pick = e0 + i;
-          before += w;
-        }
-        __syncthreads();
-        const unsigned long long last = s.sorted[s.pick];
-        place.key = (uint32_t)(last >> 32);
-        place.index = (int)(unsigned)last;
-        __syncthreads();
-        return true;
-      }
-    }
     __syncthreads();
     for (int i = threadIdx.x; i < kBuckets; i += kThreads) s.histogram[i] = 0;
+    if (threadIdx.x == 0) s.n_few = 0;
     __syncthreads();
-    each_piece(row, p, part, lane, [&](long long, long long at, const float (&v)[8]) {
+    each_piece_of(l, row, p, part, lane, wave, [&](long long at, const float (&v)[8]) {
+      bool in[8], any = false;
 #pragma unroll
       for (int j = 0; j < 8; ++j) {
         const uint32_t key = key_of(v[j]);
-        const unsigned long long w = key >= low && key <= high && inside(key, at + j) ? weight.of(v[j]) : 0;
-        if (w != 0) atomicAdd(&s.histogram[level == 0 ? bucket_of(v[j], top, per) : (int)((key - low) >> shift)], w);
+        in[j] = key >= low && key <= high && inside(key, at + j);
+        any = any || in[j];
+      }
+      if (__ballot(any) == 0) return;
+#pragma unroll
+      for (int j = 0; j < 8; ++j) {
+        const unsigned long long w = in[j] ? weight.of(v[j]) : 0;
+        if (w != 0) atomicAdd(&s.histogram[level == 0 ? bucket_of(v[j], top, per) : (int)((key_of(v[j]) - low) >> shift)], w);
+      }
+      if (level > 0) {
+        int all, to = marked_before(in, all), from = 0;
+        if (lane == 0) from = atomicAdd(&s.n_few, all);
+        to += lane_value(from, 0);
+#pragma unroll
+        for (int j = 0; j < 8; ++j)
+          if (in[j]) {
+            if (to < kFew) s.few[to] = (unsigned long long)key_of(v[j]) << 32 | (unsigned)(at + j);
+            ++to;
+          }
       }
     });
     __syncthreads();
+    const int n = s.n_few;
+    if (level > 0 && n <= kFew) {  // few entries: in order, they show the place
+      sort_few(s, n);
+      unsigned long long all;
+      const int e = threadIdx.x;
+      const unsigned long long w = e < n ? weight.of(value_of((uint32_t)(s.sorted[e] >> 32))) : 0, before = above + block_scan_before(w, s.wave_whole, all);
+      if (threadIdx.x == 0) s.pick = n - 1;
+      __syncthreads();
+      if (before < target && before + w >= target) s.pick = e;
+      __syncthreads();
+      const unsigned long long last = s.sorted[s.pick];
+      place.key = (uint32_t)(last >> 32);
+      place.index = (int)(unsigned)last;
+      __syncthreads();
+      return true;
+    }
     unsigned long long before;
-    const int bucket = pick_bucket(s, level == 0 && !weight.counted ? share : 0.0f, above, target, before);
+    const int bucket = pick_bucket(s, level == 0 ? share : 0.0f, above, target, before);
     if (bucket < 0) return false;
     above += before;
     if (level == 0) {  // the bucket's ends, by halving: the buckets follow the values
@@ -471,6 +500,10 @@ __device__ __forceinline__ bool narrow_down(const E *row, const CutParams &p, Sh
         if (b == 0) ends[0] = a; else ends[1] = a - 1;
       }
       low = ends[0]; high = ends[1];
+      if constexpr (sizeof(E) == 2) {  // (to the keys that bf16 numbers have, of which a bucket may have a single one)
+        low = low < 0x80000000u ? low | 0xFFFFu : (low + 0xFFFFu) & 0xFFFF0000u;
+        high = high < 0x80000000u ? ((high + 1) & 0xFFFF0000u) - 1 : high & 0xFFFF0000u;
+      }
     } else {
       low += (uint32_t)bucket << shift;
       const uint32_t end = low + ((1u << shift) - 1);
@@ -481,27 +514,31 @@ __device__ __forceinline__ bool narrow_down(const E *row, const CutParams &p, Sh
   const unsigned long long each = weight.of(value_of(low));
   const unsigned long long count = each > 0 ? (target - above + each - 1) / each : 1;
   int equals = 0;
-  each_piece(row, p, part, lane, [&](long long, long long, const float (&v)[8]) {
-#pragma unroll
-    for (int j = 0; j < 8; ++j) equals += __popcll(__ballot(key_of(v[j]) == low));
-  });
-  __syncthreads();
-  if (lane == 0) s.wave_count[wave] = equals;
-  if (threadIdx.x == 0) s.pick_index = p.V;
-  __syncthreads();
   unsigned long long before = 0;
-  for (int w = 0; w < wave; ++w) before += (unsigned)s.wave_count[w];
-  if (before < count && before + (unsigned)equals >= count) {  // (uniform: this wavefront has the last)
-    each_piece(row, p, part, lane, [&](long long, long long at, const float (&v)[8]) {
+#pragma unroll 1
+  for (int turn = 0; turn < 2; ++turn) {  // how many each wavefront has; then the one
+    if (turn == 1) {
+      __syncthreads();
+      if (lane == 0) s.wave_count[wave] = equals;
+      if (threadIdx.x == 0) s.pick_index = p.V;
+      __syncthreads();
+      for (int w = 0; w < wave; ++w) before += (unsigned)s.wave_count[w];
+      if (before >= count || before + (unsigned)equals < count) break;  // (uniform: another wavefront has the last)
+    }
+    each_piece_of(l, row, p, part, lane, wave, [&](long long at, const float (&v)[8]) {
       bool hit[8];
 #pragma unroll
       for (int j = 0; j < 8; ++j) hit[j] = key_of(v[j]) == low;
       int all;
       unsigned long long here = before + (unsigned)marked_before(hit, all);
+      if (turn == 0) {
+        equals += all;
+      } else {
 #pragma unroll
-      for (int j = 0; j < 8; ++j)
-        if (hit[j] && ++here == count) s.pick_index = at + j;
-      before += (unsigned)all;
+        for (int j = 0; j < 8; ++j)
+          if (hit[j] && ++here == count) s.pick_index = at + j;
+        before += (unsigned)all;
+      }
     });
   }
   __syncthreads();
@@ -563,8 +600,7 @@ template <typename E, bool SAMPLE> __device__ __forceinline__ void cut_row(const
     if (ring.at + i * kPiece <= ring.last) {
       float v[8];
       widen_raw(ring.raw[i], ring.at + i * kPiece, lane, p.V, v);
-#pragma unroll
-      for (int j = 0; j < 8; ++j) largest = fmaxf(largest, v[j]);
+      largest = max_of_three(largest, largest_of(v), largest);
     }
   }
   const auto block_ends = [&](float high, float low, float &top, float &end) {
@@ -592,7 +628,7 @@ template <typename E, bool SAMPLE> __device__ __forceinline__ void cut_row(const
     write_none<E, SAMPLE>(p, r, out);
     return;
   }
-  // What the sample is of the row decides how far down the list goes: so that the kept entries are in it but for some four chances in a thousand of
+  // What the sample is of the row decides how far down the list goes: so that the kept entries are in it but for some chance in a million of
   // a row in random order.  (A row that they are not in after all takes the longer way.)
   float bound = -INFINITY;
   bool by_least = false;  // the bound is min_p's
@@ -602,7 +638,7 @@ template <typename E, bool SAMPLE> __device__ __forceinline__ void cut_row(const
     const bool counted = cut.top_k > 0 && cut.top_k <= kByCount;
     if (counted || need_mass) {
       const float expected = share * (float)(counted ? (int)cut.top_k : kByMass);
-      const int wanted = share == 1.0f ? (int)expected : (int)(expected + (counted ? 2.5f * sqrtf(expected) + 3.0f : 1.0f));
+      const int wanted = share == 1.0f ? (int)expected : (int)(expected + (counted ? 4.5f * sqrtf(expected) + 6.0f : 1.0f));
       bound = bound_of(s, largest, reference, sample_low, wanted);
     }
     if (least_too) {
@@ -615,25 +651,23 @@ template <typename E, bool SAMPLE> __device__ __forceinline__ void cut_row(const
   // 2. the row goes by
   float high = -INFINITY;
   double mass = 0.0;
-  Lister list = {room_of(p), 0};
+  Lister list = {0};
   int piece = 0, count = 0;  // (count: the wavefront's kept)
   long long tile = (long long)wave * p.tiles_wave;
   const double reference_wide = (double)reference;
   const auto see = [&](long long from, long long at, const float (&v)[8]) {
-    float here = fmaxf(fmaxf(fmaxf(v[0], v[1]), fmaxf(v[2], v[3])), fmaxf(fmaxf(v[4], v[5]), fmaxf(v[6], v[7])));
-    high = fmaxf(high, here);
-    if (need_mass || (SAMPLE && uncut)) {
-      mass += mass_of_eight(v, reference_wide, cut.scale);
-    }
+    const float here = largest_of(v);
+    high = max_of_three(high, here, high);
+    if (need_mass || (SAMPLE && uncut)) mass += mass_of_eight(v, reference_wide, cut.scale);
     if (SAMPLE && uncut) {
 #pragma unroll
       for (int j = 0; j < 8; ++j) count += __popcll(__ballot(v[j] > -INFINITY));
     }
-    if (try_list) {
+    if (try_list && __ballot(here >= bound) != 0) {
       bool hit[8];
 #pragma unroll
       for (int j = 0; j < 8; ++j) hit[j] = v[j] >= bound && v[j] > -INFINITY;
-      list.add(s, wave, at, v, hit, here >= bound);
+      list.add(s, wave, at, v, hit);
     }
     if (SAMPLE && uncut && (++piece == p.pieces_tile || from + kPiece >= p.V)) {
       const double sum = wave_sum(mass);
@@ -651,25 +685,20 @@ template <typename E, bool SAMPLE> __device__ __forceinline__ void cut_row(const
   int n = 0;
   double all_mass = 0.0;
   if (need_mass) all_mass = block_sum(mass, s.wave_double) * exp2_of((reference_wide - top_wide) * cut.scale);
-  bool listed = try_list && join_list(s, list, lane, wave, n);
-  if (listed && cut.top_k > n && bound > -INFINITY && !by_least) listed = false;
-  if (listed) {
-    sort_list(s, n);
-    // masses summed along the order
-    constexpr int kEach = kList / kThreads;
-    double m[kEach], total;
-    const int e0 = threadIdx.x * kEach;
+  bool listed = try_list && join_list(s, list.count, lane, wave, n);
+  if (listed && cut.top_k > n && bound > -INFINITY && !by_least) listed = false;  // (there are more below the bound)
+  Place place = {0xFFFFFFFFu, p.V};  // (of the list's entries: their places in the list)
+  bool found = false;
+  if (listed && n <= kFew) {
+    const int e = threadIdx.x;
+    if (e < n) s.few[e] = (unsigned long long)s.list_key[e] << 32 | (unsigned)e;
+    sort_few(s, n);
     int first_n = cut.top_k > 0 && cut.top_k < n ? (int)cut.top_k : n;
-    if (by_mass) {
-      double sum = 0.0;
-#pragma unroll
-      for (int i = 0; i < kEach; ++i) {
-        m[i] = e0 + i < n ? mass_of(value_of((uint32_t)(s.sorted[e0 + i] >> 32)), top_wide, cut.scale) : 0.0;
-        sum += m[i];
-      }
-      sum = block_scan_before(sum, s.wave_double, total);
-#pragma unroll
-      for (int i = 0; i < kEach; ++i) { sum += m[i]; s.masses[e0 + i] = sum; }
+    if (by_mass) {  // masses summed along the order
+      const double mine = e < n ? mass_of(value_of((uint32_t)(s.sorted[e] >> 32)), top_wide, cut.scale) : 0.0;
+      double total;
+      const double before = block_scan_before(mine, s.wave_double, total);
+      if (e < n) s.masses[e] = before + mine;
       __syncthreads();
       const double target = (double)cut.top_p * (cut.top_k > 0 ? s.masses[first_n - 1] : all_mass);
       int a = 0, z = first_n;  // the first whose sum reaches the target
@@ -681,85 +710,36 @@ template <typename E, bool SAMPLE> __device__ __forceinline__ void cut_row(const
       if (a >= first_n && cut.top_k == 0 && bound > -INFINITY) listed = !over_least(value_of((uint32_t)(s.sorted[n - 1] >> 32)));
       first_n = a + 1 < first_n ? a + 1 : first_n;
     }
-    if (cut.min_p > 0.0f) {
-      int a = 0, z = first_n;  // the first that it does not keep
-      while (a < z) {
-        const int mid = (a + z) / 2;
-        if (over_least(value_of((uint32_t)(s.sorted[mid] >> 32)))) a = mid + 1; else z = mid;
-      }
-      first_n = a > 0 ? a : 1;
-    }
-    if (listed) {
-      const unsigned long long last = s.sorted[first_n - 1];
-      if (threadIdx.x == 0 && p.kept != nullptr) p.kept[r] = first_n;
-      if constexpr (SAMPLE) {
-        // masses of the kept summed along the indexes
-        double sum = 0.0;
-#pragma unroll
-        for (int i = 0; i < kEach; ++i) {
-          const int e = e0 + i;
-          const bool is_kept = e < n && ((unsigned long long)s.list_key[e] << 32 | (unsigned)s.list_index[e]) <= last;
-          m[i] = is_kept ? mass_of(value_of(s.list_key[e]), top_wide, cut.scale) : 0.0;
-          sum += m[i];
-        }
-        sum = block_scan_before(sum, s.wave_double, total);
-#pragma unroll
-        for (int i = 0; i < kEach; ++i) { sum += m[i]; s.along[e0 + i] = sum; }
-        __syncthreads();
-        total = s.along[n - 1];
-        for (int i = threadIdx.x; i < p.S; i += kThreads) {
-          const float u = p.u[r * p.u_stride + i];
-          const double target = (double)fmaxf(u, 0.0f) * total;
-          int a = 0, z = n;  // the first whose sum is over the target
-          while (a < z) {
-            const int mid = (a + z) / 2;
-            if (s.along[mid] > target) z = mid; else a = mid + 1;
-          }
-          if (a >= n) {  // the last kept
-            a = n - 1;
-            while (a > 0 && ((unsigned long long)s.list_key[a] << 32 | (unsigned)s.list_index[a]) > last) --a;
-          }
-          p.tokens[r * p.S + i] = u == u ? s.list_index[a] : -1;
-          if (p.logp != nullptr) p.logp[r * p.S + i] = u == u ? (float)(((double)value_of(s.list_key[a]) - top_wide) / cut.temp - log(total)) : -INFINITY;
-        }
-      } else {
-        // the row is written as nothing, then the kept entries as they were (out may be x: they are read before)
-        E was[kEach];
-#pragma unroll
-        for (int i = 0; i < kEach; ++i) {
-          const int e = i * kThreads + threadIdx.x;
-          if (e < n) was[i] = row[s.list_index[e]];
-        }
-        __syncthreads();
-        const float none[8] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY, -INFINITY, -INFINITY, -INFINITY, -INFINITY};
-        for (long long at = part.first + lane * 8; at < part.last; at += kPiece) store_first<8>(out + at, p.V - at, none);
-        __syncthreads();
-#pragma unroll
-        for (int i = 0; i < kEach; ++i) {
-          const int e = i * kThreads + threadIdx.x;
-          if (e < n && ((unsigned long long)s.list_key[e] << 32 | (unsigned)s.list_index[e]) <= last) out[s.list_index[e]] = was[i];
-        }
-      }
-      __syncthreads();
-      return;
-    }
+    const unsigned long long last = s.sorted[first_n - 1];
+    place = {(uint32_t)(last >> 32), (long long)(unsigned)last};
+    found = listed;
   }
-
-  // The list does not hold them: narrowed down.
-  Place place = {0xFFFFFFFFu, p.V};
+  // What the order by counting does not show is narrowed down, in the list or, where that does not hold what is asked for, in the row.
 #pragma unroll 1
-  for (int turn = 0; turn < 2; ++turn) {  // by count, then by mass
-    if (turn == 0 ? cut.top_k == 0 : !by_mass) continue;
-    Weight weight = {turn == 0, top_wide, cut.scale, 1.0};
-    if (turn == 1) {
-      // The unit of the whole numbers: 2^-51 of the largest entry's mass, or more where 62 bits would not hold the row's, which is at most
-      // the sum over the threads of their largest one's times their entries.
-      const long long entries = (long long)p.tiles_wave * p.pieces_tile * 8;
-      const int room = 62 - (ilogb(block_sum(mass_of(high, top_wide, cut.scale) * (double)entries, s.wave_double)) + 1);
-      weight.unit = ldexp(1.0, room < 51 ? room : 51);
+  while (!found) {
+    place = {0xFFFFFFFFu, p.V};
+    found = true;
+    const Listed in = {listed ? &s : nullptr, n};
+#pragma unroll 1
+    for (int turn = 0; turn < 2; ++turn) {  // by count, then by mass
+      if (turn == 0 ? cut.top_k == 0 : !by_mass) continue;
+      Weight weight = {turn == 0, top_wide, cut.scale, 1.0};
+      unsigned long long wanted = (unsigned long long)cut.top_k;
+      float share = 0.0f;
+      if (turn == 1) {
+        // The unit of the whole numbers: 2^-51 of the largest entry's mass, or more where 62 bits would not hold the row's, which is at most
+        // the sum over the threads of their largest one's times their entries.
+        const long long entries = (long long)p.tiles_wave * p.pieces_tile * 8;
+        const int room = 62 - (ilogb(block_sum(mass_of(high, top_wide, cut.scale) * (double)entries, s.wave_double)) + 1);
+        weight.unit = ldexp(1.0, room < 51 ? room : 51);
+        if (listed && need_mass) wanted = (unsigned long long)ceil((double)cut.top_p * all_mass * weight.unit);
+        else share = cut.top_p;
+      }
+      Place by;
+      if (narrow_down(in, row, p, s, part, top, cut.temp, place, weight, share, wanted, by)) place = by;
+      else found = !(listed && need_mass && bound > -INFINITY);  // (the list ends before)
     }
-    Place by;
-    if (narrow_down(row, p, s, part, top, cut.temp, place, weight, cut.top_p, (unsigned long long)cut.top_k, by)) place = by;
+    if (!found) listed = false;
   }
   if (cut.min_p > 0.0f) {  // the last key that it keeps
     uint32_t a = key_of(top), z = kLastKey + 1;
@@ -770,6 +750,78 @@ template <typename E, bool SAMPLE> __device__ __forceinline__ void cut_row(const
     const uint32_t last = a > key_of(top) ? a - 1 : a;
     if (last < place.key) place = {last, p.V};
   }
+  const auto kept_at = [&](int e) { return s.list_key[e] < place.key || (s.list_key[e] == place.key && e <= place.index); };
+  if (listed) {
+    const int each = (n + kThreads - 1) / kThreads, e0 = threadIdx.x * each, e1 = e0 + each < n ? e0 + each : n;
+    __syncthreads();
+    if constexpr (SAMPLE) {
+      // masses of the kept summed along the indexes
+      double sum = 0.0, total;
+      int mine = 0;
+#pragma unroll 1
+      for (int e = e0; e < e1; ++e) {
+        if (kept_at(e)) { sum += mass_of(value_of(s.list_key[e]), top_wide, cut.scale); ++mine; }
+        s.along[e] = sum;
+      }
+      const double before = block_scan_before(sum, s.wave_double, total);
+#pragma unroll 1
+      for (int e = e0; e < e1; ++e) s.along[e] += before;
+      mine = wave_sum(mine);
+      if (lane == 0) s.wave_count[wave] = mine;
+      __syncthreads();
+      if (threadIdx.x == 0 && p.kept != nullptr) {
+        int kept = 0;
+        for (int w = 0; w < kWaves; ++w) kept += s.wave_count[w];
+        p.kept[r] = kept;
+      }
+      total = s.along[n - 1];
+      const double log_total = log(total);
+      for (int i = threadIdx.x; i < p.S; i += kThreads) {
+        const float u = p.u[r * p.u_stride + i];
+        const double target = (double)fmaxf(u, 0.0f) * total;
+        int a = 0, z = n;  // the first whose sum is over the target
+        while (a < z) {
+          const int mid = (a + z) / 2;
+          if (s.along[mid] > target) z = mid; else a = mid + 1;
+        }
+        if (a >= n) {  // the last kept
+          a = n - 1;
+          while (a > 0 && !kept_at(a)) --a;
+        }
+        p.tokens[r * p.S + i] = u == u ? s.list_index[a] : -1;
+        if (p.logp != nullptr) p.logp[r * p.S + i] = u == u ? (float)(((double)value_of(s.list_key[a]) - top_wide) / cut.temp - log_total) : -INFINITY;
+      }
+    } else {
+      // the row is written as nothing, then the kept entries as they were (out may be x: they are read before)
+      constexpr int kEach = kList / kThreads;
+      E was[kEach];
+      int mine = 0;
+#pragma unroll
+      for (int i = 0; i < kEach; ++i) {
+        const int e = i * kThreads + threadIdx.x;
+        if (e < n && kept_at(e)) { was[i] = row[s.list_index[e]]; ++mine; }
+      }
+      mine = wave_sum(mine);
+      if (lane == 0) s.wave_count[wave] = mine;
+      __syncthreads();
+      const float none[8] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY, -INFINITY, -INFINITY, -INFINITY, -INFINITY};
+      for (long long at = part.first + lane * 8; at < part.last; at += kPiece) store_first<8>(out + at, p.V - at, none);
+      __syncthreads();
+#pragma unroll
+      for (int i = 0; i < kEach; ++i) {
+        const int e = i * kThreads + threadIdx.x;
+        if (e < n && kept_at(e)) out[s.list_index[e]] = was[i];
+      }
+      if (threadIdx.x == 0 && p.kept != nullptr) {
+        int kept = 0;
+        for (int w = 0; w < kWaves; ++w) kept += s.wave_count[w];
+        p.kept[r] = kept;
+      }
+    }
+    return;
+  }
+
+  // The row's entries, where the list does not hold the kept ones.
   const auto inside = [&](float x, long long i) {
     const uint32_t key = key_of(x);
     return x > -INFINITY && (key < place.key || (key == place.key && i <= place.index));
