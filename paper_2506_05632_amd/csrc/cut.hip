@@ -27,7 +27,7 @@ constexpr int kBuckets = 2048;    // of a histogram
 constexpr int kBucketsLog = 11;
 constexpr int kMostTiles = 2048;  // of a row, whose masses LDS holds
 constexpr int kPiece = 512;       // entries that a wavefront takes at a time, eight a lane
-template <typename E> constexpr int kAhead = sizeof(E) == 2 ? 4 : 3;  // pieces that it has asked for
+constexpr int kAhead = 4;         // pieces that it has asked for
 constexpr int kSample = 2;        // pieces of a wavefront that the sample has
 constexpr int kByMass = 256;      // entries that the list aims at where a share of the mass is asked for
 constexpr int kByCount = 1800;    // top_k up to which the list is tried
@@ -157,7 +157,7 @@ struct Shared {
   int n_few;
   unsigned long long pick_above;
   int pick;
-  long long pick_index;
+  uint32_t pick_index;
 };
 
 // Over the threads' values: the sum of those before, and of all.
@@ -185,18 +185,21 @@ template <typename T> __device__ __forceinline__ T block_sum(T v, T *s_wave) {
 template <typename E> struct Raw;
 template <> struct Raw<float> { float4_any a, b; };
 template <> struct Raw<uint16_t> { word4_any a; };
-// Where a lane's eight of a piece begin: of the last ones, where the piece is the row's end; with an entry a lane in rows of fewer than eight.
-__device__ __forceinline__ long long begin_of(long long piece, int lane, long long V) {
-  if (V < 8) return lane;
-  const long long at = piece + lane * 8;
-  return at + 8 <= V ? at : V - 8;
+template <typename E> __device__ __forceinline__ void load_eight(Raw<E> &r, const E *from) {
+  r.a = *reinterpret_cast<const decltype(r.a) *>(from);
+  if constexpr (sizeof(E) == 4) r.b = *reinterpret_cast<const decltype(r.b) *>(from + 4);
 }
-template <typename E> __device__ __forceinline__ Raw<E> load_raw(const E *row, long long piece, int lane, long long V) {
+// Where a lane's eight of a piece begin: of the last ones, where the piece is the row's end; with an entry a lane in rows of fewer than eight.
+__device__ __forceinline__ unsigned begin_of(unsigned piece, unsigned lane, unsigned V) {
+  const unsigned at = piece + lane * 8;
+  return V < 8 ? lane : at + 8 <= V ? at : V - 8;
+}
+template <typename E> __device__ __forceinline__ Raw<E> load_raw(const E *row, unsigned piece, unsigned lane, unsigned V) {
   Raw<E> r;
-  if (V >= 8) {  // (uniform)
-    const E *from = row + begin_of(piece, lane, V);
-    r.a = *reinterpret_cast<const decltype(r.a) *>(from);
-    if constexpr (sizeof(E) == 4) r.b = *reinterpret_cast<const decltype(r.b) *>(from + 4);
+  if (piece + kPiece <= V) {  // (uniform)
+    load_eight(r, row + piece + lane * 8);
+  } else if (V >= 8) {
+    load_eight(r, row + begin_of(piece, lane, V));
   } else {
     const E one = row[lane < V ? lane : 0];
     if constexpr (sizeof(E) == 4) r.a[0] = one; else r.a[0] = (uint32_t)one;
@@ -209,7 +212,7 @@ __device__ __forceinline__ float max_of_three(float a, float b, float c) {  // (
   return r;
 }
 // The entries as numbers: -inf those without mass, and those that another lane has.
-template <typename E> __device__ __forceinline__ void widen_raw(const Raw<E> &r, long long piece, int lane, long long V, float (&v)[8]) {
+template <typename E> __device__ __forceinline__ void widen_raw(const Raw<E> &r, unsigned piece, unsigned lane, unsigned V, float (&v)[8]) {
 #pragma unroll
   for (int j = 0; j < 4; ++j) {
     if constexpr (sizeof(E) == 4) {
@@ -222,53 +225,54 @@ template <typename E> __device__ __forceinline__ void widen_raw(const Raw<E> &r,
 #pragma unroll
   for (int j = 0; j < 8; ++j) nought = fmaf(v[j], 0.0f, nought);
   if (__ballot(nought != 0.0f) != 0 || piece + kPiece > V) {  // (uniform: something else, or the row's end)
-    const long long others = V < 8 ? 0 : piece + lane * 8 - begin_of(piece, lane, V);
+    const unsigned others = V < 8 ? (lane < V ? 0 : 8) : piece + lane * 8 - begin_of(piece, lane, V), mine = V < 8 ? 1 : 8;
 #pragma unroll
-    for (int j = 0; j < 8; ++j) v[j] = has_mass(v[j]) && (V < 8 ? j == 0 && lane < V : j >= others) ? v[j] : -INFINITY;
+    for (unsigned j = 0; j < 8; ++j) {
+      const bool is = has_mass(v[j]) & (j >= others) & (j < mine);
+      v[j] = is ? v[j] : -INFINITY;
+    }
   }
 }
 __device__ __forceinline__ float largest_of(const float (&v)[8]) {
   return max_of_three(max_of_three(v[0], v[1], v[2]), max_of_three(v[3], v[4], v[5]), max_of_three(v[6], v[7], v[7]));
 }
-// A wavefront's entries: `f(index of the first, its eight)` for its pieces in turn, from piece `skip` on.
+// A wavefront's entries.
 struct Part {
-  long long first, last;
+  unsigned first, last;
 };
 __device__ __forceinline__ Part part_of(const CutParams &p, int wave) {
-  const long long each = (long long)p.tiles_wave * p.pieces_tile * kPiece, first = wave * each, last = first + each;
-  return {first < p.V ? first : p.V, last < p.V ? last : p.V};
+  const unsigned long long each = (unsigned long long)p.tiles_wave * (unsigned)p.pieces_tile * kPiece, first = (unsigned)wave * each, last = first + each, V = (unsigned long long)p.V;
+  return {(unsigned)(first < V ? first : V), (unsigned)(last < V ? last : V)};
 }
-template <typename E> struct Ring {
-  static constexpr int kDepth = kAhead<E>;
-  Raw<E> raw[kDepth];
-  long long at, last;  // pieces (parts begin at whole ones; one behind the last is that one again)
-  __device__ __forceinline__ void fill(const E *row, const CutParams &p, Part part, int lane) {
-    at = part.first;
-    last = part.first < part.last ? (part.last - 1) / kPiece * kPiece : part.first - kPiece;
+// Its pieces in turn, of which DEPTH are asked for ahead: f(piece, index of a lane's first, its eight).  (A load goes to the place of the piece that was taken: copies from place
+// to place would wait for what was asked for last.)
+template <typename E, int DEPTH> struct Ring {
+  Raw<E> raw[DEPTH];
+  __device__ __forceinline__ void fill(const E *row, unsigned V, Part part, int lane) {
 #pragma unroll
-    for (int i = 0; i < kDepth; ++i)
-      if (at <= last) raw[i] = load_raw(row, at + i * kPiece < last ? at + i * kPiece : last, lane, p.V);
+    for (int i = 0; i < DEPTH; ++i)
+      if (part.first + i * kPiece < part.last) raw[i] = load_raw(row, part.first + i * kPiece, lane, V);
   }
-  template <typename F> __device__ __forceinline__ void run(const E *row, const CutParams &p, int lane, F f) {
+  template <typename F> __device__ __forceinline__ void run(const E *row, unsigned V, Part part, int lane, F f) {
 #pragma unroll 1
-    for (; at <= last; at += kPiece) {  // (uniform)
-      float v[8];
-      take(row, p, lane, v);
-      f(at, begin_of(at, lane, p.V), v);
-    }
-  }
-  __device__ __forceinline__ void take(const E *row, const CutParams &p, int lane, float (&v)[8]) {  // the piece at `at`; asks for another
-    const Raw<E> mine = raw[0];
+    for (unsigned at0 = part.first; at0 < part.last; at0 += DEPTH * kPiece) {  // (uniform)
 #pragma unroll
-    for (int i = 0; i + 1 < kDepth; ++i) raw[i] = raw[i + 1];
-    raw[kDepth - 1] = load_raw(row, at + kDepth * kPiece < last ? at + kDepth * kPiece : last, lane, p.V);
-    widen_raw(mine, at, lane, p.V, v);
+      for (int i = 0; i < DEPTH; ++i) {
+        const unsigned at = at0 + i * kPiece;
+        if (at < part.last) {
+          float v[8];
+          widen_raw(raw[i], at, lane, V, v);
+          if (at + DEPTH * kPiece < part.last) raw[i] = load_raw(row, at + DEPTH * kPiece, lane, V);
+          f(at, begin_of(at, lane, V), v);
+        }
+      }
+    }
   }
 };
 template <typename E, typename F> __device__ __forceinline__ void each_piece(const E *row, const CutParams &p, Part part, int lane, F f) {
-  Ring<E> ring;
-  ring.fill(row, p, part, lane);
-  ring.run(row, p, lane, f);
+  Ring<E, 2> ring;
+  ring.fill(row, (unsigned)p.V, part, lane);
+  ring.run(row, (unsigned)p.V, part, lane, f);
 }
 // The same of a row or of the list in its place (n entries, one piece a wavefront, whose indexes are their places in the list).
 struct Listed {
@@ -276,26 +280,32 @@ struct Listed {
   int n;
 };
 template <typename E, typename F> __device__ __forceinline__ void each_piece_of(Listed l, const E *row, const CutParams &p, Part part, int lane, int wave, F f) {
-  Ring<E> ring;
-  if (l.s != nullptr) {
-    ring.at = wave * kPiece;
-    ring.last = wave * kPiece < l.n ? ring.at : ring.at - 1;
-  } else {
-    ring.fill(row, p, part, lane);
-  }
+  const unsigned V = (unsigned)p.V;
+  if (l.s != nullptr) part = {(unsigned)wave * kPiece, wave * kPiece < l.n ? (unsigned)wave * kPiece + 1 : (unsigned)wave * kPiece};
+  constexpr int kTwo = 2;
 #pragma unroll 1
-  for (; ring.at <= ring.last; ring.at += kPiece) {
-    float v[8];
-    long long at;
+  for (unsigned at0 = part.first; at0 < part.last; at0 += kTwo * kPiece) {  // (uniform)
+    Raw<E> raw[kTwo];
+    float v[kTwo][8];
+    unsigned at[kTwo];
     if (l.s != nullptr) {
-      at = ring.at + lane * 8;
+      at[0] = at0 + lane * 8;
 #pragma unroll
-      for (int j = 0; j < 8; ++j) v[j] = at + j < l.n ? value_of(l.s->list_key[at + j]) : -INFINITY;
+      for (int j = 0; j < 8; ++j) v[0][j] = (int)at[0] + j < l.n ? value_of(l.s->list_key[at[0] + j]) : -INFINITY;
     } else {
-      at = begin_of(ring.at, lane, p.V);
-      ring.take(row, p, lane, v);
+#pragma unroll
+      for (int i = 0; i < kTwo; ++i)
+        if (at0 + i * kPiece < part.last) raw[i] = load_raw(row, at0 + i * kPiece, lane, V);
+#pragma unroll
+      for (int i = 0; i < kTwo; ++i)
+        if (at0 + i * kPiece < part.last) {
+          at[i] = begin_of(at0 + i * kPiece, lane, V);
+          widen_raw(raw[i], at0 + i * kPiece, lane, V, v[i]);
+        }
     }
-    f(at, v);
+#pragma unroll
+    for (int i = 0; i < kTwo; ++i)
+      if (at0 + i * kPiece < part.last) f(at[i], v[i]);
   }
 }
 // The masses of a lane's entries, four at a time: all at once would take more registers than there are.
@@ -325,18 +335,20 @@ __device__ __forceinline__ int marked_before(const bool (&hit)[8], int &all) {
   return before;
 }
 
-// The list: each wavefront's entries in a part of its own, in the order of their indexes.
+// The list: each wavefront's entries in a part of its own, in the order of their indexes; once they are more than it has room for, they are counted only.
 struct Lister {
   int count;
-  __device__ __forceinline__ void add(Shared &s, int wave, long long at, const float (&v)[8], const bool (&hit)[8]) {
-    int all, to = count + marked_before(hit, all);
+  __device__ __forceinline__ void add(Shared &s, int wave, unsigned at, const float (&v)[8], const bool (&hit)[8]) {
+    int all, to = wave * kRoom + count + marked_before(hit, all);
+    count += all;
+    if (count > kRoom) return;  // (uniform)
 #pragma unroll
     for (int j = 0; j < 8; ++j)
       if (hit[j]) {
-        if (to < kRoom) { s.list_key[wave * kRoom + to] = key_of(v[j]); s.list_index[wave * kRoom + to] = (int)(at + j); }
+        s.list_key[to] = key_of(v[j]);
+        s.list_index[to] = (int)(at + j);
         ++to;
       }
-    count += all;
   }
 };
 // The wavefronts' parts to one run of n; false where one did not hold its entries.
@@ -385,7 +397,7 @@ __device__ __forceinline__ void sort_few(Shared &s, int n) {
 // The place of the order where the weights' sum reaches `target`: a whole number's histogram by values, then the entries of the bucket.
 struct Place {
   uint32_t key;     // of the last entry
-  long long index;
+  uint32_t index;
 };
 __device__ __forceinline__ int bucket_of(float x, float top, float per) {
   const float at = (top - x) * per;  // (both roundings keep the order; an infinite `per` gives NaN at the top itself, and that 0)
@@ -432,7 +444,7 @@ __device__ __forceinline__ bool narrow_down(Listed l, const E *row, const CutPar
   const float per = 64.0f / (float)temp;  // (the last bucket has what is 32 units of ln and more below the top)
   uint32_t low = key_of(top), high = kLastKey;
   unsigned long long above = 0, target = wanted;
-  const auto inside = [&](uint32_t key, long long i) { return key < until.key || (key == until.key && i <= until.index); };
+  const auto inside = [&](uint32_t key, unsigned i) { return key < until.key || (key == until.key && i <= until.index); };
 #pragma unroll 1
   for (int level = 0; level == 0 || low < high; ++level) {
     const uint32_t span = high - low;
@@ -441,7 +453,7 @@ __device__ __forceinline__ bool narrow_down(Listed l, const E *row, const CutPar
     for (int i = threadIdx.x; i < kBuckets; i += kThreads) s.histogram[i] = 0;
     if (threadIdx.x == 0) s.n_few = 0;
     __syncthreads();
-    each_piece_of(l, row, p, part, lane, wave, [&](long long at, const float (&v)[8]) {
+    each_piece_of(l, row, p, part, lane, wave, [&](unsigned at, const float (&v)[8]) {
       bool in[8], any = false;
 #pragma unroll
       for (int j = 0; j < 8; ++j) {
@@ -480,7 +492,7 @@ __device__ __forceinline__ bool narrow_down(Listed l, const E *row, const CutPar
       __syncthreads();
       const unsigned long long last = s.sorted[s.pick];
       place.key = (uint32_t)(last >> 32);
-      place.index = (int)(unsigned)last;
+      place.index = (uint32_t)last;
       __syncthreads();
       return true;
     }
@@ -520,12 +532,12 @@ __device__ __forceinline__ bool narrow_down(Listed l, const E *row, const CutPar
     if (turn == 1) {
       __syncthreads();
       if (lane == 0) s.wave_count[wave] = equals;
-      if (threadIdx.x == 0) s.pick_index = p.V;
+      if (threadIdx.x == 0) s.pick_index = (uint32_t)p.V;
       __syncthreads();
       for (int w = 0; w < wave; ++w) before += (unsigned)s.wave_count[w];
       if (before >= count || before + (unsigned)equals < count) break;  // (uniform: another wavefront has the last)
     }
-    each_piece_of(l, row, p, part, lane, wave, [&](long long at, const float (&v)[8]) {
+    each_piece_of(l, row, p, part, lane, wave, [&](unsigned at, const float (&v)[8]) {
       bool hit[8];
 #pragma unroll
       for (int j = 0; j < 8; ++j) hit[j] = key_of(v[j]) == low;
@@ -584,8 +596,8 @@ template <typename E, bool SAMPLE> __device__ __forceinline__ void cut_row(const
   E *out = SAMPLE ? nullptr : reinterpret_cast<E *>(p.out) + r * p.out_stride;
   const Part part = part_of(p, wave);
   // 1. the sample
-  Ring<E> ring;
-  ring.fill(row, p, part, lane);
+  Ring<E, kAhead> ring;
+  ring.fill(row, (unsigned)p.V, part, lane);
   const Cut cut = cut_of(p, r);
   const bool by_mass = cut.top_p < 1.0f;
   // (top_p's share is of what top_k leaves, whatever min_p says: where there is a share, min_p does not shorten the list)
@@ -597,9 +609,9 @@ template <typename E, bool SAMPLE> __device__ __forceinline__ void cut_row(const
   float largest = -INFINITY;
 #pragma unroll
   for (int i = 0; i < kSample; ++i) {
-    if (ring.at + i * kPiece <= ring.last) {
+    if (part.first + i * kPiece < part.last) {
       float v[8];
-      widen_raw(ring.raw[i], ring.at + i * kPiece, lane, p.V, v);
+      widen_raw(ring.raw[i], part.first + i * kPiece, lane, (unsigned)p.V, v);
       largest = max_of_three(largest, largest_of(v), largest);
     }
   }
@@ -618,7 +630,7 @@ template <typename E, bool SAMPLE> __device__ __forceinline__ void cut_row(const
   if (cut.bad) reference = -INFINITY;
   else if (reference == -INFINITY) {  // (uniform: the sample has no mass)
     float high = -INFINITY;
-    each_piece(row, p, part, lane, [&](long long, long long, const float (&v)[8]) {
+    each_piece(row, p, part, lane, [&](unsigned, unsigned, const float (&v)[8]) {
 #pragma unroll
       for (int j = 0; j < 8; ++j) high = fmaxf(high, v[j]);
     });
@@ -655,7 +667,7 @@ template <typename E, bool SAMPLE> __device__ __forceinline__ void cut_row(const
   int piece = 0, count = 0;  // (count: the wavefront's kept)
   long long tile = (long long)wave * p.tiles_wave;
   const double reference_wide = (double)reference;
-  const auto see = [&](long long from, long long at, const float (&v)[8]) {
+  const auto see = [&](unsigned from, unsigned at, const float (&v)[8]) {
     const float here = largest_of(v);
     high = max_of_three(high, here, high);
     if (need_mass || (SAMPLE && uncut)) mass += mass_of_eight(v, reference_wide, cut.scale);
@@ -675,7 +687,7 @@ template <typename E, bool SAMPLE> __device__ __forceinline__ void cut_row(const
       ++tile; piece = 0; mass = 0.0;
     }
   };
-  ring.run(row, p, lane, see);
+  ring.run(row, (unsigned)p.V, part, lane, see);
   float top, unused;
   block_ends(high, 0.0f, top, unused);
   const double top_wide = (double)top;
@@ -687,7 +699,7 @@ template <typename E, bool SAMPLE> __device__ __forceinline__ void cut_row(const
   if (need_mass) all_mass = block_sum(mass, s.wave_double) * exp2_of((reference_wide - top_wide) * cut.scale);
   bool listed = try_list && join_list(s, list.count, lane, wave, n);
   if (listed && cut.top_k > n && bound > -INFINITY && !by_least) listed = false;  // (there are more below the bound)
-  Place place = {0xFFFFFFFFu, p.V};  // (of the list's entries: their places in the list)
+  Place place = {0xFFFFFFFFu, (uint32_t)p.V};  // (of the list's entries: their places in the list)
   bool found = false;
   if (listed && n <= kFew) {
     const int e = threadIdx.x;
@@ -711,13 +723,13 @@ template <typename E, bool SAMPLE> __device__ __forceinline__ void cut_row(const
       first_n = a + 1 < first_n ? a + 1 : first_n;
     }
     const unsigned long long last = s.sorted[first_n - 1];
-    place = {(uint32_t)(last >> 32), (long long)(unsigned)last};
+    place = {(uint32_t)(last >> 32), (uint32_t)last};
     found = listed;
   }
   // What the order by counting does not show is narrowed down, in the list or, where that does not hold what is asked for, in the row.
 #pragma unroll 1
   while (!found) {
-    place = {0xFFFFFFFFu, p.V};
+    place = {0xFFFFFFFFu, (uint32_t)p.V};
     found = true;
     const Listed in = {listed ? &s : nullptr, n};
 #pragma unroll 1
@@ -748,9 +760,9 @@ template <typename E, bool SAMPLE> __device__ __forceinline__ void cut_row(const
       if (over_least(value_of(mid))) a = mid + 1; else z = mid;
     }
     const uint32_t last = a > key_of(top) ? a - 1 : a;
-    if (last < place.key) place = {last, p.V};
+    if (last < place.key) place = {last, (uint32_t)p.V};
   }
-  const auto kept_at = [&](int e) { return s.list_key[e] < place.key || (s.list_key[e] == place.key && e <= place.index); };
+  const auto kept_at = [&](int e) { return s.list_key[e] < place.key || (s.list_key[e] == place.key && (unsigned)e <= place.index); };
   if (listed) {
     const int each = (n + kThreads - 1) / kThreads, e0 = threadIdx.x * each, e1 = e0 + each < n ? e0 + each : n;
     __syncthreads();
@@ -822,7 +834,7 @@ template <typename E, bool SAMPLE> __device__ __forceinline__ void cut_row(const
   }
 
   // The row's entries, where the list does not hold the kept ones.
-  const auto inside = [&](float x, long long i) {
+  const auto inside = [&](float x, unsigned i) {
     const uint32_t key = key_of(x);
     return x > -INFINITY && (key < place.key || (key == place.key && i <= place.index));
   };
@@ -834,7 +846,7 @@ template <typename E, bool SAMPLE> __device__ __forceinline__ void cut_row(const
       double sum_tile = 0.0;
       piece = 0;
       tile = (long long)wave * p.tiles_wave;
-      each_piece(row, p, part, lane, [&](long long from, long long at, const float (&v)[8]) {
+      each_piece(row, p, part, lane, [&](unsigned from, unsigned at, const float (&v)[8]) {
         float kept[8];
 #pragma unroll
         for (int j = 0; j < 8; ++j) {
@@ -910,7 +922,7 @@ template <typename E, bool SAMPLE> __device__ __forceinline__ void cut_row(const
       }
     }
   } else {
-    each_piece(row, p, part, lane, [&](long long from, long long at, const float (&v)[8]) {
+    each_piece(row, p, part, lane, [&](unsigned from, unsigned at, const float (&v)[8]) {
       float w[8];
 #pragma unroll
       for (int j = 0; j < 8; ++j) {
