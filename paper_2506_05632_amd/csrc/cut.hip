@@ -138,7 +138,7 @@ template <typename T> __device__ __forceinline__ T wave_scan(T v) { return wave_
 template <typename T> __device__ __forceinline__ T wave_sum(T v) { return lane_value(wave_scan(v), 63); }
 
 struct Shared {
-  uint32_t list_key[kList];
+  alignas(16) uint32_t list_key[kList];
   int list_index[kList];
   union {
     unsigned long long histogram[kBuckets];
@@ -146,7 +146,7 @@ struct Shared {
     double masses[kFew];                                    // summed along the order
     unsigned long long weights[kFew];
   };
-  unsigned long long few[kFew], sorted[kFew];  // key and index
+  unsigned long long few[kFew], sorted[kFew];  // key and index (kFew is a multiple of eight)
   uint32_t sample[kThreads];                   // a histogram of the sample's largest
   union {
     double wave_double[kWaves];
@@ -338,6 +338,31 @@ __device__ __forceinline__ int marked_before(const bool (&hit)[8], int &all) {
 // The list: each wavefront's entries in a part of its own, in the order of their indexes; once they are more than it has room for, they are counted only.
 struct Lister {
   int count;
+  // Entries from `bound` on (a number); here: a lane's largest.  Where no lane has two, which is nearly always, a lane's one is its largest.
+  __device__ __forceinline__ void add_from(float bound, Shared &s, int wave, unsigned at, const float (&v)[8], float here) {
+    const unsigned long long lanes = __ballot(here >= bound);
+    if (lanes == 0) return;  // (uniform)
+    int mine = 0, which = 0;
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+      const bool hit = v[j] >= bound;
+      mine += hit ? 1 : 0;
+      which = hit ? j : which;
+    }
+    if (__ballot(mine > 1) == 0) {  // (uniform)
+      const int to = wave * kRoom + __builtin_amdgcn_mbcnt_hi((uint32_t)(lanes >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)lanes, count));
+      count += __popcll(lanes);
+      if (mine != 0 && count <= kRoom) {
+        s.list_key[to] = key_of(here);
+        s.list_index[to] = (int)at + which;
+      }
+      return;
+    }
+    bool hit[8];
+#pragma unroll
+    for (int j = 0; j < 8; ++j) hit[j] = v[j] >= bound;
+    add(s, wave, at, v, hit);
+  }
   __device__ __forceinline__ void add(Shared &s, int wave, unsigned at, const float (&v)[8], const bool (&hit)[8]) {
     int all, to = wave * kRoom + count + marked_before(hit, all);
     count += all;
@@ -378,18 +403,46 @@ __device__ __forceinline__ bool join_list(Shared &s, int count, int lane, int wa
   __syncthreads();
   return true;
 }
-// few[0..n) in order to sorted[0..n): a thread counts what is before its entry.  (200 entries: 3 us as exchanges in LDS, 1 so.)
+// few[0..n) in order to sorted[0..n): a thread counts what is before its entry.
 __device__ __forceinline__ void sort_few(Shared &s, int n) {
   __syncthreads();
+  if ((int)threadIdx.x >= n && (int)threadIdx.x < ((n + 7) & ~7)) s.few[threadIdx.x] = ~0ULL;
+  __syncthreads();
   if ((int)(threadIdx.x & ~63u) < n) {  // (uniform)
-    const unsigned long long mine = (int)threadIdx.x < n ? s.few[threadIdx.x] : ~0ULL;
+    const unsigned long long mine = s.few[threadIdx.x];
     int rank = 0;
-    for (int i = 0; i < (n & ~3); i += 4) {
+    for (int i = 0; i < n; i += 8) {
 #pragma unroll
-      for (int j = 0; j < 4; ++j) rank += s.few[i + j] < mine ? 1 : 0;
+      for (int j = 0; j < 8; ++j) rank += s.few[i + j] < mine ? 1 : 0;
     }
-    for (int i = n & ~3; i < n; ++i) rank += s.few[i] < mine ? 1 : 0;
     if ((int)threadIdx.x < n) s.sorted[rank] = mine;
+  }
+  __syncthreads();
+}
+// The same of the list's first n entries, by key and place: 32 bits are compared, with the entry's key for those behind it, with the next for those before.
+__device__ __forceinline__ void sort_list(Shared &s, int n) {
+  const int e = threadIdx.x;
+  if (e >= n && e < ((n + 31) & ~31)) s.list_key[e] = ~0u;
+  __syncthreads();
+  if ((int)(threadIdx.x & ~63u) < n) {  // (uniform)
+    const uint32_t mine = e < n ? s.list_key[e] : 0;
+    int rank = 0;
+    for (int i = 0; i < n; i += 32) {  // (uniform)
+      uint4 k[8];
+#pragma unroll
+      for (int j = 0; j < 8; ++j) k[j] = *reinterpret_cast<const uint4 *>(s.list_key + i + 4 * j);
+#pragma unroll
+      for (int j = 0; j < 8; ++j) {
+        const uint32_t to = mine + (i + 4 * j < (e & ~3) ? 1 : 0);
+        rank += (k[j].x < to ? 1 : 0) + (k[j].y < to ? 1 : 0) + (k[j].z < to ? 1 : 0) + (k[j].w < to ? 1 : 0);
+      }
+    }
+#pragma unroll
+    for (int j = 0; j < 3; ++j) {  // equals before it among its four
+      const int f = (e & ~3) + j;
+      rank += f < e && s.list_key[f] == mine ? 1 : 0;
+    }
+    if (e < n) s.sorted[rank] = (unsigned long long)mine << 32 | (unsigned)e;
   }
   __syncthreads();
 }
@@ -599,6 +652,7 @@ template <typename E, bool SAMPLE> __device__ __forceinline__ void cut_row(const
   Ring<E, kAhead> ring;
   ring.fill(row, (unsigned)p.V, part, lane);
   const Cut cut = cut_of(p, r);
+  const float first_u = SAMPLE && (int)threadIdx.x < p.S ? p.u[r * p.u_stride + threadIdx.x] : 0.0f;  // (of a list's tokens: waited for later)
   const bool by_mass = cut.top_p < 1.0f;
   // (top_p's share is of what top_k leaves, whatever min_p says: where there is a share, min_p does not shorten the list)
   const bool least_too = cut.min_p > 0.0f && !by_mass;
@@ -667,6 +721,7 @@ template <typename E, bool SAMPLE> __device__ __forceinline__ void cut_row(const
   int piece = 0, count = 0;  // (count: the wavefront's kept)
   long long tile = (long long)wave * p.tiles_wave;
   const double reference_wide = (double)reference;
+  const float from_number = fmaxf(bound, -3.4028234663852886e38f);
   const auto see = [&](unsigned from, unsigned at, const float (&v)[8]) {
     const float here = largest_of(v);
     high = max_of_three(high, here, high);
@@ -675,12 +730,7 @@ template <typename E, bool SAMPLE> __device__ __forceinline__ void cut_row(const
 #pragma unroll
       for (int j = 0; j < 8; ++j) count += __popcll(__ballot(v[j] > -INFINITY));
     }
-    if (try_list && __ballot(here >= bound) != 0) {
-      bool hit[8];
-#pragma unroll
-      for (int j = 0; j < 8; ++j) hit[j] = v[j] >= bound && v[j] > -INFINITY;
-      list.add(s, wave, at, v, hit);
-    }
+    if (try_list) list.add_from(from_number, s, wave, at, v, here);
     if (SAMPLE && uncut && (++piece == p.pieces_tile || from + kPiece >= p.V)) {
       const double sum = wave_sum(mass);
       if (lane == 0) s.along[tile] = sum;
@@ -703,8 +753,7 @@ template <typename E, bool SAMPLE> __device__ __forceinline__ void cut_row(const
   bool found = false;
   if (listed && n <= kFew) {
     const int e = threadIdx.x;
-    if (e < n) s.few[e] = (unsigned long long)s.list_key[e] << 32 | (unsigned)e;
-    sort_few(s, n);
+    sort_list(s, n);
     int first_n = cut.top_k > 0 && cut.top_k < n ? (int)cut.top_k : n;
     if (by_mass) {  // masses summed along the order
       const double mine = e < n ? mass_of(value_of((uint32_t)(s.sorted[e] >> 32)), top_wide, cut.scale) : 0.0;
@@ -789,7 +838,7 @@ template <typename E, bool SAMPLE> __device__ __forceinline__ void cut_row(const
       total = s.along[n - 1];
       const double log_total = log(total);
       for (int i = threadIdx.x; i < p.S; i += kThreads) {
-        const float u = p.u[r * p.u_stride + i];
+        const float u = i < kThreads ? first_u : p.u[r * p.u_stride + i];
         const double target = (double)fmaxf(u, 0.0f) * total;
         int a = 0, z = n;  // the first whose sum is over the target
         while (a < z) {
