@@ -46,6 +46,13 @@ template <int G, typename S> struct Slab {
   float scale[kGroups];
   float shift[kGroups];  // -(16 + zero)
 };
+// Four slabs that follow each other, their scales and zeros as they lie in memory.
+template <int G, typename S> struct Batch {
+  static constexpr int kSlabs = 4, kGroups = kSlabs * 128 / G, kScaleWords = kGroups * sizeof(S) / 4, kZeroWords = kGroups / 4;
+  uint32_t words[kSlabs][4];
+  uint32_t scale[kScaleWords];
+  uint32_t zero[kZeroWords];
+};
 
 // Column of a slab where the quarter's word of a step starts.
 template <int G> __device__ __forceinline__ int column_of(int step, int quarter) {
@@ -91,13 +98,60 @@ __device__ __forceinline__ Slab<G, S> load_last_slab(const MatvecParams &p, cons
   load_scales(s, p, scales, zeros, slab);
   return s;
 }
+// N words from anywhere.
+template <int N> __device__ __forceinline__ void load_words(uint32_t (&w)[N], const void *from) {
+  const uint8_t *at = reinterpret_cast<const uint8_t *>(from);
+  if constexpr (N == 1) {
+    w[0] = *reinterpret_cast<const word1_byte *>(at);
+  } else if constexpr (N == 2) {
+    const word2_byte v = *reinterpret_cast<const word2_byte *>(at);
+    w[0] = v.x; w[1] = v.y;
+  } else {
+#pragma unroll
+    for (int i = 0; i < N; i += 4) {
+      const word4_byte v = *reinterpret_cast<const word4_byte *>(at + 4 * i);
+      w[i] = v.x; w[i + 1] = v.y; w[i + 2] = v.z; w[i + 3] = v.w;
+    }
+  }
+}
+template <int G, typename S> __device__ __forceinline__ void load_batch(Batch<G, S> &b, const uint8_t *codes, const S *scales, const uint8_t *zeros, int slab, int quarter) {
+#pragma unroll
+  for (int i = 0; i < Batch<G, S>::kSlabs; ++i) {
+    const uint8_t *from = codes + (long long)slab * 64 + i * 64;
+    if constexpr (G == 128) {
+      load_words(b.words[i], from + 16 * quarter);
+    } else if constexpr (G == 64) {
+      const word2_byte l = *reinterpret_cast<const word2_byte *>(from + 8 * quarter), h = *reinterpret_cast<const word2_byte *>(from + 32 + 8 * quarter);
+      b.words[i][0] = l.x; b.words[i][1] = l.y; b.words[i][2] = h.x; b.words[i][3] = h.y;
+    } else {
+#pragma unroll
+      for (int j = 0; j < 4; ++j) b.words[i][j] = *reinterpret_cast<const word1_byte *>(from + 16 * j + 4 * quarter);
+    }
+  }
+  load_words(b.scale, scales + (long long)slab * (128 / G));
+  if (zeros != nullptr) load_words(b.zero, zeros + (long long)slab * (128 / G));
+}
+template <int G, typename S> __device__ __forceinline__ Slab<G, S> slab_of(const Batch<G, S> &b, int i, bool zeros) {
+  Slab<G, S> s;
+#pragma unroll
+  for (int j = 0; j < 4; ++j) s.words[j] = b.words[i][j];
+#pragma unroll
+  for (int g = 0; g < 128 / G; ++g) {
+    const int at = i * (128 / G) + g;
+    if constexpr (sizeof(S) == 4) s.scale[g] = __uint_as_float(b.scale[at]);
+    else s.scale[g] = __uint_as_float(at % 2 == 0 ? b.scale[at / 2] << 16 : b.scale[at / 2] & 0xFFFF0000u);
+    s.shift[g] = zeros ? -16.0f - (float)((b.zero[at / 4] >> (8 * (at % 4))) & 255u) : -24.0f;
+  }
+  return s;
+}
 
-// Adds a slab's products to a tile's sums; `here`: its place in the chunk.
-template <int TILES, int PARTS, int G, typename S>
-__device__ __forceinline__ void add_slab(f32x4 (&total)[TILES], const Slab<G, S> &s, const uint4 *s_x, const float *s_sum, const int (&at_x)[TILES], int rows, int here,
-                                         int quarter) {
+// Adds a slab's products to the sums of WIDE tiles of columns, which share what is read of x; `here`: its place in the part of x in LDS.
+template <int TILES, int PARTS, int G, typename S, int WIDE>
+__device__ __forceinline__ void add_slab(f32x4 (&total)[WIDE][TILES], const Slab<G, S> (&s)[WIDE], const uint4 *s_x, const float *s_sum, const int (&at_x)[TILES], int rows,
+                                         int here, int quarter) {
   constexpr int kSteps = G / 32;  // of a group
-  f32x4 sum[TILES], low[TILES];
+  f32x4 sum[WIDE][TILES], low[WIDE][TILES];
+  int from = here * 16 * PARTS * rows;  // of x: an addition a read (all of them at once, as they follow from `here`, would take more registers than there are)
 #pragma unroll
   for (int step = 0; step < 4; ++step) {
     const int g = step / kSteps;
@@ -106,173 +160,317 @@ __device__ __forceinline__ void add_slab(f32x4 (&total)[TILES], const Slab<G, S>
       for (int t = 0; t < TILES; ++t) {
         const f32x4 sx = *reinterpret_cast<const f32x4 *>(s_sum + (here * (128 / G) + g) * (TILES * 16) + 16 * t + 4 * quarter);
 #pragma unroll
-        for (int j = 0; j < 4; ++j) sum[t][j] = s.shift[g] * sx[j];
-        low[t] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
-      }
-    }
-    const bf16x8 w = widen_codes(s.words[step]);
+        for (int w = 0; w < WIDE; ++w) {
 #pragma unroll
-    for (int t = 0; t < TILES; ++t) {
-#pragma unroll
-      for (int part = 0; part < PARTS; ++part) {
-        const bf16x8 a = __builtin_bit_cast(bf16x8, s_x[((here * 4 + step) * PARTS + part) * 4 * rows + at_x[t]]);
-        if (part == 0) sum[t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, w, sum[t], 0, 0, 0);
-        else low[t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, w, low[t], 0, 0, 0);
-      }
-    }
-    if (step % kSteps == kSteps - 1) {
-#pragma unroll
-      for (int t = 0; t < TILES; ++t)
-#pragma unroll
-        for (int j = 0; j < 4; ++j) total[t][j] = fmaf(s.scale[g], PARTS > 1 ? sum[t][j] + low[t][j] : sum[t][j], total[t][j]);
-    }
-  }
-}
-
-// x of a chunk of columns to LDS, as the operands lie: [slab][step][part][quarter][row], 16 bytes each; and the groups' sums [group][16 rows of a tile].
-template <int TILES, int PARTS, int G, typename X>
-__device__ __forceinline__ void stage_x(const MatvecParams &p, long long r0, int rows, int chunk, int slabs, uint4 *s_x, float *s_sum) {
-  const unsigned pieces = (unsigned)slabs * 16, all = pieces * (unsigned)rows;
-  for (unsigned i = threadIdx.x; i < all; i += blockDim.x) {
-    const unsigned r = i / pieces, piece = i - r * pieces;
-    const long long at = ((long long)chunk * p.chunk_slabs * 16 + piece) * 8;
-    const X *row = reinterpret_cast<const X *>(p.x) + (r0 + r) * p.x_stride;
-    float v[8];
-    if (at < p.D) {
-      load_first<8>(row + at, p.D - at, v);
-    } else {
-#pragma unroll
-      for (int j = 0; j < 8; ++j) v[j] = 0.0f;
-    }
-    float sum = 0.0f;
-#pragma unroll
-    for (int j = 0; j < 8; ++j) sum += v[j];
-    sum = sum_lanes<G / 8>(sum);
-    const unsigned slab = piece >> 4, q = piece & 15;
-    const unsigned step = G == 128 ? q & 3 : G == 64 ? (q >> 3) * 2 + (q & 1) : q >> 2;
-    const unsigned quarter = G == 128 ? q >> 2 : G == 64 ? (q >> 1) & 3 : q & 3;
-    if ((q & (G / 8 - 1)) == 0) s_sum[(slab * (128 / G) + q / (G / 8)) * (TILES * 16) + r] = sum;
-#pragma unroll
-    for (int part = 0; part < PARTS; ++part) {
-      const uint4 w = make_uint4(narrow_pair(v[0], v[4]), narrow_pair(v[1], v[5]), narrow_pair(v[2], v[6]), narrow_pair(v[3], v[7]));
-      s_x[(((slab * 4 + step) * PARTS + part) * 4 + quarter) * rows + r] = w;
-      if (part + 1 < PARTS) {  // what is left is exact
-        const uint32_t in[4] = {w.x, w.y, w.z, w.w};
-#pragma unroll
-        for (int j = 0; j < 4; ++j) {
-          float a, b;
-          split_pair(in[j], a, b);
-          v[j] -= a;
-          v[j + 4] -= b;
+          for (int j = 0; j < 4; ++j) sum[w][t][j] = s[w].shift[g] * sx[j];
+          low[w][t] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
         }
       }
     }
+    bf16x8 codes[WIDE];
+#pragma unroll
+    for (int w = 0; w < WIDE; ++w) codes[w] = widen_codes(s[w].words[step]);
+#pragma unroll
+    for (int part = 0; part < PARTS; ++part) {
+      asm volatile("" : "+s"(from));
+#pragma unroll
+      for (int t = 0; t < TILES; ++t) {
+        const bf16x8 a = __builtin_bit_cast(bf16x8, s_x[from + at_x[t]]);
+#pragma unroll
+        for (int w = 0; w < WIDE; ++w) {
+          if (part == 0) sum[w][t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, codes[w], sum[w][t], 0, 0, 0);
+          else low[w][t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, codes[w], low[w][t], 0, 0, 0);
+        }
+      }
+      from += 4 * rows;
+    }
+    if (step % kSteps == kSteps - 1) {
+#pragma unroll
+      for (int w = 0; w < WIDE; ++w)
+#pragma unroll
+        for (int t = 0; t < TILES; ++t)
+#pragma unroll
+          for (int j = 0; j < 4; ++j) total[w][t][j] = fmaf(s[w].scale[g], PARTS > 1 ? sum[w][t][j] + low[w][t][j] : sum[w][t][j], total[w][t][j]);
+    }
+    if (TILES * PARTS > 2 || step == 3) __builtin_amdgcn_sched_barrier(0);  // (what later steps read of x, read ahead, would take more registers than there are)
   }
 }
 
-template <int TILES, int PARTS, int G, typename S, typename X>
-__global__ void __launch_bounds__(kMatvecThreads) matvec_quantized_kernel(const MatvecParams p) {
-  constexpr int kAhead = 4;  // slabs that are fetched ahead
+// x to LDS as the operands lie: [slab][step][part][quarter][row], 16 bytes each; and the groups' sums [group][16 rows of a tile].  A piece is eight columns of a row.
+template <typename X> struct Piece;
+template <> struct Piece<float> { float4_any a, b; };
+template <> struct Piece<uint16_t> { word4_any a; };
+template <typename X> __device__ __forceinline__ Piece<X> load_x(const MatvecParams &p, long long r, int at) {
+  const X *row = reinterpret_cast<const X *>(p.x) + r * p.x_stride;
+  const int D = (int)p.D;
+  Piece<X> v;
+  if (at + 8 <= D) {
+    v.a = *reinterpret_cast<const decltype(v.a) *>(row + at);
+    if constexpr (sizeof(X) == 4) v.b = *reinterpret_cast<const decltype(v.b) *>(row + at + 4);
+  } else {  // nothing behind the row's end
+    X e[8];
+#pragma unroll
+    for (int j = 0; j < 8; ++j) e[j] = row[at + j < D ? at + j : D - 1];
+#pragma unroll
+    for (int j = 0; j < 8; ++j) e[j] = at + j < D ? e[j] : (X)0;
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      if constexpr (sizeof(X) == 4) {
+        v.a[j] = e[j]; v.b[j] = e[j + 4];
+      } else {
+        v.a[j] = (uint32_t)e[2 * j] | (uint32_t)e[2 * j + 1] << 16;
+      }
+    }
+  }
+  return v;
+}
+template <int TILES, int PARTS, int G, typename X> __device__ __forceinline__ void store_x(const Piece<X> &from, unsigned r, unsigned piece, int rows, uint4 *s_x, float *s_sum) {
+  float v[8];
+#pragma unroll
+  for (int j = 0; j < 4; ++j) {
+    if constexpr (sizeof(X) == 4) {
+      v[j] = from.a[j]; v[j + 4] = from.b[j];
+    } else {
+      split_pair(from.a[j], v[2 * j], v[2 * j + 1]);
+    }
+  }
+  float sum = ((v[0] + v[1]) + (v[2] + v[3])) + ((v[4] + v[5]) + (v[6] + v[7]));
+  sum = sum_lanes<G / 8>(sum);
+  const unsigned slab = piece >> 4, q = piece & 15;
+  const unsigned step = G == 128 ? q & 3 : G == 64 ? (q >> 3) * 2 + (q & 1) : q >> 2;
+  const unsigned quarter = G == 128 ? q >> 2 : G == 64 ? (q >> 1) & 3 : q & 3;
+  if ((q & (G / 8 - 1)) == 0) s_sum[(slab * (128 / G) + q / (G / 8)) * (TILES * 16) + r] = sum;
+  uint4 *to = s_x + ((slab * 4 + step) * PARTS * 4 + quarter) * rows + r;
+#pragma unroll
+  for (int part = 0; part < PARTS; ++part) {
+    const uint4 w = make_uint4(narrow_pair(v[0], v[4]), narrow_pair(v[1], v[5]), narrow_pair(v[2], v[6]), narrow_pair(v[3], v[7]));
+    to[part * 4 * rows] = w;
+    if (part + 1 < PARTS) {  // what is left is exact
+      const uint32_t in[4] = {w.x, w.y, w.z, w.w};
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        float a, b;
+        split_pair(in[j], a, b);
+        v[j] -= a;
+        v[j + 4] -= b;
+      }
+    }
+  }
+}
+
+// The sums of wavefronts that share tiles of columns are joined, and the tiles written.
+template <int TILES, int WIDE>
+__device__ __forceinline__ void finish_tiles(const MatvecParams &p, f32x4 (&total)[WIDE][TILES], float *s_join, int share, int part_of, int wave, int lane, long long r0, int rows,
+                                             const long long (&n0)[WIDE]) {
+  const int column = lane & 15, quarter = lane >> 4;
+  if (share > 1) {
+    __syncthreads();
+#pragma unroll
+    for (int w = 0; w < WIDE; ++w)
+#pragma unroll
+      for (int t = 0; t < TILES; ++t) *reinterpret_cast<f32x4 *>(s_join + (((wave * WIDE + w) * TILES + t) * 64 + lane) * 4) = total[w][t];
+    __syncthreads();
+    if (part_of == 0) {
+      for (int other = 1; other < share; ++other)
+#pragma unroll
+        for (int w = 0; w < WIDE; ++w)
+#pragma unroll
+          for (int t = 0; t < TILES; ++t) {
+            const f32x4 add = *reinterpret_cast<const f32x4 *>(s_join + ((((wave + other) * WIDE + w) * TILES + t) * 64 + lane) * 4);
+#pragma unroll
+            for (int j = 0; j < 4; ++j) total[w][t][j] += add[j];
+          }
+    }
+  }
+  if (part_of != 0) return;
+#pragma unroll
+  for (int w = 0; w < WIDE; ++w) {
+    const long long n = n0[w] + column;
+    if (n0[w] < 0 || n >= p.N) continue;
+#pragma unroll
+    for (int t = 0; t < TILES; ++t)
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        const int r = 16 * t + 4 * quarter + j;
+        if (r < rows) {
+          const long long to = (r0 + r) * p.out_stride + n;
+          if (p.out_type == LLC_F32) reinterpret_cast<float *>(p.out)[to] = total[w][t][j];
+          else reinterpret_cast<uint16_t *>(p.out)[to] = narrow<uint16_t>(total[w][t][j]);
+        }
+      }
+  }
+}
+
+template <typename S> struct Row {  // of the layer
+  const uint8_t *codes;
+  const S *scales;
+  const uint8_t *zeros;
+};
+template <typename S> __device__ __forceinline__ Row<S> row_of(const MatvecParams &p, long long n) {
+  const long long at = n < p.N ? n : p.N - 1;
+  return {p.codes + at * p.codes_stride, reinterpret_cast<const S *>(p.scales) + at * p.scales_stride, p.zeros != nullptr ? p.zeros + at * p.zeros_stride : nullptr};
+}
+
+// x in LDS as a whole, put there once; a workgroup takes several blocks of tiles with it.  Wavefronts that share a tile take a run of its slabs each, four at a
+// time, of which the next four are asked for before these are multiplied.
+template <int PARTS, int G, typename S, typename X> __global__ void __launch_bounds__(kMatvecThreads, 4) matvec_quantized_kernel(const MatvecParams p) {
+  constexpr int TILES = 1, WIDE = 1, kSlabs = Batch<G, S>::kSlabs;
   extern __shared__ __align__(16) char s_dyn[];
-  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), waves = blockDim.x >> 6;
-  const int share = 1 << p.share_log, part_of = wave & (share - 1), tile_of = wave >> p.share_log, tiles_each = waves >> p.share_log;
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int share = 1 << p.share_log, part_of = wave & (share - 1), tile_of = wave >> p.share_log, tiles_each = (blockDim.x >> 6) >> p.share_log;
   const int column = lane & 15, quarter = lane >> 4;
   const long long r0 = (long long)blockIdx.y * kMatvecRows;
   const int rows = (int)(p.R - r0 < 16 * TILES ? p.R - r0 : 16 * TILES);
   uint4 *s_x = reinterpret_cast<uint4 *>(s_dyn);
-  float *s_sum = reinterpret_cast<float *>(s_dyn + (size_t)p.chunk_slabs * 256 * PARTS * rows);
-  float *s_join = s_sum + p.chunk_slabs * (128 / G) * (TILES * 16);
-  const int chunks = (p.slabs + p.chunk_slabs - 1) / p.chunk_slabs, turns = p.chunk_slabs >> p.share_log;
-  const int whole = (int)(p.D / 128);  // whole slabs
+  float *s_sum = reinterpret_cast<float *>(s_dyn + (size_t)p.slabs * 256 * PARTS * rows);
+  float *s_join = s_sum + p.slabs * (128 / G) * (TILES * 16);
+  const int whole = (int)(p.D / 128), each = (p.slabs + share - 1) >> p.share_log;
+  const int begin = part_of * each < whole ? part_of * each : whole, end = begin + each < whole ? begin + each : whole;
+  const bool last_too = whole < p.slabs && part_of == whole / each;
   int at_x[TILES];
 #pragma unroll
   for (int t = 0; t < TILES; ++t) at_x[t] = quarter * rows + (16 * t + column < rows ? 16 * t + column : rows - 1);
   for (unsigned block = blockIdx.x; block < p.tile_blocks; block += gridDim.x) {
-    const long long n0 = ((long long)block * tiles_each + tile_of) * 16, n = n0 + column < p.N ? n0 + column : p.N - 1;
-    const uint8_t *codes = p.codes + n * p.codes_stride;
-    const S *scales = reinterpret_cast<const S *>(p.scales) + n * p.scales_stride;
-    const uint8_t *zeros = p.zeros != nullptr ? p.zeros + n * p.zeros_stride : nullptr;
-    f32x4 total[TILES];
+    const long long n0[WIDE] = {((long long)block * tiles_each + tile_of) * 16};
+    const Row<S> row = row_of<S>(p, n0[0] + column);
+    f32x4 total[WIDE][TILES];
 #pragma unroll
-    for (int t = 0; t < TILES; ++t) total[t] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
-    Slab<G, S> ring[kAhead];
-    // (a slab behind the last whole one is that one again, and is not added)
-    const auto fetch = [&](int turn) {
-      const int slab = turn * share + part_of;
-      return load_slab<G, S>(p, codes, scales, zeros, slab < whole ? slab : whole - 1, quarter);
-    };
-    for (int chunk = 0; chunk < chunks; ++chunk) {
-      if (whole > 0) {
+    for (int t = 0; t < TILES; ++t) total[0][t] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+    Batch<G, S> batch[2];
+    if (begin + kSlabs <= end) load_batch(batch[0], row.codes, row.scales, row.zeros, begin, quarter);
+    if (block == blockIdx.x) {
+      const unsigned pieces = (unsigned)p.slabs * 16;
+      for (unsigned r = 0; r < (unsigned)rows; ++r)
+        for (unsigned piece = threadIdx.x; piece < pieces; piece += blockDim.x) {
+          const Piece<X> v = load_x<X>(p, r0 + r, (int)piece * 8);
+          store_x<TILES, PARTS, G, X>(v, r, piece, rows, s_x, s_sum);
+        }
+      __syncthreads();
+    }
+    int slab = begin;
+#pragma unroll 1
+    for (; slab + kSlabs <= end; slab += 2 * kSlabs) {
 #pragma unroll
-        for (int i = 0; i < kAhead; ++i) ring[i] = fetch(chunk * turns + i);
-      }
-      const int left = p.slabs - chunk * p.chunk_slabs;
-      if (chunks > 1 || block == blockIdx.x) {
-        __syncthreads();
-        stage_x<TILES, PARTS, G, X>(p, r0, rows, chunk, left < p.chunk_slabs ? left : p.chunk_slabs, s_x, s_sum);
-        __syncthreads();
-      }
-      const int whole_here = whole - chunk * p.chunk_slabs;
-      for (int turn0 = 0; turn0 < turns; turn0 += kAhead) {
+      for (int half = 0; half < 2; ++half) {
+        const int at = slab + half * kSlabs;
+        if (at + kSlabs <= end) {  // (uniform)
+          if (at + 2 * kSlabs <= end) load_batch(batch[1 - half], row.codes, row.scales, row.zeros, at + kSlabs, quarter);
 #pragma unroll
-        for (int i = 0; i < kAhead; ++i) {
-          const int turn = turn0 + i, here = turn * share + part_of;
-          if (turn < turns && here < whole_here) {  // (uniform)
-            add_slab<TILES, PARTS, G, S>(total, ring[i], s_x, s_sum, at_x, rows, here, quarter);
-            ring[i] = fetch(chunk * turns + turn + kAhead);
+          for (int i = 0; i < kSlabs; ++i) {
+            const Slab<G, S> s[WIDE] = {slab_of(batch[half], i, row.zeros != nullptr)};
+            add_slab<TILES, PARTS, G, S, WIDE>(total, s, s_x, s_sum, at_x, rows, at + i, quarter);
           }
         }
       }
-      if (whole < p.slabs && left <= p.chunk_slabs && (whole_here & (share - 1)) == part_of)  // (uniform)
-        add_slab<TILES, PARTS, G, S>(total, load_last_slab<G, S>(p, codes, scales, zeros, whole, quarter), s_x, s_sum, at_x, rows, whole_here, quarter);
     }
-    if (share > 1) {
-      __syncthreads();
-#pragma unroll
-      for (int t = 0; t < TILES; ++t) *reinterpret_cast<f32x4 *>(s_join + ((wave * TILES + t) * 64 + lane) * 4) = total[t];
-      __syncthreads();
-      if (part_of == 0) {
-        for (int other = 1; other < share; ++other)
-#pragma unroll
-          for (int t = 0; t < TILES; ++t) {
-            const f32x4 add = *reinterpret_cast<const f32x4 *>(s_join + (((wave + other) * TILES + t) * 64 + lane) * 4);
-#pragma unroll
-            for (int j = 0; j < 4; ++j) total[t][j] += add[j];
-          }
-      }
+#pragma unroll 1
+    for (slab = begin + (end - begin) / kSlabs * kSlabs; slab < end + (last_too ? 1 : 0); ++slab) {  // fewer than four, and the row's end
+      const Slab<G, S> s[WIDE] = {slab < whole ? load_slab<G, S>(p, row.codes, row.scales, row.zeros, slab, quarter)
+                                               : load_last_slab<G, S>(p, row.codes, row.scales, row.zeros, slab, quarter)};
+      add_slab<TILES, PARTS, G, S, WIDE>(total, s, s_x, s_sum, at_x, rows, slab, quarter);
     }
-    if (part_of == 0 && n0 + column < p.N) {
-#pragma unroll
-      for (int t = 0; t < TILES; ++t)
-#pragma unroll
-        for (int j = 0; j < 4; ++j) {
-          const int r = 16 * t + 4 * quarter + j;
-          if (r < rows) {
-            const long long to = (r0 + r) * p.out_stride + n0 + column;
-            if (p.out_type == LLC_F32) reinterpret_cast<float *>(p.out)[to] = total[t][j];
-            else reinterpret_cast<uint16_t *>(p.out)[to] = narrow<uint16_t>(total[t][j]);
-          }
-        }
-    }
+    int lane_here = lane;
+    asm volatile("" : "+v"(lane_here));  // (or every address of the output would be kept in registers from block to block)
+    finish_tiles<TILES, WIDE>(p, total, s_join, share, part_of, wave, lane_here, r0, rows, n0);
   }
 }
 
-template <int PARTS, int G, typename S, typename X>
-hipError_t by_tiles(const MatvecParams &p, int tiles, dim3 grid, int threads, size_t lds, hipStream_t st) {
-  switch (tiles) {
-    case 1: matvec_quantized_kernel<1, PARTS, G, S, X><<<grid, threads, lds, st>>>(p); break;
-    case 2: matvec_quantized_kernel<2, PARTS, G, S, X><<<grid, threads, lds, st>>>(p); break;
-    case 3: matvec_quantized_kernel<3, PARTS, G, S, X><<<grid, threads, lds, st>>>(p); break;
-    default: matvec_quantized_kernel<4, PARTS, G, S, X><<<grid, threads, lds, st>>>(p); break;
+// x by parts of a slab or a few, in two places of LDS in turn: the next part is asked for before this one is multiplied, and put in its place after.  A wavefront
+// has two tiles of columns, so that what it reads of x serves both, and every workgroup takes its tiles through all of x once.
+template <int TILES, int PARTS, int G, typename S, typename X>
+__global__ void __launch_bounds__(kMatvecThreads, 2) matvec_streamed_kernel(const MatvecParams p) {
+  constexpr int WIDE = 2, kMost = kStreamedPieces<X>;
+  extern __shared__ __align__(16) char s_dyn[];
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int share = 1 << p.share_log, part_of = wave & (share - 1), tile_of = wave >> p.share_log, tiles_each = (blockDim.x >> 6) >> p.share_log;
+  const int column = lane & 15, quarter = lane >> 4;
+  const long long r0 = (long long)blockIdx.y * kMatvecRows;
+  const int rows = (int)(p.R - r0 < 16 * TILES ? p.R - r0 : 16 * TILES);
+  const int place_x = 256 * PARTS * rows << p.chunk_log, place = place_x + ((128 / G) * TILES * 64 << p.chunk_log);
+  float *s_join = reinterpret_cast<float *>(s_dyn + 2 * place);
+  const int whole = (int)(p.D / 128), chunks = (p.slabs + (1 << p.chunk_log) - 1) >> p.chunk_log;
+  int at_x[TILES];
+#pragma unroll
+  for (int t = 0; t < TILES; ++t) at_x[t] = quarter * rows + (16 * t + column < rows ? 16 * t + column : rows - 1);
+  const unsigned pieces_log = p.chunk_log + 4, all = (unsigned)rows << pieces_log;
+  {
+    long long n0[WIDE];
+    Row<S> row[WIDE];
+    f32x4 total[WIDE][TILES];
+#pragma unroll
+    for (int w = 0; w < WIDE; ++w) {
+      const int tile = tile_of + w * tiles_each;
+      const long long at = (long long)blockIdx.x * p.block_tiles + tile;
+      n0[w] = tile < p.block_tiles && at * 16 < p.N ? at * 16 : -1;
+      row[w] = row_of<S>(p, (n0[w] < 0 ? 0 : n0[w]) + column);
+#pragma unroll
+      for (int t = 0; t < TILES; ++t) total[w][t] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+    }
+    Piece<X> v[kMost];
+    const auto ask = [&](int chunk) {
+#pragma unroll
+      for (int i = 0; i < kMost; ++i) {
+        const unsigned at = i * kMatvecThreads + threadIdx.x, r = at >> pieces_log, first = (unsigned)chunk << pieces_log;
+        if (at < all) v[i] = (int)(first + at - (r << pieces_log)) * 8 < p.D ? load_x<X>(p, r0 + r, (int)(first + at - (r << pieces_log)) * 8) : Piece<X>{};
+      }
+    };
+    Slab<G, S> slab[WIDE];
+    const auto fetch = [&](int of) {
+#pragma unroll
+      for (int w = 0; w < WIDE; ++w) slab[w] = load_slab<G, S>(p, row[w].codes, row[w].scales, row[w].zeros, of, quarter);
+    };
+    ask(0);
+    if (part_of < whole) fetch(part_of);
+#pragma unroll 1
+    for (int chunk = 0; chunk < chunks; ++chunk) {
+      char *at_place = s_dyn + ((chunk & 1) != 0 ? place : 0);
+      uint4 *s_x = reinterpret_cast<uint4 *>(at_place);
+      float *s_sum = reinterpret_cast<float *>(at_place + place_x);
+#pragma unroll
+      for (int i = 0; i < kMost; ++i) {
+        const unsigned at = i * kMatvecThreads + threadIdx.x, r = at >> pieces_log;
+        if (at < all) store_x<TILES, PARTS, G, X>(v[i], r, at - (r << pieces_log), rows, s_x, s_sum);
+      }
+      if (chunk + 1 < chunks) ask(chunk + 1);
+      __syncthreads();
+#pragma unroll 1
+      for (int here = part_of; here < 1 << p.chunk_log; here += share) {
+        const int at = (chunk << p.chunk_log) + here;
+        if (at < whole) {  // (uniform)
+          Slab<G, S> now[WIDE];
+#pragma unroll
+          for (int w = 0; w < WIDE; ++w) now[w] = slab[w];
+          if (at + share < whole) fetch(at + share);
+          add_slab<TILES, PARTS, G, S, WIDE>(total, now, s_x, s_sum, at_x, rows, here, quarter);
+        } else if (at < p.slabs) {  // the row's end
+#pragma unroll
+          for (int w = 0; w < WIDE; ++w) slab[w] = load_last_slab<G, S>(p, row[w].codes, row[w].scales, row[w].zeros, at, quarter);
+          add_slab<TILES, PARTS, G, S, WIDE>(total, slab, s_x, s_sum, at_x, rows, here, quarter);
+        }
+      }
+    }
+    finish_tiles<TILES, WIDE>(p, total, s_join, share, part_of, wave, lane, r0, rows, n0);
   }
+}
+
+template <int TILES, int PARTS, int G, typename S, typename X> hipError_t launch_tiles(const MatvecParams &p, dim3 grid, size_t lds, hipStream_t st) {
+  if (p.streamed == 0) matvec_quantized_kernel<PARTS, G, S, X><<<grid, kMatvecThreads, lds, st>>>(p);  // (up to 16 rows)
+  else matvec_streamed_kernel<TILES, PARTS, G, S, X><<<grid, kMatvecThreads, lds, st>>>(p);
   return hipGetLastError();
 }
-template <int PARTS, typename X>
-hipError_t launch_matvec(const MatvecParams &p, int tiles, int group, int scales_type, dim3 grid, int threads, size_t lds, hipStream_t st) {
+template <int PARTS, int G, typename S, typename X> hipError_t by_tiles(const MatvecParams &p, int tiles, dim3 grid, size_t lds, hipStream_t st) {
+  switch (tiles) {
+    case 1: return launch_tiles<1, PARTS, G, S, X>(p, grid, lds, st);
+    case 2: return launch_tiles<2, PARTS, G, S, X>(p, grid, lds, st);
+    case 3: return launch_tiles<3, PARTS, G, S, X>(p, grid, lds, st);
+    default: return launch_tiles<4, PARTS, G, S, X>(p, grid, lds, st);
+  }
+}
+template <int PARTS, typename X> hipError_t launch_matvec(const MatvecParams &p, int tiles, int group, int scales_type, dim3 grid, size_t lds, hipStream_t st) {
   const bool wide = scales_type == LLC_F32;
-  if (group == 128) return wide ? by_tiles<PARTS, 128, float, X>(p, tiles, grid, threads, lds, st) : by_tiles<PARTS, 128, uint16_t, X>(p, tiles, grid, threads, lds, st);
-  if (group == 64) return wide ? by_tiles<PARTS, 64, float, X>(p, tiles, grid, threads, lds, st) : by_tiles<PARTS, 64, uint16_t, X>(p, tiles, grid, threads, lds, st);
-  return wide ? by_tiles<PARTS, 32, float, X>(p, tiles, grid, threads, lds, st) : by_tiles<PARTS, 32, uint16_t, X>(p, tiles, grid, threads, lds, st);
+  if (group == 128) return wide ? by_tiles<PARTS, 128, float, X>(p, tiles, grid, lds, st) : by_tiles<PARTS, 128, uint16_t, X>(p, tiles, grid, lds, st);
+  if (group == 64) return wide ? by_tiles<PARTS, 64, float, X>(p, tiles, grid, lds, st) : by_tiles<PARTS, 64, uint16_t, X>(p, tiles, grid, lds, st);
+  return wide ? by_tiles<PARTS, 32, float, X>(p, tiles, grid, lds, st) : by_tiles<PARTS, 32, uint16_t, X>(p, tiles, grid, lds, st);
 }
 
 }  // namespace

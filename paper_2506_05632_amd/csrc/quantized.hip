@@ -263,24 +263,46 @@ extern "C" int llc_matvec_quantized(const llc_matvec_quantized_args *a) {
   p.slabs = (int)((a->D + 127) / 128);
   const int rows = (int)(a->R < kMatvecRows ? a->R : kMatvecRows), tiles = (rows + 15) / 16, parts = a->dtype == LLC_F32 ? 3 : 1;
   const long long column_tiles = (a->N + 15) / 16;
-  // Few columns: wavefronts share a tile by its columns until some 2048 of them are at work, eight a CU.
   constexpr int waves = kMatvecThreads / 64;
-  constexpr size_t kXBytes = 64 << 10;  // of LDS for x
-  long long most = (long long)(kXBytes / matvec_x_bytes(parts, rows, 1));
-  if (most < 1) most = 1;
-  while (p.share_log < 3 && (column_tiles << p.share_log) < 2048 && (2 << p.share_log) <= p.slabs && (2 << p.share_log) <= most) ++p.share_log;
-  const long long wanted = (p.slabs + (1 << p.share_log) - 1) >> p.share_log << p.share_log;
-  most = most >> p.share_log << p.share_log;
-  p.chunk_slabs = (int)(wanted < most ? wanted : most);
-  const int each = waves >> p.share_log;
-  p.tile_blocks = (unsigned)((column_tiles + each - 1) / each);
-  const size_t lds = matvec_x_bytes(parts, rows, p.chunk_slabs) + matvec_sum_bytes(tiles, a->group, p.chunk_slabs) + matvec_join_bytes(tiles, waves, p.share_log);
+  constexpr size_t kLds = 156 << 10;  // that a workgroup may have, of a CU's 160 KB
+  const auto x_bytes = [&](int slabs) { return matvec_x_bytes(parts, rows, tiles, a->group, slabs); };
+  // x stays in LDS where it fits; there, few columns are shared until some 2048 wavefronts are at work, eight a CU.
+  const auto share_for = [&](int wide, int most) {
+    int log = 0;
+    while (log < 3 && (column_tiles << log) < 2048LL * wide && (2 << log) <= most) ++log;
+    return log;
+  };
+  size_t lds;
+  unsigned blocks;
+  p.share_log = share_for(1, p.slabs);
+  lds = x_bytes(p.slabs) + matvec_join_bytes(tiles, 1, p.share_log);
+  p.streamed = tiles == 1 && lds <= kLds ? 0 : 1;
+  if (p.streamed == 0) {
+    const int each = waves >> p.share_log;
+    p.tile_blocks = (unsigned)((column_tiles + each - 1) / each);
+    const unsigned resident = 256u * (unsigned)(lds <= kLds / 2 ? 2 : 1);
+    // (as many blocks for each workgroup, or one less)
+    const unsigned turns = (p.tile_blocks + resident - 1) / resident;
+    blocks = (p.tile_blocks + turns - 1) / turns;
+  } else {
+    const int most = kMatvecThreads * (parts == 3 ? kStreamedPieces<float> : kStreamedPieces<uint16_t>) / (16 * rows);  // slabs that the threads have in flight
+    const auto streamed_bytes = [&](int chunk_log, int share_log) { return 2 * x_bytes(1 << chunk_log) + matvec_join_bytes(tiles, 2, share_log); };
+    p.share_log = share_for(2, p.slabs < most ? p.slabs : most);
+    while (p.share_log > 0 && streamed_bytes(p.share_log, p.share_log) > kLds) --p.share_log;
+    p.chunk_log = p.share_log;
+    while ((2 << p.chunk_log) <= most && (1 << p.chunk_log) < p.slabs && streamed_bytes(p.chunk_log + 1, p.share_log) <= kLds) ++p.chunk_log;
+    lds = streamed_bytes(p.chunk_log, p.share_log);
+    const long long each = 2 * (waves >> p.share_log), turns = (column_tiles + 256 * each - 1) / (256 * each);
+    p.block_tiles = (int)((column_tiles + 256 * turns - 1) / (256 * turns));
+    p.tile_blocks = (unsigned)((column_tiles + p.block_tiles - 1) / p.block_tiles);
+    blocks = p.tile_blocks;
+  }
   const unsigned passes = (unsigned)((a->R + kMatvecRows - 1) / kMatvecRows);
-  const dim3 grid(p.tile_blocks < 1024 ? p.tile_blocks : 1024, passes);
+  const dim3 grid(blocks, passes);
   if ((a->flags & LLC_FLAG_DRY_RUN) != 0) return LLC_OK;
   hipStream_t st = (hipStream_t)a->stream;
   return between_events(a->ev_begin, a->ev_end, st, [&] {
-    return a->dtype == LLC_F32 ? launch_matvec_f32(p, tiles, a->group, a->scales_dtype, grid, waves * 64, lds, st)
-                               : launch_matvec_bf16(p, tiles, a->group, a->scales_dtype, grid, waves * 64, lds, st);
+    return a->dtype == LLC_F32 ? launch_matvec_f32(p, tiles, a->group, a->scales_dtype, grid, lds, st)
+                               : launch_matvec_bf16(p, tiles, a->group, a->scales_dtype, grid, lds, st);
   });
 }

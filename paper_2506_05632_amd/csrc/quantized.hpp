@@ -38,20 +38,23 @@ struct MatvecParams {
   int out_type;
   int groups;       // of a row
   int slabs;        // of 128 entries, of a row
-  int chunk_slabs;  // that the workgroup's part of x in LDS holds; a multiple of the wavefronts that share a tile
+  int streamed;     // x goes through LDS by parts
+  int chunk_log;    // log2 of the slabs of a part, which are at least as many as wavefronts share a tile
   int share_log;    // log2 of the wavefronts that share a tile by columns
   unsigned tile_blocks;  // workgroups' worth of tiles
+  int block_tiles;       // that a workgroup takes at a time, where x is streamed
 };
 constexpr int kMatvecThreads = 512;
 constexpr int kMatvecRows = 64;  // rows of x that one pass over the layer serves
 
-// Bytes of LDS of a workgroup: x, the groups' sums of x, and the sums of wavefronts that share a tile.
-inline size_t matvec_x_bytes(int parts, int rows, int chunk_slabs) { return (size_t)chunk_slabs * 256 * parts * rows; }
-inline size_t matvec_sum_bytes(int tiles, int group, int chunk_slabs) { return (size_t)chunk_slabs * (128 / group) * tiles * 64; }
-inline size_t matvec_join_bytes(int tiles, int waves, int share_log) { return share_log > 0 ? (size_t)waves * tiles * 1024 : 0; }
+template <typename X> constexpr int kStreamedPieces = 8 / sizeof(X);  // of eight columns of x that a thread has in flight
+
+// Bytes of LDS of a workgroup: x and the groups' sums of it, and the sums of wavefronts that share tiles.
+inline size_t matvec_x_bytes(int parts, int rows, int tiles, int group, int slabs) { return (size_t)slabs * ((size_t)256 * parts * rows + (size_t)(128 / group) * tiles * 64); }
+inline size_t matvec_join_bytes(int tiles, int wide, int share_log) { return share_log > 0 ? (size_t)(kMatvecThreads / 64) * wide * tiles * 1024 : 0; }
 
 // (one translation unit for each type of x)
-hipError_t launch_matvec_bf16(const MatvecParams &p, int tiles, int group, int scales_type, dim3 grid, int threads, size_t lds, hipStream_t st);
-hipError_t launch_matvec_f32(const MatvecParams &p, int tiles, int group, int scales_type, dim3 grid, int threads, size_t lds, hipStream_t st);
+hipError_t launch_matvec_bf16(const MatvecParams &p, int tiles, int group, int scales_type, dim3 grid, size_t lds, hipStream_t st);
+hipError_t launch_matvec_f32(const MatvecParams &p, int tiles, int group, int scales_type, dim3 grid, size_t lds, hipStream_t st);
 
 }  // namespace llc
