@@ -629,7 +629,8 @@ typedef struct llc_embed_quantized_args {
  * result is rounded to the output's type.  A row of x with an entry that is not finite, or over 2^120 in size, gives outputs that need not be what
  * the formula gives in that row; other rows are not touched by it.  Made for few rows: they are taken 64 at a time, and each such pass reads the layer. */
 typedef struct llc_matvec_quantized_args {
-  int64_t R, N, D;          /* R in 0..2^20, N in 1..2^31 - 5, D in 1..2^27              */
+  int64_t R, N, D;          /* R in 0..2^17, N in 1..2^31 - 5, D in 1..2^27; R times D at most 2^34, and,
+                               of more than 16 rows, R / 64 times N / 16, each rounded up, at most 2^25 */
   int32_t group;
   int32_t dtype, scales_dtype, out_dtype; /* of x, of scales and of out                  */
   const void *x;            /* device [R,D] */
@@ -642,6 +643,8 @@ typedef struct llc_matvec_quantized_args {
   int64_t zeros_stride_n;
   void *out;                /* [R,N] */
   int64_t out_stride_r;
+  void *workspace;          /* device, 256-byte aligned, >= llc_matvec_quantized_workspace_size(); may be NULL where that is 0 */
+  size_t workspace_bytes;
   void *stream;
   int32_t flags;            /* LLC_FLAG_DRY_RUN */
   void *ev_begin, *ev_end;
@@ -682,6 +685,9 @@ int llc_embed_quantized(const llc_embed_quantized_args *a);
 
 /* Products with a layer of 4 bits.  Asynchronous. */
 int llc_matvec_quantized(const llc_matvec_quantized_args *a);
+
+/* Bytes of device scratch it needs for this shape (dtype: x's): 0 for up to 16 rows that fit a CU's LDS, and on bad shapes. */
+size_t llc_matvec_quantized_workspace_size(int64_t R, int64_t N, int64_t D, int32_t group, int32_t dtype);
 
 /* Algorithm 1 on a batch (Section 3).  Asynchronous on a->stream. */
 int llc_couple(const llc_couple_args *a);

@@ -6,4 +6,5 @@ from .binding import (FLAG_DRAFT_ONLY, FLAG_DRY_RUN, FLAG_EXACT_SCAN, FLAG_MIN_F
 from .binding import (llc_clip_grad_norm, llc_clip_grad_norm_workspace_size, llc_embed, llc_embed_grad,  # noqa: F401
                       llc_embed_grad_workspace_size, llc_token_logprobs, llc_token_logprobs_grad,
                       llc_token_logprobs_workspace_size)
-from .binding import llc_embed_quantized, llc_matvec_quantized, llc_quantize, llc_sample, llc_truncate  # noqa: F401
+from .binding import (llc_embed_quantized, llc_matvec_quantized, llc_matvec_quantized_workspace_size, llc_quantize, llc_sample,  # noqa: F401
+                      llc_truncate)

@@ -32,7 +32,8 @@ EXPORTS = ["llc_couple", "llc_couple_static", "llc_couple_is", "llc_couple_topm"
            "llc_couple_workspace_size", "llc_verify_workspace_size", "llc_lml_workspace_size", "llc_status_string",
            "llc_version", "llc_token_logprobs", "llc_token_logprobs_grad", "llc_token_logprobs_workspace_size", "llc_embed",
            "llc_embed_grad", "llc_embed_grad_workspace_size", "llc_clip_grad_norm", "llc_clip_grad_norm_workspace_size",
-           "llc_sample", "llc_truncate", "llc_quantize", "llc_embed_quantized", "llc_matvec_quantized"]
+           "llc_sample", "llc_truncate", "llc_quantize", "llc_embed_quantized", "llc_matvec_quantized",
+           "llc_matvec_quantized_workspace_size"]
 
 
 class LlcStats(ctypes.Structure):
@@ -278,7 +279,8 @@ class MatvecQuantizedArgs(ctypes.Structure):
         ("R", ctypes.c_int64), ("N", ctypes.c_int64), ("D", ctypes.c_int64), ("group", ctypes.c_int32),
         ("dtype", ctypes.c_int32), ("scales_dtype", ctypes.c_int32), ("out_dtype", ctypes.c_int32),
         ("x", ctypes.c_void_p), ("x_stride_r", ctypes.c_int64), *_LAYER,
-        ("out", ctypes.c_void_p), ("out_stride_r", ctypes.c_int64), *_END,
+        ("out", ctypes.c_void_p), ("out_stride_r", ctypes.c_int64),
+        ("workspace", ctypes.c_void_p), ("workspace_bytes", ctypes.c_size_t), *_END,
     ]
 
 
@@ -332,6 +334,8 @@ def load():
                             ("llc_clip_grad_norm_workspace_size", 1)):
             getattr(lib, name).argtypes = [ctypes.c_int64] * count
             getattr(lib, name).restype = ctypes.c_size_t
+        lib.llc_matvec_quantized_workspace_size.argtypes = [ctypes.c_int64] * 3 + [ctypes.c_int32] * 2
+        lib.llc_matvec_quantized_workspace_size.restype = ctypes.c_size_t
         lib.llc_status_string.argtypes = [ctypes.c_int]
         lib.llc_status_string.restype = ctypes.c_char_p
         lib.llc_version.restype = ctypes.c_int
@@ -1150,6 +1154,10 @@ def _cut_into(a, name, logits, kind, temp, top_k, top_p, min_p):
     return R, V, dev
 
 
+def llc_matvec_quantized_workspace_size(R: int, N: int, D: int, group: int, dtype: torch.dtype) -> int:
+    return load().llc_matvec_quantized_workspace_size(R, N, D, group, _TYPES[dtype])
+
+
 def llc_sample(logits: torch.Tensor, u: torch.Tensor, *, temp=1.0, top_k=0, top_p=1.0, min_p=0.0, kind="logits", want_logp: bool = True,
                want_kept: bool = False, out: Optional[dict] = None, flags: int = 0, events=None) -> dict:
     """Draws tokens of every row's cut distribution with given uniform numbers.
@@ -1312,7 +1320,8 @@ def llc_embed_quantized(codes: torch.Tensor, scales: torch.Tensor, tokens: torch
 
 
 def llc_matvec_quantized(x: torch.Tensor, codes: torch.Tensor, scales: torch.Tensor, *, zeros: Optional[torch.Tensor] = None, group: int = 128,
-                out_dtype: Optional[torch.dtype] = None, out: Optional[torch.Tensor] = None, flags: int = 0, events=None) -> dict:
+                out_dtype: Optional[torch.dtype] = None, out: Optional[torch.Tensor] = None, workspace: Optional[torch.Tensor] = None,
+                flags: int = 0, events=None) -> dict:
     """Products with a layer in 4 bits: out[r,n] = sum over d of x[r,d] * w[n,d].
 
     x: [R,D] float32 or bfloat16, last dimension contiguous; codes, scales, zeros, group: as llc_quantize returned them, of a
@@ -1327,8 +1336,15 @@ def llc_matvec_quantized(x: torch.Tensor, codes: torch.Tensor, scales: torch.Ten
     N = _layer_into(a, codes, scales, zeros, D, group)
     if x.device != codes.device:
         raise ValueError("x must be on the codes' device")
+    nbytes = lib.llc_matvec_quantized_workspace_size(R, N, D, group, _TYPES[x.dtype])
     if out is None:
-        out = _new(x.device, {"out": (out_dtype or x.dtype, R, N)})["out"]
+        specs = {"out": (out_dtype or x.dtype, R, N)}
+        if nbytes > 0:
+            workspace = _scratch(workspace, lambda: nbytes, x.device, specs)
+        made = _new(x.device, specs)
+        out, workspace = made["out"], made.get("workspace", workspace)
+    elif nbytes > 0:
+        workspace = _scratch(workspace, lambda: nbytes, x.device)
     if (out.device != x.device or out.dtype not in _TYPES or out_dtype not in (None, out.dtype) or tuple(out.shape) != (R, N)
             or (out.stride(1) != 1 and N > 1)):
         raise ValueError("out must be [R,N], float32 or bfloat16, last dimension contiguous")
@@ -1336,6 +1352,8 @@ def llc_matvec_quantized(x: torch.Tensor, codes: torch.Tensor, scales: torch.Ten
     a.dtype, a.out_dtype = _TYPES[x.dtype], _TYPES[out.dtype]
     a.x, a.x_stride_r = x.data_ptr(), x.stride(0)
     a.out, a.out_stride_r = out.data_ptr(), _row_stride(out)
+    if nbytes > 0:
+        a.workspace, a.workspace_bytes = workspace.data_ptr(), workspace.numel()
     a.stream = _stream_handle(x.device)
     a.flags = flags
     if events is not None:

@@ -46,6 +46,13 @@ template <int G, typename S> struct Slab {
   float scale[kGroups];
   float shift[kGroups];  // -(16 + zero)
 };
+// The same with its scales and zeros as they lie in memory, until they are needed.
+template <int G, typename S> struct RawSlab {
+  static constexpr int kGroups = 128 / G;
+  uint32_t words[4];
+  S scale[kGroups];
+  uint32_t zero;
+};
 // Four slabs that follow each other, their scales and zeros as they lie in memory.
 template <int G, typename S> struct Batch {
   static constexpr int kSlabs = 4, kGroups = kSlabs * 128 / G, kScaleWords = kGroups * sizeof(S) / 4, kZeroWords = kGroups / 4;
@@ -61,19 +68,31 @@ template <int G> __device__ __forceinline__ int column_of(int step, int quarter)
   return 32 * step + 8 * quarter;
 }
 
-template <int G, typename S>
-__device__ __forceinline__ void load_scales(Slab<G, S> &s, const MatvecParams &p, const S *scales, const uint8_t *zeros, int slab) {
+template <bool Z, int G, typename S>
+__device__ __forceinline__ void load_scales(RawSlab<G, S> &s, const MatvecParams &p, const S *scales, const uint8_t *zeros, int slab) {
+  s.zero = 0;
 #pragma unroll
   for (int g = 0; g < 128 / G; ++g) {
     int of = slab * (128 / G) + g;
     of = of < p.groups ? of : p.groups - 1;  // (columns behind the row's end: x is 0 there)
-    s.scale[g] = widen(scales[of]);
-    s.shift[g] = zeros != nullptr ? -16.0f - (float)zeros[of] : -24.0f;
+    s.scale[g] = scales[of];
+    if constexpr (Z) s.zero |= (uint32_t)zeros[of] << (8 * g);
   }
 }
-template <int G, typename S>
-__device__ __forceinline__ Slab<G, S> load_slab(const MatvecParams &p, const uint8_t *codes, const S *scales, const uint8_t *zeros, int slab, int quarter) {
+template <bool Z, int G, typename S> __device__ __forceinline__ Slab<G, S> slab_of(const RawSlab<G, S> &r) {
   Slab<G, S> s;
+#pragma unroll
+  for (int j = 0; j < 4; ++j) s.words[j] = r.words[j];
+#pragma unroll
+  for (int g = 0; g < 128 / G; ++g) {
+    s.scale[g] = widen(r.scale[g]);
+    s.shift[g] = Z ? -16.0f - (float)((r.zero >> (8 * g)) & 255u) : -24.0f;
+  }
+  return s;
+}
+template <bool Z, int G, typename S>
+__device__ __forceinline__ RawSlab<G, S> load_slab(const MatvecParams &p, const uint8_t *codes, const S *scales, const uint8_t *zeros, int slab, int quarter) {
+  RawSlab<G, S> s;
   const uint8_t *from = codes + (long long)slab * 64;
   if constexpr (G == 128) {
     const word4_byte w = *reinterpret_cast<const word4_byte *>(from + 16 * quarter);
@@ -86,16 +105,16 @@ __device__ __forceinline__ Slab<G, S> load_slab(const MatvecParams &p, const uin
 #pragma unroll
     for (int i = 0; i < 4; ++i) s.words[i] = *reinterpret_cast<const word1_byte *>(from + 16 * i + 4 * quarter);
   }
-  load_scales(s, p, scales, zeros, slab);
+  load_scales<Z>(s, p, scales, zeros, slab);
   return s;
 }
 // The last slab of a row that is not a whole one.
-template <int G, typename S>
-__device__ __forceinline__ Slab<G, S> load_last_slab(const MatvecParams &p, const uint8_t *codes, const S *scales, const uint8_t *zeros, int slab, int quarter) {
-  Slab<G, S> s;
+template <bool Z, int G, typename S>
+__device__ __forceinline__ RawSlab<G, S> load_last_slab(const MatvecParams &p, const uint8_t *codes, const S *scales, const uint8_t *zeros, int slab, int quarter) {
+  RawSlab<G, S> s;
 #pragma unroll
   for (int i = 0; i < 4; ++i) s.words[i] = load_codes(codes, (long long)slab * 128 + column_of<G>(i, quarter), p.D);
-  load_scales(s, p, scales, zeros, slab);
+  load_scales<Z>(s, p, scales, zeros, slab);
   return s;
 }
 // N words from anywhere.
@@ -114,7 +133,7 @@ template <int N> __device__ __forceinline__ void load_words(uint32_t (&w)[N], co
     }
   }
 }
-template <int G, typename S> __device__ __forceinline__ void load_batch(Batch<G, S> &b, const uint8_t *codes, const S *scales, const uint8_t *zeros, int slab, int quarter) {
+template <bool Z, int G, typename S> __device__ __forceinline__ void load_batch(Batch<G, S> &b, const uint8_t *codes, const S *scales, const uint8_t *zeros, int slab, int quarter) {
 #pragma unroll
   for (int i = 0; i < Batch<G, S>::kSlabs; ++i) {
     const uint8_t *from = codes + (long long)slab * 64 + i * 64;
@@ -129,9 +148,9 @@ template <int G, typename S> __device__ __forceinline__ void load_batch(Batch<G,
     }
   }
   load_words(b.scale, scales + (long long)slab * (128 / G));
-  if (zeros != nullptr) load_words(b.zero, zeros + (long long)slab * (128 / G));
+  if constexpr (Z) load_words(b.zero, zeros + (long long)slab * (128 / G));
 }
-template <int G, typename S> __device__ __forceinline__ Slab<G, S> slab_of(const Batch<G, S> &b, int i, bool zeros) {
+template <bool Z, int G, typename S> __device__ __forceinline__ Slab<G, S> slab_of(const Batch<G, S> &b, int i) {
   Slab<G, S> s;
 #pragma unroll
   for (int j = 0; j < 4; ++j) s.words[j] = b.words[i][j];
@@ -140,25 +159,25 @@ template <int G, typename S> __device__ __forceinline__ Slab<G, S> slab_of(const
     const int at = i * (128 / G) + g;
     if constexpr (sizeof(S) == 4) s.scale[g] = __uint_as_float(b.scale[at]);
     else s.scale[g] = __uint_as_float(at % 2 == 0 ? b.scale[at / 2] << 16 : b.scale[at / 2] & 0xFFFF0000u);
-    s.shift[g] = zeros ? -16.0f - (float)((b.zero[at / 4] >> (8 * (at % 4))) & 255u) : -24.0f;
+    s.shift[g] = Z ? -16.0f - (float)((b.zero[at / 4] >> (8 * (at % 4))) & 255u) : -24.0f;
   }
   return s;
 }
 
-// Adds a slab's products to the sums of WIDE tiles of columns, which share what is read of x; `here`: its place in the part of x in LDS.
+// Adds a slab's products to the sums of WIDE tiles of columns, which share what is read of x.  s_x, s_sum: the slab's, and its groups' sums.
 template <int TILES, int PARTS, int G, typename S, int WIDE>
-__device__ __forceinline__ void add_slab(f32x4 (&total)[WIDE][TILES], const Slab<G, S> (&s)[WIDE], const uint4 *s_x, const float *s_sum, const int (&at_x)[TILES], int rows,
-                                         int here, int quarter) {
+__device__ __forceinline__ void add_slab(f32x4 (&total)[WIDE][TILES], const Slab<G, S> (&s)[WIDE], const uint4 *s_x, const float *s_sum, const int (&at_x)[TILES],
+                                         int pitch, int quarter) {
+  int from = 0;
   constexpr int kSteps = G / 32;  // of a group
   f32x4 sum[WIDE][TILES], low[WIDE][TILES];
-  int from = here * 16 * PARTS * rows;  // of x: an addition a read (all of them at once, as they follow from `here`, would take more registers than there are)
 #pragma unroll
   for (int step = 0; step < 4; ++step) {
     const int g = step / kSteps;
     if (step % kSteps == 0) {
 #pragma unroll
       for (int t = 0; t < TILES; ++t) {
-        const f32x4 sx = *reinterpret_cast<const f32x4 *>(s_sum + (here * (128 / G) + g) * (TILES * 16) + 16 * t + 4 * quarter);
+        const f32x4 sx = *reinterpret_cast<const f32x4 *>(s_sum + g * (TILES * 16) + 16 * t + 4 * quarter);
 #pragma unroll
         for (int w = 0; w < WIDE; ++w) {
 #pragma unroll
@@ -172,7 +191,7 @@ __device__ __forceinline__ void add_slab(f32x4 (&total)[WIDE][TILES], const Slab
     for (int w = 0; w < WIDE; ++w) codes[w] = widen_codes(s[w].words[step]);
 #pragma unroll
     for (int part = 0; part < PARTS; ++part) {
-      asm volatile("" : "+s"(from));
+      asm volatile("" : "+s"(from));  // (an addition a read: all the places at once, as they follow from the slab's, would take more registers than there are)
 #pragma unroll
       for (int t = 0; t < TILES; ++t) {
         const bf16x8 a = __builtin_bit_cast(bf16x8, s_x[from + at_x[t]]);
@@ -182,7 +201,7 @@ __device__ __forceinline__ void add_slab(f32x4 (&total)[WIDE][TILES], const Slab
           else low[w][t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, codes[w], low[w][t], 0, 0, 0);
         }
       }
-      from += 4 * rows;
+      from += 4 * pitch;
     }
     if (step % kSteps == kSteps - 1) {
 #pragma unroll
@@ -196,7 +215,7 @@ __device__ __forceinline__ void add_slab(f32x4 (&total)[WIDE][TILES], const Slab
   }
 }
 
-// x to LDS as the operands lie: [slab][step][part][quarter][row], 16 bytes each; and the groups' sums [group][16 rows of a tile].  A piece is eight columns of a row.
+// x to LDS as the operands lie: [slab][step][part][quarter][row], 16 bytes each, rows an odd number of them apart so that pieces of one row lie in unlike banks; and the groups' sums [group][16 rows of a tile].  A piece is eight columns of a row.
 template <typename X> struct Piece;
 template <> struct Piece<float> { float4_any a, b; };
 template <> struct Piece<uint16_t> { word4_any a; };
@@ -224,7 +243,8 @@ template <typename X> __device__ __forceinline__ Piece<X> load_x(const MatvecPar
   }
   return v;
 }
-template <int TILES, int PARTS, int G, typename X> __device__ __forceinline__ void store_x(const Piece<X> &from, unsigned r, unsigned piece, int rows, uint4 *s_x, float *s_sum) {
+template <int PARTS, int G, typename X>
+__device__ __forceinline__ void store_x(const Piece<X> &from, unsigned r, unsigned piece, int pitch, int tiles, uint4 *s_x, float *s_sum) {
   float v[8];
 #pragma unroll
   for (int j = 0; j < 4; ++j) {
@@ -239,12 +259,12 @@ template <int TILES, int PARTS, int G, typename X> __device__ __forceinline__ vo
   const unsigned slab = piece >> 4, q = piece & 15;
   const unsigned step = G == 128 ? q & 3 : G == 64 ? (q >> 3) * 2 + (q & 1) : q >> 2;
   const unsigned quarter = G == 128 ? q >> 2 : G == 64 ? (q >> 1) & 3 : q & 3;
-  if ((q & (G / 8 - 1)) == 0) s_sum[(slab * (128 / G) + q / (G / 8)) * (TILES * 16) + r] = sum;
-  uint4 *to = s_x + ((slab * 4 + step) * PARTS * 4 + quarter) * rows + r;
+  if ((q & (G / 8 - 1)) == 0) s_sum[(slab * (128 / G) + q / (G / 8)) * (tiles * 16) + r] = sum;
+  uint4 *to = s_x + ((slab * 4 + step) * PARTS * 4 + quarter) * pitch + r;
 #pragma unroll
   for (int part = 0; part < PARTS; ++part) {
     const uint4 w = make_uint4(narrow_pair(v[0], v[4]), narrow_pair(v[1], v[5]), narrow_pair(v[2], v[6]), narrow_pair(v[3], v[7]));
-    to[part * 4 * rows] = w;
+    to[part * 4 * pitch] = w;
     if (part + 1 < PARTS) {  // what is left is exact
       const uint32_t in[4] = {w.x, w.y, w.z, w.w};
 #pragma unroll
@@ -301,73 +321,79 @@ __device__ __forceinline__ void finish_tiles(const MatvecParams &p, f32x4 (&tota
   }
 }
 
-template <typename S> struct Row {  // of the layer
+// A row of the layer.
+template <typename S> struct Row {
   const uint8_t *codes;
   const S *scales;
   const uint8_t *zeros;
 };
 template <typename S> __device__ __forceinline__ Row<S> row_of(const MatvecParams &p, long long n) {
   const long long at = n < p.N ? n : p.N - 1;
-  return {p.codes + at * p.codes_stride, reinterpret_cast<const S *>(p.scales) + at * p.scales_stride, p.zeros != nullptr ? p.zeros + at * p.zeros_stride : nullptr};
+  const uint8_t *codes = p.codes + at * p.codes_stride;
+  return {codes, reinterpret_cast<const S *>(p.scales) + at * p.scales_stride, p.zeros + at * p.zeros_stride};
 }
 
 // x in LDS as a whole, put there once; a workgroup takes several blocks of tiles with it.  Wavefronts that share a tile take a run of its slabs each, four at a
 // time, of which the next four are asked for before these are multiplied.
-template <int PARTS, int G, typename S, typename X> __global__ void __launch_bounds__(kMatvecThreads, 4) matvec_quantized_kernel(const MatvecParams p) {
+template <int PARTS, int G, typename S, bool Z, typename X> __global__ void __launch_bounds__(kMatvecThreads, 4) matvec_quantized_kernel(const MatvecParams p) {
   constexpr int TILES = 1, WIDE = 1, kSlabs = Batch<G, S>::kSlabs;
   extern __shared__ __align__(16) char s_dyn[];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int share = 1 << p.share_log, part_of = wave & (share - 1), tile_of = wave >> p.share_log, tiles_each = (blockDim.x >> 6) >> p.share_log;
   const int column = lane & 15, quarter = lane >> 4;
   const long long r0 = (long long)blockIdx.y * kMatvecRows;
-  const int rows = (int)(p.R - r0 < 16 * TILES ? p.R - r0 : 16 * TILES);
+  const int rows = (int)(p.R - r0 < 16 * TILES ? p.R - r0 : 16 * TILES), pitch = pitch_of(rows);
   uint4 *s_x = reinterpret_cast<uint4 *>(s_dyn);
-  float *s_sum = reinterpret_cast<float *>(s_dyn + (size_t)p.slabs * 256 * PARTS * rows);
+  float *s_sum = reinterpret_cast<float *>(s_dyn + (size_t)p.slabs * 256 * PARTS * pitch);
   float *s_join = s_sum + p.slabs * (128 / G) * (TILES * 16);
   const int whole = (int)(p.D / 128), each = (p.slabs + share - 1) >> p.share_log;
   const int begin = part_of * each < whole ? part_of * each : whole, end = begin + each < whole ? begin + each : whole;
   const bool last_too = whole < p.slabs && part_of == whole / each;
   int at_x[TILES];
 #pragma unroll
-  for (int t = 0; t < TILES; ++t) at_x[t] = quarter * rows + (16 * t + column < rows ? 16 * t + column : rows - 1);
+  for (int t = 0; t < TILES; ++t) at_x[t] = quarter * pitch + (16 * t + column < rows ? 16 * t + column : rows - 1);
   for (unsigned block = blockIdx.x; block < p.tile_blocks; block += gridDim.x) {
     const long long n0[WIDE] = {((long long)block * tiles_each + tile_of) * 16};
     const Row<S> row = row_of<S>(p, n0[0] + column);
     f32x4 total[WIDE][TILES];
 #pragma unroll
     for (int t = 0; t < TILES; ++t) total[0][t] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+    // (each wavefront's batches: all loads of the loop under no condition, as below)
     Batch<G, S> batch[2];
-    if (begin + kSlabs <= end) load_batch(batch[0], row.codes, row.scales, row.zeros, begin, quarter);
+    const int batches = (end - begin) / kSlabs;
+    const auto fetch = [&](Batch<G, S> &to, int i) __attribute__((always_inline)) { load_batch<Z>(to, row.codes, row.scales, row.zeros, begin + (i < batches ? i : batches - 1) * kSlabs, quarter); };
+    const auto add = [&](const Batch<G, S> &from, int i) __attribute__((always_inline)) {
+#pragma unroll
+      for (int j = 0; j < kSlabs; ++j) {
+        const int slab = begin + i * kSlabs + j;
+        const Slab<G, S> s[WIDE] = {slab_of<Z>(from, j)};
+        add_slab<TILES, PARTS, G, S, WIDE>(total, s, s_x + slab * 16 * PARTS * pitch, s_sum + slab * (128 / G) * 16, at_x, pitch, quarter);
+      }
+    };
+    if (batches > 0) fetch(batch[0], 0);
     if (block == blockIdx.x) {
       const unsigned pieces = (unsigned)p.slabs * 16;
       for (unsigned r = 0; r < (unsigned)rows; ++r)
         for (unsigned piece = threadIdx.x; piece < pieces; piece += blockDim.x) {
           const Piece<X> v = load_x<X>(p, r0 + r, (int)piece * 8);
-          store_x<TILES, PARTS, G, X>(v, r, piece, rows, s_x, s_sum);
+          store_x<PARTS, G, X>(v, r, piece, pitch, TILES, s_x, s_sum);
         }
       __syncthreads();
     }
-    int slab = begin;
+    int i = 0;
 #pragma unroll 1
-    for (; slab + kSlabs <= end; slab += 2 * kSlabs) {
-#pragma unroll
-      for (int half = 0; half < 2; ++half) {
-        const int at = slab + half * kSlabs;
-        if (at + kSlabs <= end) {  // (uniform)
-          if (at + 2 * kSlabs <= end) load_batch(batch[1 - half], row.codes, row.scales, row.zeros, at + kSlabs, quarter);
-#pragma unroll
-          for (int i = 0; i < kSlabs; ++i) {
-            const Slab<G, S> s[WIDE] = {slab_of(batch[half], i, row.zeros != nullptr)};
-            add_slab<TILES, PARTS, G, S, WIDE>(total, s, s_x, s_sum, at_x, rows, at + i, quarter);
-          }
-        }
-      }
+    for (; i + 2 <= batches; i += 2) {
+      fetch(batch[1], i + 1);
+      add(batch[0], i);
+      fetch(batch[0], i + 2);
+      add(batch[1], i + 1);
     }
+    if (i < batches) add(batch[0], i);
 #pragma unroll 1
-    for (slab = begin + (end - begin) / kSlabs * kSlabs; slab < end + (last_too ? 1 : 0); ++slab) {  // fewer than four, and the row's end
-      const Slab<G, S> s[WIDE] = {slab < whole ? load_slab<G, S>(p, row.codes, row.scales, row.zeros, slab, quarter)
-                                               : load_last_slab<G, S>(p, row.codes, row.scales, row.zeros, slab, quarter)};
-      add_slab<TILES, PARTS, G, S, WIDE>(total, s, s_x, s_sum, at_x, rows, slab, quarter);
+    for (int slab = begin + batches * kSlabs; slab < end + (last_too ? 1 : 0); ++slab) {  // fewer than four, and the row's end
+      const Slab<G, S> s[WIDE] = {slab_of<Z>(slab < whole ? load_slab<Z, G, S>(p, row.codes, row.scales, row.zeros, slab, quarter)
+                                                       : load_last_slab<Z, G, S>(p, row.codes, row.scales, row.zeros, slab, quarter))};
+      add_slab<TILES, PARTS, G, S, WIDE>(total, s, s_x + slab * 16 * PARTS * pitch, s_sum + slab * (128 / G) * 16, at_x, pitch, quarter);
     }
     int lane_here = lane;
     asm volatile("" : "+v"(lane_here));  // (or every address of the output would be kept in registers from block to block)
@@ -375,96 +401,135 @@ template <int PARTS, int G, typename S, typename X> __global__ void __launch_bou
   }
 }
 
-// x by parts of a slab or a few, in two places of LDS in turn: the next part is asked for before this one is multiplied, and put in its place after.  A wavefront
-// has two tiles of columns, so that what it reads of x serves both, and every workgroup takes its tiles through all of x once.
-template <int TILES, int PARTS, int G, typename S, typename X>
-__global__ void __launch_bounds__(kMatvecThreads, 2) matvec_streamed_kernel(const MatvecParams p) {
-  constexpr int WIDE = 2, kMost = kStreamedPieces<X>;
-  extern __shared__ __align__(16) char s_dyn[];
-  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const int share = 1 << p.share_log, part_of = wave & (share - 1), tile_of = wave >> p.share_log, tiles_each = (blockDim.x >> 6) >> p.share_log;
-  const int column = lane & 15, quarter = lane >> 4;
-  const long long r0 = (long long)blockIdx.y * kMatvecRows;
-  const int rows = (int)(p.R - r0 < 16 * TILES ? p.R - r0 : 16 * TILES);
-  const int place_x = 256 * PARTS * rows << p.chunk_log, place = place_x + ((128 / G) * TILES * 64 << p.chunk_log);
-  float *s_join = reinterpret_cast<float *>(s_dyn + 2 * place);
-  const int whole = (int)(p.D / 128), chunks = (p.slabs + (1 << p.chunk_log) - 1) >> p.chunk_log;
-  int at_x[TILES];
-#pragma unroll
-  for (int t = 0; t < TILES; ++t) at_x[t] = quarter * rows + (16 * t + column < rows ? 16 * t + column : rows - 1);
-  const unsigned pieces_log = p.chunk_log + 4, all = (unsigned)rows << pieces_log;
-  {
-    long long n0[WIDE];
-    Row<S> row[WIDE];
-    f32x4 total[WIDE][TILES];
-#pragma unroll
-    for (int w = 0; w < WIDE; ++w) {
-      const int tile = tile_of + w * tiles_each;
-      const long long at = (long long)blockIdx.x * p.block_tiles + tile;
-      n0[w] = tile < p.block_tiles && at * 16 < p.N ? at * 16 : -1;
-      row[w] = row_of<S>(p, (n0[w] < 0 ? 0 : n0[w]) + column);
-#pragma unroll
-      for (int t = 0; t < TILES; ++t) total[w][t] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
-    }
-    Piece<X> v[kMost];
-    const auto ask = [&](int chunk) {
-#pragma unroll
-      for (int i = 0; i < kMost; ++i) {
-        const unsigned at = i * kMatvecThreads + threadIdx.x, r = at >> pieces_log, first = (unsigned)chunk << pieces_log;
-        if (at < all) v[i] = (int)(first + at - (r << pieces_log)) * 8 < p.D ? load_x<X>(p, r0 + r, (int)(first + at - (r << pieces_log)) * 8) : Piece<X>{};
-      }
-    };
-    Slab<G, S> slab[WIDE];
-    const auto fetch = [&](int of) {
-#pragma unroll
-      for (int w = 0; w < WIDE; ++w) slab[w] = load_slab<G, S>(p, row[w].codes, row[w].scales, row[w].zeros, of, quarter);
-    };
-    ask(0);
-    if (part_of < whole) fetch(part_of);
-#pragma unroll 1
-    for (int chunk = 0; chunk < chunks; ++chunk) {
-      char *at_place = s_dyn + ((chunk & 1) != 0 ? place : 0);
-      uint4 *s_x = reinterpret_cast<uint4 *>(at_place);
-      float *s_sum = reinterpret_cast<float *>(at_place + place_x);
-#pragma unroll
-      for (int i = 0; i < kMost; ++i) {
-        const unsigned at = i * kMatvecThreads + threadIdx.x, r = at >> pieces_log;
-        if (at < all) store_x<TILES, PARTS, G, X>(v[i], r, at - (r << pieces_log), rows, s_x, s_sum);
-      }
-      if (chunk + 1 < chunks) ask(chunk + 1);
-      __syncthreads();
-#pragma unroll 1
-      for (int here = part_of; here < 1 << p.chunk_log; here += share) {
-        const int at = (chunk << p.chunk_log) + here;
-        if (at < whole) {  // (uniform)
-          Slab<G, S> now[WIDE];
-#pragma unroll
-          for (int w = 0; w < WIDE; ++w) now[w] = slab[w];
-          if (at + share < whole) fetch(at + share);
-          add_slab<TILES, PARTS, G, S, WIDE>(total, now, s_x, s_sum, at_x, rows, here, quarter);
-        } else if (at < p.slabs) {  // the row's end
-#pragma unroll
-          for (int w = 0; w < WIDE; ++w) slab[w] = load_last_slab<G, S>(p, row[w].codes, row[w].scales, row[w].zeros, at, quarter);
-          add_slab<TILES, PARTS, G, S, WIDE>(total, slab, s_x, s_sum, at_x, rows, here, quarter);
-        }
-      }
-    }
-    finish_tiles<TILES, WIDE>(p, total, s_join, share, part_of, wave, lane, r0, rows, n0);
-  }
+// More rows, or more columns than LDS has room for: x is laid out as LDS will have it by a launch of its own, slab by slab, each with its groups' sums behind it.  A
+// wavefront takes a row of a slab.
+template <int PARTS, int G, typename X> __global__ void __launch_bounds__(256) matvec_lay_out_kernel(const MatvecParams p) {
+  const int lane = threadIdx.x & 63;
+  const long long r = blockIdx.y * 4LL + (threadIdx.x >> 6) % 4, block = r / kMatvecRows, r0 = block * kMatvecRows;
+  if (r >= p.R) return;
+  const unsigned piece = blockIdx.x * 64 + lane, slab = piece >> 4;
+  if ((int)slab >= p.slabs) return;  // (16 lanes at a time)
+  const int pitch = 16 * p.tiles;
+  char *image = p.image + block * p.image_stride + (long long)slab * slab_bytes(PARTS, p.tiles, G);
+  const Piece<X> v = (long long)piece * 8 < p.D ? load_x<X>(p, r, (int)piece * 8) : Piece<X>{};
+  store_x<PARTS, G, X>(v, (unsigned)(r - r0), piece & 15, pitch, p.tiles, reinterpret_cast<uint4 *>(image), reinterpret_cast<float *>(image + 256 * PARTS * pitch));
 }
 
-template <int TILES, int PARTS, int G, typename S, typename X> hipError_t launch_tiles(const MatvecParams &p, dim3 grid, size_t lds, hipStream_t st) {
-  if (p.streamed == 0) matvec_quantized_kernel<PARTS, G, S, X><<<grid, kMatvecThreads, lds, st>>>(p);  // (up to 16 rows)
-  else matvec_streamed_kernel<TILES, PARTS, G, S, X><<<grid, kMatvecThreads, lds, st>>>(p);
+// x by parts of a few slabs, in two places of LDS in turn: the next part, and the codes that go with it, are asked for before this one is multiplied.  A wavefront has two
+// tiles of columns, so that what it reads of x serves both; every workgroup takes its tiles through all of x once.  Wavefronts that share tiles take a slab of
+// a part each.  Every load is made under no condition, those behind an end from the last place there is: how many are under way is known then, and each is waited for by
+// itself.  (With a condition around what a part does not need, 64 rows of 4096 with 128 256 columns took 194 us.)
+template <int TILES, int PARTS, int G, typename S, bool Z, bool SHARED>
+__global__ void __launch_bounds__(kMatvecThreads, 2) matvec_streamed_kernel(const MatvecParams p) {
+  constexpr int WIDE = 2, kSlabs = streamed_slabs(TILES, PARTS), kShare = SHARED ? kSlabs : 1, kTurns = kSlabs / kShare;
+  constexpr int kSize = (int)slab_bytes(PARTS, TILES, G), kPlace = kSize * kSlabs, kUnits = kPlace / 16, kEach = (kUnits + kMatvecThreads - 1) / kMatvecThreads;
+  extern __shared__ __align__(16) char s_dyn[];
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int part_of = wave % kShare, tile_of = wave / kShare, column = lane & 15, quarter = lane >> 4;
+  constexpr int kTilesEach = (kMatvecThreads >> 6) / kShare;
+  const long long r0 = (long long)blockIdx.y * kMatvecRows;
+  const int rows = (int)(p.R - r0 < kMatvecRows ? p.R - r0 : kMatvecRows);
+  const u32x4 *image = reinterpret_cast<const u32x4 *>(p.image + blockIdx.y * p.image_stride);
+  const int whole = (int)(p.D / 128), chunks = (p.slabs + kSlabs - 1) / kSlabs, image_units = p.slabs * (kSize / 16);
+  int at_x[TILES];
+#pragma unroll
+  for (int t = 0; t < TILES; ++t) at_x[t] = quarter * 16 * TILES + 16 * t + column;
+  long long n0[WIDE];
+  Row<S> row[WIDE];
+  f32x4 total[WIDE][TILES];
+#pragma unroll
+  for (int w = 0; w < WIDE; ++w) {
+    const int tile = tile_of + w * kTilesEach;
+    const long long at = (long long)blockIdx.x * p.block_tiles + tile;
+    n0[w] = tile < p.block_tiles && at * 16 < p.N ? at * 16 : -1;
+    row[w] = row_of<S>(p, (n0[w] < 0 ? 0 : n0[w]) + column);
+    if (whole == 0) row[w] = {reinterpret_cast<const uint8_t *>(image), reinterpret_cast<const S *>(image), reinterpret_cast<const uint8_t *>(image)};  // (read, not used)
+#pragma unroll
+    for (int t = 0; t < TILES; ++t) total[w][t] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+  }
+  const int last_whole = whole > 0 ? whole - 1 : 0;
+  u32x4 next[kEach];
+  RawSlab<G, S> coming[kTurns][WIDE], here[kTurns][WIDE];
+  const auto ask = [&](int chunk) __attribute__((always_inline)) {
+#pragma unroll
+    for (int i = 0; i < kEach; ++i) {
+      const int in = i * kMatvecThreads + (int)threadIdx.x, at = chunk * kUnits + (in < kUnits ? in : kUnits - 1);
+      next[i] = image[at < image_units ? at : image_units - 1];
+    }
+#pragma unroll
+    for (int i = 0; i < kTurns; ++i) {
+      const int slab = chunk * kSlabs + i * kShare + part_of;
+#pragma unroll
+      for (int w = 0; w < WIDE; ++w) coming[i][w] = load_slab<Z, G, S>(p, row[w].codes, row[w].scales, row[w].zeros, slab < last_whole ? slab : last_whole, quarter);
+    }
+  };
+  ask(0);
+#pragma unroll 1
+  for (int chunk = 0; chunk < chunks; ++chunk) {
+    char *at_place = s_dyn + ((chunk & 1) != 0 ? kPlace : 0);  // (free: all have been through the last barrier after they were done with it)
+#pragma unroll
+    for (int i = 0; i < kEach; ++i) {
+      const int in = i * kMatvecThreads + (int)threadIdx.x;
+      reinterpret_cast<u32x4 *>(at_place)[in < kUnits ? in : kUnits - 1] = next[i];  // (the last one by several lanes, the same)
+    }
+#pragma unroll
+    for (int i = 0; i < kTurns; ++i)
+#pragma unroll
+      for (int w = 0; w < WIDE; ++w) here[i][w] = coming[i][w];
+    __builtin_amdgcn_sched_barrier(0);
+    ask(chunk + 1 < chunks ? chunk + 1 : chunk);
+    __syncthreads();
+#pragma unroll
+    for (int i = 0; i < kTurns; ++i) {
+      const int in = i * kShare + part_of, slab = chunk * kSlabs + in;
+      if (slab < whole) {  // (uniform)
+        Slab<G, S> now[WIDE];
+#pragma unroll
+        for (int w = 0; w < WIDE; ++w) now[w] = slab_of<Z>(here[i][w]);
+        const char *at = at_place + in * kSize;
+        add_slab<TILES, PARTS, G, S, WIDE>(total, now, reinterpret_cast<const uint4 *>(at), reinterpret_cast<const float *>(at + 256 * PARTS * 16 * TILES), at_x, 16 * TILES, quarter);
+      }
+    }
+  }
+  if (whole < p.slabs && (whole % kSlabs) % kShare == part_of) {  // the row's end, whose part of x is still there
+    const char *at = s_dyn + (((chunks - 1) & 1) != 0 ? kPlace : 0) + (whole % kSlabs) * kSize;
+    Slab<G, S> now[WIDE];
+#pragma unroll
+    for (int w = 0; w < WIDE; ++w) {
+      const Row<S> r = row_of<S>(p, (n0[w] < 0 ? 0 : n0[w]) + column);
+      now[w] = slab_of<Z>(load_last_slab<Z, G, S>(p, r.codes, r.scales, r.zeros, whole, quarter));
+    }
+    add_slab<TILES, PARTS, G, S, WIDE>(total, now, reinterpret_cast<const uint4 *>(at), reinterpret_cast<const float *>(at + 256 * PARTS * 16 * TILES), at_x, 16 * TILES, quarter);
+  }
+  finish_tiles<TILES, WIDE>(p, total, reinterpret_cast<float *>(s_dyn + 2 * kPlace), kShare, part_of, wave, lane, r0, rows, n0);
+}
+
+template <int PARTS, int G, typename X> hipError_t lay_out(const MatvecParams &p, hipStream_t st) {
+  const dim3 grid((unsigned)((p.slabs * 16 + 63) / 64), (unsigned)((p.R + 3) / 4));
+  matvec_lay_out_kernel<PARTS, G, X><<<grid, 256, 0, st>>>(p);
   return hipGetLastError();
 }
-template <int PARTS, int G, typename S, typename X> hipError_t by_tiles(const MatvecParams &p, int tiles, dim3 grid, size_t lds, hipStream_t st) {
-  switch (tiles) {
-    case 1: return launch_tiles<1, PARTS, G, S, X>(p, grid, lds, st);
-    case 2: return launch_tiles<2, PARTS, G, S, X>(p, grid, lds, st);
-    case 3: return launch_tiles<3, PARTS, G, S, X>(p, grid, lds, st);
-    default: return launch_tiles<4, PARTS, G, S, X>(p, grid, lds, st);
+template <int TILES, int PARTS, int G, typename S, bool Z, typename X> hipError_t launch_tiles(const MatvecParams &p, dim3 grid, size_t lds, hipStream_t st) {
+  if (p.streamed == 0) {  // (up to 16 rows)
+    matvec_quantized_kernel<PARTS, G, S, Z, X><<<grid, kMatvecThreads, lds, st>>>(p);
+  } else {
+    const hipError_t e = lay_out<PARTS, G, X>(p, st);
+    if (e != hipSuccess) return e;
+    if (p.share_log == 0) matvec_streamed_kernel<TILES, PARTS, G, S, Z, false><<<grid, kMatvecThreads, lds, st>>>(p);
+    else if constexpr (streamed_slabs(TILES, PARTS) > 1) matvec_streamed_kernel<TILES, PARTS, G, S, Z, true><<<grid, kMatvecThreads, lds, st>>>(p);
   }
+  return hipGetLastError();
+}
+template <int PARTS, int G, typename S, bool Z, typename X> hipError_t by_zeros(const MatvecParams &p, int tiles, dim3 grid, size_t lds, hipStream_t st) {
+  switch (tiles) {
+    case 1: return launch_tiles<1, PARTS, G, S, Z, X>(p, grid, lds, st);
+    case 2: return launch_tiles<2, PARTS, G, S, Z, X>(p, grid, lds, st);
+    case 3: return launch_tiles<3, PARTS, G, S, Z, X>(p, grid, lds, st);
+    default: return launch_tiles<4, PARTS, G, S, Z, X>(p, grid, lds, st);
+  }
+}
+template <int PARTS, int G, typename S, typename X> hipError_t by_tiles(const MatvecParams &p, int tiles, dim3 grid, size_t lds, hipStream_t st) {
+  return p.zeros != nullptr ? by_zeros<PARTS, G, S, true, X>(p, tiles, grid, lds, st) : by_zeros<PARTS, G, S, false, X>(p, tiles, grid, lds, st);
 }
 template <int PARTS, typename X> hipError_t launch_matvec(const MatvecParams &p, int tiles, int group, int scales_type, dim3 grid, size_t lds, hipStream_t st) {
   const bool wide = scales_type == LLC_F32;

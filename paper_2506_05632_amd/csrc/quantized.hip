@@ -244,9 +244,70 @@ extern "C" int llc_embed_quantized(const llc_embed_quantized_args *a) {
   });
 }
 
+namespace llc {
+namespace {
+
+struct MatvecPlan {
+  int tiles, parts, streamed, share_log, block_tiles;
+  unsigned tile_blocks, blocks, passes;
+  size_t lds;
+  long long image_stride;
+  size_t workspace;
+};
+MatvecPlan plan_matvec(long long R, long long N, long long D, int group, int dtype) {
+  MatvecPlan m = {};
+  const int rows = (int)(R < kMatvecRows ? R : kMatvecRows), slabs = (int)((D + 127) / 128);
+  m.tiles = (rows + 15) / 16;
+  m.parts = dtype == LLC_F32 ? 3 : 1;
+  m.passes = (unsigned)((R + kMatvecRows - 1) / kMatvecRows);
+  const long long column_tiles = (N + 15) / 16;
+  constexpr int waves = kMatvecThreads / 64;
+  constexpr size_t kLds = 156 << 10;  // that a workgroup may have, of a CU's 160 KB
+  const auto join_bytes = [&](int wide, int log) { return log > 0 ? (size_t)waves * wide * m.tiles * 1024 : 0; };
+  // Wavefronts share tiles of few columns until some 2048 of them are at work, eight a CU.
+  const auto share_for = [&](int wide, int most) {
+    int log = 0;
+    while (log < 3 && (column_tiles << log) < 2048LL * wide && (2 << log) <= most) ++log;
+    return log;
+  };
+  m.share_log = share_for(1, slabs);
+  m.lds = (size_t)slabs * ((size_t)256 * m.parts * pitch_of(rows) + (size_t)(128 / group) * 64) + join_bytes(1, m.share_log);
+  m.streamed = m.tiles == 1 && m.lds <= kLds ? 0 : 1;
+  if (m.streamed == 0) {
+    const int each = waves >> m.share_log;
+    m.tile_blocks = (unsigned)((column_tiles + each - 1) / each);
+    const unsigned resident = 256u * (m.lds <= kLds / 2 ? 2 : 1);
+    const unsigned turns = (m.tile_blocks + resident - 1) / resident;  // (as many blocks for each workgroup, or one less)
+    m.blocks = (m.tile_blocks + turns - 1) / turns;
+    return m;
+  }
+  const size_t slab = (size_t)slab_bytes(m.parts, m.tiles, group);
+  const int part = streamed_slabs(m.tiles, m.parts), part_log = part == 4 ? 2 : part == 2 ? 1 : 0;
+  m.share_log = column_tiles < 2048 && part <= slabs ? part_log : 0;
+  m.lds = 2 * slab * (size_t)part + join_bytes(2, m.share_log);
+  const long long each = 2 * (waves >> m.share_log), turns = (column_tiles + 256 * each - 1) / (256 * each);
+  m.block_tiles = (int)((column_tiles + 256 * turns - 1) / (256 * turns));
+  m.tile_blocks = m.blocks = (unsigned)((column_tiles + m.block_tiles - 1) / m.block_tiles);
+  m.image_stride = (long long)(((size_t)slabs * slab + 255) & ~(size_t)255);
+  m.workspace = (size_t)m.image_stride * m.passes;
+  return m;
+}
+// (a launch takes fewer than 2^32 threads: of the layout of x, and, of the products, for every 64 rows a workgroup for at least 13 tiles of 16 columns)
+bool matvec_sizes_ok(long long R, long long N, long long D) {
+  return R >= 0 && R <= (1LL << 17) && N >= 1 && N <= kMaxIndex && D >= 1 && D <= (1LL << 27) && R * D <= (1LL << 34) && (R <= 16 || (R + 63) / 64 * ((N + 15) / 16) <= 1LL << 25);
+}
+
+}  // namespace
+}  // namespace llc
+
+extern "C" size_t llc_matvec_quantized_workspace_size(int64_t R, int64_t N, int64_t D, int32_t group, int32_t dtype) {
+  if (!matvec_sizes_ok(R, N, D) || R == 0 || !known_group(group) || !known_type(dtype)) return 0;
+  return plan_matvec(R, N, D, group, dtype).workspace;
+}
+
 extern "C" int llc_matvec_quantized(const llc_matvec_quantized_args *a) {
   if (a == nullptr) return LLC_E_NULL;
-  if (a->R < 0 || a->R > (1LL << 20) || a->N < 1 || a->N > kMaxIndex || a->D < 1 || a->D > (1LL << 27)) return LLC_E_SHAPE;
+  if (!matvec_sizes_ok(a->R, a->N, a->D)) return LLC_E_SHAPE;
   if ((a->flags & ~LLC_FLAG_DRY_RUN) != 0 || !known_group(a->group)) return LLC_E_OPTION;
   if (a->R == 0) return LLC_OK;
   if (a->x == nullptr || a->out == nullptr) return LLC_E_NULL;
@@ -255,54 +316,21 @@ extern "C" int llc_matvec_quantized(const llc_matvec_quantized_args *a) {
   if (a->x_stride_r < 0 || a->out_stride_r < a->N) return LLC_E_SHAPE;
   if (!known_type(a->dtype) || !known_type(a->out_dtype)) return LLC_E_DTYPE;
   if (!fits(a->x, type_size(a->dtype)) || !fits(a->out, type_size(a->out_dtype))) return LLC_E_ALIGN;
+  const MatvecPlan m = plan_matvec(a->R, a->N, a->D, a->group, a->dtype);
+  if (m.workspace > 0 && (a->workspace == nullptr || !fits(a->workspace, 256) || a->workspace_bytes < m.workspace)) return LLC_E_WORKSPACE;
   MatvecParams p = {};
   p.R = a->R; p.N = a->N; p.D = a->D; p.x = a->x; p.x_stride = a->x_stride_r;
   p.codes = a->codes; p.codes_stride = a->codes_stride_n; p.scales = a->scales; p.scales_stride = a->scales_stride_n;
   p.zeros = a->zeros; p.zeros_stride = a->zeros_stride_n; p.out = a->out; p.out_stride = a->out_stride_r; p.out_type = a->out_dtype;
   p.groups = (int)groups_of(a->D, a->group);
   p.slabs = (int)((a->D + 127) / 128);
-  const int rows = (int)(a->R < kMatvecRows ? a->R : kMatvecRows), tiles = (rows + 15) / 16, parts = a->dtype == LLC_F32 ? 3 : 1;
-  const long long column_tiles = (a->N + 15) / 16;
-  constexpr int waves = kMatvecThreads / 64;
-  constexpr size_t kLds = 156 << 10;  // that a workgroup may have, of a CU's 160 KB
-  const auto x_bytes = [&](int slabs) { return matvec_x_bytes(parts, rows, tiles, a->group, slabs); };
-  // x stays in LDS where it fits; there, few columns are shared until some 2048 wavefronts are at work, eight a CU.
-  const auto share_for = [&](int wide, int most) {
-    int log = 0;
-    while (log < 3 && (column_tiles << log) < 2048LL * wide && (2 << log) <= most) ++log;
-    return log;
-  };
-  size_t lds;
-  unsigned blocks;
-  p.share_log = share_for(1, p.slabs);
-  lds = x_bytes(p.slabs) + matvec_join_bytes(tiles, 1, p.share_log);
-  p.streamed = tiles == 1 && lds <= kLds ? 0 : 1;
-  if (p.streamed == 0) {
-    const int each = waves >> p.share_log;
-    p.tile_blocks = (unsigned)((column_tiles + each - 1) / each);
-    const unsigned resident = 256u * (unsigned)(lds <= kLds / 2 ? 2 : 1);
-    // (as many blocks for each workgroup, or one less)
-    const unsigned turns = (p.tile_blocks + resident - 1) / resident;
-    blocks = (p.tile_blocks + turns - 1) / turns;
-  } else {
-    const int most = kMatvecThreads * (parts == 3 ? kStreamedPieces<float> : kStreamedPieces<uint16_t>) / (16 * rows);  // slabs that the threads have in flight
-    const auto streamed_bytes = [&](int chunk_log, int share_log) { return 2 * x_bytes(1 << chunk_log) + matvec_join_bytes(tiles, 2, share_log); };
-    p.share_log = share_for(2, p.slabs < most ? p.slabs : most);
-    while (p.share_log > 0 && streamed_bytes(p.share_log, p.share_log) > kLds) --p.share_log;
-    p.chunk_log = p.share_log;
-    while ((2 << p.chunk_log) <= most && (1 << p.chunk_log) < p.slabs && streamed_bytes(p.chunk_log + 1, p.share_log) <= kLds) ++p.chunk_log;
-    lds = streamed_bytes(p.chunk_log, p.share_log);
-    const long long each = 2 * (waves >> p.share_log), turns = (column_tiles + 256 * each - 1) / (256 * each);
-    p.block_tiles = (int)((column_tiles + 256 * turns - 1) / (256 * turns));
-    p.tile_blocks = (unsigned)((column_tiles + p.block_tiles - 1) / p.block_tiles);
-    blocks = p.tile_blocks;
-  }
-  const unsigned passes = (unsigned)((a->R + kMatvecRows - 1) / kMatvecRows);
-  const dim3 grid(blocks, passes);
+  p.streamed = m.streamed; p.share_log = m.share_log; p.tile_blocks = m.tile_blocks; p.tiles = m.tiles; p.block_tiles = m.block_tiles;
+  p.image = (char *)a->workspace; p.image_stride = m.image_stride;
+  const dim3 grid(m.blocks, m.passes);
   if ((a->flags & LLC_FLAG_DRY_RUN) != 0) return LLC_OK;
   hipStream_t st = (hipStream_t)a->stream;
   return between_events(a->ev_begin, a->ev_end, st, [&] {
-    return a->dtype == LLC_F32 ? launch_matvec_f32(p, tiles, a->group, a->scales_dtype, grid, lds, st)
-                               : launch_matvec_bf16(p, tiles, a->group, a->scales_dtype, grid, lds, st);
+    return a->dtype == LLC_F32 ? launch_matvec_f32(p, m.tiles, a->group, a->scales_dtype, grid, m.lds, st)
+                               : launch_matvec_bf16(p, m.tiles, a->group, a->scales_dtype, grid, m.lds, st);
   });
 }

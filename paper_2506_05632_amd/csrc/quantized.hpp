@@ -39,19 +39,23 @@ struct MatvecParams {
   int groups;       // of a row
   int slabs;        // of 128 entries, of a row
   int streamed;     // x goes through LDS by parts
-  int chunk_log;    // log2 of the slabs of a part, which are at least as many as wavefronts share a tile
-  int share_log;    // log2 of the wavefronts that share a tile by columns
+  int share_log;    // log2 of the wavefronts that share a tile by columns (where x is streamed: one, or as many as a part has slabs)
   unsigned tile_blocks;  // workgroups' worth of tiles
-  int block_tiles;       // that a workgroup takes at a time, where x is streamed
+  // where x is streamed:
+  int tiles;             // of 16 rows, of up to 64
+  int block_tiles;       // of 16 columns, that a workgroup takes
+  char *image;           // x as LDS has it, 64 rows at a time
+  long long image_stride;
 };
 constexpr int kMatvecThreads = 512;
 constexpr int kMatvecRows = 64;  // rows of x that one pass over the layer serves
 
-template <typename X> constexpr int kStreamedPieces = 8 / sizeof(X);  // of eight columns of x that a thread has in flight
+// Slabs of a part of x, where it is streamed: two parts fit LDS beside the sums of wavefronts that share tiles, and the next one the registers.
+__host__ __device__ constexpr int streamed_slabs(int tiles, int parts) { return parts == 1 ? (tiles <= 2 ? 4 : 2) : tiles == 1 ? 4 : tiles == 2 ? 2 : 1; }
+// Bytes of a slab of x with its groups' sums, as it is laid out.
+__host__ __device__ constexpr long long slab_bytes(int parts, int tiles, int group) { return 256LL * parts * 16 * tiles + (128 / group) * tiles * 64; }
 
-// Bytes of LDS of a workgroup: x and the groups' sums of it, and the sums of wavefronts that share tiles.
-inline size_t matvec_x_bytes(int parts, int rows, int tiles, int group, int slabs) { return (size_t)slabs * ((size_t)256 * parts * rows + (size_t)(128 / group) * tiles * 64); }
-inline size_t matvec_join_bytes(int tiles, int wide, int share_log) { return share_log > 0 ? (size_t)(kMatvecThreads / 64) * wide * tiles * 1024 : 0; }
+__host__ __device__ inline int pitch_of(int rows) { return rows | 1; }  // (of rows in LDS, where they are put there from memory)
 
 // (one translation unit for each type of x)
 hipError_t launch_matvec_bf16(const MatvecParams &p, int tiles, int group, int scales_type, dim3 grid, size_t lds, hipStream_t st);

@@ -85,10 +85,12 @@ def test_embed_arguments(kw, code):
 
 
 @pytest.mark.parametrize("kw,code", BAD_LAYERS + [
-    (dict(x=None), -1), (dict(out=None), -1), (dict(R=-1), -2), (dict(R=(1 << 20) + 1), -2), (dict(N=0), -2), (dict(D=(1 << 27) + 1), -2), (dict(x_stride_r=-1), -2),
+    (dict(x=None), -1), (dict(out=None), -1), (dict(R=-1), -2), (dict(R=(1 << 17) + 1), -2), (dict(N=0), -2), (dict(D=(1 << 27) + 1), -2), (dict(x_stride_r=-1), -2),
     (dict(out_stride_r=9), -2), (dict(dtype=2), -4), (dict(out_dtype=-1), -4), (dict(x=0x7002), -5), (dict(out=0x6002), -5), (dict(R=0, x=None), 0),
-    (dict(flags=4, R=1 << 20), 0), (dict(flags=4, N=(1 << 31) - 5, out_stride_r=1 << 31), 0),
-    (dict(flags=4, D=1 << 27, codes_stride_n=1 << 26, scales_stride_n=1 << 22, zeros_stride_n=1 << 22), 0)])
+    (dict(R=17), -6), (dict(R=17, workspace=0x8010, workspace_bytes=1 << 30), -6), (dict(R=17, workspace=0x8000, workspace_bytes=100), -6),
+    (dict(flags=4, R=1 << 17, workspace=0x8000, workspace_bytes=1 << 40), 0), (dict(R=1 << 17, D=1 << 20, codes_stride_n=1 << 20, scales_stride_n=1 << 20, zeros_stride_n=1 << 20), -2),
+    (dict(R=17, N=1 << 30, out_stride_r=1 << 30), -2), (dict(flags=4, N=(1 << 31) - 5, out_stride_r=1 << 31), 0),
+    (dict(flags=4, D=1 << 27, codes_stride_n=1 << 26, scales_stride_n=1 << 22, zeros_stride_n=1 << 22, workspace=0x8000, workspace_bytes=1 << 40), 0)])
 def test_matvec_arguments(kw, code):
     assert _code("llc_matvec_quantized", dict(LAYER, R=3, dtype=0, out_dtype=0, x=0x7000, x_stride_r=100, out=0x6000, out_stride_r=10), kw) == code
     assert llc.load().llc_matvec_quantized(None) == -1
