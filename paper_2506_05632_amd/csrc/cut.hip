@@ -8,8 +8,10 @@
 //   2. The rest of the row goes by: its largest, the list, in the order of the indexes, and, where a share of the whole mass is
 //      asked for, or no cut at all, the masses.
 //   3. The list is sorted, its masses are summed along the order, and the cut is read off; the tokens follow from sums along the indexes.
-// Rows whose kept entries the list turns out not to hold are narrowed down instead: a histogram of the masses (or counts) by value finds the range that the
-// cut is in, a list of that range's entries the place (histograms by the keys' bits, where they are too many), and tokens follow from the sums of tiles of the row.
+// Rows whose kept entries are too many for the list, by what the sample shows or the list turns out to hold, are read twice more: a histogram of
+// counts by value, 256 buckets a unit of ln, shows nearly where the cut is, and a pass with exact masses takes the sums before the buckets about it and lists what is in
+// them.  That confirms the cut or not (256 rows of 128 256 in bf16, all of them so deep: 147 us; by histograms of exact masses 260).  What is left is narrowed down by histograms of
+// masses (or counts) of the row, and by the keys' bits.  Tokens follow from the sums of tiles of the row.
 //
 // Masses are exp((x - reference) / temp) in fp64: a border in a run of 128 000 entries that share the mass is hit by rounding otherwise.  (An fp64 multiply-add takes
 // as long as one in fp32 here; an entry takes some 23 operations, which at 128 256 entries is 19 us of a CU and about what its share of the memory takes for rows
@@ -29,6 +31,9 @@ constexpr int kMostTiles = 2048;  // of a row, whose masses LDS holds
 constexpr int kPiece = 512;       // entries that a wavefront takes at a time, eight a lane
 constexpr int kAhead = 4;         // pieces that it has asked for
 constexpr int kSample = 2;        // pieces of a wavefront that the sample has
+constexpr int kFine = 8192;       // buckets of the histogram of counts
+constexpr float kFinePerUnit = 256.0f;  // of them for each unit of ln
+constexpr int kRange = 2048;      // entries about the cut that are listed
 constexpr int kByMass = 256;      // entries that the list aims at where a share of the mass is asked for
 constexpr int kByCount = 1800;    // top_k up to which the list is tried
 constexpr long long kMostRowBlocks = 1LL << 22;  // rows of a launch
@@ -138,8 +143,14 @@ template <typename T> __device__ __forceinline__ T wave_scan(T v) { return wave_
 template <typename T> __device__ __forceinline__ T wave_sum(T v) { return lane_value(wave_scan(v), 63); }
 
 struct Shared {
-  alignas(16) uint32_t list_key[kList];
-  int list_index[kList];
+  union {
+    struct {
+      alignas(16) uint32_t list_key[kList];
+      int list_index[kList];
+    };
+    int equals[kMostTiles];  // of tiles, then summed along the indexes
+    alignas(16) uint32_t fine[kFine];
+  };
   union {
     unsigned long long histogram[kBuckets];
     double along[kList > kMostTiles ? kList : kMostTiles];  // masses summed along the indexes: of the list's entries, or of tiles
@@ -155,6 +166,7 @@ struct Shared {
   int wave_count[kWaves];
   float wave_high[kWaves], wave_low[kWaves];
   int n_few;
+  int fine_first, fine_last, fine_at;
   unsigned long long pick_above;
   int pick;
   uint32_t pick_index;
@@ -322,6 +334,22 @@ __device__ __forceinline__ double mass_of_eight(const float (&v)[8], double refe
   return sum;
 }
 
+// The same, and of those before `until` among places on the histogram of counts.
+__device__ __forceinline__ double mass_of_eight(const float (&v)[8], const float (&at)[8], float until, double reference, double scale, double &before) {
+  double sum = 0.0;
+#pragma unroll
+  for (int h = 0; h < 8; h += 4) {
+    double m[4];
+#pragma unroll
+    for (int j = 0; j < 4; ++j) m[j] = mass_of(v[h + j], reference, scale);
+    sum += (m[0] + m[1]) + (m[2] + m[3]);
+#pragma unroll
+    for (int j = 0; j < 4; ++j) before += at[h + j] < until ? m[j] : 0.0;
+    __builtin_amdgcn_sched_barrier(0);
+  }
+  return sum;
+}
+
 // The lanes before, and those of all: how many entries are marked.
 __device__ __forceinline__ int marked_before(const bool (&hit)[8], int &all) {
   int before = 0;
@@ -483,6 +511,47 @@ __device__ __forceinline__ int pick_bucket(Shared &s, float share, unsigned long
   __syncthreads();
   return pick;
 }
+// Where a bucket of the histogram of counts lies: bf16 numbers are a power of two of buckets apart, which would be in few banks.
+__device__ __forceinline__ int place_of(int bucket) { return bucket ^ (bucket >> 5); }
+// The range of the histogram of counts that holds the cut, by count or by what the buckets' masses about are; false: none, or the last bucket's.
+// (Of a bucket's entries each mass is within 2^-8.5 of its middle's, on either side; 2^-12 of the whole on either side of a share is far more than that leaves in
+// rows of many entries.  The range is only where the cut is looked for.)  many: more entries than the list's masses have room for, in a single bucket then.
+__device__ __forceinline__ bool pick_range(Shared &s, float share, unsigned wanted, int &first, int &last, bool &many) {
+  constexpr int kEach = kFine / kThreads;
+  const int b0 = threadIdx.x * kEach;
+  const float rate = -1.442695f / kFinePerUnit;
+  const auto weight = [&](int b) { return share > 0.0f ? (double)((float)s.fine[place_of(b)] * __builtin_amdgcn_exp2f(((float)b + 0.5f) * rate)) : (double)s.fine[place_of(b)]; };
+  double mine = 0.0, all;
+#pragma unroll 4
+  for (int i = 0; i < kEach; ++i) mine += weight(b0 + i);
+  double upto = block_scan_before(mine, s.wave_double, all);
+  const double from = share > 0.0f ? fmax((double)share - 0x1p-12, 0.0) * all : (double)wanted;
+  const double to = share > 0.0f ? fmin((double)share + 0x1p-12, 0.5 * (1.0 + (double)share)) * all : (double)wanted;
+  const double here = share > 0.0f ? (double)share * all : (double)wanted;
+  if (threadIdx.x == 0) { s.fine_first = from > 0.0 ? kFine : 0; s.fine_last = s.fine_at = kFine - 1; }
+  __syncthreads();
+  if (upto < to && upto + mine >= from) {
+#pragma unroll 1
+    for (int i = 0; i < kEach; ++i) {
+      const double next = upto + weight(b0 + i);
+      if (upto < from && next >= from) s.fine_first = b0 + i;
+      if (upto < to && next >= to) s.fine_last = b0 + i;
+      if (upto < here && next >= here) s.fine_at = b0 + i;
+      upto = next;
+    }
+  }
+  __syncthreads();
+  first = s.fine_first;
+  last = s.fine_last;
+  int mine_within = 0, total;
+#pragma unroll 4
+  for (int i = 0; i < kEach; ++i) mine_within += b0 + i >= first && b0 + i <= last ? (int)s.fine[place_of(b0 + i)] : 0;
+  block_scan_before(mine_within, s.wave_count, total);
+  many = total > kRange;
+  if (many) first = last = s.fine_at;  // the one bucket (of numbers in 16 bits, thousands may be equal)
+  __syncthreads();
+  return first <= last && last < kFine - 1;
+}
 // Weights: of an entry 1, or its mass in units, rounded.
 struct Weight {
   bool counted;
@@ -643,7 +712,7 @@ __device__ __forceinline__ float bound_of(Shared &s, float mine, float top, floa
   return pick < 0 ? -INFINITY : top == least ? top : top - (float)(pick + 2) / per;
 }
 
-template <typename E, bool SAMPLE> __device__ __forceinline__ void cut_row(const CutParams &p, long long r, Shared &s) {
+template <typename E, bool SAMPLE, bool RANGE> __device__ __forceinline__ void cut_row(const CutParams &p, long long r, Shared &s) {
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const E *row = reinterpret_cast<const E *>(p.x) + r * p.stride;
   E *out = SAMPLE ? nullptr : reinterpret_cast<E *>(p.out) + r * p.out_stride;
@@ -660,6 +729,8 @@ template <typename E, bool SAMPLE> __device__ __forceinline__ void cut_row(const
   const bool uncut = !by_mass && cut.top_k == 0 && cut.min_p == 0.0f;
   const bool try_list = least_too || (cut.top_k > 0 ? cut.top_k <= kByCount : by_mass);
   const bool need_mass = by_mass && cut.top_k == 0;
+  const bool can_range = RANGE && (need_mass || (cut.top_k > 0 && !by_mass));
+  bool deep = !try_list && can_range;  // (no list would hold the kept entries)
   float largest = -INFINITY;
 #pragma unroll
   for (int i = 0; i < kSample; ++i) {
@@ -706,6 +777,31 @@ template <typename E, bool SAMPLE> __device__ __forceinline__ void cut_row(const
       const float expected = share * (float)(counted ? (int)cut.top_k : kByMass);
       const int wanted = share == 1.0f ? (int)expected : (int)(expected + (counted ? 4.5f * sqrtf(expected) + 6.0f : 1.0f));
       bound = bound_of(s, largest, reference, sample_low, wanted);
+      if (RANGE && need_mass && share < 1.0f) {  // a list that has less than seven tenths of the mass asked for in the sample is not made
+        float above = 0.0f, sum = 0.0f;
+#pragma unroll
+        for (int i = 0; i < kSample; ++i) {
+          if (part.first + i * kPiece < part.last) {
+            float v[8];
+            widen_raw(ring.raw[i], part.first + i * kPiece, lane, (unsigned)p.V, v);
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {
+              const float m = __builtin_amdgcn_exp2f((v[j] - reference) * (float)cut.scale);
+              sum += m;
+              above += v[j] >= bound ? m : 0.0f;
+            }
+          }
+        }
+        above = wave_sum(above);
+        sum = wave_sum(sum);
+        __syncthreads();
+        if (lane == 0) { s.wave_high[wave] = above; s.wave_low[wave] = sum; }
+        __syncthreads();
+        above = sum = 0.0f;
+#pragma unroll
+        for (int w = 0; w < kWaves; ++w) { above += s.wave_high[w]; sum += s.wave_low[w]; }
+        deep = above < 0.7f * cut.top_p * sum;
+      }
     }
     if (least_too) {
       const float to = (float)((double)reference + least);
@@ -737,71 +833,220 @@ template <typename E, bool SAMPLE> __device__ __forceinline__ void cut_row(const
       ++tile; piece = 0; mass = 0.0;
     }
   };
-  ring.run(row, (unsigned)p.V, part, lane, see);
-  float top, unused;
-  block_ends(high, 0.0f, top, unused);
-  const double top_wide = (double)top;
+  float top = reference, unused;
+  if (!deep) {
+    ring.run(row, (unsigned)p.V, part, lane, see);
+    block_ends(high, 0.0f, top, unused);
+  }
+  double top_wide = (double)top;
   const auto over_least = [&](float x) { return (double)x - top_wide >= least; };
 
   // 3. the list
   int n = 0;
   double all_mass = 0.0;
-  if (need_mass) all_mass = block_sum(mass, s.wave_double) * exp2_of((reference_wide - top_wide) * cut.scale);
-  bool listed = try_list && join_list(s, list.count, lane, wave, n);
+  if (need_mass && !deep) all_mass = block_sum(mass, s.wave_double) * exp2_of((reference_wide - top_wide) * cut.scale);
+  bool listed = try_list && !deep && join_list(s, list.count, lane, wave, n);
   if (listed && cut.top_k > n && bound > -INFINITY && !by_least) listed = false;  // (there are more below the bound)
   Place place = {0xFFFFFFFFu, (uint32_t)p.V};  // (of the list's entries: their places in the list)
-  bool found = false;
-  if (listed && n <= kFew) {
+  // What the list does not show is looked for in a range about the cut, and what that does not show narrowed down in the row.
+  bool ranged = false, found = uncut;
+  double above_mass = 0.0;  // of the entries before the range
+  int above = 0, above_mine = 0;  // (of all; of the thread's)
+  int equal_kept = 0;  // of equal entries in the range, where they are many; the mass of each
+  double each_equal = 0.0;
+  const auto look_in_few = [&]() __attribute__((always_inline)) {
+    found = true;
     const int e = threadIdx.x;
     sort_list(s, n);
-    int first_n = cut.top_k > 0 && cut.top_k < n ? (int)cut.top_k : n;
+    int first_n = cut.top_k > 0 && cut.top_k - above < n ? (int)cut.top_k - above : n;
     if (by_mass) {  // masses summed along the order
       const double mine = e < n ? mass_of(value_of((uint32_t)(s.sorted[e] >> 32)), top_wide, cut.scale) : 0.0;
       double total;
       const double before = block_scan_before(mine, s.wave_double, total);
       if (e < n) s.masses[e] = before + mine;
       __syncthreads();
-      const double target = (double)cut.top_p * (cut.top_k > 0 ? s.masses[first_n - 1] : all_mass);
+      const double target = (double)cut.top_p * (cut.top_k > 0 ? s.masses[first_n - 1] : all_mass) - above_mass;
       int a = 0, z = first_n;  // the first whose sum reaches the target
       while (a < z) {
         const int mid = (a + z) / 2;
         if (s.masses[mid] >= target) z = mid; else a = mid + 1;
       }
       // (the list may end before; min_p may cut in it all the same)
-      if (a >= first_n && cut.top_k == 0 && bound > -INFINITY) listed = !over_least(value_of((uint32_t)(s.sorted[n - 1] >> 32)));
+      if (ranged) found = a < first_n && (above == 0 || target > 0.0);
+      else if (a >= first_n && cut.top_k == 0 && bound > -INFINITY) found = !over_least(value_of((uint32_t)(s.sorted[n - 1] >> 32)));
       first_n = a + 1 < first_n ? a + 1 : first_n;
     }
     const unsigned long long last = s.sorted[first_n - 1];
     place = {(uint32_t)(last >> 32), (uint32_t)last};
-    found = listed;
-  }
-  // What the order by counting does not show is narrowed down, in the list or, where that does not hold what is asked for, in the row.
+  };
+  if (!RANGE && listed && n <= kFew) look_in_few();
 #pragma unroll 1
-  while (!found) {
+  for (int turn = deep ? 1 : 0; turn < 3 && !found; ++turn) {
+    int lane = threadIdx.x & 63;
+    if constexpr (RANGE) asm volatile("" : "+v"(lane));  // (or every address of a turn would be kept in registers from before the first)
+    if (turn == 0 && (!listed || (!RANGE && n <= kFew))) continue;
+    if (turn == 1) {
+      listed = false;
+      if (!can_range) continue;
+      if constexpr (RANGE) {
+      // a histogram of counts shows where the cut is, nearly
+      const float per = kFinePerUnit / (float)cut.temp, base = reference + 2048.0f / per;
+      __syncthreads();
+      for (int i = threadIdx.x * 4; i < kFine; i += kThreads * 4) *reinterpret_cast<uint4 *>(s.fine + i) = make_uint4(0, 0, 0, 0);
+      __syncthreads();
+      each_piece(row, p, part, lane, [&](unsigned, unsigned, const float (&v)[8]) {
+        high = max_of_three(high, largest_of(v), high);
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+          const float at = (base - v[j]) * per;
+          if (v[j] > -INFINITY) atomicAdd(&s.fine[place_of((int)fminf(fmaxf(at, 0.0f), (float)(kFine - 1)))], 1u);
+        }
+      });
+      block_ends(high, 0.0f, top, unused);
+      top_wide = (double)top;
+      int first, last;
+      bool many;
+      if (!pick_range(s, by_mass ? cut.top_p : 0.0f, (unsigned)cut.top_k, first, last, many)) continue;
+      if (sizeof(E) == 4 && many) continue;
+      // the masses of all and of those before the range, by tiles, and a list of the range
+      const float from = first > 0 ? (float)first : -INFINITY, until = (float)(last + 1);
+      const bool with_mass = SAMPLE || by_mass;
+      double sum = 0.0, sum_before = 0.0, tile_before = 0.0;
+      int equals = 0;
+      float equal_high = -INFINITY, equal_low = INFINITY;
+      piece = above = 0;
+      tile = (long long)wave * p.tiles_wave;
+      list.count = 0;
+      each_piece(row, p, part, lane, [&](unsigned from_piece, unsigned at, const float (&v)[8]) {
+        float to[8];
+        bool hit[8], any = false;
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+          to[j] = (base - v[j]) * per;
+          above += to[j] < from ? 1 : 0;
+          hit[j] = !(to[j] < from) & !(to[j] >= until);
+          any = any | hit[j];
+        }
+        if (with_mass) sum += mass_of_eight(v, to, from, top_wide, cut.scale, tile_before);
+        if (sizeof(E) == 2 && many) {
+#pragma unroll
+          for (int j = 0; j < 8; ++j) {
+            equals += hit[j] ? 1 : 0;
+            equal_high = hit[j] ? fmaxf(equal_high, v[j]) : equal_high;
+            equal_low = hit[j] ? fminf(equal_low, v[j]) : equal_low;
+          }
+        } else if (__ballot(any) != 0) {
+          list.add(s, wave, at, v, hit);
+        }
+        if (++piece == p.pieces_tile || from_piece + kPiece >= p.V) {
+          if constexpr (SAMPLE) {
+            const double before = wave_sum(tile_before);
+            if (lane == 0) s.along[kRange + tile] = before;
+          }
+          if (sizeof(E) == 2 && many) {
+            equals = wave_sum(equals);
+            if (lane == 0) s.equals[tile] = equals;
+            equals = 0;
+          }
+          ++tile;
+          sum_before += tile_before;
+          piece = 0; tile_before = 0.0;
+        }
+      });
+      all_mass = block_sum(sum, s.wave_double);
+      above_mass = block_sum(sum_before, s.wave_double);
+      const int mine = above;
+      block_scan_before(mine, s.wave_count, above);
+      __syncthreads();
+      above_mine = mine;
+      if (sizeof(E) == 2 && many) {
+        block_ends(equal_high, equal_low, equal_high, equal_low);
+        if (equal_high != equal_low) continue;
+        // of the equals, as many as it takes: the tile with the last of them, then its index
+        each_equal = mass_of(equal_high, top_wide, cut.scale);
+        const double some = by_mass ? ceil(((double)cut.top_p * all_mass - above_mass) / each_equal) : (double)(cut.top_k - above);
+        constexpr int kEach = kMostTiles / kThreads;
+        int of[kEach], mine_equal = 0, total;
+#pragma unroll
+        for (int i = 0; i < kEach; ++i) { const int t = threadIdx.x * kEach + i; of[i] = t < p.tiles ? s.equals[t] : 0; mine_equal += of[i]; }
+        int upto = block_scan_before(mine_equal, s.wave_count, total);
+        if (!(some >= 1.0 && some <= (double)total)) continue;  // (or the range is not where the cut is)
+        equal_kept = (int)some;
+#pragma unroll
+        for (int i = 0; i < kEach; ++i) {
+          const int t = threadIdx.x * kEach + i;
+          if (upto < equal_kept && upto + of[i] >= equal_kept) { s.pick = t; s.n_few = upto; }
+          upto += of[i];
+          if (t < p.tiles) s.equals[t] = upto;
+        }
+        __syncthreads();
+        const unsigned begin = (unsigned)s.pick * (unsigned)p.pieces_tile * kPiece;
+        int before = s.n_few;
+        if (wave == 0) {
+          for (int i = 0; i < p.pieces_tile && before < equal_kept; ++i) {  // (uniform; it is within the row)
+            const unsigned at0 = begin + (unsigned)i * kPiece;
+            float v[8];
+            bool hit[8];
+            widen_raw(load_raw(row, at0, lane, (unsigned)p.V), at0, lane, (unsigned)p.V, v);
+#pragma unroll
+            for (int j = 0; j < 8; ++j) hit[j] = v[j] == equal_high;
+            int all, here = before + marked_before(hit, all);
+#pragma unroll
+            for (int j = 0; j < 8; ++j)
+              if (hit[j] && ++here == equal_kept) s.pick_index = begin_of(at0, lane, (unsigned)p.V) + j;
+            before += all;
+          }
+        }
+        __syncthreads();
+        place = {key_of(equal_high), s.pick_index};
+        found = true;
+        continue;
+      }
+      listed = ranged = join_list(s, list.count, lane, wave, n);
+      }
+      if (!listed) continue;
+    }
+    if (turn == 2) {
+      listed = ranged = false;
+      above = 0;
+    }
     place = {0xFFFFFFFFu, (uint32_t)p.V};
     found = true;
+    if constexpr (RANGE) {
+      if (listed && n <= kFew) {
+        look_in_few();
+        continue;
+      }
+    }
     const Listed in = {listed ? &s : nullptr, n};
 #pragma unroll 1
-    for (int turn = 0; turn < 2; ++turn) {  // by count, then by mass
-      if (turn == 0 ? cut.top_k == 0 : !by_mass) continue;
-      Weight weight = {turn == 0, top_wide, cut.scale, 1.0};
-      unsigned long long wanted = (unsigned long long)cut.top_k;
+    for (int by = 0; by < 2; ++by) {  // by count, then by mass
+      if (by == 0 ? cut.top_k == 0 : !by_mass) continue;
+      Weight weight = {by == 0, top_wide, cut.scale, 1.0};
+      unsigned long long wanted = (unsigned long long)(cut.top_k - above);
       float share = 0.0f;
-      if (turn == 1) {
+      if (by == 1) {
         // The unit of the whole numbers: 2^-51 of the largest entry's mass, or more where 62 bits would not hold the row's, which is at most
         // the sum over the threads of their largest one's times their entries.
         const long long entries = (long long)p.tiles_wave * p.pieces_tile * 8;
         const int room = 62 - (ilogb(block_sum(mass_of(high, top_wide, cut.scale) * (double)entries, s.wave_double)) + 1);
         weight.unit = ldexp(1.0, room < 51 ? room : 51);
-        if (listed && need_mass) wanted = (unsigned long long)ceil((double)cut.top_p * all_mass * weight.unit);
-        else share = cut.top_p;
+        if (listed && need_mass) {
+          const double target = ceil(((double)cut.top_p * all_mass - above_mass) * weight.unit);
+          if (ranged && above > 0 && !(target > 0.0)) { found = false; break; }
+          wanted = target > 1.0 ? (unsigned long long)target : 1;
+        } else {
+          share = cut.top_p;
+        }
       }
-      Place by;
-      if (narrow_down(in, row, p, s, part, top, cut.temp, place, weight, share, wanted, by)) place = by;
-      else found = !(listed && need_mass && bound > -INFINITY);  // (the list ends before)
+      Place to;
+      if (narrow_down(in, row, p, s, part, top, cut.temp, place, weight, share, wanted, to)) place = to;
+      else found = !(listed && need_mass && bound > -INFINITY) && !ranged;  // (the list ends before)
     }
-    if (!found) listed = false;
   }
+  if (!listed) ranged = false;
+  if (ranged) place.index = (uint32_t)s.list_index[place.index];
+  bool tiled = ranged || equal_kept > 0;  // the tiles' masses before the range and the list are all it takes
   if (cut.min_p > 0.0f) {  // the last key that it keeps
     uint32_t a = key_of(top), z = kLastKey + 1;
     while (a < z) {
@@ -809,10 +1054,10 @@ template <typename E, bool SAMPLE> __device__ __forceinline__ void cut_row(const
       if (over_least(value_of(mid))) a = mid + 1; else z = mid;
     }
     const uint32_t last = a > key_of(top) ? a - 1 : a;
-    if (last < place.key) place = {last, (uint32_t)p.V};
+    if (last < place.key) { place = {last, (uint32_t)p.V}; tiled = false; }
   }
   const auto kept_at = [&](int e) { return s.list_key[e] < place.key || (s.list_key[e] == place.key && (unsigned)e <= place.index); };
-  if (listed) {
+  if (listed && !ranged) {
     const int each = (n + kThreads - 1) / kThreads, e0 = threadIdx.x * each, e1 = e0 + each < n ? e0 + each : n;
     __syncthreads();
     if constexpr (SAMPLE) {
@@ -891,7 +1136,23 @@ template <typename E, bool SAMPLE> __device__ __forceinline__ void cut_row(const
     // masses of the tiles (an uncut row's are there, by the sample's reference)
     const double by_wide = uncut ? reference_wide : top_wide;
     __syncthreads();
-    if (!uncut) {
+    double *along = s.along + (tiled ? kRange : 0);
+    if (equal_kept > 0 && tiled) {
+      count = wave_sum(above_mine) + (wave == 0 ? equal_kept : 0);
+    } else if (tiled) {  // masses of the range's kept, summed along the indexes
+      const int each = (n + kThreads - 1) / kThreads, e0 = threadIdx.x * each, e1 = e0 + each < n ? e0 + each : n;
+      double sum = 0.0, unused_total;
+      int mine = above_mine;
+#pragma unroll 1
+      for (int e = e0; e < e1; ++e) {
+        if (inside(value_of(s.list_key[e]), (unsigned)s.list_index[e])) { sum += mass_of(value_of(s.list_key[e]), top_wide, cut.scale); ++mine; }
+        s.along[e] = sum;
+      }
+      const double before = block_scan_before(sum, s.wave_double, unused_total);
+#pragma unroll 1
+      for (int e = e0; e < e1; ++e) s.along[e] += before;
+      count = wave_sum(mine);
+    } else if (!uncut) {
       double sum_tile = 0.0;
       piece = 0;
       tile = (long long)wave * p.tiles_wave;
@@ -916,25 +1177,40 @@ template <typename E, bool SAMPLE> __device__ __forceinline__ void cut_row(const
     const int t0 = threadIdx.x * kEach;
     double m[kEach], total, sum = 0.0;
 #pragma unroll
-    for (int i = 0; i < kEach; ++i) { m[i] = t0 + i < p.tiles ? s.along[t0 + i] : 0.0; sum += m[i]; }
+    for (int i = 0; i < kEach; ++i) { m[i] = t0 + i < p.tiles ? along[t0 + i] : 0.0; sum += m[i]; }
     sum = block_scan_before(sum, s.wave_double, total);
 #pragma unroll
-    for (int i = 0; i < kEach; ++i) { sum += m[i]; s.along[t0 + i] = sum; }
+    for (int i = 0; i < kEach; ++i) {
+      sum += m[i];
+      double with = 0.0;
+      if (tiled && equal_kept > 0) {
+        if (t0 + i < p.tiles) with = each_equal * (double)(s.equals[t0 + i] < equal_kept ? s.equals[t0 + i] : equal_kept);
+      } else if (tiled && t0 + i < p.tiles) {  // the range's up to the tile's end
+        const long long end = (long long)(t0 + i + 1) * p.pieces_tile * kPiece;
+        int a = 0, z = n;
+        while (a < z) {
+          const int mid = (a + z) / 2;
+          if (s.list_index[mid] >= end) z = mid; else a = mid + 1;
+        }
+        if (a > 0) with = s.along[a - 1];
+      }
+      along[t0 + i] = sum + with;
+    }
     __syncthreads();
-    total = s.along[p.tiles - 1];
+    total = along[p.tiles - 1];
     for (int i = wave; i < p.S; i += kWaves) {  // a wavefront a token
       const float u = p.u[r * p.u_stride + i];
       const double target = (double)fmaxf(u, 0.0f) * total;
       int a = 0, z = p.tiles;  // the first tile whose sum is over the target
       while (a < z) {
         const int mid = (a + z) / 2;
-        if (s.along[mid] > target) z = mid; else a = mid + 1;
+        if (along[mid] > target) z = mid; else a = mid + 1;
       }
       if (a >= p.tiles) {  // the last with mass
         a = p.tiles - 1;
-        while (a > 0 && s.along[a] == s.along[a - 1]) --a;
+        while (a > 0 && along[a] == along[a - 1]) --a;
       }
-      double before = a > 0 ? s.along[a - 1] : 0.0;
+      double before = a > 0 ? along[a - 1] : 0.0;
       long long found = -1, last_kept = -1;
       const long long begin = (long long)a * p.pieces_tile * kPiece, end0 = begin + (long long)p.pieces_tile * kPiece, end = end0 < p.V ? end0 : p.V;
       for (long long at0 = begin; at0 < end && found < 0; at0 += kPiece) {
@@ -999,16 +1275,19 @@ template <typename E, bool SAMPLE> __device__ __forceinline__ void cut_row(const
   __syncthreads();
 }
 
-template <typename E, bool SAMPLE> __global__ void __launch_bounds__(kThreads, 4) cut_kernel(const CutParams p) {
+template <typename E, bool SAMPLE, bool RANGE> __global__ void __launch_bounds__(kThreads, 4) cut_kernel(const CutParams p) {
   __shared__ Shared s;
-  cut_row<E, SAMPLE>(p, p.row0 + blockIdx.x, s);
+  cut_row<E, SAMPLE, RANGE>(p, p.row0 + blockIdx.x, s);
 }
 template <bool SAMPLE> hipError_t launch_cut(CutParams p, int dtype, hipStream_t st) {
   hipError_t e = hipSuccess;
+  // Whether rows may look for their cut in a range; the kernel that can needs more registers than there are, which costs the others' rows a tenth of their time.
+  const bool by_mass = p.row_top_p != nullptr || p.top_p < 1.0f;
+  const bool range = (by_mass && (p.row_top_k != nullptr || p.top_k == 0)) || p.row_top_k != nullptr || p.top_k > kByCount;
   for (; p.row0 < p.R && e == hipSuccess; p.row0 += kMostRowBlocks) {
     const unsigned blocks = (unsigned)(p.R - p.row0 < kMostRowBlocks ? p.R - p.row0 : kMostRowBlocks);
-    if (dtype == LLC_F32) cut_kernel<float, SAMPLE><<<blocks, kThreads, 0, st>>>(p);
-    else cut_kernel<uint16_t, SAMPLE><<<blocks, kThreads, 0, st>>>(p);
+    if (dtype == LLC_F32) range ? cut_kernel<float, SAMPLE, true><<<blocks, kThreads, 0, st>>>(p) : cut_kernel<float, SAMPLE, false><<<blocks, kThreads, 0, st>>>(p);
+    else range ? cut_kernel<uint16_t, SAMPLE, true><<<blocks, kThreads, 0, st>>>(p) : cut_kernel<uint16_t, SAMPLE, false><<<blocks, kThreads, 0, st>>>(p);
     e = hipGetLastError();
   }
   return e;

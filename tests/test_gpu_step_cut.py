@@ -113,6 +113,25 @@ def test_orders_that_crowd_the_kept_entries(dtype):
         _both(x, u, **settings)
 
 
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("grid", [0.0, 0.25, 2.0])
+def test_cuts_deep_in_a_row(grid, dtype):
+    # thousands of entries kept, with thousands of equals about the cut, in rows whose first entries are like the others or not
+    g = _gen(31)
+    V = 60001
+    x = 2.0 * torch.randn(5, V, generator=g, device=DEV) - 9.0
+    if grid > 0:
+        x = (x / grid).round() * grid
+    x[1, ::3] = -math.inf
+    x[2] = x[2].sort(descending=True).values
+    x[3] = x[3].sort().values
+    x[4, V - 1] = 9.0
+    x = x.to(TYPES[dtype])
+    u = torch.rand(5, 7, generator=g, device=DEV)
+    for settings in (dict(top_p=0.8), dict(top_p=0.97, temp=2.5), dict(top_p=0.99, min_p=0.02), dict(top_p=0.999, temp=0.5), dict(top_k=2500), dict(top_k=30000, temp=1.3), dict(top_k=50000, min_p=1e-5)):
+        _both(x, u, **settings)
+
+
 def test_log_weights_take_no_temperature():
     x = _zipf(4, 3001, 1.5, torch.float32, _gen(5))
     u = torch.rand(4, 2, generator=_gen(6), device=DEV)
