@@ -1251,7 +1251,7 @@ def _layer_into(a, codes, scales, zeros, D, group):
 
 
 def llc_quantize(w: torch.Tensor, *, group: int = 128, zeros: bool = False, scales_dtype: torch.dtype = torch.bfloat16,
-                  out: Optional[dict] = None, flags: int = 0, events=None) -> dict:
+                 out: Optional[dict] = None, flags: int = 0, events=None) -> dict:
     """A layer [N,D] to 4 bits: w[n,d] is near scales[n,g] * (q[n,d] - zeros[n,g]), g = d // group, q in 0..15.
 
     w: float32 or bfloat16; group 32, 64 or 128.  Returns uint8 codes [N, (D + 1) // 2], two columns a byte (even ones in
@@ -1287,8 +1287,8 @@ def llc_quantize(w: torch.Tensor, *, group: int = 128, zeros: bool = False, scal
 
 
 def llc_embed_quantized(codes: torch.Tensor, scales: torch.Tensor, tokens: torch.Tensor, D: int, *, zeros: Optional[torch.Tensor] = None,
-               group: int = 128, scale: float = 1.0, out_dtype: Optional[torch.dtype] = None, out: Optional[torch.Tensor] = None,
-               flags: int = 0, events=None) -> dict:
+                        group: int = 128, scale: float = 1.0, out_dtype: Optional[torch.dtype] = None, out: Optional[torch.Tensor] = None,
+                        flags: int = 0, events=None) -> dict:
     """llc_embed of a table in 4 bits: out[..., :] = scale * w[tokens[...], :], zeros for tokens outside the table.
 
     codes, scales, zeros, group: as llc_quantize returned them, of a table [N,D]; tokens: int32 of any shape; out has the tokens'
@@ -1320,8 +1320,8 @@ def llc_embed_quantized(codes: torch.Tensor, scales: torch.Tensor, tokens: torch
 
 
 def llc_matvec_quantized(x: torch.Tensor, codes: torch.Tensor, scales: torch.Tensor, *, zeros: Optional[torch.Tensor] = None, group: int = 128,
-                out_dtype: Optional[torch.dtype] = None, out: Optional[torch.Tensor] = None, workspace: Optional[torch.Tensor] = None,
-                flags: int = 0, events=None) -> dict:
+                         out_dtype: Optional[torch.dtype] = None, out: Optional[torch.Tensor] = None, workspace: Optional[torch.Tensor] = None,
+                         flags: int = 0, events=None) -> dict:
     """Products with a layer in 4 bits: out[r,n] = sum over d of x[r,d] * w[n,d].
 
     x: [R,D] float32 or bfloat16, last dimension contiguous; codes, scales, zeros, group: as llc_quantize returned them, of a
