@@ -48,9 +48,9 @@ template <int G, typename S> struct Slab {
 };
 // The same with its scales and zeros as they lie in memory, until they are needed.
 template <int G, typename S> struct RawSlab {
-  static constexpr int kGroups = 128 / G;
+  static constexpr int kGroups = 128 / G, kScaleWords = (kGroups * sizeof(S) + 3) / 4;
   uint32_t words[4];
-  S scale[kGroups];
+  uint32_t scale[kScaleWords];
   uint32_t zero;
 };
 // Four slabs that follow each other, their scales and zeros as they lie in memory.
@@ -68,55 +68,6 @@ template <int G> __device__ __forceinline__ int column_of(int step, int quarter)
   return 32 * step + 8 * quarter;
 }
 
-template <bool Z, int G, typename S>
-__device__ __forceinline__ void load_scales(RawSlab<G, S> &s, const MatvecParams &p, const S *scales, const uint8_t *zeros, int slab) {
-  s.zero = 0;
-#pragma unroll
-  for (int g = 0; g < 128 / G; ++g) {
-    int of = slab * (128 / G) + g;
-    of = of < p.groups ? of : p.groups - 1;  // (columns behind the row's end: x is 0 there)
-    s.scale[g] = scales[of];
-    if constexpr (Z) s.zero |= (uint32_t)zeros[of] << (8 * g);
-  }
-}
-template <bool Z, int G, typename S> __device__ __forceinline__ Slab<G, S> slab_of(const RawSlab<G, S> &r) {
-  Slab<G, S> s;
-#pragma unroll
-  for (int j = 0; j < 4; ++j) s.words[j] = r.words[j];
-#pragma unroll
-  for (int g = 0; g < 128 / G; ++g) {
-    s.scale[g] = widen(r.scale[g]);
-    s.shift[g] = Z ? -16.0f - (float)((r.zero >> (8 * g)) & 255u) : -24.0f;
-  }
-  return s;
-}
-template <bool Z, int G, typename S>
-__device__ __forceinline__ RawSlab<G, S> load_slab(const MatvecParams &p, const uint8_t *codes, const S *scales, const uint8_t *zeros, int slab, int quarter) {
-  RawSlab<G, S> s;
-  const uint8_t *from = codes + (long long)slab * 64;
-  if constexpr (G == 128) {
-    const word4_byte w = *reinterpret_cast<const word4_byte *>(from + 16 * quarter);
-    s.words[0] = w.x; s.words[1] = w.y; s.words[2] = w.z; s.words[3] = w.w;
-  } else if constexpr (G == 64) {
-    const word2_byte a = *reinterpret_cast<const word2_byte *>(from + 8 * quarter);
-    const word2_byte b = *reinterpret_cast<const word2_byte *>(from + 32 + 8 * quarter);
-    s.words[0] = a.x; s.words[1] = a.y; s.words[2] = b.x; s.words[3] = b.y;
-  } else {
-#pragma unroll
-    for (int i = 0; i < 4; ++i) s.words[i] = *reinterpret_cast<const word1_byte *>(from + 16 * i + 4 * quarter);
-  }
-  load_scales<Z>(s, p, scales, zeros, slab);
-  return s;
-}
-// The last slab of a row that is not a whole one.
-template <bool Z, int G, typename S>
-__device__ __forceinline__ RawSlab<G, S> load_last_slab(const MatvecParams &p, const uint8_t *codes, const S *scales, const uint8_t *zeros, int slab, int quarter) {
-  RawSlab<G, S> s;
-#pragma unroll
-  for (int i = 0; i < 4; ++i) s.words[i] = load_codes(codes, (long long)slab * 128 + column_of<G>(i, quarter), p.D);
-  load_scales<Z>(s, p, scales, zeros, slab);
-  return s;
-}
 // N words from anywhere.
 template <int N> __device__ __forceinline__ void load_words(uint32_t (&w)[N], const void *from) {
   const uint8_t *at = reinterpret_cast<const uint8_t *>(from);
@@ -132,6 +83,74 @@ template <int N> __device__ __forceinline__ void load_words(uint32_t (&w)[N], co
       w[i] = v.x; w[i + 1] = v.y; w[i + 2] = v.z; w[i + 3] = v.w;
     }
   }
+}
+template <typename S, int WORDS> __device__ __forceinline__ float scale_of(const uint32_t (&words)[WORDS], int at) {
+  if constexpr (sizeof(S) == 4) return __uint_as_float(words[at]);
+  return __uint_as_float(at % 2 == 0 ? words[at / 2] << 16 : words[at / 2] & 0xFFFF0000u);
+}
+template <bool Z, int G, typename S> __device__ __forceinline__ Slab<G, S> slab_of(const RawSlab<G, S> &r) {
+  Slab<G, S> s;
+#pragma unroll
+  for (int j = 0; j < 4; ++j) s.words[j] = r.words[j];
+#pragma unroll
+  for (int g = 0; g < 128 / G; ++g) {
+    s.scale[g] = scale_of<S>(r.scale, g);
+    s.shift[g] = Z ? -16.0f - (float)((r.zero >> (8 * g)) & 255u) : -24.0f;
+  }
+  return s;
+}
+template <bool Z, int G, typename S>
+__device__ __forceinline__ RawSlab<G, S> load_slab(const uint8_t *codes, const S *scales, const uint8_t *zeros, int slab, int quarter) {
+  constexpr int kGroups = 128 / G;
+  RawSlab<G, S> s;
+  const uint8_t *from = codes + (long long)slab * 64;
+  if constexpr (G == 128) {
+    load_words(s.words, from + 16 * quarter);
+  } else if constexpr (G == 64) {
+    const word2_byte a = *reinterpret_cast<const word2_byte *>(from + 8 * quarter);
+    const word2_byte b = *reinterpret_cast<const word2_byte *>(from + 32 + 8 * quarter);
+    s.words[0] = a.x; s.words[1] = a.y; s.words[2] = b.x; s.words[3] = b.y;
+  } else {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) s.words[i] = *reinterpret_cast<const word1_byte *>(from + 16 * i + 4 * quarter);
+  }
+  const S *scale = scales + (long long)slab * kGroups;
+  if constexpr (kGroups * sizeof(S) == 2) s.scale[0] = *scale;
+  else load_words(s.scale, scale);
+  if constexpr (Z) {
+    const uint8_t *zero = zeros + (long long)slab * kGroups;
+    if constexpr (kGroups == 4) s.zero = *reinterpret_cast<const word1_byte *>(zero);
+    else if constexpr (kGroups == 2) s.zero = *reinterpret_cast<const half_byte *>(zero);
+    else s.zero = *zero;
+  }
+  return s;
+}
+// The last slab of a row that is not a whole one: nothing behind the row's end is read, and what is multiplied there is no matter, since x is 0.
+template <bool Z, int G, typename S>
+__device__ __forceinline__ RawSlab<G, S> load_last_slab(const MatvecParams &p, const uint8_t *codes, const S *scales, const uint8_t *zeros, int slab, int quarter) {
+  RawSlab<G, S> s;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const long long at = (long long)slab * 64 + column_of<G>(i, quarter) / 2, last = (p.D + 1) / 2 - 4;
+    if (last < 0) {  // (uniform: a row of up to six entries)
+      s.words[i] = load_codes(codes, 2 * at, p.D);
+    } else {  // (under no condition, so that the four are under way together)
+      const uint32_t word = *reinterpret_cast<const word1_byte *>(codes + (at < last ? at : last));
+      s.words[i] = at <= last ? word : at - last < 4 ? word >> (8 * (int)(at - last)) : 0;
+    }
+  }
+#pragma unroll
+  for (int i = 0; i < RawSlab<G, S>::kScaleWords; ++i) s.scale[i] = 0;
+  s.zero = 0;
+#pragma unroll
+  for (int g = 0; g < 128 / G; ++g) {
+    int of = slab * (128 / G) + g;
+    of = of < p.groups ? of : p.groups - 1;  // (columns behind the row's end: x is 0 there)
+    if constexpr (sizeof(S) == 4) s.scale[g] = __float_as_uint(scales[of]);
+    else s.scale[g / 2] |= (uint32_t)scales[of] << (16 * (g % 2));
+    if constexpr (Z) s.zero |= (uint32_t)zeros[of] << (8 * g);
+  }
+  return s;
 }
 template <bool Z, int G, typename S> __device__ __forceinline__ void load_batch(Batch<G, S> &b, const uint8_t *codes, const S *scales, const uint8_t *zeros, int slab, int quarter) {
 #pragma unroll
@@ -157,8 +176,7 @@ template <bool Z, int G, typename S> __device__ __forceinline__ Slab<G, S> slab_
 #pragma unroll
   for (int g = 0; g < 128 / G; ++g) {
     const int at = i * (128 / G) + g;
-    if constexpr (sizeof(S) == 4) s.scale[g] = __uint_as_float(b.scale[at]);
-    else s.scale[g] = __uint_as_float(at % 2 == 0 ? b.scale[at / 2] << 16 : b.scale[at / 2] & 0xFFFF0000u);
+    s.scale[g] = scale_of<S>(b.scale, at);
     s.shift[g] = Z ? -16.0f - (float)((b.zero[at / 4] >> (8 * (at % 4))) & 255u) : -24.0f;
   }
   return s;
@@ -212,6 +230,65 @@ __device__ __forceinline__ void add_slab(f32x4 (&total)[WIDE][TILES], const Slab
           for (int j = 0; j < 4; ++j) total[w][t][j] = fmaf(s[w].scale[g], PARTS > 1 ? sum[w][t][j] + low[w][t][j] : sum[w][t][j], total[w][t][j]);
     }
     if (TILES * PARTS > 2 || step == 3) __builtin_amdgcn_sched_barrier(0);  // (what later steps read of x, read ahead, would take more registers than there are)
+  }
+}
+
+// The same with places of x that are known when this is compiled: what the next products take of x is asked for before these.
+template <int TILES, int PARTS, int G, typename S, int WIDE>
+__device__ __forceinline__ void add_streamed_slab(f32x4 (&total)[WIDE][TILES], const Slab<G, S> (&s)[WIDE], const uint4 *s_x, const float *s_sum, int lane) {
+  constexpr int kOf = G / 32 * PARTS, kAll = 4 * PARTS;  // products of a group, of the slab
+  const uint4 *at = s_x + (lane >> 4) * 16 * TILES + (lane & 15);
+  const float *at_sum = s_sum + 4 * (lane >> 4);
+  f32x4 sum[WIDE][TILES], low[WIDE][TILES], sx[TILES];
+  bf16x8 a[2][TILES], codes[WIDE];
+  const auto ask = [&](int i) __attribute__((always_inline)) {
+#pragma unroll
+    for (int t = 0; t < TILES; ++t) a[i & 1][t] = __builtin_bit_cast(bf16x8, at[i * 64 * TILES + 16 * t]);
+  };
+  const auto ask_sums = [&](int g) __attribute__((always_inline)) {
+#pragma unroll
+    for (int t = 0; t < TILES; ++t) sx[t] = *reinterpret_cast<const f32x4 *>(at_sum + g * (TILES * 16) + 16 * t);
+  };
+  ask_sums(0);
+  ask(0);
+#pragma unroll
+  for (int i = 0; i < kAll; ++i) {
+    const int g = i / kOf;
+    if (i % kOf == 0) {
+#pragma unroll
+      for (int t = 0; t < TILES; ++t)
+#pragma unroll
+        for (int w = 0; w < WIDE; ++w) {
+#pragma unroll
+          for (int j = 0; j < 4; ++j) sum[w][t][j] = s[w].shift[g] * sx[t][j];
+          low[w][t] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+        }
+    }
+    if (i + 1 < kAll) {
+      ask(i + 1);
+      if ((i + 1) % kOf == 0) ask_sums(g + 1);
+    }
+    __builtin_amdgcn_sched_barrier(0);
+    if (i % PARTS == 0) {
+#pragma unroll
+      for (int w = 0; w < WIDE; ++w) codes[w] = widen_codes(s[w].words[i / PARTS]);
+    }
+#pragma unroll
+    for (int t = 0; t < TILES; ++t)
+#pragma unroll
+      for (int w = 0; w < WIDE; ++w) {
+        if (i % PARTS == 0) sum[w][t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a[i & 1][t], codes[w], sum[w][t], 0, 0, 0);
+        else low[w][t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a[i & 1][t], codes[w], low[w][t], 0, 0, 0);
+      }
+    if (i % kOf == kOf - 1) {
+#pragma unroll
+      for (int w = 0; w < WIDE; ++w)
+#pragma unroll
+        for (int t = 0; t < TILES; ++t)
+#pragma unroll
+          for (int j = 0; j < 4; ++j) total[w][t][j] = fmaf(s[w].scale[g], PARTS > 1 ? sum[w][t][j] + low[w][t][j] : sum[w][t][j], total[w][t][j]);
+    }
+    __builtin_amdgcn_sched_barrier(0);
   }
 }
 
@@ -391,7 +468,7 @@ template <int PARTS, int G, typename S, bool Z, typename X> __global__ void __la
     if (i < batches) add(batch[0], i);
 #pragma unroll 1
     for (int slab = begin + batches * kSlabs; slab < end + (last_too ? 1 : 0); ++slab) {  // fewer than four, and the row's end
-      const Slab<G, S> s[WIDE] = {slab_of<Z>(slab < whole ? load_slab<Z, G, S>(p, row.codes, row.scales, row.zeros, slab, quarter)
+      const Slab<G, S> s[WIDE] = {slab_of<Z>(slab < whole ? load_slab<Z, G, S>(row.codes, row.scales, row.zeros, slab, quarter)
                                                        : load_last_slab<Z, G, S>(p, row.codes, row.scales, row.zeros, slab, quarter))};
       add_slab<TILES, PARTS, G, S, WIDE>(total, s, s_x + slab * 16 * PARTS * pitch, s_sum + slab * (128 / G) * 16, at_x, pitch, quarter);
     }
@@ -415,7 +492,8 @@ template <int PARTS, int G, typename X> __global__ void __launch_bounds__(256) m
   store_x<PARTS, G, X>(v, (unsigned)(r - r0), piece & 15, pitch, p.tiles, reinterpret_cast<uint4 *>(image), reinterpret_cast<float *>(image + 256 * PARTS * pitch));
 }
 
-// x by parts of a few slabs, in two places of LDS in turn: the next part, and the codes that go with it, are asked for before this one is multiplied.  A wavefront has two
+// x by parts of a few slabs, in two places of LDS in turn: the next part of x, then the codes of the one after it, are asked for before this one is multiplied (in this
+// order: loads return in the order they were asked for in).  A wavefront has two
 // tiles of columns, so that what it reads of x serves both; every workgroup takes its tiles through all of x once.  Wavefronts that share tiles take a slab of
 // a part each.  Every load is made under no condition, those behind an end from the last place there is: how many are under way is known then, and each is waited for by
 // itself.  (With a condition around what a part does not need, 64 rows of 4096 with 128 256 columns took 194 us.)
@@ -431,9 +509,6 @@ __global__ void __launch_bounds__(kMatvecThreads, 2) matvec_streamed_kernel(cons
   const int rows = (int)(p.R - r0 < kMatvecRows ? p.R - r0 : kMatvecRows);
   const u32x4 *image = reinterpret_cast<const u32x4 *>(p.image + blockIdx.y * p.image_stride);
   const int whole = (int)(p.D / 128), chunks = (p.slabs + kSlabs - 1) / kSlabs, image_units = p.slabs * (kSize / 16);
-  int at_x[TILES];
-#pragma unroll
-  for (int t = 0; t < TILES; ++t) at_x[t] = quarter * 16 * TILES + 16 * t + column;
   long long n0[WIDE];
   Row<S> row[WIDE];
   f32x4 total[WIDE][TILES];
@@ -449,47 +524,57 @@ __global__ void __launch_bounds__(kMatvecThreads, 2) matvec_streamed_kernel(cons
   }
   const int last_whole = whole > 0 ? whole - 1 : 0;
   u32x4 next[kEach];
-  RawSlab<G, S> coming[kTurns][WIDE], here[kTurns][WIDE];
-  const auto ask = [&](int chunk) __attribute__((always_inline)) {
+  RawSlab<G, S> coming[2][kTurns][WIDE];
+  const auto ask_x = [&](int chunk) __attribute__((always_inline)) {
 #pragma unroll
     for (int i = 0; i < kEach; ++i) {
       const int in = i * kMatvecThreads + (int)threadIdx.x, at = chunk * kUnits + (in < kUnits ? in : kUnits - 1);
       next[i] = image[at < image_units ? at : image_units - 1];
     }
+  };
+  const auto ask_codes = [&](RawSlab<G, S> (&to)[kTurns][WIDE], int chunk) __attribute__((always_inline)) {
 #pragma unroll
     for (int i = 0; i < kTurns; ++i) {
       const int slab = chunk * kSlabs + i * kShare + part_of;
 #pragma unroll
-      for (int w = 0; w < WIDE; ++w) coming[i][w] = load_slab<Z, G, S>(p, row[w].codes, row[w].scales, row[w].zeros, slab < last_whole ? slab : last_whole, quarter);
+      for (int w = 0; w < WIDE; ++w) to[i][w] = load_slab<Z, G, S>(row[w].codes, row[w].scales, row[w].zeros, slab < last_whole ? slab : last_whole, quarter);
     }
   };
-  ask(0);
-#pragma unroll 1
-  for (int chunk = 0; chunk < chunks; ++chunk) {
-    char *at_place = s_dyn + ((chunk & 1) != 0 ? kPlace : 0);  // (free: all have been through the last barrier after they were done with it)
+  const auto step = [&](char *at_place, RawSlab<G, S> (&codes)[kTurns][WIDE], int chunk) __attribute__((always_inline)) {
+    // (the place is free: all have been through the last barrier after they were done with it)
 #pragma unroll
     for (int i = 0; i < kEach; ++i) {
       const int in = i * kMatvecThreads + (int)threadIdx.x;
       reinterpret_cast<u32x4 *>(at_place)[in < kUnits ? in : kUnits - 1] = next[i];  // (the last one by several lanes, the same)
     }
+    Slab<G, S> now[kTurns][WIDE];
 #pragma unroll
     for (int i = 0; i < kTurns; ++i)
 #pragma unroll
-      for (int w = 0; w < WIDE; ++w) here[i][w] = coming[i][w];
+      for (int w = 0; w < WIDE; ++w) now[i][w] = slab_of<Z>(codes[i][w]);
     __builtin_amdgcn_sched_barrier(0);
-    ask(chunk + 1 < chunks ? chunk + 1 : chunk);
+    ask_x(chunk + 1 < chunks ? chunk + 1 : chunk);
+    __builtin_amdgcn_sched_barrier(0);
+    ask_codes(codes, chunk + 2 < chunks ? chunk + 2 : chunk);
     __syncthreads();
 #pragma unroll
     for (int i = 0; i < kTurns; ++i) {
       const int in = i * kShare + part_of, slab = chunk * kSlabs + in;
       if (slab < whole) {  // (uniform)
-        Slab<G, S> now[WIDE];
-#pragma unroll
-        for (int w = 0; w < WIDE; ++w) now[w] = slab_of<Z>(here[i][w]);
         const char *at = at_place + in * kSize;
-        add_slab<TILES, PARTS, G, S, WIDE>(total, now, reinterpret_cast<const uint4 *>(at), reinterpret_cast<const float *>(at + 256 * PARTS * 16 * TILES), at_x, 16 * TILES, quarter);
+        add_streamed_slab<TILES, PARTS, G, S, WIDE>(total, now[i], reinterpret_cast<const uint4 *>(at), reinterpret_cast<const float *>(at + 256 * PARTS * 16 * TILES), lane);
       }
     }
+  };
+  ask_codes(coming[0], 0);
+  ask_x(0);
+  __builtin_amdgcn_sched_barrier(0);
+  ask_codes(coming[1], chunks > 1 ? 1 : 0);
+#pragma unroll 1
+  for (int chunk = 0; chunk < chunks; chunk += 2) {
+    step(s_dyn, coming[0], chunk);
+    if (chunk + 1 >= chunks) break;
+    step(s_dyn + kPlace, coming[1], chunk + 1);
   }
   if (whole < p.slabs && (whole % kSlabs) % kShare == part_of) {  // the row's end, whose part of x is still there
     const char *at = s_dyn + (((chunks - 1) & 1) != 0 ? kPlace : 0) + (whole % kSlabs) * kSize;
@@ -499,7 +584,7 @@ __global__ void __launch_bounds__(kMatvecThreads, 2) matvec_streamed_kernel(cons
       const Row<S> r = row_of<S>(p, (n0[w] < 0 ? 0 : n0[w]) + column);
       now[w] = slab_of<Z>(load_last_slab<Z, G, S>(p, r.codes, r.scales, r.zeros, whole, quarter));
     }
-    add_slab<TILES, PARTS, G, S, WIDE>(total, now, reinterpret_cast<const uint4 *>(at), reinterpret_cast<const float *>(at + 256 * PARTS * 16 * TILES), at_x, 16 * TILES, quarter);
+    add_streamed_slab<TILES, PARTS, G, S, WIDE>(total, now, reinterpret_cast<const uint4 *>(at), reinterpret_cast<const float *>(at + 256 * PARTS * 16 * TILES), lane);
   }
   finish_tiles<TILES, WIDE>(p, total, reinterpret_cast<float *>(s_dyn + 2 * kPlace), kShare, part_of, wave, lane, r0, rows, n0);
 }

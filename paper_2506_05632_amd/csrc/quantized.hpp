@@ -9,6 +9,7 @@ inline bool known_group(int group) { return group == 32 || group == 64 || group 
 inline long long groups_of(long long D, int group) { return (D + group - 1) / group; }
 
 // Loads of bytes wherever they start.
+typedef uint16_t half_byte __attribute__((aligned(1)));
 typedef uint32_t word1_byte __attribute__((aligned(1)));
 typedef uint32_t word2_byte __attribute__((ext_vector_type(2), aligned(1)));
 typedef uint32_t word4_byte __attribute__((ext_vector_type(4), aligned(1)));
