@@ -61,11 +61,24 @@ template <int G, typename S> struct Batch {
   uint32_t zero[kZeroWords];
 };
 
-// Column of a slab where the quarter's word of a step starts.
-template <int G> __device__ __forceinline__ int column_of(int step, int quarter) {
-  if constexpr (G == 128) return 32 * quarter + 8 * step;
-  if constexpr (G == 64) return 64 * (step >> 1) + 16 * quarter + 8 * (step & 1);
-  return 32 * step + 8 * quarter;
+// A quarter has 16 bytes of a row, one after the other.  Groups of 128 take them as they lie; with smaller groups a step's words are those of one quarter's 16 bytes, so that the step
+// is within a group: four words of four quarters, turned.  (A load for each word instead, 128 256 x 4096 in groups of 32, 8 rows: 155 us.)
+template <int G> __device__ __forceinline__ void turn_words(uint32_t (&w)[4]) {
+  if constexpr (G < 128) {
+    // (what the upper half of one has goes where the lower half of the other is, and the other way round; then by rows of 16 lanes)
+    const auto halves = [](uint32_t &a, uint32_t &b) {
+      const auto r = __builtin_amdgcn_permlane32_swap(a, b, false, false);
+      a = r[0]; b = r[1];
+    };
+    const auto rows = [](uint32_t &a, uint32_t &b) {
+      const auto r = __builtin_amdgcn_permlane16_swap(a, b, false, false);
+      a = r[0]; b = r[1];
+    };
+    halves(w[0], w[2]);
+    halves(w[1], w[3]);
+    rows(w[0], w[1]);
+    rows(w[2], w[3]);
+  }
 }
 
 // N words from anywhere.
@@ -92,6 +105,7 @@ template <bool Z, int G, typename S> __device__ __forceinline__ Slab<G, S> slab_
   Slab<G, S> s;
 #pragma unroll
   for (int j = 0; j < 4; ++j) s.words[j] = r.words[j];
+  turn_words<G>(s.words);
 #pragma unroll
   for (int g = 0; g < 128 / G; ++g) {
     s.scale[g] = scale_of<S>(r.scale, g);
@@ -103,17 +117,7 @@ template <bool Z, int G, typename S>
 __device__ __forceinline__ RawSlab<G, S> load_slab(const uint8_t *codes, const S *scales, const uint8_t *zeros, int slab, int quarter) {
   constexpr int kGroups = 128 / G;
   RawSlab<G, S> s;
-  const uint8_t *from = codes + (long long)slab * 64;
-  if constexpr (G == 128) {
-    load_words(s.words, from + 16 * quarter);
-  } else if constexpr (G == 64) {
-    const word2_byte a = *reinterpret_cast<const word2_byte *>(from + 8 * quarter);
-    const word2_byte b = *reinterpret_cast<const word2_byte *>(from + 32 + 8 * quarter);
-    s.words[0] = a.x; s.words[1] = a.y; s.words[2] = b.x; s.words[3] = b.y;
-  } else {
-#pragma unroll
-    for (int i = 0; i < 4; ++i) s.words[i] = *reinterpret_cast<const word1_byte *>(from + 16 * i + 4 * quarter);
-  }
+  load_words(s.words, codes + (long long)slab * 64 + 16 * quarter);
   const S *scale = scales + (long long)slab * kGroups;
   if constexpr (kGroups * sizeof(S) == 2) s.scale[0] = *scale;
   else load_words(s.scale, scale);
@@ -131,7 +135,7 @@ __device__ __forceinline__ RawSlab<G, S> load_last_slab(const MatvecParams &p, c
   RawSlab<G, S> s;
 #pragma unroll
   for (int i = 0; i < 4; ++i) {
-    const long long at = (long long)slab * 64 + column_of<G>(i, quarter) / 2, last = (p.D + 1) / 2 - 4;
+    const long long at = (long long)slab * 64 + 16 * quarter + 4 * i, last = (p.D + 1) / 2 - 4;
     if (last < 0) {  // (uniform: a row of up to six entries)
       s.words[i] = load_codes(codes, 2 * at, p.D);
     } else {  // (under no condition, so that the four are under way together)
@@ -154,18 +158,7 @@ __device__ __forceinline__ RawSlab<G, S> load_last_slab(const MatvecParams &p, c
 }
 template <bool Z, int G, typename S> __device__ __forceinline__ void load_batch(Batch<G, S> &b, const uint8_t *codes, const S *scales, const uint8_t *zeros, int slab, int quarter) {
 #pragma unroll
-  for (int i = 0; i < Batch<G, S>::kSlabs; ++i) {
-    const uint8_t *from = codes + (long long)slab * 64 + i * 64;
-    if constexpr (G == 128) {
-      load_words(b.words[i], from + 16 * quarter);
-    } else if constexpr (G == 64) {
-      const word2_byte l = *reinterpret_cast<const word2_byte *>(from + 8 * quarter), h = *reinterpret_cast<const word2_byte *>(from + 32 + 8 * quarter);
-      b.words[i][0] = l.x; b.words[i][1] = l.y; b.words[i][2] = h.x; b.words[i][3] = h.y;
-    } else {
-#pragma unroll
-      for (int j = 0; j < 4; ++j) b.words[i][j] = *reinterpret_cast<const word1_byte *>(from + 16 * j + 4 * quarter);
-    }
-  }
+  for (int i = 0; i < Batch<G, S>::kSlabs; ++i) load_words(b.words[i], codes + (long long)(slab + i) * 64 + 16 * quarter);
   load_words(b.scale, scales + (long long)slab * (128 / G));
   if constexpr (Z) load_words(b.zero, zeros + (long long)slab * (128 / G));
 }
@@ -173,6 +166,7 @@ template <bool Z, int G, typename S> __device__ __forceinline__ Slab<G, S> slab_
   Slab<G, S> s;
 #pragma unroll
   for (int j = 0; j < 4; ++j) s.words[j] = b.words[i][j];
+  turn_words<G>(s.words);
 #pragma unroll
   for (int g = 0; g < 128 / G; ++g) {
     const int at = i * (128 / G) + g;
@@ -334,8 +328,7 @@ __device__ __forceinline__ void store_x(const Piece<X> &from, unsigned r, unsign
   float sum = ((v[0] + v[1]) + (v[2] + v[3])) + ((v[4] + v[5]) + (v[6] + v[7]));
   sum = sum_lanes<G / 8>(sum);
   const unsigned slab = piece >> 4, q = piece & 15;
-  const unsigned step = G == 128 ? q & 3 : G == 64 ? (q >> 3) * 2 + (q & 1) : q >> 2;
-  const unsigned quarter = G == 128 ? q >> 2 : G == 64 ? (q >> 1) & 3 : q & 3;
+  const unsigned step = G == 128 ? q & 3 : q >> 2, quarter = G == 128 ? q >> 2 : q & 3;
   if ((q & (G / 8 - 1)) == 0) s_sum[(slab * (128 / G) + q / (G / 8)) * (tiles * 16) + r] = sum;
   uint4 *to = s_x + ((slab * 4 + step) * PARTS * 4 + quarter) * pitch + r;
 #pragma unroll
