@@ -626,8 +626,8 @@ typedef struct llc_embed_quantized_args {
 
 /* Arguments of llc_matvec_quantized: out[r,n] = sum over d of x[r,d] w[n,d], w a layer in 4 bits.  The products x (q - zero) are summed
  * over a group in fp32 (x of 32 bits as three parts of 8 bits, which hold all of it), those sums are multiplied by their scales and summed in fp32 and the
- * result is rounded to the output's type.  A row of x with an entry that is not finite, or over 2^120 in size, gives outputs that need not be what
- * the formula gives in that row; other rows are not touched by it.  Made for few rows: they are taken 64 at a time, and each such pass reads the layer. */
+ * result is rounded to the output's type.  A row of x with an entry that is not finite, or over 2^115 in size, gives outputs that need not be what
+ * the formula gives in that row (other rows are not touched by it), and parts of x under 2^-126 may count as 0.  Made for few rows: they are taken 64 at a time, and each such pass reads the layer. */
 typedef struct llc_matvec_quantized_args {
   int64_t R, N, D;          /* R in 0..2^17, N in 1..2^31 - 5, D in 1..2^27; R times D at most 2^34, and,
                                of more than 16 rows, R / 64 times N / 16, each rounded up, at most 2^25 */

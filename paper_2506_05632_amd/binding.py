@@ -5,6 +5,7 @@ memory and the current stream.  There is no CPU fallback: if the library is
 missing, `load()` raises.
 """
 import ctypes
+import functools
 import importlib.util
 import os
 import struct
@@ -1154,6 +1155,12 @@ def _cut_into(a, name, logits, kind, temp, top_k, top_p, min_p):
     return R, V, dev
 
 
+@functools.lru_cache(maxsize=256)
+def _matvec_bytes(R, N, D, group, dtype):
+    # (sizes alone decide; a serving step has the same few again and again)
+    return load().llc_matvec_quantized_workspace_size(R, N, D, group, dtype)
+
+
 def llc_matvec_quantized_workspace_size(R: int, N: int, D: int, group: int, dtype: torch.dtype) -> int:
     return load().llc_matvec_quantized_workspace_size(R, N, D, group, _TYPES[dtype])
 
@@ -1230,24 +1237,32 @@ def llc_truncate(logits: torch.Tensor, *, temp=1.0, top_k=0, top_p=1.0, min_p=0.
 
 
 def _layer_into(a, codes, scales, zeros, D, group):
-    """The checks of a layer in 4 bits, and its arguments; its rows."""
-    if not codes.is_cuda:
+    """The checks of a layer in 4 bits, and its arguments; its rows and its device's index."""
+    # (sizes and strides are asked for once: each question takes a tenth of a microsecond, of a call's eight)
+    at = codes.get_device()
+    if at < 0:
         raise ValueError("layers in 4 bits are device tensors (there is no CPU path)")
-    if codes.dtype != torch.uint8 or codes.dim() != 2 or codes.shape[1] != (D + 1) // 2 or (codes.stride(1) != 1 and codes.shape[1] > 1):
+    size, stride = codes.shape, codes.stride()
+    if codes.dtype != torch.uint8 or len(size) != 2 or size[1] != (D + 1) // 2 or (stride[1] != 1 and size[1] > 1):
         raise ValueError("codes must be [N, (D + 1) // 2] uint8, last dimension contiguous")
     if group not in (32, 64, 128):
         raise ValueError("group must be 32, 64 or 128")
-    N, groups = codes.shape[0], -(-D // group)
-    if scales.device != codes.device or scales.dtype not in _TYPES or tuple(scales.shape) != (N, groups) or (scales.stride(1) != 1 and groups > 1):
+    N, groups = size[0], -(-D // group)
+    scales_dtype, scales_stride = _TYPES.get(scales.dtype), scales.stride()
+    if scales.get_device() != at or scales_dtype is None or scales.shape != (N, groups) or (scales_stride[1] != 1 and groups > 1):
         raise ValueError("scales must be [N, D / group rounded up], float32 or bfloat16, on the codes' device, last dimension contiguous")
-    a.group, a.scales_dtype = group, _TYPES[scales.dtype]
-    a.codes, a.codes_stride_n = codes.data_ptr(), _row_stride(codes)
-    a.scales, a.scales_stride_n = scales.data_ptr(), _row_stride(scales)
+    a.group, a.scales_dtype = group, scales_dtype
+    a.codes, a.scales = codes.data_ptr(), scales.data_ptr()
+    # (the stride of a single row, or of none, says nothing)
+    if N > 1:
+        a.codes_stride_n, a.scales_stride_n = stride[0], scales_stride[0]
+    else:
+        a.codes_stride_n, a.scales_stride_n = max(stride[0], size[1]), max(scales_stride[0], groups)
     if zeros is not None:
-        if zeros.device != codes.device or zeros.dtype != torch.uint8 or zeros.shape != scales.shape or (zeros.stride(1) != 1 and groups > 1):
+        if zeros.get_device() != at or zeros.dtype != torch.uint8 or zeros.shape != scales.shape or (zeros.stride(1) != 1 and groups > 1):
             raise ValueError("zeros must be uint8 of the scales' shape, on the codes' device, last dimension contiguous")
         a.zeros, a.zeros_stride_n = zeros.data_ptr(), _row_stride(zeros)
-    return N
+    return N, at
 
 
 def llc_quantize(w: torch.Tensor, *, group: int = 128, zeros: bool = False, scales_dtype: torch.dtype = torch.bfloat16,
@@ -1296,26 +1311,35 @@ def llc_embed_quantized(codes: torch.Tensor, scales: torch.Tensor, tokens: torch
     """
     lib = load()
     a = EmbedQuantizedArgs()
-    N = _layer_into(a, codes, scales, zeros, D, group)
-    if tokens.device != codes.device or tokens.dtype != torch.int32:
+    N, at = _layer_into(a, codes, scales, zeros, D, group)
+    if tokens.get_device() != at or tokens.dtype != torch.int32:
         raise ValueError("tokens must be int32 on the codes' device")
-    tokens, shape = _flat(tokens), tokens.shape
+    shape, device = tokens.shape, codes.device
+    T = shape[0] if len(shape) == 1 else tokens.numel()
     if out is None:
-        specs = {"out": (out_dtype or scales.dtype, *shape, D) if len(shape) < 4 else (out_dtype or scales.dtype, tokens.shape[0], D)}
-        out = _new(codes.device, specs)["out"].view(*shape, D)
-    bad = out.device != codes.device or out.dtype not in _TYPES or out_dtype not in (None, out.dtype) or tuple(out.shape) != (*shape, D)
-    rows = None if bad else out if out.dim() == 2 else _as_rows(out, tokens.shape[0], D)
-    if rows is None or (rows.stride(1) != 1 and D > 1):
+        out = _new(device, {"out": (out_dtype or scales.dtype, T, D)})["out"]
+        to, out_stride = _TYPES.get(out.dtype), D
+        if len(shape) != 1:
+            out = out.view(*shape, D)
+    else:
+        to = _TYPES.get(out.dtype)
+        bad = out.get_device() != at or out_dtype not in (None, out.dtype) or tuple(out.shape) != (*shape, D)
+        rows = None if bad else out if out.dim() == 2 else _as_rows(out, T, D)
+        if rows is None or (rows.stride(1) != 1 and D > 1):
+            to = None
+        out_stride = _row_stride(rows) if to is not None else 0
+    if to is None:
         raise ValueError("out must have the tokens' shape and D, float32 or bfloat16, rows contiguous and a stride apart")
-    a.T, a.N, a.D = tokens.shape[0], N, D
-    a.out_dtype = _TYPES[out.dtype]
+    tokens = _flat(tokens)
+    a.T, a.N, a.D = T, N, D
+    a.out_dtype = to
     a.tokens, a.tok_stride, a.scale = tokens.data_ptr(), tokens.stride(0), scale
-    a.out, a.out_stride_t = out.data_ptr(), _row_stride(rows)
-    a.stream = _stream_handle(codes.device)
+    a.out, a.out_stride_t = out.data_ptr(), out_stride
+    a.stream = _stream_handle(device)
     a.flags = flags
     if events is not None:
         a.ev_begin, a.ev_end = events
-    _called(lib.llc_embed_quantized, a, codes.device)
+    _called(lib.llc_embed_quantized, a, device)
     return {"out": out}
 
 
@@ -1329,36 +1353,43 @@ def llc_matvec_quantized(x: torch.Tensor, codes: torch.Tensor, scales: torch.Ten
     64 of them read the layer once.  Asynchronous on torch's current stream.
     """
     lib = load()
-    if x.dtype not in _TYPES or x.dim() != 2 or x.shape[1] < 1 or (x.stride(1) != 1 and x.shape[1] > 1):
+    dtype, size, stride = _TYPES.get(x.dtype), x.shape, x.stride()
+    if dtype is None or len(size) != 2 or size[1] < 1 or (stride[1] != 1 and size[1] > 1):
         raise ValueError("x must be [R,D], float32 or bfloat16, last dimension contiguous")
-    R, D = x.shape
+    R, D = size
     a = MatvecQuantizedArgs()
-    N = _layer_into(a, codes, scales, zeros, D, group)
-    if x.device != codes.device:
+    N, at = _layer_into(a, codes, scales, zeros, D, group)
+    if x.get_device() != at:
         raise ValueError("x must be on the codes' device")
-    nbytes = lib.llc_matvec_quantized_workspace_size(R, N, D, group, _TYPES[x.dtype])
+    device = x.device
+    nbytes = _matvec_bytes(R, N, D, group, dtype)
     if out is None:
         specs = {"out": (out_dtype or x.dtype, R, N)}
         if nbytes > 0:
-            workspace = _scratch(workspace, lambda: nbytes, x.device, specs)
-        made = _new(x.device, specs)
+            workspace = _scratch(workspace, lambda: nbytes, device, specs)
+        made = _new(device, specs)
         out, workspace = made["out"], made.get("workspace", workspace)
-    elif nbytes > 0:
-        workspace = _scratch(workspace, lambda: nbytes, x.device)
-    if (out.device != x.device or out.dtype not in _TYPES or out_dtype not in (None, out.dtype) or tuple(out.shape) != (R, N)
-            or (out.stride(1) != 1 and N > 1)):
+        to, out_stride = _TYPES.get(out.dtype), N
+    else:
+        if nbytes > 0:
+            workspace = _scratch(workspace, lambda: nbytes, device)
+        to = _TYPES.get(out.dtype)
+        if out.get_device() != at or out_dtype not in (None, out.dtype) or out.shape != (R, N) or (out.stride(1) != 1 and N > 1):
+            to = None
+        out_stride = _row_stride(out) if to is not None else 0
+    if to is None:
         raise ValueError("out must be [R,N], float32 or bfloat16, last dimension contiguous")
     a.R, a.N, a.D = R, N, D
-    a.dtype, a.out_dtype = _TYPES[x.dtype], _TYPES[out.dtype]
-    a.x, a.x_stride_r = x.data_ptr(), x.stride(0)
-    a.out, a.out_stride_r = out.data_ptr(), _row_stride(out)
+    a.dtype, a.out_dtype = dtype, to
+    a.x, a.x_stride_r = x.data_ptr(), stride[0]
+    a.out, a.out_stride_r = out.data_ptr(), out_stride
     if nbytes > 0:
         a.workspace, a.workspace_bytes = workspace.data_ptr(), workspace.numel()
-    a.stream = _stream_handle(x.device)
+    a.stream = _stream_handle(device)
     a.flags = flags
     if events is not None:
         a.ev_begin, a.ev_end = events
-    _called(lib.llc_matvec_quantized, a, x.device)
+    _called(lib.llc_matvec_quantized, a, device)
     return {"out": out}
 
 
