@@ -194,3 +194,20 @@ def test_the_same_bits_again_on_a_stream_and_from_a_graph():
         graph.replay()
         assert all(torch.equal(a, b) for a, b in zip(caught, all_of_them()))
         w.copy_(first)
+
+
+def test_the_longest_rows():
+    # 33 rows of 2^27 in 32 bits: x as it is laid out has more than 2^31 pieces of 16 bytes.  Ones in few places, scales powers of two: every sum is exact
+    R, N, D, G = 33, 5, 1 << 27, 128
+    g = torch.Generator(device=DEV).manual_seed(2)
+    codes = torch.randint(0, 256, (N, D // 2), generator=g, device=DEV, dtype=torch.uint8)
+    scales = torch.full((N, D // G), 0.25, device=DEV)
+    scales[:, ::3] = 2.0
+    x = torch.zeros(R, D, device=DEV)
+    at = torch.cat([torch.tensor([0, 1, D // 2 + 5, D - 128, D - 1]), torch.randint(0, D, (60,), generator=torch.Generator().manual_seed(3))]).unique().to(DEV)
+    x[:, at] = torch.randint(-2, 3, (R, len(at)), generator=g, device=DEV).float()
+    out = llc.llc_matvec_quantized(x, codes, scales, group=G)["out"]
+    byte = codes[:, at // 2].long()
+    q = torch.where(at % 2 == 0, byte & 15, byte >> 4).double() - 8.0
+    want = x[:, at].double() @ (q * scales[:, at // G].double()).t()
+    assert torch.equal(out.double(), want)
