@@ -892,7 +892,9 @@ template <typename E, bool SAMPLE, bool RANGE> __device__ __forceinline__ void c
       if (!can_range) continue;
       if constexpr (RANGE) {
       // a histogram of counts shows where the cut is, nearly
-      const float per = kFinePerUnit / (float)cut.temp, base = reference + 2048.0f / per;
+      // (from the row's largest on where it is known, else from 12 units of ln over the sample's; what is over that counts as if it were there, which shows the cut all the same where it
+      // has nearly all of the mass)
+      const float per = kFinePerUnit / (float)cut.temp, base = deep ? reference + 12.0f * kFinePerUnit / per : top;
       __syncthreads();
       for (int i = threadIdx.x * 4; i < kFine; i += kThreads * 4) *reinterpret_cast<uint4 *>(s.fine + i) = make_uint4(0, 0, 0, 0);
       __syncthreads();

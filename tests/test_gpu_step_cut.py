@@ -132,6 +132,23 @@ def test_cuts_deep_in_a_row(grid, dtype):
         _both(x, u, **settings)
 
 
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("over", [3.0, 9.0, 14.0, 40.0])
+def test_a_few_entries_far_over_the_others(over, dtype):
+    # the first entries of each part show nothing of them, and the row looks flat
+    g = _gen(41)
+    V = 70003
+    x = 1.5 * torch.randn(4, V, generator=g, device=DEV)
+    x[:, 60001] = x.amax(dim=1) + over
+    x[1, 60002] = x[1, 60001]
+    x[2, 33333] = x[2, 60001] - 0.7
+    x[3, 33333] = x[3, 60001] - 7.0
+    x = x.to(TYPES[dtype])
+    u = torch.rand(4, 5, generator=g, device=DEV)
+    for settings in (dict(top_p=0.3), dict(top_p=0.9), dict(top_p=0.9, temp=0.4), dict(top_p=0.9, temp=3.0), dict(top_p=0.9999), dict(top_k=4000), dict(top_p=0.9, min_p=0.01)):
+        _both(x, u, **settings)
+
+
 def test_log_weights_take_no_temperature():
     x = _zipf(4, 3001, 1.5, torch.float32, _gen(5))
     u = torch.rand(4, 2, generator=_gen(6), device=DEV)
