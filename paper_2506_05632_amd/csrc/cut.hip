@@ -841,6 +841,9 @@ template <typename E, bool SAMPLE, bool RANGE> __device__ __forceinline__ void c
     block_ends(high, 0.0f, top, unused);
   }
   double top_wide = (double)top;
+  // (what was summed relative to the sample's largest is no number where the row's is more than 1024 units of log2 over that, which small temperatures bring about: it
+  // is summed again, relative to the row's)
+  const auto far = [&] { return (top_wide - reference_wide) * cut.scale > 900.0; };
   const auto over_least = [&](float x) { return (double)x - top_wide >= least; };
 
   // 3. the list
@@ -1137,8 +1140,9 @@ template <typename E, bool SAMPLE, bool RANGE> __device__ __forceinline__ void c
     return x > -INFINITY && (key < place.key || (key == place.key && i <= place.index));
   };
   if constexpr (SAMPLE) {
-    // masses of the tiles (an uncut row's are there, by the sample's reference)
-    const double by_wide = uncut ? reference_wide : top_wide;
+    // masses of the tiles (an uncut row's are there, by the sample's reference, unless that is far below)
+    const bool summed = uncut && !far();
+    const double by_wide = summed ? reference_wide : top_wide;
     __syncthreads();
     double *along = s.along + (tiled ? kRange : 0);
     if (equal_kept > 0 && tiled) {
@@ -1156,9 +1160,9 @@ template <typename E, bool SAMPLE, bool RANGE> __device__ __forceinline__ void c
 #pragma unroll 1
       for (int e = e0; e < e1; ++e) s.along[e] += before;
       count = wave_sum(mine);
-    } else if (!uncut) {
+    } else if (!summed) {
       double sum_tile = 0.0;
-      piece = 0;
+      piece = count = 0;
       tile = (long long)wave * p.tiles_wave;
       each_piece(row, p, part, lane, [&](unsigned from, unsigned at, const float (&v)[8]) {
         float kept[8];

@@ -1,0 +1,66 @@
+"""Cut rows whose largest entry is far over what a row's first entries show, masked rows, and the ends of what settings and numbers may be,
+against 64-bit evaluations of the definition (needs an MI355X)."""
+import math
+
+import pytest
+import torch
+
+import paper_2506_05632_amd as llc
+import step_util
+
+pytestmark = pytest.mark.gpu
+DEV = "cuda:0"
+TYPES = {"f32": torch.float32, "bf16": torch.bfloat16}
+
+
+def _gen(seed):
+    return torch.Generator(device=DEV).manual_seed(seed)
+
+
+def _spiked(V, over, apart, dtype, g):
+    """Normal rows with a group of entries `over` the others' largest and `apart` from each other, at an index that no part of a row begins with."""
+    x = torch.randn(3, V, generator=g, device=DEV)
+    at = 70000 if V > 70000 else V - 3000
+    x[:, at] = x.amax(dim=1) + over
+    for i in range(1, 5):
+        x[1, at + 97 * i] = x[1, at] - i * apart
+    x[2, at - 1:at + 40] = x[2, at]
+    return x.to(TYPES[dtype])
+
+
+FAR = [(0.02, 15.0), (0.01, 8.0), (0.01, 6.0), (1e-3, 0.9), (1e-30, 1.0), (1.0, 800.0), (1.0, 730.0), (1.0, 650.0), (0.7, 3e4)]
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("temp,over", FAR)
+@pytest.mark.parametrize("V", [20011, 128256])
+def test_uncut_rows_with_an_entry_far_over_the_others(V, temp, over, dtype):
+    g = _gen(V)
+    x = _spiked(V, over, 0.9 * temp, dtype, g)
+    u = torch.cat([torch.tensor([0.0, 0.3, 1.0 - 2.0 ** -24], device=DEV).expand(3, 3), torch.rand(3, 5, generator=g, device=DEV)], 1)
+    step_util.check_sample(llc.llc_sample(x, u, temp=temp, want_kept=True), x, u, temp=temp)
+    # the same through a row's own settings, which may be none
+    own = dict(temp=torch.full((3,), temp, device=DEV), top_p=torch.ones(3, device=DEV))
+    step_util.check_sample(llc.llc_sample(x, u, want_kept=True, **own), x, u, **own)
+
+
+def test_uncut_rows_of_log_weights_far_apart():
+    x = _spiked(30011, 900.0, 0.9, "f32", _gen(1))
+    u = torch.rand(3, 4, generator=_gen(2), device=DEV)
+    step_util.check_sample(llc.llc_sample(x, u, kind="logw", want_kept=True), x, u)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_rows_of_several_pieces_a_tile(dtype):
+    # over 2^20 entries; the settings take the list, the range, what is narrowed down, and the tiles
+    g = _gen(51)
+    V = (1 << 20) + (1 << 17) + 77
+    x = torch.randn(2, V, generator=g, device=DEV)
+    x[0, V - 5] = 9.0
+    x[1, 1 << 20:] = -math.inf
+    x = x.to(TYPES[dtype])
+    u = torch.rand(2, 3, generator=g, device=DEV)
+    for settings in (dict(), dict(temp=1e-3), dict(top_k=40), dict(top_k=5000), dict(top_p=0.4)):
+        step_util.check_sample(llc.llc_sample(x, u, want_kept=True, **settings), x, u, **settings)
+    for settings in (dict(top_k=5000), dict(min_p=0.2)):
+        step_util.check_truncate(llc.llc_truncate(x, **settings), x, **settings)
