@@ -841,8 +841,8 @@ template <typename E, bool SAMPLE, bool RANGE> __device__ __forceinline__ void c
     block_ends(high, 0.0f, top, unused);
   }
   double top_wide = (double)top;
-  // (what was summed relative to the sample's largest is no number where the row's is more than 1024 units of log2 over that, which small temperatures bring about: it
-  // is summed again, relative to the row's)
+  // (what was summed relative to the sample's largest is no number where the row's is 1024 units of log2 over that (900, which leaves room for a row's sum), as small temperatures
+  // bring about: it is summed again, relative to the row's, and a share of it is not looked for in the list, which the longer way does without)
   const auto far = [&] { return (top_wide - reference_wide) * cut.scale > 900.0; };
   const auto over_least = [&](float x) { return (double)x - top_wide >= least; };
 
@@ -850,7 +850,7 @@ template <typename E, bool SAMPLE, bool RANGE> __device__ __forceinline__ void c
   int n = 0;
   double all_mass = 0.0;
   if (need_mass && !deep) all_mass = block_sum(mass, s.wave_double) * exp2_of((reference_wide - top_wide) * cut.scale);
-  bool listed = try_list && !deep && join_list(s, list.count, lane, wave, n);
+  bool listed = try_list && !deep && !(need_mass && far()) && join_list(s, list.count, lane, wave, n);
   if (listed && cut.top_k > n && bound > -INFINITY && !by_least) listed = false;  // (there are more below the bound)
   Place place = {0xFFFFFFFFu, (uint32_t)p.V};  // (of the list's entries: their places in the list)
   // What the list does not show is looked for in a range about the cut, and what that does not show narrowed down in the row.

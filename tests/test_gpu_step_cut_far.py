@@ -64,3 +64,57 @@ def test_rows_of_several_pieces_a_tile(dtype):
         step_util.check_sample(llc.llc_sample(x, u, want_kept=True, **settings), x, u, **settings)
     for settings in (dict(top_k=5000), dict(min_p=0.2)):
         step_util.check_truncate(llc.llc_truncate(x, **settings), x, **settings)
+
+
+SHARES = [dict(top_p=0.9), dict(top_p=0.3), dict(top_p=0.9, min_p=0.01), dict(top_p=0.5, min_p=1e-4)]
+
+
+def _both(x, u, **settings):
+    step_util.check_sample(llc.llc_sample(x, u, want_kept=True, **settings), x, u, **settings)
+    step_util.check_truncate(llc.llc_truncate(x, **settings), x, **settings)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("temp,over", FAR)
+@pytest.mark.parametrize("V", [20011, 128256])
+def test_shares_of_rows_with_an_entry_far_over_the_others(V, temp, over, dtype):
+    g = _gen(V + 1)
+    x = _spiked(V, over, 0.9 * temp, dtype, g)
+    u = torch.rand(3, 5, generator=g, device=DEV)
+    for settings in SHARES + [dict(top_p=0.9, top_k=V), dict(top_p=0.9, top_k=3)]:
+        _both(x, u, temp=temp, **settings)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("temp", [1.0, 0.01, 1e-3])
+@pytest.mark.parametrize("allowed", [3, 100, 1000])
+def test_shares_of_rows_that_allow_a_few_entries(allowed, temp, dtype):
+    # -inf but for some, as where what may follow is given: fewer than a list of a share is made for, in the sample and in all
+    g = _gen(allowed)
+    V = 128256
+    x = torch.full((4, V), -math.inf, device=DEV)
+    for r in range(4):
+        at = torch.randperm(V, generator=g, device=DEV)[:allowed]
+        x[r, at] = torch.randn(allowed, generator=g, device=DEV)
+        x[r, at[0]] = x[r].max() + 3.0 * r
+    x[3, 12345:12350] = x[3].max() - 0.4 * temp
+    x = x.to(TYPES[dtype])
+    u = torch.rand(4, 5, generator=g, device=DEV)
+    for settings in [dict()] + SHARES:
+        _both(x, u, temp=temp, **settings)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_shares_of_rows_masked_by_the_least_number(dtype):
+    # the same with the type's lowest value in the masked places, which has mass where nothing is over it
+    g = _gen(61)
+    V = 50021
+    low = torch.finfo(TYPES[dtype]).min
+    x = torch.full((4, V), low, device=DEV)
+    x[0, 30001:30011] = torch.randn(10, generator=g, device=DEV)
+    x[1, V - 1] = 1.0
+    x[2, 45000::7] = 0.5 * torch.randn(x[2, 45000::7].shape, generator=g, device=DEV)
+    x = x.to(TYPES[dtype])
+    u = torch.rand(4, 5, generator=g, device=DEV)
+    for settings in [dict(), dict(top_k=7)] + SHARES:
+        _both(x, u, **settings)
