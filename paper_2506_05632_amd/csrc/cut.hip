@@ -67,7 +67,7 @@ struct Cut {
   double scale;   // log2(e) / temp
   double temp;
   long long top_k;  // 0: off
-  float top_p;      // 1: off
+  float top_p;      // in (0, 1]; 1: off
   float min_p;      // 0: off
   bool bad;
 };
@@ -81,7 +81,8 @@ __device__ __forceinline__ Cut cut_of(const CutParams &p, long long r) {
   c.temp = (double)temp;
   c.scale = 1.4426950408889634 / c.temp;
   c.top_k = top_k > 0 && top_k < p.V ? top_k : 0;
-  c.top_p = fminf(fmaxf(top_p, 0.0f), 1.0f);
+  c.top_p = fminf(top_p, 1.0f);
+  if (top_p <= 0.0f) { c.top_k = 1; c.top_p = 1.0f; }  // (no share at all leaves the first entry)
   c.min_p = fminf(fmaxf(min_p, 0.0f), 1.0f);
   return c;
 }

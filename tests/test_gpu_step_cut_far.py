@@ -118,3 +118,27 @@ def test_shares_of_rows_masked_by_the_least_number(dtype):
     u = torch.rand(4, 5, generator=g, device=DEV)
     for settings in [dict(), dict(top_k=7)] + SHARES:
         _both(x, u, **settings)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("V", [600, 5000, 128256])
+def test_no_share_at_all_leaves_the_first_entry(V, dtype):
+    # a row's own top_p of 0 or less, where a list would hold the row's entries and where it would not
+    g = _gen(71)
+    x = torch.zeros(5, V, device=DEV)
+    x[1] = torch.linspace(-3.0, 3.0, V, device=DEV)
+    x[2] = torch.randint(0, 3, (V,), generator=g, device=DEV).float()
+    x[3] = torch.randn(V, generator=g, device=DEV)
+    x[4, ::2] = -math.inf
+    x = x.to(TYPES[dtype])
+    u = torch.tensor([[0.0, 0.5, 1.0 - 2.0 ** -24, 1.0]], device=DEV).repeat(5, 1)
+    for p in (0.0, -1.0, -math.inf):
+        top_p = torch.full((5,), p, device=DEV)
+        top_p[3] = 0.5
+        for settings in (dict(), dict(top_k=900), dict(min_p=0.2), dict(top_k=torch.tensor([0, 0, 7, 0, 3000], dtype=torch.int32, device=DEV))):
+            _both(x, u, top_p=top_p, **settings)
+    first = x.float().argmax(dim=1)
+    out = llc.llc_sample(x, u, top_p=torch.zeros(5, device=DEV), want_kept=True)
+    assert out["kept"].tolist() == [1] * 5 and torch.equal(out["tokens"].long(), first[:, None].expand(5, 4))
+    # the least positive share, as a number
+    _both(x, u, top_p=1e-45)
