@@ -1092,16 +1092,14 @@ template <typename E, bool SAMPLE, bool RANGE> __device__ __forceinline__ void c
       const double log_total = log(total);
       for (int i = threadIdx.x; i < p.S; i += kThreads) {
         const float u = i < kThreads ? first_u : p.u[r * p.u_stride + i];
-        const double target = (double)fmaxf(u, 0.0f) * total;
+        const double target = u >= 1.0f ? (double)INFINITY : (double)fmaxf(u, 0.0f) * total;
         int a = 0, z = n;  // the first whose sum is over the target
         while (a < z) {
           const int mid = (a + z) / 2;
           if (s.along[mid] > target) z = mid; else a = mid + 1;
         }
-        if (a >= n) {  // the last kept
-          a = n - 1;
-          while (a > 0 && !kept_at(a)) --a;
-        }
+        a = a < n ? a : n - 1;  // (none: the last kept)
+        while (a > 0 && !kept_at(a)) --a;  // (sums are not equal where nothing lies between: those of two threads are rounded in different orders)
         p.tokens[r * p.S + i] = u == u ? s.list_index[a] : -1;
         if (p.logp != nullptr) p.logp[r * p.S + i] = u == u ? (float)(((double)value_of(s.list_key[a]) - top_wide) / cut.temp - log_total) : -INFINITY;
       }
@@ -1209,46 +1207,47 @@ template <typename E, bool SAMPLE, bool RANGE> __device__ __forceinline__ void c
     total = along[p.tiles - 1];
     for (int i = wave; i < p.S; i += kWaves) {  // a wavefront a token
       const float u = p.u[r * p.u_stride + i];
-      const double target = (double)fmaxf(u, 0.0f) * total;
+      double target = u >= 1.0f ? (double)INFINITY : (double)fmaxf(u, 0.0f) * total;
       int a = 0, z = p.tiles;  // the first tile whose sum is over the target
       while (a < z) {
         const int mid = (a + z) / 2;
         if (along[mid] > target) z = mid; else a = mid + 1;
       }
-      if (a >= p.tiles) {  // the last with mass
-        a = p.tiles - 1;
-        while (a > 0 && along[a] == along[a - 1]) --a;
-      }
-      double before = a > 0 ? along[a - 1] : 0.0;
-      long long found = -1, last_kept = -1;
-      const long long begin = (long long)a * p.pieces_tile * kPiece, end0 = begin + (long long)p.pieces_tile * kPiece, end = end0 < p.V ? end0 : p.V;
-      for (long long at0 = begin; at0 < end && found < 0; at0 += kPiece) {
-        const long long at = begin_of(at0, lane, p.V);
-        float v[8];
-        widen_raw(load_raw(row, at0, lane, p.V), at0, lane, p.V, v);
-        double w[8], mine = 0.0;
-        long long last = -1;
+      a = a < p.tiles ? a : p.tiles - 1;
+      long long found = -1;
+      // (a tile without kept entries, which rounding alone may lead to and a number of 1 does: the last kept entry before it)
+      for (; found < 0 && a >= 0; --a, target = INFINITY) {
+        double before = a > 0 ? along[a - 1] : 0.0;
+        long long last_kept = -1;
+        const long long begin = (long long)a * p.pieces_tile * kPiece, end0 = begin + (long long)p.pieces_tile * kPiece, end = end0 < p.V ? end0 : p.V;
+        for (long long at0 = begin; at0 < end && found < 0; at0 += kPiece) {
+          const long long at = begin_of(at0, lane, p.V);
+          float v[8];
+          widen_raw(load_raw(row, at0, lane, p.V), at0, lane, p.V, v);
+          double w[8], mine = 0.0;
+          long long last = -1;
 #pragma unroll
-        for (int j = 0; j < 8; ++j) {
-          const bool in = inside(v[j], at + j);
-          w[j] = mass_of(in ? v[j] : -INFINITY, by_wide, cut.scale);
-          mine += w[j];
-          if (in) last = at + j;
-        }
-        const double upto = wave_scan(mine);
-        double here = before + (upto - mine);
-        long long hit = -1;
+          for (int j = 0; j < 8; ++j) {
+            const bool in = inside(v[j], at + j);
+            w[j] = mass_of(in ? v[j] : -INFINITY, by_wide, cut.scale);
+            mine += w[j];
+            if (in) last = at + j;
+          }
+          const double upto = wave_scan(mine);
+          double here = before + (upto - mine);
+          long long hit = -1;
 #pragma unroll
-        for (int j = 0; j < 8; ++j) {
-          here += w[j];
-          if (hit < 0 && w[j] > 0.0 && here > target) hit = at + j;
+          for (int j = 0; j < 8; ++j) {
+            here += w[j];
+            if (hit < 0 && w[j] > 0.0 && here > target) hit = at + j;
+          }
+          const unsigned long long any = __ballot(hit >= 0), some = __ballot(last >= 0);
+          if (any != 0) found = lane_value(hit, __builtin_ctzll(any));
+          if (some != 0) last_kept = lane_value(last, 63 - __builtin_clzll(some));
+          before += lane_value(upto, 63);
         }
-        const unsigned long long any = __ballot(hit >= 0), some = __ballot(last >= 0);
-        if (any != 0) found = lane_value(hit, __builtin_ctzll(any));
-        if (some != 0) last_kept = lane_value(last, 63 - __builtin_clzll(some));
-        before += lane_value(upto, 63);
+        if (found < 0) found = last_kept;  // (rounding alone keeps the sum below the target)
       }
-      if (found < 0) found = last_kept;  // (rounding alone keeps the sum below the target)
       if (lane == 0) {
         const bool number = u == u && found >= 0;
         p.tokens[r * p.S + i] = number ? (int)found : -1;

@@ -142,3 +142,29 @@ def test_no_share_at_all_leaves_the_first_entry(V, dtype):
     assert out["kept"].tolist() == [1] * 5 and torch.equal(out["tokens"].long(), first[:, None].expand(5, 4))
     # the least positive share, as a number
     _both(x, u, top_p=1e-45)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("settings", [dict(), dict(top_k=5000), dict(top_k=20000, min_p=1e-4), dict(top_p=0.97, temp=1.5), dict(top_k=60), dict(top_k=100000, top_p=0.999999)])
+def test_one_and_more_take_the_last_kept_entry(settings, dtype):
+    # rows whose ends are masked or have next to no mass: sums along them differ by roundings alone
+    g = _gen(81)
+    R, V = 20, 128256
+    x = 1.5 * torch.randn(R, V, generator=g, device=DEV)
+    for r in range(R):
+        x[r, V - 700 * r - 300:] = -math.inf if r % 2 else -45.0
+        x[r, 40000 + 900 * r:52000 + 800 * r] = -math.inf
+    x = x.to(TYPES[dtype])
+    inf = math.inf
+    u = torch.tensor([[1.0, 1.0 + 2.0 ** -23, 2.0, inf, 1.0 - 2.0 ** -24, 0.0, -0.0, -1.0, -inf, math.nan]], device=DEV).repeat(R, 1)
+    out = llc.llc_sample(x, u, want_kept=True, **settings)
+    step_util.check_sample(out, x, u, **settings)
+    cut = llc.llc_truncate(x, **settings)["logits"]
+    kept = torch.isfinite(cut)
+    index = torch.arange(V, device=DEV)
+    last, first = torch.where(kept, index, -1).amax(dim=1), torch.where(kept, index, V).amin(dim=1)
+    tokens = out["tokens"].long()
+    for s in range(4):
+        assert torch.equal(tokens[:, s], last), s
+    assert kept.gather(1, tokens[:, :9]).all()
+    assert all(torch.equal(tokens[:, s], first) for s in (5, 6, 7, 8))
