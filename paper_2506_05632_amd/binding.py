@@ -1139,14 +1139,14 @@ def _cut_into(a, name, logits, kind, temp, top_k, top_p, min_p):
     dev = logits.device
     a.R, a.V, a.dtype, a.kind = R, V, _TYPES[logits.dtype], _KINDS[kind]
     a.x, a.stride_r = logits.data_ptr(), logits.stride(0)
-    if type(temp) is float and type(top_k) is int and type(top_p) is float and type(min_p) is float and top_k < 1 << 31:
+    if type(temp) is float and type(top_k) is int and type(top_p) is float and type(min_p) is float and 0 <= top_k < 1 << 31:
         a.temp, a.top_k, a.top_p, a.min_p = temp, top_k, top_p, min_p
         return R, V, dev
     for field, value, dtype in (("temp", temp, torch.float32), ("top_k", top_k, torch.int32), ("top_p", top_p, torch.float32),
                                 ("min_p", min_p, torch.float32)):
         if not isinstance(value, torch.Tensor):
-            if field == "top_k" and (int(value) != value or value >= 1 << 31):
-                raise ValueError("top_k must be a whole number below 2^31")
+            if field == "top_k" and (int(value) != value or not -1 << 31 <= value < 1 << 31):
+                raise ValueError("top_k must be a whole number from 0 to below 2^31")
             setattr(a, field, int(value) if field == "top_k" else float(value))
             continue
         if value.device != dev or value.dtype != dtype or tuple(value.shape) != (R,) or not value.is_contiguous():
