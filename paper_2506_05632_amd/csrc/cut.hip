@@ -158,7 +158,6 @@ struct Shared {
     unsigned long long histogram[kBuckets];
     double along[kList > kMostTiles ? kList : kMostTiles];  // masses summed along the indexes: of the list's entries, or of tiles
     double masses[kFew];                                    // summed along the order
-    unsigned long long weights[kFew];
   };
   unsigned long long few[kFew], sorted[kFew];  // key and index (kFew is a multiple of eight)
   uint32_t sample[kThreads];                   // a histogram of the sample's largest
