@@ -168,3 +168,36 @@ def test_one_and_more_take_the_last_kept_entry(settings, dtype):
         assert torch.equal(tokens[:, s], last), s
     assert kept.gather(1, tokens[:, :9]).all()
     assert all(torch.equal(tokens[:, s], first) for s in (5, 6, 7, 8))
+
+
+def test_the_longest_row():
+    # V = 2^31 - 5: places of all kinds at their widest.  Numbers in 16 bits, so that thousands of equals lie about the cut
+    V = (1 << 31) - 5
+    x = torch.empty(1, V, dtype=torch.bfloat16, device=DEV).normal_(generator=_gen(91))
+    x[0, V - 1] = x[0, 1 << 30] = 9.0
+    u = torch.tensor([[0.0, 0.3, 0.7, 1.0 - 2.0 ** -24, 1.0]], device=DEV)
+    for k in (3, 5000):
+        cut = llc.llc_truncate(x, top_k=k)
+        kept = torch.isfinite(cut["logits"][0])
+        assert cut["kept"].item() == k == int(kept.sum())
+        at = kept.nonzero().view(-1)
+        last = x[0, at].min()
+        more = x[0] > last
+        assert bool(kept[more].all()) and bool((x[0, at] >= last).all())
+        n = k - int(more.sum())
+        equal = (x[0] == last).nonzero().view(-1)
+        assert len(equal) >= n > 0 and bool(kept[equal[:n]].all()) and not bool(kept[equal[n:]].any())
+        out = llc.llc_sample(x, u, top_k=k, want_kept=True)
+        upto = (x[0, at].double() - 9.0).exp().cumsum(0)
+        want = at[torch.searchsorted(upto, u[0].double() * upto[-1], right=True).clamp(max=k - 1)]
+        assert torch.equal(out["tokens"][0].long(), want) and out["kept"].item() == k
+        logp = x[0, want].double() - 9.0 - upto[-1].log()
+        assert bool(((out["logp"][0].double() - logp).abs() <= 1.01 * 2.0 ** -24 * logp.abs() + 1e-12).all())
+        del cut, kept, more, equal
+    # equal masses: every sum is a whole number
+    x.zero_()
+    out = llc.llc_sample(x, u[:, [0, 3, 4]], want_kept=True)
+    assert out["tokens"][0].tolist() == [0, V - 128, V - 1] and out["kept"].item() == V
+    assert bool((out["logp"].double() + math.log(V)).abs().max() <= 1.01 * 2.0 ** -24 * math.log(V) + 1e-12)
+    half = torch.full((1,), 0.5, device=DEV)
+    assert llc.llc_sample(x, half)["tokens"].item() == V // 2
