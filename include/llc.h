@@ -532,7 +532,7 @@ typedef struct llc_clip_grad_norm_args {
 
 /* Arguments of llc_sample: tokens[r,s] = the first index i with sum over the kept j <= i of p_j > u[r,s] times the kept
  * mass; u below 0 counts as 0, of 1 or more takes the last kept index, and a NaN gives token -1.  logp[r,s] = ln of the token's probability among
- * the kept ones (-inf with token -1), kept[r] = how many they are.  A row without mass: -1, -inf, 0. */
+ * the kept ones (-inf with token -1 and where it is below the least number of 32 bits), kept[r] = how many they are.  A row without mass: -1, -inf, 0. */
 typedef struct llc_sample_args {
   int64_t R, V, S;          /* R in 0..2^24 - 1, V in 1..2^31 - 5, S in 0..65535         */
   int32_t dtype;            /* LLC_F32 | LLC_BF16                                        */

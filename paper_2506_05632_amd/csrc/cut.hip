@@ -751,6 +751,7 @@ template <typename E, bool SAMPLE, bool RANGE> __device__ __forceinline__ void c
     top = s.wave_high[0]; end = s.wave_low[0];
 #pragma unroll
     for (int w = 1; w < kWaves; ++w) { top = fmaxf(top, s.wave_high[w]); end = fminf(end, s.wave_low[w]); }
+    top = lane_value(top, 0);  // (a scalar: it is needed to the end, and vector registers are short)
   };
   float reference, sample_low;
   block_ends(largest, largest > -INFINITY ? largest : INFINITY, reference, sample_low);
@@ -843,14 +844,14 @@ template <typename E, bool SAMPLE, bool RANGE> __device__ __forceinline__ void c
   double top_wide = (double)top;
   // (what was summed relative to the sample's largest is no number where the row's is 1024 units of log2 over that (900, which leaves room for a row's sum), as small temperatures
   // bring about: it is summed again, relative to the row's, and a share of it is not looked for in the list, which the longer way does without)
-  const auto far = [&] { return (top_wide - reference_wide) * cut.scale > 900.0; };
+  const bool far = (top_wide - reference_wide) * cut.scale > 900.0, summed = uncut && !far;  // (summed: an uncut row's tiles are, relative to the sample's)
   const auto over_least = [&](float x) { return (double)x - top_wide >= least; };
 
   // 3. the list
   int n = 0;
   double all_mass = 0.0;
   if (need_mass && !deep) all_mass = block_sum(mass, s.wave_double) * exp2_of((reference_wide - top_wide) * cut.scale);
-  bool listed = try_list && !deep && !(need_mass && far()) && join_list(s, list.count, lane, wave, n);
+  bool listed = try_list && !deep && !(need_mass && far) && join_list(s, list.count, lane, wave, n);
   if (listed && cut.top_k > n && bound > -INFINITY && !by_least) listed = false;  // (there are more below the bound)
   Place place = {0xFFFFFFFFu, (uint32_t)p.V};  // (of the list's entries: their places in the list)
   // What the list does not show is looked for in a range about the cut, and what that does not show narrowed down in the row.
@@ -1138,8 +1139,7 @@ template <typename E, bool SAMPLE, bool RANGE> __device__ __forceinline__ void c
     return x > -INFINITY && (key < place.key || (key == place.key && i <= place.index));
   };
   if constexpr (SAMPLE) {
-    // masses of the tiles (an uncut row's are there, by the sample's reference, unless that is far below)
-    const bool summed = uncut && !far();
+    // masses of the tiles
     const double by_wide = summed ? reference_wide : top_wide;
     __syncthreads();
     double *along = s.along + (tiled ? kRange : 0);

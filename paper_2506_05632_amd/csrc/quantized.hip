@@ -1,6 +1,6 @@
 // Layers held in 4 bits: making one, looking rows of it up, and the host side of the products with it.  The first two move data and compute next to
 // nothing beside it: memory bounds them.  A lane takes eight neighbouring columns (a word of codes), a wavefront 512, four times over (128 256 x 2048 in
-// fp32, groups of 64 with zeros: 220 us, 5.4 TB/s; all its rows back in bf16: 127 us, 5.2 TB/s).
+// fp32, groups of 64 with zeros: 230 us, 5.2 TB/s; all its rows back in bf16 after it: 131 us, 5.1 TB/s; again, the codes still in the caches: 95).
 #include "quantized.hpp"
 
 namespace llc {
