@@ -10,8 +10,8 @@
 //   3. The list is sorted, its masses are summed along the order, and the cut is read off; the tokens follow from sums along the indexes.
 // Rows whose kept entries are too many for the list, by what the sample shows or the list turns out to hold, are read twice more: a histogram of
 // counts by value, 256 buckets a unit of ln, shows nearly where the cut is, and a pass with exact masses takes the sums before the buckets about it and lists what is in
-// them, or counts them by tiles where thousands are equal.  That confirms the cut or not.  (256 rows of 128 256 in bf16 with settings of their own, a tenth of them so deep: 121 us, 205 by
-// histograms of masses alone; top_k of 3000: 90 and 106.)  What is left is narrowed down by histograms of masses (or counts) of the row, and by the keys' bits.  Tokens follow from the
+// them, or counts them by tiles where thousands are equal.  That confirms the cut or not.  (256 rows of 128 256 in bf16 with settings of their own, a tenth of them so deep: 128 us, some 205 by
+// histograms of masses alone; top_k of 3000 of normal rows: 86, some 106.)  What is left is narrowed down by histograms of masses (or counts) of the row, and by the keys' bits.  Tokens follow from the
 // sums of tiles of the row.
 //
 // Masses are exp((x - reference) / temp) in fp64: a border in a run of 128 000 entries that share the mass is hit by rounding otherwise.  (An fp64 multiply-add takes
@@ -30,13 +30,14 @@ constexpr int kBuckets = 2048;    // of a histogram
 constexpr int kBucketsLog = 11;
 constexpr int kMostTiles = 2048;  // of a row, whose masses LDS holds
 constexpr int kPiece = 512;       // entries that a wavefront takes at a time, eight a lane
-constexpr int kAhead = 2;         // pieces that it has asked for (four: the same, 300 rows of 50 257 in fp32 25.3 us for 24.1)
-constexpr int kSample = 2;        // pieces of a wavefront that the sample has (one: top_k 1500 of 256 rows of 128 256 in bf16 163 us for 46, top_k 40 of 1024 rows 82 for 70)
+constexpr int kAhead = 2;         // pieces that it has asked for (four: 300 rows of 50 257 in fp32 cut 31.3 us for 28.8)
+constexpr int kSample = 2;        // pieces of a wavefront that the sample has (one: top_k 1500 of 256 rows of 128 256 in bf16 186 us for 43, top_k 40 of 1024 rows 88 for 78)
 constexpr int kFine = 8192;       // buckets of the histogram of counts
 constexpr float kFinePerUnit = 256.0f;  // of them for each unit of ln
 constexpr int kRange = 2048;      // entries about the cut that are listed
-// Entries that the list aims at where a share of the mass is asked for (eight tokens of 1024 rows of 128 256 in fp32, top_p 0.9: 184 us; 128: 332, as rows miss it, 400: 192), and
-// top_k up to which the list is tried (top_k 1500 of 256 rows: 46 us, by the range 88).
+// Entries that the list aims at where a share of the mass is asked for (eight tokens of 1024 rows of 128 256 in fp32, top_p 0.9: 162 us; 128: 186, as rows miss it, 400: 173; 256 rows
+// in bf16 with settings of their own, three sets of them: 129, 133 and 101), and top_k up to which the list is tried (top_k 1500 of 256 rows: 43 us; by the range 88 of normal rows, and 310 of rows
+// that fall as a power of the rank, whose cut lies deeper than the range goes).
 constexpr int kByMass = 256, kByCount = 1800;
 constexpr long long kMostRowBlocks = 1LL << 22;  // rows of a launch
 
@@ -780,7 +781,7 @@ template <typename E, bool SAMPLE, bool RANGE> __device__ __forceinline__ void c
       const float expected = share * (float)(counted ? (int)cut.top_k : kByMass);
       const int wanted = share == 1.0f ? (int)expected : (int)(expected + (counted ? 4.5f * sqrtf(expected) + 6.0f : 1.0f));
       bound = bound_of(s, largest, reference, sample_low, wanted);
-      if (RANGE && need_mass && share < 1.0f) {  // a list that has less than half of the mass asked for in the sample is not made: of seven tenths, rows would be read once more for nothing more often (1024 of 128 256 in fp32, steep: 187 us for 173)
+      if (RANGE && need_mass && share < 1.0f) {  // a list that has less than half of the mass asked for in the sample is not made: of seven tenths, rows would be read once more for nothing more often (eight tokens of 1024 of 128 256 in fp32: 175 us for 162)
         float above = 0.0f, sum = 0.0f;
 #pragma unroll
         for (int i = 0; i < kSample; ++i) {
@@ -1289,7 +1290,7 @@ template <typename E, bool SAMPLE, bool RANGE> __global__ void __launch_bounds__
 template <bool SAMPLE> hipError_t launch_cut(CutParams p, int dtype, hipStream_t st) {
   hipError_t e = hipSuccess;
   // Whether rows may look for their cut in a range;
-  // the kernel that can needs more registers than there are, which costs rows that never do a tenth of their time (1024 of 128 256 in bf16, top_k 1: 72 us for 63).
+  // the kernel that can needs more registers than there are, which costs rows that never do a tenth of their time (1024 of 128 256 in bf16, top_k 1: 72 us for 63 when both were tried).
   const bool by_mass = p.row_top_p != nullptr || p.top_p < 1.0f;
   const bool range = (by_mass && (p.row_top_k != nullptr || p.top_k == 0)) || p.row_top_k != nullptr || p.top_k > kByCount;
   for (; p.row0 < p.R && e == hipSuccess; p.row0 += kMostRowBlocks) {
